@@ -305,6 +305,33 @@ eg_status eg_average_model(eg_ctx* ctx, const float* params, float* avg_dev,
 eg_status eg_export_state(eg_ctx* ctx, void* host_buf, size_t* bytes);
 eg_status eg_import_state(eg_ctx* ctx, const void* host_buf, size_t bytes);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators around the step.  The paper takes the gradients G_k of Eq. (dist_sgd) as given; the
+ * calls below compute them for replicas that train a residual network of gated feed-forward
+ * blocks, with the weights of all P replicas (views into one [P][replica_stride] buffer) in one
+ * call, and bound them before the step.
+ * Values are fp32, bf16 or fp16, one type per call; sums, norms and statistics are kept in 32
+ * bits or more. */
+enum { EG_F32 = 0, EG_BF16 = 1, EG_F16 = 2 };
+
+/* Clipping.  For every replica i, over all its tensors (padding between tensors is ignored):
+ *     norm_i = sqrt(sum g^2),   c_i = min(1, max_norm / norm_i),   out_i = c_i * g_i.
+ * grads ([P][replica_stride] of type dtype, only read) and out (same layout, fp32: what eg_step
+ * takes) are 16-byte aligned device buffers; out == grads is allowed for EG_F32 (in place),
+ * otherwise the two must not overlap.  Padding of out is not written.  norms_dev (device, P
+ * floats) receives the norms before clipping.  The sums are fp64 in a fixed order: the same
+ * bits on every call on the same device.
+ * A norm of 0 leaves the gradients as they are.  A norm that is not finite follows the formula
+ * (infinite: zeros, with NaN where the gradient is infinite; NaN: all NaN) unless flags has
+ * EG_CLIP_ZERO_NONFINITE: the replica's gradients then become zeros, so that it takes no part in
+ * the update of this step but averages with its neighbours.  max_norm >= 0; +infinity only
+ * computes the norms (and widens).  Only enqueues work on `stream`; the first call of a context
+ * allocates its scratch (make it outside a stream capture).  Errors: EG_ERR_INVALID,
+ * EG_ERR_STATE (the previous call's stream is still busy), EG_ERR_OOM, EG_ERR_CUDA. */
+enum { EG_CLIP_ZERO_NONFINITE = 1 };
+eg_status eg_clip_gradients(eg_ctx* ctx, const void* grads, int dtype, double max_norm, int flags,
+                            float* out, float* norms_dev, void* stream);
+
 /* Change norms without any allocation.  (The paper has no counterpart: this is a service
  * entry point of the library, not a step of the method.)
  *

@@ -33,12 +33,16 @@ EXPORTS = [
     "eg_topk_repeat_count",
     "eg_set_quantisation",
     "eg_last_quantised",
+    "eg_clip_gradients",
 ]
 STATIC_MAX_TENSORS = 192
 STATIC_MAX_PARTIALS = 524288
 FUSED_PIPELINED = 0
 FUSED_REGISTER = 1
 FUSED_AUTO = 2
+F32, BF16, F16 = 0, 1, 2
+DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+CLIP_ZERO_NONFINITE = 1
 KERNEL_GROUPS = ("norm", "decide", "topk", "fused")
 
 
@@ -114,6 +118,7 @@ def load_library() -> C.CDLL:
     lib.eg_topk_repeat_count.argtypes = [vp, u64p]
     lib.eg_set_quantisation.argtypes = [vp, C.c_int]
     lib.eg_last_quantised.argtypes = [vp, vp, vp]
+    lib.eg_clip_gradients.argtypes = [vp, vp, C.c_int, C.c_double, C.c_int, vp, vp, vp]
     lib.eg_last_cuda_error.argtypes = [vp]
     lib.eg_last_launch_count.argtypes = [vp]
     _lib = lib
@@ -363,6 +368,39 @@ class EventGrad:
         assert tuple(v.shape) == (self.P, self.replica_stride)
         _check(self._lib, self._lib.eg_write_velocity(self._h, v.data_ptr()), self._h,
                "eg_write_velocity")
+
+    # ------------------------------------------------------------------ around the step
+    def view(self, buffer: torch.Tensor, t: int, shape: Sequence[int]) -> torch.Tensor:
+        """Tensor ``t`` of every replica as a ``[P, *shape]`` view of a buffer in the library's layout."""
+        o, n = self.tensor_offset[t], self.numel[t]
+        return buffer[:, o:o + n].view(self.P, *shape)
+
+    def clip_gradients(self, grads: torch.Tensor, max_norm: float, out: Optional[torch.Tensor] = None,
+                       zero_nonfinite: bool = False, norms: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """``eg_clip_gradients``: scales the gradients of every replica to a norm (over all its
+        tensors) of at most ``max_norm``.  ``grads``: ``[P, replica_stride]`` fp32, bf16 or fp16; the
+        result goes to ``out`` (fp32, same shape; default: ``grads`` itself, which must then be fp32).
+        Returns the norms before clipping, ``[P]`` fp32 on the device."""
+        dtype = DTYPES.get(grads.dtype)
+        if out is None:
+            out = grads
+        assert dtype is not None and out.dtype == torch.float32
+        assert grads.is_cuda and out.is_cuda and grads.is_contiguous() and out.is_contiguous()
+        assert grads.shape == out.shape == (self.P, self.replica_stride)
+        s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if norms is None:
+            if stream is None:
+                norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
+            else:
+                with torch.cuda.stream(s):
+                    norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
+        assert norms.is_cuda and norms.dtype == torch.float32 and norms.is_contiguous() and norms.numel() == self.P
+        st = self._lib.eg_clip_gradients(self._h, grads.data_ptr(), dtype, float(max_norm),
+                                         CLIP_ZERO_NONFINITE if zero_nonfinite else 0, out.data_ptr(),
+                                         norms.data_ptr(), s.cuda_stream)
+        _check(self._lib, st, self._h, "eg_clip_gradients")
+        return norms
 
     def set_fused_kernel(self, kind: int):
         _check(self._lib, self._lib.eg_set_fused_kernel(self._h, int(kind)), self._h,

@@ -11,6 +11,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "eg_clip.cuh"
 #include "eg_common.cuh"
 #include "eg_fused.cuh"
 #include "eg_fused_hops.cuh"
@@ -112,6 +113,10 @@ struct eg_ctx {
     bool nvtx = false;      // EG_NVTX in the environment at eg_create: named ranges around the kernel groups
     int fused_waves = 1;    // EG_FUSED_WAVES in the environment at eg_create: CTAs of a walking pipelined kernel per resident slot
     int* ticket = nullptr;       // device: tile counter of the walking fused kernel
+    // clipping (eg_clip_gradients): partial sums of squares, allocated by the first call
+    double* clip_partials = nullptr;
+    int clip_grid = 0;
+    bool clipped = false;                // a call has run on last_stream
     // quantised messages (eg_set_quantisation)
     int quant_bits = 0;                  // 0: messages in full precision
     float* quant_tile_max = nullptr;     // [P][norm tiles]
@@ -278,6 +283,23 @@ eg_status sync_and_check(eg_ctx* c) {
     unsigned int e = 0;
     EG_CUDA(c, cudaMemcpy(&e, c->err, sizeof(e), cudaMemcpyDeviceToHost));
     return eg_status_of_error_word(e);
+}
+
+// One stream at a time: moving to another stream is allowed only once the stream of the
+// previous call has run dry.  Nothing can be asked while a graph is being recorded (on the
+// new stream or on the previous one): the caller ends the recording before moving on.
+bool claim_stream(eg_ctx* c, cudaStream_t stream) {
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &cs) != cudaSuccess) { (void)cudaGetLastError(); cs = cudaStreamCaptureStatusNone; }
+    const bool capturing = cs != cudaStreamCaptureStatusNone;
+    if ((c->stepped || c->clipped) && stream != c->last_stream && !c->last_capturing && !capturing) {
+        const cudaError_t q = cudaStreamQuery(c->last_stream);
+        if (q == cudaErrorNotReady) return false;
+        if (q != cudaSuccess) (void)cudaGetLastError();
+    }
+    c->last_capturing = capturing;
+    c->last_stream = stream;
+    return true;
 }
 
 constexpr size_t kMaxTimedPairs = 1 << 15;
@@ -675,22 +697,7 @@ eg_status eg_step_masked(eg_ctx* c, float* params, const float* grads, float lr,
     DeviceGuard guard(c->device);
     if (!guard.ok) return EG_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    // One stream at a time: moving to another stream is allowed only once the stream of the
-    // previous call has run dry.  Nothing can be asked while a graph is being recorded (on the
-    // new stream or on the previous one): the caller ends the recording before moving on.
-    bool capturing = false;
-    {
-        cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(stream, &cs) != cudaSuccess) { (void)cudaGetLastError(); cs = cudaStreamCaptureStatusNone; }
-        capturing = cs != cudaStreamCaptureStatusNone;
-    }
-    if (c->stepped && stream != c->last_stream && !c->last_capturing && !capturing) {
-        const cudaError_t q = cudaStreamQuery(c->last_stream);
-        if (q == cudaErrorNotReady) return EG_ERR_STATE;
-        if (q != cudaSuccess) (void)cudaGetLastError();
-    }
-    c->last_capturing = capturing;
-    c->last_stream = stream;
+    if (!claim_stream(c, stream)) return EG_ERR_STATE;
     int launches = 0;
     const TileTable tn_all = c->tiles_norm.view(c->err), tf_all = c->tiles_fused.view(c->err);
     const int S = c->P * c->T;
@@ -1384,6 +1391,13 @@ k_sum_partials(const double* __restrict__ in, int n, double* __restrict__ out) {
 
 }  // namespace eg
 
+template <typename T>
+static cudaError_t launch_clip(const ClipArgs& a, int grid, bool overlap, cudaStream_t stream) {
+    k_clip_sums<T><<<grid, kThreads, 0, stream>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    return e != cudaSuccess ? e : launch_pdl(overlap, k_clip_scale<T>, dim3(grid), dim3(kThreads), 0, stream, a);
+}
+
 extern "C" {
 
 eg_status eg_average_model(eg_ctx* c, const float* params, float* avg_dev, double* consensus_host,
@@ -1402,6 +1416,39 @@ eg_status eg_average_model(eg_ctx* c, const float* params, float* avg_dev, doubl
         EG_CUDA(c, cudaStreamSynchronize(stream));
     }
     EG_CUDA(c, cudaGetLastError());
+    return EG_OK;
+}
+
+eg_status eg_clip_gradients(eg_ctx* c, const void* grads, int dtype, double max_norm, int flags, float* out,
+                            float* norms_dev, void* stream_v) {
+    if (!c || !grads || !out || !norms_dev) return EG_ERR_INVALID;
+    if (dtype != EG_F32 && dtype != EG_BF16 && dtype != EG_F16) return EG_ERR_INVALID;
+    if (std::isnan(max_norm) || max_norm < 0.0 || (flags & ~EG_CLIP_ZERO_NONFINITE)) return EG_ERR_INVALID;
+    if (((uintptr_t)grads & 15u) || ((uintptr_t)out & 15u) || ((uintptr_t)norms_dev & 3u)) return EG_ERR_INVALID;
+    const size_t count = (size_t)c->P * c->stride;
+    const char *g0 = static_cast<const char*>(grads), *o0 = reinterpret_cast<const char*>(out);
+    const char *g1 = g0 + count * (dtype == EG_F32 ? 4 : 2), *o1 = o0 + count * sizeof(float);
+    // in place, or two buffers that do not touch
+    if (!(dtype == EG_F32 && g0 == o0) && g0 < o1 && o0 < g1) return EG_ERR_INVALID;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return EG_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if (!claim_stream(c, stream)) return EG_ERR_STATE;
+    if (!c->clip_partials) {
+        const int grid = c->sms * kClipCtasPerSm;
+        eg_status s = dev_alloc(c, &c->clip_partials, (size_t)c->P + grid, false);
+        if (s != EG_OK) return s;
+        c->clip_grid = grid;
+    }
+    const TileTable tt = c->tiles_norm.view(c->err);
+    const int grid = (int)std::min<long long>(c->clip_grid, (long long)c->P * tt.n_tiles);
+    const ClipArgs a{grads, out, tt, c->P, (long long)c->stride, max_norm, flags & EG_CLIP_ZERO_NONFINITE,
+                     c->clip_partials, norms_dev};
+    const cudaError_t e = dtype == EG_F32    ? launch_clip<float>(a, grid, !c->no_pdl, stream)
+                          : dtype == EG_BF16 ? launch_clip<__nv_bfloat16>(a, grid, !c->no_pdl, stream)
+                                             : launch_clip<__half>(a, grid, !c->no_pdl, stream);
+    EG_CUDA(c, e);
+    c->clipped = true;
     return EG_OK;
 }
 
