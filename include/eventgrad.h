@@ -332,6 +332,53 @@ enum { EG_CLIP_ZERO_NONFINITE = 1 };
 eg_status eg_clip_gradients(eg_ctx* ctx, const void* grads, int dtype, double max_norm, int flags,
                             float* out, float* norms_dev, void* stream);
 
+/* A matrix of every replica: element (i, row, column) is at data[i * replica_stride + row *
+ * row_stride + column] (strides in elements; columns are contiguous).  For a vector of every
+ * replica row_stride is not used.  data == NULL: not given.  Device memory. */
+typedef struct {
+    void* data;
+    int64_t replica_stride, row_stride;
+} eg_matrix;
+
+/* The norm between two residual blocks: the norm after a block, its gate, the scaled residual
+ * and the norm before the next block, in one pass over the rows.  For every replica, with
+ * rms(v) = v / sqrt(mean(v^2) + eps) along a row:
+ *     r' = scale * r + sigmoid(gate) * rms(y) * w_post,      o = rms(r') * w_pre.
+ * y, residual (r), residual_out (r'), out (o): `rows` x `width` per replica; w_post, gate, scale,
+ * w_pre: `width` per replica; all of type dtype.  What is not given drops out of the formula:
+ * w_post (y enters without a norm), gate and scale (1), y (r' = scale * r; residual_out may then
+ * be left out), w_pre together with out (no second norm).  width <= EG_NORM_MAX_WIDTH.
+ * eg_residual_norm computes residual_out and out.  residual_out may be residual itself.
+ *
+ * eg_residual_norm_backward takes d_residual_out and d_out (the gradients of r' and o; either
+ * may be left out: zero; d_out needs w_pre) and the inputs again (nothing is saved between the
+ * two calls), and computes dy, d_residual and -- as sums over the rows -- d_w_post, d_gate,
+ * d_scale, d_w_pre.  Each output may be left out; d_w_post, d_gate, d_scale and d_w_pre need
+ * their vector.  Outputs are overwritten.  It needs `workspace` of at least
+ * eg_residual_norm_workspace(P, width) bytes, 16-byte aligned, free for reuse once the stream
+ * has passed the call.  Sums over rows are fp32 in a fixed order.  rows == 0 gives zero sums.
+ * Both calls only enqueue work on `stream` of the current device, hold no state and may be
+ * recorded into a graph.  Outputs must not overlap inputs or each other except as said. */
+#define EG_NORM_MAX_WIDTH 8192
+typedef struct {
+    int64_t P, rows, width, dtype;
+    double eps;
+    eg_matrix y, residual, w_post, gate, scale, w_pre;      /* in */
+    eg_matrix residual_out, out;                            /* out of the forward call */
+    eg_matrix d_residual_out, d_out;                        /* in, backward */
+    eg_matrix dy, d_residual, d_w_post, d_gate, d_scale, d_w_pre; /* out of the backward call */
+    void* workspace;
+    int64_t workspace_bytes;
+} eg_residual_norm_args;
+eg_status eg_residual_norm(const eg_residual_norm_args* args, void* stream);
+eg_status eg_residual_norm_backward(const eg_residual_norm_args* args, void* stream);
+int64_t eg_residual_norm_workspace(int64_t P, int64_t width);
+
+/* The operators' kernels never trap and their waits are bounded; a wait that runs out sets a word
+ * of the current device.  Synchronises `stream`, returns EG_ERR_TIMEOUT if that happened in any
+ * call since the last query (EG_OK otherwise) and clears the word. */
+eg_status eg_operator_status(void* stream);
+
 /* Change norms without any allocation.  (The paper has no counterpart: this is a service
  * entry point of the library, not a step of the method.)
  *

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -33,7 +34,8 @@ EXPORTS = [
     "eg_topk_repeat_count",
     "eg_set_quantisation",
     "eg_last_quantised",
-    "eg_clip_gradients",
+    "eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace",
+    "eg_operator_status",
 ]
 STATIC_MAX_TENSORS = 192
 STATIC_MAX_PARTIALS = 524288
@@ -119,6 +121,10 @@ def load_library() -> C.CDLL:
     lib.eg_set_quantisation.argtypes = [vp, C.c_int]
     lib.eg_last_quantised.argtypes = [vp, vp, vp]
     lib.eg_clip_gradients.argtypes = [vp, vp, C.c_int, C.c_double, C.c_int, vp, vp, vp]
+    lib.eg_residual_norm.argtypes = lib.eg_residual_norm_backward.argtypes = [C.c_char_p, vp]
+    lib.eg_residual_norm_workspace.argtypes = [C.c_int64, C.c_int64]
+    lib.eg_residual_norm_workspace.restype = C.c_int64
+    lib.eg_operator_status.argtypes = [vp]
     lib.eg_last_cuda_error.argtypes = [vp]
     lib.eg_last_launch_count.argtypes = [vp]
     _lib = lib
@@ -451,6 +457,135 @@ def change_norms_static(x: torch.Tensor, xhat: torch.Tensor, tensor_offset: Sequ
                                         C.c_void_p(s.cuda_stream))
     _check(lib, st, None, "eg_change_norms_static")
     return out
+
+
+# --------------------------------------------------------------------------------------
+# operators around the step: values of one type per call, ``[P, rows, width]`` activations and
+# ``[P, ...]`` views of the replicas' weights, on torch's current stream unless one is given
+# --------------------------------------------------------------------------------------
+_NONE = (0, 0, 0)
+_NORM_ARGS = struct.Struct("=4qd48q2q")   # eg_residual_norm_args
+
+
+def _matrix(t: Optional[torch.Tensor], shape: tuple, like: torch.Tensor, what: str) -> tuple:
+    """(pointer, replica stride, row stride) of a ``[P, rows, columns]`` or ``[P, columns]`` tensor."""
+    if t is None:
+        return _NONE
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
+        raise EventGradError(f"{what}: expected {shape} {like.dtype} on {like.device}, "
+                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise EventGradError(f"{what}: the last dimension must be contiguous")
+    return (t.data_ptr(), st[0], st[1] if len(st) == 3 else 0)
+
+
+class _OnStream:
+    """Makes ``stream`` (and the tensor's device) current while outputs and workspaces are allocated, so that
+    they belong to the stream that uses them."""
+
+    def __init__(self, x: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+        if not x.is_cuda:
+            raise EventGradError("no CUDA device: this library has no CPU path")
+        self._ctx = None
+        if stream is not None:
+            self._ctx = torch.cuda.stream(stream)
+        elif x.device.index != torch.cuda.current_device():
+            self._ctx = torch.cuda.device(x.device)
+        self._device = x.device
+
+    def __enter__(self) -> int:
+        if self._ctx is not None:
+            self._ctx.__enter__()
+        return torch.cuda.current_stream(self._device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self._ctx is not None:
+            self._ctx.__exit__(*exc)
+
+
+def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                  w_pre: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  residual_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """``eg_residual_norm``: ``r' = scale * residual + sigmoid(gate) * rms(y) * w_post`` and
+    ``o = rms(r') * w_pre`` for ``[P, rows, width]`` activations and ``[P, width]`` vectors.
+
+    Returns ``(r', o)``; ``o`` is None without ``w_pre``.  ``y`` None: only the scaled residual."""
+    lib = load_library()
+    if residual.dim() != 3 or residual.dtype not in DTYPES:
+        raise EventGradError("residual_norm: residual must be [P, rows, width] fp32, bf16 or fp16")
+    shape = residual.shape
+    P, n, d = shape
+    vec = torch.Size((P, d))
+    with _OnStream(residual, stream) as s:
+        if residual_out is None:
+            residual_out = torch.empty(shape, dtype=residual.dtype, device=residual.device)
+        if out is None and w_pre is not None:
+            out = torch.empty(shape, dtype=residual.dtype, device=residual.device)
+        args = _NORM_ARGS.pack(
+            P, n, d, DTYPES[residual.dtype], eps,
+            *_matrix(y, shape, residual, "y"), *_matrix(residual, shape, residual, "residual"),
+            *_matrix(w_post, vec, residual, "w_post"), *_matrix(gate, vec, residual, "gate"),
+            *_matrix(scale, vec, residual, "scale"), *_matrix(w_pre, vec, residual, "w_pre"),
+            *_matrix(residual_out, shape, residual, "residual_out"), *_matrix(out, shape, residual, "out"),
+            *(_NONE * 8), 0, 0)
+        if n:
+            _check(lib, lib.eg_residual_norm(args, s), None, "eg_residual_norm")
+    return residual_out, out
+
+
+def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Optional[torch.Tensor],
+                           y: Optional[torch.Tensor], residual: torch.Tensor, *,
+                           w_post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                           scale: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None,
+                           eps: float = 1e-6, d_weights: Optional[Sequence] = None,
+                           stream: Optional[torch.cuda.Stream] = None):
+    """``eg_residual_norm_backward``: from the gradients of ``r'`` and ``o`` (either may be None) and the
+    inputs of the forward call, ``(dy, d_residual, (d_w_post, d_gate, d_scale, d_w_pre))``.
+
+    ``d_weights``: four ``[P, width]`` tensors that receive the last ones (views of a gradient buffer in
+    the step's layout, say; None for a vector that was not given); default: new tensors."""
+    lib = load_library()
+    if residual.dim() != 3 or residual.dtype not in DTYPES:
+        raise EventGradError("residual_norm_backward: residual must be [P, rows, width] fp32, bf16 or fp16")
+    shape = residual.shape
+    P, n, d = shape
+    vec = torch.Size((P, d))
+    new = dict(dtype=residual.dtype, device=residual.device)
+    weights = (w_post, gate, scale, w_pre)
+    with _OnStream(residual, stream) as s:
+        if d_weights is None:
+            d_weights = tuple(None if w is None else torch.empty(vec, **new) for w in weights)
+        elif len(d_weights) != 4:
+            raise EventGradError("residual_norm_backward: d_weights holds four tensors or None")
+        dy = None if y is None else torch.empty(shape, **new)
+        dr = torch.empty(shape, **new)
+        bytes_ = lib.eg_residual_norm_workspace(P, d)
+        workspace = torch.empty(bytes_, dtype=torch.uint8, device=residual.device)
+        args = _NORM_ARGS.pack(
+            P, n, d, DTYPES[residual.dtype], eps,
+            *_matrix(y, shape, residual, "y"), *_matrix(residual, shape, residual, "residual"),
+            *_matrix(w_post, vec, residual, "w_post"), *_matrix(gate, vec, residual, "gate"),
+            *_matrix(scale, vec, residual, "scale"), *_matrix(w_pre, vec, residual, "w_pre"), *(_NONE * 2),
+            *_matrix(d_residual_out, shape, residual, "d_residual_out"), *_matrix(d_out, shape, residual, "d_out"),
+            *_matrix(dy, shape, residual, "dy"), *_matrix(dr, shape, residual, "d_residual"),
+            *_matrix(d_weights[0], vec, residual, "d_w_post"), *_matrix(d_weights[1], vec, residual, "d_gate"),
+            *_matrix(d_weights[2], vec, residual, "d_scale"), *_matrix(d_weights[3], vec, residual, "d_w_pre"),
+            workspace.data_ptr(), bytes_)
+        if n:
+            _check(lib, lib.eg_residual_norm_backward(args, s), None, "eg_residual_norm_backward")
+        else:
+            for t in d_weights:
+                if t is not None:
+                    t.zero_()
+    return dy, dr, tuple(d_weights)
+
+
+def operator_status(device: Optional[torch.device] = None) -> int:
+    """``eg_operator_status`` on the current stream: 0, or EG_ERR_TIMEOUT (5) when a bounded wait ran out."""
+    return int(load_library().eg_operator_status(torch.cuda.current_stream(device).cuda_stream))
 
 
 def from_workload(wl, **overrides) -> EventGrad:

@@ -8,15 +8,15 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = [os.path.join(HERE, "csrc", "eventgrad.cu"), os.path.join(HERE, "csrc", "eg_norms_static.cu")]
+#: the operators around the step: their products may be contracted into fused multiply-adds
+OPS = [os.path.join(HERE, "csrc", "eg_residual_norm.cu")]
 LIB = os.path.join(HERE, "libeventgrad.so")
 LIB_DEBUG = os.path.join(HERE, "libeventgrad_debug.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
-FLAGS = [
-    "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--fmad=false",            # every fused multiply-add of the path is written out
-    "-Xcompiler", "-fPIC", "-shared", "-DEG_FUSED_VPT=1", "-ldl",
-]
+FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+         "-Xcompiler", "-fPIC", "-DEG_FUSED_VPT=1"]
+STEP_FLAGS = ["--fmad=false"]  # every fused multiply-add of the step is written out
 
 
 def sources():
@@ -28,8 +28,17 @@ def sources():
 def _compile(lib: str, extra, force: bool, verbose: bool) -> str:
     newest = max(os.path.getmtime(p) for p in sources())
     if force or not os.path.exists(lib) or os.path.getmtime(lib) < newest:
-        cmd = [NVCC] + FLAGS + list(extra) + (["-Xptxas", "-v"] if verbose else []) + ["-o", lib] + SRC
-        subprocess.run(cmd, check=True)
+        flags = FLAGS + list(extra) + (["-Xptxas", "-v"] if verbose else [])
+        objects, running = [], []
+        os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
+        for src in SRC + OPS:
+            obj = os.path.join(HERE, "_build", os.path.basename(lib) + "." + os.path.basename(src) + ".o")
+            objects.append(obj)
+            running.append(subprocess.Popen([NVCC] + flags + (STEP_FLAGS if src in SRC else []) + ["-c", "-o", obj, src]))
+        failed = [p.args for p in running if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.run([NVCC] + FLAGS[:2] + ["-shared", "-o", lib] + objects + ["-ldl"], check=True)
     return lib
 
 
