@@ -374,6 +374,42 @@ eg_status eg_residual_norm(const eg_residual_norm_args* args, void* stream);
 eg_status eg_residual_norm_backward(const eg_residual_norm_args* args, void* stream);
 int64_t eg_residual_norm_workspace(int64_t P, int64_t width);
 
+/* A gated feed-forward block of every replica:
+ *     G = x Wg^T,  U = x Wu^T,  H = act(G) * U,  y = H Wd^T
+ * and its gradients from dy:
+ *     dH = dy Wd,  dU = dH * act(G),  dG = dH * U * act'(G),
+ *     dx = dG Wg + dU Wu,  dWg = dG^T x,  dWu = dU^T x,  dWd = dy^T H.
+ * x, y, dy, dx: `rows` x d_model per replica; w_gate, w_up and their gradients: d_ff x d_model;
+ * w_down and its gradient: d_model x d_ff; all of type dtype.  act: silu, gelu (with erf) or relu.
+ * Products are summed in fp32.  In the 16-bit types H, dG and dU are rounded to the type (they
+ * are operands of the next product), and so are G and U where the backward call reads them.
+ *
+ * eg_feed_forward computes y.  With `saved` (device, 16-byte aligned, at least
+ * eg_feed_forward_saved_bytes) it leaves what the backward call reads there.
+ * eg_feed_forward_backward reads dy, x, the weights and `saved` and overwrites dx, d_gate, d_up,
+ * d_down; each of the four may be left out.  rows == 0 gives zero weight gradients.
+ * `workspace` (device, 16-byte aligned) holds at least eg_feed_forward_workspace(args, backward)
+ * bytes -- which depends on sizes, alignment and strides of the given matrices -- and is free for
+ * reuse once the stream has passed the call.  Rows of any stride and alignment are taken; rows on
+ * 16-byte boundaries are read in place, others are copied into the workspace first.
+ * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded
+ * into a graph; the results do not depend on the run.  Outputs must not overlap inputs or each
+ * other.  Errors: EG_ERR_INVALID, EG_ERR_CUDA. */
+enum { EG_ACT_SILU = 0, EG_ACT_GELU = 1, EG_ACT_RELU = 2 };
+typedef struct {
+    int64_t P, rows, d_model, d_ff, dtype, activation;
+    eg_matrix x, w_gate, w_up, w_down;       /* in */
+    eg_matrix y;                             /* out of the forward call */
+    eg_matrix dy;                            /* in, backward */
+    eg_matrix dx, d_gate, d_up, d_down;      /* out of the backward call */
+    void* saved;
+    int64_t saved_bytes;
+} eg_feed_forward_args;
+int64_t eg_feed_forward_saved_bytes(const eg_feed_forward_args* args);
+int64_t eg_feed_forward_workspace(const eg_feed_forward_args* args, int backward);
+eg_status eg_feed_forward(const eg_feed_forward_args* args, void* workspace, int64_t workspace_bytes, void* stream);
+eg_status eg_feed_forward_backward(const eg_feed_forward_args* args, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* The operators' kernels never trap and their waits are bounded; a wait that runs out sets a word
  * of the current device.  Synchronises `stream`, returns EG_ERR_TIMEOUT if that happened in any
  * call since the last query (EG_OK otherwise) and clears the word. */

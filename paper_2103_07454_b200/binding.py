@@ -35,7 +35,8 @@ EXPORTS = [
     "eg_set_quantisation",
     "eg_last_quantised",
     "eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace",
-    "eg_operator_status",
+    "eg_operator_status", "eg_feed_forward", "eg_feed_forward_backward", "eg_feed_forward_saved_bytes",
+    "eg_feed_forward_workspace",
 ]
 STATIC_MAX_TENSORS = 192
 STATIC_MAX_PARTIALS = 524288
@@ -45,6 +46,7 @@ FUSED_AUTO = 2
 F32, BF16, F16 = 0, 1, 2
 DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 CLIP_ZERO_NONFINITE = 1
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 KERNEL_GROUPS = ("norm", "decide", "topk", "fused")
 
 
@@ -125,6 +127,11 @@ def load_library() -> C.CDLL:
     lib.eg_residual_norm_workspace.argtypes = [C.c_int64, C.c_int64]
     lib.eg_residual_norm_workspace.restype = C.c_int64
     lib.eg_operator_status.argtypes = [vp]
+    lib.eg_feed_forward.argtypes = lib.eg_feed_forward_backward.argtypes = [C.c_char_p, vp, C.c_int64, vp]
+    lib.eg_feed_forward_saved_bytes.argtypes = [C.c_char_p]
+    lib.eg_feed_forward_saved_bytes.restype = C.c_int64
+    lib.eg_feed_forward_workspace.argtypes = [C.c_char_p, C.c_int]
+    lib.eg_feed_forward_workspace.restype = C.c_int64
     lib.eg_last_cuda_error.argtypes = [vp]
     lib.eg_last_launch_count.argtypes = [vp]
     _lib = lib
@@ -464,6 +471,7 @@ def change_norms_static(x: torch.Tensor, xhat: torch.Tensor, tensor_offset: Sequ
 # ``[P, ...]`` views of the replicas' weights, on torch's current stream unless one is given
 # --------------------------------------------------------------------------------------
 _NONE = (0, 0, 0)
+_FFN_ARGS = struct.Struct("=6q30q2q")     # eg_feed_forward_args
 _NORM_ARGS = struct.Struct("=4qd48q2q")   # eg_residual_norm_args
 
 
@@ -581,6 +589,75 @@ def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Option
                 if t is not None:
                     t.zero_()
     return dy, dr, tuple(d_weights)
+
+
+def _ffn_sizes(x: torch.Tensor, w_gate: torch.Tensor, activation: str, what: str):
+    if x.dim() != 3 or w_gate.dim() != 3 or x.dtype not in DTYPES:
+        raise EventGradError(f"{what}: x must be [P, rows, d_model] and w_gate [P, d_ff, d_model], fp32, bf16 or fp16")
+    if activation not in ACTIVATIONS:
+        raise EventGradError(f"{what}: activation must be one of {sorted(ACTIVATIONS)}")
+    P, n, d = x.shape
+    return P, n, d, w_gate.shape[1]
+
+
+def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
+                 activation: str = "silu", save: bool = False, out: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+    """``eg_feed_forward``: ``(act(x w_gate^T) * (x w_up^T)) w_down^T`` of every replica.
+
+    ``x``: ``[P, rows, d_model]``; ``w_gate``, ``w_up``: ``[P, d_ff, d_model]``; ``w_down``: ``[P, d_model, d_ff]``
+    (views of a parameter buffer, say).  With ``save`` returns ``(y, saved)``, the second for
+    ``feed_forward_backward``."""
+    lib = load_library()
+    P, n, d, f = _ffn_sizes(x, w_gate, activation, "feed_forward")
+    up, down = torch.Size((P, f, d)), torch.Size((P, d, f))
+    with _OnStream(x, stream) as s:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        head = (P, n, d, f, DTYPES[x.dtype], ACTIVATIONS[activation], *_matrix(x, x.shape, x, "x"),
+                *_matrix(w_gate, up, x, "w_gate"), *_matrix(w_up, up, x, "w_up"), *_matrix(w_down, down, x, "w_down"),
+                *_matrix(out, x.shape, x, "out"), *(_NONE * 5))
+        saved, saved_bytes = None, 0
+        if save:
+            saved_bytes = lib.eg_feed_forward_saved_bytes(_FFN_ARGS.pack(*head, 0, 0))
+            saved = torch.empty(saved_bytes, dtype=torch.uint8, device=x.device)
+        if n:
+            args = _FFN_ARGS.pack(*head, saved.data_ptr() if save else 0, saved_bytes)
+            bytes_ = lib.eg_feed_forward_workspace(args, 0)
+            workspace = torch.empty(bytes_, dtype=torch.uint8, device=x.device)
+            _check(lib, lib.eg_feed_forward(args, workspace.data_ptr(), bytes_, s), None, "eg_feed_forward")
+    return (out, saved) if save else out
+
+
+def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                          w_down: torch.Tensor, saved: torch.Tensor, *, activation: str = "silu",
+                          d_weights: Optional[Sequence] = None, stream: Optional[torch.cuda.Stream] = None):
+    """``eg_feed_forward_backward``: ``(dx, (d_gate, d_up, d_down))`` from the gradient of the output, the inputs
+    and what ``feed_forward(..., save=True)`` saved.
+
+    ``d_weights``: three tensors of the weights' shapes that receive the last ones (views of a gradient
+    buffer in the step's layout, say; None: not wanted); default: new tensors."""
+    lib = load_library()
+    P, n, d, f = _ffn_sizes(x, w_gate, activation, "feed_forward_backward")
+    up, down = torch.Size((P, f, d)), torch.Size((P, d, f))
+    if not saved.is_cuda or saved.dtype != torch.uint8 or not saved.is_contiguous():
+        raise EventGradError("feed_forward_backward: saved is what feed_forward(..., save=True) returned")
+    with _OnStream(x, stream) as s:
+        if d_weights is None:
+            d_weights = tuple(torch.empty(sh, dtype=x.dtype, device=x.device) for sh in (up, up, down))
+        elif len(d_weights) != 3:
+            raise EventGradError("feed_forward_backward: d_weights holds three tensors or None")
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        args = _FFN_ARGS.pack(
+            P, n, d, f, DTYPES[x.dtype], ACTIVATIONS[activation], *_matrix(x, x.shape, x, "x"),
+            *_matrix(w_gate, up, x, "w_gate"), *_matrix(w_up, up, x, "w_up"), *_matrix(w_down, down, x, "w_down"),
+            *_NONE, *_matrix(dy, x.shape, x, "dy"), *_matrix(dx, x.shape, x, "dx"), *_matrix(d_weights[0], up, x, "d_gate"),
+            *_matrix(d_weights[1], up, x, "d_up"), *_matrix(d_weights[2], down, x, "d_down"),
+            saved.data_ptr(), saved.numel())
+        bytes_ = lib.eg_feed_forward_workspace(args, 1)
+        workspace = torch.empty(bytes_, dtype=torch.uint8, device=x.device)
+        _check(lib, lib.eg_feed_forward_backward(args, workspace.data_ptr(), bytes_, s), None, "eg_feed_forward_backward")
+    return dx, tuple(d_weights)
 
 
 def operator_status(device: Optional[torch.device] = None) -> int:

@@ -9,7 +9,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = [os.path.join(HERE, "csrc", "eventgrad.cu"), os.path.join(HERE, "csrc", "eg_norms_static.cu")]
 #: the operators around the step: their products may be contracted into fused multiply-adds
-OPS = [os.path.join(HERE, "csrc", "eg_residual_norm.cu")]
+OPS = [os.path.join(HERE, "csrc", f) for f in ("eg_residual_norm.cu", "eg_feed_forward.cu")]
 LIB = os.path.join(HERE, "libeventgrad.so")
 LIB_DEBUG = os.path.join(HERE, "libeventgrad_debug.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

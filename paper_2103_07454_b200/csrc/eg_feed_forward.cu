@@ -1,0 +1,463 @@
+// The gated feed-forward block of every replica (eg_feed_forward) and its gradients: the plan of
+// buffers and products, and the launches.  The products run in eg_gemm.cuh.
+//
+//   forward   1. [G | U] = x [Wg | Wu]^T with H = act(G) * U formed from the accumulators   (one launch)
+//             2. y = H Wd^T
+//   backward  3. dH = dy Wd with dG, dU formed from the accumulators and the saved G, U
+//             4. dx = dG Wg + dU Wu,  dWd = dy^T H,  dWg = dG^T x,  dWu = dU^T x           (one launch)
+#include <cstring>
+
+#include "eg_gemm.cuh"
+
+namespace eg {
+namespace {
+
+struct Mat {
+    void* p;
+    long long rep, row;
+};
+
+// ----------------------------------------------------------------------------------- tensor maps
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+    static EncodeFn fn = nullptr;
+    if (!fn) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess)
+            return nullptr;
+        fn = reinterpret_cast<EncodeFn>(p);
+    }
+    return fn;
+}
+
+// Rows on 16-byte boundaries, which the copies need.
+bool in_place(const Mat& m, long long P, long long rows, size_t size) {
+    return aligned16(m.p) && (rows <= 1 || m.row * (long long)size % 16 == 0) && (P <= 1 || m.rep * (long long)size % 16 == 0);
+}
+
+// [P][rows][cols] matrix in boxes of box_rows x box_cols.
+bool encode(CUtensorMap* map, int dtype, const Mat& m, long long P, long long rows, long long cols, int box_cols, int box_rows) {
+    EncodeFn fn = encoder();
+    if (!fn) return false;
+    const size_t size = dtype == EG_F32 ? 4 : 2;
+    const long long pad = (cols * (long long)size + 15) / 16 * 16;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)P};
+    const cuuint64_t row = rows > 1 ? (cuuint64_t)(m.row * (long long)size) : (cuuint64_t)pad;
+    const cuuint64_t strides[2] = {row, P > 1 ? (cuuint64_t)(m.rep * (long long)size) : row * (cuuint64_t)rows};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    const int bytes = box_cols * (int)size;
+    return fn(map,
+              dtype == EG_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                              : dtype == EG_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+              3, m.p, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// ----------------------------------------------------------------------------------- copies
+// Rows of any stride and alignment to rows on 16-byte boundaries; one warp per row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_repack(Mat src, Mat dst, long long P, long long rows, int cols) {
+    const int lane = threadIdx.x & 31;
+    for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < P * rows; u += (long long)gridDim.x * 8) {
+        const long long i = u / rows, r = u % rows;
+        const T* s = static_cast<const T*>(src.p) + i * src.rep + r * src.row;
+        T* d = static_cast<T*>(dst.p) + i * dst.rep + r * dst.row;
+#pragma unroll 4
+        for (int c = lane; c < cols; c += 32) d[c] = s[c];
+    }
+}
+
+// fp32 rows to their three bf16 parts (matrices `plane` elements apart).
+__global__ void __launch_bounds__(256) k_split(Mat src, Mat dst, long long plane, long long P, long long rows, int cols) {
+    const int lane = threadIdx.x & 31;
+    for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < P * rows; u += (long long)gridDim.x * 8) {
+        const long long i = u / rows, r = u % rows;
+        const float* s = static_cast<const float*>(src.p) + i * src.rep + r * src.row;
+        uint32_t* d = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(dst.p) + i * dst.rep + r * dst.row);
+#pragma unroll 2
+        for (int c = 2 * lane; c < cols; c += 64) {      // the pitch is even: a last odd column takes a zero along
+            uint32_t w[kParts];
+            split2(s[c], c + 1 < cols ? s[c + 1] : 0.f, w);
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) d[(k * plane + c) / 2] = w[k];
+        }
+    }
+}
+
+// ----------------------------------------------------------------------------------- plan
+struct Bump {
+    char* base = nullptr;                         // nullptr: only the size is wanted
+    long long at = 0;
+    void* take(long long bytes) {
+        void* p = base ? base + at : nullptr;
+        at += (bytes + 255) / 256 * 256;
+        return p;
+    }
+};
+
+struct Operand {
+    Mat src, use;                                 // as given; as the products read it (fp32: the first part)
+    long long plane = 0;                          // elements from one part to the next
+    long long rows = 0, cols = 0;
+    bool copied = false;
+};
+
+struct Block {
+    const eg_feed_forward_args* q;
+    long long P, n, d, f, fp;
+    int dtype, parts;
+    size_t size;
+    Operand x, wg, wu, wd, dy;
+    Mat g, u;
+    Operand h, dg, du;
+};
+
+Mat mat(const eg_matrix& m) { return Mat{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
+
+long long pitch_of(long long cols) { return (cols + 63) / 64 * 64; }
+
+void place(Operand* o, const eg_matrix& m, const Block& b, long long rows, long long cols, Bump* w) {
+    o->src = o->use = mat(m);
+    o->rows = rows;
+    o->cols = cols;
+    if (b.dtype != EG_F32 && in_place(o->src, b.P, rows, b.size)) return;
+    o->copied = true;
+    const long long pitch = pitch_of(cols);
+    o->plane = b.P * rows * pitch;
+    o->use = Mat{w->take(o->plane * 2 * b.parts), rows * pitch, pitch};
+}
+
+bool valid(const eg_feed_forward_args* q, bool backward) {
+    if (!q) return false;
+    if (q->dtype != EG_F32 && q->dtype != EG_BF16 && q->dtype != EG_F16) return false;
+    if (q->activation != EG_ACT_SILU && q->activation != EG_ACT_GELU && q->activation != EG_ACT_RELU) return false;
+    if (q->P < 1 || q->P > 65535 || q->rows < 0 || q->rows > (1ll << 30) || q->d_model < 1 || q->d_model > (1ll << 24) ||
+        q->d_ff < 1 || q->d_ff > (1ll << 24))
+        return false;
+    const size_t size = q->dtype == EG_F32 ? 4 : 2;
+    struct { const eg_matrix* m; bool needed, written; long long rows, cols; } all[] = {
+        {&q->x, true, false, q->rows, q->d_model},         {&q->w_gate, true, false, q->d_ff, q->d_model},
+        {&q->w_up, true, false, q->d_ff, q->d_model},      {&q->w_down, true, false, q->d_model, q->d_ff},
+        {&q->y, !backward, !backward, q->rows, q->d_model}, {&q->dy, backward, false, q->rows, q->d_model},
+        {&q->dx, false, backward, q->rows, q->d_model},    {&q->d_gate, false, backward, q->d_ff, q->d_model},
+        {&q->d_up, false, backward, q->d_ff, q->d_model},  {&q->d_down, false, backward, q->d_model, q->d_ff}};
+    for (const auto& e : all) {
+        if (!e.m->data) {
+            if (e.needed && e.rows > 0) return false;
+            continue;
+        }
+        if ((uintptr_t)e.m->data % size || e.m->row_stride < 0 || e.m->replica_stride < 0) return false;
+        // neither the rows of a matrix nor the replicas' matrices overlap
+        if (e.rows > 1 && (e.m->row_stride < e.cols || e.m->row_stride >= (1ll << 36))) return false;
+        if (q->P > 1 && (e.m->replica_stride < (e.rows - 1) * e.m->row_stride + e.cols || e.m->replica_stride >= (1ll << 36)))
+            return false;
+    }
+    return true;
+}
+
+// Layout of `saved`: G, U, each [P][rows][fp] of the type, then H (fp32: its three parts).
+long long saved_bytes(const eg_feed_forward_args* q) {
+    return q->P * q->rows * pitch_of(q->d_ff) * (q->dtype == EG_F32 ? 2 * 4 + 2 * kParts : 3 * 2);
+}
+
+void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
+    b->q = q;
+    b->P = q->P; b->n = q->rows; b->d = q->d_model; b->f = q->d_ff;
+    b->fp = pitch_of(b->f);
+    b->dtype = (int)q->dtype;
+    b->size = q->dtype == EG_F32 ? 4 : 2;
+    b->parts = q->dtype == EG_F32 ? kParts : 1;
+    place(&b->x, q->x, *b, b->n, b->d, w);
+    place(&b->wg, q->w_gate, *b, b->f, b->d, w);
+    place(&b->wu, q->w_up, *b, b->f, b->d, w);
+    place(&b->wd, q->w_down, *b, b->d, b->f, w);
+    const long long plane = b->P * b->n * b->fp;
+    char* s = static_cast<char*>(q->saved);
+    b->g = Mat{s, b->n * b->fp, b->fp};
+    b->u = Mat{s ? s + plane * b->size : nullptr, b->n * b->fp, b->fp};
+    auto hidden = [&](Operand* o, void* p) {
+        o->use = Mat{p, b->n * b->fp, b->fp};
+        o->plane = plane;
+        o->rows = b->n;
+        o->cols = b->f;
+    };
+    hidden(&b->h, s ? s + 2 * plane * b->size : nullptr);
+    if (backward) {
+        place(&b->dy, q->dy, *b, b->n, b->d, w);
+        hidden(&b->dg, w->take(plane * 2 * b->parts));
+        hidden(&b->du, w->take(plane * 2 * b->parts));
+    } else if (!s) {
+        hidden(&b->h, w->take(plane * 2 * b->parts));
+    }
+}
+
+cudaError_t copy_in(const Block& b, const Operand& o, cudaStream_t stream) {
+    if (!o.copied) return cudaSuccess;
+    const long long blocks = (b.P * o.rows + 7) / 8, most = (long long)sm_count() * 8;
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    if (b.dtype == EG_F32) k_split<<<grid, 256, 0, stream>>>(o.src, o.use, o.plane, b.P, o.rows, (int)o.cols);
+    else k_repack<uint16_t><<<grid, 256, 0, stream>>>(o.src, o.use, b.P, o.rows, (int)o.cols);
+    return cudaGetLastError();
+}
+
+// ----------------------------------------------------------------------------------- products
+struct Builder {
+    GemmArgs a;
+    int maps = 0;
+    bool ok = true;
+    const Block& b;
+    int BN;
+
+    Builder(const Block& blk, int bn, unsigned int* err) : b(blk), BN(bn) {
+        a.problems = a.tiles = 0;
+        a.idesc = (1u << 4) | (b.dtype != EG_F16 ? (1u << 7) | (1u << 10) : 0u);
+        a.err = err;
+        a.act = (int)b.q->activation;
+        a.map_g = a.map_u = a.map_h = a.map_dg = a.map_du = -1;
+    }
+    int map(const Mat& m, int dtype, long long rows, long long cols, int box_cols, int box_rows) {
+        if (maps >= kGemmMaxMaps) { ok = false; return 0; }
+        ok = ok && encode(&a.maps[maps], dtype, m, b.P, rows, cols, box_cols, box_rows);
+        return maps++;
+    }
+    // a matrix of the block's type, or its parts one after the other (16-bit), in small boxes
+    int boxes(const Mat& m, int box_cols) { return map(m, b.dtype, b.n, b.f, box_cols, 32); }
+    int boxes(const Operand& o, int box_cols) {
+        const int first = maps;
+        for (int k = 0; k < b.parts; ++k) map(part(o, k), operand_type(), o.rows, o.cols, box_cols, 32);
+        return first;
+    }
+    int operand_type() const { return b.dtype == EG_F32 ? EG_BF16 : b.dtype; }
+    Mat part(const Operand& o, int k) const {
+        Mat m = o.use;
+        m.p = static_cast<uint16_t*>(m.p) + k * o.plane;
+        return m;
+    }
+    // operand of A (128 rows a CTA) or B (BN / 2): stored [mn][k] or, transposed, [k][mn]; the first of its maps
+    int operand(const Operand& o, bool mn, bool is_a) {
+        const int first = maps;
+        for (int k = 0; k < b.parts; ++k) {
+            if (mn) map(part(o, k), operand_type(), o.rows, o.cols, 64, 64);
+            else map(part(o, k), operand_type(), o.rows, o.cols, kGemmK, is_a ? 128 : BN / 2);
+        }
+        return first;
+    }
+    GemmProblem* problem(long long M, long long N, bool a_mn, bool b_mn, bool pair) {
+        GemmProblem* g = &a.p[a.problems++];
+        const int cols = pair ? BN / 2 : BN;
+        g->mt = (int)((M + kGemmM - 1) / kGemmM);
+        g->nt = (int)((N + cols - 1) / cols);
+        const long long tiles = b.P * g->mt * g->nt;
+        if (tiles + a.tiles > 0x7fffffffll) ok = false;
+        g->tiles = (int)tiles;
+        a.tiles += g->tiles;
+        g->nseg = 0;
+        g->a_mn = a_mn; g->b_mn = b_mn; g->b_pair = pair;
+        g->M = (int)M; g->N = (int)N;
+        g->out = -1;
+        return g;
+    }
+    // A B^T over K, as products of parts, the smallest ones first
+    void product(GemmProblem* g, int ma, int mb0, int mb1, long long K) {
+        for (int sum = b.parts - 1; sum >= 0; --sum) {
+            for (int i = 0; i <= sum; ++i) {
+                if (g->nseg >= kGemmMaxSegs) { ok = false; return; }
+                g->seg[g->nseg++] = GemmSeg{ma + i, mb0 + sum - i, mb1 + sum - i, (int)((K + kGemmK - 1) / kGemmK)};
+            }
+        }
+    }
+    void store_to(GemmProblem* g, const Mat& m, long long rows, long long cols) {
+        const int most = 128 / (int)b.size, columns = BN / 2 < most ? BN / 2 : most;
+        g->ptr = m.p; g->rep = m.rep; g->row = m.row;
+        g->out = in_place(m, b.P, rows, b.size) ? map(m, b.dtype, rows, cols, columns, 32) : -1;
+    }
+};
+
+template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& a, cudaStream_t stream) {
+    using Shape = GemmShape<BN>;
+    static bool raised[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !raised[dev]) {
+        e = cudaFuncSetAttribute(k_gemm<T, EPI, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) raised[dev] = true;
+    }
+    const int pairs = sm_count() / 2;
+    if (pairs < 1) return cudaErrorInvalidDevice;
+    k_gemm<T, EPI, BN><<<2 * (a.tiles < pairs ? a.tiles : pairs), kGemmThreads, Shape::kSmem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, int EPI> cudaError_t launch_gemm(const Builder& w, cudaStream_t stream) {
+    if (!w.ok) return cudaErrorInvalidValue;
+    if (w.a.tiles == 0) return cudaSuccess;
+    if constexpr (sizeof(T) == 2) {
+        if (w.BN == 256) return launch_shape<T, EPI, 256>(w.a, stream);
+    }
+    if (w.BN == 128) return launch_shape<T, EPI, 128>(w.a, stream);
+    if constexpr (EPI == kEpiStore || (EPI == kEpiGateUp && sizeof(T) == 2)) {
+        if (w.BN == 64) return launch_shape<T, EPI, 64>(w.a, stream);
+    }
+    if constexpr (EPI == kEpiStore) {
+        if (w.BN == 32) return launch_shape<T, EPI, 32>(w.a, stream);
+    }
+    return cudaErrorInvalidValue;
+}
+
+// The widest tile that still gives every pair of multiprocessors one; `cols` columns of the result
+// for a tile of 256.
+int tile_width(const Block& b, long long M, long long N, int cols, int least) {
+    const long long mt = (M + kGemmM - 1) / kGemmM, P = b.P;
+    int bn = 256;
+    if (b.dtype == EG_F32) {           // the sums of a tile in registers: 64 a thread
+        bn = 128;
+        cols /= 2;
+    }
+    while (bn > least && P * mt * ((N + cols - 1) / cols) < sm_count() / 2) {
+        bn /= 2;
+        cols /= 2;
+    }
+    return bn;
+}
+
+template <typename T> cudaError_t forward(const Block& b, unsigned int* err, cudaStream_t stream) {
+    cudaError_t e;
+    for (const Operand* o : {&b.x, &b.wg, &b.wu, &b.wd})
+        if ((e = copy_in(b, *o, stream)) != cudaSuccess) return e;
+    {
+        Builder w(b, tile_width(b, b.n, b.f, 128, b.dtype == EG_F32 ? 128 : 64), err);
+        GemmProblem* g = w.problem(b.n, b.f, false, false, true);
+        const int mx = w.operand(b.x, false, true), mg = w.operand(b.wg, false, false), mu = w.operand(b.wu, false, false);
+        w.product(g, mx, mg, mu, b.d);
+        const int box = w.BN / 4 < 32 ? w.BN / 4 : 32;
+        w.a.map_h = w.boxes(b.h, box);
+        if (b.q->saved) {
+            w.a.map_g = w.boxes(b.g, box);
+            w.a.map_u = w.boxes(b.u, box);
+        }
+        if ((e = launch_gemm<T, kEpiGateUp>(w, stream)) != cudaSuccess) return e;
+    }
+    Builder w(b, tile_width(b, b.n, b.d, 256, 32), err);
+    GemmProblem* g = w.problem(b.n, b.d, false, false, false);
+    const int mb = w.operand(b.wd, false, false);
+    w.product(g, w.operand(b.h, false, true), mb, mb, b.f);
+    w.store_to(g, mat(b.q->y), b.n, b.d);
+    return launch_gemm<T, kEpiStore>(w, stream);
+}
+
+template <typename T> cudaError_t backward(const Block& b, unsigned int* err, cudaStream_t stream) {
+    cudaError_t e;
+    const eg_feed_forward_args* q = b.q;
+    for (const Operand* o : {&b.x, &b.wg, &b.wu, &b.wd, &b.dy})
+        if ((e = copy_in(b, *o, stream)) != cudaSuccess) return e;
+    {
+        Builder w(b, tile_width(b, b.n, b.f, 256, 128), err);
+        GemmProblem* g = w.problem(b.n, b.f, false, true, false);
+        const int mb = w.operand(b.wd, true, false);
+        w.product(g, w.operand(b.dy, false, true), mb, mb, b.d);
+        w.a.map_g = w.boxes(b.g, 32);
+        w.a.map_u = w.boxes(b.u, 32);
+        w.a.map_dg = w.boxes(b.dg, 32);
+        w.a.map_du = w.boxes(b.du, 32);
+        if ((e = launch_gemm<T, kEpiDact>(w, stream)) != cudaSuccess) return e;
+    }
+    Builder w(b, b.dtype == EG_F32 ? 128 : 256, err);
+    if (q->dx.data) {
+        GemmProblem* g = w.problem(b.n, b.d, false, true, false);
+        const int mg = w.operand(b.wg, true, false), mu = w.operand(b.wu, true, false);
+        w.product(g, w.operand(b.dg, false, true), mg, mg, b.f);
+        w.product(g, w.operand(b.du, false, true), mu, mu, b.f);
+        w.store_to(g, mat(q->dx), b.n, b.d);
+    }
+    struct { const eg_matrix* out; const Operand *a, *bm; long long M, N; } grads[] = {
+        {&q->d_down, &b.dy, &b.h, b.d, b.f}, {&q->d_gate, &b.dg, &b.x, b.f, b.d}, {&q->d_up, &b.du, &b.x, b.f, b.d}};
+    for (const auto& t : grads) {
+        if (!t.out->data) continue;
+        GemmProblem* g = w.problem(t.M, t.N, true, true, false);
+        const int mb = w.operand(*t.bm, true, false);
+        w.product(g, w.operand(*t.a, true, true), mb, mb, b.n);
+        w.store_to(g, mat(*t.out), t.M, t.N);
+    }
+    return launch_gemm<T, kEpiStore>(w, stream);
+}
+
+cudaError_t zero(const eg_matrix& m, long long P, long long rows, long long cols, size_t size, cudaStream_t stream) {
+    for (long long i = 0; m.data && i < P; ++i) {
+        const cudaError_t e = cudaMemset2DAsync(static_cast<char*>(m.data) + i * m.replica_stride * (long long)size,
+                                                (rows > 1 ? m.row_stride : cols) * size, 0, cols * size, rows, stream);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+}  // namespace eg
+
+using namespace eg;
+
+extern "C" {
+
+int64_t eg_feed_forward_saved_bytes(const eg_feed_forward_args* q) {
+    if (!q || q->P < 1 || q->rows < 0 || q->d_ff < 1) return 0;
+    return saved_bytes(q);
+}
+
+int64_t eg_feed_forward_workspace(const eg_feed_forward_args* q, int backward) {
+    if (!valid(q, backward != 0)) return 0;
+    Bump w;
+    Block b;
+    plan(&b, q, backward != 0, &w);
+    return w.at;
+}
+
+eg_status eg_feed_forward(const eg_feed_forward_args* q, void* workspace, int64_t workspace_bytes, void* stream_v) {
+    if (!valid(q, false)) return EG_ERR_INVALID;
+    if (q->rows == 0) return EG_OK;
+    if (q->saved && (!aligned16(q->saved) || q->saved_bytes < saved_bytes(q))) return EG_ERR_INVALID;
+    Bump w;
+    w.base = static_cast<char*>(workspace);
+    Block b;
+    plan(&b, q, false, &w);
+    if (w.at > workspace_bytes || (w.at && (!workspace || !aligned16(workspace)))) return EG_ERR_INVALID;
+    unsigned int* err = operator_error_word();
+    if (!err) return EG_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    const cudaError_t e = q->dtype == EG_F32    ? forward<float>(b, err, stream)
+                          : q->dtype == EG_BF16 ? forward<__nv_bfloat16>(b, err, stream)
+                                                : forward<__half>(b, err, stream);
+    return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
+}
+
+eg_status eg_feed_forward_backward(const eg_feed_forward_args* q, void* workspace, int64_t workspace_bytes, void* stream_v) {
+    if (!valid(q, true)) return EG_ERR_INVALID;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if (q->rows == 0) {
+        const size_t size = q->dtype == EG_F32 ? 4 : 2;
+        const bool ok = zero(q->d_gate, q->P, q->d_ff, q->d_model, size, stream) == cudaSuccess &&
+                        zero(q->d_up, q->P, q->d_ff, q->d_model, size, stream) == cudaSuccess &&
+                        zero(q->d_down, q->P, q->d_model, q->d_ff, size, stream) == cudaSuccess;
+        return ok ? EG_OK : EG_ERR_CUDA;
+    }
+    if (!q->saved || !aligned16(q->saved) || q->saved_bytes < saved_bytes(q)) return EG_ERR_INVALID;
+    Bump w;
+    w.base = static_cast<char*>(workspace);
+    Block b;
+    plan(&b, q, true, &w);
+    if (w.at > workspace_bytes || (w.at && (!workspace || !aligned16(workspace)))) return EG_ERR_INVALID;
+    unsigned int* err = operator_error_word();
+    if (!err) return EG_ERR_CUDA;
+    const cudaError_t e = q->dtype == EG_F32    ? backward<float>(b, err, stream)
+                          : q->dtype == EG_BF16 ? backward<__nv_bfloat16>(b, err, stream)
+                                                : backward<__half>(b, err, stream);
+    return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,698 @@
+// Batched matrix products on the tensor cores for the feed-forward block (sm_100a).
+//
+// One launch works through the tiles of up to four products ("problems"), each of which is, for
+// every replica, D[M, N] = sum over segments of A[M, K] * B[N, K]^T with 16-bit operands and fp32
+// accumulators.  A segment is one pair of operand matrices; several segments add into one result
+// (dX = dG Wg + dU Wu; the parts of fp32 operands).
+//
+// fp32 operands come in kParts = 3 bf16 parts of 8 significant bits each, whose sum is the value; the six
+// products of parts that matter (part i of A with part j of B, i + j <= 2) are six segments of one
+// sum.  What is left out is below 2^-23 of |a||b|.
+//
+// Two CTAs of a cluster share a tile of 256 x BN (tcgen05.mma, cta_group::2): each stages its 128
+// rows of A and its half of B with TMA (128-byte swizzle, 64 elements of K a stage), the even CTA
+// issues the products, and each CTA keeps its 128 rows of D in its own tensor memory -- twice, so
+// that the epilogue of one tile runs under the products of the next.  An operand whose K runs
+// along its rows ("MN-major": the transposed uses of the backward pass) is staged in boxes of 64
+// columns and read by the tensor cores in that order; nothing is ever transposed in memory.
+//
+// Warps: 0 TMA producer, 1 tensor-core issue, 2 tensor memory, 4..11 epilogue (warp w reads the
+// 32 lanes w % 4 of tensor memory; warps 4..7 take the first half of the columns, 8..11 the other).
+#pragma once
+#include <cuda.h>
+
+#include "eg_ops.cuh"
+
+namespace eg {
+
+constexpr int kGemmThreads = 384;
+constexpr int kGemmEpiWarps = 8;
+constexpr int kGemmK = 64;                        // elements of K per stage: 128 bytes, one swizzle row
+constexpr int kGemmM = 256;                       // rows of a tile (two CTAs)
+constexpr int kGemmEpiBytes = 8192;               // staging per epilogue warp
+constexpr int kGemmMaxMaps = 40, kGemmMaxSegs = 12, kGemmMaxProblems = 4;
+
+struct GemmSeg {
+    int a, b0, b1;                                // maps; b0 / b1: B of the even / odd CTA
+    int ksteps;
+};
+
+// Tensor-core sums of fp32 parts are moved to registers and added there every kChunk stages: adding into the
+// accumulator truncates (about 3e-8 of it per instruction, always towards zero, so the error grows with
+// K: 5e-6 after 2816), an fp32 addition in registers rounds.  4 stages are 16 instructions, 5e-7 at most.
+constexpr int kChunk = 4;
+constexpr int kParts = 3;
+enum { kEpiStore = 0, kEpiGateUp = 1, kEpiDact = 2 };
+
+struct GemmProblem {
+    int tiles, mt, nt;                            // all tiles; tiles of one replica
+    int nseg;
+    GemmSeg seg[kGemmMaxSegs];
+    int a_mn, b_mn;                               // the operand's K runs along its rows
+    int b_pair;                                   // B of the two CTAs are two matrices, same rows
+    int M, N;                                     // of the result
+    int out;                                      // map of the result, -1: `ptr` (no 16-byte rows)
+    void* ptr;
+    long long rep, row;
+};
+
+struct GemmArgs {
+    CUtensorMap maps[kGemmMaxMaps];
+    GemmProblem p[kGemmMaxProblems];
+    int problems, tiles;
+    uint32_t idesc;                               // instruction descriptor without the majors
+    unsigned int* err;
+    // gate/up and activation-gradient epilogues: maps of 32 x 32 boxes
+    int act;
+    int map_g, map_u, map_h;                      // G, U (-1: not wanted), H; of H, dG and dU the parts follow one
+    int map_dg, map_du;                           // another where the values are fp32
+};
+
+// ------------------------------------------------------------------------------- PTX
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ bool mbar_test_now(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(op_smem(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Bounded; after a time-out anywhere in the CTA every wait returns at once and the walk goes on.
+__device__ __forceinline__ void mbar_wait(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err) {
+    if (mbar_test_now(bar, parity)) return;
+    const long long t0 = clock64();
+    unsigned spins = 0;
+    while (!mbar_test_now(bar, parity)) {
+        if ((++spins & 63u) != 0) continue;
+        if (*s_abort) return;
+        if (clock64() - t0 > kOpWaitCycles) {
+            *s_abort = 1;
+            atomicOr(err, kOpErrWaitTimeout);
+            return;
+        }
+    }
+}
+// This CTA's box of a tensor; completion on the even CTA's barrier (cluster address).
+__device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            op_smem(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                     op_smem(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(op_smem(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, const void* src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z),
+                 "r"(op_smem(src))
+                 : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+}
+// Arrives on the barrier at this address in both CTAs once the products issued so far are done.
+__device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     op_smem(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+
+#define EG_R8(a, o) "=r"(a[o]), "=r"(a[o + 1]), "=r"(a[o + 2]), "=r"(a[o + 3]), "=r"(a[o + 4]), "=r"(a[o + 5]), "=r"(a[o + 6]), "=r"(a[o + 7])
+// 32 (16, 8) columns of this warp's 32 lanes of tensor memory: thread <-> row.
+__device__ __forceinline__ void tc_load(uint32_t (&v)[32], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : EG_R8(v, 0), EG_R8(v, 8), EG_R8(v, 16), EG_R8(v, 24)
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tc_load(uint32_t (&v)[16], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : EG_R8(v, 0), EG_R8(v, 8)
+        : "r"(addr)
+        : "memory");
+}
+#undef EG_R8
+
+// Descriptor of a shared-memory operand, 128-byte swizzle.  K-major: groups of 8 rows are 1024 bytes
+// apart.  MN-major: groups of 8 rows of K are 1024 bytes apart, the next 64 columns of M or N 8192.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn) {
+    uint64_t d = (uint64_t)((addr & 0x3ffff) >> 4);
+    d |= (uint64_t)(mn ? (8192 >> 4) : 1) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= 1ull << 46;
+    d |= 2ull << 61;
+    return d;
+}
+__device__ __forceinline__ uint32_t swz128(uint32_t off) { return off ^ ((off >> 3) & 0x70u); }
+__device__ __forceinline__ uint32_t swz64(uint32_t off) { return off ^ ((off >> 3) & 0x30u); }
+
+// act(g) and its derivative.  The fast exponential (error of a few 2^-23 of its argument) serves results that
+// are rounded to 16 bits.
+template <typename T> __device__ __forceinline__ float exp_of(float x) {
+    if constexpr (sizeof(T) == 4) return expf(x);
+    else return __expf(x);
+}
+template <typename T> __device__ __forceinline__ float act_value(int act, float g) {
+    if (act == EG_ACT_SILU) return g / (1.f + exp_of<T>(-g));
+    if (act == EG_ACT_RELU) return fmaxf(g, 0.f);
+    return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+}
+template <typename T> __device__ __forceinline__ void act_both(int act, float g, float& v, float& dv) {
+    if (act == EG_ACT_SILU) {
+        const float s = 1.f / (1.f + exp_of<T>(-g));
+        v = g * s;
+        dv = s * (1.f + g * (1.f - s));
+    } else if (act == EG_ACT_RELU) {
+        v = fmaxf(g, 0.f);
+        dv = g > 0.f ? 1.f : 0.f;
+    } else {
+        const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        v = g * cdf;
+        dv = cdf + g * exp_of<T>(-0.5f * g * g) * 0.39894228040143268f;
+    }
+}
+
+// The three bf16 parts of two fp32 values, packed: each takes the 8 leading bits of what is left (exact).  A
+// value that is not finite is its own first part.
+__device__ __forceinline__ void split_parts(float x, uint32_t (&p)[kParts]) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        p[k] = __float_as_uint(x) & 0xffff0000u;
+        x -= __uint_as_float(p[k]);
+    }
+}
+__device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[kParts]) {
+    uint32_t pa[kParts], pb[kParts];
+    split_parts(a, pa);
+    split_parts(b, pb);
+    if (!isfinite(a)) { pa[0] = isnan(a) ? 0x7fc00000u : __float_as_uint(a); pa[1] = pa[2] = 0; }
+    if (!isfinite(b)) { pb[0] = isnan(b) ? 0x7fc00000u : __float_as_uint(b); pb[1] = pb[2] = 0; }
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) w[k] = (pa[k] >> 16) | pb[k];
+}
+// 32 columns of one row (fp32, in registers) as the parts' boxes of 2048 bytes.
+__device__ __forceinline__ void write_parts(unsigned char* boxes, int lane, const float (&v)[32]) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 8) {
+        uint32_t w[4][kParts];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) split2(v[e + 2 * z], v[e + 2 * z + 1], w[z]);
+        const uint32_t off = swz64(lane * 64 + e * 2);
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+            *reinterpret_cast<uint4*>(boxes + k * 2048 + off) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+    }
+}
+__device__ __forceinline__ void write_f32(unsigned char* box, int lane, const float (&v)[32]) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4)
+        *reinterpret_cast<float4*>(box + swz128(lane * 128 + e * 4)) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+}
+
+struct TilePos {
+    int problem, p, m, n;
+};
+__device__ __forceinline__ TilePos tile_pos(const GemmArgs& a, int t) {
+    TilePos q;
+    q.problem = 0;
+    while (t >= a.p[q.problem].tiles) t -= a.p[q.problem++].tiles;
+    const GemmProblem& g = a.p[q.problem];
+    const int per = g.mt * g.nt;
+    q.p = t / per;
+    t -= q.p * per;
+    q.n = t / g.mt;                 // neighbouring pairs of CTAs share their rows of B
+    q.m = t - q.n * g.mt;
+    return q;
+}
+
+template <int BN> struct GemmShape {
+    static constexpr int kABytes = 128 * kGemmK * 2, kBBytes = BN / 2 * kGemmK * 2;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kEpi = kGemmEpiWarps * kGemmEpiBytes;
+    static constexpr int kRoom = 227 * 1024 - 1024 - kEpi - 512;
+    static constexpr int kStages = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
+    static constexpr int kBars = kStages * kStageBytes + kEpi;
+    static constexpr int kSmem = 1024 + kBars + 512;
+    static constexpr int kCols = BN < 32 ? 32 : BN;         // tensor memory columns of one accumulator
+    static constexpr int kTmem = 2 * kCols;
+};
+
+// T: type of the operands and of 16-bit results; EPI: what becomes of D; BN: columns of a tile.
+template <typename T, int EPI, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant__ GemmArgs a) {
+    using Shape = GemmShape<BN>;
+    constexpr int S = Shape::kStages;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    unsigned char* epi = smem + S * Shape::kStageBytes;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + Shape::kBars);   // [S] (even CTA's are used)
+    uint64_t* empty = full + S;                                          // [S]
+    uint64_t* acc_full = empty + S;                                      // [2]
+    uint64_t* acc_empty = acc_full + 2;                                  // [2] (even CTA's are used)
+    uint64_t* epi_full = acc_empty + 2;                                  // [kGemmEpiWarps][2]
+    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + 2 * kGemmEpiWarps);
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(const_cast<int*>(s_abort) + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        *s_abort = 0;
+        for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
+        for (int q = 0; q < 2; ++q) { op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps); }
+        for (int q = 0; q < 2 * kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(op_smem(s_tmem)), "n"(Shape::kTmem)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = *s_tmem;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, round = 0;
+            for (int t = pair; t < a.tiles; t += pairs) {
+                const TilePos q = tile_pos(a, t);
+                const GemmProblem& g = a.p[q.problem];
+                const int m0 = q.m * kGemmM + (int)rank * 128;
+                const int n0 = g.b_pair ? q.n * (BN / 2) : q.n * BN + (int)rank * (BN / 2);
+                for (int e = 0; e < g.nseg; ++e) {
+                    const CUtensorMap* ma = &a.maps[g.seg[e].a];
+                    const CUtensorMap* mb = &a.maps[rank ? g.seg[e].b1 : g.seg[e].b0];
+                    for (int k = 0; k < g.seg[e].ksteps; ++k) {
+                        if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
+                        unsigned char* sa = smem + s * Shape::kStageBytes;
+                        unsigned char* sb = sa + Shape::kABytes;
+                        if (rank == 0) op_mbar_expect(&full[s], 2 * Shape::kStageBytes);
+                        const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
+                        if (g.a_mn) {
+                            tma_load_pair(sa, ma, m0, k * kGemmK, q.p, bar);
+                            tma_load_pair(sa + 8192, ma, m0 + 64, k * kGemmK, q.p, bar);
+                        } else {
+                            tma_load_pair(sa, ma, k * kGemmK, m0, q.p, bar);
+                        }
+                        if (g.b_mn) {
+#pragma unroll
+                            for (int h = 0; h < BN / 2; h += 64) tma_load_pair(sb + h * 128, mb, n0 + h, k * kGemmK, q.p, bar);
+                        } else {
+                            tma_load_pair(sb, mb, k * kGemmK, n0, q.p, bar);
+                        }
+                        if (++s == S) { s = 0; ++round; }
+                    }
+                }
+            }
+            // the last arrivals on this CTA's barriers, which the even CTA's products send, come in before it ends
+            for (int j = max(0, round * S + s - S); j < round * S + s; ++j)
+                mbar_wait(&empty[j % S], (j / S) & 1, s_abort, a.err);
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            int s = 0, round = 0, count = 0;                 // count: accumulators handed over
+            for (int t = pair; t < a.tiles; t += pairs) {
+                const TilePos q = tile_pos(a, t);
+                const GemmProblem& g = a.p[q.problem];
+                const uint32_t idesc = a.idesc | (g.a_mn ? 1u << 15 : 0u) | (g.b_mn ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
+                                       ((uint32_t)(kGemmM >> 4) << 24);
+                const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
+                uint32_t add = 0;
+                int in_chunk = 0;
+                for (int e = 0; e < g.nseg; ++e) {
+                    for (int k = 0; k < g.seg[e].ksteps; ++k) {
+                        const int buf = count & 1;
+                        const uint32_t d = tmem + buf * Shape::kCols;
+                        if (!add) {
+                            if (count >= 2) mbar_wait(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort, a.err);
+                            tc_fence_after();
+                        }
+                        mbar_wait(&full[s], round & 1, s_abort, a.err);
+                        tc_fence_after();
+                        const uint32_t sa = op_smem(smem + s * Shape::kStageBytes);
+                        const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + Shape::kABytes, g.b_mn);
+#pragma unroll
+                        for (int u = 0; u < kGemmK / 16; ++u) {
+                            tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
+                            add = 1;
+                        }
+                        tc_commit_pair(&empty[s]);
+                        if (++s == S) { s = 0; ++round; }
+                        if (sizeof(T) == 4 && ++in_chunk == kChunk) {
+                            tc_commit_pair(&acc_full[buf]);
+                            ++count;
+                            add = in_chunk = 0;
+                        }
+                    }
+                }
+                if (add) {
+                    tc_commit_pair(&acc_full[count & 1]);
+                    ++count;
+                }
+            }
+        }
+    } else if (warp >= 4) {
+        const int w = warp - 4, half = w >> 2;
+        unsigned char* buf_mem = epi + w * kGemmEpiBytes;
+        const uint32_t lanes = (uint32_t)((w & 3) * 32) << 16;
+        int count = 0, uses = 0;
+        (void)uses;
+        for (int t = pair; t < a.tiles; t += pairs) {
+            const TilePos q = tile_pos(a, t);
+            const GemmProblem& g = a.p[q.problem];
+            const int buf = count & 1;
+            const int row0 = q.m * kGemmM + (int)rank * 128 + (w & 3) * 32;
+            const uint32_t acc = tmem + buf * Shape::kCols + lanes;
+            // first column of D that this warp's x-th one is (gate/up: half of the gate's, half of the other's)
+            auto column = [&](int x) {
+                if (EPI == kEpiGateUp) return half * (BN / 4) + (x < BN / 4 ? x : BN / 4 + x);
+                return half * (BN / 2) + x;
+            };
+            float sum[sizeof(T) == 4 ? BN / 2 : 1];          // fp32: this row's BN / 2 columns, added up over the chunks
+            if constexpr (sizeof(T) == 4) {
+                int ksteps = 0;
+                for (int e = 0; e < g.nseg; ++e) ksteps += g.seg[e].ksteps;
+                const int chunks = (ksteps + kChunk - 1) / kChunk;
+#pragma unroll
+                for (int x = 0; x < BN / 2; ++x) sum[x] = 0.f;
+                for (int z = 0; z < chunks; ++z, ++count) {
+                    const int from = count & 1;
+                    constexpr int LW = BN / 2 < 32 ? 16 : 32;
+                    mbar_wait(&acc_full[from], (count >> 1) & 1, s_abort, a.err);
+                    tc_fence_after();
+#pragma unroll
+                    for (int x = 0; x < BN / 2; x += LW) {
+                        uint32_t v[LW];
+                        tc_load(v, tmem + from * Shape::kCols + lanes + column(x));
+#pragma unroll
+                        for (int e = 0; e < LW; ++e) sum[x + e] += __uint_as_float(v[e]);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[from]), 0));
+                }
+            }
+            if constexpr (EPI == kEpiStore) {
+                constexpr int CMAX = 128 / (int)sizeof(T), CW = BN / 2 < CMAX ? BN / 2 : CMAX;   // columns of one staged box
+                constexpr int ROW = CW * (int)sizeof(T);
+                auto swz = [](uint32_t off) { return ROW == 128 ? swz128(off) : ROW == 64 ? swz64(off) : off; };
+                if constexpr (sizeof(T) == 2) {
+                    mbar_wait(&acc_full[buf], (count >> 1) & 1, s_abort, a.err);
+                    tc_fence_after();
+                }
+#pragma unroll
+                for (int c = 0; c < BN / 2; c += CW) {
+                    const int col0 = q.n * BN + half * (BN / 2) + c;
+                    unsigned char* box = buf_mem + (uses & 1) * 4096;
+                    store_wait_read<1>();
+                    __syncwarp();
+                    constexpr int LW = CW < 32 ? 16 : 32;
+#pragma unroll
+                    for (int x = 0; x < CW; x += LW) {
+                        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                            for (int e = x; e < x + LW; e += 4)
+                                *reinterpret_cast<float4*>(box + swz(lane * ROW + e * 4)) =
+                                    make_float4(sum[c + e], sum[c + e + 1], sum[c + e + 2], sum[c + e + 3]);
+                        } else {
+                            uint32_t v[LW];
+                            tc_load(v, acc + half * (BN / 2) + c + x);
+#pragma unroll
+                            for (int e = 0; e < LW; e += 8) {
+                                uint32_t o[4];
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) o[z] = pack2<T>(__uint_as_float(v[e + 2 * z]), __uint_as_float(v[e + 2 * z + 1]));
+                                *reinterpret_cast<uint4*>(box + swz(lane * ROW + (x + e) * 2)) = make_uint4(o[0], o[1], o[2], o[3]);
+                            }
+                        }
+                    }
+                    if (g.out >= 0) {
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0 && row0 < g.M && col0 < g.N) tma_store(&a.maps[g.out], box, col0, row0, q.p);
+                    } else {
+                        __syncwarp();
+                        T* out = static_cast<T*>(g.ptr) + (long long)q.p * g.rep;
+                        const int rows = min(32, g.M - row0);
+                        for (int r = 0; r < rows; ++r) {
+                            for (int x = lane; x < CW; x += 32) {
+                                if (col0 + x < g.N)
+                                    out[(long long)(row0 + r) * g.row + col0 + x] =
+                                        *reinterpret_cast<const T*>(box + swz(r * ROW + x * (int)sizeof(T)));
+                            }
+                        }
+                    }
+                    if (lane == 0) store_commit();
+                    ++uses;
+                }
+            } else if constexpr (EPI == kEpiGateUp) {
+                // columns [0, BN/2) of D are the gate's, [BN/2, BN) the other projection's
+                constexpr int HW = BN / 4, CW = HW < 32 ? HW : 32;
+                if constexpr (sizeof(T) == 2) {
+                    mbar_wait(&acc_full[buf], (count >> 1) & 1, s_abort, a.err);
+                    tc_fence_after();
+                }
+#pragma unroll
+                for (int c = 0; c < HW; c += CW) {
+                    const int col0 = q.n * (BN / 2) + half * HW + c;
+                    uint32_t gv[sizeof(T) == 2 ? CW : 1], uv[sizeof(T) == 2 ? CW : 1];
+                    if constexpr (sizeof(T) == 2) {
+                        tc_load(gv, acc + half * HW + c);
+                        tc_load(uv, acc + BN / 2 + half * HW + c);
+                    }
+                    store_wait_read<0>();
+                    __syncwarp();
+                    if constexpr (sizeof(T) == 4) {
+                        static_assert(CW == 32, "boxes of 32 columns");
+                        const float *gs = sum + c, *us = sum + HW + c;
+                        float x[32];
+                        const bool in = lane == 0 && row0 < g.M && col0 < g.N;
+                        if (a.map_g >= 0) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = gs[e];
+                            write_f32(buf_mem, lane, x);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = us[e];
+                            write_f32(buf_mem + 4096, lane, x);
+                            fence_async_shared();
+                            __syncwarp();
+                            if (in) {
+                                tma_store(&a.maps[a.map_g], buf_mem, col0, row0, q.p);
+                                tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                            }
+                            if (lane == 0) store_commit();
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[e] = act_value<T>(a.act, gs[e]) * us[e];
+                        store_wait_read<0>();
+                        __syncwarp();
+                        write_parts(buf_mem, lane, x);
+                        fence_async_shared();
+                        __syncwarp();
+                        if (in) {
+#pragma unroll
+                            for (int k = 0; k < kParts; ++k) tma_store(&a.maps[a.map_h + k], buf_mem + k * 2048, col0, row0, q.p);
+                        }
+                        if (lane == 0) store_commit();
+                        continue;
+                    } else {
+#pragma unroll
+                    for (int e = 0; e < CW; e += 8) {
+                        uint32_t og[4], ou[4], oh[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const float g0 = __uint_as_float(gv[e + 2 * z]), g1 = __uint_as_float(gv[e + 2 * z + 1]);
+                            const float u0 = __uint_as_float(uv[e + 2 * z]), u1 = __uint_as_float(uv[e + 2 * z + 1]);
+                            og[z] = pack2<T>(g0, g1);
+                            ou[z] = pack2<T>(u0, u1);
+                            oh[z] = pack2<T>(act_value<T>(a.act, g0) * u0, act_value<T>(a.act, g1) * u1);
+                        }
+                        uint32_t off = lane * (CW * 2) + e * 2;
+                        off = CW == 32 ? swz64(off) : off;
+                        *reinterpret_cast<uint4*>(buf_mem + off) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+                        if (a.map_g >= 0) {
+                            *reinterpret_cast<uint4*>(buf_mem + 2048 + off) = make_uint4(og[0], og[1], og[2], og[3]);
+                            *reinterpret_cast<uint4*>(buf_mem + 4096 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                        }
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0 && row0 < g.M && col0 < g.N) {
+                        tma_store(&a.maps[a.map_h], buf_mem, col0, row0, q.p);
+                        if (a.map_g >= 0) {
+                            tma_store(&a.maps[a.map_g], buf_mem + 2048, col0, row0, q.p);
+                            tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                        }
+                    }
+                    if (lane == 0) store_commit();
+                    }
+                }
+            } else if constexpr (sizeof(T) == 4) {
+                // D = dH in fp32.  G and U fill the staging memory; the parts of dG, then of dU take their place.
+                constexpr int BOXES = BN / 2 / 32;
+                uint64_t* bar = epi_full + 2 * w;
+#pragma unroll
+                for (int c = 0; c < BOXES; ++c, ++uses) {
+                    const int col0 = q.n * BN + half * (BN / 2) + c * 32;
+                    if (lane == 0) {
+                        store_wait_read<0>();
+                        op_mbar_expect(bar, 8192);
+                        tma_load(buf_mem, &a.maps[a.map_g], col0, row0, q.p, bar);
+                        tma_load(buf_mem + 4096, &a.maps[a.map_u], col0, row0, q.p, bar);
+                    }
+                    mbar_wait(bar, uses & 1, s_abort, a.err);
+                    float xg[32], xu[32];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const uint32_t off = swz128(lane * 128 + e * 4);
+                        const float4 g4 = *reinterpret_cast<const float4*>(buf_mem + off);
+                        const float4 u4 = *reinterpret_cast<const float4*>(buf_mem + 4096 + off);
+                        const float gf[4] = {g4.x, g4.y, g4.z, g4.w}, uf[4] = {u4.x, u4.y, u4.z, u4.w};
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const float dh = sum[c * 32 + e + z];
+                            float val, der;
+                            act_both<T>(a.act, gf[z], val, der);
+                            xg[e + z] = dh * uf[z] * der;
+                            xu[e + z] = dh * val;
+                        }
+                    }
+                    const bool in = lane == 0 && row0 < g.M && col0 < g.N;
+#pragma unroll
+                    for (int half_out = 0; half_out < 2; ++half_out) {
+                        if (half_out) store_wait_read<0>();
+                        __syncwarp();
+                        write_parts(buf_mem, lane, half_out ? xu : xg);
+                        fence_async_shared();
+                        __syncwarp();
+                        if (in) {
+#pragma unroll
+                            for (int k = 0; k < kParts; ++k)
+                                tma_store(&a.maps[(half_out ? a.map_du : a.map_dg) + k], buf_mem + k * 2048, col0, row0, q.p);
+                        }
+                        if (lane == 0) store_commit();
+                    }
+                }
+            } else {
+                // D = dH.  G and U come in through the two halves of the staging memory, one box of 32 columns
+                // ahead; dG and dU go out in their place.
+                constexpr int BOXES = BN / 2 / 32;
+                uint64_t* bars = epi_full + 2 * w;
+                auto fetch = [&](int c) {
+                    const int col = q.n * BN + half * (BN / 2) + c * 32, slot = (uses + c) & 1;
+                    if (lane == 0) {
+                        op_mbar_expect(&bars[slot], 4096);
+                        tma_load(buf_mem + slot * 4096, &a.maps[a.map_g], col, row0, q.p, &bars[slot]);
+                        tma_load(buf_mem + slot * 4096 + 2048, &a.maps[a.map_u], col, row0, q.p, &bars[slot]);
+                    }
+                };
+                if (lane == 0) store_wait_read<0>();
+                __syncwarp();
+                fetch(0);
+                mbar_wait(&acc_full[buf], (count >> 1) & 1, s_abort, a.err);
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < BOXES; ++c) {
+                    const int col0 = q.n * BN + half * (BN / 2) + c * 32, slot = (uses + c) & 1;
+                    if (c + 1 < BOXES) {
+                        if (lane == 0) store_wait_read<0>();
+                        __syncwarp();
+                        fetch(c + 1);
+                    }
+                    uint32_t v[32];
+                    tc_load(v, acc + half * (BN / 2) + c * 32);
+                    mbar_wait(&bars[slot], ((uses + c) >> 1) & 1, s_abort, a.err);
+                    unsigned char* bg = buf_mem + slot * 4096;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        const uint32_t off = swz64(lane * 64 + e * 2);
+                        const uint4 g4 = *reinterpret_cast<const uint4*>(bg + off), u4 = *reinterpret_cast<const uint4*>(bg + 2048 + off);
+                        const uint32_t gw[4] = {g4.x, g4.y, g4.z, g4.w}, uw[4] = {u4.x, u4.y, u4.z, u4.w};
+                        uint32_t og[4], ou[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const float2 gf = unpack2<T>(gw[z]), uf = unpack2<T>(uw[z]);
+                            const float h0 = __uint_as_float(v[e + 2 * z]), h1 = __uint_as_float(v[e + 2 * z + 1]);
+                            float a0, d0, a1, d1;
+                            act_both<T>(a.act, gf.x, a0, d0);
+                            act_both<T>(a.act, gf.y, a1, d1);
+                            og[z] = pack2<T>(h0 * uf.x * d0, h1 * uf.y * d1);
+                            ou[z] = pack2<T>(h0 * a0, h1 * a1);
+                        }
+                        *reinterpret_cast<uint4*>(bg + off) = make_uint4(og[0], og[1], og[2], og[3]);
+                        *reinterpret_cast<uint4*>(bg + 2048 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0 && row0 < g.M && col0 < g.N) {
+                        tma_store(&a.maps[a.map_dg], bg, col0, row0, q.p);
+                        tma_store(&a.maps[a.map_du], bg + 2048, col0, row0, q.p);
+                    }
+                    if (lane == 0) store_commit();
+                }
+                uses += BOXES;
+            }
+            if constexpr (sizeof(T) == 2) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[buf]), 0));
+                ++count;
+            }
+        }
+        if (lane == 0) store_wait_all();
+    }
+    if (*s_abort) {           // a wait ran out: copies and products in flight get a millisecond to end
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) {}
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Shape::kTmem) : "memory");
+}
+
+}  // namespace eg
