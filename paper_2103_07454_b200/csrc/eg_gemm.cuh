@@ -21,6 +21,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "eg_ops.cuh"
 
 namespace eg {
@@ -73,6 +75,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
+}
+// One thread of a converged warp.  The single-thread instructions (TMA, tcgen05.mma, commits) are issued
+// behind this test and not behind `lane == 0`: only here does the compiler know that one thread is active
+// and keeps their operands in uniform registers (measured: the four products of a stage 310 -> 58 cycles, a stage's copies 475 -> 250).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -187,30 +197,45 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn) {
 __device__ __forceinline__ uint32_t swz128(uint32_t off) { return off ^ ((off >> 3) & 0x70u); }
 __device__ __forceinline__ uint32_t swz64(uint32_t off) { return off ^ ((off >> 3) & 0x30u); }
 
-// act(g) and its derivative.  The fast exponential (error of a few 2^-23 of its argument) serves results that
-// are rounded to 16 bits.
+// act(g) and its derivative.  The hardware's exponential and reciprocal (errors of a few 2^-23) serve results
+// that are rounded to 16 bits; fp32 results take the library's.
+__device__ __forceinline__ float rcp_fast(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 template <typename T> __device__ __forceinline__ float exp_of(float x) {
     if constexpr (sizeof(T) == 4) return expf(x);
     else return __expf(x);
 }
-template <typename T> __device__ __forceinline__ float act_value(int act, float g) {
-    if (act == EG_ACT_SILU) return g / (1.f + exp_of<T>(-g));
-    if (act == EG_ACT_RELU) return fmaxf(g, 0.f);
-    return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+template <typename T> __device__ __forceinline__ float sigmoid_of(float x) {
+    if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-x));
+    else return rcp_fast(1.f + __expf(-x));
 }
-template <typename T> __device__ __forceinline__ void act_both(int act, float g, float& v, float& dv) {
-    if (act == EG_ACT_SILU) {
-        const float s = 1.f / (1.f + exp_of<T>(-g));
+template <typename T, int ACT> __device__ __forceinline__ float act_value(float g) {
+    if constexpr (ACT == EG_ACT_SILU) return g * sigmoid_of<T>(g);
+    else if constexpr (ACT == EG_ACT_RELU) return g > 0.f ? g : g != g ? g : 0.f;
+    else return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+}
+template <typename T, int ACT> __device__ __forceinline__ void act_both(float g, float& v, float& dv) {
+    if constexpr (ACT == EG_ACT_SILU) {
+        const float s = sigmoid_of<T>(g);
         v = g * s;
-        dv = s * (1.f + g * (1.f - s));
-    } else if (act == EG_ACT_RELU) {
-        v = fmaxf(g, 0.f);
+        dv = fmaf(v, 1.f - s, s);
+    } else if constexpr (ACT == EG_ACT_RELU) {
+        v = g > 0.f ? g : g != g ? g : 0.f;
         dv = g > 0.f ? 1.f : 0.f;
     } else {
         const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
         v = g * cdf;
-        dv = cdf + g * exp_of<T>(-0.5f * g * g) * 0.39894228040143268f;
+        dv = fmaf(g * exp_of<T>(-0.5f * g * g), 0.39894228040143268f, cdf);
     }
+}
+// The activation is chosen once per box of columns, not per element.
+template <typename F> __device__ __forceinline__ void with_act(int act, F&& f) {
+    if (act == EG_ACT_SILU) f(std::integral_constant<int, EG_ACT_SILU>{});
+    else if (act == EG_ACT_GELU) f(std::integral_constant<int, EG_ACT_GELU>{});
+    else f(std::integral_constant<int, EG_ACT_RELU>{});
 }
 
 // The three bf16 parts of two fp32 values, packed: each takes the 8 leading bits of what is left (exact).  A
@@ -315,7 +340,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0, round = 0;
             for (int t = pair; t < a.tiles; t += pairs) {
                 const TilePos q = tile_pos(a, t);
@@ -352,7 +377,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 mbar_wait(&empty[j % S], (j / S) & 1, s_abort, a.err);
         }
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
+        if (rank == 0 && elect_one()) {
             int s = 0, round = 0, count = 0;                 // count: accumulators handed over
             for (int t = pair; t < a.tiles; t += pairs) {
                 const TilePos q = tile_pos(a, t);
@@ -472,7 +497,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     if (g.out >= 0) {
                         fence_async_shared();
                         __syncwarp();
-                        if (lane == 0 && row0 < g.M && col0 < g.N) tma_store(&a.maps[g.out], box, col0, row0, q.p);
+                        if (elect_one()) {
+                            if (row0 < g.M && col0 < g.N) tma_store(&a.maps[g.out], box, col0, row0, q.p);
+                            store_commit();
+                        }
                     } else {
                         __syncwarp();
                         T* out = static_cast<T*>(g.ptr) + (long long)q.p * g.rep;
@@ -485,7 +513,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                             }
                         }
                     }
-                    if (lane == 0) store_commit();
                     ++uses;
                 }
             } else if constexpr (EPI == kEpiGateUp) {
@@ -509,7 +536,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         static_assert(CW == 32, "boxes of 32 columns");
                         const float *gs = sum + c, *us = sum + HW + c;
                         float x[32];
-                        const bool in = lane == 0 && row0 < g.M && col0 < g.N;
+                        const bool in = row0 < g.M && col0 < g.N;
                         if (a.map_g >= 0) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) x[e] = gs[e];
@@ -519,55 +546,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                             write_f32(buf_mem + 4096, lane, x);
                             fence_async_shared();
                             __syncwarp();
-                            if (in) {
-                                tma_store(&a.maps[a.map_g], buf_mem, col0, row0, q.p);
-                                tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                            if (elect_one()) {
+                                if (in) {
+                                    tma_store(&a.maps[a.map_g], buf_mem, col0, row0, q.p);
+                                    tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                                }
+                                store_commit();
                             }
-                            if (lane == 0) store_commit();
                         }
+                        with_act(a.act, [&](auto act) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = act_value<T>(a.act, gs[e]) * us[e];
+                            for (int e = 0; e < 32; ++e) x[e] = act_value<T, decltype(act)::value>(gs[e]) * us[e];
+                        });
                         store_wait_read<0>();
                         __syncwarp();
                         write_parts(buf_mem, lane, x);
                         fence_async_shared();
                         __syncwarp();
-                        if (in) {
+                        if (elect_one()) {
+                            if (in) {
 #pragma unroll
-                            for (int k = 0; k < kParts; ++k) tma_store(&a.maps[a.map_h + k], buf_mem + k * 2048, col0, row0, q.p);
+                                for (int k = 0; k < kParts; ++k) tma_store(&a.maps[a.map_h + k], buf_mem + k * 2048, col0, row0, q.p);
+                            }
+                            store_commit();
                         }
-                        if (lane == 0) store_commit();
-                        continue;
                     } else {
+                        with_act(a.act, [&](auto act) {
 #pragma unroll
-                    for (int e = 0; e < CW; e += 8) {
-                        uint32_t og[4], ou[4], oh[4];
+                            for (int e = 0; e < CW; e += 8) {
+                                uint32_t og[4], ou[4], oh[4];
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            const float g0 = __uint_as_float(gv[e + 2 * z]), g1 = __uint_as_float(gv[e + 2 * z + 1]);
-                            const float u0 = __uint_as_float(uv[e + 2 * z]), u1 = __uint_as_float(uv[e + 2 * z + 1]);
-                            og[z] = pack2<T>(g0, g1);
-                            ou[z] = pack2<T>(u0, u1);
-                            oh[z] = pack2<T>(act_value<T>(a.act, g0) * u0, act_value<T>(a.act, g1) * u1);
+                                for (int z = 0; z < 4; ++z) {
+                                    const float g0 = __uint_as_float(gv[e + 2 * z]), g1 = __uint_as_float(gv[e + 2 * z + 1]);
+                                    const float u0 = __uint_as_float(uv[e + 2 * z]), u1 = __uint_as_float(uv[e + 2 * z + 1]);
+                                    og[z] = pack2<T>(g0, g1);
+                                    ou[z] = pack2<T>(u0, u1);
+                                    oh[z] = pack2<T>(act_value<T, decltype(act)::value>(g0) * u0, act_value<T, decltype(act)::value>(g1) * u1);
+                                }
+                                uint32_t off = lane * (CW * 2) + e * 2;
+                                off = CW == 32 ? swz64(off) : off;
+                                *reinterpret_cast<uint4*>(buf_mem + off) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+                                if (a.map_g >= 0) {
+                                    *reinterpret_cast<uint4*>(buf_mem + 2048 + off) = make_uint4(og[0], og[1], og[2], og[3]);
+                                    *reinterpret_cast<uint4*>(buf_mem + 4096 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                                }
+                            }
+                        });
+                        fence_async_shared();
+                        __syncwarp();
+                        if (elect_one()) {
+                            if (row0 < g.M && col0 < g.N) {
+                                tma_store(&a.maps[a.map_h], buf_mem, col0, row0, q.p);
+                                if (a.map_g >= 0) {
+                                    tma_store(&a.maps[a.map_g], buf_mem + 2048, col0, row0, q.p);
+                                    tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                                }
+                            }
+                            store_commit();
                         }
-                        uint32_t off = lane * (CW * 2) + e * 2;
-                        off = CW == 32 ? swz64(off) : off;
-                        *reinterpret_cast<uint4*>(buf_mem + off) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-                        if (a.map_g >= 0) {
-                            *reinterpret_cast<uint4*>(buf_mem + 2048 + off) = make_uint4(og[0], og[1], og[2], og[3]);
-                            *reinterpret_cast<uint4*>(buf_mem + 4096 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
-                        }
-                    }
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0 && row0 < g.M && col0 < g.N) {
-                        tma_store(&a.maps[a.map_h], buf_mem, col0, row0, q.p);
-                        if (a.map_g >= 0) {
-                            tma_store(&a.maps[a.map_g], buf_mem + 2048, col0, row0, q.p);
-                            tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
-                        }
-                    }
-                    if (lane == 0) store_commit();
                     }
                 }
             } else if constexpr (sizeof(T) == 4) {
@@ -577,30 +613,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
 #pragma unroll
                 for (int c = 0; c < BOXES; ++c, ++uses) {
                     const int col0 = q.n * BN + half * (BN / 2) + c * 32;
-                    if (lane == 0) {
-                        store_wait_read<0>();
+                    store_wait_read<0>();
+                    __syncwarp();
+                    if (elect_one()) {
                         op_mbar_expect(bar, 8192);
                         tma_load(buf_mem, &a.maps[a.map_g], col0, row0, q.p, bar);
                         tma_load(buf_mem + 4096, &a.maps[a.map_u], col0, row0, q.p, bar);
                     }
                     mbar_wait(bar, uses & 1, s_abort, a.err);
                     float xg[32], xu[32];
+                    with_act(a.act, [&](auto act) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const uint32_t off = swz128(lane * 128 + e * 4);
-                        const float4 g4 = *reinterpret_cast<const float4*>(buf_mem + off);
-                        const float4 u4 = *reinterpret_cast<const float4*>(buf_mem + 4096 + off);
-                        const float gf[4] = {g4.x, g4.y, g4.z, g4.w}, uf[4] = {u4.x, u4.y, u4.z, u4.w};
+                        for (int e = 0; e < 32; e += 4) {
+                            const uint32_t off = swz128(lane * 128 + e * 4);
+                            const float4 g4 = *reinterpret_cast<const float4*>(buf_mem + off);
+                            const float4 u4 = *reinterpret_cast<const float4*>(buf_mem + 4096 + off);
+                            const float gf[4] = {g4.x, g4.y, g4.z, g4.w}, uf[4] = {u4.x, u4.y, u4.z, u4.w};
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            const float dh = sum[c * 32 + e + z];
-                            float val, der;
-                            act_both<T>(a.act, gf[z], val, der);
-                            xg[e + z] = dh * uf[z] * der;
-                            xu[e + z] = dh * val;
+                            for (int z = 0; z < 4; ++z) {
+                                const float dh = sum[c * 32 + e + z];
+                                float val, der;
+                                act_both<T, decltype(act)::value>(gf[z], val, der);
+                                xg[e + z] = dh * uf[z] * der;
+                                xu[e + z] = dh * val;
+                            }
                         }
-                    }
-                    const bool in = lane == 0 && row0 < g.M && col0 < g.N;
+                    });
+                    const bool in = row0 < g.M && col0 < g.N;
 #pragma unroll
                     for (int half_out = 0; half_out < 2; ++half_out) {
                         if (half_out) store_wait_read<0>();
@@ -608,12 +647,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         write_parts(buf_mem, lane, half_out ? xu : xg);
                         fence_async_shared();
                         __syncwarp();
-                        if (in) {
+                        if (elect_one()) {
+                            if (in) {
 #pragma unroll
-                            for (int k = 0; k < kParts; ++k)
-                                tma_store(&a.maps[(half_out ? a.map_du : a.map_dg) + k], buf_mem + k * 2048, col0, row0, q.p);
+                                for (int k = 0; k < kParts; ++k)
+                                    tma_store(&a.maps[(half_out ? a.map_du : a.map_dg) + k], buf_mem + k * 2048, col0, row0, q.p);
+                            }
+                            store_commit();
                         }
-                        if (lane == 0) store_commit();
                     }
                 }
             } else {
@@ -623,13 +664,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 uint64_t* bars = epi_full + 2 * w;
                 auto fetch = [&](int c) {
                     const int col = q.n * BN + half * (BN / 2) + c * 32, slot = (uses + c) & 1;
-                    if (lane == 0) {
+                    if (elect_one()) {
                         op_mbar_expect(&bars[slot], 4096);
                         tma_load(buf_mem + slot * 4096, &a.maps[a.map_g], col, row0, q.p, &bars[slot]);
                         tma_load(buf_mem + slot * 4096 + 2048, &a.maps[a.map_u], col, row0, q.p, &bars[slot]);
                     }
                 };
-                if (lane == 0) store_wait_read<0>();
+                store_wait_read<0>();
                 __syncwarp();
                 fetch(0);
                 mbar_wait(&acc_full[buf], (count >> 1) & 1, s_abort, a.err);
@@ -638,7 +679,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 for (int c = 0; c < BOXES; ++c) {
                     const int col0 = q.n * BN + half * (BN / 2) + c * 32, slot = (uses + c) & 1;
                     if (c + 1 < BOXES) {
-                        if (lane == 0) store_wait_read<0>();
+                        store_wait_read<0>();
                         __syncwarp();
                         fetch(c + 1);
                     }
@@ -646,32 +687,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     tc_load(v, acc + half * (BN / 2) + c * 32);
                     mbar_wait(&bars[slot], ((uses + c) >> 1) & 1, s_abort, a.err);
                     unsigned char* bg = buf_mem + slot * 4096;
+                    with_act(a.act, [&](auto act) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        const uint32_t off = swz64(lane * 64 + e * 2);
-                        const uint4 g4 = *reinterpret_cast<const uint4*>(bg + off), u4 = *reinterpret_cast<const uint4*>(bg + 2048 + off);
-                        const uint32_t gw[4] = {g4.x, g4.y, g4.z, g4.w}, uw[4] = {u4.x, u4.y, u4.z, u4.w};
-                        uint32_t og[4], ou[4];
+                        for (int e = 0; e < 32; e += 8) {
+                            const uint32_t off = swz64(lane * 64 + e * 2);
+                            const uint4 g4 = *reinterpret_cast<const uint4*>(bg + off), u4 = *reinterpret_cast<const uint4*>(bg + 2048 + off);
+                            const uint32_t gw[4] = {g4.x, g4.y, g4.z, g4.w}, uw[4] = {u4.x, u4.y, u4.z, u4.w};
+                            uint32_t og[4], ou[4];
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            const float2 gf = unpack2<T>(gw[z]), uf = unpack2<T>(uw[z]);
-                            const float h0 = __uint_as_float(v[e + 2 * z]), h1 = __uint_as_float(v[e + 2 * z + 1]);
-                            float a0, d0, a1, d1;
-                            act_both<T>(a.act, gf.x, a0, d0);
-                            act_both<T>(a.act, gf.y, a1, d1);
-                            og[z] = pack2<T>(h0 * uf.x * d0, h1 * uf.y * d1);
-                            ou[z] = pack2<T>(h0 * a0, h1 * a1);
+                            for (int z = 0; z < 4; ++z) {
+                                const float2 gf = unpack2<T>(gw[z]), uf = unpack2<T>(uw[z]);
+                                const float h0 = __uint_as_float(v[e + 2 * z]), h1 = __uint_as_float(v[e + 2 * z + 1]);
+                                float a0, d0, a1, d1;
+                                act_both<T, decltype(act)::value>(gf.x, a0, d0);
+                                act_both<T, decltype(act)::value>(gf.y, a1, d1);
+                                og[z] = pack2<T>(h0 * uf.x * d0, h1 * uf.y * d1);
+                                ou[z] = pack2<T>(h0 * a0, h1 * a1);
+                            }
+                            *reinterpret_cast<uint4*>(bg + off) = make_uint4(og[0], og[1], og[2], og[3]);
+                            *reinterpret_cast<uint4*>(bg + 2048 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
                         }
-                        *reinterpret_cast<uint4*>(bg + off) = make_uint4(og[0], og[1], og[2], og[3]);
-                        *reinterpret_cast<uint4*>(bg + 2048 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
-                    }
+                    });
                     fence_async_shared();
                     __syncwarp();
-                    if (lane == 0 && row0 < g.M && col0 < g.N) {
-                        tma_store(&a.maps[a.map_dg], bg, col0, row0, q.p);
-                        tma_store(&a.maps[a.map_du], bg + 2048, col0, row0, q.p);
+                    if (elect_one()) {
+                        if (row0 < g.M && col0 < g.N) {
+                            tma_store(&a.maps[a.map_dg], bg, col0, row0, q.p);
+                            tma_store(&a.maps[a.map_du], bg + 2048, col0, row0, q.p);
+                        }
+                        store_commit();
                     }
-                    if (lane == 0) store_commit();
                 }
                 uses += BOXES;
             }
@@ -682,7 +727,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 ++count;
             }
         }
-        if (lane == 0) store_wait_all();
+        store_wait_all();
     }
     if (*s_abort) {           // a wait ran out: copies and products in flight get a millisecond to end
         const long long t0 = clock64();
