@@ -152,6 +152,28 @@ __device__ __forceinline__ bool op_mbar_wait(uint64_t* bar, uint32_t parity, vol
     }
     return true;
 }
+// The same for a barrier that the other CTA of a cluster arrives on.
+__device__ __forceinline__ bool op_mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err) {
+    const long long t0 = clock64();
+    for (unsigned spins = 1;; ++spins) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(op_smem(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if ((spins & 63u) != 0) continue;
+        if (*s_abort) return false;
+        if (clock64() - t0 > kOpWaitCycles) {
+            *s_abort = 1;
+            atomicOr(err, kOpErrWaitTimeout);
+            return false;
+        }
+    }
+}
 // 1-D bulk copy global -> shared; both addresses and the size multiples of 16 bytes.
 __device__ __forceinline__ void op_bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(op_smem(dst)),

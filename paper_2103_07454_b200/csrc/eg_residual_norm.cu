@@ -13,15 +13,25 @@
 // Bound by memory: the forward call moves four rows per token, the backward call six.  Both keep a
 // row on chip between its one load and its stores; the backward call recomputes r' from y and r
 // (12 instead of 14 bytes per element in 16-bit types, and nothing is saved by the forward call).
+//
+// k_norm_stream does both for many rows: one CTA (cluster) per multiprocessor (group of them), rows
+// streamed through shared memory by bulk copies well ahead of their use, everything else in
+// registers.  k_norm_few does the forward pass where there are few rows and a row's way through
+// shared memory would only add to its latency.
+#include <type_traits>
+
 #include "eg_ops.cuh"
 
 namespace eg {
 namespace {
 
 constexpr int kMaxWidth = EG_NORM_MAX_WIDTH;
-constexpr int kFwdThreads = 256;
-constexpr int kBwdThreads = 512;          // consumer threads of the backward kernel at most
-constexpr int kBwdMaxCtas = 160;          // one per multiprocessor; bounds the workspace
+constexpr int kFewThreads = 256;
+constexpr int kThreads = 256;             // of a streaming CTA (a ninth warp would cost each thread a third of its registers)
+constexpr int kElems = 16;                // elements of a row per thread
+constexpr int kCtaWidth = kThreads * kElems;   // columns of one CTA; wider rows are shared by a cluster
+constexpr int kMaxCtas = 160;             // one per multiprocessor; bounds the workspace
+constexpr int kMaxStages = 4;
 constexpr int kSmemMax = 227 * 1024;
 
 struct Mat {
@@ -38,7 +48,8 @@ struct NormArgs {
     Mat w_post, gate, scale, w_pre, r_out, o, dy, dr;
     float* partials;
     unsigned int* err;
-    int stages, group_rows, slot_bytes;   // backward: ring of shared-memory stages
+    // k_norm_stream: threads of a row in one CTA, CTAs of a row, columns of one CTA, shared-memory stages
+    int tpr, teams, ctas, cols, stages, slot_bytes;
 };
 
 __device__ __forceinline__ float sigmoid_f(float g) { return 1.f / (1.f + expf(-g)); }
@@ -47,43 +58,16 @@ template <typename T> __device__ __forceinline__ T* row_of(const Mat& m, int i, 
     return static_cast<T*>(m.p) + (long long)i * m.rep + t * m.row;
 }
 
-// Sums K values over the TPR threads of a group; every thread gets the result.  Groups wider than a
-// warp meet at the named barrier 1 + group; `red` (this group's slots, one per warp, K values padded
-// to a multiple of 4) must not be the one of the previous call.
-template <int K>
-__device__ __forceinline__ void group_sum(float (&v)[K], int tpr, int t, int group, float* red) {
-    const int width = tpr < 32 ? tpr : 32;
-    for (int o = width >> 1; o > 0; o >>= 1) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-    }
-    if (tpr <= 32) return;
-    constexpr int KP = (K + 3) & ~3;
-    const int warps = tpr >> 5;
-    if ((t & 31) == 0) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) red[(t >> 5) * KP + k] = v[k];
-    }
+// Sum over the tpr threads of a group, valid in all of them.  Groups wider than a warp meet at the named
+// barrier 1 + group; `red` (one float per warp of the group) must not be the one of the previous call.
+__device__ __forceinline__ float group_sum(float v, int tpr, int t, int group, float* red) {
+    for (int o = (tpr < 32 ? tpr : 32) >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (tpr <= 32) return v;
+    if ((t & 31) == 0) red[t >> 5] = v;
     op_named_barrier(1 + group, tpr);
-    if (K == 1) {
-        // padded to four floats per warp only so that both forms share one buffer size
-        float s = 0.f;
-        for (int w = 0; w < warps; ++w) s += red[w * KP];
-        v[0] = s;
-    } else {
-        float s[KP];
-#pragma unroll
-        for (int k = 0; k < KP; ++k) s[k] = 0.f;
-        for (int w = 0; w < warps; ++w) {
-#pragma unroll
-            for (int q = 0; q < KP; q += 4) {
-                const float4 a = *reinterpret_cast<const float4*>(red + w * KP + q);
-                s[q] += a.x; s[q + 1] += a.y; s[q + 2] += a.z; s[q + 3] += a.w;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] = s[k];
-    }
+    float s = 0.f;
+    for (int w = 0; w < tpr >> 5; ++w) s += red[w];
+    return s;
 }
 
 // Threads that share a row of width d with E elements each: a power of two below a warp, whole
@@ -95,13 +79,13 @@ inline int threads_per_row(int d, int E) {
     return (need + 31) / 32 * 32;
 }
 
-// ----------------------------------------------------------------------------------- forward
+// ----------------------------------------------------------------------------------- few rows
 // A CTA holds blockDim / tpr groups; each takes one row at a time of the CTA's run of rows.
 // E elements per thread: vector v of the row's VEC-element vectors v * tpr + t.
 template <typename T, int VEC, int E>
-__global__ void __launch_bounds__(512) k_norm_forward(const __grid_constant__ NormArgs a, int tpr, long long rows_per_cta) {
+__global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormArgs a, int tpr, long long rows_per_cta) {
     constexpr int NV = E / VEC;
-    __shared__ float4 s_red[2][16];
+    __shared__ float s_red[2][16];
     const int group = threadIdx.x / tpr, t = threadIdx.x % tpr, groups = blockDim.x / tpr;
     const long long W = (long long)a.P * a.rows;
     const long long u0 = blockIdx.x * rows_per_cta, u1 = min(W, u0 + rows_per_cta);
@@ -111,14 +95,13 @@ __global__ void __launch_bounds__(512) k_norm_forward(const __grid_constant__ No
     long long row = u % a.rows;
     int have = -1;                                   // replica whose factors are held
     float fa[E], fs[E];
-    float* red0 = reinterpret_cast<float*>(s_red[0] + (group * tpr >> 5));
-    float* red1 = reinterpret_cast<float*>(s_red[1] + (group * tpr >> 5));
+    float *red0 = s_red[0] + (group * tpr >> 5), *red1 = s_red[1] + (group * tpr >> 5);
     // every group makes the same number of turns: the groups of a warp shuffle together
     for (long long base = u0; base < u1; base += groups, u += groups, row += groups) {
         while (row >= a.rows) { row -= a.rows; ++i; }
         const bool active = u < u1 && group < groups;
         float y[E], r[E];
-        float sum[1] = {0.f};
+        float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * tpr + t) * VEC;
@@ -149,11 +132,10 @@ __global__ void __launch_bounds__(512) k_norm_forward(const __grid_constant__ No
         float inv1 = 1.f;
         if (post && has_y) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[0] = fmaf(y[e], y[e], sum[0]);
-            group_sum<1>(sum, tpr, t, group, red0);
-            inv1 = __frsqrt_rn(fmaf(sum[0], a.inv_d, a.eps));
+            for (int e = 0; e < E; ++e) sum = fmaf(y[e], y[e], sum);
+            inv1 = __frsqrt_rn(fmaf(group_sum(sum, tpr, t, group, red0), a.inv_d, a.eps));
         }
-        sum[0] = 0.f;
+        sum = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float sr = fs[e] * r[e];
@@ -170,9 +152,8 @@ __global__ void __launch_bounds__(512) k_norm_forward(const __grid_constant__ No
         }
         if (!pre) continue;
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[0] = fmaf(r[e], r[e], sum[0]);
-        group_sum<1>(sum, tpr, t, group, red1);
-        const float inv2 = __frsqrt_rn(fmaf(sum[0], a.inv_d, a.eps));
+        for (int e = 0; e < E; ++e) sum = fmaf(r[e], r[e], sum);
+        const float inv2 = __frsqrt_rn(fmaf(group_sum(sum, tpr, t, group, red1), a.inv_d, a.eps));
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * tpr + t) * VEC;
@@ -186,234 +167,504 @@ __global__ void __launch_bounds__(512) k_norm_forward(const __grid_constant__ No
     }
 }
 
-// ----------------------------------------------------------------------------------- backward
-// First of the W rows (replica after replica) that CTA b of G works on.
+// ----------------------------------------------------------------------------------- many rows
+// First of the W rows (replica after replica) that CTA (cluster) b of G works on.
 __host__ __device__ __forceinline__ long long cut(long long W, int b, int G) { return W * b / G; }
 
-// One CTA per multiprocessor.  The producer warp streams rows of y, r, d_r', d_o through a ring of
-// shared-memory stages (bulk copies); a stage holds one row for each group of consumer threads.
-// Unaligned rows are copied from the 16-byte boundary below them and read from the remainder.
-// A thread owns the same columns of every row: its three column sums stay in registers until the
-// replica changes, are then added up over the groups in shared memory (in the place of the factors
-// a, scale, w_pre, which the next replica reloads) and left as one partial sum per (replica, CTA)
-// pair that meet; along the walk i + b numbers these pairs without a gap.
-template <typename T, int VEC, int E>
-__global__ void __launch_bounds__(kBwdThreads + 32, 1) k_norm_backward(const __grid_constant__ NormArgs a, int tpr) {
-    constexpr int NV = E / VEC;
+// The rows of a CTA, step by step: up to `per` consecutive rows of one replica.
+struct Walk {
+    long long row, end, left;          // first row of the step and end of the CTA's rows in replica i; rows after that
+    long long rows;
+    int i, per;
+
+    __device__ __forceinline__ void start(long long u0, long long u1, long long n, int rows_a_step) {
+        rows = n;
+        per = rows_a_step;
+        i = (int)(u0 / n);
+        row = u0 - (long long)i * n;
+        end = min(n, row + (u1 - u0));
+        left = u1 - u0 - (end - row);
+    }
+    __device__ __forceinline__ bool done() const { return row >= end; }
+    __device__ __forceinline__ int count() const { return (int)min((long long)per, end - row); }
+    // true: the next step is in another replica (or there is none)
+    __device__ __forceinline__ bool next() {
+        row += per;
+        if (row < end) return false;
+        ++i;
+        row = 0;
+        end = min(rows, left);
+        left -= end;
+        return true;
+    }
+};
+
+// A thread's elements of one row, as they are stored (16-bit types: two to a register).
+template <typename T> struct Raw {
+    static constexpr int N = kElems * (int)sizeof(T) / 4;
+    uint32_t w[N];
+    __device__ __forceinline__ float2 pair(int p) const {
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
+        else return unpack2<T>(w[p]);
+    }
+    // Makes the compiler unpack again after this point instead of carrying unpacked values in registers.
+    __device__ __forceinline__ void repack() {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) asm volatile("" : "+r"(w[q]));
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int q = 0; q < N; ++q) w[q] = 0;
+    }
+    // vector v of VEC elements is number v * tpr + t of the row; `d` columns
+    template <int VEC> __device__ __forceinline__ void load(const T* p, int tpr, int t, int d) {
+        if constexpr (VEC > 1) {
+#pragma unroll
+            for (int v = 0; v < kElems / VEC; ++v) {
+                const int c = (v * tpr + t) * VEC;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (c < d) x = *reinterpret_cast<const uint4*>(p + c);
+                w[4 * v] = x.x; w[4 * v + 1] = x.y; w[4 * v + 2] = x.z; w[4 * v + 3] = x.w;
+            }
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < kElems; ++e) {
+                const int c = e * tpr + t;
+                w[e] = c < d ? __float_as_uint(p[c]) : 0u;
+            }
+        } else {
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+            for (int e = 0; e < kElems; e += 2) {
+                const int c0 = e * tpr + t, c1 = c0 + tpr;
+                w[e / 2] = (c0 < d ? (uint32_t)h[c0] : 0u) | (c1 < d ? (uint32_t)h[c1] << 16 : 0u);
+            }
+        }
+    }
+    template <int VEC> __device__ __forceinline__ void store(T* p, int tpr, int t, int d) const {
+        if constexpr (VEC > 1) {
+#pragma unroll
+            for (int v = 0; v < kElems / VEC; ++v) {
+                const int c = (v * tpr + t) * VEC;
+                if (c < d) *reinterpret_cast<uint4*>(p + c) = make_uint4(w[4 * v], w[4 * v + 1], w[4 * v + 2], w[4 * v + 3]);
+            }
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < kElems; ++e) {
+                const int c = e * tpr + t;
+                if (c < d) p[c] = __uint_as_float(w[e]);
+            }
+        } else {
+            uint16_t* h = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+            for (int e = 0; e < kElems; e += 2) {
+                const int c0 = e * tpr + t, c1 = c0 + tpr;
+                if (c0 < d) h[c0] = (uint16_t)w[e / 2];
+                if (c1 < d) h[c1] = (uint16_t)(w[e / 2] >> 16);
+            }
+        }
+    }
+    __device__ __forceinline__ void set(int p, float a, float b) {
+        if constexpr (sizeof(T) == 4) { w[2 * p] = __float_as_uint(a); w[2 * p + 1] = __float_as_uint(b); }
+        else w[p] = pack2<T>(a, b);
+    }
+};
+
+// K values (a power of two) summed over the lanes of a warp (`width` lanes, a power of two, K <= width): halves
+// are exchanged, so that every step halves the values instead of repeating all of them (16 values: 16
+// shuffles, not 80).  Lane l ends up with the sum over its group of value number held(l).
+template <int K> __device__ __forceinline__ float warp_sums(float (&v)[K], int lane, int width) {
+    int bit = 1;
+#pragma unroll
+    for (int half = K / 2; half > 0; half >>= 1, bit <<= 1) {
+#pragma unroll
+        for (int k = 0; k < half; ++k) {
+            const float give = lane & bit ? v[k] : v[k + half], keep = lane & bit ? v[k + half] : v[k];
+            v[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+        }
+    }
+    for (; bit < width; bit <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], bit);
+    return v[0];
+}
+// Value that lane l holds; it is its own inverse, so also the lane (of the first K) that holds value k.
+template <int K> __device__ __forceinline__ int held(int l) {
+    int r = 0;
+#pragma unroll
+    for (int b = 1, h = K / 2; h > 0; b <<= 1, h >>= 1) r |= l & b ? h : 0;
+    return r;
+}
+__host__ __device__ constexpr int ceil_pow2(int k) { return k <= 1 ? 1 : 2 * ceil_pow2((k + 1) / 2); }
+
+// A CTA works through its rows in steps of up to teams * ROWS * (rows of a warp) consecutive rows of one
+// replica.  The rows of y, r (and d_r', d_o) of the steps ahead come into a ring of stages in
+// shared memory, one bulk copy an array and step where the rows lie one after the other; rows off the
+// 16-byte boundaries are copied from the boundary below and read from the remainder.  A team is the tpr
+// threads of a row, or a warp with 32 / tpr rows below a warp; it takes ROWS rows at a time, so that the
+// latencies of one row's sums are covered by the other's arithmetic (one row in fp32, whose rows are twice as
+// long to move).  A thread owns the same columns of every row, so the factors a, scale, w_pre of the replica and
+// (backward) its three column sums stay in registers; at the end of a replica's rows the teams add up their
+// sums in shared memory and leave one partial sum per (replica, CTA) pair that meet; i + b numbers the pairs
+// without a gap.  Rows wider than kCtaWidth are shared by a cluster of two CTAs, which exchange the sums of a row.
+template <typename T, int VEC, bool BWD>
+__global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_constant__ NormArgs a) {
+    constexpr int E = kElems, ROWS = sizeof(T) == 2 ? 2 : 1, ARRAYS = BWD ? 4 : 2;
+    constexpr int K1 = ROWS, K2 = ceil_pow2((BWD ? 5 : 1) * ROWS);
+    constexpr int kWarps = kThreads / 32;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(8) uint64_t s_full[4], s_empty[4];
-    __shared__ float4 s_red[2][2 * (kBwdThreads / 32)];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_peer[2];
+    __shared__ float s_red[2][2 * kWarps][16];                 // [parity][CTA of the cluster, warp][value]
     __shared__ volatile int s_abort;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int R = a.group_rows, S = a.stages, d = a.d;
-    const int nc = (R * tpr + 31) & ~31;            // consumer threads
-    float* fac = reinterpret_cast<float*>(smem);    // [3][d]: a, scale, w_pre; later the column sums
-    unsigned char* ring = smem + ((3 * d * (int)sizeof(float) + 127) & ~127);
-    const int array_bytes = R * a.slot_bytes, stage_bytes = 4 * array_bytes;
-    const long long W = (long long)a.P * a.rows;
-    const int b = blockIdx.x, G = gridDim.x;
-    const long long u0 = cut(W, b, G), u1 = cut(W, b + 1, G);
+    if (BWD) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tpr = a.tpr, S = a.stages, C = a.ctas, teams = a.teams;
+    const int team_threads = tpr < 32 ? 32 : tpr, each = tpr < 32 ? 32 / tpr : 1;
+    const int nc = teams * team_threads;                       // consumer threads
+    const int rank = C > 1 ? blockIdx.x % C : 0, b = blockIdx.x / C, G = gridDim.x / C;
+    const int c0 = rank * a.cols, d = min(a.cols, a.d - c0);   // columns of this CTA
+    const bool post = a.w_post.p != nullptr && a.in[0].p != nullptr;
+    const long long W = (long long)a.P * a.rows, u0 = cut(W, b, G), u1 = cut(W, b + 1, G);
+    const int per = teams * ROWS * each;
+    const int array_bytes = per * a.slot_bytes, stage_bytes = ARRAYS * array_bytes;
+    float* s_sums = reinterpret_cast<float*>(smem);            // [3][d] where teams meet (BWD, teams > 1)
+    unsigned char* ring = smem + (BWD && teams > 1 ? (3 * a.cols * 4 + 127) & ~127 : 0);
+    const int lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         s_abort = 0;
+        int present = 0;
+        for (int q = 0; q < ARRAYS; ++q) present += a.in[q].p != nullptr;
         for (int s = 0; s < S; ++s) {
-            op_mbar_init(&s_full[s], 32);
+            op_mbar_init(&s_full[s], present);
             op_mbar_init(&s_empty[s], nc / 32);
         }
+        for (int q = 0; q < 2; ++q) op_mbar_init(&s_peer[q], 2 * nc / 32);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    Walk w;
+    w.start(u0, u1, a.rows, per);
 
-    if (threadIdx.x >= nc) {
-        // ------------------------------------------------------------------ producer warp
-        if (warp != nc / 32) return;
-        int s = 0, round = 0;
-        bool ok = true;
-        for (long long u = u0; u < u1 && ok;) {
-            const int i = (int)(u / a.rows);
-            const long long end = min(u1, (long long)(i + 1) * a.rows);
-            for (; u < end; u += R) {
-                const int n = (int)min((long long)R, end - u);
-                ok = round == 0 || op_mbar_wait(&s_empty[s], (round - 1) & 1, &s_abort, a.err);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                unsigned char* stage = ring + s * stage_bytes;
+    // the rows of array q come in by lane 0 of warp q (few warps: of the last one, q after q)
+    Walk ahead = w;
+    const int fetcher = threadIdx.x >> 5;
+    int as = 0, around = 0;
+    auto fetch = [&]() {
+        if (ahead.done()) return;
+        if (lane == 0 && fetcher < ARRAYS) {
+            for (int q = fetcher; q < ARRAYS; q += nc / 32) {
+                const Mat& m = a.in[q];
+                if (!m.p) continue;
+                const bool together = m.row == a.d && C == 1;      // rows one after the other
+                const int n = ahead.count();
+                if (around > 0 && !op_mbar_wait(&s_empty[as], (around - 1) & 1, &s_abort, a.err)) break;
+                unsigned char* dst = ring + as * stage_bytes + q * array_bytes;
+                const uintptr_t p = (uintptr_t)(row_of<T>(m, ahead.i, ahead.row) + c0);
+                if (VEC > 1 && together) {
+                    const uint32_t bytes = (uint32_t)(d * sizeof(T)) * n;
+                    op_mbar_expect(&s_full[as], bytes);
+                    op_bulk_load(dst, (const void*)p, bytes, &s_full[as]);
+                    continue;
+                }
+                const int copies = together ? 1 : n;
+                const uint32_t len = (uint32_t)(d * sizeof(T)) * (together ? n : 1);
+                const uintptr_t step = (uintptr_t)m.row * sizeof(T);
                 uint32_t bytes = 0;
-                for (int q = lane; q < 4 * n; q += 32) {
-                    const Mat& m = a.in[q / n];
-                    if (!m.p) continue;
-                    const uintptr_t p = (uintptr_t)row_of<T>(m, i, u - (long long)i * a.rows + q % n);
-                    bytes += (uint32_t)(((p + (uintptr_t)d * sizeof(T) + 15) & ~(uintptr_t)15) - (p & ~(uintptr_t)15));
+                for (int z = 0; z < copies; ++z)
+                    bytes += (uint32_t)(((p + z * step + len + 15) & ~(uintptr_t)15) - ((p + z * step) & ~(uintptr_t)15));
+                op_mbar_expect(&s_full[as], bytes);
+                for (int z = 0; z < copies; ++z) {
+                    const uintptr_t x = p + z * step, from = x & ~(uintptr_t)15;
+                    op_bulk_load(dst + z * a.slot_bytes, (const void*)from, (uint32_t)(((x + len + 15) & ~(uintptr_t)15) - from), &s_full[as]);
                 }
-                op_mbar_expect(&s_full[s], bytes);
-                for (int q = lane; q < 4 * n; q += 32) {
-                    const int k = q / n, g = q % n;
-                    const Mat& m = a.in[k];
-                    if (!m.p) continue;
-                    const uintptr_t p = (uintptr_t)row_of<T>(m, i, u - (long long)i * a.rows + g);
-                    const uintptr_t from = p & ~(uintptr_t)15;
-                    op_bulk_load(stage + k * array_bytes + g * a.slot_bytes, (const void*)from,
-                                 (uint32_t)(((p + (uintptr_t)d * sizeof(T) + 15) & ~(uintptr_t)15) - from), &s_full[s]);
-                }
-                if (++s == S) { s = 0; ++round; }
-            }
-            u = end;
-        }
-        if (!ok) {      // a wait ran out: let the copies in flight land (with a limit) before the memory is given back
-            for (int q = 0; q < S; ++q) {
-                const int uses = round + (q < s ? 1 : 0);       // of stage q so far
-                for (int tries = 0; uses > 0 && tries < 2000 && !op_mbar_test(&s_full[q], (uses - 1) & 1); ++tries) {}
             }
         }
-        return;
-    }
+        __syncwarp();
+        ahead.next();
+        if (++as == S) { as = 0; ++around; }
+    };
+    // a stage is refilled one step after its last use, when no other team should still be reading it
+    for (int q = 0; q < S - 1; ++q) fetch();
+    if (S == 1) fetch();
+    {
+        const int team = threadIdx.x / team_threads, tt = threadIdx.x % team_threads;
+        const int warps = team_threads >> 5, warp = tt >> 5;
+        const int sub = tpr < 32 ? lane / tpr : 0, t = tpr < 32 ? lane % tpr : tt;
+        int parity = 0, meets = 0;
+        // `used` of KP values of the team's rows, summed over their threads (and CTAs): v[k] in every thread
+        auto row_sums = [&](auto& v, int used) {
+            constexpr int KP = sizeof(v) / sizeof(float);
+            const int width = tpr < 32 ? tpr : 32;
+            float sum = warp_sums<KP>(v, lane, width);
+            const int first = lane & ~(width - 1);
+            if (tpr <= 32 && C == 1) {
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+                    if (k < used) v[k] = __shfl_sync(0xffffffffu, sum, first + held<KP>(k));
+                return;
+            }
+            if (lane < KP) {
+                float* to = &s_red[parity][rank * kWarps + team * warps + warp][held<KP>(lane)];
+                *to = sum;
+                if (C > 1) {
+                    uint32_t other;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(other) : "r"(op_smem(to)), "r"(rank ^ 1));
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(other), "f"(sum) : "memory");
+                }
+            }
+            if (C > 1) {
+                // every consumer warp of both CTAs tells both CTAs that its sums are there
+                __syncwarp();
+                if (lane < 2) {
+                    uint32_t bar;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(op_smem(&s_peer[parity])), "r"(lane));
+                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+                }
+                (void)op_mbar_wait_cluster(&s_peer[parity], meets >> 1 & 1, &s_abort, a.err);
+                ++meets;
+            } else {
+                op_named_barrier(1 + team, team_threads);
+            }
+            // lane l adds value l % KP of every (32 / KP)-th warp
+            constexpr int L = 32 / KP;
+            const int from = C > 1 ? 0 : team * warps, count = C > 1 ? kWarps + warps : warps;
+            sum = 0.f;
+            for (int x = lane / KP; x < count; x += L)
+                if (C == 1 || x % kWarps < warps) sum += s_red[parity][from + x][lane % KP];
+#pragma unroll
+            for (int o = KP; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+#pragma unroll
+            for (int k = 0; k < KP; ++k)
+                if (k < used) v[k] = __shfl_sync(0xffffffffu, sum, k);
+            parity ^= 1;
+        };
 
-    // ---------------------------------------------------------------------- consumers
-    const int group = threadIdx.x / tpr, t = threadIdx.x % tpr;
-    const bool post = a.w_post.p != nullptr && a.in[0].p != nullptr, has_y = a.in[0].p != nullptr;
-    const bool has_dr = a.in[2].p != nullptr, has_do = a.in[3].p != nullptr;
-    float* red0 = reinterpret_cast<float*>(&s_red[0][0]) + (group * tpr >> 5) * 8;
-    float* red1 = reinterpret_cast<float*>(&s_red[1][0]) + (group * tpr >> 5) * 8;
-    float accC[E], accD[E], accW[E];
-    int s = 0, round = 0;
-    for (long long u = u0; u < u1;) {
-        const int i = (int)(u / a.rows);
-        const long long end = min(u1, (long long)(i + 1) * a.rows);
-        op_named_barrier(15, nc);                    // the sums of the previous replica are written
-        for (int c = threadIdx.x; c < d; c += nc) {
-            float fa = has_y ? 1.f : 0.f;
-            if (a.w_post.p) fa *= to_f32(row_of<T>(a.w_post, i, 0)[c]);
-            if (a.gate.p) fa *= sigmoid_f(to_f32(row_of<T>(a.gate, i, 0)[c]));
-            fac[c] = fa;
-            fac[d + c] = a.scale.p ? to_f32(row_of<T>(a.scale, i, 0)[c]) : 1.f;
-            fac[2 * d + c] = has_do ? to_f32(row_of<T>(a.w_pre, i, 0)[c]) : 0.f;
-        }
-        op_named_barrier(15, nc);
+        int s = 0, round = 0;
+        while (!w.done()) {
+            const int i = w.i;
+            Raw<T> fs, fw;
+            float fa[E];
+            float accC[BWD ? E : 1], accD[BWD ? E : 1], accW[BWD ? E : 1];
+            {
+                Raw<T> x;
+                if (a.w_post.p) x.template load<VEC>(row_of<T>(a.w_post, i, 0) + c0, tpr, t, d);
 #pragma unroll
-        for (int e = 0; e < E; ++e) accC[e] = accD[e] = accW[e] = 0.f;
-        for (; u < end; u += R) {
-            const int n = (int)min((long long)R, end - u);
-            // after a time-out the walk goes on without waiting, so that no barrier is missed
-            (void)op_mbar_wait(&s_full[s], round & 1, &s_abort, a.err);
-            const bool active = group < n;
-            const long long row = u - (long long)i * a.rows + group;
-            const unsigned char* stage = ring + s * stage_bytes + group * a.slot_bytes;
-            const T* in[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uintptr_t p = active && a.in[k].p ? (uintptr_t)row_of<T>(a.in[k], i, row) : 0;
-                in[k] = reinterpret_cast<const T*>(stage + k * array_bytes + (p & 15));
-            }
-            float one[1] = {0.f};
-            float inv1 = 1.f;
-            if (post) {
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    const int c = (v * tpr + t) * VEC;
-                    float y[VEC];
-                    if (active && c < d) {
-                        load_vec<T, VEC>(in[0] + c, y);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) one[0] = fmaf(y[e], y[e], one[0]);
-                    }
+                for (int p = 0; p < E / 2; ++p) {
+                    const float2 f = a.w_post.p ? x.pair(p) : make_float2(1.f, 1.f);
+                    fa[2 * p] = a.in[0].p ? f.x : 0.f;
+                    fa[2 * p + 1] = a.in[0].p ? f.y : 0.f;
                 }
-                group_sum<1>(one, tpr, t, group, red0);
-                inv1 = __frsqrt_rn(fmaf(one[0], a.inv_d, a.eps));
-            }
-            // sums of rn^2, dn*rn, a*yh*d_r, a*yh*dn, a*yh*rn: c3 and c4 follow from them
-            float five[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+                if (a.gate.p) {
+                    x.template load<VEC>(row_of<T>(a.gate, i, 0) + c0, tpr, t, d);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * tpr + t) * VEC;
-                if (NV * VEC > 8) asm volatile("" ::: "memory");   // one vector's values at a time: registers
-                if (!active || c >= d) continue;
-                float y[VEC], r[VEC], g[VEC], o[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) y[e] = g[e] = o[e] = 0.f;
-                if (has_y) load_vec<T, VEC>(in[0] + c, y);
-                load_vec<T, VEC>(in[1] + c, r);
-                if (has_dr) load_vec<T, VEC>(in[2] + c, g);
-                if (has_do) load_vec<T, VEC>(in[3] + c, o);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float ay = fac[c + e] * (y[e] * inv1);
-                    const float rn = fmaf(fac[d + c + e], r[e], ay), dn = fac[2 * d + c + e] * o[e];
-                    five[0] = fmaf(rn, rn, five[0]);
-                    five[1] = fmaf(dn, rn, five[1]);
-                    five[2] = fmaf(ay, g[e], five[2]);
-                    five[3] = fmaf(ay, dn, five[3]);
-                    five[4] = fmaf(ay, rn, five[4]);
-                }
-            }
-            group_sum<5>(five, tpr, t, group, red1);
-            const float inv2 = has_do ? __frsqrt_rn(fmaf(five[0], a.inv_d, a.eps)) : 0.f;
-            const float c3 = has_do ? inv2 * inv2 * five[1] * a.inv_d : 0.f;      // inv2 * mean(dn * rh)
-            const float c4 = post ? (five[2] + inv2 * (five[3] - c3 * five[4])) * a.inv_d : 0.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * tpr + t) * VEC;
-                if (NV * VEC > 8) asm volatile("" ::: "memory");   // one vector's values at a time: registers
-                if (!active || c >= d) continue;
-                float y[VEC], r[VEC], g[VEC], o[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) y[e] = g[e] = o[e] = 0.f;
-                if (has_y) load_vec<T, VEC>(in[0] + c, y);
-                load_vec<T, VEC>(in[1] + c, r);
-                if (has_dr) load_vec<T, VEC>(in[2] + c, g);
-                if (has_do) load_vec<T, VEC>(in[3] + c, o);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float fa = fac[c + e], fs = fac[d + c + e];
-                    const float yh = y[e] * inv1;
-                    const float rn = fmaf(fs, r[e], fa * yh), dn = fac[2 * d + c + e] * o[e];
-                    const float dR = has_do ? fmaf(inv2, dn - rn * c3, g[e]) : g[e];
-                    accC[v * VEC + e] = fmaf(dR, yh, accC[v * VEC + e]);
-                    accD[v * VEC + e] = fmaf(dR, r[e], accD[v * VEC + e]);
-                    accW[v * VEC + e] = fmaf(o[e], rn * inv2, accW[v * VEC + e]);
-                    r[e] = fs * dR;
-                    y[e] = inv1 * (fa * dR - yh * c4);
-                }
-                if (a.dr.p) store_vec<T, VEC>(row_of<T>(a.dr, i, row) + c, r);
-                if (a.dy.p) store_vec<T, VEC>(row_of<T>(a.dy, i, row) + c, y);
-            }
-            __syncwarp();
-            if (lane == 0) op_mbar_arrive(&s_empty[s]);
-            if (++s == S) { s = 0; ++round; }
-        }
-        u = end;
-        // column sums of this replica: first the groups inside a warp, then group after group
-        op_named_barrier(15, nc);
-        for (int o = tpr; o < 32; o <<= 1) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                accC[e] += __shfl_xor_sync(0xffffffffu, accC[e], o);
-                accD[e] += __shfl_xor_sync(0xffffffffu, accD[e], o);
-                accW[e] += __shfl_xor_sync(0xffffffffu, accW[e], o);
-            }
-        }
-        const int turn_threads = tpr < 32 ? 32 : tpr, turns = nc / turn_threads;
-        const int my_turn = threadIdx.x / turn_threads;
-        const bool writer = tpr >= 32 || lane < tpr;
-        for (int turn = 0; turn < turns; ++turn) {
-            if (turn == my_turn && writer) {
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    const int c = (v * tpr + t) * VEC;
-                    if (c >= d) continue;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        float* f = fac + c + e;
-                        const int q = v * VEC + e;
-                        f[0] = turn ? f[0] + accC[q] : accC[q];
-                        f[d] = turn ? f[d] + accD[q] : accD[q];
-                        f[2 * d] = turn ? f[2 * d] + accW[q] : accW[q];
+                    for (int p = 0; p < E / 2; ++p) {
+                        const float2 f = x.pair(p);
+                        fa[2 * p] *= sigmoid_f(f.x);
+                        fa[2 * p + 1] *= sigmoid_f(f.y);
                     }
                 }
             }
-            op_named_barrier(15, nc);
+#pragma unroll
+            for (int p = 0; p < E / 2; ++p) fs.set(p, 1.f, 1.f);
+            fw.clear();
+            if (a.scale.p) fs.template load<VEC>(row_of<T>(a.scale, i, 0) + c0, tpr, t, d);
+            if (BWD ? a.in[3].p != nullptr : a.o.p != nullptr) fw.template load<VEC>(row_of<T>(a.w_pre, i, 0) + c0, tpr, t, d);
+            if constexpr (BWD) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) accC[e] = accD[e] = accW[e] = 0.f;
+            }
+            bool last = false;
+            while (!last) {
+                const int n = w.count(), mine = team * ROWS * each + sub;      // this thread's rows: mine + z * each
+                const unsigned char* stage = ring + s * stage_bytes;
+                (void)op_mbar_wait(&s_full[s], round & 1, &s_abort, a.err);    // after a time-out the walk just goes on
+                Raw<T> in[ARRAYS][ROWS];
+#pragma unroll
+                for (int q = 0; q < ARRAYS; ++q) {
+                    if (!a.in[q].p) {
+#pragma unroll
+                        for (int z = 0; z < ROWS; ++z) in[q][z].clear();
+                        continue;
+                    }
+                    const bool together = a.in[q].row == a.d && C == 1;
+                    const T* first = row_of<T>(a.in[q], i, w.row) + c0;
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) {
+                        const int j = mine + z * each;
+                        const T* at;
+                        if (VEC > 1) at = reinterpret_cast<const T*>(stage + q * array_bytes + j * a.slot_bytes);
+                        else if (together) at = reinterpret_cast<const T*>(stage + q * array_bytes + ((uintptr_t)first & 15)) + j * d;
+                        else at = reinterpret_cast<const T*>(stage + q * array_bytes + j * a.slot_bytes + ((uintptr_t)(first + (long long)j * a.in[q].row) & 15));
+                        if (j < n) in[q][z].template load<VEC>(at, tpr, t, d);
+                        else in[q][z].clear();
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) op_mbar_arrive(&s_empty[s]);
+                if (++s == S) { s = 0; ++round; }
+                if (S > 1) fetch();
+                float inv1[ROWS];
+#pragma unroll
+                for (int z = 0; z < ROWS; ++z) inv1[z] = 1.f;
+                if (post) {
+                    float v[K1];
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) {
+                        float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+                        for (int p = 0; p < E / 2; ++p) {
+                            const float2 y = in[0][z].pair(p);
+                            p0 = fmaf(y.x, y.x, p0);
+                            p1 = fmaf(y.y, y.y, p1);
+                        }
+                        v[z] = p0 + p1;
+                    }
+                    row_sums(v, ROWS);
+                    in[0][0].repack();
+                    in[0][ROWS - 1].repack();
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) inv1[z] = __frsqrt_rn(fmaf(v[z], a.inv_d, a.eps));
+                }
+                float v[K2];
+#pragma unroll
+                for (int k = 0; k < K2; ++k) v[k] = 0.f;
+                if constexpr (!BWD) {
+                    float rn[ROWS][E];
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) {
+                        float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+                        for (int p = 0; p < E / 2; ++p) {
+                            const float2 y = in[0][z].pair(p), r = in[1][z].pair(p), f = fs.pair(p);
+                            rn[z][2 * p] = fmaf(fa[2 * p], y.x * inv1[z], f.x * r.x);
+                            rn[z][2 * p + 1] = fmaf(fa[2 * p + 1], y.y * inv1[z], f.y * r.y);
+                            p0 = fmaf(rn[z][2 * p], rn[z][2 * p], p0);
+                            p1 = fmaf(rn[z][2 * p + 1], rn[z][2 * p + 1], p1);
+                        }
+                        v[z] = p0 + p1;
+                        const int j = mine + z * each;
+                        if (a.r_out.p && j < n) {
+                            Raw<T> x;
+#pragma unroll
+                            for (int p = 0; p < E / 2; ++p) x.set(p, rn[z][2 * p], rn[z][2 * p + 1]);
+                            x.template store<VEC>(row_of<T>(a.r_out, i, w.row + j) + c0, tpr, t, d);
+                        }
+                    }
+                    if (a.o.p) {
+                        row_sums(v, ROWS);
+#pragma unroll
+                        for (int z = 0; z < ROWS; ++z) {
+                            const float inv2 = __frsqrt_rn(fmaf(v[z], a.inv_d, a.eps));
+                            const int j = mine + z * each;
+                            Raw<T> x;
+#pragma unroll
+                            for (int p = 0; p < E / 2; ++p) {
+                                const float2 f = fw.pair(p);
+                                x.set(p, rn[z][2 * p] * inv2 * f.x, rn[z][2 * p + 1] * inv2 * f.y);
+                            }
+                            if (j < n) x.template store<VEC>(row_of<T>(a.o, i, w.row + j) + c0, tpr, t, d);
+                        }
+                    }
+                } else {
+                    // sums of rn^2, dn*rn, a*yh*d_r, a*yh*dn, a*yh*rn: c3 and c4 follow from them
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) {
+#pragma unroll
+                        for (int p = 0; p < E / 2; ++p) {
+                            const float2 y2 = in[0][z].pair(p), r2 = in[1][z].pair(p), g2 = in[2][z].pair(p), o2 = in[3][z].pair(p);
+                            const float2 f2 = fs.pair(p), q2 = fw.pair(p);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float y = h ? y2.y : y2.x, r = h ? r2.y : r2.x, g = h ? g2.y : g2.x, o = h ? o2.y : o2.x;
+                                const float ay = fa[2 * p + h] * (y * inv1[z]), rn = fmaf(h ? f2.y : f2.x, r, ay), dn = (h ? q2.y : q2.x) * o;
+                                v[5 * z] = fmaf(rn, rn, v[5 * z]);
+                                v[5 * z + 1] = fmaf(dn, rn, v[5 * z + 1]);
+                                v[5 * z + 2] = fmaf(ay, g, v[5 * z + 2]);
+                                v[5 * z + 3] = fmaf(ay, dn, v[5 * z + 3]);
+                                v[5 * z + 4] = fmaf(ay, rn, v[5 * z + 4]);
+                            }
+                        }
+                    }
+                    row_sums(v, 5 * ROWS);
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z)
+#pragma unroll
+                        for (int q = 0; q < ARRAYS; ++q) in[q][z].repack();
+                    fs.repack();
+                    fw.repack();
+                    const bool has_do = a.in[3].p != nullptr;
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) {
+                        const float inv2 = has_do ? __frsqrt_rn(fmaf(v[5 * z], a.inv_d, a.eps)) : 0.f;
+                        const float c3 = inv2 * inv2 * v[5 * z + 1] * a.inv_d;                     // inv2 * mean(dn * rh)
+                        const float c4 = post ? (v[5 * z + 2] + inv2 * (v[5 * z + 3] - c3 * v[5 * z + 4])) * a.inv_d : 0.f;
+                        Raw<T> xr, xy;
+#pragma unroll
+                        for (int p = 0; p < E / 2; ++p) {
+                            const float2 y2 = in[0][z].pair(p), r2 = in[1][z].pair(p), g2 = in[2][z].pair(p), o2 = in[3][z].pair(p);
+                            const float2 f2 = fs.pair(p), q2 = fw.pair(p);
+                            float dr[2], dy[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int e = 2 * p + h;
+                                const float y = (h ? y2.y : y2.x) * inv1[z], r = h ? r2.y : r2.x, g = h ? g2.y : g2.x, o = h ? o2.y : o2.x;
+                                const float f = h ? f2.y : f2.x;
+                                const float rn = fmaf(f, r, fa[e] * y);
+                                const float dR = has_do ? fmaf(inv2, fmaf(h ? q2.y : q2.x, o, -rn * c3), g) : g;
+                                accC[e] = fmaf(dR, y, accC[e]);
+                                accD[e] = fmaf(dR, r, accD[e]);
+                                accW[e] = fmaf(o * inv2, rn, accW[e]);
+                                dr[h] = f * dR;
+                                dy[h] = inv1[z] * fmaf(fa[e], dR, -y * c4);
+                            }
+                            xr.set(p, dr[0], dr[1]);
+                            xy.set(p, dy[0], dy[1]);
+                        }
+                        const int j = mine + z * each;
+                        if (j < n) {
+                            if (a.dr.p) xr.template store<VEC>(row_of<T>(a.dr, i, w.row + j) + c0, tpr, t, d);
+                            if (a.dy.p) xy.template store<VEC>(row_of<T>(a.dy, i, w.row + j) + c0, tpr, t, d);
+                        }
+                    }
+                }
+                last = w.next();
+                if (S == 1) fetch();
+            }
+            if constexpr (BWD) {
+                // column sums of this replica: first the rows of a warp, then team after team
+                for (int x = tpr; x < 32; x <<= 1) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        accC[e] += __shfl_xor_sync(0xffffffffu, accC[e], x);
+                        accD[e] += __shfl_xor_sync(0xffffffffu, accD[e], x);
+                        accW[e] += __shfl_xor_sync(0xffffffffu, accW[e], x);
+                    }
+                }
+                float* out = a.partials + (long long)(i + b) * 3 * a.d + c0;
+                for (int turn = 0; turn < teams; ++turn) {
+                    if (turn == team && sub == 0) {
+                        float* to = turn == teams - 1 ? out : s_sums;
+                        const int step = turn == teams - 1 ? a.d : d;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const int c = VEC > 1 ? (e / VEC * tpr + t) * VEC + e % VEC : e * tpr + t;
+                            if (c >= d) continue;
+                            to[c] = accC[e] + (turn ? s_sums[c] : 0.f);
+                            to[step + c] = accD[e] + (turn ? s_sums[d + c] : 0.f);
+                            to[2 * step + c] = accW[e] + (turn ? s_sums[2 * d + c] : 0.f);
+                        }
+                    }
+                    if (teams > 1) op_named_barrier(15, nc);
+                }
+            }
         }
-        float* out = a.partials + (long long)(i + b) * 3 * d;
-        for (int c = threadIdx.x; c < 3 * d; c += nc) out[c] = fac[c];
     }
+    if (s_abort) {            // a wait ran out: the copies in flight get a millisecond to land
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) {}
+    }
+    // no CTA of a cluster ends while the other may still write to its shared memory
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // Adds up the partial column sums of replica blockIdx.y (CTA after CTA) and forms the gradients of
@@ -496,58 +747,87 @@ eg_status check(const eg_residual_norm_args* q, NormArgs* a, bool* aligned) {
 }
 
 template <typename T, int VEC, int E>
-cudaError_t forward(const NormArgs& a, cudaStream_t stream) {
-    const int tpr = threads_per_row(a.d, E), threads = tpr > kFwdThreads ? tpr : kFwdThreads / tpr * tpr;
+cudaError_t few(const NormArgs& a, cudaStream_t stream) {
+    const int tpr = threads_per_row(a.d, E), threads = tpr > kFewThreads ? tpr : kFewThreads / tpr * tpr;
     const int groups = threads / tpr;
     const long long W = (long long)a.P * a.rows, slots = (long long)sm_count() * (threads > 256 ? 2 : 4);
     if (slots < 1) return cudaErrorInvalidDevice;
     long long per = (W + slots - 1) / slots;
     per = (per + groups - 1) / groups * groups;
-    k_norm_forward<T, VEC, E><<<(unsigned)((W + per - 1) / per), threads, 0, stream>>>(a, tpr, per);
+    k_norm_few<T, VEC, E><<<(unsigned)((W + per - 1) / per), threads, 0, stream>>>(a, tpr, per);
     return cudaGetLastError();
 }
 
-template <typename T, int VEC, int E>
-cudaError_t backward(NormArgs a, const eg_residual_norm_args* q, cudaStream_t stream) {
+// Launches k_norm_stream; *G: its CTAs (clusters).
+template <typename T, int VEC, bool BWD>
+cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     const long long W = (long long)a.P * a.rows;
+    int sms = sm_count();
+    if (sms < 1) return cudaErrorInvalidDevice;
+    sms = sms > kMaxCtas ? kMaxCtas : sms;
+    constexpr int ARRAYS = BWD ? 4 : 2;
+    a.ctas = a.d <= kCtaWidth ? 1 : 2;
+    a.cols = a.ctas == 1 ? a.d : ((a.d + 1) / 2 + 7) / 8 * 8;
+    a.tpr = threads_per_row(a.cols, kElems);
+    a.tpr = a.tpr < 16 ? 16 : a.tpr;                      // the ten sums of two rows are spread over sixteen lanes
+    constexpr int ROWS = sizeof(T) == 2 ? 2 : 1;
+    const int team = a.tpr < 32 ? 32 : a.tpr, rows = ROWS * (a.tpr < 32 ? 32 / a.tpr : 1), spots = sms / a.ctas;
+    a.teams = kThreads / team;
+    const long long need = (W + (long long)spots * rows - 1) / ((long long)spots * rows);
+    if (a.teams > need) a.teams = (int)need;              // few rows: spread over the multiprocessors first
+    a.slot_bytes = VEC > 1 ? a.cols * (int)sizeof(T) : (a.cols * (int)sizeof(T) + 30) / 16 * 16;
+    const int sums = BWD && a.teams > 1 ? (3 * a.cols * 4 + 127) & ~127 : 0;
+    const int stage = ARRAYS * a.teams * rows * a.slot_bytes;
+    a.stages = (kSmemMax - 8192 - sums) / stage;
+    a.stages = a.stages > kMaxStages ? kMaxStages : a.stages;
+    if (a.stages < 1) return cudaErrorInvalidValue;
+    const int smem = sums + a.stages * stage;
+    const long long steps = (W + (long long)a.teams * rows - 1) / ((long long)a.teams * rows);
+    *G = (int)(steps < spots ? steps : spots);
+    const void* kernel = (const void*)k_norm_stream<T, VEC, BWD>;
+    static bool raised[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !raised[dev]) {
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax - 8192)) != cudaSuccess) return e;
+        if (dev < 64) raised[dev] = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(*G * a.ctas);
+    cfg.blockDim = dim3(a.teams * team);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_norm_stream<T, VEC, BWD>, a);
+}
+
+// 16-byte accesses where every row allows them.
+template <typename T> cudaError_t forward(const NormArgs& a, bool aligned, cudaStream_t stream) {
+    constexpr int V = 16 / (int)sizeof(T);
     int G = 0;
-    if (W > 0) {
-        const int tpr = threads_per_row(a.d, E), sms = sm_count();
-        if (sms < 1) return cudaErrorInvalidDevice;
-        a.slot_bytes = VEC > 1 ? a.d * (int)sizeof(T) : (a.d * (int)sizeof(T) + 30) / 16 * 16;
-        const int factors = (3 * a.d * (int)sizeof(float) + 127) & ~127, room = kSmemMax - 2048 - factors;
-        int R = kBwdThreads / tpr;
-        while (R > 1 && 2 * 4 * R * a.slot_bytes > room) --R;      // two stages at least, while rows can be given up
-        a.group_rows = R;
-        a.stages = room / (4 * R * a.slot_bytes);
-        a.stages = a.stages > 4 ? 4 : a.stages;
-        if (a.stages < 1) return cudaErrorInvalidValue;
-        const int smem = factors + a.stages * 4 * R * a.slot_bytes;
-        G = (int)(W < sms ? W : sms);
-        G = G > kBwdMaxCtas ? kBwdMaxCtas : G;
-        cudaError_t e = cudaFuncSetAttribute(k_norm_backward<T, VEC, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    // few rows: below eight for every warp of the streaming kernel its ring hardly fills
+    if ((long long)a.P * a.rows * ((a.d + 511) / 512) > 8ll * (kThreads / 32) * sm_count())
+        return aligned ? stream_rows<T, V, false>(a, &G, stream) : stream_rows<T, 1, false>(a, &G, stream);
+    if (a.d <= 2048) return aligned ? few<T, V, 8>(a, stream) : few<T, 1, 8>(a, stream);
+    return aligned ? few<T, V, 16>(a, stream) : few<T, 1, 16>(a, stream);
+}
+
+template <typename T> cudaError_t backward(const NormArgs& a, bool aligned, const eg_residual_norm_args* q, cudaStream_t stream) {
+    constexpr int V = 16 / (int)sizeof(T);
+    int G = 0;
+    if (a.rows > 0) {
+        const cudaError_t e = aligned ? stream_rows<T, V, true>(a, &G, stream) : stream_rows<T, 1, true>(a, &G, stream);
         if (e != cudaSuccess) return e;
-        const int threads = ((R * tpr + 31) & ~31) + 32;
-        k_norm_backward<T, VEC, E><<<G, threads, smem, stream>>>(a, tpr);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (!q->d_w_post.data && !q->d_gate.data && !q->d_scale.data && !q->d_w_pre.data) return cudaSuccess;
     return launch_after(k_norm_columns<T>, dim3((a.d + 31) / 32, a.P), dim3(256), 0, stream, a, mat(q->d_w_post), mat(q->d_gate),
                         mat(q->d_scale), mat(q->d_w_pre), G);
-}
-
-// 16-byte accesses where every row allows them; eight elements a thread up to 2048 columns, so that
-// a CTA works on two rows or more at a time, sixteen above.
-template <typename T, bool BACKWARD>
-cudaError_t dispatch(const NormArgs& a, bool aligned, const eg_residual_norm_args* q, cudaStream_t stream) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if constexpr (BACKWARD) {
-        if (aligned) return a.d <= 2048 ? backward<T, V, 8>(a, q, stream) : backward<T, V, 16>(a, q, stream);
-        return a.d <= 2048 ? backward<T, 1, 8>(a, q, stream) : backward<T, 1, 16>(a, q, stream);
-    } else {
-        if (aligned) return a.d <= 2048 ? forward<T, V, 8>(a, stream) : forward<T, V, 16>(a, stream);
-        return a.d <= 2048 ? forward<T, 1, 8>(a, stream) : forward<T, 1, 16>(a, stream);
-    }
 }
 
 __device__ unsigned int g_operator_error;
@@ -588,7 +868,7 @@ eg_status eg_operator_status(void* stream_v) {
 
 int64_t eg_residual_norm_workspace(int64_t P, int64_t width) {
     if (P < 1 || P > 65535 || width < 1 || width > kMaxWidth) return 0;
-    return (P + kBwdMaxCtas) * 3 * width * (int64_t)sizeof(float);
+    return (P + kMaxCtas) * 3 * width * (int64_t)sizeof(float);
 }
 
 eg_status eg_residual_norm(const eg_residual_norm_args* q, void* stream_v) {
@@ -600,9 +880,11 @@ eg_status eg_residual_norm(const eg_residual_norm_args* q, void* stream_v) {
     if (!q->residual_out.data && (q->y.data || !q->out.data)) return EG_ERR_INVALID;
     if (a.rows == 0) return EG_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    const cudaError_t e = q->dtype == EG_F32    ? dispatch<float, false>(a, aligned, q, stream)
-                          : q->dtype == EG_BF16 ? dispatch<__nv_bfloat16, false>(a, aligned, q, stream)
-                                                : dispatch<__half, false>(a, aligned, q, stream);
+    a.err = operator_error_word();
+    if (!a.err) return EG_ERR_CUDA;
+    const cudaError_t e = q->dtype == EG_F32    ? forward<float>(a, aligned, stream)
+                          : q->dtype == EG_BF16 ? forward<__nv_bfloat16>(a, aligned, stream)
+                                                : forward<__half>(a, aligned, stream);
     return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
 }
 
@@ -621,9 +903,9 @@ eg_status eg_residual_norm_backward(const eg_residual_norm_args* q, void* stream
     a.err = operator_error_word();
     if (!a.err) return EG_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    const cudaError_t e = q->dtype == EG_F32    ? dispatch<float, true>(a, aligned, q, stream)
-                          : q->dtype == EG_BF16 ? dispatch<__nv_bfloat16, true>(a, aligned, q, stream)
-                                                : dispatch<__half, true>(a, aligned, q, stream);
+    const cudaError_t e = q->dtype == EG_F32    ? backward<float>(a, aligned, q, stream)
+                          : q->dtype == EG_BF16 ? backward<__nv_bfloat16>(a, aligned, q, stream)
+                                                : backward<__half>(a, aligned, q, stream);
     return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
 }
 
