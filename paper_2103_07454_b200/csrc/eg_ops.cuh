@@ -71,6 +71,30 @@ template <typename T, int VEC> __device__ __forceinline__ void store_vec(T* p, c
     }
 }
 
+// Two fp32 values in one register pair: one instruction for both (sm_100's packed fp32 arithmetic).
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack_f2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 pack_f2(float2 v) { return pack_f2(v.x, v.y); }
+__device__ __forceinline__ float2 unpack_f2(f32x2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // Launch that may begin while its predecessor in the stream finishes; the kernel calls
 // griddepcontrol.wait before it reads what that one wrote.
 template <typename... KArgs, typename... Args>

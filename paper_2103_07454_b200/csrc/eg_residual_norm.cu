@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormAr
         if (post && has_y) {
 #pragma unroll
             for (int e = 0; e < E; ++e) sum = fmaf(y[e], y[e], sum);
-            inv1 = __frsqrt_rn(fmaf(group_sum(sum, tpr, t, group, red0), a.inv_d, a.eps));
+            inv1 = rsqrtf(fmaf(group_sum(sum, tpr, t, group, red0), a.inv_d, a.eps));
         }
         sum = 0.f;
 #pragma unroll
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormAr
         if (!pre) continue;
 #pragma unroll
         for (int e = 0; e < E; ++e) sum = fmaf(r[e], r[e], sum);
-        const float inv2 = __frsqrt_rn(fmaf(group_sum(sum, tpr, t, group, red1), a.inv_d, a.eps));
+        const float inv2 = rsqrtf(fmaf(group_sum(sum, tpr, t, group, red1), a.inv_d, a.eps));
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * tpr + t) * VEC;
@@ -171,31 +171,33 @@ __global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormAr
 // First of the W rows (replica after replica) that CTA (cluster) b of G works on.
 __host__ __device__ __forceinline__ long long cut(long long W, int b, int G) { return W * b / G; }
 
-// The rows of a CTA, step by step: up to `per` consecutive rows of one replica.
+// The rows of a CTA, step by step: up to `per` consecutive rows of one replica.  (A CTA's rows fit 31 bits: the
+// host bounds P * rows.)
 struct Walk {
-    long long row, end, left;          // first row of the step and end of the CTA's rows in replica i; rows after that
-    long long rows;
-    int i, per;
+    long long row;                     // first row of the step in replica i
+    int i, n, here, left;              // rows of the step; rows of replica i from `row` on; rows in later replicas
 
-    __device__ __forceinline__ void start(long long u0, long long u1, long long n, int rows_a_step) {
-        rows = n;
-        per = rows_a_step;
-        i = (int)(u0 / n);
-        row = u0 - (long long)i * n;
-        end = min(n, row + (u1 - u0));
-        left = u1 - u0 - (end - row);
+    __device__ __forceinline__ void start(long long u0, long long u1, long long rows, int per) {
+        i = (int)(u0 / rows);
+        row = u0 - (long long)i * rows;
+        here = (int)min(rows - row, u1 - u0);
+        left = (int)(u1 - u0) - here;
+        n = min(per, here);
     }
-    __device__ __forceinline__ bool done() const { return row >= end; }
-    __device__ __forceinline__ int count() const { return (int)min((long long)per, end - row); }
+    __device__ __forceinline__ bool done() const { return here <= 0; }
     // true: the next step is in another replica (or there is none)
-    __device__ __forceinline__ bool next() {
-        row += per;
-        if (row < end) return false;
-        ++i;
-        row = 0;
-        end = min(rows, left);
-        left -= end;
-        return true;
+    __device__ __forceinline__ bool next(long long rows, int per) {
+        here -= n;
+        row += n;
+        const bool turn = here == 0;
+        if (turn) {
+            ++i;
+            row = 0;
+            here = (int)min(rows, (long long)left);
+            left -= here;
+        }
+        n = min(per, here);
+        return turn;
     }
 };
 
@@ -206,6 +208,11 @@ template <typename T> struct Raw {
     __device__ __forceinline__ float2 pair(int p) const {
         if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
         else return unpack2<T>(w[p]);
+    }
+    __device__ __forceinline__ f32x2 two(int p) const { return pack_f2(pair(p)); }
+    __device__ __forceinline__ void set(int p, f32x2 v) {
+        const float2 f = unpack_f2(v);
+        set(p, f.x, f.y);
     }
     // Makes the compiler unpack again after this point instead of carrying unpacked values in registers.
     __device__ __forceinline__ void repack() {
@@ -243,6 +250,18 @@ template <typename T> struct Raw {
             }
         }
     }
+    // the same from shared memory; bit v of `which`: vector v is there
+    template <int VEC> __device__ __forceinline__ void load_shared(uint32_t at, int tpr, int which) {
+#pragma unroll
+        for (int v = 0; v < kElems / VEC; ++v) {
+            w[4 * v] = w[4 * v + 1] = w[4 * v + 2] = w[4 * v + 3] = 0;
+            if (which >> v & 1)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(w[4 * v]), "=r"(w[4 * v + 1]), "=r"(w[4 * v + 2]), "=r"(w[4 * v + 3])
+                             : "r"(at + v * tpr * 16)
+                             : "memory");
+        }
+    }
     template <int VEC> __device__ __forceinline__ void store(T* p, int tpr, int t, int d) const {
         if constexpr (VEC > 1) {
 #pragma unroll
@@ -272,20 +291,36 @@ template <typename T> struct Raw {
     }
 };
 
-// K values (a power of two) summed over the lanes of a warp (`width` lanes, a power of two, K <= width): halves
-// are exchanged, so that every step halves the values instead of repeating all of them (16 values: 16
+// A factor's values for a thread's columns: unpacked where there are registers for it (the backward kernel).
+template <typename T, bool WIDE> struct Factors;
+template <typename T> struct Factors<T, true> {
+    f32x2 v[kElems / 2];
+    __device__ __forceinline__ void take(const Raw<T>& x) {
+#pragma unroll
+        for (int p = 0; p < kElems / 2; ++p) v[p] = x.two(p);
+    }
+    __device__ __forceinline__ f32x2 two(int p) const { return v[p]; }
+};
+template <typename T> struct Factors<T, false> {
+    Raw<T> v;
+    __device__ __forceinline__ void take(const Raw<T>& x) { v = x; }
+    __device__ __forceinline__ f32x2 two(int p) const { return v.two(p); }
+};
+
+// K values (8 or 16) summed over the lanes of a warp, or of each half of it (`width` 32 or 16): halves are
+// exchanged, so that every step halves the values instead of repeating all of them (16 values: 16
 // shuffles, not 80).  Lane l ends up with the sum over its group of value number held(l).
 template <int K> __device__ __forceinline__ float warp_sums(float (&v)[K], int lane, int width) {
-    int bit = 1;
 #pragma unroll
-    for (int half = K / 2; half > 0; half >>= 1, bit <<= 1) {
+    for (int half = K / 2, bit = 1; half > 0; half >>= 1, bit <<= 1) {
 #pragma unroll
         for (int k = 0; k < half; ++k) {
             const float give = lane & bit ? v[k] : v[k + half], keep = lane & bit ? v[k + half] : v[k];
             v[k] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
         }
     }
-    for (; bit < width; bit <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], bit);
+    if (K == 8) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 8);
+    if (width == 32) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 16);
     return v[0];
 }
 // Value that lane l holds; it is its own inverse, so also the lane (of the first K) that holds value k.
@@ -295,7 +330,6 @@ template <int K> __device__ __forceinline__ int held(int l) {
     for (int b = 1, h = K / 2; h > 0; b <<= 1, h >>= 1) r |= l & b ? h : 0;
     return r;
 }
-__host__ __device__ constexpr int ceil_pow2(int k) { return k <= 1 ? 1 : 2 * ceil_pow2((k + 1) / 2); }
 
 // A CTA works through its rows in steps of up to teams * ROWS * (rows of a warp) consecutive rows of one
 // replica.  The rows of y, r (and d_r', d_o) of the steps ahead come into a ring of stages in
@@ -307,10 +341,15 @@ __host__ __device__ constexpr int ceil_pow2(int k) { return k <= 1 ? 1 : 2 * cei
 // (backward) its three column sums stay in registers; at the end of a replica's rows the teams add up their
 // sums in shared memory and leave one partial sum per (replica, CTA) pair that meet; i + b numbers the pairs
 // without a gap.  Rows wider than kCtaWidth are shared by a cluster of two CTAs, which exchange the sums of a row.
+//
+// A row needs one round of sums: with p = scale * r, q = a * y (so r' = p + inv1 q) and dn = d_o * w_pre, the sums
+// of y^2, p^2, pq, q^2, dn p, dn q and q d_r' give inv1 first and then every mean that the formulas above
+// ask for.  Where p and inv1 q cancel to less than a tenth of their size, r' and what follows from it are summed
+// in a second round instead.
 template <typename T, int VEC, bool BWD>
-__global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __grid_constant__ NormArgs a) {
     constexpr int E = kElems, ROWS = sizeof(T) == 2 ? 2 : 1, ARRAYS = BWD ? 4 : 2;
-    constexpr int K1 = ROWS, K2 = ceil_pow2((BWD ? 5 : 1) * ROWS);
+    constexpr int SUMS = BWD ? 7 : 4, KP = BWD ? 8 * ROWS : 8;
     constexpr int kWarps = kThreads / 32;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_peer[2];
@@ -319,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
     if (BWD) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tpr = a.tpr, S = a.stages, C = a.ctas, teams = a.teams;
     const int team_threads = tpr < 32 ? 32 : tpr, each = tpr < 32 ? 32 / tpr : 1;
-    const int nc = teams * team_threads;                       // consumer threads
+    const int nc = teams * team_threads;                       // threads of the CTA
     const int rank = C > 1 ? blockIdx.x % C : 0, b = blockIdx.x / C, G = gridDim.x / C;
     const int c0 = rank * a.cols, d = min(a.cols, a.d - c0);   // columns of this CTA
     const bool post = a.w_post.p != nullptr && a.in[0].p != nullptr;
@@ -347,19 +386,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
 
     // the rows of array q come in by lane 0 of warp q (few warps: of the last one, q after q)
     Walk ahead = w;
-    const int fetcher = threadIdx.x >> 5;
+    const int fetcher = threadIdx.x >> 5, fetchers = nc / 32;
     int as = 0, around = 0;
+    uintptr_t from_row = 0;                                    // where the next step's rows of array `fetcher` start
     auto fetch = [&]() {
         if (ahead.done()) return;
         if (lane == 0 && fetcher < ARRAYS) {
-            for (int q = fetcher; q < ARRAYS; q += nc / 32) {
+            for (int q = fetcher; q < ARRAYS; q += fetchers) {
                 const Mat& m = a.in[q];
                 if (!m.p) continue;
                 const bool together = m.row == a.d && C == 1;      // rows one after the other
-                const int n = ahead.count();
+                const int n = ahead.n;
                 if (around > 0 && !op_mbar_wait(&s_empty[as], (around - 1) & 1, &s_abort, a.err)) break;
                 unsigned char* dst = ring + as * stage_bytes + q * array_bytes;
-                const uintptr_t p = (uintptr_t)(row_of<T>(m, ahead.i, ahead.row) + c0);
+                if (from_row == 0 || fetchers < ARRAYS) from_row = (uintptr_t)(row_of<T>(m, ahead.i, ahead.row) + c0);
+                const uintptr_t p = from_row;
+                from_row += (uintptr_t)n * m.row * sizeof(T);
                 if (VEC > 1 && together) {
                     const uint32_t bytes = (uint32_t)(d * sizeof(T)) * n;
                     op_mbar_expect(&s_full[as], bytes);
@@ -380,282 +422,295 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
             }
         }
         __syncwarp();
-        ahead.next();
+        if (ahead.next(a.rows, per)) from_row = 0;
         if (++as == S) { as = 0; ++around; }
     };
     // a stage is refilled one step after its last use, when no other team should still be reading it
     for (int q = 0; q < S - 1; ++q) fetch();
     if (S == 1) fetch();
-    {
-        const int team = threadIdx.x / team_threads, tt = threadIdx.x % team_threads;
-        const int warps = team_threads >> 5, warp = tt >> 5;
-        const int sub = tpr < 32 ? lane / tpr : 0, t = tpr < 32 ? lane % tpr : tt;
-        int parity = 0, meets = 0;
-        // `used` of KP values of the team's rows, summed over their threads (and CTAs): v[k] in every thread
-        auto row_sums = [&](auto& v, int used) {
-            constexpr int KP = sizeof(v) / sizeof(float);
-            const int width = tpr < 32 ? tpr : 32;
-            float sum = warp_sums<KP>(v, lane, width);
-            const int first = lane & ~(width - 1);
-            if (tpr <= 32 && C == 1) {
-#pragma unroll
-                for (int k = 0; k < KP; ++k)
-                    if (k < used) v[k] = __shfl_sync(0xffffffffu, sum, first + held<KP>(k));
-                return;
-            }
-            if (lane < KP) {
-                float* to = &s_red[parity][rank * kWarps + team * warps + warp][held<KP>(lane)];
-                *to = sum;
-                if (C > 1) {
-                    uint32_t other;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(other) : "r"(op_smem(to)), "r"(rank ^ 1));
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(other), "f"(sum) : "memory");
-                }
-            }
-            if (C > 1) {
-                // every consumer warp of both CTAs tells both CTAs that its sums are there
-                __syncwarp();
-                if (lane < 2) {
-                    uint32_t bar;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(op_smem(&s_peer[parity])), "r"(lane));
-                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-                }
-                (void)op_mbar_wait_cluster(&s_peer[parity], meets >> 1 & 1, &s_abort, a.err);
-                ++meets;
-            } else {
-                op_named_barrier(1 + team, team_threads);
-            }
-            // lane l adds value l % KP of every (32 / KP)-th warp
-            constexpr int L = 32 / KP;
-            const int from = C > 1 ? 0 : team * warps, count = C > 1 ? kWarps + warps : warps;
-            sum = 0.f;
-            for (int x = lane / KP; x < count; x += L)
-                if (C == 1 || x % kWarps < warps) sum += s_red[parity][from + x][lane % KP];
-#pragma unroll
-            for (int o = KP; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-#pragma unroll
-            for (int k = 0; k < KP; ++k)
-                if (k < used) v[k] = __shfl_sync(0xffffffffu, sum, k);
-            parity ^= 1;
-        };
 
-        int s = 0, round = 0;
-        while (!w.done()) {
-            const int i = w.i;
-            Raw<T> fs, fw;
-            float fa[E];
-            float accC[BWD ? E : 1], accD[BWD ? E : 1], accW[BWD ? E : 1];
-            {
-                Raw<T> x;
-                if (a.w_post.p) x.template load<VEC>(row_of<T>(a.w_post, i, 0) + c0, tpr, t, d);
+    const int team = threadIdx.x / team_threads, tt = threadIdx.x % team_threads;
+    const int warps = team_threads >> 5, warp = tt >> 5;
+    const int sub = tpr < 32 ? lane / tpr : 0, t = tpr < 32 ? lane % tpr : tt;
+    const int mine = team * ROWS * each + sub;                 // this thread's rows of a step: mine + z * each
+    const uint32_t mine_at = op_smem(ring) + mine * a.slot_bytes + t * VEC * (int)sizeof(T);
+    int in_row = 0;                                            // bit v: vector v of this thread lies in the row
+    if (VEC > 1)
+        for (int v = 0; v < E / VEC; ++v) in_row |= (v * tpr + t) * VEC < d ? 1 << v : 0;
+    int parity = 0, meets = 0;
+    // the values of the team's rows, summed over their threads (and CTAs): v[k] in every thread
+    auto row_sums = [&](float (&v)[KP]) {
+        const int width = tpr < 32 ? tpr : 32;
+        float sum = warp_sums<KP>(v, lane, width);
+        if (tpr <= 32 && C == 1) {
+            const int first = lane & ~(width - 1);
+#pragma unroll
+            for (int k = 0; k < KP; ++k) v[k] = __shfl_sync(0xffffffffu, sum, first + held<KP>(k));
+            return;
+        }
+        if (lane < KP) {
+            float* to = &s_red[parity][rank * kWarps + team * warps + warp][held<KP>(lane)];
+            *to = sum;
+            if (C > 1) {
+                uint32_t other;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(other) : "r"(op_smem(to)), "r"(rank ^ 1));
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(other), "f"(sum) : "memory");
+            }
+        }
+        if (C > 1) {
+            // every warp of both CTAs tells both CTAs that its sums are there
+            __syncwarp();
+            if (lane < 2) {
+                uint32_t bar;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(op_smem(&s_peer[parity])), "r"(lane));
+                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+            }
+            (void)op_mbar_wait_cluster(&s_peer[parity], meets >> 1 & 1, &s_abort, a.err);
+            ++meets;
+        } else {
+            op_named_barrier(1 + team, team_threads);
+        }
+        // lane l adds value l % KP of every (32 / KP)-th warp
+        constexpr int L = 32 / KP;
+        const float* from = &s_red[parity][C > 1 ? 0 : team * warps][lane % KP];
+        sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < kWarps; x += L)
+            if (x + lane / KP < warps) sum += from[(x + lane / KP) * 16];
+        if (C > 1) {
+#pragma unroll
+            for (int x = 0; x < kWarps; x += L)
+                if (x + lane / KP < warps) sum += from[(kWarps + x + lane / KP) * 16];
+        }
+        if (KP == 8) sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+#pragma unroll
+        for (int k = 0; k < KP; ++k) v[k] = __shfl_sync(0xffffffffu, sum, k);
+        parity ^= 1;
+    };
+    auto total = [](f32x2 v) {
+        const float2 f = unpack_f2(v);
+        return f.x + f.y;
+    };
+
+    int s = 0, round = 0;
+    while (!w.done()) {
+        const int i = w.i;
+        Factors<T, BWD> fs, fw;
+        f32x2 fa[E / 2];
+        f32x2 accC[BWD ? E / 2 : 1], accD[BWD ? E / 2 : 1], accW[BWD ? E / 2 : 1];
+        {
+            const float there = a.in[0].p ? 1.f : 0.f;
+            Raw<T> x;
+            if (a.w_post.p) x.template load<VEC>(row_of<T>(a.w_post, i, 0) + c0, tpr, t, d);
+#pragma unroll
+            for (int p = 0; p < E / 2; ++p) fa[p] = a.w_post.p ? x.two(p) : pack_f2(there, there);
+            if (a.gate.p) {
+                x.template load<VEC>(row_of<T>(a.gate, i, 0) + c0, tpr, t, d);
 #pragma unroll
                 for (int p = 0; p < E / 2; ++p) {
-                    const float2 f = a.w_post.p ? x.pair(p) : make_float2(1.f, 1.f);
-                    fa[2 * p] = a.in[0].p ? f.x : 0.f;
-                    fa[2 * p + 1] = a.in[0].p ? f.y : 0.f;
+                    const float2 f = x.pair(p);
+                    fa[p] = mul2(fa[p], pack_f2(sigmoid_f(f.x), sigmoid_f(f.y)));
                 }
-                if (a.gate.p) {
-                    x.template load<VEC>(row_of<T>(a.gate, i, 0) + c0, tpr, t, d);
+            }
+        }
+        {
+            Raw<T> x;
+#pragma unroll
+            for (int p = 0; p < E / 2; ++p) x.set(p, 1.f, 1.f);
+            if (a.scale.p) x.template load<VEC>(row_of<T>(a.scale, i, 0) + c0, tpr, t, d);
+            fs.take(x);
+            x.clear();
+            if (BWD ? a.in[3].p != nullptr : a.o.p != nullptr) x.template load<VEC>(row_of<T>(a.w_pre, i, 0) + c0, tpr, t, d);
+            fw.take(x);
+        }
+        if constexpr (BWD) {
+#pragma unroll
+            for (int p = 0; p < E / 2; ++p) accC[p] = accD[p] = accW[p] = 0;
+        }
+        bool last = false;
+        while (!last) {
+            const int n = w.n;
+            (void)op_mbar_wait(&s_full[s], round & 1, &s_abort, a.err);    // after a time-out the walk just goes on
+            Raw<T> in[ARRAYS][ROWS];
+            uint32_t at = mine_at + s * stage_bytes;
+#pragma unroll
+            for (int q = 0; q < ARRAYS; ++q, at += array_bytes) {
+#pragma unroll
+                for (int z = 0; z < ROWS; ++z) {
+                    if (VEC > 1) {
+                        in[q][z].template load_shared<VEC>(at + z * each * a.slot_bytes, tpr, a.in[q].p && mine + z * each < n ? in_row : 0);
+                    } else {
+                        in[q][z].clear();
+                        if (!a.in[q].p || mine + z * each >= n) continue;
+                        const int j = mine + z * each;
+                        const T* first = row_of<T>(a.in[q], i, w.row) + c0;
+                        const unsigned char* x = ring + s * stage_bytes + q * array_bytes;
+                        if (a.in[q].row == a.d && C == 1) x += ((uintptr_t)first & 15) + (size_t)j * d * sizeof(T);
+                        else x += j * a.slot_bytes + ((uintptr_t)(first + (long long)j * a.in[q].row) & 15);
+                        in[q][z].template load<VEC>(reinterpret_cast<const T*>(x), tpr, t, d);
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) op_mbar_arrive(&s_empty[s]);
+            if (++s == S) { s = 0; ++round; }
+            if (S > 1) fetch();
+
+            float v[KP];
+#pragma unroll
+            for (int k = 0; k < KP; ++k) v[k] = 0.f;
+#pragma unroll
+            for (int z = 0; z < ROWS; ++z) {
+                f32x2 sum[SUMS];
+#pragma unroll
+                for (int k = 0; k < SUMS; ++k) sum[k] = 0;
+#pragma unroll
+                for (int p = 0; p < E / 2; ++p) {
+                    const f32x2 y = in[0][z].two(p), P = mul2(fs.two(p), in[1][z].two(p)), Q = mul2(fa[p], y);
+                    sum[0] = fma2(y, y, sum[0]);
+                    sum[1] = fma2(P, P, sum[1]);
+                    sum[2] = fma2(P, Q, sum[2]);
+                    sum[3] = fma2(Q, Q, sum[3]);
+                    if constexpr (BWD) {
+                        const f32x2 dn = mul2(fw.two(p), in[3][z].two(p));
+                        sum[4] = fma2(dn, P, sum[4]);
+                        sum[5] = fma2(dn, Q, sum[5]);
+                        sum[6] = fma2(Q, in[2][z].two(p), sum[6]);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < SUMS; ++k) v[z * (KP / ROWS) + k] = total(sum[k]);
+            }
+            row_sums(v);
+#pragma unroll
+            for (int z = 0; z < ROWS; ++z)
+#pragma unroll
+                for (int q = 0; q < ARRAYS; ++q) in[q][z].repack();
+            float inv1[ROWS], rr[ROWS], dnr[ROWS], qr[ROWS];       // sums of r'^2, dn r', q r'
+            bool cancels = false;
+#pragma unroll
+            for (int z = 0; z < ROWS; ++z) {
+                const float* x = v + z * (KP / ROWS);
+                inv1[z] = post ? rsqrtf(fmaf(x[0], a.inv_d, a.eps)) : 1.f;
+                const float size = fmaf(inv1[z] * inv1[z], x[3], x[1]);
+                rr[z] = fmaf(2.f * inv1[z], x[2], size);
+                cancels = cancels || rr[z] < 0.01f * size;
+                if constexpr (BWD) {
+                    dnr[z] = fmaf(inv1[z], x[5], x[4]);
+                    qr[z] = fmaf(inv1[z], x[3], x[2]);
+                }
+            }
+            // one answer for all who sum together
+            if (tpr <= 32) cancels = __any_sync(0xffffffffu, cancels);
+            if (cancels) {
+                float again[KP];
+#pragma unroll
+                for (int k = 0; k < KP; ++k) again[k] = 0.f;
+#pragma unroll
+                for (int z = 0; z < ROWS; ++z) {
+                    f32x2 sum[3] = {0, 0, 0};
+                    const f32x2 i1 = pack_f2(inv1[z], inv1[z]);
 #pragma unroll
                     for (int p = 0; p < E / 2; ++p) {
-                        const float2 f = x.pair(p);
-                        fa[2 * p] *= sigmoid_f(f.x);
-                        fa[2 * p + 1] *= sigmoid_f(f.y);
-                    }
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < E / 2; ++p) fs.set(p, 1.f, 1.f);
-            fw.clear();
-            if (a.scale.p) fs.template load<VEC>(row_of<T>(a.scale, i, 0) + c0, tpr, t, d);
-            if (BWD ? a.in[3].p != nullptr : a.o.p != nullptr) fw.template load<VEC>(row_of<T>(a.w_pre, i, 0) + c0, tpr, t, d);
-            if constexpr (BWD) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) accC[e] = accD[e] = accW[e] = 0.f;
-            }
-            bool last = false;
-            while (!last) {
-                const int n = w.count(), mine = team * ROWS * each + sub;      // this thread's rows: mine + z * each
-                const unsigned char* stage = ring + s * stage_bytes;
-                (void)op_mbar_wait(&s_full[s], round & 1, &s_abort, a.err);    // after a time-out the walk just goes on
-                Raw<T> in[ARRAYS][ROWS];
-#pragma unroll
-                for (int q = 0; q < ARRAYS; ++q) {
-                    if (!a.in[q].p) {
-#pragma unroll
-                        for (int z = 0; z < ROWS; ++z) in[q][z].clear();
-                        continue;
-                    }
-                    const bool together = a.in[q].row == a.d && C == 1;
-                    const T* first = row_of<T>(a.in[q], i, w.row) + c0;
-#pragma unroll
-                    for (int z = 0; z < ROWS; ++z) {
-                        const int j = mine + z * each;
-                        const T* at;
-                        if (VEC > 1) at = reinterpret_cast<const T*>(stage + q * array_bytes + j * a.slot_bytes);
-                        else if (together) at = reinterpret_cast<const T*>(stage + q * array_bytes + ((uintptr_t)first & 15)) + j * d;
-                        else at = reinterpret_cast<const T*>(stage + q * array_bytes + j * a.slot_bytes + ((uintptr_t)(first + (long long)j * a.in[q].row) & 15));
-                        if (j < n) in[q][z].template load<VEC>(at, tpr, t, d);
-                        else in[q][z].clear();
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) op_mbar_arrive(&s_empty[s]);
-                if (++s == S) { s = 0; ++round; }
-                if (S > 1) fetch();
-                float inv1[ROWS];
-#pragma unroll
-                for (int z = 0; z < ROWS; ++z) inv1[z] = 1.f;
-                if (post) {
-                    float v[K1];
-#pragma unroll
-                    for (int z = 0; z < ROWS; ++z) {
-                        float p0 = 0.f, p1 = 0.f;
-#pragma unroll
-                        for (int p = 0; p < E / 2; ++p) {
-                            const float2 y = in[0][z].pair(p);
-                            p0 = fmaf(y.x, y.x, p0);
-                            p1 = fmaf(y.y, y.y, p1);
+                        const f32x2 Q = mul2(fa[p], in[0][z].two(p)), R = fma2(i1, Q, mul2(fs.two(p), in[1][z].two(p)));
+                        sum[0] = fma2(R, R, sum[0]);
+                        if constexpr (BWD) {
+                            sum[1] = fma2(mul2(fw.two(p), in[3][z].two(p)), R, sum[1]);
+                            sum[2] = fma2(Q, R, sum[2]);
                         }
-                        v[z] = p0 + p1;
                     }
-                    row_sums(v, ROWS);
-                    in[0][0].repack();
-                    in[0][ROWS - 1].repack();
 #pragma unroll
-                    for (int z = 0; z < ROWS; ++z) inv1[z] = __frsqrt_rn(fmaf(v[z], a.inv_d, a.eps));
+                    for (int k = 0; k < 3; ++k) again[z * (KP / ROWS) + k] = total(sum[k]);
                 }
-                float v[K2];
+                row_sums(again);
 #pragma unroll
-                for (int k = 0; k < K2; ++k) v[k] = 0.f;
+                for (int z = 0; z < ROWS; ++z) {
+                    rr[z] = again[z * (KP / ROWS)];
+                    dnr[z] = again[z * (KP / ROWS) + 1];
+                    qr[z] = again[z * (KP / ROWS) + 2];
+                }
+            }
+#pragma unroll
+            for (int z = 0; z < ROWS; ++z) {
+                const int j = mine + z * each;
+                const long long row = w.row + j;
+                const f32x2 i1 = pack_f2(inv1[z], inv1[z]);
                 if constexpr (!BWD) {
-                    float rn[ROWS][E];
+                    const float i2 = rsqrtf(fmaf(rr[z], a.inv_d, a.eps));
+                    const f32x2 inv2 = pack_f2(i2, i2);
+                    Raw<T> xr, xo;
 #pragma unroll
-                    for (int z = 0; z < ROWS; ++z) {
-                        float p0 = 0.f, p1 = 0.f;
-#pragma unroll
-                        for (int p = 0; p < E / 2; ++p) {
-                            const float2 y = in[0][z].pair(p), r = in[1][z].pair(p), f = fs.pair(p);
-                            rn[z][2 * p] = fmaf(fa[2 * p], y.x * inv1[z], f.x * r.x);
-                            rn[z][2 * p + 1] = fmaf(fa[2 * p + 1], y.y * inv1[z], f.y * r.y);
-                            p0 = fmaf(rn[z][2 * p], rn[z][2 * p], p0);
-                            p1 = fmaf(rn[z][2 * p + 1], rn[z][2 * p + 1], p1);
-                        }
-                        v[z] = p0 + p1;
-                        const int j = mine + z * each;
-                        if (a.r_out.p && j < n) {
-                            Raw<T> x;
-#pragma unroll
-                            for (int p = 0; p < E / 2; ++p) x.set(p, rn[z][2 * p], rn[z][2 * p + 1]);
-                            x.template store<VEC>(row_of<T>(a.r_out, i, w.row + j) + c0, tpr, t, d);
-                        }
+                    for (int p = 0; p < E / 2; ++p) {
+                        const f32x2 R = fma2(i1, mul2(fa[p], in[0][z].two(p)), mul2(fs.two(p), in[1][z].two(p)));
+                        xr.set(p, R);
+                        xo.set(p, mul2(mul2(R, inv2), fw.two(p)));
                     }
-                    if (a.o.p) {
-                        row_sums(v, ROWS);
-#pragma unroll
-                        for (int z = 0; z < ROWS; ++z) {
-                            const float inv2 = __frsqrt_rn(fmaf(v[z], a.inv_d, a.eps));
-                            const int j = mine + z * each;
-                            Raw<T> x;
-#pragma unroll
-                            for (int p = 0; p < E / 2; ++p) {
-                                const float2 f = fw.pair(p);
-                                x.set(p, rn[z][2 * p] * inv2 * f.x, rn[z][2 * p + 1] * inv2 * f.y);
-                            }
-                            if (j < n) x.template store<VEC>(row_of<T>(a.o, i, w.row + j) + c0, tpr, t, d);
-                        }
+                    if (j < n) {
+                        if (a.r_out.p) xr.template store<VEC>(row_of<T>(a.r_out, i, row) + c0, tpr, t, d);
+                        if (a.o.p) xo.template store<VEC>(row_of<T>(a.o, i, row) + c0, tpr, t, d);
                     }
                 } else {
-                    // sums of rn^2, dn*rn, a*yh*d_r, a*yh*dn, a*yh*rn: c3 and c4 follow from them
-#pragma unroll
-                    for (int z = 0; z < ROWS; ++z) {
-#pragma unroll
-                        for (int p = 0; p < E / 2; ++p) {
-                            const float2 y2 = in[0][z].pair(p), r2 = in[1][z].pair(p), g2 = in[2][z].pair(p), o2 = in[3][z].pair(p);
-                            const float2 f2 = fs.pair(p), q2 = fw.pair(p);
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float y = h ? y2.y : y2.x, r = h ? r2.y : r2.x, g = h ? g2.y : g2.x, o = h ? o2.y : o2.x;
-                                const float ay = fa[2 * p + h] * (y * inv1[z]), rn = fmaf(h ? f2.y : f2.x, r, ay), dn = (h ? q2.y : q2.x) * o;
-                                v[5 * z] = fmaf(rn, rn, v[5 * z]);
-                                v[5 * z + 1] = fmaf(dn, rn, v[5 * z + 1]);
-                                v[5 * z + 2] = fmaf(ay, g, v[5 * z + 2]);
-                                v[5 * z + 3] = fmaf(ay, dn, v[5 * z + 3]);
-                                v[5 * z + 4] = fmaf(ay, rn, v[5 * z + 4]);
-                            }
-                        }
-                    }
-                    row_sums(v, 5 * ROWS);
-#pragma unroll
-                    for (int z = 0; z < ROWS; ++z)
-#pragma unroll
-                        for (int q = 0; q < ARRAYS; ++q) in[q][z].repack();
-                    fs.repack();
-                    fw.repack();
                     const bool has_do = a.in[3].p != nullptr;
+                    const float x6 = v[z * (KP / ROWS) + 6], x5 = v[z * (KP / ROWS) + 5];
+                    const float i2 = has_do ? rsqrtf(fmaf(rr[z], a.inv_d, a.eps)) : 0.f;
+                    const float c3 = has_do ? i2 * i2 * dnr[z] * a.inv_d : 0.f;                    // inv2 * mean(dn * rh)
+                    const float c4 = post ? inv1[z] * (x6 + i2 * (x5 - c3 * qr[z])) * a.inv_d : 0.f;
+                    const f32x2 inv2 = pack_f2(i2, i2), k3 = pack_f2(-i2 * c3, -i2 * c3);
+                    const float k = -inv1[z] * inv1[z] * c4;
+                    const f32x2 k4 = pack_f2(k, k);
+                    Raw<T> xr, xy;
 #pragma unroll
-                    for (int z = 0; z < ROWS; ++z) {
-                        const float inv2 = has_do ? __frsqrt_rn(fmaf(v[5 * z], a.inv_d, a.eps)) : 0.f;
-                        const float c3 = inv2 * inv2 * v[5 * z + 1] * a.inv_d;                     // inv2 * mean(dn * rh)
-                        const float c4 = post ? (v[5 * z + 2] + inv2 * (v[5 * z + 3] - c3 * v[5 * z + 4])) * a.inv_d : 0.f;
-                        Raw<T> xr, xy;
-#pragma unroll
-                        for (int p = 0; p < E / 2; ++p) {
-                            const float2 y2 = in[0][z].pair(p), r2 = in[1][z].pair(p), g2 = in[2][z].pair(p), o2 = in[3][z].pair(p);
-                            const float2 f2 = fs.pair(p), q2 = fw.pair(p);
-                            float dr[2], dy[2];
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int e = 2 * p + h;
-                                const float y = (h ? y2.y : y2.x) * inv1[z], r = h ? r2.y : r2.x, g = h ? g2.y : g2.x, o = h ? o2.y : o2.x;
-                                const float f = h ? f2.y : f2.x;
-                                const float rn = fmaf(f, r, fa[e] * y);
-                                const float dR = has_do ? fmaf(inv2, fmaf(h ? q2.y : q2.x, o, -rn * c3), g) : g;
-                                accC[e] = fmaf(dR, y, accC[e]);
-                                accD[e] = fmaf(dR, r, accD[e]);
-                                accW[e] = fmaf(o * inv2, rn, accW[e]);
-                                dr[h] = f * dR;
-                                dy[h] = inv1[z] * fmaf(fa[e], dR, -y * c4);
-                            }
-                            xr.set(p, dr[0], dr[1]);
-                            xy.set(p, dy[0], dy[1]);
-                        }
-                        const int j = mine + z * each;
-                        if (j < n) {
-                            if (a.dr.p) xr.template store<VEC>(row_of<T>(a.dr, i, w.row + j) + c0, tpr, t, d);
-                            if (a.dy.p) xy.template store<VEC>(row_of<T>(a.dy, i, w.row + j) + c0, tpr, t, d);
-                        }
+                    for (int p = 0; p < E / 2; ++p) {
+                        const f32x2 y = in[0][z].two(p), r = in[1][z].two(p), o = in[3][z].two(p), f = fs.two(p);
+                        const f32x2 R = fma2(i1, mul2(fa[p], y), mul2(f, r));
+                        const f32x2 dR = fma2(k3, R, fma2(inv2, mul2(fw.two(p), o), in[2][z].two(p)));
+                        const f32x2 tR = mul2(dR, i1);
+                        accC[p] = fma2(tR, y, accC[p]);
+                        accD[p] = fma2(dR, r, accD[p]);
+                        accW[p] = fma2(o, mul2(R, inv2), accW[p]);
+                        xr.set(p, mul2(f, dR));
+                        xy.set(p, fma2(k4, y, mul2(fa[p], tR)));
+                    }
+                    if (j < n) {
+                        if (a.dr.p) xr.template store<VEC>(row_of<T>(a.dr, i, row) + c0, tpr, t, d);
+                        if (a.dy.p) xy.template store<VEC>(row_of<T>(a.dy, i, row) + c0, tpr, t, d);
                     }
                 }
-                last = w.next();
-                if (S == 1) fetch();
             }
-            if constexpr (BWD) {
-                // column sums of this replica: first the rows of a warp, then team after team
-                for (int x = tpr; x < 32; x <<= 1) {
+            last = w.next(a.rows, per);
+            if (S == 1) fetch();
+        }
+        if constexpr (BWD) {
+            // column sums of this replica: first the rows of a warp, then team after team
+            float* out = a.partials + (long long)(i + b) * 3 * a.d + c0;
+            float sums[3][E];
+#pragma unroll
+            for (int p = 0; p < E / 2; ++p) {
+                const float2 x = unpack_f2(accC[p]), y = unpack_f2(accD[p]), z = unpack_f2(accW[p]);
+                sums[0][2 * p] = x.x; sums[0][2 * p + 1] = x.y;
+                sums[1][2 * p] = y.x; sums[1][2 * p + 1] = y.y;
+                sums[2][2 * p] = z.x; sums[2][2 * p + 1] = z.y;
+            }
+            if (tpr < 32) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) sums[k][e] += __shfl_xor_sync(0xffffffffu, sums[k][e], 16);
+            }
+            for (int turn = 0; turn < teams; ++turn) {
+                if (turn == team && sub == 0) {
+                    float* to = turn == teams - 1 ? out : s_sums;
+                    const int step = turn == teams - 1 ? a.d : d;
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        accC[e] += __shfl_xor_sync(0xffffffffu, accC[e], x);
-                        accD[e] += __shfl_xor_sync(0xffffffffu, accD[e], x);
-                        accW[e] += __shfl_xor_sync(0xffffffffu, accW[e], x);
-                    }
-                }
-                float* out = a.partials + (long long)(i + b) * 3 * a.d + c0;
-                for (int turn = 0; turn < teams; ++turn) {
-                    if (turn == team && sub == 0) {
-                        float* to = turn == teams - 1 ? out : s_sums;
-                        const int step = turn == teams - 1 ? a.d : d;
+                        const int c = VEC > 1 ? (e / VEC * tpr + t) * VEC + e % VEC : e * tpr + t;
+                        if (c >= d) continue;
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const int c = VEC > 1 ? (e / VEC * tpr + t) * VEC + e % VEC : e * tpr + t;
-                            if (c >= d) continue;
-                            to[c] = accC[e] + (turn ? s_sums[c] : 0.f);
-                            to[step + c] = accD[e] + (turn ? s_sums[d + c] : 0.f);
-                            to[2 * step + c] = accW[e] + (turn ? s_sums[2 * d + c] : 0.f);
-                        }
+                        for (int k = 0; k < 3; ++k) to[k * step + c] = sums[k][e] + (turn ? s_sums[k * d + c] : 0.f);
                     }
-                    if (teams > 1) op_named_barrier(15, nc);
                 }
+                if (teams > 1) op_named_barrier(15, nc);
             }
         }
     }
@@ -715,7 +770,7 @@ bool whole_vectors(const Mat& m, size_t size, bool vector) {
 eg_status check(const eg_residual_norm_args* q, NormArgs* a, bool* aligned) {
     if (!q) return EG_ERR_INVALID;
     if (q->dtype != EG_F32 && q->dtype != EG_BF16 && q->dtype != EG_F16) return EG_ERR_INVALID;
-    if (q->P < 1 || q->P > 65535 || q->rows < 0 || q->rows > (1ll << 40) || q->width < 1 || q->width > kMaxWidth)
+    if (q->P < 1 || q->P > 65535 || q->rows < 0 || q->rows > (1ll << 37) / q->P || q->width < 1 || q->width > kMaxWidth)
         return EG_ERR_INVALID;
     if (!(q->eps >= 0.0) || q->eps > 3e38) return EG_ERR_INVALID;
     if (!q->residual.data) return EG_ERR_INVALID;
@@ -769,16 +824,17 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     a.ctas = a.d <= kCtaWidth ? 1 : 2;
     a.cols = a.ctas == 1 ? a.d : ((a.d + 1) / 2 + 7) / 8 * 8;
     a.tpr = threads_per_row(a.cols, kElems);
-    a.tpr = a.tpr < 16 ? 16 : a.tpr;                      // the ten sums of two rows are spread over sixteen lanes
+    a.tpr = a.tpr < 16 ? 16 : a.tpr;                      // the sums of two rows are spread over sixteen lanes
     constexpr int ROWS = sizeof(T) == 2 ? 2 : 1;
-    const int team = a.tpr < 32 ? 32 : a.tpr, rows = ROWS * (a.tpr < 32 ? 32 / a.tpr : 1), spots = sms / a.ctas;
+    constexpr int RESIDENT = BWD ? 1 : 2;                 // CTAs of a multiprocessor
+    const int team = a.tpr < 32 ? 32 : a.tpr, rows = ROWS * (a.tpr < 32 ? 32 / a.tpr : 1), spots = RESIDENT * sms / a.ctas;
     a.teams = kThreads / team;
     const long long need = (W + (long long)spots * rows - 1) / ((long long)spots * rows);
     if (a.teams > need) a.teams = (int)need;              // few rows: spread over the multiprocessors first
     a.slot_bytes = VEC > 1 ? a.cols * (int)sizeof(T) : (a.cols * (int)sizeof(T) + 30) / 16 * 16;
     const int sums = BWD && a.teams > 1 ? (3 * a.cols * 4 + 127) & ~127 : 0;
     const int stage = ARRAYS * a.teams * rows * a.slot_bytes;
-    a.stages = (kSmemMax - 8192 - sums) / stage;
+    a.stages = ((kSmemMax - 8192) / RESIDENT - sums) / stage;
     a.stages = a.stages > kMaxStages ? kMaxStages : a.stages;
     if (a.stages < 1) return cudaErrorInvalidValue;
     const int smem = sums + a.stages * stage;
@@ -790,7 +846,7 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !raised[dev]) {
-        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax - 8192)) != cudaSuccess) return e;
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kSmemMax - 8192) / RESIDENT)) != cudaSuccess) return e;
         if (dev < 64) raised[dev] = true;
     }
     cudaLaunchConfig_t cfg{};
