@@ -398,21 +398,18 @@ class EventGrad:
         dtype = DTYPES.get(grads.dtype)
         if out is None:
             out = grads
-        assert dtype is not None and out.dtype == torch.float32
+        assert dtype is not None and out.dtype is torch.float32
         assert grads.is_cuda and out.is_cuda and grads.is_contiguous() and out.is_contiguous()
         assert grads.shape == out.shape == (self.P, self.replica_stride)
-        s = stream if stream is not None else torch.cuda.current_stream(self.device)
-        if norms is None:
-            if stream is None:
-                norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
-            else:
-                with torch.cuda.stream(s):
-                    norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
-        assert norms.is_cuda and norms.dtype == torch.float32 and norms.is_contiguous() and norms.numel() == self.P
-        st = self._lib.eg_clip_gradients(self._h, grads.data_ptr(), dtype, float(max_norm),
-                                         CLIP_ZERO_NONFINITE if zero_nonfinite else 0, out.data_ptr(),
-                                         norms.data_ptr(), s.cuda_stream)
-        _check(self._lib, st, self._h, "eg_clip_gradients")
+        with _on_stream(grads, stream) as s:
+            if norms is None:
+                norms = out.new_empty(self.P)
+            assert norms.is_cuda and norms.dtype is torch.float32 and norms.is_contiguous() and norms.numel() == self.P
+            st = self._lib.eg_clip_gradients(self._h, grads.data_ptr(), dtype, max_norm,
+                                             CLIP_ZERO_NONFINITE if zero_nonfinite else 0, out.data_ptr(),
+                                             norms.data_ptr(), s)
+        if st:
+            _check(self._lib, st, self._h, "eg_clip_gradients")
         return norms
 
     def set_fused_kernel(self, kind: int):
@@ -471,45 +468,76 @@ def change_norms_static(x: torch.Tensor, xhat: torch.Tensor, tensor_offset: Sequ
 # ``[P, ...]`` views of the replicas' weights, on torch's current stream unless one is given
 # --------------------------------------------------------------------------------------
 _NONE = (0, 0, 0)
+_NONE5, _NONE8 = _NONE * 5, _NONE * 8
 _FFN_ARGS = struct.Struct("=6q30q2q")     # eg_feed_forward_args
 _NORM_ARGS = struct.Struct("=4qd48q2q")   # eg_residual_norm_args
 
 
-def _matrix(t: Optional[torch.Tensor], shape: tuple, like: torch.Tensor, what: str) -> tuple:
-    """(pointer, replica stride, row stride) of a ``[P, rows, columns]`` or ``[P, columns]`` tensor."""
+def _matrix(t: Optional[torch.Tensor], shape: torch.Size, dtype: torch.dtype, device: int, what: str) -> tuple:
+    """(pointer, replica stride, row stride) of a ``[P, rows, columns]`` tensor."""
     if t is None:
         return _NONE
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
-        raise EventGradError(f"{what}: expected {shape} {like.dtype} on {like.device}, "
-                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
-    st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise _unexpected(t, shape, dtype, device, what)
+    a, b, c = t.stride()
+    if c != 1 and shape[2] > 1:
         raise EventGradError(f"{what}: the last dimension must be contiguous")
-    return (t.data_ptr(), st[0], st[1] if len(st) == 3 else 0)
+    return t.data_ptr(), a, b
 
 
-class _OnStream:
-    """Makes ``stream`` (and the tensor's device) current while outputs and workspaces are allocated, so that
-    they belong to the stream that uses them."""
+def _vector(t: Optional[torch.Tensor], shape: torch.Size, dtype: torch.dtype, device: int, what: str) -> tuple:
+    """(pointer, replica stride, 0) of a ``[P, columns]`` tensor."""
+    if t is None:
+        return _NONE
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise _unexpected(t, shape, dtype, device, what)
+    a, b = t.stride()
+    if b != 1 and shape[1] > 1:
+        raise EventGradError(f"{what}: the last dimension must be contiguous")
+    return t.data_ptr(), a, 0
 
-    def __init__(self, x: torch.Tensor, stream: Optional[torch.cuda.Stream]):
-        if not x.is_cuda:
-            raise EventGradError("no CUDA device: this library has no CPU path")
-        self._ctx = None
-        if stream is not None:
-            self._ctx = torch.cuda.stream(stream)
-        elif x.device.index != torch.cuda.current_device():
-            self._ctx = torch.cuda.device(x.device)
-        self._device = x.device
+
+def _unexpected(t, shape, dtype, device, what):
+    return EventGradError(f"{what}: expected {tuple(shape)} {dtype} on cuda:{device}, "
+                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+class _Elsewhere:
+    """Makes ``stream``, or else the tensors' device, current: outputs and workspaces then belong to the stream
+    that uses them."""
+
+    def __init__(self, device: int, stream: Optional[torch.cuda.Stream]):
+        self._ctx = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
+        self._device = device
 
     def __enter__(self) -> int:
-        if self._ctx is not None:
-            self._ctx.__enter__()
+        self._ctx.__enter__()
         return torch.cuda.current_stream(self._device).cuda_stream
 
     def __exit__(self, *exc):
-        if self._ctx is not None:
-            self._ctx.__exit__(*exc)
+        self._ctx.__exit__(*exc)
+
+
+class _Here:
+    """The current stream of the current device, without the cost of looking up stream objects."""
+
+    def __init__(self, handle: int):
+        self._handle = handle
+
+    def __enter__(self) -> int:
+        return self._handle
+
+    def __exit__(self, *exc):
+        pass
+
+
+def _on_stream(x: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+    device = x.get_device()
+    if device < 0:
+        raise EventGradError("no CUDA device: this library has no CPU path")
+    if stream is None and device == torch._C._cuda_getDevice():
+        return _Here(torch._C._cuda_getCurrentRawStream(device))
+    return _Elsewhere(device, stream)
 
 
 def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: Optional[torch.Tensor] = None,
@@ -522,25 +550,26 @@ def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: 
 
     Returns ``(r', o)``; ``o`` is None without ``w_pre``.  ``y`` None: only the scaled residual."""
     lib = load_library()
-    if residual.dim() != 3 or residual.dtype not in DTYPES:
+    shape, dtype = residual.shape, residual.dtype
+    if len(shape) != 3 or dtype not in DTYPES:
         raise EventGradError("residual_norm: residual must be [P, rows, width] fp32, bf16 or fp16")
-    shape = residual.shape
     P, n, d = shape
-    vec = torch.Size((P, d))
-    with _OnStream(residual, stream) as s:
+    vec, dev = torch.Size((P, d)), residual.get_device()
+    with _on_stream(residual, stream) as s:
         if residual_out is None:
-            residual_out = torch.empty(shape, dtype=residual.dtype, device=residual.device)
+            residual_out = residual.new_empty(shape)
         if out is None and w_pre is not None:
-            out = torch.empty(shape, dtype=residual.dtype, device=residual.device)
+            out = residual.new_empty(shape)
         args = _NORM_ARGS.pack(
-            P, n, d, DTYPES[residual.dtype], eps,
-            *_matrix(y, shape, residual, "y"), *_matrix(residual, shape, residual, "residual"),
-            *_matrix(w_post, vec, residual, "w_post"), *_matrix(gate, vec, residual, "gate"),
-            *_matrix(scale, vec, residual, "scale"), *_matrix(w_pre, vec, residual, "w_pre"),
-            *_matrix(residual_out, shape, residual, "residual_out"), *_matrix(out, shape, residual, "out"),
-            *(_NONE * 8), 0, 0)
+            P, n, d, DTYPES[dtype], eps,
+            *_matrix(y, shape, dtype, dev, "y"), *_matrix(residual, shape, dtype, dev, "residual"),
+            *_vector(w_post, vec, dtype, dev, "w_post"), *_vector(gate, vec, dtype, dev, "gate"),
+            *_vector(scale, vec, dtype, dev, "scale"), *_vector(w_pre, vec, dtype, dev, "w_pre"),
+            *_matrix(residual_out, shape, dtype, dev, "residual_out"), *_matrix(out, shape, dtype, dev, "out"), *_NONE8, 0, 0)
         if n:
-            _check(lib, lib.eg_residual_norm(args, s), None, "eg_residual_norm")
+            st = lib.eg_residual_norm(args, s)
+            if st:
+                _check(lib, st, None, "eg_residual_norm")
     return residual_out, out
 
 
@@ -556,48 +585,49 @@ def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Option
     ``d_weights``: four ``[P, width]`` tensors that receive the last ones (views of a gradient buffer in
     the step's layout, say; None for a vector that was not given); default: new tensors."""
     lib = load_library()
-    if residual.dim() != 3 or residual.dtype not in DTYPES:
+    shape, dtype = residual.shape, residual.dtype
+    if len(shape) != 3 or dtype not in DTYPES:
         raise EventGradError("residual_norm_backward: residual must be [P, rows, width] fp32, bf16 or fp16")
-    shape = residual.shape
     P, n, d = shape
-    vec = torch.Size((P, d))
-    new = dict(dtype=residual.dtype, device=residual.device)
-    weights = (w_post, gate, scale, w_pre)
-    with _OnStream(residual, stream) as s:
+    vec, dev = torch.Size((P, d)), residual.get_device()
+    with _on_stream(residual, stream) as s:
         if d_weights is None:
-            d_weights = tuple(None if w is None else torch.empty(vec, **new) for w in weights)
+            d_weights = tuple(None if w is None else residual.new_empty(vec) for w in (w_post, gate, scale, w_pre))
         elif len(d_weights) != 4:
             raise EventGradError("residual_norm_backward: d_weights holds four tensors or None")
-        dy = None if y is None else torch.empty(shape, **new)
-        dr = torch.empty(shape, **new)
+        dy = None if y is None else residual.new_empty(shape)
+        dr = residual.new_empty(shape)
         bytes_ = lib.eg_residual_norm_workspace(P, d)
-        workspace = torch.empty(bytes_, dtype=torch.uint8, device=residual.device)
+        workspace = residual.new_empty(bytes_, dtype=torch.uint8)
+        g = d_weights
         args = _NORM_ARGS.pack(
-            P, n, d, DTYPES[residual.dtype], eps,
-            *_matrix(y, shape, residual, "y"), *_matrix(residual, shape, residual, "residual"),
-            *_matrix(w_post, vec, residual, "w_post"), *_matrix(gate, vec, residual, "gate"),
-            *_matrix(scale, vec, residual, "scale"), *_matrix(w_pre, vec, residual, "w_pre"), *(_NONE * 2),
-            *_matrix(d_residual_out, shape, residual, "d_residual_out"), *_matrix(d_out, shape, residual, "d_out"),
-            *_matrix(dy, shape, residual, "dy"), *_matrix(dr, shape, residual, "d_residual"),
-            *_matrix(d_weights[0], vec, residual, "d_w_post"), *_matrix(d_weights[1], vec, residual, "d_gate"),
-            *_matrix(d_weights[2], vec, residual, "d_scale"), *_matrix(d_weights[3], vec, residual, "d_w_pre"),
+            P, n, d, DTYPES[dtype], eps,
+            *_matrix(y, shape, dtype, dev, "y"), *_matrix(residual, shape, dtype, dev, "residual"),
+            *_vector(w_post, vec, dtype, dev, "w_post"), *_vector(gate, vec, dtype, dev, "gate"),
+            *_vector(scale, vec, dtype, dev, "scale"), *_vector(w_pre, vec, dtype, dev, "w_pre"), *_NONE, *_NONE,
+            *_matrix(d_residual_out, shape, dtype, dev, "d_residual_out"), *_matrix(d_out, shape, dtype, dev, "d_out"),
+            *_matrix(dy, shape, dtype, dev, "dy"), *_matrix(dr, shape, dtype, dev, "d_residual"),
+            *_vector(g[0], vec, dtype, dev, "d_w_post"), *_vector(g[1], vec, dtype, dev, "d_gate"),
+            *_vector(g[2], vec, dtype, dev, "d_scale"), *_vector(g[3], vec, dtype, dev, "d_w_pre"),
             workspace.data_ptr(), bytes_)
         if n:
             _check(lib, lib.eg_residual_norm_backward(args, s), None, "eg_residual_norm_backward")
         else:
-            for t in d_weights:
+            for t in g:
                 if t is not None:
                     t.zero_()
     return dy, dr, tuple(d_weights)
 
 
 def _ffn_sizes(x: torch.Tensor, w_gate: torch.Tensor, activation: str, what: str):
-    if x.dim() != 3 or w_gate.dim() != 3 or x.dtype not in DTYPES:
+    shape, up = x.shape, w_gate.shape
+    if len(shape) != 3 or len(up) != 3 or x.dtype not in DTYPES:
         raise EventGradError(f"{what}: x must be [P, rows, d_model] and w_gate [P, d_ff, d_model], fp32, bf16 or fp16")
     if activation not in ACTIVATIONS:
         raise EventGradError(f"{what}: activation must be one of {sorted(ACTIVATIONS)}")
-    P, n, d = x.shape
-    return P, n, d, w_gate.shape[1]
+    P, n, d = shape
+    f = up[1]
+    return P, n, d, f, torch.Size((P, f, d)), torch.Size((P, d, f))
 
 
 def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
@@ -609,23 +639,25 @@ def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_do
     (views of a parameter buffer, say).  With ``save`` returns ``(y, saved)``, the second for
     ``feed_forward_backward``."""
     lib = load_library()
-    P, n, d, f = _ffn_sizes(x, w_gate, activation, "feed_forward")
-    up, down = torch.Size((P, f, d)), torch.Size((P, d, f))
-    with _OnStream(x, stream) as s:
+    P, n, d, f, up, down = _ffn_sizes(x, w_gate, activation, "feed_forward")
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
+    with _on_stream(x, stream) as s:
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        head = (P, n, d, f, DTYPES[x.dtype], ACTIVATIONS[activation], *_matrix(x, x.shape, x, "x"),
-                *_matrix(w_gate, up, x, "w_gate"), *_matrix(w_up, up, x, "w_up"), *_matrix(w_down, down, x, "w_down"),
-                *_matrix(out, x.shape, x, "out"), *(_NONE * 5))
+            out = x.new_empty(shape)
+        head = (P, n, d, f, DTYPES[dtype], ACTIVATIONS[activation], *_matrix(x, shape, dtype, dev, "x"),
+                *_matrix(w_gate, up, dtype, dev, "w_gate"), *_matrix(w_up, up, dtype, dev, "w_up"),
+                *_matrix(w_down, down, dtype, dev, "w_down"), *_matrix(out, shape, dtype, dev, "out"), *_NONE5)
         saved, saved_bytes = None, 0
         if save:
             saved_bytes = lib.eg_feed_forward_saved_bytes(_FFN_ARGS.pack(*head, 0, 0))
-            saved = torch.empty(saved_bytes, dtype=torch.uint8, device=x.device)
+            saved = x.new_empty(saved_bytes, dtype=torch.uint8)
         if n:
             args = _FFN_ARGS.pack(*head, saved.data_ptr() if save else 0, saved_bytes)
             bytes_ = lib.eg_feed_forward_workspace(args, 0)
-            workspace = torch.empty(bytes_, dtype=torch.uint8, device=x.device)
-            _check(lib, lib.eg_feed_forward(args, workspace.data_ptr(), bytes_, s), None, "eg_feed_forward")
+            workspace = x.new_empty(bytes_, dtype=torch.uint8).data_ptr() if bytes_ else 0
+            st = lib.eg_feed_forward(args, workspace, bytes_, s)
+            if st:
+                _check(lib, st, None, "eg_feed_forward")
     return (out, saved) if save else out
 
 
@@ -638,24 +670,25 @@ def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
     ``d_weights``: three tensors of the weights' shapes that receive the last ones (views of a gradient
     buffer in the step's layout, say; None: not wanted); default: new tensors."""
     lib = load_library()
-    P, n, d, f = _ffn_sizes(x, w_gate, activation, "feed_forward_backward")
-    up, down = torch.Size((P, f, d)), torch.Size((P, d, f))
-    if not saved.is_cuda or saved.dtype != torch.uint8 or not saved.is_contiguous():
+    P, n, d, f, up, down = _ffn_sizes(x, w_gate, activation, "feed_forward_backward")
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
+    if saved.get_device() != dev or saved.dtype is not torch.uint8 or not saved.is_contiguous():
         raise EventGradError("feed_forward_backward: saved is what feed_forward(..., save=True) returned")
-    with _OnStream(x, stream) as s:
+    with _on_stream(x, stream) as s:
         if d_weights is None:
-            d_weights = tuple(torch.empty(sh, dtype=x.dtype, device=x.device) for sh in (up, up, down))
+            d_weights = tuple(x.new_empty(sh) for sh in (up, up, down))
         elif len(d_weights) != 3:
             raise EventGradError("feed_forward_backward: d_weights holds three tensors or None")
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = x.new_empty(shape)
         args = _FFN_ARGS.pack(
-            P, n, d, f, DTYPES[x.dtype], ACTIVATIONS[activation], *_matrix(x, x.shape, x, "x"),
-            *_matrix(w_gate, up, x, "w_gate"), *_matrix(w_up, up, x, "w_up"), *_matrix(w_down, down, x, "w_down"),
-            *_NONE, *_matrix(dy, x.shape, x, "dy"), *_matrix(dx, x.shape, x, "dx"), *_matrix(d_weights[0], up, x, "d_gate"),
-            *_matrix(d_weights[1], up, x, "d_up"), *_matrix(d_weights[2], down, x, "d_down"),
+            P, n, d, f, DTYPES[dtype], ACTIVATIONS[activation], *_matrix(x, shape, dtype, dev, "x"),
+            *_matrix(w_gate, up, dtype, dev, "w_gate"), *_matrix(w_up, up, dtype, dev, "w_up"),
+            *_matrix(w_down, down, dtype, dev, "w_down"), *_NONE, *_matrix(dy, shape, dtype, dev, "dy"),
+            *_matrix(dx, shape, dtype, dev, "dx"), *_matrix(d_weights[0], up, dtype, dev, "d_gate"),
+            *_matrix(d_weights[1], up, dtype, dev, "d_up"), *_matrix(d_weights[2], down, dtype, dev, "d_down"),
             saved.data_ptr(), saved.numel())
         bytes_ = lib.eg_feed_forward_workspace(args, 1)
-        workspace = torch.empty(bytes_, dtype=torch.uint8, device=x.device)
+        workspace = x.new_empty(bytes_, dtype=torch.uint8)
         _check(lib, lib.eg_feed_forward_backward(args, workspace.data_ptr(), bytes_, s), None, "eg_feed_forward_backward")
     return dx, tuple(d_weights)
 
