@@ -5,8 +5,11 @@
 //             2. y = H Wd^T
 //   backward  3. dH = dy Wd with dG, dU formed from the accumulators and the saved G, U
 //             4. dx = dG Wg + dU Wu,  dWd = dy^T H,  dWg = dG^T x,  dWu = dU^T x           (one launch)
-#include <cstring>
+//
+// Without `saved`, few tokens take two streams over the weights instead (eg_ffn_few.cuh).
+#include <initializer_list>
 
+#include "eg_ffn_few.cuh"
 #include "eg_gemm.cuh"
 
 namespace eg {
@@ -60,32 +63,46 @@ bool encode(CUtensorMap* map, int dtype, const Mat& m, long long P, long long ro
 }
 
 // ----------------------------------------------------------------------------------- copies
-// Rows of any stride and alignment to rows on 16-byte boundaries; one warp per row.
-template <typename T>
-__global__ void __launch_bounds__(256) k_repack(Mat src, Mat dst, long long P, long long rows, int cols) {
-    const int lane = threadIdx.x & 31;
-    for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < P * rows; u += (long long)gridDim.x * 8) {
-        const long long i = u / rows, r = u % rows;
-        const T* s = static_cast<const T*>(src.p) + i * src.rep + r * src.row;
-        T* d = static_cast<T*>(dst.p) + i * dst.rep + r * dst.row;
-#pragma unroll 4
-        for (int c = lane; c < cols; c += 32) d[c] = s[c];
-    }
-}
+// Operands that the products cannot read in place: 16-bit rows of any stride and alignment go to rows on 16-byte
+// boundaries, fp32 rows to their three bf16 parts (matrices `plane` elements apart).  One launch for all of a
+// call; a warp takes 512 columns of one row, all its loads ahead of its stores.
+constexpr int kCopyMax = 5, kCopyCols = 512;
+struct CopyArgs {
+    struct { Mat src, dst; long long plane, rows, begin; int cols, chunks; } m[kCopyMax];   // begin: first unit of the matrix
+    long long units;
+    int count;
+};
 
-// fp32 rows to their three bf16 parts (matrices `plane` elements apart).
-__global__ void __launch_bounds__(256) k_split(Mat src, Mat dst, long long plane, long long P, long long rows, int cols) {
+template <typename T> __global__ void __launch_bounds__(256) k_copy_in(const __grid_constant__ CopyArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
-    for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < P * rows; u += (long long)gridDim.x * 8) {
-        const long long i = u / rows, r = u % rows;
-        const float* s = static_cast<const float*>(src.p) + i * src.rep + r * src.row;
-        uint32_t* d = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(dst.p) + i * dst.rep + r * dst.row);
-#pragma unroll 2
-        for (int c = 2 * lane; c < cols; c += 64) {      // the pitch is even: a last odd column takes a zero along
-            uint32_t w[kParts];
-            split2(s[c], c + 1 < cols ? s[c + 1] : 0.f, w);
+    for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < a.units; u += (long long)gridDim.x * 8) {
+        int k = 0;
+        while (k + 1 < a.count && u >= a.m[k + 1].begin) ++k;
+        const auto& m = a.m[k];
+        const long long at = u - m.begin, line = at / m.chunks, i = line / m.rows, r = line % m.rows;
+        const int c0 = (int)(at % m.chunks) * kCopyCols + 2 * lane;
+        const T* s = static_cast<const T*>(m.src.p) + i * m.src.rep + r * m.src.row;
+        uint16_t* d = static_cast<uint16_t*>(m.dst.p) + i * m.dst.rep + r * m.dst.row;
+        T v[kCopyCols / 32];
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) d[(k * plane + c) / 2] = w[k];
+        for (int q = 0; q < kCopyCols / 64; ++q) {      // the pitch is even: a last odd column takes a zero along
+            const int c = c0 + q * 64;
+            v[2 * q] = c < m.cols ? s[c] : T(0);
+            v[2 * q + 1] = c + 1 < m.cols ? s[c + 1] : T(0);
+        }
+#pragma unroll
+        for (int q = 0; q < kCopyCols / 64; ++q) {
+            const int c = c0 + q * 64;
+            if (c >= m.cols) continue;
+            if constexpr (sizeof(T) == 4) {
+                uint32_t w[kParts];
+                split2(v[2 * q], v[2 * q + 1], w);
+#pragma unroll
+                for (int z = 0; z < kParts; ++z) *reinterpret_cast<uint32_t*>(d + z * m.plane + c) = w[z];
+            } else {
+                *reinterpret_cast<uint32_t*>(d + c) = (uint32_t)v[2 * q] | (uint32_t)v[2 * q + 1] << 16;
+            }
         }
     }
 }
@@ -116,6 +133,7 @@ struct Block {
     Operand x, wg, wu, wd, dy;
     Mat g, u;
     Operand h, dg, du;
+    int few = 0;                                  // 1: k_few_mma, 2: k_few_dot; 0: tiles
 };
 
 Mat mat(const eg_matrix& m) { return Mat{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
@@ -166,6 +184,18 @@ long long saved_bytes(const eg_feed_forward_args* q) {
     return q->P * q->rows * pitch_of(q->d_ff) * (q->dtype == EG_F32 ? 2 * 4 + 2 * kParts : 3 * 2);
 }
 
+// Which kernels a forward call without `saved` takes.  Measured at d_model 1024, d_ff 2816, 4 replicas, bf16:
+// (see k_few_mma) streams 13 us for 1 token; tiles FEW_TABLE.
+int few_kind(const eg_feed_forward_args* q) {
+    if (q->saved || q->P > 65535) return 0;
+    const size_t size = q->dtype == EG_F32 ? 4 : 2;
+    const bool rows16 = in_place(mat(q->x), q->P, q->rows, size) && in_place(mat(q->w_gate), q->P, q->d_ff, size) &&
+                        in_place(mat(q->w_up), q->P, q->d_ff, size) && in_place(mat(q->w_down), q->P, q->d_model, size) &&
+                        q->d_model * size % 16 == 0 && q->d_ff * size % 16 == 0;
+    if (q->dtype != EG_F32 && rows16 && q->rows <= kFewMmaTokens) return 1;
+    return q->rows <= kFewDotTokens ? 2 : 0;
+}
+
 void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
     b->q = q;
     b->P = q->P; b->n = q->rows; b->d = q->d_model; b->f = q->d_ff;
@@ -173,6 +203,10 @@ void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
     b->dtype = (int)q->dtype;
     b->size = q->dtype == EG_F32 ? 4 : 2;
     b->parts = q->dtype == EG_F32 ? kParts : 1;
+    if (!backward && (b->few = few_kind(q)) != 0) {
+        b->h.use = Mat{w->take(b->P * b->n * b->fp * (long long)b->size), b->n * b->fp, b->fp};
+        return;
+    }
     place(&b->x, q->x, *b, b->n, b->d, w);
     place(&b->wg, q->w_gate, *b, b->f, b->d, w);
     place(&b->wu, q->w_up, *b, b->f, b->d, w);
@@ -197,12 +231,23 @@ void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
     }
 }
 
-cudaError_t copy_in(const Block& b, const Operand& o, cudaStream_t stream) {
-    if (!o.copied) return cudaSuccess;
-    const long long blocks = (b.P * o.rows + 7) / 8, most = (long long)sm_count() * 8;
+cudaError_t copy_in(const Block& b, std::initializer_list<const Operand*> operands, cudaStream_t stream) {
+    CopyArgs a;
+    a.count = 0;
+    a.units = 0;
+    for (const Operand* o : operands) {
+        if (!o->copied) continue;
+        auto& m = a.m[a.count++];
+        m.src = o->src; m.dst = o->use; m.plane = o->plane; m.rows = o->rows; m.cols = (int)o->cols;
+        m.chunks = (m.cols + kCopyCols - 1) / kCopyCols;
+        m.begin = a.units;
+        a.units += b.P * o->rows * m.chunks;
+    }
+    if (a.units == 0) return cudaSuccess;
+    const long long blocks = (a.units + 7) / 8, most = (long long)sm_count() * 8;
     const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-    if (b.dtype == EG_F32) k_split<<<grid, 256, 0, stream>>>(o.src, o.use, o.plane, b.P, o.rows, (int)o.cols);
-    else k_repack<uint16_t><<<grid, 256, 0, stream>>>(o.src, o.use, b.P, o.rows, (int)o.cols);
+    if (b.dtype == EG_F32) k_copy_in<float><<<grid, 256, 0, stream>>>(a);
+    else k_copy_in<uint16_t><<<grid, 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -258,17 +303,23 @@ struct Builder {
         g->tiles = (int)tiles;
         a.tiles += g->tiles;
         g->nseg = 0;
+        g->small = 0;
         g->a_mn = a_mn; g->b_mn = b_mn; g->b_pair = pair;
         g->M = (int)M; g->N = (int)N;
         g->out = -1;
         return g;
     }
-    // A B^T over K, as products of parts, the smallest ones first
-    void product(GemmProblem* g, int ma, int mb0, int mb1, long long K) {
+    // sum of A B^T over K of one or two pairs, as products of parts, the smaller ones first
+    struct Pair { int ma, mb0, mb1; };
+    void product(GemmProblem* g, std::initializer_list<Pair> pairs, long long K) {
+        const int ksteps = (int)((K + kGemmK - 1) / kGemmK);
         for (int sum = b.parts - 1; sum >= 0; --sum) {
-            for (int i = 0; i <= sum; ++i) {
-                if (g->nseg >= kGemmMaxSegs) { ok = false; return; }
-                g->seg[g->nseg++] = GemmSeg{ma + i, mb0 + sum - i, mb1 + sum - i, (int)((K + kGemmK - 1) / kGemmK)};
+            for (const Pair& p : pairs) {
+                for (int i = 0; i <= sum; ++i) {
+                    if (g->nseg >= kGemmMaxSegs) { ok = false; return; }
+                    g->seg[g->nseg++] = GemmSeg{p.ma + i, p.mb0 + sum - i, p.mb1 + sum - i, ksteps};
+                    if (sum > 0) g->small += ksteps;
+                }
             }
         }
     }
@@ -312,31 +363,61 @@ template <typename T, int EPI> cudaError_t launch_gemm(const Builder& w, cudaStr
     return cudaErrorInvalidValue;
 }
 
-// The widest tile that still gives every pair of multiprocessors one; `cols` columns of the result
-// for a tile of 256.
-int tile_width(const Block& b, long long M, long long N, int cols, int least) {
-    const long long mt = (M + kGemmM - 1) / kGemmM, P = b.P;
-    int bn = 256;
-    if (b.dtype == EG_F32) {           // the sums of a tile in registers: 64 a thread
-        bn = 128;
-        cols /= 2;
+// Tile width of a launch: the one whose last pair of multiprocessors should be done first.  A stage of 64 of K
+// takes 2 cycles a column of the tile on the tensor cores, but no less than 300 for its copies and barriers;
+// filling and draining a tile's pipeline costs about 2500 and its epilogue 8 a column.  `cols`: columns of the
+// result for a tile of 256.
+int tile_width(const Block& b, long long M, long long N, long long K, int cols, int least) {
+    const long long mt = (M + kGemmM - 1) / kGemmM, ksteps = (K + kGemmK - 1) / kGemmK * (b.dtype == EG_F32 ? 6 : 1);
+    const long long pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+    int best = 0;
+    long long best_time = 0;
+    for (int bn = b.dtype == EG_F32 ? 128 : 256; bn >= least; bn /= 2) {       // fp32: a tile's sums in registers, 64 a thread
+        const long long c = (long long)cols * bn / 256, tiles = b.P * mt * ((N + c - 1) / c), waves = (tiles + pairs - 1) / pairs;
+        const long long time = waves * (ksteps * (2 * bn > 300 ? 2 * bn : 300) + 8 * bn) + 2500;
+        if (!best || time < best_time) {
+            best = bn;
+            best_time = time;
+        }
     }
-    while (bn > least && P * mt * ((N + cols - 1) / cols) < sm_count() / 2) {
-        bn /= 2;
-        cols /= 2;
+    return best;
+}
+
+template <typename T> cudaError_t few_tokens(const Block& b, cudaStream_t stream) {
+    const eg_feed_forward_args* q = b.q;
+    FewArgs up{q->w_gate.data, q->w_up.data, q->w_gate.replica_stride, q->w_gate.row_stride, q->w_up.replica_stride,
+               q->w_up.row_stride, q->x.data, q->x.replica_stride, q->x.row_stride, b.h.use.p, b.h.use.rep, b.h.use.row,
+               (int)b.P, (int)b.n, (int)b.f, (int)b.d, (int)q->activation, 1};
+    FewArgs down{q->w_down.data, nullptr, q->w_down.replica_stride, q->w_down.row_stride, 0, 0, b.h.use.p, b.h.use.rep,
+                 b.h.use.row, q->y.data, q->y.replica_stride, q->y.row_stride, (int)b.P, (int)b.n, (int)b.d, (int)b.f, (int)q->activation, 1};
+    cudaError_t e;
+    if constexpr (sizeof(T) == 2) {
+        if (b.few == 1) {
+            e = launch_few_mma<T, true>(up, stream);
+            return e != cudaSuccess ? e : launch_few_mma<T, false>(down, stream);
+        }
     }
-    return bn;
+    const bool v = sizeof(T) == 4 && in_place(mat(q->x), b.P, b.n, 4) && in_place(mat(q->w_gate), b.P, b.f, 4) &&
+                   in_place(mat(q->w_up), b.P, b.f, 4) && in_place(mat(q->w_down), b.P, b.d, 4) && b.d % 4 == 0 && b.f % 4 == 0;
+    if constexpr (sizeof(T) == 4) {
+        if (v) {
+            e = launch_few_dot<T, 4, true>(up, (int)b.P, stream);
+            return e != cudaSuccess ? e : launch_few_dot<T, 4, false>(down, (int)b.P, stream);
+        }
+    }
+    e = launch_few_dot<T, 1, true>(up, (int)b.P, stream);
+    return e != cudaSuccess ? e : launch_few_dot<T, 1, false>(down, (int)b.P, stream);
 }
 
 template <typename T> cudaError_t forward(const Block& b, unsigned int* err, cudaStream_t stream) {
+    if (b.few) return few_tokens<T>(b, stream);
     cudaError_t e;
-    for (const Operand* o : {&b.x, &b.wg, &b.wu, &b.wd})
-        if ((e = copy_in(b, *o, stream)) != cudaSuccess) return e;
+    if ((e = copy_in(b, {&b.x, &b.wg, &b.wu, &b.wd}, stream)) != cudaSuccess) return e;
     {
-        Builder w(b, tile_width(b, b.n, b.f, 128, b.dtype == EG_F32 ? 128 : 64), err);
+        Builder w(b, tile_width(b, b.n, b.f, b.d, 128, b.dtype == EG_F32 ? 128 : 64), err);
         GemmProblem* g = w.problem(b.n, b.f, false, false, true);
         const int mx = w.operand(b.x, false, true), mg = w.operand(b.wg, false, false), mu = w.operand(b.wu, false, false);
-        w.product(g, mx, mg, mu, b.d);
+        w.product(g, {{mx, mg, mu}}, b.d);
         const int box = w.BN / 4 < 32 ? w.BN / 4 : 32;
         w.a.map_h = w.boxes(b.h, box);
         if (b.q->saved) {
@@ -345,10 +426,10 @@ template <typename T> cudaError_t forward(const Block& b, unsigned int* err, cud
         }
         if ((e = launch_gemm<T, kEpiGateUp>(w, stream)) != cudaSuccess) return e;
     }
-    Builder w(b, tile_width(b, b.n, b.d, 256, 32), err);
+    Builder w(b, tile_width(b, b.n, b.d, b.f, 256, 32), err);
     GemmProblem* g = w.problem(b.n, b.d, false, false, false);
     const int mb = w.operand(b.wd, false, false);
-    w.product(g, w.operand(b.h, false, true), mb, mb, b.f);
+    w.product(g, {{w.operand(b.h, false, true), mb, mb}}, b.f);
     w.store_to(g, mat(b.q->y), b.n, b.d);
     return launch_gemm<T, kEpiStore>(w, stream);
 }
@@ -356,13 +437,12 @@ template <typename T> cudaError_t forward(const Block& b, unsigned int* err, cud
 template <typename T> cudaError_t backward(const Block& b, unsigned int* err, cudaStream_t stream) {
     cudaError_t e;
     const eg_feed_forward_args* q = b.q;
-    for (const Operand* o : {&b.x, &b.wg, &b.wu, &b.wd, &b.dy})
-        if ((e = copy_in(b, *o, stream)) != cudaSuccess) return e;
+    if ((e = copy_in(b, {&b.x, &b.wg, &b.wu, &b.wd, &b.dy}, stream)) != cudaSuccess) return e;
     {
-        Builder w(b, tile_width(b, b.n, b.f, 256, 128), err);
+        Builder w(b, tile_width(b, b.n, b.f, b.d, 256, 128), err);
         GemmProblem* g = w.problem(b.n, b.f, false, true, false);
         const int mb = w.operand(b.wd, true, false);
-        w.product(g, w.operand(b.dy, false, true), mb, mb, b.d);
+        w.product(g, {{w.operand(b.dy, false, true), mb, mb}}, b.d);
         w.a.map_g = w.boxes(b.g, 32);
         w.a.map_u = w.boxes(b.u, 32);
         w.a.map_dg = w.boxes(b.dg, 32);
@@ -373,8 +453,8 @@ template <typename T> cudaError_t backward(const Block& b, unsigned int* err, cu
     if (q->dx.data) {
         GemmProblem* g = w.problem(b.n, b.d, false, true, false);
         const int mg = w.operand(b.wg, true, false), mu = w.operand(b.wu, true, false);
-        w.product(g, w.operand(b.dg, false, true), mg, mg, b.f);
-        w.product(g, w.operand(b.du, false, true), mu, mu, b.f);
+        const int ag = w.operand(b.dg, false, true), au = w.operand(b.du, false, true);
+        w.product(g, {{ag, mg, mg}, {au, mu, mu}}, b.f);
         w.store_to(g, mat(q->dx), b.n, b.d);
     }
     struct { const eg_matrix* out; const Operand *a, *bm; long long M, N; } grads[] = {
@@ -383,7 +463,7 @@ template <typename T> cudaError_t backward(const Block& b, unsigned int* err, cu
         if (!t.out->data) continue;
         GemmProblem* g = w.problem(t.M, t.N, true, true, false);
         const int mb = w.operand(*t.bm, true, false);
-        w.product(g, w.operand(*t.a, true, true), mb, mb, b.n);
+        w.product(g, {{w.operand(*t.a, true, true), mb, mb}}, b.n);
         w.store_to(g, mat(*t.out), t.M, t.N);
     }
     return launch_gemm<T, kEpiStore>(w, stream);

@@ -39,9 +39,10 @@ struct GemmSeg {
     int ksteps;
 };
 
-// Tensor-core sums of fp32 parts are moved to registers and added there every kChunk stages: adding into the
-// accumulator truncates (about 3e-8 of it per instruction, always towards zero, so the error grows with
-// K: 5e-6 after 2816), an fp32 addition in registers rounds.  4 stages are 16 instructions, 5e-7 at most.
+// Adding into the accumulator truncates: about 3e-8 of it per instruction, always towards zero, so that the
+// error of a sum grows with K (5e-6 after 2816).  In fp32 the accumulator is therefore moved to registers,
+// where an addition rounds, every kChunk stages of the products of first parts (16 instructions: 5e-7 at most).
+// The products of smaller parts come first, all in one accumulator: they are 2^-8 of the sum, and so is their error.
 constexpr int kChunk = 4;
 constexpr int kParts = 3;
 enum { kEpiStore = 0, kEpiGateUp = 1, kEpiDact = 2 };
@@ -50,6 +51,7 @@ struct GemmProblem {
     int tiles, mt, nt;                            // all tiles; tiles of one replica
     int nseg;
     GemmSeg seg[kGemmMaxSegs];
+    int small;                                    // fp32: stages of the products of smaller parts, which come first
     int a_mn, b_mn;                               // the operand's K runs along its rows
     int b_pair;                                   // B of the two CTAs are two matrices, same rows
     int M, N;                                     // of the result
@@ -386,7 +388,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                                        ((uint32_t)(kGemmM >> 4) << 24);
                 const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
                 uint32_t add = 0;
-                int in_chunk = 0;
+                int in_chunk = sizeof(T) == 4 ? kChunk - g.small : 0;    // reaches kChunk where the accumulator is handed over
                 for (int e = 0; e < g.nseg; ++e) {
                     for (int k = 0; k < g.seg[e].ksteps; ++k) {
                         const int buf = count & 1;
@@ -440,7 +442,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
             if constexpr (sizeof(T) == 4) {
                 int ksteps = 0;
                 for (int e = 0; e < g.nseg; ++e) ksteps += g.seg[e].ksteps;
-                const int chunks = (ksteps + kChunk - 1) / kChunk;
+                const int chunks = (g.small > 0) + (ksteps - g.small + kChunk - 1) / kChunk;
 #pragma unroll
                 for (int x = 0; x < BN / 2; ++x) sum[x] = 0.f;
                 for (int z = 0; z < chunks; ++z, ++count) {
