@@ -382,7 +382,7 @@ int64_t eg_residual_norm_workspace(int64_t P, int64_t width);
  * x, y, dy, dx: `rows` x d_model per replica; w_gate, w_up and their gradients: d_ff x d_model;
  * w_down and its gradient: d_model x d_ff; all of type dtype.  act: silu, gelu (with erf) or relu.
  * Products are summed in fp32.  In the 16-bit types H, dG and dU are rounded to the type (they
- * are operands of the next product), and so are G and U where the backward call reads them.
+ * are operands of the next product), and so are act(G) and U * act'(G), which the backward call reads.
  *
  * eg_feed_forward computes y.  With `saved` (device, 16-byte aligned, at least
  * eg_feed_forward_saved_bytes) it leaves what the backward call reads there.

@@ -3,7 +3,8 @@
 //
 //   forward   1. [G | U] = x [Wg | Wu]^T with H = act(G) * U formed from the accumulators   (one launch)
 //             2. y = H Wd^T
-//   backward  3. dH = dy Wd with dG, dU formed from the accumulators and the saved G, U
+//   backward  3. dH = dy Wd with dU = dH * act(G), dG = dH * U act'(G) formed from the accumulators and the
+//                saved factors (which the forward pass has in fp32: one rounding each, and no exponential here)
 //             4. dx = dG Wg + dU Wu,  dWd = dy^T H,  dWg = dG^T x,  dWu = dU^T x           (one launch)
 //
 // Without `saved`, few tokens take two streams over the weights instead (eg_ffn_few.cuh).
@@ -75,6 +76,7 @@ struct CopyArgs {
 
 template <typename T> __global__ void __launch_bounds__(256) k_copy_in(const __grid_constant__ CopyArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < a.units; u += (long long)gridDim.x * 8) {
         int k = 0;
@@ -131,7 +133,7 @@ struct Block {
     int dtype, parts;
     size_t size;
     Operand x, wg, wu, wd, dy;
-    Mat g, u;
+    Mat ma, mb;                                   // act(G), U act'(G): dU and dG are dH times these
     Operand h, dg, du;
     int few = 0;                                  // 1: k_few_mma, 2: k_few_dot; 0: tiles
 };
@@ -179,7 +181,7 @@ bool valid(const eg_feed_forward_args* q, bool backward) {
     return true;
 }
 
-// Layout of `saved`: G, U, each [P][rows][fp] of the type, then H (fp32: its three parts).
+// Layout of `saved`: act(G), U act'(G), each [P][rows][fp] of the type, then H (fp32: its three parts).
 long long saved_bytes(const eg_feed_forward_args* q) {
     return q->P * q->rows * pitch_of(q->d_ff) * (q->dtype == EG_F32 ? 2 * 4 + 2 * kParts : 3 * 2);
 }
@@ -213,8 +215,8 @@ void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
     place(&b->wd, q->w_down, *b, b->d, b->f, w);
     const long long plane = b->P * b->n * b->fp;
     char* s = static_cast<char*>(q->saved);
-    b->g = Mat{s, b->n * b->fp, b->fp};
-    b->u = Mat{s ? s + plane * b->size : nullptr, b->n * b->fp, b->fp};
+    b->ma = Mat{s, b->n * b->fp, b->fp};
+    b->mb = Mat{s ? s + plane * b->size : nullptr, b->n * b->fp, b->fp};
     auto hidden = [&](Operand* o, void* p) {
         o->use = Mat{p, b->n * b->fp, b->fp};
         o->plane = plane;
@@ -246,9 +248,8 @@ cudaError_t copy_in(const Block& b, std::initializer_list<const Operand*> operan
     if (a.units == 0) return cudaSuccess;
     const long long blocks = (a.units + 7) / 8, most = (long long)sm_count() * 8;
     const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-    if (b.dtype == EG_F32) k_copy_in<float><<<grid, 256, 0, stream>>>(a);
-    else k_copy_in<uint16_t><<<grid, 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return b.dtype == EG_F32 ? launch_after(k_copy_in<float>, dim3(grid), dim3(256), 0, stream, a)
+                             : launch_after(k_copy_in<uint16_t>, dim3(grid), dim3(256), 0, stream, a);
 }
 
 // ----------------------------------------------------------------------------------- products
@@ -264,7 +265,7 @@ struct Builder {
         a.idesc = (1u << 4) | (b.dtype != EG_F16 ? (1u << 7) | (1u << 10) : 0u);
         a.err = err;
         a.act = (int)b.q->activation;
-        a.map_g = a.map_u = a.map_h = a.map_dg = a.map_du = -1;
+        a.map_a = a.map_b = a.map_h = a.map_dg = a.map_du = -1;
     }
     int map(const Mat& m, int dtype, long long rows, long long cols, int box_cols, int box_rows) {
         if (maps >= kGemmMaxMaps) { ok = false; return 0; }
@@ -343,8 +344,7 @@ template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& 
     }
     const int pairs = sm_count() / 2;
     if (pairs < 1) return cudaErrorInvalidDevice;
-    k_gemm<T, EPI, BN><<<2 * (a.tiles < pairs ? a.tiles : pairs), kGemmThreads, Shape::kSmem, stream>>>(a);
-    return cudaGetLastError();
+    return launch_after(k_gemm<T, EPI, BN>, dim3(2 * (a.tiles < pairs ? a.tiles : pairs)), dim3(kGemmThreads), Shape::kSmem, stream, a);
 }
 
 template <typename T, int EPI> cudaError_t launch_gemm(const Builder& w, cudaStream_t stream) {
@@ -421,8 +421,8 @@ template <typename T> cudaError_t forward(const Block& b, unsigned int* err, cud
         const int box = w.BN / 4 < 32 ? w.BN / 4 : 32;
         w.a.map_h = w.boxes(b.h, box);
         if (b.q->saved) {
-            w.a.map_g = w.boxes(b.g, box);
-            w.a.map_u = w.boxes(b.u, box);
+            w.a.map_a = w.boxes(b.ma, box);
+            w.a.map_b = w.boxes(b.mb, box);
         }
         if ((e = launch_gemm<T, kEpiGateUp>(w, stream)) != cudaSuccess) return e;
     }
@@ -443,8 +443,8 @@ template <typename T> cudaError_t backward(const Block& b, unsigned int* err, cu
         GemmProblem* g = w.problem(b.n, b.f, false, true, false);
         const int mb = w.operand(b.wd, true, false);
         w.product(g, {{w.operand(b.dy, false, true), mb, mb}}, b.d);
-        w.a.map_g = w.boxes(b.g, 32);
-        w.a.map_u = w.boxes(b.u, 32);
+        w.a.map_a = w.boxes(b.ma, 32);
+        w.a.map_b = w.boxes(b.mb, 32);
         w.a.map_dg = w.boxes(b.dg, 32);
         w.a.map_du = w.boxes(b.du, 32);
         if ((e = launch_gemm<T, kEpiDact>(w, stream)) != cudaSuccess) return e;

@@ -45,6 +45,13 @@ template <typename T> __device__ __forceinline__ float few_result(int act, float
     return h;
 }
 
+// The first kernel of a call waits for whatever came before and only then lets the second one start: the second
+// reads its first weights without waiting, and what came before the call may have written them.
+template <bool GATE> __device__ __forceinline__ void few_begin() {
+    if (GATE) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // A unit is 16 outputs of a replica; a CTA takes units blockIdx.x, blockIdx.x + gridDim.x, ...  The weights of the
 // next unit are on their way while the sums of this one are put together.  NT: eights of tokens.
 template <typename T, int NT, bool GATE>
@@ -52,7 +59,6 @@ __global__ void __launch_bounds__(256, 2) k_few_mma(const FewArgs a) {
     constexpr int W = GATE ? 2 : 1, BATCH = GATE ? 4 : 6;
     constexpr int ROW = NT * 8 + 1, WARPS = 8;
     __shared__ float s_part[WARPS][W][16][ROW];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, q = lane & 3;
     const int steps = (a.K + 31) / 32, blocks = (a.rows + 15) / 16;
@@ -75,8 +81,9 @@ __global__ void __launch_bounds__(256, 2) k_few_mma(const FewArgs a) {
         }
     };
     long long unit = blockIdx.x;
+    few_begin<GATE>();
     if (unit < units) fetch(unit, warp);
-    if (!GATE) asm volatile("griddepcontrol.wait;" ::: "memory");     // the first kernel of a call depends on nothing that still runs
+    if (!GATE) asm volatile("griddepcontrol.wait;" ::: "memory");
     for (; unit < units; unit += gridDim.x) {
         const int p = (int)(unit / blocks), row0 = (int)(unit % blocks) * 16;
         const T* x = static_cast<const T*>(a.x) + p * a.x_rep + g * a.x_row + q * 8;
@@ -138,7 +145,6 @@ template <typename T, int VEC, int N, int R, bool GATE>
 __global__ void __launch_bounds__(256) k_few_dot(const FewArgs a) {
     constexpr int OUT = GATE ? R / 2 : R;             // outputs of a unit
     __shared__ float s_part[8][R * N];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, p = blockIdx.y;
     const int unit = blockIdx.x * (8 / a.splits) + warp / a.splits, split = warp % a.splits;
     const int r0 = unit * OUT, count = min(OUT, a.rows - r0);
@@ -151,6 +157,7 @@ __global__ void __launch_bounds__(256) k_few_dot(const FewArgs a) {
 #pragma unroll
         for (int t = 0; t < N; ++t) acc[r][t] = 0.f;
     const int stride = a.splits * 32 * VEC;
+    few_begin<GATE>();
     bool waited = GATE;
     if (count > 0) {
         constexpr int BATCH = R * N <= 4 ? 4 : R * N <= 16 ? 2 : 1;
@@ -219,9 +226,7 @@ template <typename T, bool GATE> cudaError_t launch_few_mma(const FewArgs& a, cu
     const long long units = (long long)a.P * ((a.rows + 15) / 16), most = 2ll * sm_count();
     auto go = [&](auto kernel) {
         const dim3 grid((unsigned)(units < most ? units : most));
-        if (!GATE) return launch_after(kernel, grid, dim3(256), 0, stream, a);
-        kernel<<<grid, 256, 0, stream>>>(a);
-        return cudaGetLastError();
+        return launch_after(kernel, grid, dim3(256), 0, stream, a);
     };
     return a.n <= 8 ? go(k_few_mma<T, 1, GATE>) : go(k_few_mma<T, 2, GATE>);
 }
@@ -234,9 +239,7 @@ template <typename T, int VEC, bool GATE> cudaError_t launch_few_dot(FewArgs a, 
         while (a.splits > 1 && ((long long)units * P * a.splits > 32ll * sm_count() || a.K < a.splits * 32 * VEC)) a.splits /= 2;
         const int per = 8 / a.splits;
         const dim3 grid((units + per - 1) / per, P), block(256);
-        if (!GATE) return launch_after(kernel, grid, block, 0, stream, a);
-        kernel<<<grid, block, 0, stream>>>(a);
-        return cudaGetLastError();
+        return launch_after(kernel, grid, block, 0, stream, a);
     };
     if (a.n <= 1) return go(k_few_dot<T, VEC, 1, 2, GATE>, 2);
     if (a.n <= 2) return go(k_few_dot<T, VEC, 2, 4, GATE>, 4);

@@ -68,8 +68,8 @@ struct GemmArgs {
     unsigned int* err;
     // gate/up and activation-gradient epilogues: maps of 32 x 32 boxes
     int act;
-    int map_g, map_u, map_h;                      // G, U (-1: not wanted), H; of H, dG and dU the parts follow one
-    int map_dg, map_du;                           // another where the values are fp32
+    int map_a, map_b, map_h;                      // act(G), U act'(G) (-1: not wanted), H; of H, dG and dU the parts
+    int map_dg, map_du;                           // follow one another where the values are fp32
 };
 
 // ------------------------------------------------------------------------------- PTX
@@ -322,6 +322,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(const_cast<int*>(s_abort) + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         *s_abort = 0;
         for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
@@ -339,6 +340,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
+    // set up while the kernel before this one finished; from here on its results are read and overwritten
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (warp == 0) {
@@ -537,29 +540,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     if constexpr (sizeof(T) == 4) {
                         static_assert(CW == 32, "boxes of 32 columns");
                         const float *gs = sum + c, *us = sum + HW + c;
-                        float x[32];
+                        float x[32], y[32], z[32];
                         const bool in = row0 < g.M && col0 < g.N;
-                        if (a.map_g >= 0) {
+                        with_act(a.act, [&](auto act) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = gs[e];
-                            write_f32(buf_mem, lane, x);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = us[e];
-                            write_f32(buf_mem + 4096, lane, x);
+                            for (int e = 0; e < 32; ++e) {
+                                act_both<T, decltype(act)::value>(gs[e], y[e], z[e]);
+                                x[e] = y[e] * us[e];
+                                z[e] *= us[e];
+                            }
+                        });
+                        if (a.map_a >= 0) {
+                            write_f32(buf_mem, lane, y);
+                            write_f32(buf_mem + 4096, lane, z);
                             fence_async_shared();
                             __syncwarp();
                             if (elect_one()) {
                                 if (in) {
-                                    tma_store(&a.maps[a.map_g], buf_mem, col0, row0, q.p);
-                                    tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                                    tma_store(&a.maps[a.map_a], buf_mem, col0, row0, q.p);
+                                    tma_store(&a.maps[a.map_b], buf_mem + 4096, col0, row0, q.p);
                                 }
                                 store_commit();
                             }
                         }
-                        with_act(a.act, [&](auto act) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = act_value<T, decltype(act)::value>(gs[e]) * us[e];
-                        });
                         store_wait_read<0>();
                         __syncwarp();
                         write_parts(buf_mem, lane, x);
@@ -576,21 +579,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         with_act(a.act, [&](auto act) {
 #pragma unroll
                             for (int e = 0; e < CW; e += 8) {
-                                uint32_t og[4], ou[4], oh[4];
+                                uint32_t oa[4], ob[4], oh[4];
 #pragma unroll
                                 for (int z = 0; z < 4; ++z) {
-                                    const float g0 = __uint_as_float(gv[e + 2 * z]), g1 = __uint_as_float(gv[e + 2 * z + 1]);
                                     const float u0 = __uint_as_float(uv[e + 2 * z]), u1 = __uint_as_float(uv[e + 2 * z + 1]);
-                                    og[z] = pack2<T>(g0, g1);
-                                    ou[z] = pack2<T>(u0, u1);
-                                    oh[z] = pack2<T>(act_value<T, decltype(act)::value>(g0) * u0, act_value<T, decltype(act)::value>(g1) * u1);
+                                    float a0, d0, a1, d1;
+                                    act_both<T, decltype(act)::value>(__uint_as_float(gv[e + 2 * z]), a0, d0);
+                                    act_both<T, decltype(act)::value>(__uint_as_float(gv[e + 2 * z + 1]), a1, d1);
+                                    oa[z] = pack2<T>(a0, a1);
+                                    ob[z] = pack2<T>(d0 * u0, d1 * u1);
+                                    oh[z] = pack2<T>(a0 * u0, a1 * u1);
                                 }
                                 uint32_t off = lane * (CW * 2) + e * 2;
                                 off = CW == 32 ? swz64(off) : off;
                                 *reinterpret_cast<uint4*>(buf_mem + off) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-                                if (a.map_g >= 0) {
-                                    *reinterpret_cast<uint4*>(buf_mem + 2048 + off) = make_uint4(og[0], og[1], og[2], og[3]);
-                                    *reinterpret_cast<uint4*>(buf_mem + 4096 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                                if (a.map_a >= 0) {
+                                    *reinterpret_cast<uint4*>(buf_mem + 2048 + off) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
+                                    *reinterpret_cast<uint4*>(buf_mem + 4096 + off) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
                                 }
                             }
                         });
@@ -599,9 +604,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         if (elect_one()) {
                             if (row0 < g.M && col0 < g.N) {
                                 tma_store(&a.maps[a.map_h], buf_mem, col0, row0, q.p);
-                                if (a.map_g >= 0) {
-                                    tma_store(&a.maps[a.map_g], buf_mem + 2048, col0, row0, q.p);
-                                    tma_store(&a.maps[a.map_u], buf_mem + 4096, col0, row0, q.p);
+                                if (a.map_a >= 0) {
+                                    tma_store(&a.maps[a.map_a], buf_mem + 2048, col0, row0, q.p);
+                                    tma_store(&a.maps[a.map_b], buf_mem + 4096, col0, row0, q.p);
                                 }
                             }
                             store_commit();
@@ -609,7 +614,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     }
                 }
             } else if constexpr (sizeof(T) == 4) {
-                // D = dH in fp32.  G and U fill the staging memory; the parts of dG, then of dU take their place.
+                // D = dH in fp32.  act(G) and U act'(G) fill the staging memory; the parts of dG, then of dU take their place.
                 constexpr int BOXES = BN / 2 / 32;
                 uint64_t* bar = epi_full + 2 * w;
 #pragma unroll
@@ -619,28 +624,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     __syncwarp();
                     if (elect_one()) {
                         op_mbar_expect(bar, 8192);
-                        tma_load(buf_mem, &a.maps[a.map_g], col0, row0, q.p, bar);
-                        tma_load(buf_mem + 4096, &a.maps[a.map_u], col0, row0, q.p, bar);
+                        tma_load(buf_mem, &a.maps[a.map_a], col0, row0, q.p, bar);
+                        tma_load(buf_mem + 4096, &a.maps[a.map_b], col0, row0, q.p, bar);
                     }
                     mbar_wait(bar, uses & 1, s_abort, a.err);
                     float xg[32], xu[32];
-                    with_act(a.act, [&](auto act) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            const uint32_t off = swz128(lane * 128 + e * 4);
-                            const float4 g4 = *reinterpret_cast<const float4*>(buf_mem + off);
-                            const float4 u4 = *reinterpret_cast<const float4*>(buf_mem + 4096 + off);
-                            const float gf[4] = {g4.x, g4.y, g4.z, g4.w}, uf[4] = {u4.x, u4.y, u4.z, u4.w};
+                    for (int e = 0; e < 32; e += 4) {
+                        const uint32_t off = swz128(lane * 128 + e * 4);
+                        const float4 a4 = *reinterpret_cast<const float4*>(buf_mem + off);
+                        const float4 b4 = *reinterpret_cast<const float4*>(buf_mem + 4096 + off);
+                        const float af[4] = {a4.x, a4.y, a4.z, a4.w}, bf[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const float dh = sum[c * 32 + e + z];
-                                float val, der;
-                                act_both<T, decltype(act)::value>(gf[z], val, der);
-                                xg[e + z] = dh * uf[z] * der;
-                                xu[e + z] = dh * val;
-                            }
+                        for (int z = 0; z < 4; ++z) {
+                            const float dh = sum[c * 32 + e + z];
+                            xg[e + z] = dh * bf[z];
+                            xu[e + z] = dh * af[z];
                         }
-                    });
+                    }
                     const bool in = row0 < g.M && col0 < g.N;
 #pragma unroll
                     for (int half_out = 0; half_out < 2; ++half_out) {
@@ -660,16 +661,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     }
                 }
             } else {
-                // D = dH.  G and U come in through the two halves of the staging memory, one box of 32 columns
-                // ahead; dG and dU go out in their place.
+                // D = dH.  act(G) and U act'(G) come in through the two halves of the staging memory, one box of 32
+                // columns ahead; dU and dG go out in their place.
                 constexpr int BOXES = BN / 2 / 32;
                 uint64_t* bars = epi_full + 2 * w;
                 auto fetch = [&](int c) {
                     const int col = q.n * BN + half * (BN / 2) + c * 32, slot = (uses + c) & 1;
                     if (elect_one()) {
                         op_mbar_expect(&bars[slot], 4096);
-                        tma_load(buf_mem + slot * 4096, &a.maps[a.map_g], col, row0, q.p, &bars[slot]);
-                        tma_load(buf_mem + slot * 4096 + 2048, &a.maps[a.map_u], col, row0, q.p, &bars[slot]);
+                        tma_load(buf_mem + slot * 4096, &a.maps[a.map_a], col, row0, q.p, &bars[slot]);
+                        tma_load(buf_mem + slot * 4096 + 2048, &a.maps[a.map_b], col, row0, q.p, &bars[slot]);
                     }
                 };
                 store_wait_read<0>();
@@ -689,33 +690,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     tc_load(v, acc + half * (BN / 2) + c * 32);
                     mbar_wait(&bars[slot], ((uses + c) >> 1) & 1, s_abort, a.err);
                     unsigned char* bg = buf_mem + slot * 4096;
-                    with_act(a.act, [&](auto act) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            const uint32_t off = swz64(lane * 64 + e * 2);
-                            const uint4 g4 = *reinterpret_cast<const uint4*>(bg + off), u4 = *reinterpret_cast<const uint4*>(bg + 2048 + off);
-                            const uint32_t gw[4] = {g4.x, g4.y, g4.z, g4.w}, uw[4] = {u4.x, u4.y, u4.z, u4.w};
-                            uint32_t og[4], ou[4];
+                    for (int e = 0; e < 32; e += 8) {
+                        const uint32_t off = swz64(lane * 64 + e * 2);
+                        const uint4 a4 = *reinterpret_cast<const uint4*>(bg + off), b4 = *reinterpret_cast<const uint4*>(bg + 2048 + off);
+                        const uint32_t aw[4] = {a4.x, a4.y, a4.z, a4.w}, bw[4] = {b4.x, b4.y, b4.z, b4.w};
+                        uint32_t ou[4], og[4];
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const float2 gf = unpack2<T>(gw[z]), uf = unpack2<T>(uw[z]);
-                                const float h0 = __uint_as_float(v[e + 2 * z]), h1 = __uint_as_float(v[e + 2 * z + 1]);
-                                float a0, d0, a1, d1;
-                                act_both<T, decltype(act)::value>(gf.x, a0, d0);
-                                act_both<T, decltype(act)::value>(gf.y, a1, d1);
-                                og[z] = pack2<T>(h0 * uf.x * d0, h1 * uf.y * d1);
-                                ou[z] = pack2<T>(h0 * a0, h1 * a1);
-                            }
-                            *reinterpret_cast<uint4*>(bg + off) = make_uint4(og[0], og[1], og[2], og[3]);
-                            *reinterpret_cast<uint4*>(bg + 2048 + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                        for (int z = 0; z < 4; ++z) {
+                            const float2 af = unpack2<T>(aw[z]), bf = unpack2<T>(bw[z]);
+                            const float h0 = __uint_as_float(v[e + 2 * z]), h1 = __uint_as_float(v[e + 2 * z + 1]);
+                            ou[z] = pack2<T>(h0 * af.x, h1 * af.y);
+                            og[z] = pack2<T>(h0 * bf.x, h1 * bf.y);
                         }
-                    });
+                        *reinterpret_cast<uint4*>(bg + off) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                        *reinterpret_cast<uint4*>(bg + 2048 + off) = make_uint4(og[0], og[1], og[2], og[3]);
+                    }
                     fence_async_shared();
                     __syncwarp();
                     if (elect_one()) {
                         if (row0 < g.M && col0 < g.N) {
-                            tma_store(&a.maps[a.map_dg], bg, col0, row0, q.p);
-                            tma_store(&a.maps[a.map_du], bg + 2048, col0, row0, q.p);
+                            tma_store(&a.maps[a.map_du], bg, col0, row0, q.p);
+                            tma_store(&a.maps[a.map_dg], bg + 2048, col0, row0, q.p);
                         }
                         store_commit();
                     }
