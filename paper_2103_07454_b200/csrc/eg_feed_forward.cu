@@ -290,10 +290,11 @@ struct Builder {
         const int first = maps;
         for (int k = 0; k < b.parts; ++k) {
             if (mn) map(part(o, k), operand_type(), o.rows, o.cols, 64, 64);
-            else map(part(o, k), operand_type(), o.rows, o.cols, kGemmK, is_a ? 128 : BN / 2);
+            else map(part(o, k), operand_type(), o.rows, o.cols, kGemmK, is_a ? a_box(o.rows) : BN / 2);
         }
         return first;
     }
+    static int a_box(long long M) { return M < 128 ? (int)(M + 7) / 8 * 8 : 128; }
     GemmProblem* problem(long long M, long long N, bool a_mn, bool b_mn, bool pair) {
         GemmProblem* g = &a.p[a.problems++];
         const int cols = pair ? BN / 2 : BN;
@@ -305,6 +306,7 @@ struct Builder {
         a.tiles += g->tiles;
         g->nseg = 0;
         g->small = 0;
+        g->a_box = a_box(M);
         g->a_mn = a_mn; g->b_mn = b_mn; g->b_pair = pair;
         g->M = (int)M; g->N = (int)N;
         g->out = -1;
@@ -331,8 +333,16 @@ struct Builder {
     }
 };
 
-template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& a, cudaStream_t stream) {
-    using Shape = GemmShape<BN>;
+template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& args, cudaStream_t stream) {
+    using Shape = GemmShape<T, EPI, BN>;
+    static_assert(Shape::kRing / 1024 * 1024 / (128 * kGemmK * 2 + Shape::kBBytes) >= 4, "stages");
+    GemmArgs a = args;
+    a.a_pitch = 0;
+    for (int k = 0; k < a.problems; ++k) {
+        const int rows = !a.p[k].a_mn ? a.p[k].a_box : a.p[k].M > 64 ? 128 : 64;
+        if (a.a_pitch < rows * 128) a.a_pitch = rows * 128;
+    }
+    a.stages = Shape::stages(a.a_pitch);
     static bool raised[64] = {false};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

@@ -16,7 +16,7 @@
 // along its rows ("MN-major": the transposed uses of the backward pass) is staged in boxes of 64
 // columns and read by the tensor cores in that order; nothing is ever transposed in memory.
 //
-// Warps: 0 TMA producer, 1 tensor-core issue, 2 tensor memory, 4..11 epilogue (warp w reads the
+// Warps: 0 and 3 TMA producers (A, B), 1 tensor-core issue, 2 tensor memory, 4..11 epilogue (warp w reads the
 // 32 lanes w % 4 of tensor memory; warps 4..7 take the first half of the columns, 8..11 the other).
 #pragma once
 #include <cuda.h>
@@ -31,7 +31,7 @@ constexpr int kGemmThreads = 384;
 constexpr int kGemmEpiWarps = 8;
 constexpr int kGemmK = 64;                        // elements of K per stage: 128 bytes, one swizzle row
 constexpr int kGemmM = 256;                       // rows of a tile (two CTAs)
-constexpr int kGemmEpiBytes = 8192;               // staging per epilogue warp
+constexpr int kGemmMaxStages = 24;
 constexpr int kGemmMaxMaps = 40, kGemmMaxSegs = 12, kGemmMaxProblems = 4;
 
 struct GemmSeg {
@@ -53,6 +53,7 @@ struct GemmProblem {
     GemmSeg seg[kGemmMaxSegs];
     int small;                                    // fp32: stages of the products of smaller parts, which come first
     int a_mn, b_mn;                               // the operand's K runs along its rows
+    int a_box;                                    // rows of a box of A (K along the columns): 128, fewer where M is smaller
     int b_pair;                                   // B of the two CTAs are two matrices, same rows
     int M, N;                                     // of the result
     int out;                                      // map of the result, -1: `ptr` (no 16-byte rows)
@@ -64,6 +65,9 @@ struct GemmArgs {
     CUtensorMap maps[kGemmMaxMaps];
     GemmProblem p[kGemmMaxProblems];
     int problems, tiles;
+    // Stages, and bytes of A from one to the next.  A tile with few rows fetches only those; the tensor cores then
+    // read on into the next stage, for rows of D that nobody stores.
+    int stages, a_pitch;
     uint32_t idesc;                               // instruction descriptor without the majors
     unsigned int* err;
     // gate/up and activation-gradient epilogues: maps of 32 x 32 boxes
@@ -293,29 +297,50 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs& a, int t) {
     return q;
 }
 
-template <int BN> struct GemmShape {
-    static constexpr int kABytes = 128 * kGemmK * 2, kBBytes = BN / 2 * kGemmK * 2;
-    static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kEpi = kGemmEpiWarps * kGemmEpiBytes;
-    static constexpr int kRoom = 227 * 1024 - 1024 - kEpi - 512;
-    static constexpr int kStages = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
-    static constexpr int kBars = kStages * kStageBytes + kEpi;
-    static constexpr int kSmem = 1024 + kBars + 512;
-    static constexpr int kCols = BN < 32 ? 32 : BN;         // tensor memory columns of one accumulator
+template <typename T, int EPI, int BN> struct GemmShape {
+    static constexpr int kBBytes = BN / 2 * kGemmK * 2;         // of a stage
+    // staging of an epilogue warp: two boxes of results, or what the other epilogues lay out in 8 KB
+    static constexpr int kBoxCols = BN / 2 < 128 / (int)sizeof(T) ? BN / 2 : 128 / (int)sizeof(T);
+    static constexpr int kEpiBytes = EPI == kEpiStore ? 2 * 32 * kBoxCols * (int)sizeof(T) : 8192;
+    static constexpr int kEpi = kGemmEpiWarps * kEpiBytes;
+    static constexpr int kBarBytes = 1024;
+    static constexpr int kRing = 227 * 1024 - 1024 - kEpi - kBarBytes;   // both rings of stages
+    static constexpr int kBars = kRing / 1024 * 1024 + kEpi;
+    static constexpr int kSmem = 1024 + kBars + kBarBytes;
+    static constexpr int kCols = BN < 32 ? 32 : BN;             // tensor memory columns of one accumulator
     static constexpr int kTmem = 2 * kCols;
+    // stages for A boxes of a_pitch bytes
+    static int stages(int a_pitch) {
+        const int n = kRing / 1024 * 1024 / (a_pitch + kBBytes);
+        return n < kGemmMaxStages ? n : kGemmMaxStages;
+    }
 };
+
+// What one CTA fetches per stage for rows m0.. of A, rows n0.. of B.
+__device__ __forceinline__ uint32_t a_bytes(const GemmProblem& g, int m0) {
+    if (g.a_mn) return m0 + 64 < g.M ? 16384u : m0 < g.M ? 8192u : 0u;
+    return m0 < g.M ? (uint32_t)g.a_box * 128u : 0u;
+}
+template <int BN> __device__ __forceinline__ uint32_t b_bytes(const GemmProblem& g, int n0) {
+    if (!g.b_mn) return n0 < g.N ? (uint32_t)(BN / 2) * 128u : 0u;
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int h = 0; h < BN / 2; h += 64) bytes += n0 + h < g.N ? 8192u : 0u;
+    return bytes;
+}
 
 // T: type of the operands and of 16-bit results; EPI: what becomes of D; BN: columns of a tile.
 template <typename T, int EPI, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant__ GemmArgs a) {
-    using Shape = GemmShape<BN>;
-    constexpr int S = Shape::kStages;
+    using Shape = GemmShape<T, EPI, BN>;
+    const int S = a.stages;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    unsigned char* epi = smem + S * Shape::kStageBytes;
+    unsigned char* ring_b = smem + S * a.a_pitch;
+    unsigned char* epi = smem + Shape::kBars - Shape::kEpi;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Shape::kBars);   // [S] (even CTA's are used)
-    uint64_t* empty = full + S;                                          // [S]
-    uint64_t* acc_full = empty + S;                                      // [2]
+    uint64_t* empty = full + kGemmMaxStages;                             // [S]
+    uint64_t* acc_full = empty + kGemmMaxStages;                                      // [2]
     uint64_t* acc_empty = acc_full + 2;                                  // [2] (even CTA's are used)
     uint64_t* epi_full = acc_empty + 2;                                  // [kGemmEpiWarps][2]
     volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + 2 * kGemmEpiWarps);
@@ -344,35 +369,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
+        // warp 0 fetches A (and announces a stage's bytes), warp 3 fetches B
         if (elect_one()) {
             int s = 0, round = 0;
             for (int t = pair; t < a.tiles; t += pairs) {
                 const TilePos q = tile_pos(a, t);
                 const GemmProblem& g = a.p[q.problem];
-                const int m0 = q.m * kGemmM + (int)rank * 128;
-                const int n0 = g.b_pair ? q.n * (BN / 2) : q.n * BN + (int)rank * (BN / 2);
+                const int m0 = q.m * kGemmM + (int)rank * 128, n0 = g.b_pair ? q.n * (BN / 2) : q.n * BN + (int)rank * (BN / 2);
+                // boxes wholly outside the operands stay away: rows and columns of D that nobody stores
+                const uint32_t bytes = a_bytes(g, q.m * kGemmM) + a_bytes(g, q.m * kGemmM + 128) +
+                                       b_bytes<BN>(g, g.b_pair ? n0 : q.n * BN) + b_bytes<BN>(g, g.b_pair ? n0 : q.n * BN + BN / 2);
+                const bool mn = warp == 0 ? g.a_mn : g.b_mn;
+                const int row = warp == 0 ? m0 : n0, rows = warp == 0 ? g.M : g.N;
                 for (int e = 0; e < g.nseg; ++e) {
-                    const CUtensorMap* ma = &a.maps[g.seg[e].a];
-                    const CUtensorMap* mb = &a.maps[rank ? g.seg[e].b1 : g.seg[e].b0];
-                    for (int k = 0; k < g.seg[e].ksteps; ++k) {
+                    const CUtensorMap* map = &a.maps[warp == 0 ? g.seg[e].a : rank ? g.seg[e].b1 : g.seg[e].b0];
+                    const int ksteps = g.seg[e].ksteps;
+                    for (int k = 0; k < ksteps; ++k) {
                         if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
-                        unsigned char* sa = smem + s * Shape::kStageBytes;
-                        unsigned char* sb = sa + Shape::kABytes;
-                        if (rank == 0) op_mbar_expect(&full[s], 2 * Shape::kStageBytes);
+                        unsigned char* to = warp == 0 ? smem + s * a.a_pitch : ring_b + s * Shape::kBBytes;
+                        if (warp == 0 && rank == 0) op_mbar_expect(&full[s], bytes);
                         const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
-                        if (g.a_mn) {
-                            tma_load_pair(sa, ma, m0, k * kGemmK, q.p, bar);
-                            tma_load_pair(sa + 8192, ma, m0 + 64, k * kGemmK, q.p, bar);
-                        } else {
-                            tma_load_pair(sa, ma, k * kGemmK, m0, q.p, bar);
-                        }
-                        if (g.b_mn) {
-#pragma unroll
-                            for (int h = 0; h < BN / 2; h += 64) tma_load_pair(sb + h * 128, mb, n0 + h, k * kGemmK, q.p, bar);
-                        } else {
-                            tma_load_pair(sb, mb, k * kGemmK, n0, q.p, bar);
-                        }
+                        if (row < rows) tma_load_pair(to, map, mn ? row : k * kGemmK, mn ? k * kGemmK : row, q.p, bar);
+                        if (mn && (warp == 0 || BN == 256) && row + 64 < rows)
+                            tma_load_pair(to + 8192, map, row + 64, k * kGemmK, q.p, bar);
                         if (++s == S) { s = 0; ++round; }
                     }
                 }
@@ -402,8 +422,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         }
                         mbar_wait(&full[s], round & 1, s_abort, a.err);
                         tc_fence_after();
-                        const uint32_t sa = op_smem(smem + s * Shape::kStageBytes);
-                        const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + Shape::kABytes, g.b_mn);
+                        const uint64_t da = smem_desc(op_smem(smem + s * a.a_pitch), g.a_mn);
+                        const uint64_t db = smem_desc(op_smem(ring_b + s * Shape::kBBytes), g.b_mn);
 #pragma unroll
                         for (int u = 0; u < kGemmK / 16; ++u) {
                             tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
@@ -426,7 +446,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
         }
     } else if (warp >= 4) {
         const int w = warp - 4, half = w >> 2;
-        unsigned char* buf_mem = epi + w * kGemmEpiBytes;
+        unsigned char* buf_mem = epi + w * Shape::kEpiBytes;
         const uint32_t lanes = (uint32_t)((w & 3) * 32) << 16;
         int count = 0, uses = 0;
         (void)uses;
@@ -476,7 +496,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
 #pragma unroll
                 for (int c = 0; c < BN / 2; c += CW) {
                     const int col0 = q.n * BN + half * (BN / 2) + c;
-                    unsigned char* box = buf_mem + (uses & 1) * 4096;
+                    unsigned char* box = buf_mem + (uses & 1) * (Shape::kEpiBytes / 2);
                     store_wait_read<1>();
                     __syncwarp();
                     constexpr int LW = CW < 32 ? 16 : 32;
