@@ -186,8 +186,10 @@ long long saved_bytes(const eg_feed_forward_args* q) {
     return q->P * q->rows * pitch_of(q->d_ff) * (q->dtype == EG_F32 ? 2 * 4 + 2 * kParts : 3 * 2);
 }
 
-// Which kernels a forward call without `saved` takes.  Measured at d_model 1024, d_ff 2816, 4 replicas, bf16:
-// (see k_few_mma) streams 13 us for 1 token; tiles FEW_TABLE.
+// Which kernels a forward call without `saved` takes.  Measured with 4 replicas, us:
+//   bf16 1024 x 2816   k_few_mma 15 for 1 token, 17 for 8, 22 for 16, 40 for 32; tiles 23 up to 24, 24 for 64
+//   fp32 1024 x 2816   k_few_dot 26 for 1 token, 91 for 8, 233 for 16;           tiles 188
+//   bf16 1001 x 2817   k_few_dot 41 for 1 token, 48 for 2, 90 for 4;             tiles 57
 int few_kind(const eg_feed_forward_args* q) {
     if (q->saved || q->P > 65535) return 0;
     const size_t size = q->dtype == EG_F32 ? 4 : 2;
@@ -195,7 +197,7 @@ int few_kind(const eg_feed_forward_args* q) {
                         in_place(mat(q->w_up), q->P, q->d_ff, size) && in_place(mat(q->w_down), q->P, q->d_model, size) &&
                         q->d_model * size % 16 == 0 && q->d_ff * size % 16 == 0;
     if (q->dtype != EG_F32 && rows16 && q->rows <= kFewMmaTokens) return 1;
-    return q->rows <= kFewDotTokens ? 2 : 0;
+    return q->rows <= (q->dtype == EG_F32 ? kFewDotTokens32 : kFewDotTokens16) ? 2 : 0;
 }
 
 void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
@@ -333,6 +335,22 @@ struct Builder {
     }
 };
 
+template <typename T, int EPI, int BN, int G> cudaError_t launch_kernel(const GemmArgs& a, cudaStream_t stream) {
+    constexpr int smem = GemmShape<T, EPI, BN>::kSmem;
+    static bool raised[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !raised[dev]) {
+        e = cudaFuncSetAttribute(k_gemm<T, EPI, BN, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) raised[dev] = true;
+    }
+    const int pairs = sm_count() / 2;
+    if (pairs < 1) return cudaErrorInvalidDevice;
+    return launch_after(k_gemm<T, EPI, BN, G>, dim3(2 * (a.tiles < pairs ? a.tiles : pairs)), dim3(kGemmThreads), smem, stream, a);
+}
+
 template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& args, cudaStream_t stream) {
     using Shape = GemmShape<T, EPI, BN>;
     static_assert(Shape::kRing / 1024 * 1024 / (128 * kGemmK * 2 + Shape::kBBytes) >= 4, "stages");
@@ -342,23 +360,25 @@ template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& 
         const int rows = !a.p[k].a_mn ? a.p[k].a_box : a.p[k].M > 64 ? 128 : 64;
         if (a.a_pitch < rows * 128) a.a_pitch = rows * 128;
     }
-    a.stages = Shape::stages(a.a_pitch);
-    static bool raised[64] = {false};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev >= 64 || !raised[dev]) {
-        e = cudaFuncSetAttribute(k_gemm<T, EPI, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) raised[dev] = true;
+    const int stages = Shape::stages(a.a_pitch);
+    // (fp32 hands its accumulator over every few stages and counts them one by one)
+    if constexpr (sizeof(T) == 2 && EPI != kEpiDact) {
+        if (stages >= 16) {
+            a.stages = stages / 4;
+            return launch_kernel<T, EPI, BN, 4>(a, stream);
+        }
+        if (stages >= 8) {
+            a.stages = stages / 2;
+            return launch_kernel<T, EPI, BN, 2>(a, stream);
+        }
     }
-    const int pairs = sm_count() / 2;
-    if (pairs < 1) return cudaErrorInvalidDevice;
-    return launch_after(k_gemm<T, EPI, BN>, dim3(2 * (a.tiles < pairs ? a.tiles : pairs)), dim3(kGemmThreads), Shape::kSmem, stream, a);
+    a.stages = stages;
+    return launch_kernel<T, EPI, BN, 1>(a, stream);
 }
 
-template <typename T, int EPI> cudaError_t launch_gemm(const Builder& w, cudaStream_t stream) {
+template <typename T, int EPI> cudaError_t launch_gemm(Builder& w, cudaStream_t stream) {
     if (!w.ok) return cudaErrorInvalidValue;
+    w.a.n_maps = w.maps;
     if (w.a.tiles == 0) return cudaSuccess;
     if constexpr (sizeof(T) == 2) {
         if (w.BN == 256) return launch_shape<T, EPI, 256>(w.a, stream);

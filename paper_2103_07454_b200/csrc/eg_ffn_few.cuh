@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(256) k_few_dot(const FewArgs a) {
     }
 }
 
-constexpr int kFewMmaTokens = 16, kFewDotTokens = 16;
+constexpr int kFewMmaTokens = 16, kFewDotTokens32 = 8, kFewDotTokens16 = 2;
 
 template <typename T, bool GATE> cudaError_t launch_few_mma(const FewArgs& a, cudaStream_t stream) {
     const long long units = (long long)a.P * ((a.rows + 15) / 16), most = 2ll * sm_count();
@@ -242,10 +242,11 @@ template <typename T, int VEC, bool GATE> cudaError_t launch_few_dot(FewArgs a, 
         return launch_after(kernel, grid, block, 0, stream, a);
     };
     if (a.n <= 1) return go(k_few_dot<T, VEC, 1, 2, GATE>, 2);
-    if (a.n <= 2) return go(k_few_dot<T, VEC, 2, 4, GATE>, 4);
-    if (a.n <= 4) return go(k_few_dot<T, VEC, 4, 4, GATE>, 4);
-    if (a.n <= 8) return go(k_few_dot<T, VEC, 8, 8, GATE>, 8);
-    return go(k_few_dot<T, VEC, 16, 4, GATE>, 4);
+    if constexpr (sizeof(T) == 4) {
+        if (a.n > 4) return go(k_few_dot<T, VEC, 8, 8, GATE>, 8);
+        if (a.n > 2) return go(k_few_dot<T, VEC, 4, 4, GATE>, 4);
+    }
+    return go(k_few_dot<T, VEC, 2, 4, GATE>, 4);
 }
 
 }  // namespace eg

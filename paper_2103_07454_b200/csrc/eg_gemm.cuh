@@ -68,6 +68,7 @@ struct GemmArgs {
     // Stages, and bytes of A from one to the next.  A tile with few rows fetches only those; the tensor cores then
     // read on into the next stage, for rows of D that nobody stores.
     int stages, a_pitch;
+    int n_maps;
     uint32_t idesc;                               // instruction descriptor without the majors
     unsigned int* err;
     // gate/up and activation-gradient epilogues: maps of 32 x 32 boxes
@@ -148,7 +149,6 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, const void* sr
 }
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -329,14 +329,15 @@ template <int BN> __device__ __forceinline__ uint32_t b_bytes(const GemmProblem&
     return bytes;
 }
 
-// T: type of the operands and of 16-bit results; EPI: what becomes of D; BN: columns of a tile.
-template <typename T, int EPI, int BN>
+// T: type of the operands and of 16-bit results; EPI: what becomes of D; BN: columns of a tile; G: stages under one
+// barrier -- where stages are small, one wait serves several.
+template <typename T, int EPI, int BN, int G>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant__ GemmArgs a) {
     using Shape = GemmShape<T, EPI, BN>;
     const int S = a.stages;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    unsigned char* ring_b = smem + S * a.a_pitch;
+    unsigned char* ring_b = smem + S * G * a.a_pitch;
     unsigned char* epi = smem + Shape::kBars - Shape::kEpi;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Shape::kBars);   // [S] (even CTA's are used)
     uint64_t* empty = full + kGemmMaxStages;                             // [S]
@@ -354,6 +355,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
         for (int q = 0; q < 2; ++q) { op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps); }
         for (int q = 0; q < 2 * kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3) {
+        for (int m = lane; m < a.n_maps; m += 32) asm volatile("prefetch.tensormap [%0];" ::"l"(&a.maps[m]) : "memory");
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(op_smem(s_tmem)), "n"(Shape::kTmem)
@@ -385,14 +389,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 for (int e = 0; e < g.nseg; ++e) {
                     const CUtensorMap* map = &a.maps[warp == 0 ? g.seg[e].a : rank ? g.seg[e].b1 : g.seg[e].b0];
                     const int ksteps = g.seg[e].ksteps;
-                    for (int k = 0; k < ksteps; ++k) {
+                    for (int k = 0; k < ksteps; k += G) {
                         if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
-                        unsigned char* to = warp == 0 ? smem + s * a.a_pitch : ring_b + s * Shape::kBBytes;
-                        if (warp == 0 && rank == 0) op_mbar_expect(&full[s], bytes);
+                        const int n = G == 1 ? 1 : min(G, ksteps - k), pitch = warp == 0 ? a.a_pitch : Shape::kBBytes;
+                        unsigned char* to = (warp == 0 ? smem : ring_b) + s * G * pitch;
+                        if (warp == 0 && rank == 0) op_mbar_expect(&full[s], n * bytes);
                         const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
-                        if (row < rows) tma_load_pair(to, map, mn ? row : k * kGemmK, mn ? k * kGemmK : row, q.p, bar);
-                        if (mn && (warp == 0 || BN == 256) && row + 64 < rows)
-                            tma_load_pair(to + 8192, map, row + 64, k * kGemmK, q.p, bar);
+#pragma unroll
+                        for (int h = 0; h < G; ++h, to += pitch) {
+                            if (h >= n) break;
+                            const int at = (k + h) * kGemmK;
+                            if (row < rows) tma_load_pair(to, map, mn ? row : at, mn ? at : row, q.p, bar);
+                            if (mn && (warp == 0 || BN == 256) && row + 64 < rows) tma_load_pair(to + 8192, map, row + 64, at, q.p, bar);
+                        }
                         if (++s == S) { s = 0; ++round; }
                     }
                 }
@@ -413,7 +422,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 uint32_t add = 0;
                 int in_chunk = sizeof(T) == 4 ? kChunk - g.small : 0;    // reaches kChunk where the accumulator is handed over
                 for (int e = 0; e < g.nseg; ++e) {
-                    for (int k = 0; k < g.seg[e].ksteps; ++k) {
+                    const int ksteps = g.seg[e].ksteps;
+                    for (int k = 0; k < ksteps; k += G) {
                         const int buf = count & 1;
                         const uint32_t d = tmem + buf * Shape::kCols;
                         if (!add) {
@@ -422,12 +432,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         }
                         mbar_wait(&full[s], round & 1, s_abort, a.err);
                         tc_fence_after();
-                        const uint64_t da = smem_desc(op_smem(smem + s * a.a_pitch), g.a_mn);
-                        const uint64_t db = smem_desc(op_smem(ring_b + s * Shape::kBBytes), g.b_mn);
+                        const int n = G == 1 ? 1 : min(G, ksteps - k);
+                        uint64_t da = smem_desc(op_smem(smem + s * G * a.a_pitch), g.a_mn);
+                        uint64_t db = smem_desc(op_smem(ring_b + s * G * Shape::kBBytes), g.b_mn);
 #pragma unroll
-                        for (int u = 0; u < kGemmK / 16; ++u) {
-                            tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
-                            add = 1;
+                        for (int h = 0; h < G; ++h, da += a.a_pitch >> 4, db += Shape::kBBytes >> 4) {
+                            if (h >= n) break;
+#pragma unroll
+                            for (int u = 0; u < kGemmK / 16; ++u) {
+                                tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
+                                add = 1;
+                            }
                         }
                         tc_commit_pair(&empty[s]);
                         if (++s == S) { s = 0; ++round; }
@@ -745,7 +760,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 ++count;
             }
         }
-        store_wait_all();
+        store_wait_read<0>();
     }
     if (*s_abort) {           // a wait ran out: copies and products in flight get a millisecond to end
         const long long t0 = clock64();
