@@ -262,6 +262,20 @@ template <typename T> struct Raw {
                              : "memory");
         }
     }
+    template <int VEC> __device__ __forceinline__ void load_shared(uint32_t at, int tpr) {
+#pragma unroll
+        for (int v = 0; v < kElems / VEC; ++v)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[4 * v]), "=r"(w[4 * v + 1]), "=r"(w[4 * v + 2]), "=r"(w[4 * v + 3])
+                         : "r"(at + v * tpr * 16)
+                         : "memory");
+    }
+    // all vectors, to a thread's first one
+    template <int VEC> __device__ __forceinline__ void store_whole(T* p, int tpr) const {
+#pragma unroll
+        for (int v = 0; v < kElems / VEC; ++v)
+            *reinterpret_cast<uint4*>(p + v * tpr * VEC) = make_uint4(w[4 * v], w[4 * v + 1], w[4 * v + 2], w[4 * v + 3]);
+    }
     template <int VEC> __device__ __forceinline__ void store(T* p, int tpr, int t, int d) const {
         if constexpr (VEC > 1) {
 #pragma unroll
@@ -291,20 +305,14 @@ template <typename T> struct Raw {
     }
 };
 
-// A factor's values for a thread's columns: unpacked where there are registers for it (the backward kernel).
-template <typename T, bool WIDE> struct Factors;
-template <typename T> struct Factors<T, true> {
+// A factor's values for a thread's columns, unpacked.
+template <typename T> struct Factors {
     f32x2 v[kElems / 2];
     __device__ __forceinline__ void take(const Raw<T>& x) {
 #pragma unroll
         for (int p = 0; p < kElems / 2; ++p) v[p] = x.two(p);
     }
     __device__ __forceinline__ f32x2 two(int p) const { return v[p]; }
-};
-template <typename T> struct Factors<T, false> {
-    Raw<T> v;
-    __device__ __forceinline__ void take(const Raw<T>& x) { v = x; }
-    __device__ __forceinline__ f32x2 two(int p) const { return v.two(p); }
 };
 
 // K values (8 or 16) summed over the lanes of a warp, or of each half of it (`width` 32 or 16): halves are
@@ -331,13 +339,17 @@ template <int K> __device__ __forceinline__ int held(int l) {
     return r;
 }
 
+// Rows that a thread works on at a time: as many as its 255 registers hold.
+template <typename T, bool BWD> __host__ __device__ constexpr int rows_at_once() {
+    return (BWD ? 1 : 2) * (sizeof(T) == 2 ? 2 : 1);
+}
+
 // A CTA works through its rows in steps of up to teams * ROWS * (rows of a warp) consecutive rows of one
 // replica.  The rows of y, r (and d_r', d_o) of the steps ahead come into a ring of stages in
 // shared memory, one bulk copy an array and step where the rows lie one after the other; rows off the
 // 16-byte boundaries are copied from the boundary below and read from the remainder.  A team is the tpr
 // threads of a row, or a warp with 32 / tpr rows below a warp; it takes ROWS rows at a time, so that the
-// latencies of one row's sums are covered by the other's arithmetic (one row in fp32, whose rows are twice as
-// long to move).  A thread owns the same columns of every row, so the factors a, scale, w_pre of the replica and
+// latencies of one row's sums are covered by the others' arithmetic.  A thread owns the same columns of every row, so the factors a, scale, w_pre of the replica and
 // (backward) its three column sums stay in registers; at the end of a replica's rows the teams add up their
 // sums in shared memory and leave one partial sum per (replica, CTA) pair that meet; i + b numbers the pairs
 // without a gap.  Rows wider than kCtaWidth are shared by a cluster of two CTAs, which exchange the sums of a row.
@@ -347,9 +359,9 @@ template <int K> __device__ __forceinline__ int held(int l) {
 // ask for.  Where p and inv1 q cancel to less than a tenth of their size, r' and what follows from it are summed
 // in a second round instead.
 template <typename T, int VEC, bool BWD>
-__global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __grid_constant__ NormArgs a) {
-    constexpr int E = kElems, ROWS = sizeof(T) == 2 ? 2 : 1, ARRAYS = BWD ? 4 : 2;
-    constexpr int SUMS = BWD ? 7 : 4, KP = BWD ? 8 * ROWS : 8;
+__global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_constant__ NormArgs a) {
+    constexpr int E = kElems, ROWS = rows_at_once<T, BWD>(), ARRAYS = BWD ? 4 : 2;
+    constexpr int SUMS = BWD ? 7 : 4, KP = BWD ? 8 * ROWS : 4 * ROWS;
     constexpr int kWarps = kThreads / 32;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_peer[2];
@@ -383,6 +395,7 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     Walk w;
     w.start(u0, u1, a.rows, per);
+    asm volatile("griddepcontrol.wait;" ::: "memory");         // set up while the kernel before this one finished
 
     // the rows of array q come in by lane 0 of warp q (few warps: of the last one, q after q)
     Walk ahead = w;
@@ -390,8 +403,8 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
     int as = 0, around = 0;
     uintptr_t from_row = 0;                                    // where the next step's rows of array `fetcher` start
     auto fetch = [&]() {
-        if (ahead.done()) return;
-        if (lane == 0 && fetcher < ARRAYS) {
+        if (fetcher >= ARRAYS || ahead.done()) return;
+        if (lane == 0) {
             for (int q = fetcher; q < ARRAYS; q += fetchers) {
                 const Mat& m = a.in[q];
                 if (!m.p) continue;
@@ -437,6 +450,9 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
     int in_row = 0;                                            // bit v: vector v of this thread lies in the row
     if (VEC > 1)
         for (int v = 0; v < E / VEC; ++v) in_row |= (v * tpr + t) * VEC < d ? 1 << v : 0;
+    bool in_whole = VEC > 1 && in_row == (1 << E / VEC) - 1;
+#pragma unroll
+    for (int q = 0; q < ARRAYS; ++q) in_whole = in_whole && a.in[q].p;
     int parity = 0, meets = 0;
     // the values of the team's rows, summed over their threads (and CTAs): v[k] in every thread
     auto row_sums = [&](float (&v)[KP]) {
@@ -496,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
     int s = 0, round = 0;
     while (!w.done()) {
         const int i = w.i;
-        Factors<T, BWD> fs, fw;
+        Factors<T> fs, fw;
         f32x2 fa[E / 2];
         f32x2 accC[BWD ? E / 2 : 1], accD[BWD ? E / 2 : 1], accW[BWD ? E / 2 : 1];
         {
@@ -513,9 +529,6 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
                     fa[p] = mul2(fa[p], pack_f2(sigmoid_f(f.x), sigmoid_f(f.y)));
                 }
             }
-        }
-        {
-            Raw<T> x;
 #pragma unroll
             for (int p = 0; p < E / 2; ++p) x.set(p, 1.f, 1.f);
             if (a.scale.p) x.template load<VEC>(row_of<T>(a.scale, i, 0) + c0, tpr, t, d);
@@ -528,12 +541,29 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
 #pragma unroll
             for (int p = 0; p < E / 2; ++p) accC[p] = accD[p] = accW[p] = 0;
         }
+        // this thread's first row of the step in the two results, and the way to the next step's
+        const Mat &m0 = BWD ? a.dr : a.r_out, &m1 = BWD ? a.dy : a.o;
+        // (fp32 gradients have no registers left for them and work them out at every step)
+        constexpr bool KEPT = !BWD || sizeof(T) == 2;
+        T* out0 = m0.p ? row_of<T>(m0, i, w.row + mine) + c0 : nullptr;
+        T* out1 = m1.p ? row_of<T>(m1, i, w.row + mine) + c0 : nullptr;
+        auto put = [&](const Raw<T>& x, T* to, bool whole) {
+            if (VEC > 1 && whole) x.template store_whole<VEC>(to + t * VEC, tpr);
+            else x.template store<VEC>(to, tpr, t, d);
+        };
         bool last = false;
         while (!last) {
             const int n = w.n;
             (void)op_mbar_wait(&s_full[s], round & 1, &s_abort, a.err);    // after a time-out the walk just goes on
             Raw<T> in[ARRAYS][ROWS];
             uint32_t at = mine_at + s * stage_bytes;
+            const bool whole = in_whole && n == per;           // nothing of what this thread takes is missing
+            if (VEC > 1 && whole) {
+#pragma unroll
+                for (int q = 0; q < ARRAYS; ++q, at += array_bytes)
+#pragma unroll
+                    for (int z = 0; z < ROWS; ++z) in[q][z].template load_shared<VEC>(at + z * each * a.slot_bytes, tpr);
+            } else
 #pragma unroll
             for (int q = 0; q < ARRAYS; ++q, at += array_bytes) {
 #pragma unroll
@@ -634,8 +664,9 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
 #pragma unroll
             for (int z = 0; z < ROWS; ++z) {
                 const int j = mine + z * each;
-                const long long row = w.row + j;
                 const f32x2 i1 = pack_f2(inv1[z], inv1[z]);
+                if (!KEPT && m0.p) out0 = row_of<T>(m0, i, w.row + mine) + c0;
+                if (!KEPT && m1.p) out1 = row_of<T>(m1, i, w.row + mine) + c0;
                 if constexpr (!BWD) {
                     const float i2 = rsqrtf(fmaf(rr[z], a.inv_d, a.eps));
                     const f32x2 inv2 = pack_f2(i2, i2);
@@ -647,8 +678,8 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
                         xo.set(p, mul2(mul2(R, inv2), fw.two(p)));
                     }
                     if (j < n) {
-                        if (a.r_out.p) xr.template store<VEC>(row_of<T>(a.r_out, i, row) + c0, tpr, t, d);
-                        if (a.o.p) xo.template store<VEC>(row_of<T>(a.o, i, row) + c0, tpr, t, d);
+                        if (out0) put(xr, out0 + z * each * m0.row, whole);
+                        if (out1) put(xo, out1 + z * each * m1.row, whole);
                     }
                 } else {
                     const bool has_do = a.in[3].p != nullptr;
@@ -673,11 +704,13 @@ __global__ void __launch_bounds__(kThreads, BWD ? 1 : 2) k_norm_stream(const __g
                         xy.set(p, fma2(k4, y, mul2(fa[p], tR)));
                     }
                     if (j < n) {
-                        if (a.dr.p) xr.template store<VEC>(row_of<T>(a.dr, i, row) + c0, tpr, t, d);
-                        if (a.dy.p) xy.template store<VEC>(row_of<T>(a.dy, i, row) + c0, tpr, t, d);
+                        if (out0) put(xr, out0 + z * each * m0.row, whole);
+                        if (out1) put(xy, out1 + z * each * m1.row, whole);
                     }
                 }
             }
+            if (KEPT && out0) out0 += per * m0.row;
+            if (KEPT && out1) out1 += per * m1.row;
             last = w.next(a.rows, per);
             if (S == 1) fetch();
         }
@@ -825,16 +858,15 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     a.cols = a.ctas == 1 ? a.d : ((a.d + 1) / 2 + 7) / 8 * 8;
     a.tpr = threads_per_row(a.cols, kElems);
     a.tpr = a.tpr < 16 ? 16 : a.tpr;                      // the sums of two rows are spread over sixteen lanes
-    constexpr int ROWS = sizeof(T) == 2 ? 2 : 1;
-    constexpr int RESIDENT = BWD ? 1 : 2;                 // CTAs of a multiprocessor
-    const int team = a.tpr < 32 ? 32 : a.tpr, rows = ROWS * (a.tpr < 32 ? 32 / a.tpr : 1), spots = RESIDENT * sms / a.ctas;
+    constexpr int ROWS = rows_at_once<T, BWD>();
+    const int team = a.tpr < 32 ? 32 : a.tpr, rows = ROWS * (a.tpr < 32 ? 32 / a.tpr : 1), spots = sms / a.ctas;
     a.teams = kThreads / team;
     const long long need = (W + (long long)spots * rows - 1) / ((long long)spots * rows);
     if (a.teams > need) a.teams = (int)need;              // few rows: spread over the multiprocessors first
     a.slot_bytes = VEC > 1 ? a.cols * (int)sizeof(T) : (a.cols * (int)sizeof(T) + 30) / 16 * 16;
     const int sums = BWD && a.teams > 1 ? (3 * a.cols * 4 + 127) & ~127 : 0;
     const int stage = ARRAYS * a.teams * rows * a.slot_bytes;
-    a.stages = ((kSmemMax - 8192) / RESIDENT - sums) / stage;
+    a.stages = (kSmemMax - 8192 - sums) / stage;
     a.stages = a.stages > kMaxStages ? kMaxStages : a.stages;
     if (a.stages < 1) return cudaErrorInvalidValue;
     const int smem = sums + a.stages * stage;
@@ -846,7 +878,7 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !raised[dev]) {
-        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kSmemMax - 8192) / RESIDENT)) != cudaSuccess) return e;
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax - 8192)) != cudaSuccess) return e;
         if (dev < 64) raised[dev] = true;
     }
     cudaLaunchConfig_t cfg{};
@@ -854,12 +886,14 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     cfg.blockDim = dim3(a.teams * team);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = a.ctas;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = a.ctas > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, k_norm_stream<T, VEC, BWD>, a);
 }
 
