@@ -377,8 +377,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
     const long long W = (long long)a.P * a.rows, u0 = cut(W, b, G), u1 = cut(W, b + 1, G);
     const int per = teams * ROWS * each;
     const int array_bytes = per * a.slot_bytes, stage_bytes = ARRAYS * array_bytes;
-    float* s_sums = reinterpret_cast<float*>(smem);            // [3][d] where teams meet (BWD, teams > 1)
-    unsigned char* ring = smem + (BWD && teams > 1 ? (3 * a.cols * 4 + 127) & ~127 : 0);
+    float* s_sums = reinterpret_cast<float*>(smem);            // BWD: [elements of a thread][threads]
+    unsigned char* ring = smem + (BWD ? E * nc * 4 : 0);
     const int lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -395,6 +395,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     Walk w;
     w.start(u0, u1, a.rows, per);
+    {   // the factors of the first two replicas of this CTA are wanted soon
+        const int c = c0 + (int)threadIdx.x * (128 / (int)sizeof(T));
+        for (int q = w.i; q < min(a.P, w.i + 2) && c < c0 + d; ++q)
+            for (const Mat* m : {&a.w_post, &a.gate, &a.scale, &a.w_pre})
+                if (m->p) asm volatile("prefetch.global.L2 [%0];" ::"l"(row_of<T>(*m, q, 0) + c));
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");         // set up while the kernel before this one finished
 
     // the rows of array q come in by lane 0 of warp q (few warps: of the last one, q after q)
@@ -715,35 +721,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
             if (S == 1) fetch();
         }
         if constexpr (BWD) {
-            // column sums of this replica: first the rows of a warp, then team after team
+            // column sums of this replica: first over the rows of a warp, then over the teams, one of the three at a time
             float* out = a.partials + (long long)(i + b) * 3 * a.d + c0;
-            float sums[3][E];
 #pragma unroll
-            for (int p = 0; p < E / 2; ++p) {
-                const float2 x = unpack_f2(accC[p]), y = unpack_f2(accD[p]), z = unpack_f2(accW[p]);
-                sums[0][2 * p] = x.x; sums[0][2 * p + 1] = x.y;
-                sums[1][2 * p] = y.x; sums[1][2 * p + 1] = y.y;
-                sums[2][2 * p] = z.x; sums[2][2 * p + 1] = z.y;
-            }
-            if (tpr < 32) {
+            for (int k = 0; k < 3; ++k) {
+                const f32x2* acc = k == 0 ? accC : k == 1 ? accD : accW;
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) sums[k][e] += __shfl_xor_sync(0xffffffffu, sums[k][e], 16);
-            }
-            for (int turn = 0; turn < teams; ++turn) {
-                if (turn == team && sub == 0) {
-                    float* to = turn == teams - 1 ? out : s_sums;
-                    const int step = turn == teams - 1 ? a.d : d;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const int c = VEC > 1 ? (e / VEC * tpr + t) * VEC + e % VEC : e * tpr + t;
-                        if (c >= d) continue;
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) to[k * step + c] = sums[k][e] + (turn ? s_sums[k * d + c] : 0.f);
+                for (int p = 0; p < E / 2; ++p) {
+                    float2 x = unpack_f2(acc[p]);
+                    if (tpr < 32) {
+                        x.x += __shfl_xor_sync(0xffffffffu, x.x, 16);
+                        x.y += __shfl_xor_sync(0xffffffffu, x.y, 16);
                     }
+                    s_sums[2 * p * nc + threadIdx.x] = x.x;
+                    s_sums[(2 * p + 1) * nc + threadIdx.x] = x.y;
                 }
-                if (teams > 1) op_named_barrier(15, nc);
+                op_named_barrier(15, nc);
+                for (int c = threadIdx.x; c < d; c += nc) {
+                    const int v = c / VEC, e = v / tpr * VEC + c % VEC;      // whose element e column c is
+                    const float* from = s_sums + e * nc + v % tpr;
+                    float sum = 0.f;
+                    for (int m = 0; m < teams; ++m) sum += from[m * team_threads];
+                    out[k * a.d + c] = sum;
+                }
+                op_named_barrier(15, nc);
             }
         }
     }
@@ -864,7 +865,7 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     const long long need = (W + (long long)spots * rows - 1) / ((long long)spots * rows);
     if (a.teams > need) a.teams = (int)need;              // few rows: spread over the multiprocessors first
     a.slot_bytes = VEC > 1 ? a.cols * (int)sizeof(T) : (a.cols * (int)sizeof(T) + 30) / 16 * 16;
-    const int sums = BWD && a.teams > 1 ? (3 * a.cols * 4 + 127) & ~127 : 0;
+    const int sums = BWD ? kElems * a.teams * team * 4 : 0;
     const int stage = ARRAYS * a.teams * rows * a.slot_bytes;
     a.stages = (kSmemMax - 8192 - sums) / stage;
     a.stages = a.stages > kMaxStages ? kMaxStages : a.stages;
