@@ -1395,7 +1395,8 @@ template <typename T>
 static cudaError_t launch_clip(const ClipArgs& a, int grid, bool overlap, cudaStream_t stream) {
     k_clip_sums<T><<<grid, kThreads, 0, stream>>>(a);
     const cudaError_t e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_pdl(overlap, k_clip_scale<T>, dim3(grid), dim3(kThreads), 0, stream, a);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(overlap, k_clip_scale<T>, dim3(a.tt.n_tiles, a.P), dim3(kThreads), 0, stream, a);
 }
 
 extern "C" {
@@ -1436,14 +1437,17 @@ eg_status eg_clip_gradients(eg_ctx* c, const void* grads, int dtype, double max_
     if (!claim_stream(c, stream)) return EG_ERR_STATE;
     if (!c->clip_partials) {
         const int grid = c->sms * kClipCtasPerSm;
-        eg_status s = dev_alloc(c, &c->clip_partials, (size_t)c->P + grid, false);
+        // partial sums, factors, the replicas' first CTAs, and the count of finished CTAs (zero; each call leaves it so)
+        eg_status s = dev_alloc(c, &c->clip_partials, 3 * (size_t)c->P + grid + 1);
         if (s != EG_OK) return s;
         c->clip_grid = grid;
     }
     const TileTable tt = c->tiles_norm.view(c->err);
     const int grid = (int)std::min<long long>(c->clip_grid, (long long)c->P * tt.n_tiles);
     const ClipArgs a{grads, out, tt, c->P, (long long)c->stride, max_norm, flags & EG_CLIP_ZERO_NONFINITE,
-                     c->clip_partials, norms_dev};
+                     c->clip_partials, c->clip_partials + c->P + c->clip_grid,
+                     reinterpret_cast<int*>(c->clip_partials + 2 * (size_t)c->P + c->clip_grid),
+                     reinterpret_cast<unsigned int*>(c->clip_partials + 3 * (size_t)c->P + c->clip_grid), norms_dev};
     const cudaError_t e = dtype == EG_F32    ? launch_clip<float>(a, grid, !c->no_pdl, stream)
                           : dtype == EG_BF16 ? launch_clip<__nv_bfloat16>(a, grid, !c->no_pdl, stream)
                                              : launch_clip<__half>(a, grid, !c->no_pdl, stream);
