@@ -485,6 +485,12 @@ def _matrix(t: Optional[torch.Tensor], shape: torch.Size, dtype: torch.dtype, de
     return t.data_ptr(), a, b
 
 
+def _new(x: torch.Tensor, shape: torch.Size) -> tuple:
+    """A new tensor of x's type and its (pointer, replica stride, row stride)."""
+    t = x.new_empty(shape)
+    return t, (t.data_ptr(), shape[1] * shape[2], shape[2])
+
+
 def _vector(t: Optional[torch.Tensor], shape: torch.Size, dtype: torch.dtype, device: int, what: str) -> tuple:
     """(pointer, replica stride, 0) of a ``[P, columns]`` tensor."""
     if t is None:
@@ -557,15 +563,19 @@ def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: 
     vec, dev = torch.Size((P, d)), residual.get_device()
     with _on_stream(residual, stream) as s:
         if residual_out is None:
-            residual_out = residual.new_empty(shape)
+            residual_out, m_res = _new(residual, shape)
+        else:
+            m_res = _matrix(residual_out, shape, dtype, dev, "residual_out")
         if out is None and w_pre is not None:
-            out = residual.new_empty(shape)
+            out, m_out = _new(residual, shape)
+        else:
+            m_out = _matrix(out, shape, dtype, dev, "out")
         args = _NORM_ARGS.pack(
             P, n, d, DTYPES[dtype], eps,
             *_matrix(y, shape, dtype, dev, "y"), *_matrix(residual, shape, dtype, dev, "residual"),
             *_vector(w_post, vec, dtype, dev, "w_post"), *_vector(gate, vec, dtype, dev, "gate"),
             *_vector(scale, vec, dtype, dev, "scale"), *_vector(w_pre, vec, dtype, dev, "w_pre"),
-            *_matrix(residual_out, shape, dtype, dev, "residual_out"), *_matrix(out, shape, dtype, dev, "out"), *_NONE8, 0, 0)
+            *m_res, *m_out, *_NONE8, 0, 0)
         if n:
             st = lib.eg_residual_norm(args, s)
             if st:
@@ -595,8 +605,8 @@ def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Option
             d_weights = tuple(None if w is None else residual.new_empty(vec) for w in (w_post, gate, scale, w_pre))
         elif len(d_weights) != 4:
             raise EventGradError("residual_norm_backward: d_weights holds four tensors or None")
-        dy = None if y is None else residual.new_empty(shape)
-        dr = residual.new_empty(shape)
+        dy, m_dy = (None, _NONE) if y is None else _new(residual, shape)
+        dr, m_dr = _new(residual, shape)
         bytes_ = lib.eg_residual_norm_workspace(P, d)
         workspace = residual.new_empty(bytes_, dtype=torch.uint8)
         g = d_weights
@@ -606,7 +616,7 @@ def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Option
             *_vector(w_post, vec, dtype, dev, "w_post"), *_vector(gate, vec, dtype, dev, "gate"),
             *_vector(scale, vec, dtype, dev, "scale"), *_vector(w_pre, vec, dtype, dev, "w_pre"), *_NONE, *_NONE,
             *_matrix(d_residual_out, shape, dtype, dev, "d_residual_out"), *_matrix(d_out, shape, dtype, dev, "d_out"),
-            *_matrix(dy, shape, dtype, dev, "dy"), *_matrix(dr, shape, dtype, dev, "d_residual"),
+            *m_dy, *m_dr,
             *_vector(g[0], vec, dtype, dev, "d_w_post"), *_vector(g[1], vec, dtype, dev, "d_gate"),
             *_vector(g[2], vec, dtype, dev, "d_scale"), *_vector(g[3], vec, dtype, dev, "d_w_pre"),
             workspace.data_ptr(), bytes_)
@@ -643,10 +653,12 @@ def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_do
     shape, dtype, dev = x.shape, x.dtype, x.get_device()
     with _on_stream(x, stream) as s:
         if out is None:
-            out = x.new_empty(shape)
+            out, m_out = _new(x, shape)
+        else:
+            m_out = _matrix(out, shape, dtype, dev, "out")
         head = (P, n, d, f, DTYPES[dtype], ACTIVATIONS[activation], *_matrix(x, shape, dtype, dev, "x"),
                 *_matrix(w_gate, up, dtype, dev, "w_gate"), *_matrix(w_up, up, dtype, dev, "w_up"),
-                *_matrix(w_down, down, dtype, dev, "w_down"), *_matrix(out, shape, dtype, dev, "out"), *_NONE5)
+                *_matrix(w_down, down, dtype, dev, "w_down"), *m_out, *_NONE5)
         saved, saved_bytes = None, 0
         if save:
             saved_bytes = lib.eg_feed_forward_saved_bytes(_FFN_ARGS.pack(*head, 0, 0))
@@ -679,12 +691,12 @@ def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
             d_weights = tuple(x.new_empty(sh) for sh in (up, up, down))
         elif len(d_weights) != 3:
             raise EventGradError("feed_forward_backward: d_weights holds three tensors or None")
-        dx = x.new_empty(shape)
+        dx, m_dx = _new(x, shape)
         args = _FFN_ARGS.pack(
             P, n, d, f, DTYPES[dtype], ACTIVATIONS[activation], *_matrix(x, shape, dtype, dev, "x"),
             *_matrix(w_gate, up, dtype, dev, "w_gate"), *_matrix(w_up, up, dtype, dev, "w_up"),
             *_matrix(w_down, down, dtype, dev, "w_down"), *_NONE, *_matrix(dy, shape, dtype, dev, "dy"),
-            *_matrix(dx, shape, dtype, dev, "dx"), *_matrix(d_weights[0], up, dtype, dev, "d_gate"),
+            *m_dx, *_matrix(d_weights[0], up, dtype, dev, "d_gate"),
             *_matrix(d_weights[1], up, dtype, dev, "d_up"), *_matrix(d_weights[2], down, dtype, dev, "d_down"),
             saved.data_ptr(), saved.numel())
         bytes_ = lib.eg_feed_forward_workspace(args, 1)
