@@ -329,7 +329,7 @@ struct Builder {
         }
     }
     void store_to(GemmProblem* g, const Mat& m, long long rows, long long cols) {
-        const int most = 128 / (int)b.size, columns = BN / 2 < most ? BN / 2 : most;
+        const int columns = BN / 2 < 32 ? BN / 2 : 32;
         g->ptr = m.p; g->rep = m.rep; g->row = m.row;
         g->out = in_place(m, b.P, rows, b.size) ? map(m, b.dtype, rows, cols, columns, 32) : -1;
     }
@@ -359,6 +359,20 @@ template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& 
     for (int k = 0; k < a.problems; ++k) {
         const int rows = !a.p[k].a_mn ? a.p[k].a_box : a.p[k].M > 64 ? 128 : 64;
         if (a.a_pitch < rows * 128) a.a_pitch = rows * 128;
+    }
+    a.heavy = a.extra = 0;
+    if (a.problems > 1 && a.tiles > sm_count() / 2) {      // (pairs: as launch_kernel counts them)
+        auto stages_of = [](const GemmProblem& g) {
+            int n = 0;
+            for (int e = 0; e < g.nseg; ++e) n += g.seg[e].ksteps;
+            return n;
+        };
+        const int pairs = sm_count() / 2, first = stages_of(a.p[0]), other = stages_of(a.p[1]), r = a.p[0].tiles % pairs;
+        if (other > 0 && first > other && r > 0) {
+            a.heavy = a.p[0].tiles;
+            const int fit = (a.tiles - a.heavy) / (pairs - r);
+            a.extra = first / other < fit ? first / other : fit;
+        }
     }
     const int stages = Shape::stages(a.a_pitch);
     // (fp32 hands its accumulator over every few stages and counts them one by one)

@@ -65,6 +65,8 @@ struct GemmArgs {
     CUtensorMap maps[kGemmMaxMaps];
     GemmProblem p[kGemmMaxProblems];
     int problems, tiles;
+    // The first `heavy` tiles take much longer than the others: see tile_of.
+    int heavy, extra;
     // Stages, and bytes of A from one to the next.  A tile with few rows fetches only those; the tensor cores then
     // read on into the next stage, for rows of D that nobody stores.
     int stages, a_pitch;
@@ -281,6 +283,28 @@ __device__ __forceinline__ void write_f32(unsigned char* box, int lane, const fl
         *reinterpret_cast<float4*>(box + swz128(lane * 128 + e * 4)) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
 }
 
+// The i-th tile of a pair of CTAs, -1 after its last.  Pairs take turns.  Where the first problem's tiles are longer
+// than the others' and do not come out even, the pairs that have one less of them (all from `r` on) first take
+// `extra` rounds of the others among themselves; the turns after that run backwards, so that a last, broken one
+// falls to those pairs too.
+__device__ __forceinline__ int tile_of(const GemmArgs& a, int pair, int pairs, int i) {
+    if (a.heavy == 0) {
+        const int t = pair + i * pairs;
+        return t < a.tiles ? t : -1;
+    }
+    const int r = a.heavy % pairs, mine = a.heavy / pairs + (pair < r);
+    if (i < mine) return pair + i * pairs;
+    int j = i - mine;
+    int t = a.heavy;
+    if (pair >= r && j < a.extra) {
+        t += j * (pairs - r) + pair - r;
+    } else {
+        if (pair >= r) j -= a.extra;
+        t += a.extra * (pairs - r) + j * pairs + pairs - 1 - pair;
+    }
+    return t < a.tiles ? t : -1;
+}
+
 struct TilePos {
     int problem, p, m, n;
 };
@@ -299,9 +323,10 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs& a, int t) {
 
 template <typename T, int EPI, int BN> struct GemmShape {
     static constexpr int kBBytes = BN / 2 * kGemmK * 2;         // of a stage
-    // staging of an epilogue warp: two boxes of results, or what the other epilogues lay out in 8 KB
-    static constexpr int kBoxCols = BN / 2 < 128 / (int)sizeof(T) ? BN / 2 : 128 / (int)sizeof(T);
-    static constexpr int kEpiBytes = EPI == kEpiStore ? 2 * 32 * kBoxCols * (int)sizeof(T) : 8192;
+    // Staging of an epilogue warp, as small as it gets: what it takes is missing for stages.  Two boxes of 64 bytes a
+    // row; the gradients' epilogue fetches its factors a box ahead, the fp32 ones stage values of 4 bytes.
+    static constexpr int kBoxCols = BN / 2 < 32 ? BN / 2 : 32;
+    static constexpr int kEpiBytes = EPI == kEpiStore ? 2 * 32 * kBoxCols * (int)sizeof(T) : EPI == kEpiGateUp && sizeof(T) == 2 ? 4096 : 8192;
     static constexpr int kEpi = kGemmEpiWarps * kEpiBytes;
     static constexpr int kBarBytes = 1024;
     static constexpr int kRing = 227 * 1024 - 1024 - kEpi - kBarBytes;   // both rings of stages
@@ -377,7 +402,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
         // warp 0 fetches A (and announces a stage's bytes), warp 3 fetches B
         if (elect_one()) {
             int s = 0, round = 0;
-            for (int t = pair; t < a.tiles; t += pairs) {
+            for (int turn = 0, t; (t = tile_of(a, pair, pairs, turn)) >= 0; ++turn) {
                 const TilePos q = tile_pos(a, t);
                 const GemmProblem& g = a.p[q.problem];
                 const int m0 = q.m * kGemmM + (int)rank * 128, n0 = g.b_pair ? q.n * (BN / 2) : q.n * BN + (int)rank * (BN / 2);
@@ -413,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
             int s = 0, round = 0, count = 0;                 // count: accumulators handed over
-            for (int t = pair; t < a.tiles; t += pairs) {
+            for (int turn = 0, t; (t = tile_of(a, pair, pairs, turn)) >= 0; ++turn) {
                 const TilePos q = tile_pos(a, t);
                 const GemmProblem& g = a.p[q.problem];
                 const uint32_t idesc = a.idesc | (g.a_mn ? 1u << 15 : 0u) | (g.b_mn ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
@@ -465,7 +490,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
         const uint32_t lanes = (uint32_t)((w & 3) * 32) << 16;
         int count = 0, uses = 0;
         (void)uses;
-        for (int t = pair; t < a.tiles; t += pairs) {
+        for (int turn = 0, t; (t = tile_of(a, pair, pairs, turn)) >= 0; ++turn) {
             const TilePos q = tile_pos(a, t);
             const GemmProblem& g = a.p[q.problem];
             const int buf = count & 1;
@@ -501,7 +526,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 }
             }
             if constexpr (EPI == kEpiStore) {
-                constexpr int CMAX = 128 / (int)sizeof(T), CW = BN / 2 < CMAX ? BN / 2 : CMAX;   // columns of one staged box
+                constexpr int CW = Shape::kBoxCols;                  // columns of one staged box
                 constexpr int ROW = CW * (int)sizeof(T);
                 auto swz = [](uint32_t off) { return ROW == 128 ? swz128(off) : ROW == 64 ? swz64(off) : off; };
                 if constexpr (sizeof(T) == 2) {
@@ -611,40 +636,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                             store_commit();
                         }
                     } else {
+                        uint32_t oh[CW / 2], oa[CW / 2], ob[CW / 2];
                         with_act(a.act, [&](auto act) {
 #pragma unroll
-                            for (int e = 0; e < CW; e += 8) {
-                                uint32_t oa[4], ob[4], oh[4];
-#pragma unroll
-                                for (int z = 0; z < 4; ++z) {
-                                    const float u0 = __uint_as_float(uv[e + 2 * z]), u1 = __uint_as_float(uv[e + 2 * z + 1]);
-                                    float a0, d0, a1, d1;
-                                    act_both<T, decltype(act)::value>(__uint_as_float(gv[e + 2 * z]), a0, d0);
-                                    act_both<T, decltype(act)::value>(__uint_as_float(gv[e + 2 * z + 1]), a1, d1);
-                                    oa[z] = pack2<T>(a0, a1);
-                                    ob[z] = pack2<T>(d0 * u0, d1 * u1);
-                                    oh[z] = pack2<T>(a0 * u0, a1 * u1);
-                                }
-                                uint32_t off = lane * (CW * 2) + e * 2;
-                                off = CW == 32 ? swz64(off) : off;
-                                *reinterpret_cast<uint4*>(buf_mem + off) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-                                if (a.map_a >= 0) {
-                                    *reinterpret_cast<uint4*>(buf_mem + 2048 + off) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
-                                    *reinterpret_cast<uint4*>(buf_mem + 4096 + off) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
-                                }
+                            for (int z = 0; z < CW / 2; ++z) {
+                                const float u0 = __uint_as_float(uv[2 * z]), u1 = __uint_as_float(uv[2 * z + 1]);
+                                float a0, d0, a1, d1;
+                                act_both<T, decltype(act)::value>(__uint_as_float(gv[2 * z]), a0, d0);
+                                act_both<T, decltype(act)::value>(__uint_as_float(gv[2 * z + 1]), a1, d1);
+                                oh[z] = pack2<T>(a0 * u0, a1 * u1);
+                                oa[z] = pack2<T>(a0, a1);
+                                ob[z] = pack2<T>(d0 * u0, d1 * u1);
                             }
                         });
-                        fence_async_shared();
-                        __syncwarp();
-                        if (elect_one()) {
-                            if (row0 < g.M && col0 < g.N) {
-                                tma_store(&a.maps[a.map_h], buf_mem, col0, row0, q.p);
-                                if (a.map_a >= 0) {
-                                    tma_store(&a.maps[a.map_a], buf_mem + 2048, col0, row0, q.p);
-                                    tma_store(&a.maps[a.map_b], buf_mem + 4096, col0, row0, q.p);
-                                }
+                        auto send = [&](const uint32_t (&v)[CW / 2], unsigned char* box, int map) {
+#pragma unroll
+                            for (int z = 0; z < CW / 2; z += 4) {
+                                const uint32_t off = lane * (CW * 2) + z * 4;
+                                *reinterpret_cast<uint4*>(box + (CW == 32 ? swz64(off) : off)) = make_uint4(v[z], v[z + 1], v[z + 2], v[z + 3]);
                             }
-                            store_commit();
+                            fence_async_shared();
+                            __syncwarp();
+                            if (elect_one()) {
+                                if (row0 < g.M && col0 < g.N) tma_store(&a.maps[map], box, col0, row0, q.p);
+                                store_commit();
+                            }
+                        };
+                        send(oh, buf_mem, a.map_h);
+                        if (a.map_a >= 0) {
+                            send(oa, buf_mem + 2048, a.map_a);
+                            store_wait_read<1>();
+                            __syncwarp();
+                            send(ob, buf_mem, a.map_b);
                         }
                     }
                 }
