@@ -8,6 +8,10 @@
 //               tile of which 128 - n rows are empty.)
 //   k_few_dot   everything else (fp32; 16-bit rows off the 16-byte boundaries): dot products in fp32, lanes along K.
 //
+// Bound by the memory: 1 token, 4 replicas, 1024 x 2816 in bf16: 10.3 us (4.5 TB/s) + 7.1 us (3.3 TB/s), of which some 2 us
+// each are the launch and the first load's latency.  Tried and slower: one unit of outputs per CTA (15.3 + 10.9 us:
+// every CTA begins with an empty memory pipe), two sixteens of outputs a warp for 32 tokens (46 us, 40 with one).
+//
 // Both split K over the warps of a CTA and add the warps' sums in order in shared memory.  They run twice:
 // for H = act(x Wg^T) * (x Wu^T) and for y = H Wd^T, the second as a dependent launch that fetches its first
 // weights before it waits for H.
