@@ -573,6 +573,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                             store_commit();
                         }
                     } else {
+                        if (elect_one()) store_commit();     // an empty group: the wait above counts one a box
                         __syncwarp();
                         T* out = static_cast<T*>(g.ptr) + (long long)q.p * g.rep;
                         const int rows = min(32, g.M - row0);
