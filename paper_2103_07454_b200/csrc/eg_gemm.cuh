@@ -327,6 +327,75 @@ __device__ __forceinline__ TilePos tile_pos(const GemmArgs& a, int t) {
     return q;
 }
 
+// `rows` (of 32) rows x `n` columns out of staged boxes of CW columns (WC in all, box after box `next` bytes apart) to
+// rows of any alignment; eight rows are read before the first of them is written, since the compiler cannot see that
+// the two do not overlap.  16-bit values go out in whole words, one of each row's WC / 2 a lane: rows that start in the
+// middle of a word take half of it from the lane before, and their first and last value go by themselves.
+template <typename T, int CW, int WC>
+__device__ __forceinline__ void write_rows(T* out, long long row, int rows, int n, int lane, const unsigned char* boxes, int next) {
+    constexpr int ROW = CW * (int)sizeof(T);
+    const bool whole = rows == 32 && n == WC;
+    if constexpr (sizeof(T) == 4) {
+        constexpr int X = (WC + 31) / 32;
+        float* to = out + lane;
+#pragma unroll 1
+        for (int k = 0; k < 32; k += 8) {
+            float v[8][X];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int x = 0; x < X; ++x)
+                    v[u][x] = *reinterpret_cast<const float*>(
+                        boxes + x * next + (k + u) * ROW + ((lane % CW * 4) ^ (ROW == 128 ? u << 4 : ROW == 64 ? (u >> 1 & 3) << 4 : 0)));
+#pragma unroll
+            for (int u = 0; u < 8; ++u, to += row)
+#pragma unroll
+                for (int x = 0; x < X; ++x)
+                    if (whole ? WC >= 32 || lane < WC : k + u < rows && x * 32 + lane < n) to[x * 32] = v[u][x];
+        }
+    } else {
+        constexpr int LANES = WC / 2, EACH = 32 / LANES;        // lanes of a row, rows at a time
+        const int j = lane % LANES, sub = lane / LANES;
+        uintptr_t at = reinterpret_cast<uintptr_t>(out + sub * row) + 4 * j;
+        const unsigned char* from = boxes + 2 * j / CW * next + sub * ROW;
+#pragma unroll 1
+        for (int k = 0; k < 32; k += 8 * EACH) {
+            uint32_t v[8], before[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = *reinterpret_cast<const uint32_t*>(
+                    from + (k + u * EACH) * ROW + ((2 * j % CW * 2) ^ (ROW == 64 ? (u * EACH >> 1 & 3) << 4 : 0)));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) before[u] = __shfl_sync(0xffffffffu, v[u], (j - 1) & (LANES - 1), LANES);
+#pragma unroll
+            for (int u = 0; u < 8; ++u, at += EACH * row * 2) {
+                const bool odd = at & 2;
+                const uint32_t word = odd ? __byte_perm(before[u], v[u], 0x5432) : v[u];
+                uint32_t* to = reinterpret_cast<uint32_t*>(at & ~(uintptr_t)3);
+                uint16_t* first = reinterpret_cast<uint16_t*>(at);
+                if (whole) {
+                    if (!odd || j > 0) {
+                        *to = word;
+                    } else {
+                        first[0] = (uint16_t)v[u];
+                        first[WC - 1] = (uint16_t)(before[u] >> 16);
+                    }
+                } else if (k + u * EACH + sub < rows) {
+                    const int x = 2 * j - odd;
+                    if (x < 0) {
+                        if (n > 0) first[0] = (uint16_t)v[u];
+                        if (n == WC) first[WC - 1] = (uint16_t)(before[u] >> 16);
+                    } else if (x + 1 < n) {
+                        *to = word;
+                    } else if (x < n) {
+                        *reinterpret_cast<uint16_t*>(to) = (uint16_t)word;
+                    }
+                }
+            }
+        }
+    }
+}
+
 template <typename T, int EPI, int BN> struct GemmShape {
     static constexpr int kBBytes = BN / 2 * kGemmK * 2;         // of a stage
     // Staging of an epilogue warp, as small as it gets: what it takes is missing for stages.  Two boxes of 64 bytes a
@@ -574,15 +643,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         }
                     } else {
                         if (elect_one()) store_commit();     // an empty group: the wait above counts one a box
-                        __syncwarp();
-                        T* out = static_cast<T*>(g.ptr) + (long long)q.p * g.rep;
-                        const int rows = min(32, g.M - row0);
-                        for (int r = 0; r < rows; ++r) {
-                            for (int x = lane; x < CW; x += 32) {
-                                if (col0 + x < g.N)
-                                    out[(long long)(row0 + r) * g.row + col0 + x] =
-                                        *reinterpret_cast<const T*>(box + swz(r * ROW + x * (int)sizeof(T)));
-                            }
+                        // two boxes at a time where there are two: longer runs of each row
+                        constexpr int WC = BN / 2 < 2 * CW ? BN / 2 : 2 * CW;
+                        if ((c + CW) % WC == 0) {
+                            __syncwarp();
+                            T* out = static_cast<T*>(g.ptr) + (long long)q.p * g.rep + (long long)row0 * g.row + (col0 + CW - WC);
+                            write_rows<T, CW, WC>(out, g.row, min(32, g.M - row0), min(WC, g.N - (col0 + CW - WC)), lane,
+                                                  WC == CW ? box : buf_mem, Shape::kEpiBytes / 2);
+                            __syncwarp();
                         }
                     }
                     ++uses;
