@@ -1,4 +1,4 @@
-"""Thin ctypes binding of the C ABI in ``include/eventgrad.h``.
+"""Thin binding of the C ABI in ``include/eventgrad.h``: ctypes for the step, ``csrc/marshal.cpp`` for the operators.
 
 Argument marshalling only: every step of the path runs in the CUDA library.  PyTorch is used
 for device memory and streams.  There is no fallback — if ``libeventgrad.so`` has not been
@@ -6,6 +6,7 @@ built (``python -m paper_2103_07454_b200.build``) the first use raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import struct
@@ -65,11 +66,12 @@ class EventGradError(RuntimeError):
 
 
 _lib = None
+_native = None        # csrc/marshal.cpp: the operators' arguments
 
 
 def load_library() -> C.CDLL:
     """Loads the CUDA library; raises if it is missing (there is no CPU path)."""
-    global _lib
+    global _lib, _native
     if _lib is not None:
         return _lib
     # EG_LIBRARY names another build of the same library (the bounds-checked one, for instance)
@@ -134,7 +136,14 @@ def load_library() -> C.CDLL:
     lib.eg_feed_forward_workspace.restype = C.c_int64
     lib.eg_last_cuda_error.argtypes = [vp]
     lib.eg_last_launch_count.argtypes = [vp]
-    _lib = lib
+    try:
+        from . import _marshal
+    except ImportError as e:
+        raise EventGradError(f"{e}: build it with `python -m paper_2103_07454_b200.build`") from e
+    _marshal.init(EventGradError, *(C.cast(getattr(lib, f), vp).value for f in (
+        "eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace", "eg_feed_forward",
+        "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace")))
+    _lib, _native = lib, _marshal
     return lib
 
 
@@ -395,22 +404,12 @@ class EventGrad:
         tensors) of at most ``max_norm``.  ``grads``: ``[P, replica_stride]`` fp32, bf16 or fp16; the
         result goes to ``out`` (fp32, same shape; default: ``grads`` itself, which must then be fp32).
         Returns the norms before clipping, ``[P]`` fp32 on the device."""
-        dtype = DTYPES.get(grads.dtype)
-        if out is None:
-            out = grads
-        assert dtype is not None and out.dtype is torch.float32
-        assert grads.is_cuda and out.is_cuda and grads.is_contiguous() and out.is_contiguous()
-        assert grads.shape == out.shape == (self.P, self.replica_stride)
-        with _on_stream(grads, stream) as s:
-            if norms is None:
-                norms = out.new_empty(self.P)
-            assert norms.is_cuda and norms.dtype is torch.float32 and norms.is_contiguous() and norms.numel() == self.P
-            st = self._lib.eg_clip_gradients(self._h, grads.data_ptr(), dtype, max_norm,
-                                             CLIP_ZERO_NONFINITE if zero_nonfinite else 0, out.data_ptr(),
-                                             norms.data_ptr(), s)
-        if st:
-            _check(self._lib, st, self._h, "eg_clip_gradients")
-        return norms
+        with _on(stream):
+            r = _native.clip_gradients(self._h.value if self._h else 0, self.P, self.replica_stride, grads, out, max_norm,
+                                       CLIP_ZERO_NONFINITE if zero_nonfinite else 0, norms)
+        if r.__class__ is int:
+            _check(self._lib, r, self._h, "eg_clip_gradients")
+        return r
 
     def set_fused_kernel(self, kind: int):
         _check(self._lib, self._lib.eg_set_fused_kernel(self._h, int(kind)), self._h,
@@ -467,83 +466,22 @@ def change_norms_static(x: torch.Tensor, xhat: torch.Tensor, tensor_offset: Sequ
 # operators around the step: values of one type per call, ``[P, rows, width]`` activations and
 # ``[P, ...]`` views of the replicas' weights, on torch's current stream unless one is given
 # --------------------------------------------------------------------------------------
-_NONE = (0, 0, 0)
-_NONE5, _NONE8 = _NONE * 5, _NONE * 8
 _FFN_ARGS = struct.Struct("=6q30q2q")     # eg_feed_forward_args
 _NORM_ARGS = struct.Struct("=4qd48q2q")   # eg_residual_norm_args
+_CURRENT = contextlib.nullcontext()
 
 
-def _matrix(t: Optional[torch.Tensor], shape: torch.Size, dtype: torch.dtype, device: int, what: str) -> tuple:
-    """(pointer, replica stride, row stride) of a ``[P, rows, columns]`` tensor."""
-    if t is None:
-        return _NONE
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
-        raise _unexpected(t, shape, dtype, device, what)
-    a, b, c = t.stride()
-    if c != 1 and shape[2] > 1:
-        raise EventGradError(f"{what}: the last dimension must be contiguous")
-    return t.data_ptr(), a, b
+def _on(stream: Optional[torch.cuda.Stream]):
+    """Makes ``stream`` current: outputs and workspaces then belong to the stream that uses them."""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
 
 
-def _new(x: torch.Tensor, shape: torch.Size) -> tuple:
-    """A new tensor of x's type and its (pointer, replica stride, row stride)."""
-    t = x.new_empty(shape)
-    return t, (t.data_ptr(), shape[1] * shape[2], shape[2])
-
-
-def _vector(t: Optional[torch.Tensor], shape: torch.Size, dtype: torch.dtype, device: int, what: str) -> tuple:
-    """(pointer, replica stride, 0) of a ``[P, columns]`` tensor."""
-    if t is None:
-        return _NONE
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
-        raise _unexpected(t, shape, dtype, device, what)
-    a, b = t.stride()
-    if b != 1 and shape[1] > 1:
-        raise EventGradError(f"{what}: the last dimension must be contiguous")
-    return t.data_ptr(), a, 0
-
-
-def _unexpected(t, shape, dtype, device, what):
-    return EventGradError(f"{what}: expected {tuple(shape)} {dtype} on cuda:{device}, "
-                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
-
-
-class _Elsewhere:
-    """Makes ``stream``, or else the tensors' device, current: outputs and workspaces then belong to the stream
-    that uses them."""
-
-    def __init__(self, device: int, stream: Optional[torch.cuda.Stream]):
-        self._ctx = torch.cuda.stream(stream) if stream is not None else torch.cuda.device(device)
-        self._device = device
-
-    def __enter__(self) -> int:
-        self._ctx.__enter__()
-        return torch.cuda.current_stream(self._device).cuda_stream
-
-    def __exit__(self, *exc):
-        self._ctx.__exit__(*exc)
-
-
-class _Here:
-    """The current stream of the current device, without the cost of looking up stream objects."""
-
-    def __init__(self, handle: int):
-        self._handle = handle
-
-    def __enter__(self) -> int:
-        return self._handle
-
-    def __exit__(self, *exc):
-        pass
-
-
-def _on_stream(x: torch.Tensor, stream: Optional[torch.cuda.Stream]):
-    device = x.get_device()
-    if device < 0:
-        raise EventGradError("no CUDA device: this library has no CPU path")
-    if stream is None and device == torch._C._cuda_getDevice():
-        return _Here(torch._C._cuda_getCurrentRawStream(device))
-    return _Elsewhere(device, stream)
+def _some(d_weights: Optional[Sequence], n: int, what: str) -> Optional[tuple]:
+    if d_weights is None:
+        return None
+    if len(d_weights) != n:
+        raise EventGradError(f"{what}: d_weights holds {n} tensors or None")
+    return tuple(d_weights)
 
 
 def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: Optional[torch.Tensor] = None,
@@ -556,31 +494,11 @@ def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: 
 
     Returns ``(r', o)``; ``o`` is None without ``w_pre``.  ``y`` None: only the scaled residual."""
     lib = load_library()
-    shape, dtype = residual.shape, residual.dtype
-    if len(shape) != 3 or dtype not in DTYPES:
-        raise EventGradError("residual_norm: residual must be [P, rows, width] fp32, bf16 or fp16")
-    P, n, d = shape
-    vec, dev = torch.Size((P, d)), residual.get_device()
-    with _on_stream(residual, stream) as s:
-        if residual_out is None:
-            residual_out, m_res = _new(residual, shape)
-        else:
-            m_res = _matrix(residual_out, shape, dtype, dev, "residual_out")
-        if out is None and w_pre is not None:
-            out, m_out = _new(residual, shape)
-        else:
-            m_out = _matrix(out, shape, dtype, dev, "out")
-        args = _NORM_ARGS.pack(
-            P, n, d, DTYPES[dtype], eps,
-            *_matrix(y, shape, dtype, dev, "y"), *_matrix(residual, shape, dtype, dev, "residual"),
-            *_vector(w_post, vec, dtype, dev, "w_post"), *_vector(gate, vec, dtype, dev, "gate"),
-            *_vector(scale, vec, dtype, dev, "scale"), *_vector(w_pre, vec, dtype, dev, "w_pre"),
-            *m_res, *m_out, *_NONE8, 0, 0)
-        if n:
-            st = lib.eg_residual_norm(args, s)
-            if st:
-                _check(lib, st, None, "eg_residual_norm")
-    return residual_out, out
+    with _on(stream):
+        r = _native.residual_norm(y, residual, w_post, gate, scale, w_pre, eps, residual_out, out)
+    if r.__class__ is int:
+        _check(lib, r, None, "eg_residual_norm")
+    return r
 
 
 def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Optional[torch.Tensor],
@@ -595,49 +513,18 @@ def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Option
     ``d_weights``: four ``[P, width]`` tensors that receive the last ones (views of a gradient buffer in
     the step's layout, say; None for a vector that was not given); default: new tensors."""
     lib = load_library()
-    shape, dtype = residual.shape, residual.dtype
-    if len(shape) != 3 or dtype not in DTYPES:
-        raise EventGradError("residual_norm_backward: residual must be [P, rows, width] fp32, bf16 or fp16")
-    P, n, d = shape
-    vec, dev = torch.Size((P, d)), residual.get_device()
-    with _on_stream(residual, stream) as s:
-        if d_weights is None:
-            d_weights = tuple(None if w is None else residual.new_empty(vec) for w in (w_post, gate, scale, w_pre))
-        elif len(d_weights) != 4:
-            raise EventGradError("residual_norm_backward: d_weights holds four tensors or None")
-        dy, m_dy = (None, _NONE) if y is None else _new(residual, shape)
-        dr, m_dr = _new(residual, shape)
-        bytes_ = lib.eg_residual_norm_workspace(P, d)
-        workspace = residual.new_empty(bytes_, dtype=torch.uint8)
-        g = d_weights
-        args = _NORM_ARGS.pack(
-            P, n, d, DTYPES[dtype], eps,
-            *_matrix(y, shape, dtype, dev, "y"), *_matrix(residual, shape, dtype, dev, "residual"),
-            *_vector(w_post, vec, dtype, dev, "w_post"), *_vector(gate, vec, dtype, dev, "gate"),
-            *_vector(scale, vec, dtype, dev, "scale"), *_vector(w_pre, vec, dtype, dev, "w_pre"), *_NONE, *_NONE,
-            *_matrix(d_residual_out, shape, dtype, dev, "d_residual_out"), *_matrix(d_out, shape, dtype, dev, "d_out"),
-            *m_dy, *m_dr,
-            *_vector(g[0], vec, dtype, dev, "d_w_post"), *_vector(g[1], vec, dtype, dev, "d_gate"),
-            *_vector(g[2], vec, dtype, dev, "d_scale"), *_vector(g[3], vec, dtype, dev, "d_w_pre"),
-            workspace.data_ptr(), bytes_)
-        if n:
-            _check(lib, lib.eg_residual_norm_backward(args, s), None, "eg_residual_norm_backward")
-        else:
-            for t in g:
-                if t is not None:
-                    t.zero_()
-    return dy, dr, tuple(d_weights)
+    d_weights = _some(d_weights, 4, "residual_norm_backward")
+    with _on(stream):
+        r = _native.residual_norm_backward(d_residual_out, d_out, y, residual, w_post, gate, scale, w_pre, eps, d_weights)
+    if r.__class__ is int:
+        _check(lib, r, None, "eg_residual_norm_backward")
+    return r
 
 
-def _ffn_sizes(x: torch.Tensor, w_gate: torch.Tensor, activation: str, what: str):
-    shape, up = x.shape, w_gate.shape
-    if len(shape) != 3 or len(up) != 3 or x.dtype not in DTYPES:
-        raise EventGradError(f"{what}: x must be [P, rows, d_model] and w_gate [P, d_ff, d_model], fp32, bf16 or fp16")
-    if activation not in ACTIVATIONS:
-        raise EventGradError(f"{what}: activation must be one of {sorted(ACTIVATIONS)}")
-    P, n, d = shape
-    f = up[1]
-    return P, n, d, f, torch.Size((P, f, d)), torch.Size((P, d, f))
+def _activation(name: str) -> int:
+    if name not in ACTIVATIONS:
+        raise EventGradError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    return ACTIVATIONS[name]
 
 
 def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
@@ -649,28 +536,11 @@ def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_do
     (views of a parameter buffer, say).  With ``save`` returns ``(y, saved)``, the second for
     ``feed_forward_backward``."""
     lib = load_library()
-    P, n, d, f, up, down = _ffn_sizes(x, w_gate, activation, "feed_forward")
-    shape, dtype, dev = x.shape, x.dtype, x.get_device()
-    with _on_stream(x, stream) as s:
-        if out is None:
-            out, m_out = _new(x, shape)
-        else:
-            m_out = _matrix(out, shape, dtype, dev, "out")
-        head = (P, n, d, f, DTYPES[dtype], ACTIVATIONS[activation], *_matrix(x, shape, dtype, dev, "x"),
-                *_matrix(w_gate, up, dtype, dev, "w_gate"), *_matrix(w_up, up, dtype, dev, "w_up"),
-                *_matrix(w_down, down, dtype, dev, "w_down"), *m_out, *_NONE5)
-        saved, saved_bytes = None, 0
-        if save:
-            saved_bytes = lib.eg_feed_forward_saved_bytes(_FFN_ARGS.pack(*head, 0, 0))
-            saved = x.new_empty(saved_bytes, dtype=torch.uint8)
-        if n:
-            args = _FFN_ARGS.pack(*head, saved.data_ptr() if save else 0, saved_bytes)
-            bytes_ = lib.eg_feed_forward_workspace(args, 0)
-            workspace = x.new_empty(bytes_, dtype=torch.uint8).data_ptr() if bytes_ else 0
-            st = lib.eg_feed_forward(args, workspace, bytes_, s)
-            if st:
-                _check(lib, st, None, "eg_feed_forward")
-    return (out, saved) if save else out
+    with _on(stream):
+        r = _native.feed_forward(x, w_gate, w_up, w_down, _activation(activation), bool(save), out)
+    if r.__class__ is int:
+        _check(lib, r, None, "eg_feed_forward")
+    return r
 
 
 def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
@@ -682,27 +552,12 @@ def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
     ``d_weights``: three tensors of the weights' shapes that receive the last ones (views of a gradient
     buffer in the step's layout, say; None: not wanted); default: new tensors."""
     lib = load_library()
-    P, n, d, f, up, down = _ffn_sizes(x, w_gate, activation, "feed_forward_backward")
-    shape, dtype, dev = x.shape, x.dtype, x.get_device()
-    if saved.get_device() != dev or saved.dtype is not torch.uint8 or not saved.is_contiguous():
-        raise EventGradError("feed_forward_backward: saved is what feed_forward(..., save=True) returned")
-    with _on_stream(x, stream) as s:
-        if d_weights is None:
-            d_weights = tuple(x.new_empty(sh) for sh in (up, up, down))
-        elif len(d_weights) != 3:
-            raise EventGradError("feed_forward_backward: d_weights holds three tensors or None")
-        dx, m_dx = _new(x, shape)
-        args = _FFN_ARGS.pack(
-            P, n, d, f, DTYPES[dtype], ACTIVATIONS[activation], *_matrix(x, shape, dtype, dev, "x"),
-            *_matrix(w_gate, up, dtype, dev, "w_gate"), *_matrix(w_up, up, dtype, dev, "w_up"),
-            *_matrix(w_down, down, dtype, dev, "w_down"), *_NONE, *_matrix(dy, shape, dtype, dev, "dy"),
-            *m_dx, *_matrix(d_weights[0], up, dtype, dev, "d_gate"),
-            *_matrix(d_weights[1], up, dtype, dev, "d_up"), *_matrix(d_weights[2], down, dtype, dev, "d_down"),
-            saved.data_ptr(), saved.numel())
-        bytes_ = lib.eg_feed_forward_workspace(args, 1)
-        workspace = x.new_empty(bytes_, dtype=torch.uint8)
-        _check(lib, lib.eg_feed_forward_backward(args, workspace.data_ptr(), bytes_, s), None, "eg_feed_forward_backward")
-    return dx, tuple(d_weights)
+    d_weights = _some(d_weights, 3, "feed_forward_backward")
+    with _on(stream):
+        r = _native.feed_forward_backward(x, w_gate, w_up, w_down, _activation(activation), dy, saved, d_weights)
+    if r.__class__ is int:
+        _check(lib, r, None, "eg_feed_forward_backward")
+    return r
 
 
 def operator_status(device: Optional[torch.device] = None) -> int:

@@ -5,12 +5,16 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = [os.path.join(HERE, "csrc", "eventgrad.cu"), os.path.join(HERE, "csrc", "eg_norms_static.cu")]
 #: the operators around the step: their products may be contracted into fused multiply-adds
 OPS = [os.path.join(HERE, "csrc", f) for f in ("eg_residual_norm.cu", "eg_feed_forward.cu")]
 LIB = os.path.join(HERE, "libeventgrad.so")
+#: torch tensors to C arguments, for the operators
+MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 LIB_DEBUG = os.path.join(HERE, "libeventgrad_debug.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
@@ -42,7 +46,22 @@ def _compile(lib: str, extra, force: bool, verbose: bool) -> str:
     return lib
 
 
+def build_marshal(force: bool = False) -> str:
+    newest = max(os.path.getmtime(p) for p in (MARSHAL_SRC, os.path.join(HERE, "..", "include", "eventgrad.h")))
+    if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < newest:
+        import torch
+        top = os.path.dirname(torch.__file__)
+        include = [os.path.join(top, "include"), os.path.join(top, "include", "torch", "csrc", "api", "include"),
+                   sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")]
+        subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+                       + [a for d in include for a in ("-isystem", d)] + ["-o", MARSHAL, MARSHAL_SRC, "-L" + os.path.join(top, "lib")]
+                       + ["-l" + n for n in ("torch_python", "torch_cuda", "c10_cuda", "torch_cpu", "c10")], check=True)
+    return MARSHAL
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_marshal(force)
     return _compile(LIB, [], force, verbose)
 
 
