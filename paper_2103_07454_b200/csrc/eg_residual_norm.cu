@@ -20,7 +20,7 @@
 // k_norm_stream does both for many rows: one CTA (cluster) per multiprocessor (group of them), rows
 // streamed through shared memory by bulk copies well ahead of their use, everything else in
 // registers.  k_norm_few does the forward pass where there are few rows and a row's way through
-// shared memory would only add to its latency.
+// shared memory would only add to its latency, k_norm_rows that of few unaligned rows and the gradients of few rows.
 #include <type_traits>
 
 #include "eg_ops.cuh"
@@ -35,6 +35,7 @@ constexpr int kElems = 16;                // elements of a row per thread
 constexpr int kCtaWidth = kThreads * kElems;   // columns of one CTA; wider rows are shared by a cluster
 constexpr int kMaxCtas = 160;             // one per multiprocessor; bounds the workspace
 constexpr int kMaxStages = 4;
+constexpr int kRowThreads = 512;
 constexpr int kSmemMax = 227 * 1024;
 
 struct Mat {
@@ -759,6 +760,139 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// The same for few rows where k_norm_few does not serve: gradients, and rows off the 16-byte boundaries.  Such calls
+// are bound by latency, that of fetching the code of unrolled loops included, so this one is short: a CTA takes one
+// row after the other, a thread the same columns of every row, and the passes over a row after the first find it in
+// the L1.  The column sums of a replica's rows lie in shared memory, each thread's by itself.
+// Measured, 4 rows of 1024 on 2 replicas with gradients: 12 us with k_norm_columns, k_norm_stream 36.
+template <typename T, int VEC, bool BWD>
+__global__ void __launch_bounds__(kRowThreads) k_norm_rows(const __grid_constant__ NormArgs a) {
+    constexpr int K = BWD ? 5 : 1;
+    extern __shared__ float s_acc[];
+    __shared__ float s_red[2][K][kRowThreads / 32];
+    if (BWD) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int b = blockIdx.x, G = gridDim.x, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const long long W = (long long)a.P * a.rows, u1 = cut(W, b + 1, G);
+    long long u = cut(W, b, G);
+    int i = (int)(u / a.rows);
+    long long row = u % a.rows;
+    const bool has_y = a.in[0].p != nullptr, post = has_y && a.w_post.p, has_do = BWD && a.in[3].p, second = BWD ? has_do : a.o.p != nullptr;
+    struct Values { float v[VEC]; };
+    auto value = [](const Mat& m, int i, long long t, int c, float otherwise) {
+        Values x;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x.v[e] = otherwise;
+        if (m.p) load_vec<T, VEC>(row_of<T>(m, i, t) + c, x.v);
+        return x;
+    };
+    auto factor = [&](int c) {
+        Values f = value(a.w_post, i, 0, c, has_y ? 1.f : 0.f);
+        if (a.gate.p) {
+            const Values g = value(a.gate, i, 0, c, 0.f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f.v[e] *= sigmoid_f(g.v[e]);
+        }
+        return f;
+    };
+    auto sums = [&](float (&v)[K], int which) {          // over the threads of the CTA
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+            if (lane == 0) s_red[which][k][threadIdx.x >> 5] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = lane < warps ? s_red[which][k][lane] : 0.f;
+            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
+    };
+    bool begun = false;                                  // rows of replica i lie in the column sums
+    for (; u < u1; ++u) {
+        float v[K] = {}, inv1 = 1.f;
+        if (post) {
+            for (int c = threadIdx.x * VEC; c < a.d; c += blockDim.x * VEC) {
+                const Values y = value(a.in[0], i, row, c, 0.f);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[0] = fmaf(y.v[e], y.v[e], v[0]);
+            }
+            sums(v, 0);
+            inv1 = rsqrtf(fmaf(v[0], a.inv_d, a.eps));
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = 0.f;
+        if (BWD || second) {
+            for (int c = threadIdx.x * VEC; c < a.d; c += blockDim.x * VEC) {
+                const Values y = value(a.in[0], i, row, c, 0.f), r = value(a.in[1], i, row, c, 0.f), dr = value(a.in[2], i, row, c, 0.f);
+                const Values o = value(a.in[3], i, row, c, 0.f), w = value(a.w_pre, i, 0, c, 0.f), s = value(a.scale, i, 0, c, 1.f);
+                const Values f = factor(c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float Q = f.v[e] * y.v[e], R = fmaf(inv1, Q, s.v[e] * r.v[e]);
+                    v[0] = fmaf(R, R, v[0]);
+                    if constexpr (BWD) {
+                        const float dn = has_do ? w.v[e] * o.v[e] : 0.f;
+                        v[1] = fmaf(dn, R, v[1]);
+                        v[2] = fmaf(Q, dr.v[e], v[2]);
+                        v[3] = fmaf(dn, Q, v[3]);
+                        v[4] = fmaf(Q, R, v[4]);
+                    }
+                }
+            }
+            sums(v, 1);
+        }
+        const float inv2 = second ? rsqrtf(fmaf(v[0], a.inv_d, a.eps)) : 0.f;
+        float c3 = 0.f, c4 = 0.f;
+        if constexpr (BWD) {
+            c3 = inv2 * inv2 * v[1] * a.inv_d;                                       // inv2 * mean(dn * rh)
+            c4 = post ? inv1 * (v[2] + inv2 * (v[3] - c3 * v[4])) * a.inv_d : 0.f;
+        }
+        const bool last = u + 1 == u1 || row + 1 == a.rows;
+        float* out = a.partials + (long long)(i + b) * 3 * a.d;
+        for (int c = threadIdx.x * VEC; c < a.d; c += blockDim.x * VEC) {
+            const Values y = value(a.in[0], i, row, c, 0.f), r = value(a.in[1], i, row, c, 0.f), f = factor(c);
+            const Values w = value(a.w_pre, i, 0, c, 0.f), s = value(a.scale, i, 0, c, 1.f);
+            float x0[VEC], x1[VEC];
+            if constexpr (!BWD) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    x0[e] = fmaf(inv1, f.v[e] * y.v[e], s.v[e] * r.v[e]);
+                    x1[e] = x0[e] * inv2 * w.v[e];
+                }
+                if (a.r_out.p) store_vec<T, VEC>(row_of<T>(a.r_out, i, row) + c, x0);
+                if (second) store_vec<T, VEC>(row_of<T>(a.o, i, row) + c, x1);
+            } else {
+                const Values dr = value(a.in[2], i, row, c, 0.f), o = value(a.in[3], i, row, c, 0.f);
+                float part[3][VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float R = fmaf(inv1, f.v[e] * y.v[e], s.v[e] * r.v[e]), dn = has_do ? w.v[e] * o.v[e] : 0.f;
+                    const float dR = fmaf(-inv2 * c3, R, fmaf(inv2, dn, dr.v[e])), tR = dR * inv1;
+                    x0[e] = s.v[e] * dR;
+                    x1[e] = fmaf(-inv1 * inv1 * c4, y.v[e], f.v[e] * tR);
+                    part[0][e] = tR * y.v[e];
+                    part[1][e] = dR * r.v[e];
+                    part[2][e] = o.v[e] * (R * inv2);
+                }
+                if (a.dr.p) store_vec<T, VEC>(row_of<T>(a.dr, i, row) + c, x0);
+                if (a.dy.p) store_vec<T, VEC>(row_of<T>(a.dy, i, row) + c, x1);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        if (begun) part[k][e] += s_acc[k * a.d + c + e];
+                        if (last) out[k * a.d + c + e] = part[k][e];
+                        else s_acc[k * a.d + c + e] = part[k][e];
+                    }
+                }
+            }
+        }
+        begun = !last;
+        if (++row == a.rows) { row = 0; ++i; }
+    }
+}
+
 // Adds up the partial column sums of replica blockIdx.y (CTA after CTA) and forms the gradients of
 // the four vectors.  G == 0: there were no rows.
 template <typename T>
@@ -905,12 +1039,40 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     return cudaLaunchKernelEx(&cfg, k_norm_stream<T, VEC, BWD>, a);
 }
 
+// Launches k_norm_rows where its CTAs get few rows; *G: its CTAs, 0 otherwise.  Measured, us, against k_norm_stream:
+// bf16, 2 rows a CTA: 1024 columns 16 against 23, 2984 24 against 26, 4567 43 against 35; 1 row: 4567 28 against 30, 8192
+// 33 against 27; 4 rows: 1001 25 against 24; fp32, 2 rows: 1024 13 against 17, 2984 21 against 28, 4567 42 against 35;
+// 1 row: 8192 25 against 30.
+template <typename T, int VEC, bool BWD> cudaError_t short_runs(const NormArgs& a, int* G, cudaStream_t stream) {
+    const long long W = (long long)a.P * a.rows;
+    const int sms = sm_count() < kMaxCtas ? sm_count() : kMaxCtas;
+    if (sms < 1) return cudaErrorInvalidDevice;
+    *G = 0;
+    const long long ctas = BWD ? sms : 4ll * sms;         // (the backward call's workspace holds that many CTAs' sums)
+    if (W > (a.d <= kCtaWidth ? 2 : 1) * ctas) return cudaSuccess;
+    *G = (int)(W < ctas ? W : ctas);
+    const int each = (a.d + VEC - 1) / VEC, threads = each < kRowThreads ? (each + 31) / 32 * 32 : kRowThreads;
+    const int smem = BWD && W > *G ? 3 * a.d * (int)sizeof(float) : 0;
+    cudaError_t e;
+    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(k_norm_rows<T, VEC, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMaxWidth * 4)) != cudaSuccess)
+        return e;
+    return launch_after(k_norm_rows<T, VEC, BWD>, dim3(*G), dim3(threads), smem, stream, a);
+}
+
 // 16-byte accesses where every row allows them.
 template <typename T> cudaError_t forward(const NormArgs& a, bool aligned, cudaStream_t stream) {
     constexpr int V = 16 / (int)sizeof(T);
     int G = 0;
+    const long long W = (long long)a.P * a.rows;
+    // Rows off the 16-byte boundaries, us: bf16 of 1001 columns, k_norm_rows 6 for 148 rows, 11 for 592, k_norm_few 13 and 14; of
+    // 4567 columns 15 and 34 against 23 and 58; fp32 of 8191 columns 25 against 17 for 148 rows.  k_norm_few of wide ones takes 47
+    // for 296 rows, 63 for 592, k_norm_stream 34 for 1184.
+    if (!aligned && a.d <= 6144) {
+        const cudaError_t e = short_runs<T, 1, false>(a, &G, stream);
+        if (e != cudaSuccess || G > 0) return e;
+    }
     // few rows: below eight for every warp of the streaming kernel its ring hardly fills
-    if ((long long)a.P * a.rows * ((a.d + 511) / 512) > 8ll * (kThreads / 32) * sm_count())
+    if (W * ((a.d + 511) / 512) > 8ll * (kThreads / 32) * sm_count() || (!aligned && a.d > 2048 && W > sm_count()))
         return aligned ? stream_rows<T, V, false>(a, &G, stream) : stream_rows<T, 1, false>(a, &G, stream);
     if (a.d <= 2048) return aligned ? few<T, V, 8>(a, stream) : few<T, 1, 8>(a, stream);
     return aligned ? few<T, V, 16>(a, stream) : few<T, 1, 16>(a, stream);
@@ -920,7 +1082,8 @@ template <typename T> cudaError_t backward(const NormArgs& a, bool aligned, cons
     constexpr int V = 16 / (int)sizeof(T);
     int G = 0;
     if (a.rows > 0) {
-        const cudaError_t e = aligned ? stream_rows<T, V, true>(a, &G, stream) : stream_rows<T, 1, true>(a, &G, stream);
+        cudaError_t e = aligned ? short_runs<T, V, true>(a, &G, stream) : short_runs<T, 1, true>(a, &G, stream);
+        if (e == cudaSuccess && G == 0) e = aligned ? stream_rows<T, V, true>(a, &G, stream) : stream_rows<T, 1, true>(a, &G, stream);
         if (e != cudaSuccess) return e;
     }
     if (!q->d_w_post.data && !q->d_gate.data && !q->d_scale.data && !q->d_w_pre.data) return cudaSuccess;
