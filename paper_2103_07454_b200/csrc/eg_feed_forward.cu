@@ -342,25 +342,18 @@ struct Builder {
         g->tiles = (int)tiles;
         a.tiles += g->tiles;
         g->nseg = 0;
-        g->small = 0;
         g->a_box = a_box(M);
         g->a_mn = a_mn; g->b_mn = b_mn; g->b_pair = pair;
         g->M = (int)M; g->N = (int)N;
         g->out = -1;
         return g;
     }
-    // sum of A B^T over K of one or two pairs, as products of parts, the smaller ones first
+    // sum of A B^T over K of one or two pairs
     struct Pair { int ma, mb0, mb1; };
     void product(GemmProblem* g, std::initializer_list<Pair> pairs, long long K) {
-        const int ksteps = (int)((K + kGemmK - 1) / kGemmK);
-        for (int sum = b.parts - 1; sum >= 0; --sum) {
-            for (const Pair& p : pairs) {
-                for (int i = 0; i <= sum; ++i) {
-                    if (g->nseg >= kGemmMaxSegs) { ok = false; return; }
-                    g->seg[g->nseg++] = GemmSeg{p.ma + i, p.mb0 + sum - i, p.mb1 + sum - i, ksteps};
-                    if (sum > 0) g->small += ksteps;
-                }
-            }
+        for (const Pair& p : pairs) {
+            if (g->nseg >= kGemmMaxSegs) { ok = false; return; }
+            g->seg[g->nseg++] = GemmSeg{p.ma, p.mb0, p.mb1, (int)((K + kGemmK - 1) / kGemmK)};
         }
     }
     void store_to(GemmProblem* g, const Mat& m, long long rows, long long cols) {
@@ -400,7 +393,7 @@ template <typename T, int EPI, int BN> cudaError_t launch_shape(const GemmArgs& 
         // a tile's time in stages: its epilogue, which runs under the next tile's products, takes some 8 (plain stores 16)
         auto stages_of = [](const GemmProblem& g) {
             int n = 0;
-            for (int e = 0; e < g.nseg; ++e) n += g.seg[e].ksteps;
+            for (int e = 0; e < g.nseg; ++e) n += g.seg[e].ksteps * (sizeof(T) == 4 ? 6 : 1);
             const int epilogue = g.out >= 0 ? 8 : 16;
             return n > epilogue ? n : epilogue;
         };
@@ -445,17 +438,19 @@ template <typename T, int EPI> cudaError_t launch_gemm(Builder& w, cudaStream_t 
 }
 
 // Tile width of a launch: the one whose last pair of multiprocessors should be done first.  A stage of 64 of K
-// takes 2 cycles a column of the tile on the tensor cores, but no less than 300 for its copies and barriers;
+// takes 2 cycles a column of the tile on the tensor cores, but no less than 300 for its copies and barriers (fp32: six
+// products of three stages);
 // filling and draining a tile's pipeline costs about 2500 and its epilogue 8 a column.  `cols`: columns of the
 // result for a tile of 256.
 int tile_width(const Block& b, long long M, long long N, long long K, int cols, int least) {
-    const long long mt = (M + kGemmM - 1) / kGemmM, ksteps = (K + kGemmK - 1) / kGemmK * (b.dtype == EG_F32 ? 6 : 1);
+    const long long mt = (M + kGemmM - 1) / kGemmM, ksteps = (K + kGemmK - 1) / kGemmK;
     const long long pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
     int best = 0;
     long long best_time = 0;
     for (int bn = b.dtype == EG_F32 ? 128 : 256; bn >= least; bn /= 2) {       // fp32: a tile's sums in registers, 64 a thread
         const long long c = (long long)cols * bn / 256, tiles = b.P * mt * ((N + c - 1) / c), waves = (tiles + pairs - 1) / pairs;
-        const long long time = waves * (ksteps * (2 * bn > 300 ? 2 * bn : 300) + 8 * bn) + 2500;
+        const int step = b.dtype == EG_F32 ? (12 * bn > 900 ? 12 * bn : 900) : 2 * bn > 300 ? 2 * bn : 300;
+        const long long time = waves * (ksteps * step + 8 * bn) + 2500;
         if (!best || time < best_time) {
             best = bn;
             best_time = time;

@@ -6,8 +6,8 @@
 // (dX = dG Wg + dU Wu; the parts of fp32 operands).
 //
 // fp32 operands come in kParts = 3 bf16 parts of 8 significant bits each, whose sum is the value; the six
-// products of parts that matter (part i of A with part j of B, i + j <= 2) are six segments of one
-// sum.  What is left out is below 2^-23 of |a||b|.
+// products of parts that matter (part i of A with part j of B, i + j <= 2) are formed from one copy of the
+// parts in shared memory.  What is left out is below 2^-23 of |a||b|.
 //
 // Two CTAs of a cluster share a tile of 256 x BN (tcgen05.mma, cta_group::2): each stages its 128
 // rows of A and its half of B with TMA (128-byte swizzle, 64 elements of K a stage), the even CTA
@@ -38,17 +38,17 @@ constexpr int kGemmEpiWarps = 8;
 constexpr int kGemmK = 64;                        // elements of K per stage: 128 bytes, one swizzle row
 constexpr int kGemmM = 256;                       // rows of a tile (two CTAs)
 constexpr int kGemmMaxStages = 24;
-constexpr int kGemmMaxMaps = 40, kGemmMaxSegs = 12, kGemmMaxProblems = 4;
+constexpr int kGemmMaxMaps = 40, kGemmMaxSegs = 2, kGemmMaxProblems = 4;
 
 struct GemmSeg {
-    int a, b0, b1;                                // maps; b0 / b1: B of the even / odd CTA
+    int a, b0, b1;                                // maps (fp32: of the first part); b0 / b1: B of the even / odd CTA
     int ksteps;
 };
 
 // Adding into the accumulator truncates: about 3e-8 of it per instruction, always towards zero, so that the
 // error of a sum grows with K (5e-6 after 2816).  In fp32 the accumulator is therefore moved to registers,
-// where an addition rounds, every kChunk stages of the products of first parts (16 instructions: 5e-7 at most).
-// The products of smaller parts come first, all in one accumulator: they are 2^-8 of the sum, and so is their error.
+// where an addition rounds, every kChunk steps of the products of first parts (16 instructions: 5e-7 at most).
+// The products of smaller parts have an accumulator of their own for all of a tile: they are 2^-8 of the sum, and so is their error.
 constexpr int kChunk = 4;
 constexpr int kParts = 3;
 enum { kEpiStore = 0, kEpiGateUp = 1, kEpiDact = 2 };
@@ -57,7 +57,6 @@ struct GemmProblem {
     int tiles, mt, nt;                            // all tiles; tiles of one replica
     int nseg;
     GemmSeg seg[kGemmMaxSegs];
-    int small;                                    // fp32: stages of the products of smaller parts, which come first
     int a_mn, b_mn;                               // the operand's K runs along its rows
     int a_box;                                    // rows of a box of A (K along the columns): 128, fewer where M is smaller
     int b_pair;                                   // B of the two CTAs are two matrices, same rows
@@ -408,7 +407,7 @@ template <typename T, int EPI, int BN> struct GemmShape {
     static constexpr int kBars = kRing / 1024 * 1024 + kEpi;
     static constexpr int kSmem = 1024 + kBars + kBarBytes;
     static constexpr int kCols = BN < 32 ? 32 : BN;             // tensor memory columns of one accumulator
-    static constexpr int kTmem = 2 * kCols;
+    static constexpr int kTmem = (sizeof(T) == 4 ? 4 : 2) * kCols;      // fp32: two more for the smaller products
     // stages for A boxes of a_pitch bytes
     static int stages(int a_pitch) {
         const int n = kRing / 1024 * 1024 / (a_pitch + kBBytes);
@@ -444,7 +443,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     uint64_t* acc_full = empty + kGemmMaxStages;                                      // [2]
     uint64_t* acc_empty = acc_full + 2;                                  // [2] (even CTA's are used)
     uint64_t* epi_full = acc_empty + 2;                                  // [kGemmEpiWarps][2]
-    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + 2 * kGemmEpiWarps);
+    uint64_t* small_full = epi_full + 2 * kGemmEpiWarps;                 // [2]: fp32, the smaller products' accumulators
+    uint64_t* small_empty = small_full + 2;                              // [2] (even CTA's are used)
+    volatile int* s_abort = reinterpret_cast<volatile int*>(small_empty + 2);
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(const_cast<int*>(s_abort) + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -452,7 +453,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
     if (threadIdx.x == 0) {
         *s_abort = 0;
         for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
-        for (int q = 0; q < 2; ++q) { op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps); }
+        for (int q = 0; q < 2; ++q) {
+            op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps);
+            op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kGemmEpiWarps);
+        }
         for (int q = 0; q < 2 * kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -490,19 +494,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     const CUtensorMap* map = &a.maps[warp == 0 ? g.seg[e].a : rank ? g.seg[e].b1 : g.seg[e].b0];
                     const int ksteps = g.seg[e].ksteps;
                     for (int k = 0; k < ksteps; k += G) {
-                        if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
-                        const int n = G == 1 ? 1 : min(G, ksteps - k), pitch = warp == 0 ? a.a_pitch : Shape::kBBytes;
-                        unsigned char* to = (warp == 0 ? smem : ring_b) + s * G * pitch;
-                        if (warp == 0 && rank == 0) op_mbar_expect(&full[s], n * bytes);
-                        const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
+                        // fp32: a step's parts in the order in which their stages become free, 1, 0, 2
+#pragma unroll 1
+                        for (int part = sizeof(T) == 4 ? 1 : 0, z = 0; z < (sizeof(T) == 4 ? kParts : 1); ++z, part = z == 1 ? 0 : 2) {
+                            if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
+                            const int n = G == 1 ? 1 : min(G, ksteps - k), pitch = warp == 0 ? a.a_pitch : Shape::kBBytes;
+                            unsigned char* to = (warp == 0 ? smem : ring_b) + s * G * pitch;
+                            if (warp == 0 && rank == 0) op_mbar_expect(&full[s], n * bytes);
+                            const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
 #pragma unroll
-                        for (int h = 0; h < G; ++h, to += pitch) {
-                            if (h >= n) break;
-                            const int at = (k + h) * kGemmK;
-                            if (row < rows) tma_load_pair(to, map, mn ? row : at, mn ? at : row, q.p, bar);
-                            if (mn && (warp == 0 || BN == 256) && row + 64 < rows) tma_load_pair(to + 8192, map, row + 64, at, q.p, bar);
+                            for (int h = 0; h < G; ++h, to += pitch) {
+                                if (h >= n) break;
+                                const int at = (k + h) * kGemmK;
+                                if (row < rows) tma_load_pair(to, map + part, mn ? row : at, mn ? at : row, q.p, bar);
+                                if (mn && (warp == 0 || BN == 256) && row + 64 < rows)
+                                    tma_load_pair(to + 8192, map + part, row + 64, at, q.p, bar);
+                            }
+                            if (++s == S) { s = 0; ++round; }
                         }
-                        if (++s == S) { s = 0; ++round; }
                     }
                 }
             }
@@ -520,41 +529,88 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                                        ((uint32_t)(kGemmM >> 4) << 24);
                 const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
                 uint32_t add = 0;
-                int in_chunk = sizeof(T) == 4 ? kChunk - g.small : 0;    // reaches kChunk where the accumulator is handed over
-                for (int e = 0; e < g.nseg; ++e) {
-                    const int ksteps = g.seg[e].ksteps;
-                    for (int k = 0; k < ksteps; k += G) {
-                        const int buf = count & 1;
-                        const uint32_t d = tmem + buf * Shape::kCols;
-                        if (!add) {
-                            if (count >= 2) mbar_wait(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort, a.err);
-                            tc_fence_after();
+                if constexpr (sizeof(T) == 4) {
+                    const uint32_t small = tmem + (2 + (turn & 1)) * Shape::kCols;
+                    uint32_t add_small = 0;
+                    int in_chunk = 0;
+                    auto product = [&](uint32_t d, int sa, int sb, uint32_t& add) {
+                        const uint64_t da = smem_desc(op_smem(smem + sa * a.a_pitch), g.a_mn);
+                        const uint64_t db = smem_desc(op_smem(ring_b + sb * Shape::kBBytes), g.b_mn);
+#pragma unroll
+                        for (int u = 0; u < kGemmK / 16; ++u) {
+                            tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
+                            add = 1;
                         }
+                    };
+                    int at[kParts];                              // stages of the parts
+                    auto next = [&](int part) {
                         mbar_wait(&full[s], round & 1, s_abort, a.err);
                         tc_fence_after();
-                        const int n = G == 1 ? 1 : min(G, ksteps - k);
-                        uint64_t da = smem_desc(op_smem(smem + s * G * a.a_pitch), g.a_mn);
-                        uint64_t db = smem_desc(op_smem(ring_b + s * G * Shape::kBBytes), g.b_mn);
-#pragma unroll
-                        for (int h = 0; h < G; ++h, da += a.a_pitch >> 4, db += Shape::kBBytes >> 4) {
-                            if (h >= n) break;
-#pragma unroll
-                            for (int u = 0; u < kGemmK / 16; ++u) {
-                                tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
-                                add = 1;
+                        at[part] = s;
+                        if (++s == S) { s = 0; ++round; }
+                    };
+                    if (turn >= 2) {
+                        mbar_wait(&small_empty[turn & 1], ((turn >> 1) - 1) & 1, s_abort, a.err);
+                        tc_fence_after();
+                    }
+                    for (int e = 0; e < g.nseg; ++e) {
+                        for (int k = 0; k < g.seg[e].ksteps; ++k) {
+                            const int buf = count & 1;
+                            if (!add) {
+                                if (count >= 2) mbar_wait(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort, a.err);
+                                tc_fence_after();
+                            }
+                            next(1);
+                            product(small, at[1], at[1], add_small);
+                            next(0);
+                            product(small, at[0], at[1], add_small);
+                            product(small, at[1], at[0], add_small);
+                            tc_commit_pair(&empty[at[1]]);
+                            product(tmem + buf * Shape::kCols, at[0], at[0], add);
+                            next(2);
+                            product(small, at[0], at[2], add_small);
+                            product(small, at[2], at[0], add_small);
+                            tc_commit_pair(&empty[at[0]]);
+                            tc_commit_pair(&empty[at[2]]);
+                            if (++in_chunk == kChunk) {
+                                tc_commit_pair(&acc_full[buf]);
+                                ++count;
+                                add = in_chunk = 0;
                             }
                         }
-                        tc_commit_pair(&empty[s]);
-                        if (++s == S) { s = 0; ++round; }
-                        if (sizeof(T) == 4 && ++in_chunk == kChunk) {
-                            tc_commit_pair(&acc_full[buf]);
-                            ++count;
-                            add = in_chunk = 0;
+                    }
+                    if (add) {
+                        tc_commit_pair(&acc_full[count & 1]);
+                        ++count;
+                    }
+                    tc_commit_pair(&small_full[turn & 1]);
+                } else {
+                    const int buf = count & 1;
+                    const uint32_t d = tmem + buf * Shape::kCols;
+                    if (count >= 2) mbar_wait(&acc_empty[buf], ((count >> 1) - 1) & 1, s_abort, a.err);
+                    tc_fence_after();
+                    for (int e = 0; e < g.nseg; ++e) {
+                        const int ksteps = g.seg[e].ksteps;
+                        for (int k = 0; k < ksteps; k += G) {
+                            mbar_wait(&full[s], round & 1, s_abort, a.err);
+                            tc_fence_after();
+                            const int n = G == 1 ? 1 : min(G, ksteps - k);
+                            uint64_t da = smem_desc(op_smem(smem + s * G * a.a_pitch), g.a_mn);
+                            uint64_t db = smem_desc(op_smem(ring_b + s * G * Shape::kBBytes), g.b_mn);
+#pragma unroll
+                            for (int h = 0; h < G; ++h, da += a.a_pitch >> 4, db += Shape::kBBytes >> 4) {
+                                if (h >= n) break;
+#pragma unroll
+                                for (int u = 0; u < kGemmK / 16; ++u) {
+                                    tc_mma_pair(d, da + u * a_step, db + u * b_step, idesc, add);
+                                    add = 1;
+                                }
+                            }
+                            tc_commit_pair(&empty[s]);
+                            if (++s == S) { s = 0; ++round; }
                         }
                     }
-                }
-                if (add) {
-                    tc_commit_pair(&acc_full[count & 1]);
+                    tc_commit_pair(&acc_full[buf]);
                     ++count;
                 }
             }
@@ -580,25 +636,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
             if constexpr (sizeof(T) == 4) {
                 int ksteps = 0;
                 for (int e = 0; e < g.nseg; ++e) ksteps += g.seg[e].ksteps;
-                const int chunks = (g.small > 0) + (ksteps - g.small + kChunk - 1) / kChunk;
+                const int chunks = (ksteps + kChunk - 1) / kChunk;
 #pragma unroll
                 for (int x = 0; x < BN / 2; ++x) sum[x] = 0.f;
-                for (int z = 0; z < chunks; ++z, ++count) {
-                    const int from = count & 1;
+                auto take = [&](uint32_t from) {
                     constexpr int LW = BN / 2 < 32 ? 16 : 32;
-                    mbar_wait(&acc_full[from], (count >> 1) & 1, s_abort, a.err);
                     tc_fence_after();
 #pragma unroll
                     for (int x = 0; x < BN / 2; x += LW) {
                         uint32_t v[LW];
-                        tc_load(v, tmem + from * Shape::kCols + lanes + column(x));
+                        tc_load(v, from + lanes + column(x));
 #pragma unroll
                         for (int e = 0; e < LW; ++e) sum[x + e] += __uint_as_float(v[e]);
                     }
                     tc_fence_before();
                     __syncwarp();
+                };
+                for (int z = 0; z < chunks; ++z, ++count) {
+                    const int from = count & 1;
+                    mbar_wait(&acc_full[from], (count >> 1) & 1, s_abort, a.err);
+                    take(tmem + from * Shape::kCols);
                     if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[from]), 0));
                 }
+                mbar_wait(&small_full[turn & 1], (turn >> 1) & 1, s_abort, a.err);
+                take(tmem + (2 + (turn & 1)) * Shape::kCols);
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&small_empty[turn & 1]), 0));
             }
             if constexpr (EPI == kEpiStore) {
                 constexpr int CW = Shape::kBoxCols;                  // columns of one staged box
