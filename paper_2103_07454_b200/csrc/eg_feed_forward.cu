@@ -459,6 +459,30 @@ int tile_width(const Block& b, long long M, long long N, long long K, int cols, 
     return best;
 }
 
+// Tile width of the gradients' launch: 128 where the pairs of multiprocessors would wait for a few long tiles.  Measured
+// in bf16, us of a training step with 256 and 128: 300 tokens, 1024 x 4096 84 and 66; 49, 2512 x 8064 148 and 140; 3 x
+// 4485, 88 x 200 64 and 57; 2 x 428, 1408 x 4800, which the rule leaves at 256, 140 and 156.
+int gradient_width(const Block& b) {
+    if (b.dtype == EG_F32) return 128;
+    const long long pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+    long long best = 0;
+    int width = 256;
+    for (int bn = 256; bn >= 128; bn /= 2) {
+        auto tiles = [&](long long M, long long N) { return b.P * ((M + kGemmM - 1) / kGemmM) * ((N + bn - 1) / bn); };
+        const long long step = bn == 256 ? 512 : 400, epilogue = 16 * bn;      // cycles; narrow tiles copy more for each product
+        const long long long_tile = b.q->dx.data ? 2 * ((b.f + kGemmK - 1) / kGemmK) * step : 0;
+        const long long n = (b.n + kGemmK - 1) / kGemmK * step, tile = n > epilogue ? n : epilogue;
+        const long long others = (b.q->d_down.data ? tiles(b.d, b.f) : 0) + ((b.q->d_gate.data ? 1 : 0) + (b.q->d_up.data ? 1 : 0)) * tiles(b.f, b.d);
+        const long long all = (tiles(b.n, b.d) * long_tile + others * tile) / pairs;
+        const long long longest = long_tile > tile ? long_tile : tile, time = all > longest ? all : longest;
+        if (bn == 256 || time * 10 < best * 9) {
+            best = time;
+            width = bn;
+        }
+    }
+    return width;
+}
+
 template <typename T> cudaError_t few_tokens(const Block& b, cudaStream_t stream) {
     const eg_feed_forward_args* q = b.q;
     FewArgs up{q->w_gate.data, q->w_up.data, q->w_gate.replica_stride, q->w_gate.row_stride, q->w_up.replica_stride,
@@ -525,7 +549,7 @@ template <typename T> cudaError_t backward(const Block& b, unsigned int* err, cu
         w.a.map_du = w.boxes(b.du, 32);
         if ((e = launch_gemm<T, kEpiDact>(w, stream)) != cudaSuccess) return e;
     }
-    Builder w(b, b.dtype == EG_F32 ? 128 : 256, err);
+    Builder w(b, gradient_width(b), err);
     if (q->dx.data) {
         GemmProblem* g = w.problem(b.n, b.d, false, true, false);
         const int mg = w.operand(b.wg, true, false), mu = w.operand(b.wu, true, false);
