@@ -225,6 +225,10 @@ long long saved_bytes(const eg_feed_forward_args* q) {
 //   bf16 1024 x 2816   k_few_mma 15 for 1 token, 17 for 8, 22 for 16, 40 for 32; tiles 23 up to 24, 24 for 64
 //   fp32 1024 x 2816   k_few_dot 26 for 1 token, 91 for 8, 233 for 16;           tiles 188
 //   bf16 1001 x 2817   k_few_dot 41 for 1 token, 48 for 2, 90 for 4;             tiles 57
+// and, with the tokens in groups (fp32: 8, 16-bit: 2), the tiles' time behind the stroke:
+//   fp32 2 x 1024 x 2816   16 tokens 62 / 105, 24 98 / 105, 32 129 / 106;    3 x 401 x 896   16 28 / 39, 24 36 / 39, 32 48 / 39
+//   fp32 8 x 128 x 280     16 tokens 17 / 26, 64 23 / 26;                    bf16 8 x 129 x 280   4 8 / 14, 8 14 / 16, 12 19 / 15
+//   bf16 3 x 401 x 896     4 tokens 14 / 16, 6 18 / 16;                      bf16 2 x 1001 x 2817   4 43 / 33
 int few_kind(const eg_feed_forward_args* q) {
     if (q->saved || q->P > 65535) return 0;
     const size_t size = q->dtype == EG_F32 ? 4 : 2;
@@ -232,7 +236,12 @@ int few_kind(const eg_feed_forward_args* q) {
                         in_place(mat(q->w_up), q->P, q->d_ff, size) && in_place(mat(q->w_down), q->P, q->d_model, size) &&
                         q->d_model * size % 16 == 0 && q->d_ff * size % 16 == 0;
     if (q->dtype != EG_F32 && rows16 && q->rows <= kFewMmaTokens) return 1;
-    return q->rows <= (q->dtype == EG_F32 ? kFewDotTokens32 : kFewDotTokens16) ? 2 : 0;
+    // k_few_dot reads the weights once for every group of tokens, the tiles copy them once and have longer launches
+    const bool f32 = q->dtype == EG_F32;
+    const int64_t each = f32 ? kFewDotTokens32 : kFewDotTokens16, groups = (q->rows + each - 1) / each;
+    const int64_t bytes = q->P * 3 * q->d_model * q->d_ff * (int64_t)size;
+    if (groups <= 1) return 2;
+    return q->rows <= 64 && bytes <= (64ll << 20) * (f32 ? 2 : 1) && bytes * (groups - (f32 ? 2 : 1)) <= (f32 ? 14000000 : 6600000) ? 2 : 0;
 }
 
 void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {

@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(256, 2) k_few_mma(const FewArgs a) {
     }
 }
 
-// grid (CTAs, P), 256 threads.  A unit is R weight rows: gate and up of R / 2 outputs, or R outputs -- more of
+// grid (CTAs, P, groups of N tokens), 256 threads.  A unit is R weight rows: gate and up of R / 2 outputs, or R outputs -- more of
 // them for more tokens, so that a token's values serve several rows once they are in registers.
 // Elements VEC * (32 * split + lane) ... of K belong to lane `lane` of the unit's warp `split`.
 template <typename T, int VEC, int N, int R, bool GATE>
@@ -154,7 +154,8 @@ __global__ void __launch_bounds__(256) k_few_dot(const FewArgs a) {
     const int r0 = unit * OUT, count = min(OUT, a.rows - r0);
     const T* wa = static_cast<const T*>(a.wa) + p * a.wa_rep + (long long)r0 * a.wa_row;
     const T* wb = GATE ? static_cast<const T*>(a.wb) + p * a.wb_rep + (long long)r0 * a.wb_row : wa;
-    const T* x = static_cast<const T*>(a.x) + p * a.x_rep;
+    const int t0 = blockIdx.z * N, n = a.n - t0;
+    const T* x = static_cast<const T*>(a.x) + p * a.x_rep + t0 * a.x_row;
     float acc[R][N];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(256) k_few_dot(const FewArgs a) {
                 if (k >= a.K) continue;
 #pragma unroll
                 for (int t = 0; t < N; ++t) {
-                    if (t >= a.n) continue;
+                    if (t >= n) continue;
                     float xv[VEC];
                     load_vec<T, VEC>(x + t * a.x_row + k, xv);
 #pragma unroll
@@ -213,13 +214,13 @@ __global__ void __launch_bounds__(256) k_few_dot(const FewArgs a) {
     if (split != 0) return;
     for (int o = lane; o < count * N; o += 32) {
         const int r = o / N, t = o % N;
-        if (t >= a.n) continue;
+        if (t >= n) continue;
         float g = 0.f, u = 0.f;
         for (int v = 0; v < a.splits; ++v) {
             g += s_part[warp + v][(GATE ? 2 * r : r) * N + t];
             if (GATE) u += s_part[warp + v][(2 * r + 1) * N + t];
         }
-        T* out = static_cast<T*>(a.out) + p * a.out_rep + t * a.out_row + r0 + r;
+        T* out = static_cast<T*>(a.out) + p * a.out_rep + (t0 + t) * a.out_row + r0 + r;
         *out = from_f32<T>(GATE ? few_result<T>(a.act, g, u) : g);
     }
 }
@@ -236,21 +237,21 @@ template <typename T, bool GATE> cudaError_t launch_few_mma(const FewArgs& a, cu
 }
 
 template <typename T, int VEC, bool GATE> cudaError_t launch_few_dot(FewArgs a, int P, cudaStream_t stream) {
-    auto go = [&](auto kernel, int R) {
+    auto go = [&](auto kernel, int N, int R) {
         const int outs = GATE ? R / 2 : R, units = (a.rows + outs - 1) / outs;
         // warps per unit: enough of them to fill the multiprocessors, each with some K to work on
         a.splits = 8;
         while (a.splits > 1 && ((long long)units * P * a.splits > 32ll * sm_count() || a.K < a.splits * 32 * VEC)) a.splits /= 2;
         const int per = 8 / a.splits;
-        const dim3 grid((units + per - 1) / per, P), block(256);
+        const dim3 grid((units + per - 1) / per, P, (a.n + N - 1) / N), block(256);
         return launch_after(kernel, grid, block, 0, stream, a);
     };
-    if (a.n <= 1) return go(k_few_dot<T, VEC, 1, 2, GATE>, 2);
+    if (a.n <= 1) return go(k_few_dot<T, VEC, 1, 2, GATE>, 1, 2);
     if constexpr (sizeof(T) == 4) {
-        if (a.n > 4) return go(k_few_dot<T, VEC, 8, 8, GATE>, 8);
-        if (a.n > 2) return go(k_few_dot<T, VEC, 4, 4, GATE>, 4);
+        if (a.n > 4) return go(k_few_dot<T, VEC, 8, 8, GATE>, 8, 8);
+        if (a.n > 2) return go(k_few_dot<T, VEC, 4, 4, GATE>, 4, 4);
     }
-    return go(k_few_dot<T, VEC, 2, 4, GATE>, 4);
+    return go(k_few_dot<T, VEC, 2, 4, GATE>, 2, 4);
 }
 
 }  // namespace eg
