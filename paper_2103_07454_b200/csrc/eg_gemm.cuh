@@ -18,7 +18,8 @@
 //
 // Measured, 4 replicas x 4096 tokens, 2048 x 5504, bf16: gate/up with activation 470 us (1.57 PFLOP/s), down 214-228
 // us (1.62-1.73), activation gradient 290-300 us (1.23-1.27: its epilogue moves four more matrices), the four
-// gradients 1236 us (1.49); a stage of 64 of K takes 540-580 cycles of 512 on the tensor cores.  8 x 512 tokens, 1024
+// gradients 1236 us (1.49); a stage of 64 of K takes 540-580 cycles of 512 on the tensor cores; fp32, 8 x 1021 tokens, 1280 x
+// 4992: gradients 2077 us (1.51 PFLOP/s of products of parts).  8 x 512 tokens, 1024
 // x 2816: 45 + 23 + 35 + 95 us, 750-850 cycles a stage: the weights come from memory, and the 160-190 KB of
 // stages in flight do not cover their latency (asking for them earlier into the L2 was slower).
 //
