@@ -222,9 +222,9 @@ long long saved_bytes(const eg_feed_forward_args* q) {
 }
 
 // Which kernels a forward call without `saved` takes.  Measured with 4 replicas, us:
-//   bf16 1024 x 2816   k_few_mma 15 for 1 token, 17 for 8, 22 for 16, 40 for 32; tiles 23 up to 24, 24 for 64
-//   fp32 1024 x 2816   k_few_dot 26 for 1 token, 91 for 8, 233 for 16;           tiles 188
-//   bf16 1001 x 2817   k_few_dot 41 for 1 token, 48 for 2, 90 for 4;             tiles 57
+//   bf16 1024 x 2816   k_few_mma 15 for 1 token, 17 for 8, 22 for 16, 40 for 32; tiles 26 from 17 to 64
+//   fp32 1024 x 2816   k_few_dot 31 for 1 token, 91 for 8;           tiles 159
+//   bf16 1001 x 2817   k_few_dot 49 for 1 token, 47 for 2, 90 for 4;             tiles 55
 // and, with the tokens in groups (fp32: 8, 16-bit: 2), the tiles' time behind the stroke:
 //   fp32 2 x 1024 x 2816   16 tokens 62 / 105, 24 98 / 105, 32 129 / 106;    3 x 401 x 896   16 28 / 39, 24 36 / 39, 32 48 / 39
 //   fp32 8 x 128 x 280     16 tokens 17 / 26, 64 23 / 26;                    bf16 8 x 129 x 280   4 8 / 14, 8 14 / 16, 12 19 / 15

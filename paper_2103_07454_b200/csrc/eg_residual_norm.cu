@@ -1053,8 +1053,8 @@ template <typename T, int VEC, bool BWD> cudaError_t short_runs(const NormArgs& 
     *G = (int)(W < ctas ? W : ctas);
     const int each = (a.d + VEC - 1) / VEC, threads = each < kRowThreads ? (each + 31) / 32 * 32 : kRowThreads;
     const int smem = BWD && W > *G ? 3 * a.d * (int)sizeof(float) : 0;
-    cudaError_t e;
-    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(k_norm_rows<T, VEC, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMaxWidth * 4)) != cudaSuccess)
+    cudaError_t e;       // (48 KB need no permission, but s_red is part of them)
+    if (smem > 40 * 1024 && (e = cudaFuncSetAttribute(k_norm_rows<T, VEC, BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kCtaWidth * 4)) != cudaSuccess)
         return e;
     return launch_after(k_norm_rows<T, VEC, BWD>, dim3(*G), dim3(threads), smem, stream, a);
 }

@@ -94,3 +94,11 @@ def test_native_marshalling_refuses():
         B.feed_forward(x["y"], x["y"], None, x["y"])
     with pytest.raises(B.EventGradError):
         B.feed_forward_backward(x["y"], x["y"], x["y"], x["y"], x["y"], None)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(2, 100, 4096), (1, 200, 4090), (1, 296, 4095), (1, 150, 3400)])
+def test_norm_short_runs_of_the_widest_rows(P, n, d, dtype):
+    """Column sums of nearly 48 KB in shared memory."""
+    x, w = N.inputs(P, n, d, dtype, seed=17)
+    N.run_and_check(x, w, dtype)
