@@ -239,9 +239,9 @@ int few_kind(const eg_feed_forward_args* q) {
     // k_few_dot reads the weights once for every group of tokens, the tiles copy them once and have longer launches
     const bool f32 = q->dtype == EG_F32;
     const int64_t each = f32 ? kFewDotTokens32 : kFewDotTokens16, groups = (q->rows + each - 1) / each;
-    const int64_t bytes = q->P * 3 * q->d_model * q->d_ff * (int64_t)size;
+    const double bytes = 3.0 * q->P * q->d_model * q->d_ff * size;
     if (groups <= 1) return 2;
-    return q->rows <= 64 && bytes <= (64ll << 20) * (f32 ? 2 : 1) && bytes * (groups - (f32 ? 2 : 1)) <= (f32 ? 14000000 : 6600000) ? 2 : 0;
+    return q->rows <= 64 && bytes <= (f32 ? 134e6 : 67e6) && bytes * (groups - (f32 ? 2 : 1)) <= (f32 ? 14e6 : 6.6e6) ? 2 : 0;
 }
 
 void plan(Block* b, const eg_feed_forward_args* q, bool backward, Bump* w) {
