@@ -63,7 +63,8 @@ template <typename T> __device__ __forceinline__ T* row_of(const Mat& m, int i, 
 }
 
 // Sum over the tpr threads of a group, valid in all of them.  Groups wider than a warp meet at the named
-// barrier 1 + group; `red` (one float per warp of the group) must not be the one of the previous call.
+// barrier 1 + group; `red` (one float per warp of the group) must not be the one of the previous call, whose sums a
+// warp that is behind may still be reading: the callers take two in turn, call by call.
 __device__ __forceinline__ float group_sum(float v, int tpr, int t, int group, float* red) {
     for (int o = (tpr < 32 ? tpr : 32) >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (tpr <= 32) return v;
@@ -99,7 +100,8 @@ __global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormAr
     long long row = u % a.rows;
     int have = -1;                                   // replica whose factors are held
     float fa[E], fs[E];
-    float *red0 = s_red[0] + (group * tpr >> 5), *red1 = s_red[1] + (group * tpr >> 5);
+    const int red_at = group * tpr >> 5;
+    int turn = 0;                                    // of the two buffers of sums: another one at every call
     // every group makes the same number of turns: the groups of a warp shuffle together
     for (long long base = u0; base < u1; base += groups, u += groups, row += groups) {
         while (row >= a.rows) { row -= a.rows; ++i; }
@@ -137,7 +139,8 @@ __global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormAr
         if (post && has_y) {
 #pragma unroll
             for (int e = 0; e < E; ++e) sum = fmaf(y[e], y[e], sum);
-            inv1 = rsqrtf(fmaf(group_sum(sum, tpr, t, group, red0), a.inv_d, a.eps));
+            inv1 = rsqrtf(fmaf(group_sum(sum, tpr, t, group, s_red[turn] + red_at), a.inv_d, a.eps));
+            turn ^= 1;
         }
         sum = 0.f;
 #pragma unroll
@@ -157,7 +160,8 @@ __global__ void __launch_bounds__(512) k_norm_few(const __grid_constant__ NormAr
         if (!pre) continue;
 #pragma unroll
         for (int e = 0; e < E; ++e) sum = fmaf(r[e], r[e], sum);
-        const float inv2 = rsqrtf(fmaf(group_sum(sum, tpr, t, group, red1), a.inv_d, a.eps));
+        const float inv2 = rsqrtf(fmaf(group_sum(sum, tpr, t, group, s_red[turn] + red_at), a.inv_d, a.eps));
+        turn ^= 1;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * tpr + t) * VEC;

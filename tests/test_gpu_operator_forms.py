@@ -1,0 +1,38 @@
+"""Forms of the operators that leave something out, and values at the ends of their ranges, at the sizes where each kernel
+takes them, against the formulas in 64 bits."""
+import pytest
+import torch
+
+import test_gpu_residual_norm as N
+from paper_2103_07454_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def forward_again_and_again(x, w, dtype, turns=8):
+    """The forward call against the formula, and the same bits every time."""
+    want_r, want_o, _ = N.exact(x, w, 1e-6, use=("d_r",))
+    d = want_r.shape[2]
+    first = B.residual_norm(x["y"], x["residual"], **w)
+    N.check(first[0], want_r, dtype, 1, want_r.pow(2).mean().sqrt(), "r'")
+    N.check(first[1], want_o, dtype, d, None if want_o is None else want_o.pow(2).mean().sqrt(), "o")
+    for _ in range(turns):
+        for a, b in zip(B.residual_norm(x["y"], x["residual"], **w), first):
+            assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(2, 1024, 1024), (4, 1100, 512), (1, 1100, 4096), (2, 700, 2048), (3, 500, 1001)])
+@pytest.mark.parametrize("given", [("w_post",), ("w_pre",), ("gate", "scale", "w_pre"), ("w_post", "gate", "scale")])
+def test_norm_of_some_thousand_rows_with_one_of_the_two_norms(given, P, n, d, dtype):
+    """Several rows a group of warps, one sum a row: the buffer of a row's sums is not the one before's."""
+    x, w = N.inputs(P, n, d, dtype, seed=21, given=given)
+    forward_again_and_again(x, w, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(2, 1024, 1024), (1, 1100, 4096), (3, 500, 1001)])
+def test_norm_of_some_thousand_rows_without_a_block_before(P, n, d, dtype):
+    x, w = N.inputs(P, n, d, dtype, seed=22, given=("scale", "w_pre"))
+    x["y"] = None
+    forward_again_and_again(x, w, dtype)
