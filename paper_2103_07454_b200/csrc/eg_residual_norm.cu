@@ -799,7 +799,8 @@ __global__ void __launch_bounds__(kRowThreads) k_norm_rows(const __grid_constant
         }
         return f;
     };
-    auto sums = [&](float (&v)[K], int which) {          // over the threads of the CTA
+    int which = 0;                                       // of the two buffers: taken in turn, since only one barrier parts
+    auto sums = [&](float (&v)[K]) {                     // a call's reads from the next one's writes; over the threads of the CTA
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
@@ -811,6 +812,7 @@ __global__ void __launch_bounds__(kRowThreads) k_norm_rows(const __grid_constant
             v[k] = lane < warps ? s_red[which][k][lane] : 0.f;
             for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
         }
+        which ^= 1;
     };
     bool begun = false;                                  // rows of replica i lie in the column sums
     for (; u < u1; ++u) {
@@ -821,7 +823,7 @@ __global__ void __launch_bounds__(kRowThreads) k_norm_rows(const __grid_constant
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[0] = fmaf(y.v[e], y.v[e], v[0]);
             }
-            sums(v, 0);
+            sums(v);
             inv1 = rsqrtf(fmaf(v[0], a.inv_d, a.eps));
         }
 #pragma unroll
@@ -844,7 +846,7 @@ __global__ void __launch_bounds__(kRowThreads) k_norm_rows(const __grid_constant
                     }
                 }
             }
-            sums(v, 1);
+            sums(v);
         }
         const float inv2 = second ? rsqrtf(fmaf(v[0], a.inv_d, a.eps)) : 0.f;
         float c3 = 0.f, c4 = 0.f;

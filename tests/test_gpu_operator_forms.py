@@ -36,3 +36,25 @@ def test_norm_of_some_thousand_rows_without_a_block_before(P, n, d, dtype):
     x, w = N.inputs(P, n, d, dtype, seed=22, given=("scale", "w_pre"))
     x["y"] = None
     forward_again_and_again(x, w, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(1, 900, 1001), (3, 220, 333), (1, 1184, 4095), (2, 500, 777)])
+@pytest.mark.parametrize("given", [("w_post",), ("w_pre",), ("gate", "scale", "w_pre"), ("w_post", "gate", "scale")])
+def test_norm_of_unaligned_rows_two_a_block_with_one_of_the_two_norms(given, P, n, d, dtype):
+    x, w = N.inputs(P, n, d, dtype, seed=23, given=given)
+    forward_again_and_again(x, w, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(1, 200, 1024), (2, 140, 4096), (1, 290, 1001), (5, 50, 640)])
+@pytest.mark.parametrize("given", [(), ("w_pre",), ("scale", "w_pre"), ("gate", "scale", "w_pre")])
+def test_norm_gradients_of_two_rows_a_block_without_the_first_norm(given, P, n, d, dtype):
+    x, w = N.inputs(P, n, d, dtype, seed=24, given=given)
+    N.run_and_check(x, w, dtype)
+    call = lambda: B.residual_norm_backward(x["d_r"], x["d_o"] if "w_pre" in given else None, x["y"], x["residual"], **w)  # noqa: E731
+    first = call()
+    for _ in range(8):
+        again = call()
+        for a, b in zip((*first[:2], *first[2]), (*again[:2], *again[2])):
+            assert (a is None and b is None) or torch.equal(a, b)
