@@ -58,3 +58,29 @@ def test_norm_gradients_of_two_rows_a_block_without_the_first_norm(given, P, n, 
         again = call()
         for a, b in zip((*first[:2], *first[2]), (*again[:2], *again[2])):
             assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(2, 701, 96), (2, 701, 1024), (1, 1101, 4096), (3, 333, 513), (1, 301, 5000), (2, 60, 96)])
+@pytest.mark.parametrize("given", [N.NAMES, ("w_pre",), ("w_post", "gate")])
+def test_norm_without_an_epsilon(given, P, n, d, dtype):
+    """eps = 0 is defined for rows that are not zero, however many rows the last step of a run holds."""
+    x, w = N.inputs(P, n, d, dtype, seed=25, given=given)
+    N.run_and_check(x, w, dtype, eps=0.0)
+
+
+@pytest.mark.parametrize("given", [N.NAMES, ("w_pre",), ("w_post",)])
+def test_norm_without_an_epsilon_keeps_zero_rows_to_themselves(given):
+    """0 / 0 in its own row and replica, nowhere else."""
+    x, w = N.inputs(3, 333, 96, "fp32", seed=26, given=given)
+    args = lambda: (x["d_r"], x["d_o"] if "w_pre" in given else None, x["y"], x["residual"])  # noqa: E731
+    clean = B.residual_norm_backward(*args(), eps=0.0, **w)
+    x["y"][1, 7] = 0
+    x["residual"][1, 7] = 0
+    got = B.residual_norm_backward(*args(), eps=0.0, **w)
+    rows = torch.ones(3, 333, dtype=torch.bool, device="cuda")
+    rows[1, 7] = False
+    for a, b in zip(got[:2], clean[:2]):
+        assert torch.equal(a[rows], b[rows])
+    for a, b in zip(got[2], clean[2]):
+        assert a is None or torch.equal(a[[0, 2]], b[[0, 2]])
