@@ -364,8 +364,8 @@ template <typename T, bool BWD> __host__ __device__ constexpr int rows_at_once()
 //
 // A row needs one round of sums: with p = scale * r, q = a * y (so r' = p + inv1 q) and dn = d_o * w_pre, the sums
 // of y^2, p^2, pq, q^2, dn p, dn q and q d_r' give inv1 first and then every mean that the formulas above
-// ask for.  Where p and inv1 q cancel to less than a tenth of their size, r' and what follows from it are summed
-// in a second round instead.
+// ask for.  Where p and inv1 q cancel to less than a tenth of their size, or one of these sums passes the range of 32 bits
+// (q^2 may where r'^2 does not), r' and what follows from it are summed in a second round instead.
 template <typename T, int VEC, bool BWD>
 __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_constant__ NormArgs a) {
     constexpr int E = kElems, ROWS = rows_at_once<T, BWD>(), ARRAYS = BWD ? 4 : 2;
@@ -632,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
 #pragma unroll
                 for (int q = 0; q < ARRAYS; ++q) in[q][z].repack();
             float inv1[ROWS], rr[ROWS], dnr[ROWS], qr[ROWS];       // sums of r'^2, dn r', q r'
-            bool cancels = false;
+            bool cancels = false, twice[ROWS];
 #pragma unroll
             for (int z = 0; z < ROWS; ++z) {
                 const float* x = v + z * (KP / ROWS);
@@ -640,7 +640,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
                 inv1[z] = mine + z * each >= n ? 0.f : post ? rsqrtf(fmaf(x[0], a.inv_d, a.eps)) : 1.f;
                 const float size = fmaf(inv1[z] * inv1[z], x[3], x[1]);
                 rr[z] = fmaf(2.f * inv1[z], x[2], size);
-                cancels = cancels || rr[z] < 0.01f * size;
+                twice[z] = !(rr[z] >= 0.01f * size) || size > 3e38f;
+                cancels = cancels || twice[z];
                 if constexpr (BWD) {
                     dnr[z] = fmaf(inv1[z], x[5], x[4]);
                     qr[z] = fmaf(inv1[z], x[3], x[2]);
@@ -671,6 +672,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
                 row_sums(again);
 #pragma unroll
                 for (int z = 0; z < ROWS; ++z) {
+                    if (!twice[z]) continue;                           // the others' bits do not depend on their neighbours
                     rr[z] = again[z * (KP / ROWS)];
                     dnr[z] = again[z * (KP / ROWS) + 1];
                     qr[z] = again[z * (KP / ROWS) + 2];

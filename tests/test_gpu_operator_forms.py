@@ -84,3 +84,34 @@ def test_norm_without_an_epsilon_keeps_zero_rows_to_themselves(given):
         assert torch.equal(a[rows], b[rows])
     for a, b in zip(got[2], clean[2]):
         assert a is None or torch.equal(a[[0, 2]], b[[0, 2]])
+
+
+SUMS_BEYOND = [(2, 33, 1024), (2, 200, 1024), (2, 3000, 1024), (1, 2500, 96), (1, 1200, 4104), (2, 700, 1001)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", SUMS_BEYOND)
+def test_norm_where_the_squares_of_a_block_pass_32_bits(P, n, d, dtype):
+    """A sum of squares that is infinite in 32 bits makes rms(y) zero, in every kernel: r' = scale * r and what follows from it."""
+    x, w = N.inputs(P, n, d, dtype, seed=27)
+    none = dict(x, y=torch.zeros_like(x["y"]))
+    want_r, want_o, g = N.exact(none, w, 1e-6)
+    x["y"] = torch.where(x["y"] > 0, 5e18, -5e18).to(N.TYPES[dtype])       # 96 squares of them: 2.4e39
+    r, o = B.residual_norm(x["y"], x["residual"], **w)
+    N.check(r, want_r, dtype, 1, want_r.pow(2).mean().sqrt(), "r'")
+    N.check(o, want_o, dtype, d, want_o.pow(2).mean().sqrt(), "o")
+    dy, dr, dw = B.residual_norm_backward(x["d_r"], x["d_o"], x["y"], x["residual"], **w)
+    N.check(dr, g["residual"], dtype, d, N.amplitudes(none, w, 1e-6, ("d_r", "d_o"))[0].expand_as(dr), "dr")
+    assert torch.all(dy == 0) and torch.all(dw[0] == 0) and torch.all(dw[1] == 0)
+    for name, t in list(zip(N.NAMES, dw))[2:]:
+        N.check(t, g[name], dtype, d + n, torch.full_like(g[name], 0.9 * n ** 0.5), name)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", SUMS_BEYOND)
+def test_norm_where_only_the_weighted_squares_pass_32_bits(P, n, d, dtype):
+    """(a y)^2 passes the range of 32 bits, y^2 and r'^2 do not."""
+    x, w = N.inputs(P, n, d, dtype, seed=28, given=("w_post", "scale", "w_pre"))
+    x["y"] = (x["y"].float() * 3e16).to(N.TYPES[dtype])
+    w["w_post"] = (w["w_post"].float() * 256).to(N.TYPES[dtype])
+    N.run_and_check(x, w, dtype)
