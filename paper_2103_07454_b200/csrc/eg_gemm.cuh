@@ -5,9 +5,10 @@
 // accumulators.  A segment is one pair of operand matrices; several segments add into one result
 // (dX = dG Wg + dU Wu; the parts of fp32 operands).
 //
-// fp32 operands come in kParts = 3 bf16 parts of 8 significant bits each, whose sum is the value; the six
-// products of parts that matter (part i of A with part j of B, i + j <= 2) are formed from one copy of the
-// parts in shared memory.  What is left out is below 2^-23 of |a||b|.
+// fp32 operands come in kParts = 3 bf16 parts, each the nearest to what the ones before leave, whose sum is the value
+// (down to 2^-109, where the last parts leave bf16's range).  The second part is at most 2^-8 of the value, the third 2^-17,
+// and their signs are as often one as the other.  The six products of parts that matter (part i of A with part j of B,
+// i + j <= 2) are formed from one copy of the parts in shared memory.  What is left out is at most 2^-24 of |a||b|.
 //
 // Two CTAs of a cluster share a tile of 256 x BN (tcgen05.mma, cta_group::2): each stages its 128
 // rows of A and its half of B with TMA (128-byte swizzle, 64 elements of K a stage), the even CTA
@@ -49,7 +50,9 @@ struct GemmSeg {
 // Adding into the accumulator truncates: about 3e-8 of it per instruction, always towards zero, so that the
 // error of a sum grows with K (5e-6 after 2816).  In fp32 the accumulator is therefore moved to registers,
 // where an addition rounds, every kChunk steps of the products of first parts (16 instructions: 5e-7 at most).
-// The products of smaller parts have an accumulator of their own for all of a tile: they are 2^-8 of the sum, and so is their error.
+// The products of smaller parts have an accumulator of their own for all of a tile.  It holds at most 2^-7 of the sum of
+// |a||b| and meets five instructions for every 16 of K: 4e-11 K of that sum at most (3e-7 for K = 8192), and only
+// where all these products have one sign.
 constexpr int kChunk = 4;
 constexpr int kParts = 3;
 enum { kEpiStore = 0, kEpiGateUp = 1, kEpiDact = 2 };
@@ -252,23 +255,31 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F&& f) {
     else f(std::integral_constant<int, EG_ACT_RELU>{});
 }
 
-// The three bf16 parts of two fp32 values, packed: each takes the 8 leading bits of what is left (exact).  A
-// value that is not finite is its own first part.
-__device__ __forceinline__ void split_parts(float x, uint32_t (&p)[kParts]) {
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-        p[k] = __float_as_uint(x) & 0xffff0000u;
-        x -= __uint_as_float(p[k]);
-    }
-}
+// The three bf16 parts of two fp32 values, packed.  Each is rounded to nearest: truncated ones have the value's sign, and
+// what the products leave out (2^-21 then) would make every sum too small.  A value that rounds to infinity keeps its leading
+// 8 bits as its first part; one that is not finite is its own first part.
 __device__ __forceinline__ void split2(float a, float b, uint32_t (&w)[kParts]) {
-    uint32_t pa[kParts], pb[kParts];
-    split_parts(a, pa);
-    split_parts(b, pb);
-    if (!isfinite(a)) { pa[0] = isnan(a) ? 0x7fc00000u : __float_as_uint(a); pa[1] = pa[2] = 0; }
-    if (!isfinite(b)) { pb[0] = isnan(b) ? 0x7fc00000u : __float_as_uint(b); pb[1] = pb[2] = 0; }
+    constexpr float kTop = 3.3961775e38f;                          // half way from the largest bf16 to infinity
+    w[0] = pack2<__nv_bfloat16>(a, b);
+    float ra = a - __uint_as_float(w[0] << 16), rb = b - __uint_as_float(w[0] & 0xffff0000u);
+    if (!(fabsf(a) < kTop && fabsf(b) < kTop)) {
+        if (fabsf(a) >= kTop) {
+            w[0] = (w[0] & 0xffff0000u) | __float_as_uint(a) >> 16;
+            ra = a - __uint_as_float(w[0] << 16);
+        }
+        if (fabsf(b) >= kTop) {
+            w[0] = (w[0] & 0xffffu) | (__float_as_uint(b) & 0xffff0000u);
+            rb = b - __uint_as_float(w[0] & 0xffff0000u);
+        }
+        if (!isfinite(a)) ra = 0.f;
+        if (!isfinite(b)) rb = 0.f;
+    }
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) w[k] = (pa[k] >> 16) | pb[k];
+    for (int k = 1; k < kParts; ++k) {
+        w[k] = pack2<__nv_bfloat16>(ra, rb);
+        ra -= __uint_as_float(w[k] << 16);
+        rb -= __uint_as_float(w[k] & 0xffff0000u);
+    }
 }
 // 32 columns of one row (fp32, in registers) as the parts' boxes of 2048 bytes.
 __device__ __forceinline__ void write_parts(unsigned char* boxes, int lane, const float (&v)[32]) {

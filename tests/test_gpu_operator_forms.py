@@ -115,3 +115,47 @@ def test_norm_where_only_the_weighted_squares_pass_32_bits(P, n, d, dtype):
     x["y"] = (x["y"].float() * 3e16).to(N.TYPES[dtype])
     w["w_post"] = (w["w_post"].float() * 256).to(N.TYPES[dtype])
     N.run_and_check(x, w, dtype)
+
+
+def products_alone(x, w):
+    """x w^T of the tiles' kernel by itself: with relu, U = 1 and a projection that is a piece of the unit matrix, y = G."""
+    P, n, d = x.shape
+    f = w.shape[1]
+    x[..., 0] = 1.0
+    w_up = torch.zeros(P, f, d, device="cuda")
+    w_up[..., 0] = 1.0
+    w_down = torch.eye(d, f, device="cuda").expand(P, d, f).contiguous()
+    k = min(d, f)
+    y, _ = B.feed_forward(x, w, w_up, w_down, activation="relu", save=True)
+    return y[..., :k], (x.double() @ w.double().transpose(1, 2))[..., :k]
+
+
+@pytest.mark.parametrize("kind", ["worst", "random"])
+@pytest.mark.parametrize("d", [16, 64, 256, 1024])
+def test_products_of_fp32_parts(kind, d):
+    """Positive values, so that errors of one sign show.  In units u = 2^-23 of the sum: parts left out 1/2; an addition into the
+    accumulator of the first parts truncates by one of what it holds so far (d / 16 of them grow to the sum, at most 16
+    at a time); their sums are added in 32 bits, 1/2 each of what there is; the accumulator of the smaller parts holds 2^-7 and meets
+    5 d / 16 additions; the last addition 1/2."""
+    worst = torch.tensor([0x3f80ffff], dtype=torch.int32).view(torch.float32).item()     # parts by truncation: 2^-7 and 2^-15 left
+    gen = torch.Generator(device="cuda").manual_seed(29)
+    make = lambda *s: torch.full(s, worst, device="cuda") if kind == "worst" else 1 + torch.rand(s, generator=gen, device="cuda")  # noqa: E731
+    y, want = products_alone(make(1, 300, d), make(1, 128, d))
+    adds = max(1, d // 16)
+    chunks = -(-adds // 16)
+    units = 0.5 + (min(adds, 16) + 1) / 2 + (chunks + 1) / 4 * (chunks > 1) + 5 * adds / 2 * 2 ** -7 + 0.5
+    assert float(((y.double() - want) / want).abs().max()) <= units * 2.0 ** -23
+
+
+def test_products_of_fp32_values_near_the_ends_of_their_range():
+    """The largest finite values keep their parts (rounded to bf16 they would be infinite); the smallest ones lose at most what
+    bf16 cannot hold."""
+    top = torch.finfo(torch.float32).max
+    x = torch.zeros(1, 70, 16, device="cuda")
+    w = torch.zeros(1, 16, 16, device="cuda")
+    w[0, :, 1] = 0.5
+    values = [top, top * (1 - 2.0 ** -9), 3.39e38, 3.4e38, 1e38, 2.0 ** -100, 1.7e-33, 2.0 ** -126]
+    for i, v in enumerate(values):
+        x[0, i, 1] = v
+    y, want = products_alone(x, w)
+    assert torch.all((y.double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -133)
