@@ -651,7 +651,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 const int chunks = (ksteps + kChunk - 1) / kChunk;
 #pragma unroll
                 for (int x = 0; x < BN / 2; ++x) sum[x] = 0.f;
-                auto take = [&](uint32_t from) {
+                // (what is left of a sum that is not finite is infinity times the zeros of the other's smaller parts)
+                auto take = [&](uint32_t from, auto smaller) {
                     constexpr int LW = BN / 2 < 32 ? 16 : 32;
                     tc_fence_after();
 #pragma unroll
@@ -659,7 +660,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                         uint32_t v[LW];
                         tc_load(v, from + lanes + column(x));
 #pragma unroll
-                        for (int e = 0; e < LW; ++e) sum[x + e] += __uint_as_float(v[e]);
+                        for (int e = 0; e < LW; ++e)
+                            if (!decltype(smaller)::value || isfinite(sum[x + e])) sum[x + e] += __uint_as_float(v[e]);
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -667,11 +669,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 for (int z = 0; z < chunks; ++z, ++count) {
                     const int from = count & 1;
                     mbar_wait(&acc_full[from], (count >> 1) & 1, s_abort, a.err);
-                    take(tmem + from * Shape::kCols);
+                    take(tmem + from * Shape::kCols, std::false_type{});
                     if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[from]), 0));
                 }
                 mbar_wait(&small_full[turn & 1], (turn >> 1) & 1, s_abort, a.err);
-                take(tmem + (2 + (turn & 1)) * Shape::kCols);
+                take(tmem + (2 + (turn & 1)) * Shape::kCols, std::true_type{});
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&small_empty[turn & 1]), 0));
             }
             if constexpr (EPI == kEpiStore) {

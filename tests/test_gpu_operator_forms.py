@@ -159,3 +159,28 @@ def test_products_of_fp32_values_near_the_ends_of_their_range():
         x[0, i, 1] = v
     y, want = products_alone(x, w)
     assert torch.all((y.double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -133)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n", [1, 8, 40, 300])
+def test_an_infinite_operand_has_one_result_in_every_kernel(n, dtype):
+    """Positive operands: infinity times any of them is infinity, whatever kernel the number of tokens goes to and whether or not
+    the other has smaller parts."""
+    d, f, dt = 64, 96, N.TYPES[dtype]
+    full = lambda rows, cols, v: torch.full((1, rows, cols), v, device="cuda").to(dt)  # noqa: E731
+    for value in (0.5, 0.3):                          # one part, three parts
+        w = (full(f, d, value), full(f, d, value), full(d, f, value))
+        x = full(n, d, 1.0)
+        x[0, 0, 3] = float("inf")
+        alone = B.feed_forward(x, *w)
+        y, saved = B.feed_forward(x, *w, save=True)
+        for got in (alone, y):
+            assert torch.all(torch.isposinf(got[0, 0])) and torch.isfinite(got[0, 1:]).all()
+        x[0, 0, 3] = 1.0
+        dy = full(n, d, 0.25)
+        dy[0, 0, 5] = float("inf")
+        _, saved = B.feed_forward(x, *w, save=True)
+        dx, (d_gate, d_up, d_down) = B.feed_forward_backward(dy, x, *w, saved)
+        assert torch.all(torch.isposinf(dx[0, 0])) and torch.isfinite(dx[0, 1:]).all()
+        assert torch.all(torch.isposinf(d_gate)) and torch.all(torch.isposinf(d_up)) and torch.all(torch.isposinf(d_down[0, 5]))
+        assert torch.isfinite(d_down[0, 6:]).all()
