@@ -389,9 +389,11 @@ int64_t eg_residual_norm_workspace(int64_t P, int64_t width);
  * eg_feed_forward_backward reads dy, x, the weights and `saved` and overwrites dx, d_gate, d_up,
  * d_down; each of the four may be left out.  rows == 0 gives zero weight gradients.
  * `workspace` (device, 16-byte aligned) holds at least eg_feed_forward_workspace(args, backward)
- * bytes -- which depends on sizes, alignment and strides of the given matrices -- and is free for
- * reuse once the stream has passed the call.  Rows of any stride and alignment are taken; rows on
- * 16-byte boundaries are read in place, others are copied into the workspace first.
+ * bytes -- which depends on sizes, alignment and strides of the given matrices, and on whether
+ * `saved` is given -- and is free for reuse once the stream has passed the call.  Rows of any stride
+ * and alignment are taken, and replicas one after the other or row by row in turn ([rows][P][columns]);
+ * rows on 16-byte boundaries are read in place, others are copied into the workspace first.  Matrices
+ * whose rows or replicas overlap (one matrix for all replicas: a stride of 0) are refused.
  * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded
  * into a graph; the results do not depend on the run.  Outputs must not overlap inputs or each
  * other.  Errors: EG_ERR_INVALID, EG_ERR_CUDA. */

@@ -208,10 +208,14 @@ bool valid(const eg_feed_forward_args* q, bool backward) {
             continue;
         }
         if ((uintptr_t)e.m->data % size || e.m->row_stride < 0 || e.m->replica_stride < 0) return false;
-        // neither the rows of a matrix nor the replicas' matrices overlap
+        // neither the rows of a matrix nor the replicas' matrices overlap: the replicas' lie one after the other, or take
+        // turns row by row
         if (e.rows > 1 && (e.m->row_stride < e.cols || e.m->row_stride >= (1ll << 36))) return false;
-        if (q->P > 1 && (e.m->replica_stride < (e.rows - 1) * e.m->row_stride + e.cols || e.m->replica_stride >= (1ll << 36)))
-            return false;
+        if (q->P > 1) {
+            const long long rep = e.m->replica_stride, row = e.m->row_stride;
+            const bool apart = rep >= (e.rows - 1) * row + e.cols, in_turn = rep >= e.cols && row >= (q->P - 1) * rep + e.cols;
+            if (rep >= (1ll << 36) || !(apart || in_turn)) return false;
+        }
     }
     return true;
 }

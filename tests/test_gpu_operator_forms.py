@@ -3,6 +3,7 @@ takes them, against the formulas in 64 bits."""
 import pytest
 import torch
 
+import test_gpu_feed_forward as F
 import test_gpu_residual_norm as N
 from paper_2103_07454_b200 import binding as B
 
@@ -184,3 +185,30 @@ def test_an_infinite_operand_has_one_result_in_every_kernel(n, dtype):
         assert torch.all(torch.isposinf(dx[0, 0])) and torch.isfinite(dx[0, 1:]).all()
         assert torch.all(torch.isposinf(d_gate)) and torch.all(torch.isposinf(d_up)) and torch.all(torch.isposinf(d_down[0, 5]))
         assert torch.isfinite(d_down[0, 6:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("P,n,d,f", [(3, 1, 64, 96), (2, 9, 64, 96), (3, 45, 64, 104), (2, 300, 264, 136), (3, 5, 33, 51), (2, 70, 41, 66)])
+@pytest.mark.parametrize("room", [0, 8])
+def test_feed_forward_of_replicas_that_take_turns_row_by_row(P, n, d, f, room, dtype):
+    """[rows][P][columns]: the same bits as one replica after the other, and nothing between the rows is written."""
+    t = F.inputs(P, n, d, f, dtype, seed=30)
+    names = ("x", "w_gate", "w_up", "w_down", "dy")
+
+    def in_turn(m, fill):
+        to = torch.full((m.shape[1], P, m.shape[2] + room), fill, dtype=m.dtype, device="cuda")
+        to[..., :m.shape[2]] = m.transpose(0, 1)
+        return to
+
+    x, wg, wu, wd, dy = (in_turn(t[k], 7.0)[..., :t[k].shape[2]].transpose(0, 1) for k in names)
+    buffers = [in_turn(torch.full_like(t[k], 3.0), 3.0) for k in ("x", "w_gate", "w_up", "w_down")]
+    out, *grads = (b[..., :t[k].shape[2]].transpose(0, 1) for b, k in zip(buffers, names))
+    want = F.run(t, "silu")
+    assert torch.equal(B.feed_forward(x, wg, wu, wd), want["alone"])
+    y, saved = B.feed_forward(x, wg, wu, wd, save=True, out=out)
+    dx, _ = B.feed_forward_backward(dy, x, wg, wu, wd, saved, d_weights=grads)
+    for name, got in zip(F.NAMES, (y, dx, *grads)):
+        assert torch.equal(got, want[name]), name
+    for b, k in zip(buffers, names):
+        assert torch.all(b[..., t[k].shape[2]:] == 3.0)
+    assert B.operator_status() == 0

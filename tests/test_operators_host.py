@@ -119,3 +119,15 @@ def test_tensors_on_the_host_are_refused():
         B.residual_norm_backward(x, None, x, x)
     with pytest.raises(B.EventGradError):
         B.feed_forward_backward(x, x, w, w, w, torch.zeros(8, dtype=torch.uint8))
+
+
+def test_feed_forward_takes_replicas_row_by_row():
+    """[rows][P][columns], with room between; one element less and they overlap."""
+    lib = B.load_library()
+    need = lib.eg_feed_forward_workspace(ffn_args(saved=(0, 0)), 0)
+    for x in ((A, 64, 128), (A, 64, 192), (A, 72, 136)):
+        assert lib.eg_feed_forward_workspace(ffn_args(saved=(0, 0), x=x), 0) == need
+    assert lib.eg_feed_forward_workspace(ffn_args(saved=(0, 0), x=(A + 2, 64, 128)), 0) > need
+    for x in ((A, 63, 128), (A, 64, 127), (A, 0, 64), (A, 0, 1 << 20)):
+        assert lib.eg_feed_forward_workspace(ffn_args(saved=(0, 0), x=x), 0) == 0
+        assert lib.eg_feed_forward(ffn_args(x=x), A, 1 << 40, None) == INVALID
