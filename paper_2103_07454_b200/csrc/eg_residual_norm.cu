@@ -962,10 +962,15 @@ eg_status check(const eg_residual_norm_args* q, NormArgs* a, bool* aligned) {
     const eg_matrix* vectors[] = {&q->w_post, &q->gate, &q->scale, &q->w_pre, &q->d_w_post, &q->d_gate, &q->d_scale, &q->d_w_pre};
     for (const eg_matrix* m : vectors)
         if (m->data && (((uintptr_t)m->data % size) || m->replica_stride < 0)) return EG_ERR_INVALID;
-    // outputs are written once: rows and replicas of an output must not fall on one another
+    // outputs are written once: rows and replicas of an output must not fall on one another; the replicas' lie one after the
+    // other, or take turns row by row
     const eg_matrix* written[] = {&q->residual_out, &q->out, &q->dy, &q->d_residual};
-    for (const eg_matrix* m : written)
-        if (m->data && ((q->rows > 1 && m->row_stride < q->width) || (q->P > 1 && m->replica_stride < q->width))) return EG_ERR_INVALID;
+    for (const eg_matrix* m : written) {
+        if (!m->data) continue;
+        const long long rep = m->replica_stride, row = m->row_stride;
+        if ((q->rows > 1 && row < q->width) || (q->P > 1 && rep < q->width)) return EG_ERR_INVALID;
+        if (q->rows > 1 && q->P > 1 && (rep - q->width) / (q->rows - 1) < row && (row - q->width) / (q->P - 1) < rep) return EG_ERR_INVALID;
+    }
     const eg_matrix* sums[] = {&q->d_w_post, &q->d_gate, &q->d_scale, &q->d_w_pre};
     for (const eg_matrix* m : sums)
         if (m->data && q->P > 1 && m->replica_stride < q->width) return EG_ERR_INVALID;

@@ -212,3 +212,24 @@ def test_feed_forward_of_replicas_that_take_turns_row_by_row(P, n, d, f, room, d
     for b, k in zip(buffers, names):
         assert torch.all(b[..., t[k].shape[2]:] == 3.0)
     assert B.operator_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("P,n,d", [(3, 5, 64), (2, 700, 96), (2, 9, 33), (4, 2, 8)])
+@pytest.mark.parametrize("room", [0, 8])
+def test_norm_of_replicas_that_take_turns_row_by_row(P, n, d, room, dtype):
+    x, w = N.inputs(P, n, d, dtype, seed=31)
+    want = B.residual_norm(x["y"], x["residual"], **w)
+    back = B.residual_norm_backward(x["d_r"], x["d_o"], x["y"], x["residual"], **w)
+    buffers = [torch.full((n, P, d + room), 3.0, dtype=N.TYPES[dtype], device="cuda") for _ in range(6)]
+    views = [b[..., :d].transpose(0, 1) for b in buffers]
+    for v, k in zip(views, ("y", "residual", "d_r", "d_o")):
+        v.copy_(x[k])
+    y, r, d_r, d_o, r_out, out = views
+    got = B.residual_norm(y, r, residual_out=r_out, out=out, **w)
+    assert got[0].data_ptr() == r_out.data_ptr()
+    size = {"fp32": 2.0 ** -20, "bf16": 2.0 ** -6}[dtype]             # another kernel may take other strides: other sums, one unit
+    for a, b in zip((*got, *B.residual_norm_backward(d_r, d_o, y, r, **w)[:2]), (*want, *back[:2])):
+        assert torch.all((a.double() - b.double()).abs() <= size * b.double().abs().amax(-1, keepdim=True))
+    for b in buffers:
+        assert torch.all(b[..., d:] == 3.0)

@@ -131,3 +131,16 @@ def test_feed_forward_takes_replicas_row_by_row():
     for x in ((A, 63, 128), (A, 64, 127), (A, 0, 64), (A, 0, 1 << 20)):
         assert lib.eg_feed_forward_workspace(ffn_args(saved=(0, 0), x=x), 0) == 0
         assert lib.eg_feed_forward(ffn_args(x=x), A, 1 << 40, None) == INVALID
+
+
+@pytest.mark.parametrize("rows,P", [(2, 2), (4, 2), (4, 3), (5, 2)])
+def test_norm_refuses_results_that_fall_on_one_another(rows, P):
+    """Replicas apart: at least (rows - 1) * row + width; in turn: a row of at least (P - 1) * replica + width."""
+    lib = B.load_library()
+    w = 64
+    outs = ("residual_out", "out")
+    grads = ("dy", "d_residual")
+    for rep, row in (((rows - 1) * w + w - 1, w), (w, w * P - 1), (w, w), (3 * w * (rows - 1) + w - 1, 3 * w), (2 * w, 2 * w * (P - 1) + w - 1)):
+        for name in outs + grads:
+            call = lib.eg_residual_norm if name in outs else lib.eg_residual_norm_backward
+            assert call(norm_args(P=P, rows=rows, width=w, **{name: (A, rep, row)}), None) == INVALID, (name, rep, row)
