@@ -66,12 +66,14 @@ class EventGradError(RuntimeError):
 
 
 _lib = None
-_native = None        # csrc/marshal.cpp: the operators' arguments
+_native = None        # csrc/marshal.cpp: the operators' arguments (see _operators)
+_OPERATORS = ("eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace", "eg_feed_forward",
+              "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace")
 
 
 def load_library() -> C.CDLL:
     """Loads the CUDA library; raises if it is missing (there is no CPU path)."""
-    global _lib, _native
+    global _lib
     if _lib is not None:
         return _lib
     # EG_LIBRARY names another build of the same library (the bounds-checked one, for instance)
@@ -124,27 +126,36 @@ def load_library() -> C.CDLL:
     lib.eg_topk_repeat_count.argtypes = [vp, u64p]
     lib.eg_set_quantisation.argtypes = [vp, C.c_int]
     lib.eg_last_quantised.argtypes = [vp, vp, vp]
-    lib.eg_clip_gradients.argtypes = [vp, vp, C.c_int, C.c_double, C.c_int, vp, vp, vp]
-    lib.eg_residual_norm.argtypes = lib.eg_residual_norm_backward.argtypes = [C.c_char_p, vp]
-    lib.eg_residual_norm_workspace.argtypes = [C.c_int64, C.c_int64]
-    lib.eg_residual_norm_workspace.restype = C.c_int64
-    lib.eg_operator_status.argtypes = [vp]
-    lib.eg_feed_forward.argtypes = lib.eg_feed_forward_backward.argtypes = [C.c_char_p, vp, C.c_int64, vp]
-    lib.eg_feed_forward_saved_bytes.argtypes = [C.c_char_p]
-    lib.eg_feed_forward_saved_bytes.restype = C.c_int64
-    lib.eg_feed_forward_workspace.argtypes = [C.c_char_p, C.c_int]
-    lib.eg_feed_forward_workspace.restype = C.c_int64
     lib.eg_last_cuda_error.argtypes = [vp]
     lib.eg_last_launch_count.argtypes = [vp]
-    try:
-        from . import _marshal
-    except ImportError as e:
-        raise EventGradError(f"{e}: build it with `python -m paper_2103_07454_b200.build`") from e
-    _marshal.init(EventGradError, *(C.cast(getattr(lib, f), vp).value for f in (
-        "eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace", "eg_feed_forward",
-        "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace")))
-    _lib, _native = lib, _marshal
+    if hasattr(lib, "eg_operator_status"):      # builds from before the operators serve the step
+        lib.eg_clip_gradients.argtypes = [vp, vp, C.c_int, C.c_double, C.c_int, vp, vp, vp]
+        lib.eg_residual_norm.argtypes = lib.eg_residual_norm_backward.argtypes = [C.c_char_p, vp]
+        lib.eg_residual_norm_workspace.argtypes = [C.c_int64, C.c_int64]
+        lib.eg_residual_norm_workspace.restype = C.c_int64
+        lib.eg_operator_status.argtypes = [vp]
+        lib.eg_feed_forward.argtypes = lib.eg_feed_forward_backward.argtypes = [C.c_char_p, vp, C.c_int64, vp]
+        lib.eg_feed_forward_saved_bytes.argtypes = [C.c_char_p]
+        lib.eg_feed_forward_saved_bytes.restype = C.c_int64
+        lib.eg_feed_forward_workspace.argtypes = [C.c_char_p, C.c_int]
+        lib.eg_feed_forward_workspace.restype = C.c_int64
+    _lib = lib
     return lib
+
+
+def _operators():
+    """The operators' marshalling.  The step does without it, and without the operators in the library."""
+    global _native
+    if _native is None:
+        lib = load_library()
+        try:
+            from . import _marshal
+            addresses = [C.cast(getattr(lib, f), C.c_void_p).value for f in _OPERATORS]
+        except (ImportError, AttributeError) as e:
+            raise EventGradError(f"{e}: build it with `python -m paper_2103_07454_b200.build`") from e
+        _marshal.init(EventGradError, *addresses)
+        _native = _marshal
+    return _native
 
 
 def _check(lib, status: int, ctx=None, what: str = ""):
@@ -404,9 +415,10 @@ class EventGrad:
         tensors) of at most ``max_norm``.  ``grads``: ``[P, replica_stride]`` fp32, bf16 or fp16; the
         result goes to ``out`` (fp32, same shape; default: ``grads`` itself, which must then be fp32).
         Returns the norms before clipping, ``[P]`` fp32 on the device."""
+        native = _native or _operators()
         with _on(stream):
-            r = _native.clip_gradients(self._h.value if self._h else 0, self.P, self.replica_stride, grads, out, max_norm,
-                                       CLIP_ZERO_NONFINITE if zero_nonfinite else 0, norms)
+            r = native.clip_gradients(self._h.value if self._h else 0, self.P, self.replica_stride, grads, out, max_norm,
+                                      CLIP_ZERO_NONFINITE if zero_nonfinite else 0, norms)
         if r.__class__ is int:
             _check(self._lib, r, self._h, "eg_clip_gradients")
         return r
@@ -493,11 +505,11 @@ def residual_norm(y: Optional[torch.Tensor], residual: torch.Tensor, *, w_post: 
     ``o = rms(r') * w_pre`` for ``[P, rows, width]`` activations and ``[P, width]`` vectors.
 
     Returns ``(r', o)``; ``o`` is None without ``w_pre``.  ``y`` None: only the scaled residual."""
-    lib = load_library()
+    native = _native or _operators()
     with _on(stream):
-        r = _native.residual_norm(y, residual, w_post, gate, scale, w_pre, eps, residual_out, out)
+        r = native.residual_norm(y, residual, w_post, gate, scale, w_pre, eps, residual_out, out)
     if r.__class__ is int:
-        _check(lib, r, None, "eg_residual_norm")
+        _check(_lib, r, None, "eg_residual_norm")
     return r
 
 
@@ -512,12 +524,12 @@ def residual_norm_backward(d_residual_out: Optional[torch.Tensor], d_out: Option
 
     ``d_weights``: four ``[P, width]`` tensors that receive the last ones (views of a gradient buffer in
     the step's layout, say; None for a vector that was not given); default: new tensors."""
-    lib = load_library()
+    native = _native or _operators()
     d_weights = _some(d_weights, 4, "residual_norm_backward")
     with _on(stream):
-        r = _native.residual_norm_backward(d_residual_out, d_out, y, residual, w_post, gate, scale, w_pre, eps, d_weights)
+        r = native.residual_norm_backward(d_residual_out, d_out, y, residual, w_post, gate, scale, w_pre, eps, d_weights)
     if r.__class__ is int:
-        _check(lib, r, None, "eg_residual_norm_backward")
+        _check(_lib, r, None, "eg_residual_norm_backward")
     return r
 
 
@@ -535,11 +547,11 @@ def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_do
     ``x``: ``[P, rows, d_model]``; ``w_gate``, ``w_up``: ``[P, d_ff, d_model]``; ``w_down``: ``[P, d_model, d_ff]``
     (views of a parameter buffer, say).  With ``save`` returns ``(y, saved)``, the second for
     ``feed_forward_backward``."""
-    lib = load_library()
+    native = _native or _operators()
     with _on(stream):
-        r = _native.feed_forward(x, w_gate, w_up, w_down, _activation(activation), bool(save), out)
+        r = native.feed_forward(x, w_gate, w_up, w_down, _activation(activation), bool(save), out)
     if r.__class__ is int:
-        _check(lib, r, None, "eg_feed_forward")
+        _check(_lib, r, None, "eg_feed_forward")
     return r
 
 
@@ -551,12 +563,12 @@ def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
 
     ``d_weights``: three tensors of the weights' shapes that receive the last ones (views of a gradient
     buffer in the step's layout, say; None: not wanted); default: new tensors."""
-    lib = load_library()
+    native = _native or _operators()
     d_weights = _some(d_weights, 3, "feed_forward_backward")
     with _on(stream):
-        r = _native.feed_forward_backward(x, w_gate, w_up, w_down, _activation(activation), dy, saved, d_weights)
+        r = native.feed_forward_backward(x, w_gate, w_up, w_down, _activation(activation), dy, saved, d_weights)
     if r.__class__ is int:
-        _check(lib, r, None, "eg_feed_forward_backward")
+        _check(_lib, r, None, "eg_feed_forward_backward")
     return r
 
 

@@ -61,8 +61,9 @@ def build_marshal(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    lib = _compile(LIB, [], force, verbose)     # first: the step does without the rest
     build_marshal(force)
-    return _compile(LIB, [], force, verbose)
+    return lib
 
 
 def build_debug(force: bool = False, verbose: bool = False) -> str:
