@@ -2,6 +2,7 @@
 bounds-checked build, ``libeventgrad_debug.so``)."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -15,6 +16,8 @@ LIB = os.path.join(HERE, "libeventgrad.so")
 #: torch tensors to C arguments, for the operators
 MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")
 MARSHAL = os.path.join(HERE, "_marshal.so")
+#: what it was built for: it fits one interpreter and one torch
+MARSHAL_STAMP = os.path.join(HERE, "_build", "_marshal.txt")
 LIB_DEBUG = os.path.join(HERE, "libeventgrad_debug.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
@@ -46,9 +49,20 @@ def _compile(lib: str, extra, force: bool, verbose: bool) -> str:
     return lib
 
 
+def _stamp() -> str:
+    """Interpreter and torch by version and place, from the latter's files (importing it takes seconds)."""
+    top = os.path.dirname(importlib.util.find_spec("torch").origin)
+    with open(os.path.join(top, "version.py")) as f:
+        return f"{sys.version}\n{sysconfig.get_config_var('SOABI')}\n{top}\n{f.read()}"
+
+
 def build_marshal(force: bool = False) -> str:
     newest = max(os.path.getmtime(p) for p in (MARSHAL_SRC, os.path.join(HERE, "..", "include", "eventgrad.h")))
-    if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < newest:
+    stamp, built_for = _stamp(), None
+    if os.path.exists(MARSHAL_STAMP):
+        with open(MARSHAL_STAMP) as f:
+            built_for = f.read()
+    if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < newest or built_for != stamp:
         import torch
         top = os.path.dirname(torch.__file__)
         include = [os.path.join(top, "include"), os.path.join(top, "include", "torch", "csrc", "api", "include"),
@@ -57,6 +71,9 @@ def build_marshal(force: bool = False) -> str:
                         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
                        + [a for d in include for a in ("-isystem", d)] + ["-o", MARSHAL, MARSHAL_SRC, "-L" + os.path.join(top, "lib")]
                        + ["-l" + n for n in ("torch_python", "torch_cuda", "c10_cuda", "torch_cpu", "c10")], check=True)
+        os.makedirs(os.path.dirname(MARSHAL_STAMP), exist_ok=True)
+        with open(MARSHAL_STAMP, "w") as f:
+            f.write(stamp)
     return MARSHAL
 
 

@@ -49,3 +49,34 @@ def test_operators_are_there_in_this_build():
     assert B._operators() is B._operators()
     with pytest.raises(TypeError):
         B._operators().residual_norm()
+
+
+def test_the_extension_is_built_again_for_another_torch_or_interpreter(tmp_path, monkeypatch):
+    """It is compiled against both; its source's time says nothing about them."""
+    from paper_2103_07454_b200 import build
+    calls = []
+
+    def compiler(cmd, check):
+        calls.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+
+    monkeypatch.setattr(build, "MARSHAL", str(tmp_path / "_marshal.so"))
+    monkeypatch.setattr(build, "MARSHAL_STAMP", str(tmp_path / "deep" / "_marshal.txt"))
+    monkeypatch.setattr(build.subprocess, "run", compiler)
+    build.build_marshal()
+    build.build_marshal()
+    assert len(calls) == 1
+    monkeypatch.setattr(build.sys, "version", "another interpreter")
+    build.build_marshal()
+    build.build_marshal()
+    assert len(calls) == 2
+    here = build._stamp()
+    monkeypatch.setattr(build, "_stamp", lambda: here + "another torch")
+    build.build_marshal()
+    build.build_marshal()
+    assert len(calls) == 3
+    build.build_marshal(force=True)
+    assert len(calls) == 4
+    os.remove(tmp_path / "_marshal.so")
+    build.build_marshal()
+    assert len(calls) == 5
