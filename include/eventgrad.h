@@ -413,9 +413,15 @@ eg_status eg_feed_forward(const eg_feed_forward_args* args, void* workspace, int
 eg_status eg_feed_forward_backward(const eg_feed_forward_args* args, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* The operators' kernels never trap and their waits are bounded; a wait that runs out sets a word
- * of the current device.  Synchronises `stream`, returns EG_ERR_TIMEOUT if that happened in any
- * call since the last query (EG_OK otherwise) and clears the word. */
+ * of the current device (one for all its streams and callers) and leaves that call's results
+ * undefined.  Synchronises `stream`, returns EG_ERR_TIMEOUT if that happened in any call on the
+ * device since the last query (EG_OK otherwise) and clears the word. */
 eg_status eg_operator_status(void* stream);
+
+/* Lets the operators' bounded wait number `which` (0, 1 or 2) run out on a barrier that nobody
+ * arrives on, with a limit of about a millisecond; eg_operator_status then reports it.  Only
+ * enqueues work on `stream`. */
+eg_status eg_selftest_operator_wait(int which, void* stream);
 
 /* Change norms without any allocation.  (The paper has no counterpart: this is a service
  * entry point of the library, not a step of the method.)

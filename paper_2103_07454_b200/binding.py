@@ -37,7 +37,7 @@ EXPORTS = [
     "eg_last_quantised",
     "eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace",
     "eg_operator_status", "eg_feed_forward", "eg_feed_forward_backward", "eg_feed_forward_saved_bytes",
-    "eg_feed_forward_workspace",
+    "eg_feed_forward_workspace", "eg_selftest_operator_wait",
 ]
 STATIC_MAX_TENSORS = 192
 STATIC_MAX_PARTIALS = 524288
@@ -575,6 +575,13 @@ def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
 def operator_status(device: Optional[torch.device] = None) -> int:
     """``eg_operator_status`` on the current stream: 0, or EG_ERR_TIMEOUT (5) when a bounded wait ran out."""
     return int(load_library().eg_operator_status(torch.cuda.current_stream(device).cuda_stream))
+
+
+def selftest_operator_wait(which: int, device: Optional[torch.device] = None):
+    """``eg_selftest_operator_wait``: one of the operators' bounded waits (0, 1, 2) runs out; ``operator_status`` tells."""
+    lib = load_library()
+    stream = C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    _check(lib, lib.eg_selftest_operator_wait(C.c_int(which), stream), None, "eg_selftest_operator_wait")
 
 
 def from_workload(wl, **overrides) -> EventGrad:

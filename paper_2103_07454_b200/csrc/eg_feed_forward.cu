@@ -591,6 +591,21 @@ cudaError_t zero(const eg_matrix& m, long long P, long long rows, long long cols
     return cudaSuccess;
 }
 
+// A wait on a barrier that nobody arrives on, with a limit of `cycles`.
+__global__ void k_selftest_operator_wait(int which, long long cycles, unsigned int* err) {
+    __shared__ __align__(8) uint64_t s_bar;
+    __shared__ volatile int s_abort;
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        op_mbar_init(&s_bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (which == 0) (void)op_mbar_wait(&s_bar, 0, &s_abort, err, cycles);
+    else if (which == 1) (void)op_mbar_wait_cluster(&s_bar, 0, &s_abort, err, cycles);
+    else mbar_wait(&s_bar, 0, &s_abort, err, cycles);
+}
+
 }  // namespace
 }  // namespace eg
 
@@ -651,6 +666,14 @@ eg_status eg_feed_forward_backward(const eg_feed_forward_args* q, void* workspac
                           : q->dtype == EG_BF16 ? backward<__nv_bfloat16>(b, err, stream)
                                                 : backward<__half>(b, err, stream);
     return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
+}
+
+eg_status eg_selftest_operator_wait(int which, void* stream_v) {
+    if (which < 0 || which > 2) return EG_ERR_INVALID;
+    unsigned int* err = operator_error_word();
+    if (!err) return EG_ERR_CUDA;
+    k_selftest_operator_wait<<<1, 64, 0, static_cast<cudaStream_t>(stream_v)>>>(which, 2000000ll /* about a millisecond */, err);
+    return cudaGetLastError() == cudaSuccess ? EG_OK : EG_ERR_CUDA;
 }
 
 }  // extern "C"

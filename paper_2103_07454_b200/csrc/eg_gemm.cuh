@@ -125,14 +125,15 @@ __device__ __forceinline__ bool mbar_test_now(uint64_t* bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded; after a time-out anywhere in the CTA every wait returns at once and the walk goes on.
-__device__ __forceinline__ void mbar_wait(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err) {
+__device__ __forceinline__ void mbar_wait(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err,
+                                          long long cycles = kOpWaitCycles) {
     if (mbar_test_now(bar, parity)) return;
     const long long t0 = clock64();
     unsigned spins = 0;
     while (!mbar_test_now(bar, parity)) {
         if ((++spins & 63u) != 0) continue;
         if (*s_abort) return;
-        if (clock64() - t0 > kOpWaitCycles) {
+        if (clock64() - t0 > cycles) {
             *s_abort = 1;
             atomicOr(err, kOpErrWaitTimeout);
             return;

@@ -161,14 +161,15 @@ __device__ __forceinline__ bool op_mbar_test(uint64_t* bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool op_mbar_wait(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err) {
+__device__ __forceinline__ bool op_mbar_wait(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err,
+                                             long long cycles = kOpWaitCycles) {
     if (op_mbar_test(bar, parity)) return true;
     const long long t0 = clock64();
     unsigned spins = 0;
     while (!op_mbar_test(bar, parity)) {
         if ((++spins & 63u) != 0) continue;
         if (*s_abort) return false;
-        if (clock64() - t0 > kOpWaitCycles) {
+        if (clock64() - t0 > cycles) {
             *s_abort = 1;
             atomicOr(err, kOpErrWaitTimeout);
             return false;
@@ -177,7 +178,8 @@ __device__ __forceinline__ bool op_mbar_wait(uint64_t* bar, uint32_t parity, vol
     return true;
 }
 // The same for a barrier that the other CTA of a cluster arrives on.
-__device__ __forceinline__ bool op_mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err) {
+__device__ __forceinline__ bool op_mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned int* err,
+                                                     long long cycles = kOpWaitCycles) {
     const long long t0 = clock64();
     for (unsigned spins = 1;; ++spins) {
         uint32_t ok;
@@ -191,7 +193,7 @@ __device__ __forceinline__ bool op_mbar_wait_cluster(uint64_t* bar, uint32_t par
         if (ok) return true;
         if ((spins & 63u) != 0) continue;
         if (*s_abort) return false;
-        if (clock64() - t0 > kOpWaitCycles) {
+        if (clock64() - t0 > cycles) {
             *s_abort = 1;
             atomicOr(err, kOpErrWaitTimeout);
             return false;

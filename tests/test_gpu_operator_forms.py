@@ -233,3 +233,20 @@ def test_norm_of_replicas_that_take_turns_row_by_row(P, n, d, room, dtype):
         assert torch.all((a.double() - b.double()).abs() <= size * b.double().abs().amax(-1, keepdim=True))
     for b in buffers:
         assert torch.all(b[..., d:] == 3.0)
+
+
+def test_a_wait_that_runs_out_is_reported_once_and_leaves_the_device_usable():
+    assert B.operator_status() == 0
+    x, w = N.inputs(2, 400, 512, "bf16", seed=32)
+    want = B.residual_norm(x["y"], x["residual"], **w)
+    for which in (0, 1, 2):
+        B.selftest_operator_wait(which)
+        assert B.operator_status() == 5               # EG_ERR_TIMEOUT
+        assert B.operator_status() == 0
+        for a, b in zip(B.residual_norm(x["y"], x["residual"], **w), want):
+            assert torch.equal(a, b)
+    t = F.inputs(2, 40, 64, 96, "bf16", seed=32)
+    F.run_and_check(t, "bf16")
+    for which in (-1, 3):
+        with pytest.raises(B.EventGradError):
+            B.selftest_operator_wait(which)
