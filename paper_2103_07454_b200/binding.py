@@ -477,6 +477,7 @@ def change_norms_static(x: torch.Tensor, xhat: torch.Tensor, tensor_offset: Sequ
 # --------------------------------------------------------------------------------------
 # operators around the step: values of one type per call, ``[P, rows, width]`` activations and
 # ``[P, ...]`` views of the replicas' weights, on torch's current stream unless one is given
+# (not differentiable by autograd: tensors that require gradients are refused outside of torch.no_grad())
 # --------------------------------------------------------------------------------------
 _FFN_ARGS = struct.Struct("=6q30q2q")     # eg_feed_forward_args
 _NORM_ARGS = struct.Struct("=4qd48q2q")   # eg_residual_norm_args

@@ -5,6 +5,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -50,6 +51,14 @@ const at::Tensor& on_device(const at::Tensor& t) {
     return t;
 }
 
+// The calls take no part in autograd.  Results without a graph where one is expected would be gradients lost without a word.
+const at::Tensor& plain(const at::Tensor& t, const char* what) {
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        throw Refused{std::string(what) + " requires a gradient, but the operators take no part in autograd: call them under "
+                                          "torch.no_grad(), and the *_backward calls for the gradients"};
+    return t;
+}
+
 // What a call's tensors have in common.
 struct Kind {
     at::ScalarType type;
@@ -69,6 +78,7 @@ eg_matrix given(PyObject* o, at::IntArrayRef sizes, const Kind& k, const char* w
         for (int64_t n : t.sizes()) s += std::to_string(n) + ", ";
         throw Refused{s + "] " + c10::toString(t.scalar_type()) + " on " + t.device().str()};
     }
+    plain(t, what);
     const auto st = t.strides();
     if (st.back() != 1 && sizes.back() > 1) throw Refused{std::string(what) + ": the last dimension must be contiguous"};
     return eg_matrix{t.data_ptr(), st[0], sizes.size() == 3 ? st[1] : 0};
@@ -151,6 +161,7 @@ struct NormCall {
 
     NormCall(const at::Tensor& residual, PyObject* y, PyObject* const* vectors, PyObject* eps, const char* what)
         : r(on_device(shaped(residual, what))), k{r.scalar_type(), r.device()}, guard(k.device) {
+        plain(r, "residual");
         q.P = r.size(0); q.rows = r.size(1); q.width = r.size(2);
         q.dtype = type_of(r);
         q.eps = number(eps);
@@ -301,7 +312,7 @@ PyObject* feed_forward_backward(PyObject* const* a) {
 // ------------------------------------------------------------------------------- clipping
 // context, P, replica_stride, grads, out, max_norm, flags, norms
 PyObject* clip_gradients(PyObject* const* a) {
-    const at::Tensor &g = tensor(a[3], "grads"), &out = a[4] == Py_None ? g : tensor(a[4], "out");
+    const at::Tensor &g = plain(tensor(a[3], "grads"), "grads"), &out = a[4] == Py_None ? g : plain(tensor(a[4], "out"), "out");
     const int64_t P = integer(a[1]), sizes[] = {P, integer(a[2])};
     const int type = type_of(g);
     const char* wrong = nullptr;

@@ -250,3 +250,35 @@ def test_a_wait_that_runs_out_is_reported_once_and_leaves_the_device_usable():
     for which in (-1, 3):
         with pytest.raises(B.EventGradError):
             B.selftest_operator_wait(which)
+
+
+def test_tensors_that_require_gradients_are_refused():
+    """The operators take no part in autograd: no result without a graph where one is expected."""
+    x, w = N.inputs(2, 5, 64, "fp32", seed=33)
+    t = F.inputs(2, 5, 64, 96, "fp32", seed=33)
+    weights = (t["w_gate"], t["w_up"], t["w_down"])
+    y, saved = B.feed_forward(t["x"], *weights, save=True)
+    eg = B.EventGrad(2, [40])
+    g = torch.ones(2, eg.replica_stride, device="cuda")
+
+    def calls(leaf):
+        swap = lambda m: m.requires_grad_() if m is leaf else m  # noqa: E731
+        norm = {k: swap(v) for k, v in w.items()}
+        ffn = [swap(m) for m in weights]
+        yield (x["y"], x["residual"], *w.values()), lambda: B.residual_norm(swap(x["y"]), swap(x["residual"]), **norm)[1]
+        yield (x["d_r"], x["d_o"], x["y"], x["residual"], *w.values()), lambda: B.residual_norm_backward(
+            swap(x["d_r"]), swap(x["d_o"]), swap(x["y"]), swap(x["residual"]), **norm)[0]
+        yield (t["x"], *weights), lambda: B.feed_forward(swap(t["x"]), *ffn)
+        yield (t["dy"], t["x"], *weights), lambda: B.feed_forward_backward(swap(t["dy"]), swap(t["x"]), *ffn, saved)[0]
+        yield (g,), lambda: eg.clip_gradients(swap(g), 1e9)
+
+    for number in range(5):
+        tensors, call = list(calls(None))[number]
+        want = call()
+        for leaf in tensors:
+            _, call = list(calls(leaf))[number]
+            with pytest.raises(B.EventGradError, match="autograd"):
+                call()
+            with torch.no_grad():
+                assert torch.equal(call(), want)
+            leaf.requires_grad_(False)
