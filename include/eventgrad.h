@@ -324,10 +324,11 @@ enum { EG_F32 = 0, EG_BF16 = 1, EG_F16 = 2 };
  * A norm of 0 leaves the gradients as they are.  A norm that is not finite follows the formula
  * (infinite: zeros, with NaN where the gradient is infinite; NaN: all NaN) unless flags has
  * EG_CLIP_ZERO_NONFINITE: the replica's gradients then become zeros, so that it takes no part in
- * the update of this step but averages with its neighbours.  max_norm >= 0; +infinity only
- * computes the norms (and widens).  Only enqueues work on `stream`; the first call of a context
- * allocates its scratch (make it outside a stream capture).  Errors: EG_ERR_INVALID,
- * EG_ERR_STATE (the previous call's stream is still busy), EG_ERR_OOM, EG_ERR_CUDA. */
+ * the update of this step but averages with its neighbours.  max_norm >= 0; +infinity only computes
+ * the norms (and widens), but for a NaN norm, which follows the formula here too.  Only enqueues
+ * work on `stream`; the first call of a context allocates its scratch (make it outside a stream
+ * capture).  Errors: EG_ERR_INVALID, EG_ERR_STATE (the previous call's stream is still busy),
+ * EG_ERR_OOM, EG_ERR_CUDA. */
 enum { EG_CLIP_ZERO_NONFINITE = 1 };
 eg_status eg_clip_gradients(eg_ctx* ctx, const void* grads, int dtype, double max_norm, int flags,
                             float* out, float* norms_dev, void* stream);
@@ -350,15 +351,17 @@ typedef struct {
  * be left out), w_pre together with out (no second norm).  width <= EG_NORM_MAX_WIDTH.
  * eg_residual_norm computes residual_out and out.  residual_out may be residual itself.
  *
- * eg_residual_norm_backward takes d_residual_out and d_out (the gradients of r' and o; either
- * may be left out: zero; d_out needs w_pre) and the inputs again (nothing is saved between the
- * two calls), and computes dy, d_residual and -- as sums over the rows -- d_w_post, d_gate,
- * d_scale, d_w_pre.  Each output may be left out; d_w_post, d_gate, d_scale and d_w_pre need
- * their vector.  Outputs are overwritten.  It needs `workspace` of at least
- * eg_residual_norm_workspace(P, width) bytes, 16-byte aligned, free for reuse once the stream
- * has passed the call.  Sums over rows are fp32 in a fixed order.  rows == 0 gives zero sums.
- * Both calls only enqueue work on `stream` of the current device, hold no state and may be
- * recorded into a graph.  Outputs must not overlap inputs or each other except as said. */
+ * eg_residual_norm_backward takes d_residual_out and d_out (the gradients of r' and o; either may
+ * be left out: zero; d_out needs w_pre) and the inputs again (nothing is saved between the two
+ * calls), and computes dy, d_residual and -- as sums over the rows -- d_w_post, d_gate, d_scale,
+ * d_w_pre.  Each output may be left out; d_w_post, d_gate, d_scale and d_w_pre need their vector.
+ * A row with an infinity or a NaN in it has results and gradients that are not finite in general
+ * (also through terms that drop out), the other rows their own.  Where the squares of a row pass
+ * the range of 32 bits, its rms(.) is zero.  Outputs are overwritten.  It needs `workspace` of at
+ * least eg_residual_norm_workspace(P, width) bytes, 16-byte aligned, free for reuse once the stream
+ * has passed the call.  Sums over rows are fp32 in a fixed order.  rows == 0 gives zero sums. Both
+ * calls only enqueue work on `stream` of the current device, hold no state and may be recorded into
+ * a graph.  Outputs must not overlap inputs or each other except as said. */
 #define EG_NORM_MAX_WIDTH 8192
 typedef struct {
     int64_t P, rows, width, dtype;
@@ -383,6 +386,10 @@ int64_t eg_residual_norm_workspace(int64_t P, int64_t width);
  * w_down and its gradient: d_model x d_ff; all of type dtype.  act: silu, gelu (with erf) or relu.
  * Products are summed in fp32.  In the 16-bit types H, dG and dU are rounded to the type (they
  * are operands of the next product), and so are act(G) and U * act'(G), which the backward call reads.
+ * In fp16 any of these above 65504 becomes infinite and below 2^-25 zero, also where y or dx would
+ * lie in range: keep the activations in range and scale dy, or take bf16.  fp32 operands are
+ * multiplied as three bf16 parts; an operand that is infinite or NaN makes the sums it enters what
+ * the formula makes them.
  *
  * eg_feed_forward computes y.  With `saved` (device, 16-byte aligned, at least
  * eg_feed_forward_saved_bytes) it leaves what the backward call reads there.

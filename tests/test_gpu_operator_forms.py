@@ -282,3 +282,16 @@ def test_tensors_that_require_gradients_are_refused():
             with torch.no_grad():
                 assert torch.equal(call(), want)
             leaf.requires_grad_(False)
+
+
+@pytest.mark.parametrize("n", [1, 5, 40, 300])
+def test_values_between_the_products_have_the_range_of_the_type(n):
+    """H passes 65504 in fp16, y would not: infinite in every kernel, and never another number; bf16 has the range."""
+    d, f = 64, 96
+    for dtype, infinite in (("fp16", True), ("bf16", False), ("fp32", False)):
+        full = lambda rows, cols, v: torch.full((1, rows, cols), v, device="cuda").to(N.TYPES[dtype])  # noqa: E731
+        w = (full(f, d, 2.0), full(f, d, 2.0), full(d, f, 2.0 ** -12))
+        x = full(n, d, 4.0)                                  # G = U = 512, H = 2^18, y = 6144
+        y, saved = B.feed_forward(x, *w, save=True)
+        for got in (y, B.feed_forward(x, *w)):
+            assert torch.all(torch.isposinf(got) if infinite else got == 6144.0)
