@@ -632,16 +632,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
 #pragma unroll
                 for (int q = 0; q < ARRAYS; ++q) in[q][z].repack();
             float inv1[ROWS], rr[ROWS], dnr[ROWS], qr[ROWS];       // sums of r'^2, dn r', q r'
-            bool cancels = false, twice[ROWS];
+            bool cancels = false;
+            auto inexact = [](float rr, float size) { return !(rr >= 0.01f * size && size < 3e38f); };
 #pragma unroll
             for (int z = 0; z < ROWS; ++z) {
                 const float* x = v + z * (KP / ROWS);
                 // (rows past the step's last are zeros here and must add zeros to the column sums, also where eps is 0)
-                inv1[z] = mine + z * each >= n ? 0.f : post ? rsqrtf(fmaf(x[0], a.inv_d, a.eps)) : 1.f;
+                inv1[z] = post ? rsqrtf(fmaf(x[0], a.inv_d, a.eps)) : 1.f;
+                if (BWD && n < per && mine + z * each >= n) inv1[z] = 0.f;
                 const float size = fmaf(inv1[z] * inv1[z], x[3], x[1]);
                 rr[z] = fmaf(2.f * inv1[z], x[2], size);
-                twice[z] = !(rr[z] >= 0.01f * size) || size > 3e38f;
-                cancels = cancels || twice[z];
+                cancels = cancels || inexact(rr[z], size);
                 if constexpr (BWD) {
                     dnr[z] = fmaf(inv1[z], x[5], x[4]);
                     qr[z] = fmaf(inv1[z], x[3], x[2]);
@@ -672,7 +673,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
                 row_sums(again);
 #pragma unroll
                 for (int z = 0; z < ROWS; ++z) {
-                    if (!twice[z]) continue;                           // the others' bits do not depend on their neighbours
+                    const float* x = v + z * (KP / ROWS);
+                    if (!inexact(rr[z], fmaf(inv1[z] * inv1[z], x[3], x[1]))) continue;    // others' bits do not depend on it
                     rr[z] = again[z * (KP / ROWS)];
                     dnr[z] = again[z * (KP / ROWS) + 1];
                     qr[z] = again[z * (KP / ROWS) + 2];
@@ -701,7 +703,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_stream(const __grid_consta
                 } else {
                     const bool has_do = a.in[3].p != nullptr;
                     const float x6 = v[z * (KP / ROWS) + 6], x5 = v[z * (KP / ROWS) + 5];
-                    const float i2 = has_do && j < n ? rsqrtf(fmaf(rr[z], a.inv_d, a.eps)) : 0.f;
+                    float i2 = has_do ? rsqrtf(fmaf(rr[z], a.inv_d, a.eps)) : 0.f;
+                    if (n < per && j >= n) i2 = 0.f;
                     const float c3 = has_do ? i2 * i2 * dnr[z] * a.inv_d : 0.f;                    // inv2 * mean(dn * rh)
                     const float c4 = post ? inv1[z] * (x6 + i2 * (x5 - c3 * qr[z])) * a.inv_d : 0.f;
                     const f32x2 inv2 = pack_f2(i2, i2), k3 = pack_f2(-i2 * c3, -i2 * c3);
