@@ -241,6 +241,9 @@ int few_kind(const eg_feed_forward_args* q) {
                         q->d_model * size % 16 == 0 && q->d_ff * size % 16 == 0;
     if (q->dtype != EG_F32 && rows16 && q->rows <= kFewMmaTokens) return 1;
     // k_few_dot reads the weights once for every group of tokens, the tiles copy them once and have longer launches
+    // (the limits are fits to the figures above, no sizes of the chip: what the further groups read again, fp32 from the third on,
+    // 16-bit from the second, is 12.9 and 6.5 MB where k_few_dot is last ahead and 25.9 and 8.7 MB where it first is behind; fp32 at
+    // 8 x 128 x 280 is ahead at 20.6 MB too.  Weights above 134 and 67 MB were not measured and go to the tiles)
     const bool f32 = q->dtype == EG_F32;
     const int64_t each = f32 ? kFewDotTokens32 : kFewDotTokens16, groups = (q->rows + each - 1) / each;
     const double bytes = 3.0 * q->P * q->d_model * q->d_ff * size;

@@ -20,9 +20,10 @@
 // Measured, 4 replicas x 4096 tokens, 2048 x 5504, bf16: gate/up with activation 470 us (1.57 PFLOP/s), down 214-228
 // us (1.62-1.73), activation gradient 290-300 us (1.23-1.27: its epilogue moves four more matrices), the four
 // gradients 1236 us (1.49); a stage of 64 of K takes 540-580 cycles of 512 on the tensor cores; fp32, 8 x 1021 tokens, 1280 x
-// 4992: gradients 2077 us (1.51 PFLOP/s of products of parts).  8 x 512 tokens, 1024
-// x 2816: 45 + 23 + 35 + 95 us, 750-850 cycles a stage: the weights come from memory, and the 160-190 KB of
-// stages in flight do not cover their latency (asking for them earlier into the L2 was slower).
+// 4992: forward 1.51 ms, forward and backward with the copies of both 4.6-4.8 ms (1.2 PFLOP/s of products of parts).  8 x 512
+// tokens, 1024 x 2816: 45 + 23 + 35 + 95 us, 750-850 cycles a stage, with the tensor cores 30-56 % and the memory 33-39 %
+// busy: why a stage takes so long there is not known (160-190 KB of stages look some 3000 cycles ahead, which covers the
+// memory's latency; asking for the weights earlier into the L2 was slower).
 //
 // Warps: 0 and 3 TMA producers (A, B), 1 tensor-core issue, 2 tensor memory, 4..11 epilogue (warp w reads the
 // 32 lanes w % 4 of tensor memory; warps 4..7 take the first half of the columns, 8..11 the other).

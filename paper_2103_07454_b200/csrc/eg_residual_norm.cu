@@ -14,7 +14,7 @@
 // row on chip between its one load and its stores; the backward call recomputes r' from y and r
 // (12 instead of 14 bytes per element in 16-bit types, and nothing is saved by the forward call).
 //
-// Measured: 4 x 8192 rows of 4096 in bf16, forward 179 us (6.0 TB/s), backward 350 us (4.6 TB/s, bound by its
+// Measured: 4 x 8192 rows of 4096 in bf16, forward 173 us (6.2 TB/s), backward 358 us (4.5 TB/s, bound by its
 // instructions: 43 an element, 1.7 a cycle, and 8 warps to hide their latencies); one row of 1024 on 4 replicas 4.0 us.
 //
 // k_norm_stream does both for many rows: one CTA (cluster) per multiprocessor (group of them), rows
