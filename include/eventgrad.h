@@ -419,6 +419,73 @@ int64_t eg_feed_forward_workspace(const eg_feed_forward_args* args, int backward
 eg_status eg_feed_forward(const eg_feed_forward_args* args, void* workspace, int64_t workspace_bytes, void* stream);
 eg_status eg_feed_forward_backward(const eg_feed_forward_args* args, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Rows of a table for tokens, and the table's gradient.  For every replica, with t = tokens[place]:
+ *     out[place] = scale * weight[t],          d_weight[v] = scale * sum of dy[place] over the places with t == v.
+ * tokens: `rows` whole numbers of 4 or 8 bytes (token_bytes) per replica, place j of replica i at
+ * i * token_replica_stride + j * token_stride (in numbers; strides of 0 let replicas share them).  A token
+ * outside of 0 .. vocabulary - 1 is none: its row of `out` is zero, its row of dy is not read.  weight, d_weight:
+ * `vocabulary` x `width` per replica; out, dy: `rows` x `width`; all of type dtype.
+ *
+ * eg_embedding computes out.  eg_embedding_backward overwrites d_weight (rows of tokens that do not come become zero) or, with
+ * `accumulate`, adds to it (a table that is also the output's matrix) and leaves the rows of other tokens alone.  It
+ * sums in fp32, in an order that depends on the tokens only, and needs `workspace` (device, 16-byte aligned) of at least
+ * eg_embedding_workspace(args) bytes, free for reuse once the stream has passed the call.
+ * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded into a
+ * graph.  Outputs must not overlap inputs, and neither rows nor replicas of an output each other (EG_ERR_INVALID). */
+typedef struct {
+    int64_t P, rows, vocabulary, width, dtype, token_bytes, accumulate;
+    double scale;
+    const void* tokens;
+    int64_t token_replica_stride, token_stride;
+    eg_matrix weight, out;          /* forward: in, out */
+    eg_matrix dy, d_weight;         /* backward: in, out */
+} eg_embedding_args;
+int64_t eg_embedding_workspace(const eg_embedding_args* args);
+eg_status eg_embedding(const eg_embedding_args* args, void* stream);
+eg_status eg_embedding_backward(const eg_embedding_args* args, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Attention heads of every replica: element (i, row, head, column) is at data[i * replica_stride + row * row_stride + head *
+ * head_stride + column] (strides in elements, in any order of size; columns are contiguous). */
+typedef struct {
+    void* data;
+    int64_t replica_stride, row_stride, head_stride;
+} eg_heads;
+
+/* The norm of every head of the queries and keys, and their rotation by position, in one pass.  For every head's row x
+ * (`width` values):
+ *     z = x / sqrt(mean(x^2) + eps) * w,        out = z with its first `rotary` values turned in pairs,
+ * pair j of the row at position p by the angle p * base^(-2 j / rotary):
+ *     (a, b) -> (a cos - b sin, a sin + b cos),
+ * where pair j is (j, j + rotary / 2), or (2 j, 2 j + 1) with `interleaved`.  rotary is even; 0: no rotation.
+ * w_q, w_k: `width` per replica, one vector for all heads; not given: z = x.  q, k: `rows` x q_heads (k_heads) x width per replica;
+ * k_heads may be 0.  positions: whole numbers of 4 or 8 bytes (position_bytes) per row, of any size and sign;
+ * NULL: 0, 1, 2, ...  Everything else is of type dtype; sums are fp32, angles are reduced in 64 bits.
+ *
+ * eg_head_norm computes q_out and k_out, which may be q and k themselves.  eg_head_norm_backward takes the gradients of both
+ * (dq_out, dk_out) and the inputs again, and computes dq and dk (which may be dq_out and dk_out themselves) and, as sums over rows
+ * and heads in a fixed order, d_w_q and d_w_k; each of the four may be left out.  rows == 0 gives zero sums.  It
+ * needs `workspace` (device, 16-byte aligned) of at least eg_head_norm_workspace(args) bytes, free for reuse once the stream has passed
+ * the call.  A row with an infinity or a NaN in it has results that are not finite in general, the other rows their own.
+ * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded into a
+ * graph.  Outputs must not overlap inputs or each other except as said; elements of an output that fall on one
+ * another are refused (EG_ERR_INVALID). */
+#define EG_HEAD_MAX_WIDTH 256
+typedef struct {
+    int64_t P, rows, q_heads, k_heads, width, dtype, rotary, interleaved;
+    double base, eps;
+    const void* positions;
+    int64_t position_bytes, position_replica_stride, position_stride;
+    eg_matrix w_q, w_k;             /* in */
+    eg_heads q, k;                  /* in */
+    eg_heads q_out, k_out;          /* out of the forward call */
+    eg_heads dq_out, dk_out;        /* in, backward */
+    eg_heads dq, dk;                /* out of the backward call */
+    eg_matrix d_w_q, d_w_k;         /* out of the backward call */
+} eg_head_norm_args;
+int64_t eg_head_norm_workspace(const eg_head_norm_args* args);
+eg_status eg_head_norm(const eg_head_norm_args* args, void* stream);
+eg_status eg_head_norm_backward(const eg_head_norm_args* args, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* The operators' kernels never trap and their waits are bounded; a wait that runs out sets a word
  * of the current device (one for all its streams and callers) and leaves that call's results
  * undefined.  Synchronises `stream`, returns EG_ERR_TIMEOUT if that happened in any call on the

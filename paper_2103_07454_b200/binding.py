@@ -38,6 +38,7 @@ EXPORTS = [
     "eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace",
     "eg_operator_status", "eg_feed_forward", "eg_feed_forward_backward", "eg_feed_forward_saved_bytes",
     "eg_feed_forward_workspace", "eg_selftest_operator_wait",
+    "eg_embedding", "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward", "eg_head_norm_workspace",
 ]
 STATIC_MAX_TENSORS = 192
 STATIC_MAX_PARTIALS = 524288
@@ -68,7 +69,8 @@ class EventGradError(RuntimeError):
 _lib = None
 _native = None        # csrc/marshal.cpp: the operators' arguments (see _operators)
 _OPERATORS = ("eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace", "eg_feed_forward",
-              "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace")
+              "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace", "eg_embedding",
+              "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward", "eg_head_norm_workspace")
 
 
 def load_library() -> C.CDLL:
@@ -570,6 +572,71 @@ def feed_forward_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tenso
         r = native.feed_forward_backward(x, w_gate, w_up, w_down, _activation(activation), dy, saved, d_weights)
     if r.__class__ is int:
         _check(_lib, r, None, "eg_feed_forward_backward")
+    return r
+
+
+def embedding(tokens: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``eg_embedding``: ``scale * weight[token]`` of every replica, ``[P, rows, width]``.
+
+    ``tokens``: ``[P, rows]`` int32 or int64 of any strides; one outside of the table (-1, say) is none, and its row is zero.
+    ``weight``: ``[P, vocabulary, width]`` (a view of a parameter buffer, say)."""
+    native = _native or _operators()
+    with _on(stream):
+        r = native.embedding(tokens, weight, scale, out)
+    if r.__class__ is int:
+        _check(_lib, r, None, "eg_embedding")
+    return r
+
+
+def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, *, vocabulary: Optional[int] = None, scale: float = 1.0,
+                       d_weight: Optional[torch.Tensor] = None, accumulate: bool = False,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``eg_embedding_backward``: the gradient of the table, ``scale`` times the sum of ``dy`` over the places of every token.
+
+    It goes to ``d_weight`` (``[P, vocabulary, width]``, a view of a gradient buffer in the step's layout, say; default: a new
+    tensor of ``vocabulary`` rows), whose other rows become zero; with ``accumulate`` it is added to what ``d_weight`` holds."""
+    native = _native or _operators()
+    with _on(stream):
+        r = native.embedding_backward(dy, tokens, vocabulary, scale, d_weight, bool(accumulate))
+    if r.__class__ is int:
+        _check(_lib, r, None, "eg_embedding_backward")
+    return r
+
+
+def head_norm(q: torch.Tensor, k: Optional[torch.Tensor], *, w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None,
+              positions: Optional[torch.Tensor] = None, rotary: Optional[int] = None, base: float = 10000.0, interleaved: bool = False,
+              eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None):
+    """``eg_head_norm``: the norm of every head of queries and keys and their rotation by position.  Returns ``(q', k')``.
+
+    ``q``, ``k``: ``[P, rows, heads, width]`` (parts of one projection, say; ``k`` may be None); ``w_q``, ``w_k``: ``[P, width]``,
+    None: no norm.  ``positions``: ``[P, rows]`` int32 or int64, None: 0, 1, 2, ...  ``rotary``: leading values of a head that are
+    rotated (default: all pairs; 0: none), paired as halves or, ``interleaved``, as neighbours.  ``q_out``, ``k_out`` may be
+    ``q`` and ``k`` themselves."""
+    native = _native or _operators()
+    with _on(stream):
+        r = native.head_norm(q, k, w_q, w_k, positions, rotary, base, bool(interleaved), eps, q_out, k_out)
+    if r.__class__ is int:
+        _check(_lib, r, None, "eg_head_norm")
+    return r
+
+
+def head_norm_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor], *,
+                       w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                       rotary: Optional[int] = None, base: float = 10000.0, interleaved: bool = False, eps: float = 1e-6,
+                       dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None, d_weights: Optional[Sequence] = None,
+                       stream: Optional[torch.cuda.Stream] = None):
+    """``eg_head_norm_backward``: ``(dq, dk, (d_w_q, d_w_k))`` from the gradients of ``head_norm``'s results and its inputs.
+
+    ``dq``, ``dk`` receive the first two (parts of the projection's gradient, say, or ``dq_out`` and ``dk_out`` themselves),
+    ``d_weights`` the last two (two ``[P, width]`` tensors; None: not wanted); default: new tensors."""
+    native = _native or _operators()
+    d_weights = _some(d_weights, 2, "head_norm_backward")
+    with _on(stream):
+        r = native.head_norm_backward(q, k, w_q, w_k, positions, rotary, base, bool(interleaved), eps, dq_out, dk_out, dq, dk, d_weights)
+    if r.__class__ is int:
+        _check(_lib, r, None, "eg_head_norm_backward")
     return r
 
 

@@ -1,0 +1,474 @@
+// Embedding of tokens (eg_embedding) and its gradient (eg_embedding_backward).
+//
+//   forward   y[t] = scale * W[token t]                      (a token outside of the table: zeros)
+//   backward  dW[v] = scale * sum of dy over the places t of token v   (+ what dW holds, where it is to be added to)
+//
+// Bound by memory: the forward call moves a row in and a row out for every place; the gradient reads every row of dy
+// once and writes the whole table, most of whose rows are zero (32000 rows and 1024 places on each of 8 replicas: 525 of
+// 542 MB).
+//
+// The gradient sorts the places by token, so that every row of dW is one run of places, summed in the order of the places:
+// no atomics on values, the same bits every time.
+//   1. k_embed_sort: one CTA per range of the table's rows reads all tokens of its replica twice.  It counts the tokens
+//      below its range (which is where its part of the sorted list begins) and each of its own, then puts the places into
+//      the list.  The tokens come out of the L2 and nobody waits for another CTA; a sort in several passes would read them
+//      about as often and launch five kernels.  It also writes the zeros of the rows without a place.
+//   2. k_embed_sum: a warp adds up one chunk of the list over some columns.  Chunks have equal length, however often a token
+//      comes; a run that crosses chunks leaves a partial sum in each.
+//   3. k_embed_join: adds the partial sums of such runs, in order.
+#include "eg_ops.cuh"
+
+namespace eg {
+namespace {
+
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+constexpr int kRangeMax = 512;             // rows of the table that a sorting CTA owns, at most
+constexpr int kMaxVectors = 4;             // 16-byte vectors of a row that a warp's lane holds (forward)
+
+struct Rows {
+    void* p;
+    long long rep, row;                    // strides in elements
+};
+
+struct EmbedArgs {
+    int P;
+    long long n, V;
+    int d;
+    float scale;
+    const void* tokens;
+    long long token_rep, token_step;
+    int wide;                              // tokens of 64 bits
+    Rows weight, out;                      // forward: table and y; backward: dy and the table's gradient
+    int accumulate;
+    // backward
+    int range;                             // rows of the table per sorting CTA
+    int chunk, chunks;                     // places of a chunk; chunks of a replica
+    int pitch;                             // columns of a partial sum, up to whole vectors
+    int *order, *key, *count;              // [P][n] places and tokens of the sorted list, [P] its length
+    float* partial;                        // [P][chunks][2][pitch]: of a run from the chunk before, of one into the next
+};
+
+// The token at place t, -1 where it is none of the table's.
+__device__ __forceinline__ int token_at(const EmbedArgs& a, int i, long long t) {
+    const long long at = i * a.token_rep + t * a.token_step;
+    const long long v = a.wide ? __ldg(static_cast<const long long*>(a.tokens) + at) : (long long)__ldg(static_cast<const int*>(a.tokens) + at);
+    return v >= 0 && v < a.V ? (int)v : -1;
+}
+template <typename T> __device__ __forceinline__ T* row_of(const Rows& m, int i, long long t) {
+    return static_cast<T*>(m.p) + (long long)i * m.rep + t * m.row;
+}
+
+// ----------------------------------------------------------------------------------- forward
+// A warp takes 32 * U vectors of one row, all its loads ahead of its stores.
+template <typename T, int VEC, int U>
+__global__ void __launch_bounds__(256) k_embed(const __grid_constant__ EmbedArgs a, int slices) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), rows = a.P * a.n;
+    if (unit >= rows * slices) return;
+    const long long line = unit / slices;
+    const int i = (int)(line / a.n);
+    const long long t = line - i * a.n;
+    const int c0 = (int)(unit - line * slices) * 32 * U * VEC, token = token_at(a, i, t);
+    float v[U][VEC];
+    const T* from = row_of<T>(a.weight, i, token < 0 ? 0 : token);
+    T* to = row_of<T>(a.out, i, t);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c = c0 + (u * 32 + lane) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[u][e] = 0.f;
+        if (c < a.d && token >= 0) load_vec<T, VEC>(from + c, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c = c0 + (u * 32 + lane) * VEC;
+        if (c >= a.d) continue;
+        if (token >= 0) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[u][e] *= a.scale;
+        }
+        store_vec<T, VEC>(to + c, v[u]);
+    }
+}
+
+// ----------------------------------------------------------------------------------- backward
+// Sum over the CTA, valid in all threads; `red` holds kSortWarps values.
+__device__ __forceinline__ int block_total(int v, int* red) {
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) s += red[w];
+    return s;
+}
+
+template <typename T, int VEC> __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_constant__ EmbedArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ int s_at[kSortWarps][kRangeMax];          // first how often, then where to
+    __shared__ int s_sum[kRangeMax], s_red[kSortWarps];
+    const int i = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long first = (long long)blockIdx.x * a.range;
+    const int mine = (int)(a.V - first < a.range ? a.V - first : a.range);
+    for (int q = threadIdx.x; q < kSortWarps * kRangeMax; q += kSortThreads) (&s_at[0][0])[q] = 0;
+    __syncthreads();
+    // every warp takes its own stretch of the places, 32 at a time, four of them on their way at once
+    const long long each = ((a.n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
+    const long long t0 = warp * each, t1 = t0 + each < a.n ? t0 + each : a.n;
+    int below = 0;
+    for (long long t = t0; t < t1; t += 128) {
+        int v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const long long at = v[u] - first;
+            below += v[u] >= 0 && at < 0;
+            if (v[u] >= 0 && at >= 0 && at < mine) atomicAdd(&s_at[warp][at], 1);
+        }
+    }
+    const int base = block_total(below, s_red);          // (its barriers also end the counting)
+    // where the places of row r go that warp w finds: behind those of the rows before and of the warps before
+    const int r = threadIdx.x;
+    int total = 0;
+    if (r < mine) {
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) total += s_at[w][r];
+    }
+    int upto = total;                                    // sum over the rows up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    __syncthreads();
+    if (lane == 31) s_red[warp] = upto;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+        before += w < warp ? s_red[w] : 0;
+        all += s_red[w];
+    }
+    if (r < mine) {
+        s_sum[r] = total;
+        int at = base + before + upto - total;
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            const int x = s_at[w][r];
+            s_at[w][r] = at;
+            at += x;
+        }
+    }
+    if (threadIdx.x == 0 && first + mine == a.V) a.count[i] = base + all;
+    __syncthreads();
+    if (all > 0) {
+        int *order = a.order + i * a.n, *key = a.key + i * a.n;
+        for (long long t = t0; t < t1; t += 128) {
+            int v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const long long rel = v[u] - first;
+                const bool in = v[u] >= 0 && rel >= 0 && rel < mine;
+                if (!__any_sync(0xffffffffu, in)) continue;
+                const unsigned same = __match_any_sync(0xffffffffu, in ? v[u] : -1);
+                const int rank = __popc(same & ((1u << lane) - 1));
+                int at = 0;
+                if (in) at = s_at[warp][rel];
+                __syncwarp();
+                if (in) {
+                    order[at + rank] = (int)(t + u * 32 + lane);
+                    key[at + rank] = v[u];
+                    if (rank == 0) s_at[warp][rel] = at + __popc(same);
+                }
+                __syncwarp();
+            }
+        }
+    }
+    if (a.accumulate) return;
+    const float zero[VEC] = {};
+    for (int q = warp; q < mine; q += kSortWarps) {
+        if (s_sum[q] != 0) continue;
+        T* to = row_of<T>(a.out, i, first + q);
+        for (int c = lane * VEC; c < a.d; c += 32 * VEC) store_vec<T, VEC>(to + c, zero);
+    }
+}
+
+// Adds to or writes a row's columns.
+template <typename T, int VEC> __device__ __forceinline__ void finish(const EmbedArgs& a, int i, int token, int c, const float* sum) {
+    T* to = row_of<T>(a.out, i, token) + c;
+    float v[VEC];
+    if (a.accumulate) load_vec<T, VEC>(to, v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = a.accumulate ? fmaf(a.scale, sum[e], v[e]) : a.scale * sum[e];
+    store_vec<T, VEC>(to, v);
+}
+
+// A warp: one chunk of the sorted list, 32 * U vectors of columns.
+template <typename T, int VEC, int U> __global__ void __launch_bounds__(256) k_embed_sum(const __grid_constant__ EmbedArgs a, int slices) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    constexpr int AHEAD = 4;                             // rows on their way at once
+    const int lane = threadIdx.x & 31, i = blockIdx.y;
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long chunk = unit / slices;
+    if (chunk >= a.chunks) return;
+    const int c0 = (int)(unit - chunk * slices) * 32 * U * VEC + lane * VEC, count = a.count[i];
+    const long long first = chunk * a.chunk;
+    if (first >= count) return;
+    const int n = count - first < a.chunk ? (int)(count - first) : a.chunk;
+    const int *order = a.order + i * a.n + first, *key = a.key + i * a.n + first;
+    const bool from_before = first > 0 && key[-1] == key[0], into_next = first + n < count && key[n] == key[n - 1];
+    float* partial = a.partial + ((long long)i * a.chunks + chunk) * 2 * a.pitch;
+    float sum[U][VEC];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[u][e] = 0.f;
+    bool at_first = true;                                // in the chunk's first run
+    for (int j0 = 0; j0 < n; j0 += 32) {
+        const int m = n - j0 < 32 ? n - j0 : 32;
+        const int place = lane < m ? order[j0 + lane] : 0, token = lane < m ? key[j0 + lane] : -1;
+        const int after = j0 + lane + 1 < n && lane < m ? key[j0 + lane + 1] : -1;
+        for (int j = 0; j < m; j += AHEAD) {
+            float v[AHEAD][U][VEC];
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h) {
+                const T* from = row_of<T>(a.weight, i, __shfl_sync(0xffffffffu, place, (j + h) & 31)) + c0;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (j + h < m && c0 + u * 32 * VEC < a.d) load_vec<T, VEC>(from + u * 32 * VEC, v[h][u]);
+            }
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h) {
+                if (j + h >= m) break;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[u][e] += v[h][u][e];
+                const int here = __shfl_sync(0xffffffffu, token, j + h), next = __shfl_sync(0xffffffffu, after, j + h);
+                if (here == next) continue;
+                // the end of a run, or of the chunk
+                const bool last = j0 + j + h + 1 == n;
+                const int slot = at_first && from_before ? 0 : last && into_next ? 1 : -1;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int c = c0 + u * 32 * VEC;
+                    if (c < a.d) {
+                        if (slot < 0) {
+                            finish<T, VEC>(a, i, here, c, sum[u]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) partial[slot * a.pitch + c + e] = sum[u][e];
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[u][e] = 0.f;
+                }
+                at_first = false;
+            }
+        }
+    }
+}
+
+// A warp: the run that begins in one chunk and goes on into the next, 32 vectors of columns.
+template <typename T, int VEC> __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ EmbedArgs a, int slices) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, i = blockIdx.y;
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long chunk = unit / slices;
+    if (chunk >= a.chunks) return;
+    const int c = ((int)(unit - chunk * slices) * 32 + lane) * VEC, count = a.count[i];
+    const long long first = chunk * a.chunk, end = first + a.chunk;
+    if (end >= count) return;
+    const int* key = a.key + i * a.n;
+    const int token = key[end - 1];
+    if (key[end] != token || (first > 0 && key[first - 1] == token)) return;
+    // chunks that the run goes on through: those that begin with its token
+    long long more = 1;
+    for (long long q = chunk + 1;; q += 32) {
+        const long long begin = (q + lane) * a.chunk;
+        const unsigned on = __ballot_sync(0xffffffffu, begin < count && key[begin < count ? begin : 0] == token);
+        if (on != 0xffffffffu) {
+            more = q - chunk - 1 + __popc(on);           // (sorted: the ones with the token come first)
+            break;
+        }
+    }
+    if (c >= a.d) return;
+    const float* partial = a.partial + ((long long)i * a.chunks + chunk) * 2 * a.pitch + c;
+    float sum[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum[e] = partial[a.pitch + e];
+#pragma unroll 8
+    for (long long q = 1; q <= more; ++q) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] += partial[q * 2 * a.pitch + e];
+    }
+    finish<T, VEC>(a, i, token, c, sum);
+}
+
+// ----------------------------------------------------------------------------------- host
+Rows rows(const eg_matrix& m) { return Rows{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
+
+bool whole_vectors(const eg_matrix& m, int64_t P, int64_t rows, size_t size) {
+    return aligned16(m.data) && (P <= 1 || m.replica_stride * (int64_t)size % 16 == 0) && (rows <= 1 || m.row_stride * (int64_t)size % 16 == 0);
+}
+
+// written: neither the rows of a replica nor the replicas fall on one another; the replicas lie one after the other, or take
+// turns row by row.
+bool usable(const eg_matrix& m, int64_t P, int64_t rows, int64_t cols, size_t size, bool written) {
+    if (!m.data || (uintptr_t)m.data % size || m.row_stride < 0 || m.replica_stride < 0 || m.row_stride >= (1ll << 36) ||
+        m.replica_stride >= (1ll << 42))
+        return false;
+    if (!written) return true;
+    if (rows > 1 && m.row_stride < cols) return false;
+    if (P > 1) {
+        const int64_t rep = m.replica_stride, row = rows > 1 ? m.row_stride : 0;
+        if (!(rep >= (rows - 1) * row + cols || (rep >= cols && row >= (P - 1) * rep + cols))) return false;
+    }
+    return true;
+}
+
+bool valid(const eg_embedding_args* q, bool backward) {
+    if (!q) return false;
+    if (q->dtype != EG_F32 && q->dtype != EG_BF16 && q->dtype != EG_F16) return false;
+    if (q->P < 1 || q->P > 65535 || q->rows < 0 || q->rows > (1ll << 30) || q->vocabulary < 1 || q->vocabulary > (1ll << 30) ||
+        q->width < 1 || q->width > (1ll << 24))
+        return false;
+    if (!(q->scale >= -3e38 && q->scale <= 3e38)) return false;
+    const size_t size = q->dtype == EG_F32 ? 4 : 2;
+    if (q->rows > 0) {
+        if (q->token_bytes != 4 && q->token_bytes != 8) return false;
+        if (!q->tokens || (uintptr_t)q->tokens % (size_t)q->token_bytes || q->token_replica_stride < 0 || q->token_stride < 0 ||
+            q->token_replica_stride >= (1ll << 42) || q->token_stride >= (1ll << 36))
+            return false;
+        if (!usable(backward ? q->dy : q->out, q->P, q->rows, q->width, size, !backward)) return false;
+    }
+    if (!usable(backward ? q->d_weight : q->weight, q->P, q->vocabulary, q->width, size, backward)) return false;
+    return true;
+}
+
+// Chunks of 32 places; of more where a run over all places would have more than 1024 partial sums to join.
+int chunk_of(int64_t n) {
+    int c = 32;
+    while (c * 1024ll < n) c *= 2;
+    return c;
+}
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+struct Layout {
+    int64_t order, key, count, partial, bytes;
+    int chunk, chunks, pitch;
+};
+Layout layout(const eg_embedding_args* q) {
+    Layout l;
+    const int64_t n = q->rows > 0 ? q->rows : 1;
+    l.chunk = chunk_of(n);
+    l.chunks = (int)((n + l.chunk - 1) / l.chunk);
+    l.pitch = (int)((q->width + 7) / 8 * 8);
+    l.order = 0;
+    l.key = up16(4 * q->P * n);
+    l.count = l.key + up16(4 * q->P * n);
+    l.partial = l.count + up16(4 * q->P);
+    l.bytes = l.partial + q->P * (int64_t)l.chunks * 2 * l.pitch * 4;
+    return l;
+}
+
+void fill(EmbedArgs* a, const eg_embedding_args* q, bool backward) {
+    *a = EmbedArgs{};
+    a->P = (int)q->P; a->n = q->rows; a->V = q->vocabulary; a->d = (int)q->width;
+    a->scale = (float)q->scale;
+    a->tokens = q->tokens; a->token_rep = q->token_replica_stride; a->token_step = q->token_stride;
+    a->wide = q->token_bytes == 8;
+    a->weight = rows(backward ? q->dy : q->weight);
+    a->out = rows(backward ? q->d_weight : q->out);
+    a->accumulate = q->accumulate != 0;
+}
+
+template <typename T, int VEC> cudaError_t forward(const EmbedArgs& a, cudaStream_t stream) {
+    auto launch = [&](auto kernel, int U) {
+        const int per = 32 * U * VEC, slices = (a.d + per - 1) / per;
+        const long long blocks = (a.P * a.n * slices + 7) / 8;
+        if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+        return launch_after(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a, slices);
+    };
+    if (a.d <= 32 * VEC) return launch(k_embed<T, VEC, 1>, 1);
+    if (a.d <= 64 * VEC) return launch(k_embed<T, VEC, 2>, 2);
+    return launch(k_embed<T, VEC, kMaxVectors>, kMaxVectors);
+}
+
+template <typename T, int VEC> cudaError_t backward(const EmbedArgs& a, cudaStream_t stream) {
+    const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
+    cudaError_t e = launch_after(k_embed_sort<T, VEC>, dim3(ranges, a.P), dim3(kSortThreads), 0, stream, a);
+    if (e != cudaSuccess || a.n == 0) return e;
+    auto blocks = [&](int slices) { return (unsigned)(((long long)a.chunks * slices + 7) / 8); };
+    constexpr int U = VEC > 1 ? 2 : 4;
+    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC), narrow = (a.d + 32 * VEC - 1) / (32 * VEC);
+    e = launch_after(k_embed_sum<T, VEC, U>, dim3(blocks(slices), a.P), dim3(256), 0, stream, a, slices);
+    if (e != cudaSuccess || a.chunks == 1) return e;
+    return launch_after(k_embed_join<T, VEC>, dim3(blocks(narrow), a.P), dim3(256), 0, stream, a, narrow);
+}
+
+}  // namespace
+}  // namespace eg
+
+using namespace eg;
+
+extern "C" {
+
+eg_status eg_embedding(const eg_embedding_args* q, void* stream_v) {
+    if (!valid(q, false)) return EG_ERR_INVALID;
+    if (q->rows == 0) return EG_OK;
+    EmbedArgs a;
+    fill(&a, q, false);
+    const size_t size = q->dtype == EG_F32 ? 4 : 2;
+    const bool vec = q->width * size % 16 == 0 && whole_vectors(q->weight, q->P, q->vocabulary, size) && whole_vectors(q->out, q->P, q->rows, size);
+    cudaStream_t s = static_cast<cudaStream_t>(stream_v);
+    cudaError_t e;
+    if (q->dtype == EG_F32) e = vec ? forward<float, 4>(a, s) : forward<float, 1>(a, s);
+    else if (q->dtype == EG_BF16) e = vec ? forward<__nv_bfloat16, 8>(a, s) : forward<__nv_bfloat16, 1>(a, s);
+    else e = vec ? forward<__half, 8>(a, s) : forward<__half, 1>(a, s);
+    return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
+}
+
+int64_t eg_embedding_workspace(const eg_embedding_args* q) {
+    if (!valid(q, true)) return 0;
+    return layout(q).bytes;
+}
+
+eg_status eg_embedding_backward(const eg_embedding_args* q, void* workspace, int64_t workspace_bytes, void* stream_v) {
+    if (!valid(q, true)) return EG_ERR_INVALID;
+    if (q->rows == 0 && q->accumulate) return EG_OK;
+    const Layout l = layout(q);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < l.bytes) return EG_ERR_INVALID;
+    const int sms = sm_count();
+    if (sms < 1) return EG_ERR_CUDA;
+    EmbedArgs a;
+    fill(&a, q, true);
+    char* w = static_cast<char*>(workspace);
+    a.order = reinterpret_cast<int*>(w + l.order);
+    a.key = reinterpret_cast<int*>(w + l.key);
+    a.count = reinterpret_cast<int*>(w + l.count);
+    a.partial = reinterpret_cast<float*>(w + l.partial);
+    a.chunk = l.chunk; a.chunks = l.chunks; a.pitch = l.pitch;
+    // ranges long enough that the tokens are not read more often than needed, short enough that every multiprocessor has some
+    a.range = kRangeMax;
+    while (a.range > 64 && a.P * ((a.V + a.range - 1) / a.range) < 4ll * sms) a.range /= 2;
+    const size_t size = q->dtype == EG_F32 ? 4 : 2;
+    const bool vec = q->width * size % 16 == 0 && (q->rows == 0 || whole_vectors(q->dy, q->P, q->rows, size)) &&
+                     whole_vectors(q->d_weight, q->P, q->vocabulary, size);
+    cudaStream_t s = static_cast<cudaStream_t>(stream_v);
+    cudaError_t e;
+    if (q->dtype == EG_F32) e = vec ? backward<float, 4>(a, s) : backward<float, 1>(a, s);
+    else if (q->dtype == EG_BF16) e = vec ? backward<__nv_bfloat16, 8>(a, s) : backward<__nv_bfloat16, 1>(a, s);
+    else e = vec ? backward<__half, 8>(a, s) : backward<__half, 1>(a, s);
+    return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -25,6 +25,12 @@ struct Library {
     decltype(&eg_feed_forward_backward) ffn_backward;
     decltype(&eg_feed_forward_saved_bytes) ffn_saved;
     decltype(&eg_feed_forward_workspace) ffn_workspace;
+    decltype(&eg_embedding) embed;
+    decltype(&eg_embedding_backward) embed_backward;
+    decltype(&eg_embedding_workspace) embed_workspace;
+    decltype(&eg_head_norm) heads;
+    decltype(&eg_head_norm_backward) heads_backward;
+    decltype(&eg_head_norm_workspace) heads_workspace;
 } lib;
 PyObject* error_class = nullptr;
 
@@ -309,6 +315,179 @@ PyObject* feed_forward_backward(PyObject* const* a) {
     return tuple(wrap(dx), a[7] != Py_None ? same(a[7]) : tuple(wrap(fresh[0]), wrap(fresh[1]), wrap(fresh[2])));
 }
 
+// ------------------------------------------------------------------------------- tokens
+// [P, rows] whole numbers on the device, of any strides: (pointer, bytes, replica stride, stride).
+struct Numbers {
+    const void* data;
+    int64_t bytes, replica_stride, stride;
+};
+Numbers numbers(const at::Tensor& t, int64_t P, int64_t rows, const Kind& k, const char* what) {
+    if (t.dim() != 2 || t.size(0) != P || t.size(1) != rows || (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) || t.device() != k.device)
+        throw Refused{std::string(what) + ": expected [" + std::to_string(P) + ", " + std::to_string(rows) + "] int32 or int64 on " + k.device.str()};
+    return Numbers{t.data_ptr(), t.scalar_type() == at::kInt ? 4 : 8, t.stride(0), t.stride(1)};
+}
+
+void* stream_of(const Kind& k) { return c10::cuda::getCurrentCUDAStream(k.device.index()).stream(); }
+
+void set_tokens(eg_embedding_args& q, const at::Tensor& tokens, const Kind& k, const char* what) {
+    if (tokens.dim() != 2) throw Refused{std::string(what) + ": tokens must be [P, rows]"};
+    q.P = tokens.size(0);
+    q.rows = tokens.size(1);
+    const Numbers n = numbers(tokens, q.P, q.rows, k, "tokens");
+    q.tokens = n.data; q.token_bytes = n.bytes; q.token_replica_stride = n.replica_stride; q.token_stride = n.stride;
+}
+
+// tokens, weight, scale, out
+PyObject* embedding(PyObject* const* a) {
+    const at::Tensor &tokens = tensor(a[0], "tokens"), &w = on_device(tensor(a[1], "weight"));
+    if (w.dim() != 3 || type_of(w) < 0) throw Refused{"embedding: weight must be [P, vocabulary, width] fp32, bf16 or fp16"};
+    const Kind k{w.scalar_type(), w.device()};
+    const c10::cuda::CUDAGuard guard(k.device);
+    eg_embedding_args q{};
+    set_tokens(q, tokens, k, "embedding");
+    q.vocabulary = w.size(1); q.width = w.size(2); q.dtype = type_of(w);
+    q.scale = number(a[2]);
+    const int64_t table[] = {q.P, q.vocabulary, q.width}, sizes[] = {q.P, q.rows, q.width};
+    q.weight = given(a[1], table, k, "weight");
+    at::Tensor out;
+    q.out = a[3] != Py_None ? given(a[3], sizes, k, "out") : made(out = k.empty(sizes));
+    void* s = stream_of(k);
+    const eg_status st = unlocked([&] { return lib.embed(&q, s); });
+    if (st != EG_OK) return PyLong_FromLong(st);
+    return out.defined() ? wrap(out) : same(a[3]);
+}
+
+// dy, tokens, vocabulary, scale, d_weight, accumulate
+PyObject* embedding_backward(PyObject* const* a) {
+    const at::Tensor &dy = on_device(tensor(a[0], "dy")), &tokens = tensor(a[1], "tokens");
+    if (dy.dim() != 3 || type_of(dy) < 0) throw Refused{"embedding_backward: dy must be [P, rows, width] fp32, bf16 or fp16"};
+    const Kind k{dy.scalar_type(), dy.device()};
+    const c10::cuda::CUDAGuard guard(k.device);
+    eg_embedding_args q{};
+    set_tokens(q, tokens, k, "embedding_backward");
+    q.width = dy.size(2); q.dtype = type_of(dy);
+    q.scale = number(a[3]);
+    q.accumulate = a[5] == Py_True;
+    const int64_t sizes[] = {q.P, q.rows, q.width};
+    q.dy = given(a[0], sizes, k, "dy");
+    at::Tensor fresh;
+    if (a[4] != Py_None) {
+        const at::Tensor& d = tensor(a[4], "d_weight");
+        if (d.dim() != 3 || (a[2] != Py_None && d.size(1) != integer(a[2])))
+            throw Refused{"embedding_backward: d_weight must be [P, vocabulary, width]"};
+        q.vocabulary = d.size(1);
+        const int64_t table[] = {q.P, q.vocabulary, q.width};
+        q.d_weight = given(a[4], table, k, "d_weight");
+    } else {
+        if (q.accumulate) throw Refused{"embedding_backward: accumulate adds to a given d_weight"};
+        if (a[2] == Py_None) throw Refused{"embedding_backward: give d_weight or the vocabulary's size"};
+        q.vocabulary = integer(a[2]);
+        if (q.vocabulary < 1) throw Refused{"embedding_backward: the vocabulary has at least one row"};
+        const int64_t table[] = {q.P, q.vocabulary, q.width};
+        q.d_weight = made(fresh = k.empty(table));
+    }
+    const int64_t bytes = lib.embed_workspace(&q);
+    const at::Tensor workspace = k.bytes(bytes);
+    void *w = workspace.data_ptr(), *s = stream_of(k);
+    const eg_status st = unlocked([&] { return lib.embed_backward(&q, w, bytes, s); });
+    if (st != EG_OK) return PyLong_FromLong(st);
+    return fresh.defined() ? wrap(fresh) : same(a[4]);
+}
+
+// ------------------------------------------------------------------------------- heads
+eg_heads given_heads(PyObject* o, at::IntArrayRef sizes, const Kind& k, const char* what) {
+    if (o == Py_None) return eg_heads{};
+    const at::Tensor& t = tensor(o, what);
+    if (t.sizes() != sizes || t.scalar_type() != k.type || t.device() != k.device) {
+        std::string s = std::string(what) + ": expected [";
+        for (int64_t n : sizes) s += std::to_string(n) + ", ";
+        throw Refused{s + "] " + c10::toString(k.type) + " on " + k.device.str()};
+    }
+    plain(t, what);
+    if (t.stride(3) != 1 && sizes[3] > 1) throw Refused{std::string(what) + ": the last dimension must be contiguous"};
+    return eg_heads{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+}
+eg_heads made_heads(const at::Tensor& t) { return eg_heads{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)}; }
+
+struct HeadsCall {
+    const at::Tensor& q_;
+    Kind k;
+    c10::cuda::CUDAGuard guard;
+    eg_head_norm_args q{};
+    int64_t q_sizes[4], k_sizes[4], vec[2];
+    bool keys;
+
+    // q, k, w_q, w_k, positions, rotary, base, interleaved, eps
+    HeadsCall(PyObject* const* a, const char* what) : q_(on_device(shaped(a, what))), k{q_.scalar_type(), q_.device()}, guard(k.device) {
+        keys = a[1] != Py_None;
+        q.P = q_.size(0); q.rows = q_.size(1); q.q_heads = q_.size(2); q.width = q_.size(3);
+        q.k_heads = keys ? THPVariable_Unpack(a[1]).size(2) : 0;
+        q.dtype = type_of(q_);
+        const int64_t qs[] = {q.P, q.rows, q.q_heads, q.width}, ks[] = {q.P, q.rows, q.k_heads, q.width};
+        std::memcpy(q_sizes, qs, sizeof qs);
+        std::memcpy(k_sizes, ks, sizeof ks);
+        vec[0] = q.P; vec[1] = q.width;
+        q.q = given_heads(a[0], q_sizes, k, "q");
+        q.k = given_heads(a[1], k_sizes, k, "k");
+        q.w_q = given(a[2], vec, k, "w_q");
+        q.w_k = given(a[3], vec, k, "w_k");
+        if (a[4] != Py_None) {
+            const Numbers n = numbers(tensor(a[4], "positions"), q.P, q.rows, k, "positions");
+            q.positions = n.data; q.position_bytes = n.bytes; q.position_replica_stride = n.replica_stride; q.position_stride = n.stride;
+        }
+        q.rotary = a[5] == Py_None ? q.width / 2 * 2 : integer(a[5]);
+        q.base = number(a[6]);
+        q.interleaved = a[7] == Py_True;
+        q.eps = number(a[8]);
+    }
+    static const at::Tensor& shaped(PyObject* const* a, const char* what) {
+        const at::Tensor& t = tensor(a[0], "q");
+        if (t.dim() != 4 || type_of(t) < 0) throw Refused{std::string(what) + ": q must be [P, rows, heads, width] fp32, bf16 or fp16"};
+        if (a[1] != Py_None && tensor(a[1], "k").dim() != 4) throw Refused{std::string(what) + ": k must be [P, rows, heads, width]"};
+        return t;
+    }
+};
+
+// q, k, w_q, w_k, positions, rotary, base, interleaved, eps, q_out, k_out
+PyObject* head_norm(PyObject* const* a) {
+    HeadsCall c(a, "head_norm");
+    if (!c.keys && a[10] != Py_None) throw Refused{"head_norm: k_out without k"};
+    at::Tensor q_out, k_out;
+    c.q.q_out = a[9] != Py_None ? given_heads(a[9], c.q_sizes, c.k, "q_out") : made_heads(q_out = c.k.empty(c.q_sizes));
+    if (a[10] != Py_None) c.q.k_out = given_heads(a[10], c.k_sizes, c.k, "k_out");
+    else if (c.keys) c.q.k_out = made_heads(k_out = c.k.empty(c.k_sizes));
+    void* s = stream_of(c.k);
+    const eg_status st = unlocked([&] { return lib.heads(&c.q, s); });
+    if (st != EG_OK) return PyLong_FromLong(st);
+    return tuple(q_out.defined() ? wrap(q_out) : same(a[9]), k_out.defined() ? wrap(k_out) : same(a[10]));
+}
+
+// q, k, w_q, w_k, positions, rotary, base, interleaved, eps, dq_out, dk_out, dq, dk, d_weights (tuple of two, or None)
+PyObject* head_norm_backward(PyObject* const* a) {
+    HeadsCall c(a, "head_norm_backward");
+    if (!c.keys && (a[10] != Py_None || a[12] != Py_None)) throw Refused{"head_norm_backward: dk_out or dk without k"};
+    if (a[9] == Py_None || (c.keys && a[10] == Py_None)) throw Refused{"head_norm_backward: the gradients of both outputs are needed"};
+    c.q.dq_out = given_heads(a[9], c.q_sizes, c.k, "dq_out");
+    c.q.dk_out = given_heads(a[10], c.k_sizes, c.k, "dk_out");
+    at::Tensor dq, dk, fresh[2];
+    c.q.dq = a[11] != Py_None ? given_heads(a[11], c.q_sizes, c.k, "dq") : made_heads(dq = c.k.empty(c.q_sizes));
+    if (a[12] != Py_None) c.q.dk = given_heads(a[12], c.k_sizes, c.k, "dk");
+    else if (c.keys) c.q.dk = made_heads(dk = c.k.empty(c.k_sizes));
+    eg_matrix* to[] = {&c.q.d_w_q, &c.q.d_w_k};
+    static const char* const names[] = {"d_w_q", "d_w_k"};
+    for (int i = 0; i < 2; ++i) {
+        if (a[13] != Py_None) *to[i] = given(PyTuple_GET_ITEM(a[13], i), c.vec, c.k, names[i]);
+        else if (a[2 + i] != Py_None) *to[i] = made(fresh[i] = c.k.empty(c.vec));
+    }
+    const int64_t bytes = lib.heads_workspace(&c.q);
+    const at::Tensor workspace = c.k.bytes(bytes);
+    void *w = workspace.data_ptr(), *s = stream_of(c.k);
+    const eg_status st = unlocked([&] { return lib.heads_backward(&c.q, w, bytes, s); });
+    if (st != EG_OK) return PyLong_FromLong(st);
+    PyObject* weights = a[13] != Py_None ? same(a[13]) : tuple(fresh[0].defined() ? wrap(fresh[0]) : none(), fresh[1].defined() ? wrap(fresh[1]) : none());
+    return tuple(dq.defined() ? wrap(dq) : same(a[11]), dk.defined() ? wrap(dk) : same(a[12]), weights);
+}
+
 // ------------------------------------------------------------------------------- clipping
 // context, P, replica_stride, grads, out, max_norm, flags, norms
 PyObject* clip_gradients(PyObject* const* a) {
@@ -354,8 +533,9 @@ PyObject* init(PyObject* const* a) {
 }
 
 #define EG_ENTRY(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f, n>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {EG_ENTRY(init, 9), EG_ENTRY(residual_norm, 9), EG_ENTRY(residual_norm_backward, 10), EG_ENTRY(feed_forward, 7),
-                         EG_ENTRY(feed_forward_backward, 8), EG_ENTRY(clip_gradients, 8), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {EG_ENTRY(init, 1 + sizeof(Library) / sizeof(void*)), EG_ENTRY(residual_norm, 9), EG_ENTRY(residual_norm_backward, 10), EG_ENTRY(feed_forward, 7),
+                         EG_ENTRY(feed_forward_backward, 8), EG_ENTRY(clip_gradients, 8), EG_ENTRY(embedding, 4), EG_ENTRY(embedding_backward, 6),
+                         EG_ENTRY(head_norm, 11), EG_ENTRY(head_norm_backward, 14), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
