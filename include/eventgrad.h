@@ -486,6 +486,40 @@ int64_t eg_head_norm_workspace(const eg_head_norm_args* args);
 eg_status eg_head_norm(const eg_head_norm_args* args, void* stream);
 eg_status eg_head_norm_backward(const eg_head_norm_args* args, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Orthogonal updates: for every matrix of every replica, with g its gradient and v its velocity (fp32),
+ *     v' = momentum * v + g,      u = g + momentum * v' with `nesterov`, else v'       (no velocity: u = g)
+ *     X = u / |u| (the root of the sum of its squares),   transposed where it has more rows than columns
+ *     `steps` times:  X <- a X + (b A + c A^2) X,  A = X X^T
+ *     out = scale * X (transposed back).
+ * The polynomial pulls the singular values of X towards 1 and leaves its singular vectors: out is, roughly, the orthogonal
+ * matrix next to u.  coefficients: a, b, c of every step (steps x 3, host), NULL: 3.4445, -4.7750, 2.0315 in each.  They may not
+ * let the singular values grow beyond 64 on their way from 0 .. 1.  A matrix of zeros gives zeros, one whose norm is not finite
+ * NaN everywhere.
+ *
+ * grad is of type dtype, out of out_dtype, which is dtype or EG_F32; velocity and velocity_out are fp32 (velocity not given: none;
+ * velocity_out not given: velocity itself is updated).  out may be grad itself and velocity_out velocity itself.  The
+ * accuracy goes by out_dtype: bf16 results come from products whose operands are rounded to 11 bits (their error is about that of the
+ * result's own rounding), fp16 and fp32 ones from operands of 22 bits; sums are fp32, the norm's fp64.
+ * Any number of matrices of any sizes up to 2^20 share a call; `matrices` and `coefficients` are read before it returns.
+ * `workspace` (device, 128-byte aligned) holds at least eg_orthogonalise_workspace(args) bytes (some 8 to 16 for every value,
+ * of up to 1 GB of matrices at a time) and is free for reuse once the stream has passed the call.
+ * The call only enqueues work on `stream` of the current device, holds no state and may be recorded into a graph; the results do
+ * not depend on the run.  Outputs must not overlap inputs or each other except as said; rows and replicas of an output that fall on
+ * one another are refused.  Errors: EG_ERR_INVALID, EG_ERR_CUDA. */
+typedef struct {
+    int64_t rows, columns;
+    double scale;
+    eg_matrix grad, out, velocity, velocity_out;
+} eg_orthogonal_matrix;
+typedef struct {
+    int64_t P, count, dtype, out_dtype, steps, nesterov;
+    double momentum;
+    const double* coefficients;
+    const eg_orthogonal_matrix* matrices;
+} eg_orthogonalise_args;
+int64_t eg_orthogonalise_workspace(const eg_orthogonalise_args* args);
+eg_status eg_orthogonalise(const eg_orthogonalise_args* args, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* The operators' kernels never trap and their waits are bounded; a wait that runs out sets a word
  * of the current device (one for all its streams and callers) and leaves that call's results
  * undefined.  Synchronises `stream`, returns EG_ERR_TIMEOUT if that happened in any call on the

@@ -39,6 +39,7 @@ EXPORTS = [
     "eg_operator_status", "eg_feed_forward", "eg_feed_forward_backward", "eg_feed_forward_saved_bytes",
     "eg_feed_forward_workspace", "eg_selftest_operator_wait",
     "eg_embedding", "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward", "eg_head_norm_workspace",
+    "eg_orthogonalise", "eg_orthogonalise_workspace",
 ]
 STATIC_MAX_TENSORS = 192
 STATIC_MAX_PARTIALS = 524288
@@ -70,7 +71,8 @@ _lib = None
 _native = None        # csrc/marshal.cpp: the operators' arguments (see _operators)
 _OPERATORS = ("eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace", "eg_feed_forward",
               "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace", "eg_embedding",
-              "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward", "eg_head_norm_workspace")
+              "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward", "eg_head_norm_workspace",
+              "eg_orthogonalise", "eg_orthogonalise_workspace")
 
 
 def load_library() -> C.CDLL:
@@ -637,6 +639,45 @@ def head_norm_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: 
         r = native.head_norm_backward(q, k, w_q, w_k, positions, rotary, base, bool(interleaved), eps, dq_out, dk_out, dq, dk, d_weights)
     if r.__class__ is int:
         _check(_lib, r, None, "eg_head_norm_backward")
+    return r
+
+
+def _tensors(tensors: Optional[Sequence], n: int, what: str) -> Optional[tuple]:
+    if tensors is None:
+        return None
+    tensors = tuple(tensors)
+    if len(tensors) != n:
+        raise EventGradError(f"orthogonalise: {what} holds one entry for every gradient")
+    return tensors
+
+
+def orthogonalise(grads: Sequence[torch.Tensor], *, out: Optional[Sequence[torch.Tensor]] = None,
+                  velocity: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                  velocity_out: Optional[Sequence[Optional[torch.Tensor]]] = None, momentum: float = 0.95, nesterov: bool = True,
+                  steps: int = 5, coefficients: Optional[Sequence] = None, scale=1.0,
+                  stream: Optional[torch.cuda.Stream] = None) -> tuple:
+    """``eg_orthogonalise``: of every gradient matrix (of what momentum makes of it) the orthogonal matrix next to it, roughly, as
+    an update for the step.
+
+    ``grads``: tensors ``[P, rows, columns]`` of one type (views of a gradient buffer in the step's layout, say).  The results go to
+    ``out`` (same shapes, the gradients' type or fp32; default: ``grads`` themselves) and are returned.  ``velocity``: fp32
+    tensors of the same shapes (entries may be None: no momentum), which become ``momentum * velocity + grad`` in
+    ``velocity_out`` (default: in place); with ``nesterov`` the update looks ahead by ``grad + momentum * velocity``.
+    ``coefficients``: three numbers, or three for each of ``steps``; ``scale``: a factor for all results, or one for each."""
+    native = _native or _operators()
+    grads = tuple(grads)
+    n = len(grads)
+    out, velocity, velocity_out = (_tensors(v, n, what) for v, what in ((out, "out"), (velocity, "velocity"), (velocity_out, "velocity_out")))
+    scales = (scale,) * n if isinstance(scale, (int, float)) else _tensors(scale, n, "scale")
+    if coefficients is not None:
+        rows = [tuple(c) if isinstance(c, Sequence) else (c,) for c in coefficients]
+        coefficients = sum(rows, ())
+        if len(coefficients) == 3 and all(len(r) == 1 for r in rows):
+            coefficients = coefficients * max(0, int(steps))
+    with _on(stream):
+        r = native.orthogonalise(grads, out, velocity, velocity_out, momentum, bool(nesterov), steps, coefficients, scales)
+    if r.__class__ is int:
+        _check(_lib, r, None, "eg_orthogonalise")
     return r
 
 

@@ -11,7 +11,8 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = [os.path.join(HERE, "csrc", "eventgrad.cu"), os.path.join(HERE, "csrc", "eg_norms_static.cu")]
 #: the operators around the step: their products may be contracted into fused multiply-adds
-OPS = [os.path.join(HERE, "csrc", f) for f in ("eg_residual_norm.cu", "eg_feed_forward.cu", "eg_embedding.cu", "eg_head_norm.cu")]
+OPS = [os.path.join(HERE, "csrc", f) for f in ("eg_residual_norm.cu", "eg_feed_forward.cu", "eg_embedding.cu", "eg_head_norm.cu",
+                                              "eg_orthogonalise.cu")]
 LIB = os.path.join(HERE, "libeventgrad.so")
 #: torch tensors to C arguments, for the operators
 MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")

@@ -12,6 +12,7 @@
 
 #include "eg_ffn_few.cuh"
 #include "eg_gemm.cuh"
+#include "eg_tensor_map.cuh"
 
 namespace eg {
 namespace {
@@ -22,23 +23,6 @@ struct Mat {
 };
 
 // ----------------------------------------------------------------------------------- tensor maps
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encoder() {
-    static EncodeFn fn = nullptr;
-    if (!fn) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess ||
-            r != cudaDriverEntryPointSuccess)
-            return nullptr;
-        fn = reinterpret_cast<EncodeFn>(p);
-    }
-    return fn;
-}
-
 // Rows on 16-byte boundaries, which the copies need.
 bool in_place(const Mat& m, long long P, long long rows, size_t size) {
     return aligned16(m.p) && (rows <= 1 || m.row * (long long)size % 16 == 0) && (P <= 1 || m.rep * (long long)size % 16 == 0);

@@ -1,0 +1,461 @@
+// The products of eg_orthogonalise on the tensor cores (sm_100a).
+//
+// One launch forms one of the three products of a step for all matrices of all replicas (instances):
+//   gram     A = X X^T                                    X: m x n, m <= n
+//   square   B = b A + c A^2
+//   apply    X <- a X + B X                               (the last step: into the caller's matrix)
+//
+// Everything in between lies in the workspace as fp16 boxes of 64 x 64, each 8 KB in one piece and already in the order that the
+// tensor cores want in shared memory (128-byte swizzle): one tensor map serves all matrices of any size, a copy is a whole box,
+// and nothing has rows to be aligned.  Boxes of a column lie one after another.  Edges are filled up with zeros, which stay zeros.
+//
+// Values are bounded (a singular value starts at most at 1 and the polynomial keeps it below a bound that the host
+// derives), so that fp16 with a power of two in front is as wide as needed and has three bits more than bf16.  A value is held as two
+// fp16 parts, hi + lo: 22 bits and a sign, an error of 2^-23 at most.
+//   PARTS == 1 (results of 8 bits): the products take hi alone, which costs 2^-12 of a value each, about what the result's own
+//     rounding does.  X is nevertheless carried on in both parts: the term a X, which alone carries small singular values
+//     (485 times over in five steps), sees no rounding to 11 bits.  (One part throughout: error 15 % for a matrix of rank 1.)
+//   PARTS == 2 (results of 11 and 24 bits): hi hi + hi lo + lo hi.  lo lo, 2^-22 of a product, is left out.
+//
+// A and B are symmetric: only tiles of 256 x 256 on and below the diagonal are formed and stored.  An operand above it is read
+// from the box on the other side, as its transpose: the tensor cores take either order, step by step of K.
+//
+// Tiles, warps and barriers are those of eg_gemm.cuh: pairs of CTAs share a tile of 256 x BN, tcgen05.mma by one thread, the
+// accumulators of two tiles in tensor memory.  PARTS == 2: BN = 128, an accumulator for hi hi that moves to registers every
+// kOrthoChunk steps (adding into it truncates) and one for the smaller products.
+#pragma once
+#include "eg_gemm.cuh"
+
+namespace eg {
+
+constexpr int kBox = 64, kBoxBytes = 8192;
+constexpr int kOrthoMats = 48;                    // matrices of one launch
+constexpr int kOrthoChunk = 2;
+enum { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
+
+struct Strided {
+    void* p;
+    long long rep, row;
+};
+
+struct OrthoMat {
+    int m, n, rb, cb;                             // sides of X, and in boxes
+    int flip;                                     // X is the gradient's transpose
+    int tiles[2];                                 // of one replica: of the symmetric products, of X
+    int first;                                    // instance of replica 0
+    float scale;
+    long long x[2], a, b;                         // first boxes of replica 0: X before and after a step, A, B
+    long long x_rep, s_rep;                       // boxes from one replica to the next (X, A and B); lo parts lie half as far
+    Strided grad, out, velocity, velocity_out;
+    // k_ortho_norm: rows of `cols` values, units of kNormUnit of them; blocks of an instance
+    long long view_rows, view_cols, units;
+    int blocks, begin;                            // begin: first block of replica 0
+    int boxes_begin;                              // k_ortho_in: first block
+};
+
+struct OrthoArgs {
+    CUtensorMap map;                              // the workspace as rows of 128 bytes
+    unsigned char* ws;
+    double* partial;                              // [instances][kNormBlocks] sums of squares
+    float* turn;                                  // [instances] what is left of 1 / |u| after a power of two
+    unsigned int* err;
+    int P, count;
+    int tiles[2];
+    float momentum;
+    int nesterov;
+    float sx;                                     // powers of two before X, A, B
+    float gram, ca, cb, ci;                       // gram: D -> A;  square: A -> B (b), D -> B (c);  apply: D -> X
+    float a, out;                                 // a;  X -> result
+    OrthoMat mat[kOrthoMats];
+};
+
+template <int PARTS> struct OrthoShape {
+    static constexpr int kBN = PARTS == 2 ? 128 : 256;
+    static constexpr int kA = 2 * kBoxBytes * PARTS, kB = kBN / 128 * kBoxBytes * PARTS;     // of a stage and CTA
+    static constexpr int kStages = PARTS == 2 ? 3 : 5;
+    static constexpr int kEpi = kGemmEpiWarps * kBoxBytes;                                  // hi and lo of 32 rows x 64 columns
+    static constexpr int kBars = kStages * (kA + kB) + kEpi;
+    static constexpr int kSmem = 1024 + kBars + 1024;
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+    static constexpr int kChunks = kBN / 128;                                               // of 64 columns for a warp
+};
+
+// The tiles in order, one pair's at a time: t only grows.
+struct OrthoWalk {
+    int k = 0;
+    int base = 0;
+};
+struct OrthoPos {
+    int k, p, i, j;                               // matrix, replica, tile row and column
+};
+template <int PARTS, int PASS> __device__ __forceinline__ OrthoPos ortho_pos(const OrthoArgs& a, OrthoWalk& w, int t) {
+    constexpr int S = PASS >= kApply ? 1 : 0, BOXES = OrthoShape<PARTS>::kBN / kBox;
+    while (t - w.base >= a.mat[w.k].tiles[S] * a.P) w.base += a.mat[w.k++].tiles[S] * a.P;
+    const OrthoMat& m = a.mat[w.k];
+    OrthoPos q;
+    q.k = w.k;
+    int r = t - w.base;
+    q.p = r / m.tiles[S];
+    r -= q.p * m.tiles[S];
+    if (S == 1) {
+        const int rows = (m.rb + 3) / 4;
+        q.j = r / rows;                           // neighbouring pairs share their columns of X
+        q.i = r - q.j * rows;
+    } else {
+        const int cols = (m.rb + BOXES - 1) / BOXES;
+        q.i = 0;
+        for (;; ++q.i) {
+            const int here = min(cols, (q.i + 1) * (4 / BOXES));
+            if (r < here) break;
+            r -= here;
+        }
+        q.j = r;
+    }
+    return q;
+}
+
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(op_smem(src)), "r"(bytes) : "memory");
+}
+
+// Two values as hi and lo words.
+__device__ __forceinline__ void split_half2(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = pack2<__half>(x, y);
+    const float2 f = unpack2<__half>(hi);
+    lo = pack2<__half>(x - f.x, y - f.y);
+}
+
+// T: type of the caller's matrices (kLast).
+template <typename T, int PARTS, int PASS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_ortho(const __grid_constant__ OrthoArgs a, int step) {
+    using Shape = OrthoShape<PARTS>;
+    constexpr int BN = Shape::kBN, S = Shape::kStages;
+    constexpr bool SYMMETRIC = PASS == kGram || PASS == kSquare;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    unsigned char* ring_b = smem + S * Shape::kA;
+    unsigned char* epi = ring_b + S * Shape::kB;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + Shape::kBars);   // [S] (even CTA's are used)
+    uint64_t* empty = full + S;                                          // [S]
+    uint64_t* acc_full = empty + S;                                      // [2]
+    uint64_t* acc_empty = acc_full + 2;                                  // [2] (even CTA's are used)
+    uint64_t* small_full = acc_empty + 2;                                // [2]: accumulators of the smaller products
+    uint64_t* small_empty = small_full + 2;                              // [2] (even CTA's are used)
+    uint64_t* epi_full = small_empty + 2;                                // [kGemmEpiWarps]
+    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + kGemmEpiWarps);
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(const_cast<int*>(s_abort) + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        *s_abort = 0;
+        for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
+        for (int q = 0; q < 2; ++q) {
+            op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps);
+            op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kGemmEpiWarps);
+        }
+        for (int q = 0; q < kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&a.map) : "memory");
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(op_smem(s_tmem)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = *s_tmem;
+    // set up while the kernel before this one finished; from here on its results are read and overwritten
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = a.tiles[SYMMETRIC ? 0 : 1];
+    const int from = step & 1;
+    OrthoWalk walk;
+
+    if (warp == 0 || warp == 3) {
+        // warp 0 fetches the left operand (and announces a stage's bytes), warp 3 the right one
+        if (elect_one()) {
+            int s = 0, round = 0;
+            for (int t = pair; t < tiles; t += pairs) {
+                const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
+                const OrthoMat& g = a.mat[q.k];
+                const bool left = warp == 0;
+                const long long x = g.x[from] + q.p * g.x_rep, sym = (PASS == kSquare ? g.a : g.b) + q.p * g.s_rep;
+                const int ksteps = PASS == kGram ? g.cb : g.rb;
+                constexpr int RIGHT = BN / 128;                           // boxes of the right operand that a CTA fetches
+                const int limit = left || SYMMETRIC ? g.rb : g.cb;
+                const int box0 = left ? q.i * 4 + (int)rank * 2 : q.j * (2 * RIGHT) + (int)rank * RIGHT;
+                // boxes that are there: what the other rows and columns of D become, nobody stores
+                const int have = max(0, min(left ? 2 : RIGHT, limit - box0));
+                uint32_t bytes = 0;
+                if (left && rank == 0) {
+                    const int r_limit = SYMMETRIC ? g.rb : g.cb;
+                    bytes = (uint32_t)(min(4, g.rb - q.i * 4) + min(2 * RIGHT, r_limit - q.j * (2 * RIGHT))) * kBoxBytes * PARTS;
+                }
+                for (int k = 0; k < ksteps; ++k) {
+                    if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
+                    unsigned char* to = left ? smem + s * Shape::kA : ring_b + s * Shape::kB;
+                    if (left && rank == 0) op_mbar_expect(&full[s], bytes);
+                    const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
+                    // (row, k) of a stored box; above the diagonal of a symmetric operand its mirror image; X by its columns
+                    long long box, next, lo;
+                    const bool is_x = PASS == kGram || (!SYMMETRIC && !left);
+                    if (is_x) {
+                        const bool by_column = !SYMMETRIC;
+                        box = x + (by_column ? (long long)box0 * g.rb + k : (long long)k * g.rb + box0);
+                        next = by_column ? g.rb : 1;
+                        lo = g.x_rep / 2;
+                    } else {
+                        const bool mirror = k / 4 > box0 / 4;
+                        box = sym + (mirror ? (long long)box0 * g.rb + k : (long long)k * g.rb + box0);
+                        next = mirror ? g.rb : 1;
+                        lo = g.s_rep / 2;
+                    }
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (h < have)
+                                tma_load_pair(to + (part * (left ? 2 : RIGHT) + h) * kBoxBytes, &a.map, 0, (int)((box + h * next + part * lo) * kBox), 0, bar);
+                        }
+                    }
+                    if (++s == S) { s = 0; ++round; }
+                }
+            }
+            // the last arrivals on this CTA's barriers, which the even CTA's products send, come in before it ends
+            for (int j = max(0, round * S + s - S); j < round * S + s; ++j) mbar_wait(&empty[j % S], (j / S) & 1, s_abort, a.err);
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
+            int s = 0, round = 0, count = 0, turn = 0;          // count: accumulators handed over; turn: tiles
+            for (int t = pair; t < tiles; t += pairs, ++turn) {
+                const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
+                const OrthoMat& g = a.mat[q.k];
+                const int ksteps = PASS == kGram ? g.cb : g.rb, right_block = q.j * (BN / kBox) / 4;
+                uint32_t add = 0, add_small = 0;
+                const uint32_t small = tmem + (2 + (turn & 1)) * 128;
+                if (PARTS == 2 && turn >= 2) mbar_wait(&small_empty[turn & 1], ((turn >> 1) - 1) & 1, s_abort, a.err);
+                for (int k = 0; k < ksteps; ++k) {
+                    const bool a_mn = PASS != kGram && k / 4 > q.i, b_mn = PASS >= kApply || (PASS == kSquare && k / 4 > right_block);
+                    const uint32_t idesc = (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
+                                           ((uint32_t)(kGemmM >> 4) << 24);
+                    const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+                    if (!add) {
+                        if (count >= 2) mbar_wait(&acc_empty[count & 1], ((count >> 1) - 1) & 1, s_abort, a.err);
+                        tc_fence_after();
+                    }
+                    const uint32_t d = tmem + (count & 1) * BN;
+                    mbar_wait(&full[s], round & 1, s_abort, a.err);
+                    tc_fence_after();
+                    auto product = [&](uint32_t to, int pa, int pb, uint32_t& add_to) {
+                        const uint64_t da = smem_desc(op_smem(smem + s * Shape::kA + pa * 2 * kBoxBytes), a_mn);
+                        const uint64_t db = smem_desc(op_smem(ring_b + s * Shape::kB + pb * (BN / 128) * kBoxBytes), b_mn);
+#pragma unroll
+                        for (int u = 0; u < kGemmK / 16; ++u) {
+                            tc_mma_pair(to, da + u * a_step, db + u * b_step, idesc, add_to);
+                            add_to = 1;
+                        }
+                    };
+                    product(d, 0, 0, add);
+                    if constexpr (PARTS == 2) {
+                        product(small, 0, 1, add_small);
+                        product(small, 1, 0, add_small);
+                    }
+                    tc_commit_pair(&empty[s]);
+                    if (++s == S) { s = 0; ++round; }
+                    if (PARTS == 2 && k + 1 < ksteps && (k + 1) % kOrthoChunk == 0) {
+                        tc_commit_pair(&acc_full[count & 1]);
+                        ++count;
+                        add = 0;
+                    }
+                }
+                tc_commit_pair(&acc_full[count & 1]);
+                ++count;
+                if (PARTS == 2) tc_commit_pair(&small_full[turn & 1]);
+            }
+        }
+    } else if (warp >= 4) {
+        const int w = warp - 4, half = w >> 2, quad = w & 3;
+        unsigned char* buf = epi + w * kBoxBytes;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        int count = 0, turn = 0, uses = 0;
+        for (int t = pair; t < tiles; t += pairs, ++turn) {
+            const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
+            const OrthoMat& g = a.mat[q.k];
+            const int ksteps = PASS == kGram ? g.cb : g.rb;
+            const int rbox = q.i * 4 + (int)rank * 2 + (quad >> 1), cols = SYMMETRIC ? g.rb : g.cb;
+            const long long x = g.x[from] + q.p * g.x_rep, sym_a = g.a + q.p * g.s_rep, sym_b = g.b + q.p * g.s_rep;
+            const float left_of = step == 0 ? a.turn[g.first + q.p] : 1.f;
+            auto cbox = [&](int c) { return q.j * (BN / kBox) + half * Shape::kChunks + c; };
+            auto inside = [&](int c) { return rbox < g.rb && cbox(c) < cols; };
+            auto place = [&](long long matrix, int c) { return a.ws + (matrix + (long long)cbox(c) * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096; };
+            // what the result is added to comes in ahead of the products
+            auto fetch = [&](int c) {
+                if (PASS == kGram || !inside(c)) return;
+                store_wait_read<0>();
+                __syncwarp();
+                if (elect_one()) {
+                    constexpr bool BOTH = PARTS == 2 || PASS != kSquare;
+                    const long long matrix = PASS == kSquare ? sym_a : x, lo = (PASS == kSquare ? g.s_rep : g.x_rep) / 2;
+                    op_mbar_expect(&epi_full[w], BOTH ? 8192 : 4096);
+                    op_bulk_load(buf, place(matrix, c), 4096, &epi_full[w]);
+                    if (BOTH) op_bulk_load(buf + 4096, place(matrix + lo, c), 4096, &epi_full[w]);
+                }
+            };
+            fetch(0);
+            float sum[PARTS == 2 ? 64 : 1];                       // this row's 64 columns, added up over the chunks
+            if constexpr (PARTS == 2) {
+#pragma unroll
+                for (int e = 0; e < 64; ++e) sum[e] = 0.f;
+                auto take = [&](uint32_t acc) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int e = 0; e < 64; e += 32) {
+                        uint32_t v[32];
+                        tc_load(v, acc + lanes + half * 64 + e);
+#pragma unroll
+                        for (int z = 0; z < 32; ++z) sum[e + z] += __uint_as_float(v[z]);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                };
+                for (int z = 0; z < (ksteps + kOrthoChunk - 1) / kOrthoChunk; ++z, ++count) {
+                    mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
+                    take(tmem + (count & 1) * BN);
+                    if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
+                }
+                mbar_wait(&small_full[turn & 1], (turn >> 1) & 1, s_abort, a.err);
+                take(tmem + (2 + (turn & 1)) * 128);
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&small_empty[turn & 1]), 0));
+            } else {
+                mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
+                tc_fence_after();
+            }
+            const uint32_t acc = tmem + (count & 1) * BN + lanes + half * (BN / 2);
+#pragma unroll 1
+            for (int c = 0; c < Shape::kChunks; ++c) {
+                if (c > 0) fetch(c);
+                if (!inside(c)) continue;
+                if (PASS == kGram) {
+                    store_wait_read<0>();
+                    __syncwarp();
+                } else {
+                    mbar_wait(&epi_full[w], uses & 1, s_abort, a.err);
+                    ++uses;
+                }
+                float v[PASS == kLast ? 64 : 32];
+#pragma unroll
+                for (int x0 = 0; x0 < 64; x0 += 32) {
+                    uint32_t d[32];
+                    if constexpr (PARTS == 1) tc_load(d, acc + c * 64 + x0);
+                    float* r = v + (PASS == kLast ? x0 : 0);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) r[e] = PARTS == 2 ? sum[PARTS == 2 ? x0 + e : 0] : __uint_as_float(d[e]);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        unsigned char* at = buf + lane * 128 + ((((x0 + e) >> 3) ^ (lane & 7)) << 4);
+                        if constexpr (PASS == kGram) {
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) r[e + z] *= a.gram * left_of * left_of;
+                        } else {
+                            const uint4 h4 = *reinterpret_cast<const uint4*>(at);
+                            uint4 l4 = make_uint4(0, 0, 0, 0);
+                            if (PARTS == 2 || PASS != kSquare) l4 = *reinterpret_cast<const uint4*>(at + 4096);
+                            const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+                            const float with = PASS == kSquare ? a.ca : a.a, by = PASS == kSquare ? a.cb : a.ci;
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const float2 hf = unpack2<__half>(hw[z]), lf = unpack2<__half>(lw[z]);
+                                r[e + 2 * z] = fmaf(with, hf.x, fmaf(with, lf.x, by * r[e + 2 * z]));
+                                r[e + 2 * z + 1] = fmaf(with, hf.y, fmaf(with, lf.y, by * r[e + 2 * z + 1]));
+                                if (PASS >= kApply) {
+                                    r[e + 2 * z] *= left_of;
+                                    r[e + 2 * z + 1] *= left_of;
+                                }
+                            }
+                        }
+                        if constexpr (PASS != kLast) {
+                            uint32_t hw[4], lw[4];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) split_half2(r[e + 2 * z], r[e + 2 * z + 1], hw[z], lw[z]);
+                            *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                            if (PARTS == 2 || PASS == kApply) *reinterpret_cast<uint4*>(at + 4096) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                        }
+                    }
+                }
+                if constexpr (PASS != kLast) {
+                    fence_async_shared();
+                    __syncwarp();
+                    if (elect_one()) {
+                        const long long matrix = PASS == kGram ? sym_a : PASS == kSquare ? sym_b : g.x[from ^ 1] + q.p * g.x_rep;
+                        const long long lo = (SYMMETRIC ? g.s_rep : g.x_rep) / 2;
+                        bulk_store(place(matrix, c), buf, 4096);
+                        if (PARTS == 2 || PASS == kApply) bulk_store(place(matrix + lo, c), buf + 4096, 4096);
+                        store_commit();
+                    }
+                } else {
+                    const float scale = a.out * g.scale;
+                    const int row0 = rbox * kBox + (quad & 1) * 32, col0 = cbox(c) * kBox;
+                    T* out = static_cast<T*>(g.out.p) + q.p * g.out.rep;
+                    if (g.flip) {                                 // a row of X is a column of the result
+                        if (row0 + lane < g.m) {
+                            T* to = out + (long long)col0 * g.out.row + row0 + lane;
+#pragma unroll
+                            for (int e = 0; e < 64; ++e)
+                                if (col0 + e < g.n) to[e * g.out.row] = from_f32<T>(v[e] * scale);
+                        }
+                    } else {
+                        // through shared memory, 32 rows of 64 values, to runs along the rows
+                        __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < 64; e += 4)
+                            *reinterpret_cast<float4*>(buf + lane * 256 + (((e >> 2) ^ (lane & 15)) << 4)) =
+                                make_float4(v[e] * scale, v[e + 1] * scale, v[e + 2] * scale, v[e + 3] * scale);
+                        __syncwarp();
+                        const int rows = min(32, g.m - row0), n = min(64, g.n - col0);
+                        T* to = out + (long long)row0 * g.out.row + col0;
+                        auto value = [&](int r, int x) { return buf + r * 256 + (((x >> 2) ^ (r & 15)) << 4) + (x & 3) * 4; };
+                        const bool pairs_of = sizeof(T) == 2 && ((uintptr_t)to & 3) == 0 && (g.out.row & 1) == 0;
+#pragma unroll 4
+                        for (int r = 0; r < rows; ++r, to += g.out.row) {
+                            if (pairs_of) {
+                                const int x0 = 2 * lane;
+                                const float2 f = *reinterpret_cast<const float2*>(value(r, x0));
+                                if constexpr (sizeof(T) == 2) {
+                                    if (x0 + 1 < n) *reinterpret_cast<uint32_t*>(to + x0) = pack2<T>(f.x, f.y);
+                                    else if (x0 < n) to[x0] = from_f32<T>(f.x);
+                                }
+                            } else {
+                                const float f0 = *reinterpret_cast<const float*>(value(r, lane)), f1 = *reinterpret_cast<const float*>(value(r, lane + 32));
+                                if (lane < n) to[lane] = from_f32<T>(f0);
+                                if (lane + 32 < n) to[lane + 32] = from_f32<T>(f1);
+                            }
+                        }
+                        // the next box's copy comes by another way than these reads
+                        fence_async_shared();
+                        __syncwarp();
+                    }
+                }
+            }
+            if constexpr (PARTS == 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
+                ++count;
+            }
+        }
+        store_wait_read<0>();
+    }
+    if (*s_abort) {           // a wait ran out: copies and products in flight get a millisecond to end
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) {}
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+}  // namespace eg

@@ -1,0 +1,447 @@
+// Orthogonal updates (eg_orthogonalise): every matrix of every replica as its momentum's nearest orthogonal matrix, roughly.
+//
+//   v' = momentum * v + g,   u = v' or g + momentum * v'        (without a velocity u = g)
+//   X = u / |u|,  transposed where it has more rows than columns (m x n, m <= n)
+//   steps times   X <- a X + (b A + c A^2) X,   A = X X^T       (an odd polynomial of X's singular values, which pulls them to 1)
+//   out = scale * X
+//
+// Launches: k_ortho_norm (velocity, sums of squares), k_ortho_in (X in the workspace's boxes), then three products a step
+// (eg_orthogonal_gemm.cuh), each over all matrices of all replicas: a network's small matrices fill the machine together.
+//
+// Only a power of two of 1 / |u| goes into X at first, so that gradients of 16 bits enter the products without a rounding; the rest,
+// between 1 and 2, is multiplied onto the first step's results in 32 bits.
+#include <math.h>
+
+#include "eg_orthogonal_gemm.cuh"
+#include "eg_tensor_map.cuh"
+
+namespace eg {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kNormUnit = 4 * kThreads;           // values of a row that a block takes at a time
+constexpr int kNormBlocks = 128;                  // of an instance, at most
+constexpr long long kGroupBytes = 1ll << 30;      // workspace of one group of matrices that share their launches (one matrix may need more)
+
+// u of four neighbouring values, and v' where it is formed.
+template <typename T, bool FORM> __device__ __forceinline__ void update4(const OrthoArgs& a, const OrthoMat& m, int p, long long row, long long col,
+                                                                       int n, bool vec, float (&u)[4]) {
+    const T* g = static_cast<const T*>(m.grad.p) + p * m.grad.rep + row * m.grad.row + col;
+    const float* v = m.velocity.p ? static_cast<const float*>(FORM ? m.velocity.p : m.velocity_out.p) +
+                                        p * (FORM ? m.velocity.rep : m.velocity_out.rep) + row * (FORM ? m.velocity.row : m.velocity_out.row) + col
+                                  : nullptr;
+    float* to = FORM && v ? static_cast<float*>(m.velocity_out.p) + p * m.velocity_out.rep + row * m.velocity_out.row + col : nullptr;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool need_g = FORM || !v || a.nesterov;
+    const bool whole = vec && n >= 4;
+    if (whole) {
+        if (need_g) {
+            if constexpr (sizeof(T) == 4) {
+                load_vec<T, 4>(g, u);
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(g);
+                const float2 f0 = unpack2<T>(x.x), f1 = unpack2<T>(x.y);
+                u[0] = f0.x; u[1] = f0.y; u[2] = f1.x; u[3] = f1.y;
+            }
+        }
+        if (v) load_vec<float, 4>(v, w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            u[e] = e < n && need_g ? to_f32(g[e]) : 0.f;
+            if (v) w[e] = e < n ? v[e] : 0.f;
+        }
+    }
+    if (!v) return;
+    if (FORM) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = fmaf(a.momentum, w[e], u[e]);
+        if (whole) {
+            store_vec<float, 4>(to, w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < n) to[e] = w[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = a.nesterov ? fmaf(a.momentum, w[e], u[e]) : w[e];
+}
+
+__device__ __forceinline__ bool quads(const OrthoMat& m, size_t size) {
+    auto fits = [](const Strided& s, size_t bytes) { return !s.p || (((uintptr_t)s.p | (uintptr_t)(s.rep * (long long)bytes) | (uintptr_t)(s.row * (long long)bytes)) & (4 * bytes - 1)) == 0; };
+    return fits(m.grad, size) && fits(m.velocity, 4) && fits(m.velocity_out, 4);
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads) k_ortho_norm(const __grid_constant__ OrthoArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ double s_sum[kThreads / 32];
+    int k = 0;
+    while (k + 1 < a.count && (int)blockIdx.x >= a.mat[k + 1].begin) ++k;
+    const OrthoMat& m = a.mat[k];
+    const int at = blockIdx.x - m.begin, p = at / m.blocks, b = at - p * m.blocks;
+    const bool vec = quads(m, sizeof(T));
+    const long long per = (m.view_cols + kNormUnit - 1) / kNormUnit;
+    double sum = 0.0;
+    for (long long q = b; q < m.units; q += m.blocks) {
+        const long long row = q / per, c = (q - row * per) * kNormUnit + threadIdx.x * 4;
+        if (c >= m.view_cols) continue;
+        const int n = m.view_cols - c < 4 ? (int)(m.view_cols - c) : 4;
+        float u[4];
+        update4<T, true>(a, m, p, row, c, n, vec, u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) sum = fma((double)u[e], (double)u[e], sum);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / 32; ++w) sum += s_sum[w];
+        a.partial[(long long)(m.first + p) * kNormBlocks + b] = sum;
+    }
+}
+
+// A block: one box of X.
+template <typename T> __global__ void __launch_bounds__(kThreads) k_ortho_in(const __grid_constant__ OrthoArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ double s_sum[kNormBlocks / 32];
+    __shared__ float s_box[kBox][kBox + 1];
+    int k = 0;
+    while (k + 1 < a.count && (int)blockIdx.x >= a.mat[k + 1].boxes_begin) ++k;
+    const OrthoMat& m = a.mat[k];
+    const int boxes = m.rb * m.cb, at = blockIdx.x - m.boxes_begin, p = at / boxes, box = at - p * boxes;
+    const int cbox = box / m.rb, rbox = box - cbox * m.rb;
+    if (threadIdx.x < kNormBlocks) {
+        double s = (int)threadIdx.x < m.blocks ? a.partial[(long long)(m.first + p) * kNormBlocks + threadIdx.x] : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = s;
+    }
+    const bool vec = quads(m, sizeof(T));
+    // quad z of a thread: row z * 16 + threadIdx.x / 16 of the box (of the gradient's), columns 4 * (threadIdx.x % 16)
+    float u[4][4];
+    const int quad = threadIdx.x & 15, first = threadIdx.x >> 4;
+    const int row0 = (m.flip ? cbox : rbox) * kBox, col0 = (m.flip ? rbox : cbox) * kBox + quad * 4;
+    const int rows = m.flip ? m.n : m.m, cols = m.flip ? m.m : m.n;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+        const int r = row0 + z * 16 + first;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[z][e] = 0.f;
+        if (r < rows && col0 < cols) update4<T, false>(a, m, p, r, col0, cols - col0 < 4 ? cols - col0 : 4, vec, u[z]);
+    }
+    __syncthreads();
+    double total = 0.0;
+#pragma unroll
+    for (int w = 0; w < kNormBlocks / 32; ++w) total += s_sum[w];
+    const double norm = sqrt(total);
+    int ex = 0;
+    double fraction = 0.0;
+    const bool finite = norm <= 1.7e308;                  // (false for NaN too)
+    if (finite) fraction = frexp(norm, &ex);              // norm = fraction * 2^ex, 1/2 <= fraction < 1
+    const double by = ldexp((double)a.sx, -ex);
+    if (box == 0 && threadIdx.x == 0)
+        a.turn[m.first + p] = !finite ? __int_as_float(0x7fffffff) : fraction > 0.0 ? (float)(1.0 / fraction) : 0.f;
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[z][e] = (float)((double)u[z][e] * by);
+    if (m.flip) {
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_box[quad * 4 + e][z * 16 + first] = u[z][e];
+        __syncthreads();
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[z][e] = s_box[z * 16 + first][quad * 4 + e];
+    }
+    unsigned char* hi = a.ws + (m.x[0] + p * m.x_rep + box) * kBoxBytes;
+    unsigned char* lo = hi + m.x_rep / 2 * kBoxBytes;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+        uint32_t h0, h1, l0, l1;
+        split_half2(u[z][0], u[z][1], h0, l0);
+        split_half2(u[z][2], u[z][3], h1, l1);
+        const uint32_t off = swz128((z * 16 + first) * 128 + quad * 8);
+        *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
+        *reinterpret_cast<uint2*>(lo + off) = make_uint2(l0, l1);
+    }
+}
+
+// ----------------------------------------------------------------------------------- host
+constexpr int kMaxSteps = 64;
+const double kDefault[3] = {3.4445, -4.7750, 2.0315};
+
+struct Scales {
+    float sx, sa, sb[kMaxSteps];
+    double c[kMaxSteps][3];
+};
+
+float power_below(double most) {                          // the largest power of two with most * it <= 60000, at most 2^14
+    int e = 0;
+    frexp(60000.0 / most, &e);
+    const int k = e - 1 < 14 ? e - 1 : 14;
+    return (float)ldexp(1.0, k);
+}
+
+// Bounds of the singular values, step by step, and the powers of two that they allow; false where the polynomials let them grow
+// beyond 64.
+bool scales(const eg_orthogonalise_args* q, Scales* s) {
+    double bound = 1.0, most = 1.0;
+    for (int k = 0; k < q->steps; ++k) {
+        for (int z = 0; z < 3; ++z) {
+            s->c[k][z] = q->coefficients ? q->coefficients[3 * k + z] : kDefault[z];
+            if (!(fabs(s->c[k][z]) <= 1e4)) return false;
+        }
+        const double a = s->c[k][0], b = s->c[k][1], c = s->c[k][2], top = bound * bound;
+        // |B| in the spectral norm: b x + c x^2 on 0 .. bound^2
+        double highest = fabs(b * top + c * top * top);
+        if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < top) highest = fmax(highest, fabs(b * b / (4 * c)));
+        s->sb[k] = power_below(fmax(highest, 1e-3) * 1.02);
+        auto value = [&](double x) { return fabs(sqrt(x) * (a + x * (b + c * x))); };   // x: a square
+        double next = value(top);
+        const double disc = 9 * b * b - 20 * a * c;          // of a + 3 b x + 5 c x^2
+        if (c != 0.0 && disc >= 0.0) {
+            for (double sign : {-1.0, 1.0}) {
+                const double x = (-3 * b + sign * sqrt(disc)) / (10 * c);
+                if (x > 0.0 && x < top) next = fmax(next, value(x));
+            }
+        } else if (c == 0.0 && b != 0.0) {
+            const double x = -a / (3 * b);
+            if (x > 0.0 && x < top) next = fmax(next, value(x));
+        }
+        most = fmax(most, bound);
+        bound = next * 1.01;
+        if (bound > 64.0) return false;
+    }
+    most = fmax(most, bound);
+    s->sx = power_below(most * 1.02);
+    s->sa = power_below(most * most * 1.02);
+    return true;
+}
+
+bool usable(const eg_matrix& m, int64_t P, int64_t rows, int64_t cols, size_t size, bool written) {
+    if (!m.data || (uintptr_t)m.data % size || m.row_stride < 0 || m.replica_stride < 0 || m.row_stride >= (1ll << 36) ||
+        m.replica_stride >= (1ll << 42))
+        return false;
+    if (!written) return true;
+    if (rows > 1 && m.row_stride < cols) return false;
+    if (P > 1) {
+        const int64_t rep = m.replica_stride, row = rows > 1 ? m.row_stride : 0;
+        if (!(rep >= (rows - 1) * row + cols || (rep >= cols && row >= (P - 1) * rep + cols))) return false;
+    }
+    return true;
+}
+
+size_t size_of(int64_t dtype) { return dtype == EG_F32 ? 4 : 2; }
+bool known(int64_t dtype) { return dtype == EG_F32 || dtype == EG_BF16 || dtype == EG_F16; }
+
+bool valid(const eg_orthogonalise_args* q, Scales* s) {
+    if (!q || !known(q->dtype) || !known(q->out_dtype) || (q->out_dtype != q->dtype && q->out_dtype != EG_F32)) return false;
+    if (q->P < 1 || q->P > 4096 || q->count < 0 || q->count > 65536 || (q->count > 0 && !q->matrices)) return false;
+    if (q->steps < 1 || q->steps > kMaxSteps || !(fabs(q->momentum) <= 1e4) || !scales(q, s)) return false;
+    for (int64_t i = 0; i < q->count; ++i) {
+        const eg_orthogonal_matrix& m = q->matrices[i];
+        if (m.rows < 1 || m.columns < 1 || m.rows > (1 << 20) || m.columns > (1 << 20) || !(fabs(m.scale) <= 3e38)) return false;
+        const int64_t boxes = (m.rows + 63) / 64 * ((m.columns + 63) / 64);
+        const int64_t side = ((m.rows < m.columns ? m.rows : m.columns) + 63) / 64;
+        if (q->P * (4 * boxes + 4 * side * side) > (1ll << 24)) return false;              // 128 GB of workspace
+        if (!usable(m.grad, q->P, m.rows, m.columns, size_of(q->dtype), false)) return false;
+        if (!usable(m.out, q->P, m.rows, m.columns, size_of(q->out_dtype), true)) return false;
+        if (m.velocity.data && !usable(m.velocity, q->P, m.rows, m.columns, 4, !m.velocity_out.data)) return false;
+        if (m.velocity_out.data && (!m.velocity.data || !usable(m.velocity_out, q->P, m.rows, m.columns, 4, true))) return false;
+    }
+    return true;
+}
+
+int parts_of(const eg_orthogonalise_args* q) { return q->out_dtype == EG_BF16 ? 1 : 2; }
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+struct Sides {
+    int64_t rb, cb, boxes;                                // of one replica: X twice and A and B, in two parts
+};
+Sides sides(const eg_orthogonal_matrix& m) {
+    const int64_t r = m.rows <= m.columns ? m.rows : m.columns, c = m.rows <= m.columns ? m.columns : m.rows;
+    Sides s{up(r, kBox) / kBox, up(c, kBox) / kBox, 0};
+    s.boxes = 4 * s.rb * s.cb + 4 * s.rb * s.rb;
+    return s;
+}
+// Matrices [first, *end) share their launches.  Returns their boxes.
+int64_t group(const eg_orthogonalise_args* q, int64_t first, int64_t* end) {
+    int64_t boxes = 0, i = first;
+    for (; i < q->count && i - first < kOrthoMats; ++i) {
+        const int64_t more = q->P * sides(q->matrices[i]).boxes;
+        if (i > first && (boxes + more) * kBoxBytes > kGroupBytes) break;
+        boxes += more;
+    }
+    *end = i;
+    return boxes;
+}
+int64_t tail_bytes(const eg_orthogonalise_args* q) {      // partial sums and scalars of a group
+    return up(q->P * kOrthoMats * (int64_t)kNormBlocks * 8, 1024) + up(q->P * kOrthoMats * 4, 1024);
+}
+int64_t workspace_of(const eg_orthogonalise_args* q) {
+    int64_t most = 0, end = 0;
+    for (int64_t i = 0; i < q->count; i = end) {
+        const int64_t boxes = group(q, i, &end);
+        most = boxes > most ? boxes : most;
+    }
+    return most * kBoxBytes + tail_bytes(q);
+}
+
+Strided strided(const eg_matrix& m) { return Strided{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
+
+bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t end, unsigned char* ws, int64_t boxes, int* norm_blocks, int* in_blocks) {
+    const int parts = parts_of(q);
+    a->ws = ws;
+    a->partial = reinterpret_cast<double*>(ws + boxes * kBoxBytes);
+    a->turn = reinterpret_cast<float*>(ws + boxes * kBoxBytes + up(q->P * kOrthoMats * (int64_t)kNormBlocks * 8, 1024));
+    a->P = (int)q->P;
+    a->count = (int)(end - first);
+    a->tiles[0] = a->tiles[1] = 0;
+    a->momentum = (float)q->momentum;
+    a->nesterov = q->nesterov != 0;
+    int64_t at = 0, begin = 0, begin_boxes = 0, tiles[2] = {0, 0};
+    for (int64_t i = first; i < end; ++i) {
+        const eg_orthogonal_matrix& s = q->matrices[i];
+        OrthoMat* m = &a->mat[i - first];
+        const Sides z = sides(s);
+        m->flip = s.rows > s.columns;
+        m->m = (int)(m->flip ? s.columns : s.rows);
+        m->n = (int)(m->flip ? s.rows : s.columns);
+        m->rb = (int)z.rb; m->cb = (int)z.cb;
+        m->first = (int)((i - first) * q->P);
+        m->scale = (float)s.scale;
+        const int64_t plane = z.rb * z.cb, square = z.rb * z.rb;
+        m->x_rep = 2 * plane; m->s_rep = 2 * square;
+        m->x[0] = at;
+        m->x[1] = at + q->P * 2 * plane;
+        m->a = at + q->P * 4 * plane;
+        m->b = m->a + q->P * 2 * square;
+        at += q->P * z.boxes;
+        m->grad = strided(s.grad); m->out = strided(s.out); m->velocity = strided(s.velocity);
+        m->velocity_out = s.velocity_out.data ? strided(s.velocity_out) : m->velocity;
+        const int wide = parts == 2 ? 2 : 4;              // boxes of a tile's columns
+        const int64_t rt = (z.rb + 3) / 4, ct = (z.rb + wide - 1) / wide;
+        int64_t low = 0;
+        for (int64_t r = 0; r < rt; ++r) low += ct < (r + 1) * (4 / wide) ? ct : (r + 1) * (4 / wide);
+        m->tiles[0] = (int)low;
+        m->tiles[1] = (int)(rt * ((z.cb + wide - 1) / wide));
+        tiles[0] += q->P * low;
+        tiles[1] += q->P * (int64_t)m->tiles[1];
+        // values one after another are one row
+        const bool flat = (s.grad.row_stride == s.columns || s.rows == 1) &&
+                          (!s.velocity.data || ((s.velocity.row_stride == s.columns || s.rows == 1) && (m->velocity_out.row == s.columns || s.rows == 1)));
+        m->view_rows = flat ? 1 : s.rows;
+        m->view_cols = flat ? s.rows * s.columns : s.columns;
+        m->units = m->view_rows * ((m->view_cols + kNormUnit - 1) / kNormUnit);
+        const int64_t blocks = (m->units + 1) / 2;
+        m->blocks = (int)(blocks < kNormBlocks ? blocks : kNormBlocks);
+        m->begin = (int)begin;
+        m->boxes_begin = (int)begin_boxes;
+        begin += q->P * m->blocks;
+        begin_boxes += q->P * plane;
+    }
+    if (tiles[0] > 0x3fffffff || tiles[1] > 0x3fffffff || begin > 0x3fffffff || begin_boxes > 0x3fffffff) return false;
+    a->tiles[0] = (int)tiles[0];
+    a->tiles[1] = (int)tiles[1];
+    *norm_blocks = (int)begin;
+    *in_blocks = (int)begin_boxes;
+    EncodeFn fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {64, (cuuint64_t)(boxes * kBox), 1}, strides[2] = {128, (cuuint64_t)(boxes * kBoxBytes)};
+    const cuuint32_t box[3] = {64, 64, 1}, one[3] = {1, 1, 1};
+    return fn(&a->map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, ws, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& a, int step, cudaStream_t stream) {
+    constexpr int smem = OrthoShape<PARTS>::kSmem;
+    static bool raised[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !raised[dev]) {
+        e = cudaFuncSetAttribute(k_ortho<T, PARTS, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) raised[dev] = true;
+    }
+    const int pairs = sm_count() / 2, tiles = a.tiles[PASS >= kApply ? 1 : 0];
+    if (pairs < 1) return cudaErrorInvalidDevice;
+    return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kGemmThreads), smem, stream, a, step);
+}
+
+template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, int norm_blocks, int in_blocks, cudaStream_t stream) {
+    constexpr int PARTS = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 2;
+    a.sx = s.sx;
+    cudaError_t e;
+    auto given = [&](auto value) {
+        using G = decltype(value);
+        const cudaError_t r = launch_after(k_ortho_norm<G>, dim3(norm_blocks), dim3(kThreads), 0, stream, a);
+        return r != cudaSuccess ? r : launch_after(k_ortho_in<G>, dim3(in_blocks), dim3(kThreads), 0, stream, a);
+    };
+    e = q->dtype == EG_F32 ? given(0.f) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}) : given(__half{});
+    if (e != cudaSuccess) return e;
+    for (int k = 0; k < q->steps; ++k) {
+        a.a = (float)s.c[k][0];
+        a.gram = s.sa / (s.sx * s.sx);
+        a.ca = (float)(s.c[k][1] * s.sb[k] / s.sa);
+        a.cb = (float)(s.c[k][2] * s.sb[k] / ((double)s.sa * s.sa));
+        a.ci = 1.f / s.sb[k];
+        a.out = 1.f / s.sx;
+        // what only the last launch depends on is the caller's type: the others are shared
+        if ((e = product<float, PARTS, kGram>(a, k, stream)) != cudaSuccess) return e;
+        if (k + 1 < q->steps) {
+            if ((e = product<float, PARTS, kSquare>(a, k, stream)) != cudaSuccess) return e;
+            if ((e = product<float, PARTS, kApply>(a, k, stream)) != cudaSuccess) return e;
+        } else {
+            if ((e = product<float, PARTS, kSquare>(a, k, stream)) != cudaSuccess) return e;
+            if ((e = product<T, PARTS, kLast>(a, k, stream)) != cudaSuccess) return e;
+        }
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+}  // namespace eg
+
+using namespace eg;
+
+extern "C" {
+
+int64_t eg_orthogonalise_workspace(const eg_orthogonalise_args* q) {
+    Scales s;
+    if (!valid(q, &s)) return 0;
+    return workspace_of(q);
+}
+
+eg_status eg_orthogonalise(const eg_orthogonalise_args* q, void* workspace, int64_t workspace_bytes, void* stream_v) {
+    Scales s;
+    if (!valid(q, &s)) return EG_ERR_INVALID;
+    if (q->count == 0) return EG_OK;
+    if (!workspace || (uintptr_t)workspace % 128 || workspace_bytes < workspace_of(q)) return EG_ERR_INVALID;
+    unsigned int* err = operator_error_word();
+    if (!err) return EG_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    int64_t end = 0;
+    for (int64_t i = 0; i < q->count; i = end) {
+        const int64_t boxes = group(q, i, &end);
+        OrthoArgs a;
+        a.err = err;
+        int norm_blocks = 0, in_blocks = 0;
+        if (!fill(&a, q, i, end, static_cast<unsigned char*>(workspace), boxes, &norm_blocks, &in_blocks)) return EG_ERR_CUDA;
+        const cudaError_t e = q->out_dtype == EG_F32    ? run<float>(a, s, q, norm_blocks, in_blocks, stream)
+                              : q->out_dtype == EG_BF16 ? run<__nv_bfloat16>(a, s, q, norm_blocks, in_blocks, stream)
+                                                        : run<__half>(a, s, q, norm_blocks, in_blocks, stream);
+        if (e != cudaSuccess) return EG_ERR_CUDA;
+    }
+    return EG_OK;
+}
+
+}  // extern "C"

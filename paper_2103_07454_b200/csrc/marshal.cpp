@@ -9,8 +9,10 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <algorithm>
 #include <cstring>
 #include <string>
+#include <vector>
 
 #include "../../include/eventgrad.h"
 
@@ -31,6 +33,8 @@ struct Library {
     decltype(&eg_head_norm) heads;
     decltype(&eg_head_norm_backward) heads_backward;
     decltype(&eg_head_norm_workspace) heads_workspace;
+    decltype(&eg_orthogonalise) ortho;
+    decltype(&eg_orthogonalise_workspace) ortho_workspace;
 } lib;
 PyObject* error_class = nullptr;
 
@@ -488,6 +492,58 @@ PyObject* head_norm_backward(PyObject* const* a) {
     return tuple(dq.defined() ? wrap(dq) : same(a[11]), dk.defined() ? wrap(dk) : same(a[12]), weights);
 }
 
+// ------------------------------------------------------------------------------- matrices
+// The i-th of a tuple, or None.
+PyObject* item(PyObject* o, Py_ssize_t i) { return o == Py_None ? Py_None : PyTuple_GET_ITEM(o, i); }
+
+// grads, out, velocity, velocity_out (tuples or None), momentum, nesterov, steps, coefficients (tuple of numbers, or None), scales (tuple)
+PyObject* orthogonalise(PyObject* const* a) {
+    const Py_ssize_t count = PyTuple_GET_SIZE(a[0]);
+    if (count == 0) return PyTuple_New(0);
+    const at::Tensor& first = on_device(tensor(PyTuple_GET_ITEM(a[0], 0), "grads"));
+    if (first.dim() != 3 || type_of(first) < 0) throw Refused{"orthogonalise: a gradient must be [P, rows, columns] fp32, bf16 or fp16"};
+    const Kind k{first.scalar_type(), first.device()}, wide{at::kFloat, k.device};
+    const at::Tensor& first_out = a[1] == Py_None ? first : tensor(PyTuple_GET_ITEM(a[1], 0), "out");
+    const Kind result{first_out.scalar_type(), k.device};
+    const c10::cuda::CUDAGuard guard(k.device);
+    eg_orthogonalise_args q{};
+    q.P = first.size(0); q.count = count; q.dtype = type_of(first); q.out_dtype = type_of(first_out);
+    q.momentum = number(a[4]);
+    q.nesterov = a[5] == Py_True;
+    q.steps = integer(a[6]);
+    std::vector<double> coefficients;
+    if (a[7] != Py_None) {
+        if (q.steps < 1 || PyTuple_GET_SIZE(a[7]) != 3 * q.steps) throw Refused{"orthogonalise: three coefficients, or three for every step"};
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[7]); ++i) coefficients.push_back(number(PyTuple_GET_ITEM(a[7], i)));
+        q.coefficients = coefficients.data();
+    }
+    std::vector<eg_orthogonal_matrix> all(count);
+    q.matrices = all.data();
+    std::vector<const void*> written;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor& g = tensor(PyTuple_GET_ITEM(a[0], i), "grads");
+        if (g.dim() != 3) throw Refused{"orthogonalise: a gradient must be [P, rows, columns]"};
+        const int64_t sizes[] = {q.P, g.size(1), g.size(2)};
+        eg_orthogonal_matrix& m = all[i];
+        m.rows = sizes[1]; m.columns = sizes[2];
+        m.scale = number(PyTuple_GET_ITEM(a[8], i));
+        m.grad = given(PyTuple_GET_ITEM(a[0], i), sizes, k, "grads");
+        m.out = a[1] == Py_None ? m.grad : given(PyTuple_GET_ITEM(a[1], i), sizes, result, "out");
+        m.velocity = given(item(a[2], i), sizes, wide, "velocity");
+        m.velocity_out = given(item(a[3], i), sizes, wide, "velocity_out");
+        written.push_back(m.out.data);
+        if (m.velocity.data) written.push_back(m.velocity_out.data ? m.velocity_out.data : m.velocity.data);
+    }
+    std::sort(written.begin(), written.end());
+    if (std::adjacent_find(written.begin(), written.end()) != written.end()) throw Refused{"orthogonalise: two results lie on one another"};
+    const int64_t bytes = lib.ortho_workspace(&q);
+    const at::Tensor workspace = k.bytes(bytes);
+    void *w = workspace.data_ptr(), *s = stream_of(k);
+    const eg_status st = unlocked([&] { return lib.ortho(&q, w, bytes, s); });
+    if (st != EG_OK) return PyLong_FromLong(st);
+    return same(a[1] == Py_None ? a[0] : a[1]);
+}
+
 // ------------------------------------------------------------------------------- clipping
 // context, P, replica_stride, grads, out, max_norm, flags, norms
 PyObject* clip_gradients(PyObject* const* a) {
@@ -535,7 +591,7 @@ PyObject* init(PyObject* const* a) {
 #define EG_ENTRY(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {EG_ENTRY(init, 1 + sizeof(Library) / sizeof(void*)), EG_ENTRY(residual_norm, 9), EG_ENTRY(residual_norm_backward, 10), EG_ENTRY(feed_forward, 7),
                          EG_ENTRY(feed_forward_backward, 8), EG_ENTRY(clip_gradients, 8), EG_ENTRY(embedding, 4), EG_ENTRY(embedding_backward, 6),
-                         EG_ENTRY(head_norm, 11), EG_ENTRY(head_norm_backward, 14), {nullptr, nullptr, 0, nullptr}};
+                         EG_ENTRY(head_norm, 11), EG_ENTRY(head_norm_backward, 14), EG_ENTRY(orthogonalise, 9), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -135,3 +135,76 @@ def test_tensors_on_the_host_are_refused():
         B.head_norm(q, q)
     with pytest.raises(B.EventGradError):
         B.head_norm_backward(q, q, q, q)
+
+
+class OrthogonalMatrix(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("columns", C.c_int64), ("scale", C.c_double)] + [(n, Matrix) for n in ("grad", "out", "velocity", "velocity_out")]
+
+
+class Orthogonalise(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("P", "count", "dtype", "out_dtype", "steps", "nesterov")] +
+                [("momentum", C.c_double), ("coefficients", C.POINTER(C.c_double)), ("matrices", C.POINTER(OrthogonalMatrix))])
+
+
+def orthogonalise(matrices=None, coefficients=None, **change):
+    """One 64 x 96 matrix of 2 replicas with a velocity, unless others are given; `matrices`: changes of it, one each."""
+    P, r, c = 2, 64, 96
+    all_ = []
+    for m in matrices or [{}]:
+        v = dict(rows=r, columns=c, scale=1.0, grad=Matrix(A, r * c, c), out=Matrix(A, r * c, c), velocity=Matrix(A, r * c, c), velocity_out=Matrix())
+        v.update(m)
+        all_.append(OrthogonalMatrix(**v))
+    q = dict(P=P, count=len(all_), dtype=B.BF16, out_dtype=B.BF16, steps=5, nesterov=1, momentum=0.95, matrices=(OrthogonalMatrix * len(all_))(*all_))
+    if coefficients is not None:
+        q["coefficients"] = (C.c_double * len(coefficients))(*coefficients)
+    q.update(change)
+    return Orthogonalise(**q)
+
+
+def workspace(q):
+    lib = library()
+    lib.eg_orthogonalise_workspace.restype = C.c_int64
+    return lib.eg_orthogonalise_workspace(C.byref(q))
+
+
+def refused(q):
+    lib = library()
+    lib.eg_orthogonalise.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+    return workspace(q) == 0 and lib.eg_orthogonalise(C.byref(q), A, 1 << 50, None) == INVALID
+
+
+@pytest.mark.parametrize("bad", [dict(P=0), dict(P=4097), dict(count=-1), dict(dtype=3), dict(out_dtype=3), dict(out_dtype=B.F16), dict(dtype=B.F32), dict(steps=0),
+                                 dict(steps=65), dict(momentum=float("nan")), dict(momentum=float("inf")), dict(matrices=[dict(rows=0)]),
+                                 dict(matrices=[dict(columns=(1 << 20) + 1)]), dict(matrices=[dict(scale=float("nan"))]), dict(matrices=[dict(grad=Matrix())]),
+                                 dict(matrices=[dict(out=Matrix())]), dict(matrices=[dict(out=Matrix(A, 6143, 96))]), dict(matrices=[dict(out=Matrix(A, 6144, 95))]),
+                                 dict(matrices=[dict(out=Matrix(A, 0, 96))]), dict(matrices=[dict(grad=Matrix(A + 1, 6144, 96))]),
+                                 dict(matrices=[dict(velocity=Matrix(A + 2, 6144, 96))]), dict(matrices=[dict(velocity=Matrix(A, 6143, 96))]),
+                                 dict(matrices=[dict(velocity=Matrix(), velocity_out=Matrix(A, 6144, 96))]), dict(matrices=[{}, dict(rows=-1)]),
+                                 dict(coefficients=[float("nan")] * 15), dict(coefficients=[2e4, 0.0, 0.0] * 5), dict(coefficients=[3.0, 0.0, 0.0] * 5)])
+def test_orthogonalise_refuses(bad):
+    assert refused(orthogonalise(**bad))
+
+
+def test_orthogonalise_takes_what_it_should():
+    lib = library()
+    one = workspace(orthogonalise())
+    assert one >= 2 * (4 * 2 + 4) * 8192                      # of two replicas: X twice, A and B, in two parts
+    assert workspace(orthogonalise(out_dtype=B.F32)) == one
+    assert workspace(orthogonalise(matrices=[{}] * 3)) > one
+    assert workspace(orthogonalise(coefficients=[1.5, -0.5, 0.0] * 5)) == one
+    assert workspace(orthogonalise(coefficients=[1.875, -1.25, 0.375] * 64, steps=64)) == one
+    assert workspace(orthogonalise(matrices=[dict(out=Matrix(A, 96, 192), grad=Matrix(A, 0, 0))])) == one
+    assert workspace(orthogonalise(matrices=[dict(velocity=Matrix(A, 0, 96), velocity_out=Matrix(A, 6144, 96))])) == one
+    big = [dict(rows=8192, columns=16384, grad=Matrix(A, 1 << 27, 16384), out=Matrix(A, 1 << 27, 16384), velocity=Matrix())]
+    assert workspace(orthogonalise(matrices=big * 3)) == workspace(orthogonalise(matrices=big))       # one after another
+    q = orthogonalise()
+    lib.eg_orthogonalise.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+    for w, size in ((A, one - 1), (A + 64, one), (None, one)):
+        assert lib.eg_orthogonalise(C.byref(q), w, size, None) == INVALID
+    assert lib.eg_orthogonalise(C.byref(orthogonalise(count=0)), None, 0, None) == 0
+    assert lib.eg_orthogonalise(None, A, one, None) == INVALID
+
+
+def test_matrices_on_the_host_are_refused():
+    with pytest.raises(B.EventGradError):
+        B.orthogonalise([torch.zeros(1, 4, 8)])
