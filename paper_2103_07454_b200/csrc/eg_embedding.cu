@@ -12,9 +12,10 @@
 //   1. k_embed_sort: one CTA per range of the table's rows reads all tokens of its replica twice.  It counts the tokens
 //      below its range (which is where its part of the sorted list begins) and each of its own, then puts the places into
 //      the list.  The tokens come out of the L2 and nobody waits for another CTA; a sort in several passes would read them
-//      about as often and launch five kernels.  It also writes the zeros of the rows without a place.
+//      about as often and launch five kernels.  It notes which rows have a place.
 //   2. k_embed_sum: a warp adds up one chunk of the list over some columns.  Chunks have equal length, however often a token
-//      comes; a run that crosses chunks leaves a partial sum in each.
+//      comes; a run that crosses chunks leaves a partial sum in each.  Other blocks of the launch write the zeros of the rows without
+//      a place meanwhile, the same number of rows each.
 //   3. k_embed_join: adds the partial sums of such runs, in order.
 #include "eg_ops.cuh"
 
@@ -44,7 +45,10 @@ struct EmbedArgs {
     int range;                             // rows of the table per sorting CTA
     int chunk, chunks;                     // places of a chunk; chunks of a replica
     int pitch;                             // columns of a partial sum, up to whole vectors
+    int sum_blocks;                        // of k_embed_sum, per replica; the rest write zeros
     int *order, *key, *count;              // [P][n] places and tokens of the sorted list, [P] its length
+    unsigned int* named;                   // [P][words] one bit for every row of the table that has a place
+    int words;
     float* partial;                        // [P][chunks][2][pitch]: of a run from the chunk before, of one into the next
 };
 
@@ -106,26 +110,27 @@ __device__ __forceinline__ int block_total(int v, int* red) {
     return s;
 }
 
-template <typename T, int VEC> __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_constant__ EmbedArgs a) {
+__global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_constant__ EmbedArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ int s_at[kSortWarps][kRangeMax];          // first how often, then where to
-    __shared__ int s_sum[kRangeMax], s_red[kSortWarps];
+    __shared__ int s_red[kSortWarps];
     const int i = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long first = (long long)blockIdx.x * a.range;
     const int mine = (int)(a.V - first < a.range ? a.V - first : a.range);
     for (int q = threadIdx.x; q < kSortWarps * kRangeMax; q += kSortThreads) (&s_at[0][0])[q] = 0;
     __syncthreads();
-    // every warp takes its own stretch of the places, 32 at a time, four of them on their way at once
+    // every warp takes its own stretch of the places, 32 at a time, SCAN of them on their way at once
+    constexpr int SCAN = 8;
     const long long each = ((a.n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
     const long long t0 = warp * each, t1 = t0 + each < a.n ? t0 + each : a.n;
     int below = 0;
-    for (long long t = t0; t < t1; t += 128) {
-        int v[4];
+    for (long long t = t0; t < t1; t += 32 * SCAN) {
+        int v[SCAN];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
+        for (int u = 0; u < SCAN; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < SCAN; ++u) {
             const long long at = v[u] - first;
             below += v[u] >= 0 && at < 0;
             if (v[u] >= 0 && at >= 0 && at < mine) atomicAdd(&s_at[warp][at], 1);
@@ -154,8 +159,9 @@ template <typename T, int VEC> __global__ void __launch_bounds__(kSortThreads) k
         before += w < warp ? s_red[w] : 0;
         all += s_red[w];
     }
+    const unsigned some = __ballot_sync(0xffffffffu, total > 0);
+    if (lane == 0 && r < mine) a.named[(long long)i * a.words + (first + r) / 32] = some;     // (ranges are whole words)
     if (r < mine) {
-        s_sum[r] = total;
         int at = base + before + upto - total;
 #pragma unroll
         for (int w = 0; w < kSortWarps; ++w) {
@@ -168,12 +174,12 @@ template <typename T, int VEC> __global__ void __launch_bounds__(kSortThreads) k
     __syncthreads();
     if (all > 0) {
         int *order = a.order + i * a.n, *key = a.key + i * a.n;
-        for (long long t = t0; t < t1; t += 128) {
-            int v[4];
+        for (long long t = t0; t < t1; t += 32 * SCAN) {
+            int v[SCAN];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
+            for (int u = 0; u < SCAN; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < SCAN; ++u) {
                 const long long rel = v[u] - first;
                 const bool in = v[u] >= 0 && rel >= 0 && rel < mine;
                 if (!__any_sync(0xffffffffu, in)) continue;
@@ -191,13 +197,6 @@ template <typename T, int VEC> __global__ void __launch_bounds__(kSortThreads) k
             }
         }
     }
-    if (a.accumulate) return;
-    const float zero[VEC] = {};
-    for (int q = warp; q < mine; q += kSortWarps) {
-        if (s_sum[q] != 0) continue;
-        T* to = row_of<T>(a.out, i, first + q);
-        for (int c = lane * VEC; c < a.d; c += 32 * VEC) store_vec<T, VEC>(to + c, zero);
-    }
 }
 
 // Adds to or writes a row's columns.
@@ -210,12 +209,47 @@ template <typename T, int VEC> __device__ __forceinline__ void finish(const Embe
     store_vec<T, VEC>(to, v);
 }
 
-// A warp: one chunk of the sorted list, 32 * U vectors of columns.
+// Values as they lie in memory.
+template <typename T, int VEC> struct Raw {
+    uint4 v;
+    __device__ __forceinline__ void load(const T* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void add_to(float* sum) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (sizeof(T) == 4) {
+                sum[q] += __uint_as_float(w[q]);
+            } else {
+                const float2 f = unpack2<T>(w[q]);
+                sum[2 * q] += f.x;
+                sum[2 * q + 1] += f.y;
+            }
+        }
+    }
+};
+template <typename T> struct Raw<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void add_to(float* sum) const { sum[0] += to_f32(v); }
+};
+
+// A warp: one chunk of the sorted list, 32 * U vectors of columns; or zeros for rows without a place.
 template <typename T, int VEC, int U> __global__ void __launch_bounds__(256) k_embed_sum(const __grid_constant__ EmbedArgs a, int slices) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    constexpr int AHEAD = 4;                             // rows on their way at once
+    constexpr int AHEAD = 8 / U;                         // rows on their way at once
     const int lane = threadIdx.x & 31, i = blockIdx.y;
+    if ((int)blockIdx.x >= a.sum_blocks) {
+        const float zero[VEC] = {};
+        const long long b = blockIdx.x - a.sum_blocks, blocks = gridDim.x - a.sum_blocks;
+        const long long v0 = a.V * b / blocks, v1 = a.V * (b + 1) / blocks;
+        for (long long v = v0 + (threadIdx.x >> 5); v < v1; v += 8) {
+            if (a.n > 0 && (a.named[(long long)i * a.words + v / 32] >> (v & 31) & 1)) continue;
+            T* to = row_of<T>(a.out, i, v);
+            for (int c = lane * VEC; c < a.d; c += 32 * VEC) store_vec<T, VEC>(to + c, zero);
+        }
+        return;
+    }
     const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     const long long chunk = unit / slices;
     if (chunk >= a.chunks) return;
@@ -237,21 +271,20 @@ template <typename T, int VEC, int U> __global__ void __launch_bounds__(256) k_e
         const int place = lane < m ? order[j0 + lane] : 0, token = lane < m ? key[j0 + lane] : -1;
         const int after = j0 + lane + 1 < n && lane < m ? key[j0 + lane + 1] : -1;
         for (int j = 0; j < m; j += AHEAD) {
-            float v[AHEAD][U][VEC];
+            Raw<T, VEC> v[AHEAD][U];
 #pragma unroll
             for (int h = 0; h < AHEAD; ++h) {
                 const T* from = row_of<T>(a.weight, i, __shfl_sync(0xffffffffu, place, (j + h) & 31)) + c0;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (j + h < m && c0 + u * 32 * VEC < a.d) load_vec<T, VEC>(from + u * 32 * VEC, v[h][u]);
+                    if (j + h < m && c0 + u * 32 * VEC < a.d) v[h][u].load(from + u * 32 * VEC);
             }
 #pragma unroll
             for (int h = 0; h < AHEAD; ++h) {
                 if (j + h >= m) break;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) sum[u][e] += v[h][u][e];
+                    if (c0 + u * 32 * VEC < a.d) v[h][u].add_to(sum[u]);
                 const int here = __shfl_sync(0xffffffffu, token, j + h), next = __shfl_sync(0xffffffffu, after, j + h);
                 if (here == next) continue;
                 // the end of a run, or of the chunk
@@ -277,19 +310,20 @@ template <typename T, int VEC, int U> __global__ void __launch_bounds__(256) k_e
     }
 }
 
-// A warp: the run that begins in one chunk and goes on into the next, 32 vectors of columns.
-template <typename T, int VEC> __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ EmbedArgs a, int slices) {
+// A warp: the run that begins in one chunk and goes on into the next, 32 * 4 columns.
+template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ EmbedArgs a, int slices) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    constexpr int AHEAD = 8;
     const int lane = threadIdx.x & 31, i = blockIdx.y;
     const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     const long long chunk = unit / slices;
     if (chunk >= a.chunks) return;
-    const int c = ((int)(unit - chunk * slices) * 32 + lane) * VEC, count = a.count[i];
+    const int c = ((int)(unit - chunk * slices) * 32 + lane) * 4, count = a.count[i];
     const long long first = chunk * a.chunk, end = first + a.chunk;
     if (end >= count) return;
     const int* key = a.key + i * a.n;
-    const int token = key[end - 1];
-    if (key[end] != token || (first > 0 && key[first - 1] == token)) return;
+    const int token = key[end - 1], next = key[end], before = first > 0 ? key[first - 1] : -1;
+    if (next != token || before == token) return;
     // chunks that the run goes on through: those that begin with its token
     long long more = 1;
     for (long long q = chunk + 1;; q += 32) {
@@ -302,15 +336,24 @@ template <typename T, int VEC> __global__ void __launch_bounds__(256) k_embed_jo
     }
     if (c >= a.d) return;
     const float* partial = a.partial + ((long long)i * a.chunks + chunk) * 2 * a.pitch + c;
-    float sum[VEC];
+    float sum[4];
+    load_vec<float, 4>(partial + a.pitch, sum);
+    for (long long q = 1; q <= more; q += AHEAD) {
+        float v[AHEAD][4];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) sum[e] = partial[a.pitch + e];
-#pragma unroll 8
-    for (long long q = 1; q <= more; ++q) {
+        for (int h = 0; h < AHEAD; ++h) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] += partial[q * 2 * a.pitch + e];
+            for (int e = 0; e < 4; ++e) v[h][e] = 0.f;
+            if (q + h <= more) load_vec<float, 4>(partial + (q + h) * 2 * a.pitch, v[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += v[h][e];
     }
-    finish<T, VEC>(a, i, token, c, sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.d) finish<T, 1>(a, i, token, c + e, sum + e);
 }
 
 // ----------------------------------------------------------------------------------- host
@@ -354,28 +397,34 @@ bool valid(const eg_embedding_args* q, bool backward) {
     return true;
 }
 
-// Chunks of 32 places; of more where a run over all places would have more than 1024 partial sums to join.
-int chunk_of(int64_t n) {
+// Chunks of 8 to 32 places, so that there are some eight warps for every multiprocessor; of more where a run over all places would
+// have more than 1024 partial sums to join.  (3 x 777 rows of 509 in fp32: chunks of 32 took 42 us.)
+int chunk_of(const eg_embedding_args* q) {
+    const int64_t n = q->rows, columns = q->dtype == EG_F32 ? 128 : 256;
+    const double all = (double)q->P * (double)n * (double)((q->width + columns - 1) / columns);
     int c = 32;
+    while (c > 8 && all / c < 8.0 * 148) c /= 2;
     while (c * 1024ll < n) c *= 2;
     return c;
 }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 struct Layout {
-    int64_t order, key, count, partial, bytes;
-    int chunk, chunks, pitch;
+    int64_t order, key, count, named, partial, bytes;
+    int chunk, chunks, pitch, words;
 };
 Layout layout(const eg_embedding_args* q) {
     Layout l;
     const int64_t n = q->rows > 0 ? q->rows : 1;
-    l.chunk = chunk_of(n);
+    l.chunk = chunk_of(q);
     l.chunks = (int)((n + l.chunk - 1) / l.chunk);
     l.pitch = (int)((q->width + 7) / 8 * 8);
     l.order = 0;
     l.key = up16(4 * q->P * n);
     l.count = l.key + up16(4 * q->P * n);
-    l.partial = l.count + up16(4 * q->P);
+    l.named = l.count + up16(4 * q->P);
+    l.words = (int)((q->vocabulary + 31) / 32);
+    l.partial = l.named + up16(4 * q->P * (int64_t)l.words);
     l.bytes = l.partial + q->P * (int64_t)l.chunks * 2 * l.pitch * 4;
     return l;
 }
@@ -403,16 +452,27 @@ template <typename T, int VEC> cudaError_t forward(const EmbedArgs& a, cudaStrea
     return launch(k_embed<T, VEC, kMaxVectors>, kMaxVectors);
 }
 
-template <typename T, int VEC> cudaError_t backward(const EmbedArgs& a, cudaStream_t stream) {
-    const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
-    cudaError_t e = launch_after(k_embed_sort<T, VEC>, dim3(ranges, a.P), dim3(kSortThreads), 0, stream, a);
-    if (e != cudaSuccess || a.n == 0) return e;
+template <typename T, int VEC> cudaError_t backward(EmbedArgs a, cudaStream_t stream) {
+    cudaError_t e;
+    if (a.n > 0) {
+        const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
+        if ((e = launch_after(k_embed_sort, dim3(ranges, a.P), dim3(kSortThreads), 0, stream, a)) != cudaSuccess) return e;
+    }
     auto blocks = [&](int slices) { return (unsigned)(((long long)a.chunks * slices + 7) / 8); };
-    constexpr int U = VEC > 1 ? 2 : 4;
-    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC), narrow = (a.d + 32 * VEC - 1) / (32 * VEC);
-    e = launch_after(k_embed_sum<T, VEC, U>, dim3(blocks(slices), a.P), dim3(256), 0, stream, a, slices);
-    if (e != cudaSuccess || a.chunks == 1) return e;
-    return launch_after(k_embed_join<T, VEC>, dim3(blocks(narrow), a.P), dim3(256), 0, stream, a, narrow);
+    constexpr int U = VEC > 1 ? 1 : 4;
+    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC), narrow = (a.d + 127) / 128;
+    a.sum_blocks = a.n > 0 ? (int)blocks(slices) : 0;
+    // zeros: 64 KB or so a block, at least a few blocks for every multiprocessor
+    long long zeros = 0;
+    if (!a.accumulate) {
+        zeros = (long long)((double)a.V * a.d * sizeof(T) / 65536.0) + 1;
+        const long long least = (4ll * sm_count() + a.P - 1) / a.P, most = (a.V + 7) / 8;
+        if (zeros < least) zeros = least;
+        if (zeros > most) zeros = most;
+    }
+    e = launch_after(k_embed_sum<T, VEC, U>, dim3((unsigned)(a.sum_blocks + zeros), a.P), dim3(256), 0, stream, a, slices);
+    if (e != cudaSuccess || a.n == 0 || a.chunks == 1) return e;
+    return launch_after(k_embed_join<T>, dim3(blocks(narrow), a.P), dim3(256), 0, stream, a, narrow);
 }
 
 }  // namespace
@@ -455,6 +515,8 @@ eg_status eg_embedding_backward(const eg_embedding_args* q, void* workspace, int
     a.order = reinterpret_cast<int*>(w + l.order);
     a.key = reinterpret_cast<int*>(w + l.key);
     a.count = reinterpret_cast<int*>(w + l.count);
+    a.named = reinterpret_cast<unsigned int*>(w + l.named);
+    a.words = l.words;
     a.partial = reinterpret_cast<float*>(w + l.partial);
     a.chunk = l.chunk; a.chunks = l.chunks; a.pitch = l.pitch;
     // ranges long enough that the tokens are not read more often than needed, short enough that every multiprocessor has some

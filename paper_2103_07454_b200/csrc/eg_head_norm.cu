@@ -7,11 +7,12 @@
 //
 // Bound by memory: forward moves a value in and out, backward two in and one out (nothing is saved between them).
 //
-// A head's row is small, so a few threads share it, each with whole pairs: a "slot" is two vectors of VEC values whose
-// elements are partners (halves: j and j + rotary / 2; neighbours: inside either vector).  A CTA takes a few places of one replica
-// at a time and forms their cosines and sines once, in shared memory, for all heads of the queries and keys: a sine costs
-// some forty instructions, a value of a row about four.  An angle is reduced in 64 bits, where positions of any
-// size keep their fraction of a turn, and only the fraction goes on in 32.
+// A head's row is small, so a team of a few threads shares it, each with whole pairs: a "slot" is two vectors of VEC values whose
+// elements are partners (halves: j and j + rotary / 2; neighbours: inside either vector).  A warp takes one place after
+// another, all heads of the queries or of the keys, a row a team at a time; cosines and sines of the place stay in registers for all
+// of them (a sine costs some forty instructions, a value of a row about six), each formed by one team and handed to
+// the others.  An angle is reduced in 64 bits, where positions of any size keep their fraction of a turn; only the
+// fraction goes on in 32.
 #include <type_traits>
 
 #include "eg_ops.cuh"
@@ -19,10 +20,8 @@
 namespace eg {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxWidth = EG_HEAD_MAX_WIDTH, kMaxPairs = kMaxWidth / 2;
-constexpr int kMaxTile = 16;                // places whose angles a CTA holds
-constexpr int kTableMax = 2048;             // cosines and sines that it holds
 constexpr int kCtasPerSm = 4;
 
 struct Heads {
@@ -34,6 +33,14 @@ struct Vec {
     long long rep;
 };
 
+// The queries, or the keys.
+struct Side {
+    int heads, ctas, split;                 // ctas: of a replica; split: warps that share a place's heads
+    Heads x, out, d_out;                    // forward: x, out; backward: x, d_out and in out the gradient of x
+    Vec w;
+    float* partial;                         // [P][ctas][d] sums of dz * xh
+};
+
 struct HeadArgs {
     int P;
     long long n;
@@ -43,13 +50,8 @@ struct HeadArgs {
     const void* positions;                  // nullptr: 0, 1, ...
     long long pos_rep, pos_step;
     int wide;
-    int tile;                               // places at a time
-    int table;                              // pairs of the table (neighbours: all of a row's, those that stay with cosine 1)
-    int slots, team, ctas;                  // of a row; threads of a row; CTAs of a replica
-    int heads[2];                           // of the queries, of the keys
-    Heads x[2], out[2], d_out[2];           // forward: x, out; backward: x, d_out and in out the gradient of x
-    Vec w[2];
-    float* partial;                         // [P][ctas][2][d] sums of dz * xh
+    int slots;                              // of a row
+    Side side[2];
     double turns[kMaxPairs];                // turns of pair j per place
 };
 
@@ -57,18 +59,45 @@ template <typename T> __device__ __forceinline__ T* head_at(const Heads& m, int 
     return static_cast<T*>(m.p) + (long long)i * m.rep + t * m.row + (long long)h * m.head;
 }
 
-// Where the two vectors of slot s begin, and whether they are there.
-template <int VEC> __device__ __forceinline__ void slot_place(const HeadArgs& a, int s, int& first, int& second, bool& turned) {
-    if (a.interleaved) {
-        first = 2 * s * VEC;
-        second = first + VEC;
-        turned = true;
-    } else {
-        const int lead = a.half / VEC;                       // slots that turn
-        turned = s < lead;
-        first = turned ? s * VEC : a.rotary + 2 * (s - lead) * VEC;
-        second = turned ? a.half + s * VEC : first + VEC;
+// VEC values in one access, as they lie in memory; widened where they are used.
+template <typename T, int VEC> struct Packed {
+    static constexpr int kWords = VEC * (int)sizeof(T) / 4 > 0 ? VEC * (int)sizeof(T) / 4 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) w[q] = 0;
     }
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (VEC * sizeof(T) == 16) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else if constexpr (VEC * sizeof(T) == 8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[0] = v.x; w[1] = v.y;
+        } else if constexpr (VEC * sizeof(T) == 4) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void widen(float (&v)[VEC]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] = __uint_as_float(w[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+                const float2 f = unpack2<T>(w[e / 2]);
+                v[e] = f.x;
+                if (e + 1 < VEC) v[e + 1 < VEC ? e + 1 : e] = f.y;
+            }
+        }
+    }
+};
+template <typename T, int VEC> __device__ __forceinline__ void store_some(T* p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1 || VEC * sizeof(T) == 16) store_vec<T, VEC>(p, v);
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    else *reinterpret_cast<uint32_t*>(p) = pack2<T>(v[0], v[1]);
 }
 
 // (a, b) by the angle (c, s); BACK: by its opposite.
@@ -77,181 +106,204 @@ template <bool BACK> __device__ __forceinline__ void turn(float& a, float& b, fl
     a = fmaf(-s, b, cs.x * x);
     b = fmaf(s, x, cs.x * b);
 }
-template <int VEC, bool BACK> __device__ __forceinline__ void turn_slot(const HeadArgs& a, int s, bool turned, bool second, const float2* table,
-                                                                       float (&x)[2][VEC]) {
-    if (!turned) return;
+// A slot's VEC pairs: (x[0][e], x[1][e]), or neighbours inside either vector.  Pairs that stay have cosine 1.
+template <int VEC, bool BACK> __device__ __forceinline__ void turn_slot(bool interleaved, const float2* cs, float (&x)[2][VEC]) {
     if constexpr (VEC > 1) {
-        if (a.interleaved) {
+        if (interleaved) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (k == 1 && !second) return;               // (the table ends with the row)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int e = 0; e < VEC; e += 2) turn<BACK>(x[k][e], x[k][e + 1], table[((2 * s + k) * VEC + e) / 2]);
-            }
+                for (int e = 0; e < VEC; e += 2) turn<BACK>(x[k][e], x[k][e + 1], cs[(k * VEC + e) / 2]);
             return;
         }
     }
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) turn<BACK>(x[0][e], x[1][e], table[s * VEC + e]);
+    for (int e = 0; e < VEC; ++e) turn<BACK>(x[0][e], x[1][e], cs[e]);
 }
 
-// Sums over the `team` threads of a row (a power of two, at most a warp).
-__device__ __forceinline__ float team_sum(float v, int team) {
-    for (int o = team >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+// Sums over the TEAM threads of a row.
+template <int TEAM> __device__ __forceinline__ float team_sum(float v) {
+#pragma unroll
+    for (int o = TEAM >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// NS: slots of a thread.
-template <typename T, int VEC, int NS, bool BWD>
-__global__ void __launch_bounds__(kThreads) k_head_norm(const __grid_constant__ HeadArgs a) {
+// NS: slots of a thread; TEAM: threads of a row.
+template <typename T, int VEC, int NS, int TEAM, bool BWD>
+__global__ void __launch_bounds__(kThreads, BWD ? 2 : 3) k_head_norm(const __grid_constant__ HeadArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    __shared__ float2 s_table[kTableMax];
-    __shared__ float s_sum[BWD ? kThreads / 32 : 1][BWD ? kMaxWidth : 1];
-    const int i = blockIdx.y, b = blockIdx.x;
-    const long long t0 = a.n * b / a.ctas, t1 = a.n * (b + 1) / a.ctas;
-    const int lane = threadIdx.x % a.team, group = threadIdx.x / a.team, groups = kThreads / a.team;
-    float w[2][NS][2][VEC], dw[BWD ? 2 : 1][NS][2][VEC];
+    constexpr int GROUPS = 32 / TEAM, PAIRS = NS * VEC, AHEAD = NS > 2 ? 1 : 2;
+    __shared__ float s_sum[BWD ? kWarps : 1][BWD ? kMaxWidth : 1];
+    const int m = (int)blockIdx.x >= a.side[0].ctas, i = blockIdx.y;
+    const Side& side = a.side[m];
+    const int b = blockIdx.x - (m ? a.side[0].ctas : 0);
+    const long long t0 = a.n * b / side.ctas, t1 = a.n * (b + 1) / side.ctas;
+    const int lane = threadIdx.x % TEAM, group = threadIdx.x % 32 / TEAM, warp = threadIdx.x >> 5;
+    const bool normed = side.w.p != nullptr;
+    float w[NS][2][VEC], dw[BWD ? NS : 1][2][VEC];
     int at[NS][2];
-    bool turned[NS], here[NS][2];
+    bool here[NS][2];
 #pragma unroll
     for (int z = 0; z < NS; ++z) {
-        const int s = z * a.team + lane;
-        slot_place<VEC>(a, s, at[z][0], at[z][1], turned[z]);
+        const int s = z * TEAM + lane;
+        if (a.interleaved) {
+            at[z][0] = 2 * s * VEC;
+            at[z][1] = at[z][0] + VEC;
+        } else {
+            const int lead = a.half / VEC;                   // slots that turn
+            at[z][0] = s < lead ? s * VEC : a.rotary + 2 * (s - lead) * VEC;
+            at[z][1] = s < lead ? a.half + s * VEC : at[z][0] + VEC;
+        }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) here[z][k] = s < a.slots && at[z][k] < a.d;
-        turned[z] = turned[z] && here[z][0];
+        for (int k = 0; k < 2; ++k) {
+            here[z][k] = s < a.slots && at[z][k] < a.d;
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+            for (int e = 0; e < VEC; ++e) {
+                w[z][k][e] = normed && here[z][k] ? to_f32(static_cast<const T*>(side.w.p)[i * side.w.rep + at[z][k] + e]) : 1.f;
+                if (BWD) dw[z][k][e] = 0.f;
+            }
+        }
+    }
+    const int part = warp % side.split, H = side.heads;
+    for (long long t = t0 + warp / side.split; t < t1; t += kWarps / side.split) {
+        // this place's cosines and sines: pair q of a thread is formed by team q % GROUPS
+        float2 cs[PAIRS];
+        if (a.half > 0) {
+            const long long u = i * a.pos_rep + t * a.pos_step;
+            const double pos = !a.positions ? (double)t
+                               : a.wide     ? (double)__ldg(static_cast<const long long*>(a.positions) + u)
+                                            : (double)__ldg(static_cast<const int*>(a.positions) + u);
+            float2 own[(PAIRS + GROUPS - 1) / GROUPS];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    w[m][z][k][e] = a.w[m].p && here[z][k] ? to_f32(static_cast<const T*>(a.w[m].p)[i * a.w[m].rep + at[z][k] + e]) : 1.f;
-                    if (BWD) dw[m][z][k][e] = 0.f;
+            for (int q = 0; q < (PAIRS + GROUPS - 1) / GROUPS; ++q) {
+                const int pair = q * GROUPS + group, z = pair / VEC, e = pair % VEC, s = z * TEAM + lane;
+                const int j = s * VEC + e;
+                own[q] = make_float2(1.f, 0.f);
+                if (pair < PAIRS && j < a.half) {
+                    double x = pos * a.turns[j];
+                    x -= rint(x);
+                    const float hi = (float)x, lo = (float)(x - (double)hi) * 6.283185307179586f;
+                    float sn, c;
+                    sincospif(2.f * hi, &sn, &c);
+                    own[q] = make_float2(fmaf(-lo, sn, c), fmaf(lo, c, sn));
                 }
             }
-    }
-    for (long long t = t0; t < t1; t += a.tile) {
-        const int places = (int)(t1 - t < a.tile ? t1 - t : a.tile);
-        if (t > t0) __syncthreads();
-        for (int q = threadIdx.x; q < places * a.table; q += kThreads) {
-            const int place = q / a.table, j = q - place * a.table;
-            float2 cs = make_float2(1.f, 0.f);
-            if (j < a.half) {
-                const long long u = i * a.pos_rep + (t + place) * a.pos_step;
-                const double pos = !a.positions ? (double)(t + place)
-                                   : a.wide     ? (double)__ldg(static_cast<const long long*>(a.positions) + u)
-                                                : (double)__ldg(static_cast<const int*>(a.positions) + u);
-                double x = pos * a.turns[j];
-                x -= rint(x);
-                const float hi = (float)x, lo = (float)(x - (double)hi) * 6.283185307179586f;
-                float s, c;
-                sincospif(2.f * hi, &s, &c);
-                cs = make_float2(fmaf(-lo, s, c), fmaf(lo, c, s));
-            }
-            s_table[q] = cs;
-        }
-        __syncthreads();
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int H = a.heads[m], rows = places * H;
-            const bool normed = a.w[m].p != nullptr;
-            // every group makes the same number of turns: the groups of a warp shuffle together
-#pragma unroll 2
-            for (int base = 0; base < rows; base += groups) {
-                const int r = base + group;
-                const bool active = r < rows;
-                const int place = active ? r / H : 0, h = active ? r - place * H : 0;
-                const float2* table = s_table + place * a.table;
-                float x[NS][2][VEC], g[BWD ? NS : 1][2][VEC];
-                const T* from = head_at<T>(a.x[m], i, t + place, h);
-                const T* grad = BWD ? head_at<T>(a.d_out[m], i, t + place, h) : nullptr;
+            for (int q = 0; q < PAIRS; ++q) {
+                if constexpr (GROUPS == 1) {
+                    cs[q] = own[q];
+                } else {
+                    const int from = q % GROUPS * TEAM + lane;
+                    cs[q] = make_float2(__shfl_sync(0xffffffffu, own[q / GROUPS].x, from), __shfl_sync(0xffffffffu, own[q / GROUPS].y, from));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < PAIRS; ++q) cs[q] = make_float2(1.f, 0.f);
+        }
+        const T* const x0 = head_at<T>(side.x, i, t, 0);
+        const T* const g0 = BWD ? head_at<T>(side.d_out, i, t, 0) : nullptr;
+        T* const o0 = side.out.p ? head_at<T>(side.out, i, t, 0) : nullptr;
+        // every team makes the same number of turns: they shuffle together.  The loads of AHEAD turns come before the first one's
+        // stores (results may lie where inputs do, so the compiler cannot move them).
+        const int turns = (H - part * GROUPS + side.split * GROUPS - 1) / (side.split * GROUPS);
+        for (int q0 = 0; q0 < turns; q0 += AHEAD) {
+            Packed<T, VEC> px[AHEAD][NS][2], pg[BWD ? AHEAD : 1][BWD ? NS : 1][2];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                const int h = (part + (q0 + q) * side.split) * GROUPS + group;
 #pragma unroll
                 for (int z = 0; z < NS; ++z)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            x[z][k][e] = 0.f;
-                            if (BWD) g[z][k][e] = 0.f;
-                        }
-                        if (active && here[z][k]) {
-                            load_vec<T, VEC>(from + at[z][k], x[z][k]);
-                            if (BWD) load_vec<T, VEC>(grad + at[z][k], g[z][k]);
+                        px[q][z][k].clear();
+                        if (BWD) pg[q][z][k].clear();
+                        if (h < H && here[z][k]) {
+                            px[q][z][k].load(x0 + h * side.x.head + at[z][k]);
+                            if (BWD) pg[q][z][k].load(g0 + h * side.d_out.head + at[z][k]);
                         }
                     }
-                float square = 0.f, along = 0.f;
-#pragma unroll
-                for (int z = 0; z < NS; ++z) {
-                    if (BWD) turn_slot<VEC, true>(a, z * a.team + lane, turned[z], here[z][1], table, g[z]);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            square = fmaf(x[z][k][e], x[z][k][e], square);
-                            if (BWD) along = fmaf(g[z][k][e] * w[m][z][k][e], x[z][k][e], along);
-                        }
-                }
-                float inv = 1.f;
-                if (normed) inv = 1.f / sqrtf(fmaf(team_sum(square, a.team), a.inv_d, a.eps));
-                if (!active) inv = 0.f;                      // (eps may be 0: no infinity times the zeros of a missing row)
-                if constexpr (!BWD) {
-                    T* to = head_at<T>(a.out[m], i, t + place, h);
-#pragma unroll
-                    for (int z = 0; z < NS; ++z) {
-#pragma unroll
-                        for (int k = 0; k < 2; ++k)
-#pragma unroll
-                            for (int e = 0; e < VEC; ++e) x[z][k][e] *= inv * w[m][z][k][e];
-                        turn_slot<VEC, false>(a, z * a.team + lane, turned[z], here[z][1], table, x[z]);
-#pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            if (active && here[z][k]) store_vec<T, VEC>(to + at[z][k], x[z][k]);
-                    }
-                } else {
-                    float back = 0.f;
-                    if (normed) back = team_sum(along, a.team) * a.inv_d * inv * inv;
-                    T* to = a.out[m].p ? head_at<T>(a.out[m], i, t + place, h) : nullptr;
-#pragma unroll
-                    for (int z = 0; z < NS; ++z)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            float dx[VEC];
-#pragma unroll
-                            for (int e = 0; e < VEC; ++e) {
-                                dw[m][z][k][e] = fmaf(g[z][k][e], x[z][k][e] * inv, dw[m][z][k][e]);
-                                dx[e] = inv * fmaf(-back, x[z][k][e], g[z][k][e] * w[m][z][k][e]);
-                            }
-                            if (to && active && here[z][k]) store_vec<T, VEC>(to + at[z][k], dx);
-                        }
-                }
             }
-        }
-    }
-    if constexpr (BWD) {
-        // sums of the CTA: over the groups of a warp, then over the warps
-        if (!a.partial) return;
-        for (int m = 0; m < 2; ++m) {
-            __syncthreads();
+#pragma unroll
+          for (int q = 0; q < AHEAD; ++q) {
+            const int h = (part + (q0 + q) * side.split) * GROUPS + group;
+            const bool active = h < H;
+            float x[NS][2][VEC], g[BWD ? NS : 1][2][VEC];
 #pragma unroll
             for (int z = 0; z < NS; ++z)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    px[q][z][k].widen(x[z][k]);
+                    if (BWD) pg[q][z][k].widen(g[z][k]);
+                }
+            float square = 0.f, along = 0.f;
+#pragma unroll
+            for (int z = 0; z < NS; ++z) {
+                if (BWD) turn_slot<VEC, true>(a.interleaved, cs + z * VEC, g[z]);
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        float v = m == 0 ? dw[0][z][k][e] : dw[1][z][k][e];
-                        for (int o = a.team; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                        if ((threadIdx.x & 31) < a.team && here[z][k]) s_sum[threadIdx.x >> 5][at[z][k] + e] = v;
+                        square = fmaf(x[z][k][e], x[z][k][e], square);
+                        if (BWD) along = fmaf(g[z][k][e] * w[z][k][e], x[z][k][e], along);
                     }
-            __syncthreads();
-            float* to = a.partial + (((long long)i * a.ctas + b) * 2 + m) * a.d;
-            for (int c = threadIdx.x; c < a.d; c += kThreads) {
-                float v = 0.f;
-#pragma unroll
-                for (int q = 0; q < kThreads / 32; ++q) v += s_sum[q][c];
-                to[c] = v;
             }
+            float inv = 1.f;
+            if (normed) inv = 1.f / sqrtf(fmaf(team_sum<TEAM>(square), a.inv_d, a.eps));
+            if (!active) inv = 0.f;                          // (eps may be 0: no infinity times the zeros of a missing row)
+            if constexpr (!BWD) {
+#pragma unroll
+                for (int z = 0; z < NS; ++z) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) x[z][k][e] *= inv * w[z][k][e];
+                    turn_slot<VEC, false>(a.interleaved, cs + z * VEC, x[z]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        if (active && here[z][k]) store_some<T, VEC>(o0 + h * side.out.head + at[z][k], x[z][k]);
+                }
+            } else {
+                float back = 0.f;
+                if (normed) back = team_sum<TEAM>(along) * a.inv_d * inv * inv;
+#pragma unroll
+                for (int z = 0; z < NS; ++z)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float dx[VEC];
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            dw[z][k][e] = fmaf(g[z][k][e], x[z][k][e] * inv, dw[z][k][e]);
+                            dx[e] = inv * fmaf(-back, x[z][k][e], g[z][k][e] * w[z][k][e]);
+                        }
+                        if (o0 && active && here[z][k]) store_some<T, VEC>(o0 + h * side.out.head + at[z][k], dx);
+                    }
+            }
+          }
+        }
+    }
+    if constexpr (BWD) {
+        // sums of the CTA: over the teams of a warp, then over the warps
+        if (!side.partial) return;
+#pragma unroll
+        for (int z = 0; z < NS; ++z)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    float v = dw[z][k][e];
+#pragma unroll
+                    for (int o = TEAM; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                    if (group == 0 && here[z][k]) s_sum[warp][at[z][k] + e] = v;
+                }
+        __syncthreads();
+        float* to = side.partial + ((long long)i * side.ctas + b) * a.d;
+        for (int c = threadIdx.x; c < a.d; c += kThreads) {
+            float v = 0.f;
+#pragma unroll
+            for (int q = 0; q < kWarps; ++q) v += s_sum[q][c];
+            to[c] = v;
         }
     }
 }
@@ -262,18 +314,19 @@ template <typename T> __global__ void __launch_bounds__(256) k_head_sums(const _
     const int c = blockIdx.x * 32 + threadIdx.x % 32, part = threadIdx.x / 32, i = blockIdx.y, m = blockIdx.z;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     float v = 0.f;
+    const Vec to = m ? d_k : d_q;
+    if (!to.p) return;
     if (c < a.d && a.n > 0) {
-        const float* p = a.partial + ((long long)i * a.ctas * 2 + m) * a.d + c;
+        const float* p = a.side[m].partial + (long long)i * a.side[m].ctas * a.d + c;
 #pragma unroll 8
-        for (int b = part; b < a.ctas; b += 8) v += p[(long long)b * 2 * a.d];
+        for (int b = part; b < a.side[m].ctas; b += 8) v += p[(long long)b * a.d];
     }
     s_part[part][threadIdx.x % 32] = v;
     __syncthreads();
     if (part != 0 || c >= a.d) return;
 #pragma unroll
     for (int q = 1; q < 8; ++q) v += s_part[q][threadIdx.x];
-    const Vec to = m ? d_k : d_q;
-    if (to.p) static_cast<T*>(to.p)[i * to.rep + c] = from_f32<T>(v);
+    static_cast<T*>(to.p)[i * to.rep + c] = from_f32<T>(v);
 }
 
 // ----------------------------------------------------------------------------------- host
@@ -307,9 +360,10 @@ bool usable(const eg_heads& m, int64_t P, int64_t rows, int64_t H, int64_t width
         if (s < 0 || s >= (1ll << 42)) return false;
     return !written || apart(m, P, rows, H, width);
 }
-bool whole_vectors(const eg_heads& m, int64_t P, int64_t rows, int64_t H, size_t size) {
-    return !m.data || (aligned16(m.data) && (P <= 1 || m.replica_stride * (int64_t)size % 16 == 0) &&
-                       (rows <= 1 || m.row_stride * (int64_t)size % 16 == 0) && (H <= 1 || m.head_stride * (int64_t)size % 16 == 0));
+// Whether every row begins on a multiple of so many bytes.
+bool begins_on(const eg_heads& m, int64_t P, int64_t rows, int64_t H, size_t size, size_t bytes) {
+    return !m.data || ((uintptr_t)m.data % bytes == 0 && (P <= 1 || m.replica_stride * size % bytes == 0) &&
+                       (rows <= 1 || m.row_stride * size % bytes == 0) && (H <= 1 || m.head_stride * size % bytes == 0));
 }
 
 bool valid(const eg_head_norm_args* q, bool backward) {
@@ -342,72 +396,90 @@ bool valid(const eg_head_norm_args* q, bool backward) {
     return true;
 }
 
-// CTAs of a replica; bounds the workspace too.
-int ctas_of(int64_t P, int64_t rows) {
-    const int64_t all = (int64_t)sm_count() * kCtasPerSm;
-    int64_t each = all / P > 1 ? all / P : 1;
-    if (each > rows) each = rows > 0 ? rows : 1;
-    return (int)each;
+// CTAs of a replica for one side; bounds the workspace too.
+int ctas_of(int64_t P, int64_t rows, int64_t mine, int64_t other) {
+    if (mine == 0) return 0;
+    // both sides' warps take as long: their heads, and a place's sines (as long as about four)
+    const double share = (double)(mine + 4) / (double)(mine + 4 + (other ? other + 4 : 0));
+    int64_t each = (int64_t)((double)(sm_count() * kCtasPerSm) * share / (double)P);
+    if (each > (rows + 1) / 2) each = (rows + 1) / 2;
+    return (int)(each > 1 ? each : 1);
 }
 
-// Fills the arguments; returns whether 16-byte vectors serve every row.
-bool fill(HeadArgs* a, const eg_head_norm_args* q, bool backward) {
+struct Sizes {
+    int ctas[2];
+    int64_t bytes;
+};
+Sizes sizes_of(const eg_head_norm_args* q) {
+    Sizes s;
+    s.ctas[0] = ctas_of(q->P, q->rows, q->q_heads, q->k_heads);
+    s.ctas[1] = ctas_of(q->P, q->rows, q->k_heads, q->q_heads);
+    s.bytes = q->P * (int64_t)(s.ctas[0] + s.ctas[1]) * q->width * 4;
+    return s;
+}
+
+// Fills the arguments; returns how many values an access takes: 16 bytes, 2 values, 1.
+int fill(HeadArgs* a, const eg_head_norm_args* q, bool backward, float* partial) {
     *a = HeadArgs{};
     a->P = (int)q->P; a->n = q->rows; a->d = (int)q->width; a->rotary = (int)q->rotary; a->half = a->rotary / 2;
     a->interleaved = q->interleaved != 0;
     a->eps = (float)q->eps; a->inv_d = 1.f / (float)q->width;
     a->positions = q->positions; a->pos_rep = q->position_replica_stride; a->pos_step = q->position_stride;
     a->wide = q->position_bytes == 8;
-    a->heads[0] = (int)q->q_heads; a->heads[1] = (int)q->k_heads;
-    a->x[0] = heads(q->q); a->x[1] = heads(q->k);
-    a->out[0] = heads(backward ? q->dq : q->q_out); a->out[1] = heads(backward ? q->dk : q->k_out);
-    a->d_out[0] = heads(q->dq_out); a->d_out[1] = heads(q->dk_out);
-    a->w[0] = Vec{q->w_q.data, (long long)q->w_q.replica_stride};
-    a->w[1] = Vec{q->w_k.data, (long long)q->w_k.replica_stride};
+    const Sizes n = sizes_of(q);
+    const size_t size = q->dtype == EG_F32 ? 4 : 2;
+    const struct { const eg_heads *x, *out, *d_out; const eg_matrix *w, *dw; int64_t H; } both[] = {
+        {&q->q, backward ? &q->dq : &q->q_out, &q->dq_out, &q->w_q, &q->d_w_q, q->q_heads},
+        {&q->k, backward ? &q->dk : &q->k_out, &q->dk_out, &q->w_k, &q->d_w_k, q->k_heads}};
+    auto serves = [&](int v) {
+        if (a->d % v || (!a->interleaved && a->half % v)) return false;
+        for (const auto& b : both) {
+            if (b.H == 0) continue;
+            for (const eg_heads* m : {b.x, b.out, b.d_out})
+                if ((m != b.d_out || backward) && !begins_on(*m, q->P, q->rows, b.H, size, v * size)) return false;
+        }
+        return true;
+    };
+    const int v = serves(16 / (int)size) ? 16 / (int)size : serves(2) ? 2 : 1;
+    a->slots = a->interleaved ? (a->d + 2 * v - 1) / (2 * v) : a->half / v + (a->d - a->rotary + 2 * v - 1) / (2 * v);
+    for (int m = 0; m < 2; ++m) {
+        Side* s = &a->side[m];
+        s->heads = (int)both[m].H;
+        s->ctas = n.ctas[m];
+        // few places of a CTA: warps share their heads
+        const int64_t places = s->ctas ? (q->rows + s->ctas - 1) / s->ctas : 1;
+        s->split = 1;
+        while (s->split < kWarps && places * s->split < kWarps) s->split *= 2;
+        s->x = heads(*both[m].x); s->out = heads(*both[m].out); s->d_out = heads(*both[m].d_out);
+        s->w = Vec{both[m].w->data, (long long)both[m].w->replica_stride};
+        s->partial = backward && both[m].dw->data ? partial + (m ? q->P * (int64_t)n.ctas[0] * q->width : 0) : nullptr;
+    }
     const double full = 6.283185307179586476925;
     const double step = a->rotary > 0 ? -2.0 * log(q->base) / a->rotary : 0.0;
     for (int j = 0; j < a->half; ++j) a->turns[j] = exp(step * j) / full;
-    a->ctas = ctas_of(q->P, q->rows);
-    const size_t size = q->dtype == EG_F32 ? 4 : 2;
-    const int V = 16 / (int)size;
-    bool vec = a->d % V == 0 && (a->interleaved || (a->half % V == 0 && a->rotary % V == 0));
-    const struct { const eg_heads *x, *out, *d_out; int64_t H; } both[] = {{&q->q, backward ? &q->dq : &q->q_out, &q->dq_out, q->q_heads},
-                                                                          {&q->k, backward ? &q->dk : &q->k_out, &q->dk_out, q->k_heads}};
-    for (const auto& b : both) {
-        if (b.H == 0) continue;
-        vec = vec && whole_vectors(*b.x, q->P, q->rows, b.H, size) && whole_vectors(*b.out, q->P, q->rows, b.H, size) &&
-              (!backward || whole_vectors(*b.d_out, q->P, q->rows, b.H, size));
-    }
-    const int v = vec ? V : 1;
-    if (a->interleaved) {
-        // single values: the slot's two are neighbours, (2 s, 2 s + 1)
-        a->slots = (a->d + 2 * v - 1) / (2 * v);
-        a->table = (a->d + 1) / 2;
-    } else {
-        a->slots = a->half / v + (a->d - a->rotary + 2 * v - 1) / (2 * v);
-        a->table = a->half;
-    }
-    a->team = 1;
-    while (a->team < 32 && a->team < a->slots) a->team *= 2;
-    a->tile = kMaxTile;
-    while (a->tile > 1 && a->tile * a->table > kTableMax) a->tile /= 2;
-    return vec;
+    return v;
 }
 
-template <typename T, bool BWD> cudaError_t launch(const HeadArgs& a, bool vec, cudaStream_t stream) {
+template <typename T, bool BWD> cudaError_t launch(const HeadArgs& a, int v, cudaStream_t stream) {
     constexpr int V = 16 / (int)sizeof(T);
-    const dim3 grid(a.ctas, a.P);
-    static_assert(kMaxWidth / (2 * V) <= 32 && kMaxWidth / 2 <= 4 * 32, "slots of a row");
-    if (vec) return launch_after(k_head_norm<T, V, 1, BWD>, grid, dim3(kThreads), 0, stream, a);
-    if (a.slots <= 32) return launch_after(k_head_norm<T, 1, 1, BWD>, grid, dim3(kThreads), 0, stream, a);
-    if (a.slots <= 64) return launch_after(k_head_norm<T, 1, 2, BWD>, grid, dim3(kThreads), 0, stream, a);
-    return launch_after(k_head_norm<T, 1, 4, BWD>, grid, dim3(kThreads), 0, stream, a);
+    const dim3 grid(a.side[0].ctas + a.side[1].ctas, a.P);
+    auto run = [&](auto kernel) { return launch_after(kernel, grid, dim3(kThreads), 0, stream, a); };
+    static_assert(kMaxWidth / (2 * V) <= 32 && kMaxWidth / 4 <= 2 * 32 && kMaxWidth / 2 <= 4 * 32, "slots of a row");
+    if (v == V) {
+        if (a.slots <= 2) return run(k_head_norm<T, V, 1, 2, BWD>);
+        if (a.slots <= 4) return run(k_head_norm<T, V, 1, 4, BWD>);
+        if (a.slots <= 8) return run(k_head_norm<T, V, 1, 8, BWD>);
+        if (a.slots <= 16) return run(k_head_norm<T, V, 1, 16, BWD>);
+        return run(k_head_norm<T, V, 1, 32, BWD>);
+    }
+    if (v == 2) return a.slots <= 32 ? run(k_head_norm<T, 2, 1, 32, BWD>) : run(k_head_norm<T, 2, 2, 32, BWD>);
+    if (a.slots <= 32) return run(k_head_norm<T, 1, 1, 32, BWD>);
+    return a.slots <= 64 ? run(k_head_norm<T, 1, 2, 32, BWD>) : run(k_head_norm<T, 1, 4, 32, BWD>);
 }
 
-template <typename T> cudaError_t backward(HeadArgs a, bool vec, const eg_head_norm_args* q, cudaStream_t stream) {
-    if (!q->d_w_q.data && !q->d_w_k.data) a.partial = nullptr;
+template <typename T> cudaError_t backward(const HeadArgs& a, int v, const eg_head_norm_args* q, cudaStream_t stream) {
     if (a.n > 0) {
-        const cudaError_t e = launch<T, true>(a, vec, stream);
+        const cudaError_t e = launch<T, true>(a, v, stream);
         if (e != cudaSuccess) return e;
     }
     if (!q->d_w_q.data && !q->d_w_k.data) return cudaSuccess;
@@ -427,17 +499,17 @@ eg_status eg_head_norm(const eg_head_norm_args* q, void* stream_v) {
     if (q->rows == 0) return EG_OK;
     if (sm_count() < 1) return EG_ERR_CUDA;
     HeadArgs a;
-    const bool vec = fill(&a, q, false);
+    const int v = fill(&a, q, false, nullptr);
     cudaStream_t s = static_cast<cudaStream_t>(stream_v);
-    const cudaError_t e = q->dtype == EG_F32    ? launch<float, false>(a, vec, s)
-                          : q->dtype == EG_BF16 ? launch<__nv_bfloat16, false>(a, vec, s)
-                                                : launch<__half, false>(a, vec, s);
+    const cudaError_t e = q->dtype == EG_F32    ? launch<float, false>(a, v, s)
+                          : q->dtype == EG_BF16 ? launch<__nv_bfloat16, false>(a, v, s)
+                                                : launch<__half, false>(a, v, s);
     return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
 }
 
 int64_t eg_head_norm_workspace(const eg_head_norm_args* q) {
     if (!valid(q, true) || sm_count() < 1) return 0;
-    return q->P * (int64_t)ctas_of(q->P, q->rows) * 2 * q->width * 4;
+    return sizes_of(q).bytes;
 }
 
 eg_status eg_head_norm_backward(const eg_head_norm_args* q, void* workspace, int64_t workspace_bytes, void* stream_v) {
@@ -445,12 +517,11 @@ eg_status eg_head_norm_backward(const eg_head_norm_args* q, void* workspace, int
     if (sm_count() < 1) return EG_ERR_CUDA;
     if (!workspace || !aligned16(workspace) || workspace_bytes < eg_head_norm_workspace(q)) return EG_ERR_INVALID;
     HeadArgs a;
-    const bool vec = fill(&a, q, true);
-    a.partial = static_cast<float*>(workspace);
+    const int v = fill(&a, q, true, static_cast<float*>(workspace));
     cudaStream_t s = static_cast<cudaStream_t>(stream_v);
-    const cudaError_t e = q->dtype == EG_F32    ? backward<float>(a, vec, q, s)
-                          : q->dtype == EG_BF16 ? backward<__nv_bfloat16>(a, vec, q, s)
-                                                : backward<__half>(a, vec, q, s);
+    const cudaError_t e = q->dtype == EG_F32    ? backward<float>(a, v, q, s)
+                          : q->dtype == EG_BF16 ? backward<__nv_bfloat16>(a, v, q, s)
+                                                : backward<__half>(a, v, q, s);
     return e == cudaSuccess ? EG_OK : EG_ERR_CUDA;
 }
 
