@@ -52,12 +52,23 @@ struct EmbedArgs {
     float* partial;                        // [P][chunks][2][pitch]: of a run from the chunk before, of one into the next
 };
 
-// The token at place t, -1 where it is none of the table's.
-__device__ __forceinline__ int token_at(const EmbedArgs& a, int i, long long t) {
-    const long long at = i * a.token_rep + t * a.token_step;
-    const long long v = a.wide ? __ldg(static_cast<const long long*>(a.tokens) + at) : (long long)__ldg(static_cast<const int*>(a.tokens) + at);
-    return v >= 0 && v < a.V ? (int)v : -1;
-}
+// The token at place t of replica i, -1 where it is none of the table's.
+struct Tokens {
+    const char* p;
+    long long step;                        // bytes
+    int wide;
+    unsigned V;
+    __device__ __forceinline__ Tokens(const EmbedArgs& a, int i)
+        : p(static_cast<const char*>(a.tokens) + i * a.token_rep * (a.wide ? 8 : 4)), step(a.token_step * (a.wide ? 8 : 4)), wide(a.wide), V((unsigned)a.V) {}
+    __device__ __forceinline__ int at(long long t) const {
+        if (wide) {
+            const unsigned long long v = __ldg(reinterpret_cast<const unsigned long long*>(p + t * step));
+            return v < V ? (int)v : -1;
+        }
+        const unsigned v = __ldg(reinterpret_cast<const unsigned*>(p + t * step));
+        return v < V ? (int)v : -1;
+    }
+};
 template <typename T> __device__ __forceinline__ T* row_of(const Rows& m, int i, long long t) {
     return static_cast<T*>(m.p) + (long long)i * m.rep + t * m.row;
 }
@@ -74,7 +85,7 @@ __global__ void __launch_bounds__(256) k_embed(const __grid_constant__ EmbedArgs
     const long long line = unit / slices;
     const int i = (int)(line / a.n);
     const long long t = line - i * a.n;
-    const int c0 = (int)(unit - line * slices) * 32 * U * VEC, token = token_at(a, i, t);
+    const int c0 = (int)(unit - line * slices) * 32 * U * VEC, token = Tokens(a, i).at(t);
     float v[U][VEC];
     const T* from = row_of<T>(a.weight, i, token < 0 ? 0 : token);
     T* to = row_of<T>(a.out, i, t);
@@ -124,16 +135,18 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_consta
     constexpr int SCAN = 8;
     const long long each = ((a.n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
     const long long t0 = warp * each, t1 = t0 + each < a.n ? t0 + each : a.n;
+    const Tokens tokens(a, i);
+    const int first_row = (int)first;
     int below = 0;
     for (long long t = t0; t < t1; t += 32 * SCAN) {
         int v[SCAN];
 #pragma unroll
-        for (int u = 0; u < SCAN; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
+        for (int u = 0; u < SCAN; ++u) v[u] = t + u * 32 + lane < t1 ? tokens.at(t + u * 32 + lane) : -1;
 #pragma unroll
         for (int u = 0; u < SCAN; ++u) {
-            const long long at = v[u] - first;
-            below += v[u] >= 0 && at < 0;
-            if (v[u] >= 0 && at >= 0 && at < mine) atomicAdd(&s_at[warp][at], 1);
+            const unsigned at = (unsigned)(v[u] - first_row);
+            below += v[u] >= 0 && v[u] < first_row;
+            if (v[u] >= 0 && at < (unsigned)mine) atomicAdd(&s_at[warp][at], 1);
         }
     }
     const int base = block_total(below, s_red);          // (its barriers also end the counting)
@@ -177,11 +190,11 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_consta
         for (long long t = t0; t < t1; t += 32 * SCAN) {
             int v[SCAN];
 #pragma unroll
-            for (int u = 0; u < SCAN; ++u) v[u] = t + u * 32 + lane < t1 ? token_at(a, i, t + u * 32 + lane) : -1;
+            for (int u = 0; u < SCAN; ++u) v[u] = t + u * 32 + lane < t1 ? tokens.at(t + u * 32 + lane) : -1;
 #pragma unroll
             for (int u = 0; u < SCAN; ++u) {
-                const long long rel = v[u] - first;
-                const bool in = v[u] >= 0 && rel >= 0 && rel < mine;
+                const unsigned rel = (unsigned)(v[u] - first_row);
+                const bool in = v[u] >= 0 && rel < (unsigned)mine;
                 if (!__any_sync(0xffffffffu, in)) continue;
                 const unsigned same = __match_any_sync(0xffffffffu, in ? v[u] : -1);
                 const int rank = __popc(same & ((1u << lane) - 1));
@@ -234,10 +247,10 @@ template <typename T> struct Raw<T, 1> {
 };
 
 // A warp: one chunk of the sorted list, 32 * U vectors of columns; or zeros for rows without a place.
-template <typename T, int VEC, int U> __global__ void __launch_bounds__(256) k_embed_sum(const __grid_constant__ EmbedArgs a, int slices) {
+template <typename T, int VEC, int U> __global__ void __launch_bounds__(256, 4) k_embed_sum(const __grid_constant__ EmbedArgs a, int slices) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    constexpr int AHEAD = 8 / U;                         // rows on their way at once
+    constexpr int AHEAD = 4;                             // rows on their way at once
     const int lane = threadIdx.x & 31, i = blockIdx.y;
     if ((int)blockIdx.x >= a.sum_blocks) {
         const float zero[VEC] = {};
@@ -310,18 +323,15 @@ template <typename T, int VEC, int U> __global__ void __launch_bounds__(256) k_e
     }
 }
 
-// A warp: the run that begins in one chunk and goes on into the next, 32 * 4 columns.
-template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ EmbedArgs a, int slices) {
+// A block: the run that begins in one chunk and goes on into the next, 4 columns a thread.
+template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ EmbedArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int AHEAD = 8;
     const int lane = threadIdx.x & 31, i = blockIdx.y;
-    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const long long chunk = unit / slices;
-    if (chunk >= a.chunks) return;
-    const int c = ((int)(unit - chunk * slices) * 32 + lane) * 4, count = a.count[i];
-    const long long first = chunk * a.chunk, end = first + a.chunk;
-    if (end >= count) return;
+    const long long chunk = blockIdx.x, first = chunk * a.chunk, end = first + a.chunk;
     const int* key = a.key + i * a.n;
+    const int count = a.count[i];
+    if (end >= count) return;
     const int token = key[end - 1], next = key[end], before = first > 0 ? key[first - 1] : -1;
     if (next != token || before == token) return;
     // chunks that the run goes on through: those that begin with its token
@@ -334,26 +344,27 @@ template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const 
             break;
         }
     }
-    if (c >= a.d) return;
-    const float* partial = a.partial + ((long long)i * a.chunks + chunk) * 2 * a.pitch + c;
-    float sum[4];
-    load_vec<float, 4>(partial + a.pitch, sum);
-    for (long long q = 1; q <= more; q += AHEAD) {
-        float v[AHEAD][4];
+    for (int c = threadIdx.x * 4; c < a.d; c += 1024) {
+        const float* partial = a.partial + ((long long)i * a.chunks + chunk) * 2 * a.pitch + c;
+        float sum[4];
+        load_vec<float, 4>(partial + a.pitch, sum);
+        for (long long q = 1; q <= more; q += AHEAD) {
+            float v[AHEAD][4];
 #pragma unroll
-        for (int h = 0; h < AHEAD; ++h) {
+            for (int h = 0; h < AHEAD; ++h) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[h][e] = 0.f;
-            if (q + h <= more) load_vec<float, 4>(partial + (q + h) * 2 * a.pitch, v[h]);
+                for (int e = 0; e < 4; ++e) v[h][e] = 0.f;
+                if (q + h <= more) load_vec<float, 4>(partial + (q + h) * 2 * a.pitch, v[h]);
+            }
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += v[h][e];
         }
 #pragma unroll
-        for (int h = 0; h < AHEAD; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += v[h][e];
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.d) finish<T, 1>(a, i, token, c + e, sum + e);
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < a.d) finish<T, 1>(a, i, token, c + e, sum + e);
 }
 
 // ----------------------------------------------------------------------------------- host
@@ -460,7 +471,7 @@ template <typename T, int VEC> cudaError_t backward(EmbedArgs a, cudaStream_t st
     }
     auto blocks = [&](int slices) { return (unsigned)(((long long)a.chunks * slices + 7) / 8); };
     constexpr int U = VEC > 1 ? 1 : 4;
-    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC), narrow = (a.d + 127) / 128;
+    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC);
     a.sum_blocks = a.n > 0 ? (int)blocks(slices) : 0;
     // zeros: 64 KB or so a block, at least a few blocks for every multiprocessor
     long long zeros = 0;
@@ -472,7 +483,7 @@ template <typename T, int VEC> cudaError_t backward(EmbedArgs a, cudaStream_t st
     }
     e = launch_after(k_embed_sum<T, VEC, U>, dim3((unsigned)(a.sum_blocks + zeros), a.P), dim3(256), 0, stream, a, slices);
     if (e != cudaSuccess || a.n == 0 || a.chunks == 1) return e;
-    return launch_after(k_embed_join<T>, dim3(blocks(narrow), a.P), dim3(256), 0, stream, a, narrow);
+    return launch_after(k_embed_join<T>, dim3((unsigned)a.chunks, a.P), dim3(256), 0, stream, a);
 }
 
 }  // namespace
@@ -521,7 +532,7 @@ eg_status eg_embedding_backward(const eg_embedding_args* q, void* workspace, int
     a.chunk = l.chunk; a.chunks = l.chunks; a.pitch = l.pitch;
     // ranges long enough that the tokens are not read more often than needed, short enough that every multiprocessor has some
     a.range = kRangeMax;
-    while (a.range > 64 && a.P * ((a.V + a.range - 1) / a.range) < 4ll * sms) a.range /= 2;
+    while (a.range > 64 && a.P * ((a.V + a.range - 1) / a.range) < sms) a.range /= 2;
     const size_t size = q->dtype == EG_F32 ? 4 : 2;
     const bool vec = q->width * size % 16 == 0 && (q->rows == 0 || whole_vectors(q->dy, q->P, q->rows, size)) &&
                      whole_vectors(q->d_weight, q->P, q->vocabulary, size);

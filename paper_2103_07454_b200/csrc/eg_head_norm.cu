@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxWidth = EG_HEAD_MAX_WIDTH, kMaxPairs = kMaxWidth / 2;
-constexpr int kCtasPerSm = 4;
+constexpr int kCtasForward = 3, kCtasBackward = 2;      // of a multiprocessor: all resident at once
 
 struct Heads {
     void* p;
@@ -130,7 +130,7 @@ template <int TEAM> __device__ __forceinline__ float team_sum(float v) {
 
 // NS: slots of a thread; TEAM: threads of a row.
 template <typename T, int VEC, int NS, int TEAM, bool BWD>
-__global__ void __launch_bounds__(kThreads, BWD ? 2 : 3) k_head_norm(const __grid_constant__ HeadArgs a) {
+__global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) k_head_norm(const __grid_constant__ HeadArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     constexpr int GROUPS = 32 / TEAM, PAIRS = NS * VEC, AHEAD = NS > 2 ? 1 : 2;
@@ -165,29 +165,32 @@ __global__ void __launch_bounds__(kThreads, BWD ? 2 : 3) k_head_norm(const __gri
             }
         }
     }
+    // pair q of a thread is formed by team q % GROUPS; the turns of those that this one forms
+    constexpr int OWN = (PAIRS + GROUPS - 1) / GROUPS;
+    double turns_of[OWN];
+#pragma unroll
+    for (int q = 0; q < OWN; ++q) {
+        const int pair = q * GROUPS + group, j = (pair / VEC * TEAM + lane) * VEC + pair % VEC;
+        turns_of[q] = pair < PAIRS && j < a.half ? a.turns[j] : 0.0;
+    }
     const int part = warp % side.split, H = side.heads;
     for (long long t = t0 + warp / side.split; t < t1; t += kWarps / side.split) {
-        // this place's cosines and sines: pair q of a thread is formed by team q % GROUPS
+        // this place's cosines and sines
         float2 cs[PAIRS];
         if (a.half > 0) {
             const long long u = i * a.pos_rep + t * a.pos_step;
             const double pos = !a.positions ? (double)t
                                : a.wide     ? (double)__ldg(static_cast<const long long*>(a.positions) + u)
                                             : (double)__ldg(static_cast<const int*>(a.positions) + u);
-            float2 own[(PAIRS + GROUPS - 1) / GROUPS];
+            float2 own[OWN];
 #pragma unroll
-            for (int q = 0; q < (PAIRS + GROUPS - 1) / GROUPS; ++q) {
-                const int pair = q * GROUPS + group, z = pair / VEC, e = pair % VEC, s = z * TEAM + lane;
-                const int j = s * VEC + e;
-                own[q] = make_float2(1.f, 0.f);
-                if (pair < PAIRS && j < a.half) {
-                    double x = pos * a.turns[j];
-                    x -= rint(x);
-                    const float hi = (float)x, lo = (float)(x - (double)hi) * 6.283185307179586f;
-                    float sn, c;
-                    sincospif(2.f * hi, &sn, &c);
-                    own[q] = make_float2(fmaf(-lo, sn, c), fmaf(lo, c, sn));
-                }
+            for (int q = 0; q < OWN; ++q) {                  // (no turns: cosine 1)
+                double x = pos * turns_of[q];
+                x -= rint(x);
+                const float hi = (float)x, lo = (float)(x - (double)hi) * 6.283185307179586f;
+                float sn, c;
+                sincospif(2.f * hi, &sn, &c);
+                own[q] = make_float2(fmaf(-lo, sn, c), fmaf(lo, c, sn));
             }
 #pragma unroll
             for (int q = 0; q < PAIRS; ++q) {
@@ -397,11 +400,11 @@ bool valid(const eg_head_norm_args* q, bool backward) {
 }
 
 // CTAs of a replica for one side; bounds the workspace too.
-int ctas_of(int64_t P, int64_t rows, int64_t mine, int64_t other) {
+int ctas_of(int64_t P, int64_t rows, int64_t mine, int64_t other, int per_sm) {
     if (mine == 0) return 0;
     // both sides' warps take as long: their heads, and a place's sines (as long as about four)
     const double share = (double)(mine + 4) / (double)(mine + 4 + (other ? other + 4 : 0));
-    int64_t each = (int64_t)((double)(sm_count() * kCtasPerSm) * share / (double)P);
+    int64_t each = (int64_t)((double)(sm_count() * per_sm) * share / (double)P);
     if (each > (rows + 1) / 2) each = (rows + 1) / 2;
     return (int)(each > 1 ? each : 1);
 }
@@ -410,10 +413,10 @@ struct Sizes {
     int ctas[2];
     int64_t bytes;
 };
-Sizes sizes_of(const eg_head_norm_args* q) {
+Sizes sizes_of(const eg_head_norm_args* q, bool backward) {
     Sizes s;
-    s.ctas[0] = ctas_of(q->P, q->rows, q->q_heads, q->k_heads);
-    s.ctas[1] = ctas_of(q->P, q->rows, q->k_heads, q->q_heads);
+    s.ctas[0] = ctas_of(q->P, q->rows, q->q_heads, q->k_heads, backward ? kCtasBackward : kCtasForward);
+    s.ctas[1] = ctas_of(q->P, q->rows, q->k_heads, q->q_heads, backward ? kCtasBackward : kCtasForward);
     s.bytes = q->P * (int64_t)(s.ctas[0] + s.ctas[1]) * q->width * 4;
     return s;
 }
@@ -426,7 +429,7 @@ int fill(HeadArgs* a, const eg_head_norm_args* q, bool backward, float* partial)
     a->eps = (float)q->eps; a->inv_d = 1.f / (float)q->width;
     a->positions = q->positions; a->pos_rep = q->position_replica_stride; a->pos_step = q->position_stride;
     a->wide = q->position_bytes == 8;
-    const Sizes n = sizes_of(q);
+    const Sizes n = sizes_of(q, backward);
     const size_t size = q->dtype == EG_F32 ? 4 : 2;
     const struct { const eg_heads *x, *out, *d_out; const eg_matrix *w, *dw; int64_t H; } both[] = {
         {&q->q, backward ? &q->dq : &q->q_out, &q->dq_out, &q->w_q, &q->d_w_q, q->q_heads},
@@ -509,7 +512,7 @@ eg_status eg_head_norm(const eg_head_norm_args* q, void* stream_v) {
 
 int64_t eg_head_norm_workspace(const eg_head_norm_args* q) {
     if (!valid(q, true) || sm_count() < 1) return 0;
-    return sizes_of(q).bytes;
+    return sizes_of(q, true).bytes;
 }
 
 eg_status eg_head_norm_backward(const eg_head_norm_args* q, void* workspace, int64_t workspace_bytes, void* stream_v) {
