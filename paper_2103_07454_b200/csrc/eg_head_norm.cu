@@ -133,7 +133,7 @@ template <typename T, int VEC, int NS, int TEAM, bool BWD>
 __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) k_head_norm(const __grid_constant__ HeadArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    constexpr int GROUPS = 32 / TEAM, PAIRS = NS * VEC, AHEAD = NS > 2 ? 1 : 2;
+    constexpr int GROUPS = 32 / TEAM, PAIRS = NS * VEC;
     __shared__ float s_sum[BWD ? kWarps : 1][BWD ? kMaxWidth : 1];
     const int m = (int)blockIdx.x >= a.side[0].ctas, i = blockIdx.y;
     const Side& side = a.side[m];
@@ -174,71 +174,85 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
         turns_of[q] = pair < PAIRS && j < a.half ? a.turns[j] : 0.0;
     }
     const int part = warp % side.split, H = side.heads;
-    for (long long t = t0 + warp / side.split; t < t1; t += kWarps / side.split) {
-        // this place's cosines and sines
-        float2 cs[PAIRS];
-        if (a.half > 0) {
-            const long long u = i * a.pos_rep + t * a.pos_step;
-            const double pos = !a.positions ? (double)t
-                               : a.wide     ? (double)__ldg(static_cast<const long long*>(a.positions) + u)
-                                            : (double)__ldg(static_cast<const int*>(a.positions) + u);
+    // A unit: the rows that the teams take at one turn, of one place.  The next unit's values are on their way while one is worked
+    // on (results may lie where inputs do, so the compiler cannot bring loads ahead of stores).
+    const int turns = (H - part * GROUPS + side.split * GROUPS - 1) / (side.split * GROUPS), stride = kWarps / side.split;
+    struct Unit {
+        Packed<T, VEC> x[NS][2], g[BWD ? NS : 1][2];
+    };
+    auto load = [&](Unit& u, long long t, int turn) {
+        const int h = (part + turn * side.split) * GROUPS + group;
+        const T* const x0 = head_at<T>(side.x, i, t, h);
+        const T* const g0 = BWD ? head_at<T>(side.d_out, i, t, h) : nullptr;
+#pragma unroll
+        for (int z = 0; z < NS; ++z)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                u.x[z][k].clear();
+                if (BWD) u.g[z][k].clear();
+                if (h < H && here[z][k]) {
+                    u.x[z][k].load(x0 + at[z][k]);
+                    if (BWD) u.g[z][k].load(g0 + at[z][k]);
+                }
+            }
+    };
+    auto place = [&](long long t) {
+        const long long u = i * a.pos_rep + t * a.pos_step;
+        return !a.positions ? (double)t
+               : a.wide     ? (double)__ldg(static_cast<const long long*>(a.positions) + u)
+                            : (double)__ldg(static_cast<const int*>(a.positions) + u);
+    };
+    Unit unit, next;
+    long long t = t0 + warp / side.split;
+    int q = 0;
+    double pos = 0.0;
+    float2 cs[PAIRS];
+    if (t < t1 && turns > 0) {
+        load(unit, t, 0);
+        pos = place(t);
+    }
+    while (t < t1 && turns > 0) {
+        const bool another = q + 1 == turns;                 // the next unit is of another place
+        const int q1 = another ? 0 : q + 1;
+        const long long t2 = another ? t + stride : t;
+        double pos2 = pos;
+        if (t2 < t1) {
+            load(next, t2, q1);
+            if (another) pos2 = place(t2);
+        }
+        if (q == 0) {
+            // this place's cosines and sines (no turns: cosine 1)
             float2 own[OWN];
 #pragma unroll
-            for (int q = 0; q < OWN; ++q) {                  // (no turns: cosine 1)
-                double x = pos * turns_of[q];
+            for (int z = 0; z < OWN; ++z) {
+                double x = pos * turns_of[z];
                 x -= rint(x);
                 const float hi = (float)x, lo = (float)(x - (double)hi) * 6.283185307179586f;
                 float sn, c;
                 sincospif(2.f * hi, &sn, &c);
-                own[q] = make_float2(fmaf(-lo, sn, c), fmaf(lo, c, sn));
+                own[z] = make_float2(fmaf(-lo, sn, c), fmaf(lo, c, sn));
             }
 #pragma unroll
-            for (int q = 0; q < PAIRS; ++q) {
+            for (int z = 0; z < PAIRS; ++z) {
                 if constexpr (GROUPS == 1) {
-                    cs[q] = own[q];
+                    cs[z] = own[z];
                 } else {
-                    const int from = q % GROUPS * TEAM + lane;
-                    cs[q] = make_float2(__shfl_sync(0xffffffffu, own[q / GROUPS].x, from), __shfl_sync(0xffffffffu, own[q / GROUPS].y, from));
+                    const int from = z % GROUPS * TEAM + lane;
+                    cs[z] = make_float2(__shfl_sync(0xffffffffu, own[z / GROUPS].x, from), __shfl_sync(0xffffffffu, own[z / GROUPS].y, from));
                 }
             }
-        } else {
-#pragma unroll
-            for (int q = 0; q < PAIRS; ++q) cs[q] = make_float2(1.f, 0.f);
         }
-        const T* const x0 = head_at<T>(side.x, i, t, 0);
-        const T* const g0 = BWD ? head_at<T>(side.d_out, i, t, 0) : nullptr;
-        T* const o0 = side.out.p ? head_at<T>(side.out, i, t, 0) : nullptr;
-        // every team makes the same number of turns: they shuffle together.  The loads of AHEAD turns come before the first one's
-        // stores (results may lie where inputs do, so the compiler cannot move them).
-        const int turns = (H - part * GROUPS + side.split * GROUPS - 1) / (side.split * GROUPS);
-        for (int q0 = 0; q0 < turns; q0 += AHEAD) {
-            Packed<T, VEC> px[AHEAD][NS][2], pg[BWD ? AHEAD : 1][BWD ? NS : 1][2];
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                const int h = (part + (q0 + q) * side.split) * GROUPS + group;
-#pragma unroll
-                for (int z = 0; z < NS; ++z)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        px[q][z][k].clear();
-                        if (BWD) pg[q][z][k].clear();
-                        if (h < H && here[z][k]) {
-                            px[q][z][k].load(x0 + h * side.x.head + at[z][k]);
-                            if (BWD) pg[q][z][k].load(g0 + h * side.d_out.head + at[z][k]);
-                        }
-                    }
-            }
-#pragma unroll
-          for (int q = 0; q < AHEAD; ++q) {
-            const int h = (part + (q0 + q) * side.split) * GROUPS + group;
+        {
+            const int h = (part + q * side.split) * GROUPS + group;
             const bool active = h < H;
+            T* const o0 = side.out.p ? head_at<T>(side.out, i, t, h) : nullptr;
             float x[NS][2][VEC], g[BWD ? NS : 1][2][VEC];
 #pragma unroll
             for (int z = 0; z < NS; ++z)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    px[q][z][k].widen(x[z][k]);
-                    if (BWD) pg[q][z][k].widen(g[z][k]);
+                    unit.x[z][k].widen(x[z][k]);
+                    if (BWD) unit.g[z][k].widen(g[z][k]);
                 }
             float square = 0.f, along = 0.f;
 #pragma unroll
@@ -265,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
                     turn_slot<VEC, false>(a.interleaved, cs + z * VEC, x[z]);
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
-                        if (active && here[z][k]) store_some<T, VEC>(o0 + h * side.out.head + at[z][k], x[z][k]);
+                        if (active && here[z][k]) store_some<T, VEC>(o0 + at[z][k], x[z][k]);
                 }
             } else {
                 float back = 0.f;
@@ -280,11 +294,14 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
                             dw[z][k][e] = fmaf(g[z][k][e], x[z][k][e] * inv, dw[z][k][e]);
                             dx[e] = inv * fmaf(-back, x[z][k][e], g[z][k][e] * w[z][k][e]);
                         }
-                        if (o0 && active && here[z][k]) store_some<T, VEC>(o0 + h * side.out.head + at[z][k], dx);
+                        if (o0 && active && here[z][k]) store_some<T, VEC>(o0 + at[z][k], dx);
                     }
             }
-          }
         }
+        unit = next;
+        pos = pos2;
+        t = t2;
+        q = q1;
     }
     if constexpr (BWD) {
         // sums of the CTA: over the teams of a warp, then over the warps
