@@ -456,7 +456,7 @@ typedef struct {
  *     z = x / sqrt(mean(x^2) + eps) * w,        out = z with its first `rotary` values turned in pairs,
  * pair j of the row at position p by the angle p * base^(-2 j / rotary):
  *     (a, b) -> (a cos - b sin, a sin + b cos),
- * where pair j is (j, j + rotary / 2), or (2 j, 2 j + 1) with `interleaved`.  rotary is even; 0: no rotation.
+ * where pair j is (j, j + rotary / 2), or (2 j, 2 j + 1) with `interleaved`.  rotary is even; 0: no rotation.  base >= 1.
  * w_q, w_k: `width` per replica, one vector for all heads; not given: z = x.  q, k: `rows` x q_heads (k_heads) x width per replica;
  * k_heads may be 0.  positions: whole numbers of 4 or 8 bytes (position_bytes) per row, of any size and sign;
  * NULL: 0, 1, 2, ...  Everything else is of type dtype; sums are fp32, angles are reduced in 64 bits.

@@ -14,8 +14,10 @@
 //      the list.  The tokens come out of the L2 and nobody waits for another CTA; a sort in several passes would read them
 //      about as often and launch five kernels.  It notes which rows have a place.
 //   2. k_embed_sum: a warp adds up one chunk of the list over some columns.  Chunks have equal length, however often a token
-//      comes; a run that crosses chunks leaves a partial sum in each.  Other blocks of the launch write the zeros of the rows without
-//      a place meanwhile, the same number of rows each.
+//      comes; a run that crosses chunks leaves a partial sum in each.
+// The table's zeros are written by further blocks of these launches, the same number of rows each: beside the sort, for all rows, where
+// there are fewer places than rows (the sort, 10 to 30 us of latencies, is then for nothing), beside the sums, for the rows
+// without a place, where there are more.
 //   3. k_embed_join: adds the partial sums of such runs, in order.
 #include "eg_ops.cuh"
 
@@ -46,6 +48,7 @@ struct EmbedArgs {
     int chunk, chunks;                     // places of a chunk; chunks of a replica
     int pitch;                             // columns of a partial sum, up to whole vectors
     int sum_blocks;                        // of k_embed_sum, per replica; the rest write zeros
+    int sort_blocks;                       // of k_embed_sort
     int *order, *key, *count;              // [P][n] places and tokens of the sorted list, [P] its length
     unsigned int* named;                   // [P][words] one bit for every row of the table that has a place
     int words;
@@ -109,6 +112,17 @@ __global__ void __launch_bounds__(256) k_embed(const __grid_constant__ EmbedArgs
 }
 
 // ----------------------------------------------------------------------------------- backward
+// Zeros for block b's share of a replica's rows; `some`: only for rows without a place.
+template <typename T, int VEC> __device__ __forceinline__ void write_zeros(const EmbedArgs& a, int i, int b, int blocks, bool some) {
+    const float zero[VEC] = {};
+    const long long v0 = a.V * b / blocks, v1 = a.V * (b + 1) / blocks;
+    for (long long v = v0 + (threadIdx.x >> 5); v < v1; v += blockDim.x >> 5) {
+        if (some && (a.named[(long long)i * a.words + v / 32] >> (v & 31) & 1)) continue;
+        T* to = row_of<T>(a.out, i, v);
+        for (int c = (int)(threadIdx.x & 31) * VEC; c < a.d; c += 32 * VEC) store_vec<T, VEC>(to + c, zero);
+    }
+}
+
 // Sum over the CTA, valid in all threads; `red` holds kSortWarps values.
 __device__ __forceinline__ int block_total(int v, int* red) {
     v = __reduce_add_sync(0xffffffffu, v);
@@ -121,12 +135,16 @@ __device__ __forceinline__ int block_total(int v, int* red) {
     return s;
 }
 
-__global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_constant__ EmbedArgs a) {
+template <typename T, int VEC> __global__ void __launch_bounds__(kSortThreads) k_embed_sort(const __grid_constant__ EmbedArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ int s_at[kSortWarps][kRangeMax];          // first how often, then where to
     __shared__ int s_red[kSortWarps];
     const int i = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x >= a.sort_blocks) {
+        write_zeros<T, VEC>(a, i, blockIdx.x - a.sort_blocks, gridDim.x - a.sort_blocks, false);
+        return;
+    }
     const long long first = (long long)blockIdx.x * a.range;
     const int mine = (int)(a.V - first < a.range ? a.V - first : a.range);
     for (int q = threadIdx.x; q < kSortWarps * kRangeMax; q += kSortThreads) (&s_at[0][0])[q] = 0;
@@ -253,14 +271,7 @@ template <typename T, int VEC, int U> __global__ void __launch_bounds__(256, 4) 
     constexpr int AHEAD = 4;                             // rows on their way at once
     const int lane = threadIdx.x & 31, i = blockIdx.y;
     if ((int)blockIdx.x >= a.sum_blocks) {
-        const float zero[VEC] = {};
-        const long long b = blockIdx.x - a.sum_blocks, blocks = gridDim.x - a.sum_blocks;
-        const long long v0 = a.V * b / blocks, v1 = a.V * (b + 1) / blocks;
-        for (long long v = v0 + (threadIdx.x >> 5); v < v1; v += 8) {
-            if (a.n > 0 && (a.named[(long long)i * a.words + v / 32] >> (v & 31) & 1)) continue;
-            T* to = row_of<T>(a.out, i, v);
-            for (int c = lane * VEC; c < a.d; c += 32 * VEC) store_vec<T, VEC>(to + c, zero);
-        }
+        write_zeros<T, VEC>(a, i, blockIdx.x - a.sum_blocks, gridDim.x - a.sum_blocks, true);
         return;
     }
     const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -323,10 +334,10 @@ template <typename T, int VEC, int U> __global__ void __launch_bounds__(256, 4) 
     }
 }
 
-// A block: the run that begins in one chunk and goes on into the next, 4 columns a thread.
+// A block: the run that begins in one chunk and goes on into the next, 1024 columns.
 template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ EmbedArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    constexpr int AHEAD = 8;
+    constexpr int AHEAD = 16;
     const int lane = threadIdx.x & 31, i = blockIdx.y;
     const long long chunk = blockIdx.x, first = chunk * a.chunk, end = first + a.chunk;
     const int* key = a.key + i * a.n;
@@ -344,7 +355,8 @@ template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const 
             break;
         }
     }
-    for (int c = threadIdx.x * 4; c < a.d; c += 1024) {
+    const int c = ((int)blockIdx.z * 256 + (int)threadIdx.x) * 4;
+    if (c < a.d) {
         const float* partial = a.partial + ((long long)i * a.chunks + chunk) * 2 * a.pitch + c;
         float sum[4];
         load_vec<float, 4>(partial + a.pitch, sum);
@@ -464,15 +476,6 @@ template <typename T, int VEC> cudaError_t forward(const EmbedArgs& a, cudaStrea
 }
 
 template <typename T, int VEC> cudaError_t backward(EmbedArgs a, cudaStream_t stream) {
-    cudaError_t e;
-    if (a.n > 0) {
-        const unsigned ranges = (unsigned)((a.V + a.range - 1) / a.range);
-        if ((e = launch_after(k_embed_sort, dim3(ranges, a.P), dim3(kSortThreads), 0, stream, a)) != cudaSuccess) return e;
-    }
-    auto blocks = [&](int slices) { return (unsigned)(((long long)a.chunks * slices + 7) / 8); };
-    constexpr int U = VEC > 1 ? 1 : 4;
-    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC);
-    a.sum_blocks = a.n > 0 ? (int)blocks(slices) : 0;
     // zeros: 64 KB or so a block, at least a few blocks for every multiprocessor
     long long zeros = 0;
     if (!a.accumulate) {
@@ -481,9 +484,16 @@ template <typename T, int VEC> cudaError_t backward(EmbedArgs a, cudaStream_t st
         if (zeros < least) zeros = least;
         if (zeros > most) zeros = most;
     }
-    e = launch_after(k_embed_sum<T, VEC, U>, dim3((unsigned)(a.sum_blocks + zeros), a.P), dim3(256), 0, stream, a, slices);
-    if (e != cudaSuccess || a.n == 0 || a.chunks == 1) return e;
-    return launch_after(k_embed_join<T>, dim3((unsigned)a.chunks, a.P), dim3(256), 0, stream, a);
+    const bool early = a.n <= a.V;
+    a.sort_blocks = a.n > 0 ? (int)((a.V + a.range - 1) / a.range) : 0;
+    cudaError_t e = launch_after(k_embed_sort<T, VEC>, dim3((unsigned)(a.sort_blocks + (early ? zeros : 0)), a.P), dim3(kSortThreads), 0, stream, a);
+    if (e != cudaSuccess || a.n == 0) return e;
+    constexpr int U = VEC > 1 ? 1 : 4;
+    const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC);
+    a.sum_blocks = (int)(((long long)a.chunks * slices + 7) / 8);
+    e = launch_after(k_embed_sum<T, VEC, U>, dim3((unsigned)(a.sum_blocks + (early ? 0 : zeros)), a.P), dim3(256), 0, stream, a, slices);
+    if (e != cudaSuccess || a.chunks == 1) return e;
+    return launch_after(k_embed_join<T>, dim3((unsigned)a.chunks, a.P, (a.d + 1023) / 1024), dim3(256), 0, stream, a);
 }
 
 }  // namespace

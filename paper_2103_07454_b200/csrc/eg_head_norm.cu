@@ -11,8 +11,8 @@
 // elements are partners (halves: j and j + rotary / 2; neighbours: inside either vector).  A warp takes one place after
 // another, all heads of the queries or of the keys, a row a team at a time; cosines and sines of the place stay in registers for all
 // of them (a sine costs some forty instructions, a value of a row about six), each formed by one team and handed to
-// the others.  An angle is reduced in 64 bits, where positions of any size keep their fraction of a turn; only the
-// fraction goes on in 32.
+// the others.  Angles are whole 64-bit numbers in units of 2^-64 of a turn, which overflow where a turn ends: a product of
+// position and frequency keeps its fraction for positions of any size and sign.
 #include <type_traits>
 
 #include "eg_ops.cuh"
@@ -52,73 +52,111 @@ struct HeadArgs {
     int wide;
     int slots;                              // of a row
     Side side[2];
-    double turns[kMaxPairs];                // turns of pair j per place
+    unsigned long long turns[kMaxPairs];    // turns of pair j per place, in 2^-64
 };
 
 template <typename T> __device__ __forceinline__ T* head_at(const Heads& m, int i, long long t, int h) {
     return static_cast<T*>(m.p) + (long long)i * m.rep + t * m.row + (long long)h * m.head;
 }
 
-// VEC values in one access, as they lie in memory; widened where they are used.
-template <typename T, int VEC> struct Packed {
-    static constexpr int kWords = VEC * (int)sizeof(T) / 4 > 0 ? VEC * (int)sizeof(T) / 4 : 1;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int q = 0; q < kWords; ++q) w[q] = 0;
+// VEC values on their way through shared memory: a thread copies what it will itself read, so that nobody waits for anybody.
+template <typename T, int VEC> struct Piece {
+    static constexpr int kBytes = VEC * (int)sizeof(T) < 4 ? 4 : VEC * (int)sizeof(T);
+    static constexpr int kWords = kBytes / 4;
+    // A single 16-bit value comes with the other half of its word.
+    __device__ __forceinline__ static const void* word(const T* p) { return reinterpret_cast<const void*>((uintptr_t)p & ~(uintptr_t)3); }
+    __device__ __forceinline__ static void copy(unsigned char* to, const T* from, bool there) {
+        const uint32_t dst = op_smem(to);
+        const int bytes = there ? kBytes : 0;                // the rest becomes zero
+        const void* src = word(from);
+        if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(bytes) : "memory");
     }
-    __device__ __forceinline__ void load(const T* p) {
-        if constexpr (VEC * sizeof(T) == 16) {
-            const uint4 v = *reinterpret_cast<const uint4*>(p);
+    __device__ __forceinline__ static void read(const unsigned char* at, const T* from, uint32_t (&w)[kWords]) {
+        if constexpr (kWords == 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(at);
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-        } else if constexpr (VEC * sizeof(T) == 8) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
+        } else if constexpr (kWords == 2) {
+            const uint2 v = *reinterpret_cast<const uint2*>(at);
             w[0] = v.x; w[1] = v.y;
-        } else if constexpr (VEC * sizeof(T) == 4) {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
         } else {
-            w[0] = *reinterpret_cast<const uint16_t*>(p);
-        }
-    }
-    __device__ __forceinline__ void widen(float (&v)[VEC]) const {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = __uint_as_float(w[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; e += 2) {
-                const float2 f = unpack2<T>(w[e / 2]);
-                v[e] = f.x;
-                if (e + 1 < VEC) v[e + 1 < VEC ? e + 1 : e] = f.y;
-            }
+            w[0] = *reinterpret_cast<const uint32_t*>(at);
+            if (VEC * sizeof(T) == 2 && ((uintptr_t)from & 2)) w[0] >>= 16;
         }
     }
 };
+
+// The two vectors of a slot as VEC pairs of registers, for packed arithmetic: neighbours of one vector (VEC == 1: the two vectors' values).
+template <typename T, int VEC> __device__ __forceinline__ void widen(const uint32_t (&w)[2][Piece<T, VEC>::kWords], f32x2 (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        if constexpr (sizeof(T) == 4) v[0] = pack_f2(__uint_as_float(w[0][0]), __uint_as_float(w[1][0]));
+        else v[0] = pack_f2(unpack2<T>(w[0][0]).x, unpack2<T>(w[1][0]).x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC / 2; ++e) {
+                if constexpr (sizeof(T) == 4) v[k * (VEC / 2) + e] = pack_f2(__uint_as_float(w[k][2 * e]), __uint_as_float(w[k][2 * e + 1]));
+                else v[k * (VEC / 2) + e] = pack_f2(unpack2<T>(w[k][e]));
+            }
+    }
+}
+// The values of vector k.
+template <int VEC> __device__ __forceinline__ void values_of(const f32x2 (&v)[VEC], int k, float (&x)[VEC]) {
+    if constexpr (VEC == 1) {
+        const float2 f = unpack_f2(v[0]);
+        x[0] = k ? f.y : f.x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC / 2; ++e) {
+            const float2 f = unpack_f2(v[k * (VEC / 2) + e]);
+            x[2 * e] = f.x;
+            x[2 * e + 1] = f.y;
+        }
+    }
+}
 template <typename T, int VEC> __device__ __forceinline__ void store_some(T* p, const float (&v)[VEC]) {
     if constexpr (VEC == 1 || VEC * sizeof(T) == 16) store_vec<T, VEC>(p, v);
     else if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
     else *reinterpret_cast<uint32_t*>(p) = pack2<T>(v[0], v[1]);
 }
 
-// (a, b) by the angle (c, s); BACK: by its opposite.
-template <bool BACK> __device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
-    const float s = BACK ? -cs.y : cs.y, x = a;
-    a = fmaf(-s, b, cs.x * x);
-    b = fmaf(s, x, cs.x * b);
-}
-// A slot's VEC pairs: (x[0][e], x[1][e]), or neighbours inside either vector.  Pairs that stay have cosine 1.
-template <int VEC, bool BACK> __device__ __forceinline__ void turn_slot(bool interleaved, const float2* cs, float (&x)[2][VEC]) {
+// A slot's VEC pairs by their angles (cosine, sine); pairs that stay have cosine 1.
+//   halves: partners in the two vectors;  neighbours (and single values): partners in one pair of registers
+template <int VEC> __device__ __forceinline__ void turn_slot(bool interleaved, const float2* cs, f32x2 (&x)[VEC]) {
+    if (VEC == 1 || interleaved) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float2 f = unpack_f2(x[e]);
+            x[e] = fma2(x[e], pack_f2(cs[e].x, cs[e].x), mul2(pack_f2(f.y, f.x), pack_f2(-cs[e].y, cs[e].y)));
+        }
+        return;
+    }
     if constexpr (VEC > 1) {
-        if (interleaved) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int e = 0; e < VEC; e += 2) turn<BACK>(x[k][e], x[k][e + 1], cs[(k * VEC + e) / 2]);
-            return;
+        for (int e = 0; e < VEC / 2; ++e) {
+            const f32x2 a = x[e], b = x[e + VEC / 2], c = pack_f2(cs[2 * e].x, cs[2 * e + 1].x), s = pack_f2(cs[2 * e].y, cs[2 * e + 1].y);
+            x[e] = fma2(c, a, mul2(pack_f2(-cs[2 * e].y, -cs[2 * e + 1].y), b));
+            x[e + VEC / 2] = fma2(c, b, mul2(s, a));
         }
     }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) turn<BACK>(x[0][e], x[1][e], cs[e]);
+}
+
+// Cosine and sine of an angle in 2^-64 of a turn.  16-bit results take the hardware's (2^-21, after the reduction).
+template <typename T> __device__ __forceinline__ float2 cos_sin(unsigned long long angle) {
+    const int top = (int)(angle >> 32);                      // -1/2 to 1/2 of a turn
+    const float hi = (float)top;
+    float s, c;
+    if constexpr (sizeof(T) == 2) {
+        const float x = hi * 1.4629180792671596e-9f;         // 2 pi / 2^32
+        s = __sinf(x);
+        c = __cosf(x);
+        return make_float2(c, s);
+    } else {
+        const float lo = (float)(int)((long long)top - (long long)hi) * 1.4629180792671596e-9f;   // what 24 bits left over
+        sincospif(hi * 4.656612873077393e-10f, &s, &c);      // 2 / 2^32
+        return make_float2(fmaf(-lo, s, c), fmaf(lo, c, s));
+    }
 }
 
 // Sums over the TEAM threads of a row.
@@ -127,6 +165,14 @@ template <int TEAM> __device__ __forceinline__ float team_sum(float v) {
     for (int o = TEAM >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+
+// Shared memory of a thread for one unit (a row's slots, their gradients, the place): as many units as DEPTH are on their way.
+template <typename T, int VEC, int NS, bool BWD> struct Ring {
+    static constexpr int kPieces = NS * 2 * (BWD ? 2 : 1);
+    static constexpr int kUnit = kPieces * Piece<T, VEC>::kBytes + 8;
+    static constexpr int kDepth = 3 + (kUnit < 40) + (kUnit < 24);
+    static constexpr int kBytes = kDepth * kUnit * kThreads;
+};
 
 // NS: slots of a thread; TEAM: threads of a row.
 template <typename T, int VEC, int NS, int TEAM, bool BWD>
@@ -141,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
     const long long t0 = a.n * b / side.ctas, t1 = a.n * (b + 1) / side.ctas;
     const int lane = threadIdx.x % TEAM, group = threadIdx.x % 32 / TEAM, warp = threadIdx.x >> 5;
     const bool normed = side.w.p != nullptr;
-    float w[NS][2][VEC], dw[BWD ? NS : 1][2][VEC];
+    f32x2 w[NS][VEC], dw[BWD ? NS : 1][VEC];
     int at[NS][2];
     bool here[NS][2];
 #pragma unroll
@@ -155,82 +201,80 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
             at[z][0] = s < lead ? s * VEC : a.rotary + 2 * (s - lead) * VEC;
             at[z][1] = s < lead ? a.half + s * VEC : at[z][0] + VEC;
         }
+        float f[2][VEC];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             here[z][k] = s < a.slots && at[z][k] < a.d;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                w[z][k][e] = normed && here[z][k] ? to_f32(static_cast<const T*>(side.w.p)[i * side.w.rep + at[z][k] + e]) : 1.f;
-                if (BWD) dw[z][k][e] = 0.f;
-            }
+            for (int e = 0; e < VEC; ++e)
+                f[k][e] = normed && here[z][k] ? to_f32(static_cast<const T*>(side.w.p)[i * side.w.rep + at[z][k] + e]) : 1.f;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            w[z][e] = VEC == 1 ? pack_f2(f[0][0], f[1][0]) : pack_f2(f[2 * e / VEC][2 * e % VEC], f[2 * e / VEC][(2 * e + 1) % VEC]);
+            if (BWD) dw[z][e] = 0;
         }
     }
     // pair q of a thread is formed by team q % GROUPS; the turns of those that this one forms
     constexpr int OWN = (PAIRS + GROUPS - 1) / GROUPS;
-    double turns_of[OWN];
+    unsigned long long turns_of[OWN];
 #pragma unroll
     for (int q = 0; q < OWN; ++q) {
         const int pair = q * GROUPS + group, j = (pair / VEC * TEAM + lane) * VEC + pair % VEC;
-        turns_of[q] = pair < PAIRS && j < a.half ? a.turns[j] : 0.0;
+        turns_of[q] = pair < PAIRS && j < a.half ? a.turns[j] : 0;
     }
     const int part = warp % side.split, H = side.heads;
-    // A unit: the rows that the teams take at one turn, of one place.  The next unit's values are on their way while one is worked
-    // on (results may lie where inputs do, so the compiler cannot bring loads ahead of stores).
+    // A unit: the rows that the teams take at one turn, of one place.  Its values come by way of shared memory, DEPTH - 1 units ahead:
+    // in registers a multiprocessor held too few bytes on their way (8192 places of 16 + 4 heads of 128 on 4 replicas: 79 and 153 us).
+    using R = Ring<T, VEC, NS, BWD>;
+    using P = Piece<T, VEC>;
+    constexpr int DEPTH = R::kDepth;
+    extern __shared__ __align__(16) unsigned char s_ring[];
     const int turns = (H - part * GROUPS + side.split * GROUPS - 1) / (side.split * GROUPS), stride = kWarps / side.split;
-    struct Unit {
-        Packed<T, VEC> x[NS][2], g[BWD ? NS : 1][2];
-    };
-    auto load = [&](Unit& u, long long t, int turn) {
-        const int h = (part + turn * side.split) * GROUPS + group;
-        const T* const x0 = head_at<T>(side.x, i, t, h);
-        const T* const g0 = BWD ? head_at<T>(side.d_out, i, t, h) : nullptr;
+    auto piece = [&](int slot, int n) { return s_ring + ((slot * R::kPieces + n) * kThreads + threadIdx.x) * P::kBytes; };
+    auto place_at = [&](int slot) { return s_ring + DEPTH * R::kPieces * kThreads * P::kBytes + (slot * kThreads + threadIdx.x) * 8; };
+    long long t = t0 + warp / side.split, ta = t;            // the unit worked on, and the one to fetch
+    int q = 0, qa = 0, slot = 0, slot_a = 0;
+    auto fetch = [&]() {
+        if (ta < t1 && turns > 0) {
+            const int h = (part + qa * side.split) * GROUPS + group;
+            const bool active = h < H;
+            const T* const x0 = head_at<T>(side.x, i, ta, active ? h : 0);
+            const T* const g0 = BWD ? head_at<T>(side.d_out, i, ta, active ? h : 0) : nullptr;
 #pragma unroll
-        for (int z = 0; z < NS; ++z)
+            for (int z = 0; z < NS; ++z)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                u.x[z][k].clear();
-                if (BWD) u.g[z][k].clear();
-                if (h < H && here[z][k]) {
-                    u.x[z][k].load(x0 + at[z][k]);
-                    if (BWD) u.g[z][k].load(g0 + at[z][k]);
+                for (int k = 0; k < 2; ++k) {
+                    const bool there = active && here[z][k];
+                    P::copy(piece(slot_a, z * 2 + k), x0 + (there ? at[z][k] : 0), there);
+                    if (BWD) P::copy(piece(slot_a, NS * 2 + z * 2 + k), g0 + (there ? at[z][k] : 0), there);
                 }
+            if (qa == 0 && a.positions) {
+                const char* p = static_cast<const char*>(a.positions) + (i * a.pos_rep + ta * a.pos_step) * (a.wide ? 8 : 4);
+                if (a.wide) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(op_smem(place_at(slot_a))), "l"(p) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(op_smem(place_at(slot_a))), "l"(p) : "memory");
             }
-    };
-    auto place = [&](long long t) {
-        const long long u = i * a.pos_rep + t * a.pos_step;
-        return !a.positions ? (double)t
-               : a.wide     ? (double)__ldg(static_cast<const long long*>(a.positions) + u)
-                            : (double)__ldg(static_cast<const int*>(a.positions) + u);
-    };
-    Unit unit, next;
-    long long t = t0 + warp / side.split;
-    int q = 0;
-    double pos = 0.0;
-    float2 cs[PAIRS];
-    if (t < t1 && turns > 0) {
-        load(unit, t, 0);
-        pos = place(t);
-    }
-    while (t < t1 && turns > 0) {
-        const bool another = q + 1 == turns;                 // the next unit is of another place
-        const int q1 = another ? 0 : q + 1;
-        const long long t2 = another ? t + stride : t;
-        double pos2 = pos;
-        if (t2 < t1) {
-            load(next, t2, q1);
-            if (another) pos2 = place(t2);
+            if (++qa == turns) { qa = 0; ta += stride; }
+            if (++slot_a == DEPTH) slot_a = 0;
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    float2 cs[PAIRS];
+#pragma unroll
+    for (int n = 0; n < DEPTH - 1; ++n) fetch();
+    while (t < t1 && turns > 0) {
+        fetch();
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
         if (q == 0) {
             // this place's cosines and sines (no turns: cosine 1)
             float2 own[OWN];
+            const unsigned long long pos = (unsigned long long)(!a.positions ? t
+                                                                : a.wide     ? *reinterpret_cast<const long long*>(place_at(slot))
+                                                                             : (long long)*reinterpret_cast<const int*>(place_at(slot)));
 #pragma unroll
             for (int z = 0; z < OWN; ++z) {
-                double x = pos * turns_of[z];
-                x -= rint(x);
-                const float hi = (float)x, lo = (float)(x - (double)hi) * 6.283185307179586f;
-                float sn, c;
-                sincospif(2.f * hi, &sn, &c);
-                own[z] = make_float2(fmaf(-lo, sn, c), fmaf(lo, c, sn));
+                own[z] = cos_sin<T>(pos * turns_of[z]);
+                if (BWD) own[z].y = -own[z].y;               // back
             }
 #pragma unroll
             for (int z = 0; z < PAIRS; ++z) {
@@ -246,62 +290,73 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
             const int h = (part + q * side.split) * GROUPS + group;
             const bool active = h < H;
             T* const o0 = side.out.p ? head_at<T>(side.out, i, t, h) : nullptr;
-            float x[NS][2][VEC], g[BWD ? NS : 1][2][VEC];
-#pragma unroll
-            for (int z = 0; z < NS; ++z)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    unit.x[z][k].widen(x[z][k]);
-                    if (BWD) unit.g[z][k].widen(g[z][k]);
-                }
-            float square = 0.f, along = 0.f;
+            const T* const x0 = head_at<T>(side.x, i, t, h);         // (single 16-bit values: which half of their word)
+            const T* const g0 = BWD ? head_at<T>(side.d_out, i, t, h) : nullptr;
+            f32x2 x[NS][VEC], g[BWD ? NS : 1][VEC], squares = 0, along2 = 0;
 #pragma unroll
             for (int z = 0; z < NS; ++z) {
-                if (BWD) turn_slot<VEC, true>(a.interleaved, cs + z * VEC, g[z]);
+                uint32_t raw[2][P::kWords];
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 2; ++k) P::read(piece(slot, z * 2 + k), x0 + at[z][k], raw[k]);
+                widen<T, VEC>(raw, x[z]);
+                if constexpr (BWD) {
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        square = fmaf(x[z][k][e], x[z][k][e], square);
-                        if (BWD) along = fmaf(g[z][k][e] * w[z][k][e], x[z][k][e], along);
-                    }
+                    for (int k = 0; k < 2; ++k) P::read(piece(slot, NS * 2 + z * 2 + k), g0 + at[z][k], raw[k]);
+                    widen<T, VEC>(raw, g[z]);
+                    turn_slot<VEC>(a.interleaved, cs + z * VEC, g[z]);
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    squares = fma2(x[z][e], x[z][e], squares);
+                    if (BWD) along2 = fma2(mul2(g[z][e], w[z][e]), x[z][e], along2);
+                }
             }
             float inv = 1.f;
-            if (normed) inv = 1.f / sqrtf(fmaf(team_sum<TEAM>(square), a.inv_d, a.eps));
+            if (normed) {
+                const float2 f = unpack_f2(squares);
+                inv = rsqrtf(fmaf(team_sum<TEAM>(f.x + f.y), a.inv_d, a.eps));
+            }
             if (!active) inv = 0.f;                          // (eps may be 0: no infinity times the zeros of a missing row)
+            const f32x2 inv2 = pack_f2(inv, inv);
             if constexpr (!BWD) {
 #pragma unroll
                 for (int z = 0; z < NS; ++z) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                    for (int e = 0; e < VEC; ++e) x[z][e] = mul2(x[z][e], mul2(inv2, w[z][e]));
+                    turn_slot<VEC>(a.interleaved, cs + z * VEC, x[z]);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) x[z][k][e] *= inv * w[z][k][e];
-                    turn_slot<VEC, false>(a.interleaved, cs + z * VEC, x[z]);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        if (active && here[z][k]) store_some<T, VEC>(o0 + at[z][k], x[z][k]);
+                    for (int k = 0; k < 2; ++k) {
+                        float f[VEC];
+                        values_of<VEC>(x[z], k, f);
+                        if (active && here[z][k]) store_some<T, VEC>(o0 + at[z][k], f);
+                    }
                 }
             } else {
                 float back = 0.f;
-                if (normed) back = team_sum<TEAM>(along) * a.inv_d * inv * inv;
+                if (normed) {
+                    const float2 f = unpack_f2(along2);
+                    back = -team_sum<TEAM>(f.x + f.y) * a.inv_d * inv * inv;
+                }
+                const f32x2 back2 = pack_f2(back, back);
 #pragma unroll
-                for (int z = 0; z < NS; ++z)
+                for (int z = 0; z < NS; ++z) {
+                    f32x2 dx[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        dw[z][e] = fma2(g[z][e], mul2(x[z][e], inv2), dw[z][e]);
+                        dx[e] = mul2(inv2, fma2(back2, x[z][e], mul2(g[z][e], w[z][e])));
+                    }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        float dx[VEC];
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            dw[z][k][e] = fmaf(g[z][k][e], x[z][k][e] * inv, dw[z][k][e]);
-                            dx[e] = inv * fmaf(-back, x[z][k][e], g[z][k][e] * w[z][k][e]);
-                        }
-                        if (o0 && active && here[z][k]) store_some<T, VEC>(o0 + at[z][k], dx);
+                        float f[VEC];
+                        values_of<VEC>(dx, k, f);
+                        if (o0 && active && here[z][k]) store_some<T, VEC>(o0 + at[z][k], f);
                     }
+                }
             }
         }
-        unit = next;
-        pos = pos2;
-        t = t2;
-        q = q1;
+        if (++q == turns) { q = 0; t += stride; }
+        if (++slot == DEPTH) slot = 0;
     }
     if constexpr (BWD) {
         // sums of the CTA: over the teams of a warp, then over the warps
@@ -309,14 +364,17 @@ __global__ void __launch_bounds__(kThreads, BWD ? kCtasBackward : kCtasForward) 
 #pragma unroll
         for (int z = 0; z < NS; ++z)
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k) {
+                float f[VEC];
+                values_of<VEC>(dw[z], k, f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    float v = dw[z][k][e];
+                    float v = f[e];
 #pragma unroll
                     for (int o = TEAM; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
                     if (group == 0 && here[z][k]) s_sum[warp][at[z][k] + e] = v;
                 }
+            }
         __syncthreads();
         float* to = side.partial + ((long long)i * side.ctas + b) * a.d;
         for (int c = threadIdx.x; c < a.d; c += kThreads) {
@@ -392,7 +450,7 @@ bool valid(const eg_head_norm_args* q, bool backward) {
     if (q->P < 1 || q->P > 65535 || q->rows < 0 || q->rows > (1ll << 30) || q->width < 1 || q->width > kMaxWidth) return false;
     if (q->q_heads < 1 || q->q_heads > 65535 || q->k_heads < 0 || q->k_heads > 65535) return false;
     if (q->rotary < 0 || q->rotary > q->width || q->rotary % 2) return false;
-    if (!(q->eps >= 0.0) || q->eps > 3e38 || !(q->base >= 1e-30) || q->base > 1e30) return false;
+    if (!(q->eps >= 0.0) || q->eps > 3e38 || !(q->base >= 1.0) || q->base > 1e30) return false;
     const size_t size = q->dtype == EG_F32 ? 4 : 2;
     if (q->positions && ((q->position_bytes != 4 && q->position_bytes != 8) || (uintptr_t)q->positions % (size_t)q->position_bytes ||
                          q->position_replica_stride < 0 || q->position_stride < 0 || q->position_replica_stride >= (1ll << 40) ||
@@ -466,35 +524,47 @@ int fill(HeadArgs* a, const eg_head_norm_args* q, bool backward, float* partial)
         Side* s = &a->side[m];
         s->heads = (int)both[m].H;
         s->ctas = n.ctas[m];
-        // few places of a CTA: warps share their heads
+        // few places of a CTA: warps share their heads.  A warp's places times its turns for each, and about one for the sines
         const int64_t places = s->ctas ? (q->rows + s->ctas - 1) / s->ctas : 1;
-        s->split = 1;
-        while (s->split < kWarps && places * s->split < kWarps) s->split *= 2;
+        int team = v * (int)size == 16 ? 2 : 32;
+        while (team < 32 && team < a->slots) team *= 2;
+        const int64_t turns = (s->heads * team + 31) / 32;
+        int64_t least = 0;
+        for (int split = 1; split <= kWarps; split *= 2) {
+            const int64_t time = (places * split + kWarps - 1) / kWarps * ((turns + split - 1) / split + 1);
+            if (split == 1 || time < least) {
+                least = time;
+                s->split = split;
+            }
+        }
         s->x = heads(*both[m].x); s->out = heads(*both[m].out); s->d_out = heads(*both[m].d_out);
         s->w = Vec{both[m].w->data, (long long)both[m].w->replica_stride};
         s->partial = backward && both[m].dw->data ? partial + (m ? q->P * (int64_t)n.ctas[0] * q->width : 0) : nullptr;
     }
-    const double full = 6.283185307179586476925;
-    const double step = a->rotary > 0 ? -2.0 * log(q->base) / a->rotary : 0.0;
-    for (int j = 0; j < a->half; ++j) a->turns[j] = exp(step * j) / full;
+    const double full = 6.283185307179586476925, step = a->rotary > 0 ? -2.0 * log(q->base) / a->rotary : 0.0;
+    for (int j = 0; j < a->half; ++j) a->turns[j] = (unsigned long long)(exp(step * j) / full * 18446744073709551616.0);   // (below 0.16 of a turn)
     return v;
 }
 
 template <typename T, bool BWD> cudaError_t launch(const HeadArgs& a, int v, cudaStream_t stream) {
     constexpr int V = 16 / (int)sizeof(T);
     const dim3 grid(a.side[0].ctas + a.side[1].ctas, a.P);
-    auto run = [&](auto kernel) { return launch_after(kernel, grid, dim3(kThreads), 0, stream, a); };
+    auto run = [&](auto kernel, int smem) {
+        cudaError_t e = cudaSuccess;                         // (48 KB need no permission, but the sums are part of them)
+        if (smem > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        return e != cudaSuccess ? e : launch_after(kernel, grid, dim3(kThreads), smem, stream, a);
+    };
     static_assert(kMaxWidth / (2 * V) <= 32 && kMaxWidth / 4 <= 2 * 32 && kMaxWidth / 2 <= 4 * 32, "slots of a row");
     if (v == V) {
-        if (a.slots <= 2) return run(k_head_norm<T, V, 1, 2, BWD>);
-        if (a.slots <= 4) return run(k_head_norm<T, V, 1, 4, BWD>);
-        if (a.slots <= 8) return run(k_head_norm<T, V, 1, 8, BWD>);
-        if (a.slots <= 16) return run(k_head_norm<T, V, 1, 16, BWD>);
-        return run(k_head_norm<T, V, 1, 32, BWD>);
+        if (a.slots <= 2) return run(k_head_norm<T, V, 1, 2, BWD>, Ring<T, V, 1, BWD>::kBytes);
+        if (a.slots <= 4) return run(k_head_norm<T, V, 1, 4, BWD>, Ring<T, V, 1, BWD>::kBytes);
+        if (a.slots <= 8) return run(k_head_norm<T, V, 1, 8, BWD>, Ring<T, V, 1, BWD>::kBytes);
+        if (a.slots <= 16) return run(k_head_norm<T, V, 1, 16, BWD>, Ring<T, V, 1, BWD>::kBytes);
+        return run(k_head_norm<T, V, 1, 32, BWD>, Ring<T, V, 1, BWD>::kBytes);
     }
-    if (v == 2) return a.slots <= 32 ? run(k_head_norm<T, 2, 1, 32, BWD>) : run(k_head_norm<T, 2, 2, 32, BWD>);
-    if (a.slots <= 32) return run(k_head_norm<T, 1, 1, 32, BWD>);
-    return a.slots <= 64 ? run(k_head_norm<T, 1, 2, 32, BWD>) : run(k_head_norm<T, 1, 4, 32, BWD>);
+    if (v == 2) return a.slots <= 32 ? run(k_head_norm<T, 2, 1, 32, BWD>, Ring<T, 2, 1, BWD>::kBytes) : run(k_head_norm<T, 2, 2, 32, BWD>, Ring<T, 2, 2, BWD>::kBytes);
+    if (a.slots <= 32) return run(k_head_norm<T, 1, 1, 32, BWD>, Ring<T, 1, 1, BWD>::kBytes);
+    return a.slots <= 64 ? run(k_head_norm<T, 1, 2, 32, BWD>, Ring<T, 1, 2, BWD>::kBytes) : run(k_head_norm<T, 1, 4, 32, BWD>, Ring<T, 1, 4, BWD>::kBytes);
 }
 
 template <typename T> cudaError_t backward(const HeadArgs& a, int v, const eg_head_norm_args* q, cudaStream_t stream) {
