@@ -1,9 +1,14 @@
 // The products of eg_orthogonalise on the tensor cores (sm_100a).
 //
-// One launch forms one of the three products of a step for all matrices of all replicas (instances):
-//   gram     A = X X^T                                    X: m x n, m <= n
-//   square   B = b A + c A^2
-//   apply    X <- a X + B X                               (the last step: into the caller's matrix)
+// One launch forms one product of a step for all matrices of all replicas (instances).  X: m x n, m <= n.
+//   gram     A = X X^T
+//   sym      f0 E0 + f1 E1 + fd L R          of symmetric m x m matrices that commute (all are polynomials of A)
+//   apply    X <- a X + S X                  (the last one: into the caller's matrix)
+// One step is gram, B = b A + c A^2, apply with B.  Where products are of full precision, two steps share one gram and one apply, since
+// the second step's gram is known from the first one's:  Q0 = a0 + B0,  A1 = Q0 A Q0 = a0^2 A + 2 a0 C + C B0 with C = A B0,
+// Q1 Q0 = a0 a1 + (a1 B0 + a0 B1 + B1 B0).  Five symmetric products of m^3 take the place of 3 m^2 n + 2 m^3: never more work, and 40 % less
+// where n = 9 m (8 ResNet-18s: 3.5 -> 2.4 ms).  With operands of 11 bits the second step would see three times the
+// error, and two steps stay two.
 //
 // Everything in between lies in the workspace as fp16 boxes of 64 x 64, each 8 KB in one piece and already in the order that the
 // tensor cores want in shared memory (128-byte swizzle): one tensor map serves all matrices of any size, a copy is a whole box,
@@ -31,7 +36,8 @@ namespace eg {
 constexpr int kBox = 64, kBoxBytes = 8192;
 constexpr int kOrthoMats = 48;                    // matrices of one launch
 constexpr int kOrthoChunk = 2;
-enum { kGram = 0, kSquare = 1, kApply = 2, kLast = 3 };
+// kSym0, kSym1, kSym2: with so many terms E.
+enum { kGram = 0, kSym0 = 1, kSym1 = 2, kSym2 = 3, kApply = 4, kLast = 5 };
 
 struct Strided {
     void* p;
@@ -44,28 +50,34 @@ struct OrthoMat {
     int tiles[2];                                 // of one replica: of the symmetric products, of X
     int first;                                    // instance of replica 0
     float scale;
-    long long x[2], a, b;                         // first boxes of replica 0: X before and after a step, A, B
-    long long x_rep, s_rep;                       // boxes from one replica to the next (X, A and B); lo parts lie half as far
+    long long x[2], s[3];                         // first boxes of replica 0: X before and after a step, symmetric matrices
+    long long x_rep, s_rep;                       // boxes from one replica to the next; lo parts lie half as far
     Strided grad, out, velocity, velocity_out;
-    // k_ortho_norm: rows of `cols` values, units of kNormUnit of them; blocks of an instance
-    long long view_rows, view_cols, units;
-    int blocks, begin;                            // begin: first block of replica 0
-    int boxes_begin;                              // k_ortho_in: first block
+    int items, begin;                             // of k_ortho_in: items of an instance, the first one of replica 0
+};
+
+// One launch.
+struct OrthoPass {
+    int from;                                     // which X is read
+    int first;                                    // X is still to be multiplied by `turn`
+    int l, r, e0, e1, to;                         // symmetric matrices; apply: l
+    float f0, f1, fd;                             // gram: fd;  apply: f0 X + fd S X
 };
 
 struct OrthoArgs {
     CUtensorMap map;                              // the workspace as rows of 128 bytes
     unsigned char* ws;
-    double* partial;                              // [instances][kNormBlocks] sums of squares
+    double* partial;                              // [instances][kMaxItems] sums of squares
+    int* done;                                    // [instances] items whose sum of squares is there
+    int* ticket;                                  // of k_ortho_in
+    int items, lag;
     float* turn;                                  // [instances] what is left of 1 / |u| after a power of two
     unsigned int* err;
     int P, count;
     int tiles[2];
     float momentum;
     int nesterov;
-    float sx;                                     // powers of two before X, A, B
-    float gram, ca, cb, ci;                       // gram: D -> A;  square: A -> B (b), D -> B (c);  apply: D -> X
-    float a, out;                                 // a;  X -> result
+    float sx, out;                                // power of two before X; X -> result
     OrthoMat mat[kOrthoMats];
 };
 
@@ -127,10 +139,11 @@ __device__ __forceinline__ void split_half2(float x, float y, uint32_t& hi, uint
 
 // T: type of the caller's matrices (kLast).
 template <typename T, int PARTS, int PASS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_ortho(const __grid_constant__ OrthoArgs a, int step) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_ortho(const __grid_constant__ OrthoArgs a, const OrthoPass pass) {
     using Shape = OrthoShape<PARTS>;
     constexpr int BN = Shape::kBN, S = Shape::kStages;
-    constexpr bool SYMMETRIC = PASS == kGram || PASS == kSquare;
+    constexpr bool SYMMETRIC = PASS < kApply;
+    constexpr int TERMS = PASS == kGram || PASS == kSym0 ? 0 : PASS == kSym2 ? 2 : 1;      // that come in from memory
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring_b = smem + S * Shape::kA;
@@ -170,7 +183,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
     // set up while the kernel before this one finished; from here on its results are read and overwritten
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = a.tiles[SYMMETRIC ? 0 : 1];
-    const int from = step & 1;
+    const int from = pass.from;
     OrthoWalk walk;
 
     if (warp == 0 || warp == 3) {
@@ -181,7 +194,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                 const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
                 const OrthoMat& g = a.mat[q.k];
                 const bool left = warp == 0;
-                const long long x = g.x[from] + q.p * g.x_rep, sym = (PASS == kSquare ? g.a : g.b) + q.p * g.s_rep;
+                const long long x = g.x[from] + q.p * g.x_rep, sym = g.s[left ? pass.l : pass.r] + q.p * g.s_rep;
                 const int ksteps = PASS == kGram ? g.cb : g.rb;
                 constexpr int RIGHT = BN / 128;                           // boxes of the right operand that a CTA fetches
                 const int limit = left || SYMMETRIC ? g.rb : g.cb;
@@ -237,7 +250,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                 const uint32_t small = tmem + (2 + (turn & 1)) * 128;
                 if (PARTS == 2 && turn >= 2) mbar_wait(&small_empty[turn & 1], ((turn >> 1) - 1) & 1, s_abort, a.err);
                 for (int k = 0; k < ksteps; ++k) {
-                    const bool a_mn = PASS != kGram && k / 4 > q.i, b_mn = PASS >= kApply || (PASS == kSquare && k / 4 > right_block);
+                    const bool a_mn = PASS != kGram && k / 4 > q.i, b_mn = PASS >= kApply || (PASS != kGram && k / 4 > right_block);
                     const uint32_t idesc = (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) |
                                            ((uint32_t)(kGemmM >> 4) << 24);
                     const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
@@ -285,29 +298,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
             const OrthoMat& g = a.mat[q.k];
             const int ksteps = PASS == kGram ? g.cb : g.rb;
             const int rbox = q.i * 4 + (int)rank * 2 + (quad >> 1), cols = SYMMETRIC ? g.rb : g.cb;
-            const long long x = g.x[from] + q.p * g.x_rep, sym_a = g.a + q.p * g.s_rep, sym_b = g.b + q.p * g.s_rep;
-            const float left_of = step == 0 ? a.turn[g.first + q.p] : 1.f;
+            const long long x = g.x[from] + q.p * g.x_rep, lo = (SYMMETRIC ? g.s_rep : g.x_rep) / 2;
+            const long long to = SYMMETRIC ? g.s[pass.to] + q.p * g.s_rep : g.x[from ^ 1] + q.p * g.x_rep;
+            const float left_of = pass.first && (PASS == kGram || PASS >= kApply) ? a.turn[g.first + q.p] : 1.f;
             auto cbox = [&](int c) { return q.j * (BN / kBox) + half * Shape::kChunks + c; };
             auto inside = [&](int c) { return rbox < g.rb && cbox(c) < cols; };
             auto place = [&](long long matrix, int c) { return a.ws + (matrix + (long long)cbox(c) * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096; };
-            // what the result is added to comes in ahead of the products
-            auto fetch = [&](int c) {
-                if (PASS == kGram || !inside(c)) return;
+            // what the result is added to
+            auto fetch = [&](int c, int term) {
+                if (TERMS == 0 || !inside(c)) return;
                 store_wait_read<0>();
                 __syncwarp();
                 if (elect_one()) {
-                    constexpr bool BOTH = PARTS == 2 || PASS != kSquare;
-                    const long long matrix = PASS == kSquare ? sym_a : x, lo = (PASS == kSquare ? g.s_rep : g.x_rep) / 2;
+                    constexpr bool BOTH = PARTS == 2 || !SYMMETRIC;
+                    const long long matrix = SYMMETRIC ? g.s[term ? pass.e1 : pass.e0] + q.p * g.s_rep : x;
                     op_mbar_expect(&epi_full[w], BOTH ? 8192 : 4096);
                     op_bulk_load(buf, place(matrix, c), 4096, &epi_full[w]);
                     if (BOTH) op_bulk_load(buf + 4096, place(matrix + lo, c), 4096, &epi_full[w]);
                 }
             };
-            fetch(0);
-            float sum[PARTS == 2 ? 64 : 1];                       // this row's 64 columns, added up over the chunks
+            fetch(0, 0);
+            float sum[PARTS == 2 ? 64 : 1];                       // this row's 64 columns: the terms, then the products' chunks
             if constexpr (PARTS == 2) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e) sum[e] = 0.f;
+                if (inside(0)) {
+#pragma unroll 1
+                    for (int term = 0; term < TERMS; ++term) {
+                        if (term > 0) fetch(0, term);
+                        mbar_wait(&epi_full[w], uses & 1, s_abort, a.err);
+                        ++uses;
+                        const float f = term ? pass.f1 : pass.f0;
+#pragma unroll
+                        for (int e = 0; e < 64; e += 8) {
+                            const unsigned char* at = buf + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4);
+                            const uint4 h4 = *reinterpret_cast<const uint4*>(at), l4 = *reinterpret_cast<const uint4*>(at + 4096);
+                            const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const float2 hf = unpack2<__half>(hw[z]), lf = unpack2<__half>(lw[z]);
+                                sum[e + 2 * z] = fmaf(f, hf.x, fmaf(f, lf.x, sum[e + 2 * z]));
+                                sum[e + 2 * z + 1] = fmaf(f, hf.y, fmaf(f, lf.y, sum[e + 2 * z + 1]));
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
                 auto take = [&](uint32_t acc) {
                     tc_fence_after();
 #pragma unroll
@@ -315,7 +351,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                         uint32_t v[32];
                         tc_load(v, acc + lanes + half * 64 + e);
 #pragma unroll
-                        for (int z = 0; z < 32; ++z) sum[e + z] += __uint_as_float(v[z]);
+                        for (int z = 0; z < 32; ++z) sum[e + z] = fmaf(pass.fd, __uint_as_float(v[z]), sum[e + z]);
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -335,12 +371,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
             const uint32_t acc = tmem + (count & 1) * BN + lanes + half * (BN / 2);
 #pragma unroll 1
             for (int c = 0; c < Shape::kChunks; ++c) {
-                if (c > 0) fetch(c);
+                if (PARTS == 1 && c > 0) fetch(c, 0);
                 if (!inside(c)) continue;
-                if (PASS == kGram) {
+                if (TERMS == 0) {
                     store_wait_read<0>();
                     __syncwarp();
-                } else {
+                } else if (PARTS == 1) {
                     mbar_wait(&epi_full[w], uses & 1, s_abort, a.err);
                     ++uses;
                 }
@@ -351,29 +387,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                     if constexpr (PARTS == 1) tc_load(d, acc + c * 64 + x0);
                     float* r = v + (PASS == kLast ? x0 : 0);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) r[e] = PARTS == 2 ? sum[PARTS == 2 ? x0 + e : 0] : __uint_as_float(d[e]);
+                    for (int e = 0; e < 32; ++e) r[e] = PARTS == 2 ? sum[PARTS == 2 ? x0 + e : 0] : pass.fd * __uint_as_float(d[e]);
+                    const float by = PASS == kGram ? left_of * left_of : left_of;
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         unsigned char* at = buf + lane * 128 + ((((x0 + e) >> 3) ^ (lane & 7)) << 4);
-                        if constexpr (PASS == kGram) {
-#pragma unroll
-                            for (int z = 0; z < 8; ++z) r[e + z] *= a.gram * left_of * left_of;
-                        } else {
+                        if constexpr (PARTS == 1 && TERMS > 0) {
                             const uint4 h4 = *reinterpret_cast<const uint4*>(at);
                             uint4 l4 = make_uint4(0, 0, 0, 0);
-                            if (PARTS == 2 || PASS != kSquare) l4 = *reinterpret_cast<const uint4*>(at + 4096);
+                            if (!SYMMETRIC) l4 = *reinterpret_cast<const uint4*>(at + 4096);
                             const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
-                            const float with = PASS == kSquare ? a.ca : a.a, by = PASS == kSquare ? a.cb : a.ci;
 #pragma unroll
                             for (int z = 0; z < 4; ++z) {
                                 const float2 hf = unpack2<__half>(hw[z]), lf = unpack2<__half>(lw[z]);
-                                r[e + 2 * z] = fmaf(with, hf.x, fmaf(with, lf.x, by * r[e + 2 * z]));
-                                r[e + 2 * z + 1] = fmaf(with, hf.y, fmaf(with, lf.y, by * r[e + 2 * z + 1]));
-                                if (PASS >= kApply) {
-                                    r[e + 2 * z] *= left_of;
-                                    r[e + 2 * z + 1] *= left_of;
-                                }
+                                r[e + 2 * z] = fmaf(pass.f0, hf.x, fmaf(pass.f0, lf.x, r[e + 2 * z]));
+                                r[e + 2 * z + 1] = fmaf(pass.f0, hf.y, fmaf(pass.f0, lf.y, r[e + 2 * z + 1]));
                             }
+                        }
+                        if constexpr (PASS == kGram || PASS >= kApply) {
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) r[e + z] *= by;
                         }
                         if constexpr (PASS != kLast) {
                             uint32_t hw[4], lw[4];
@@ -388,10 +421,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                     fence_async_shared();
                     __syncwarp();
                     if (elect_one()) {
-                        const long long matrix = PASS == kGram ? sym_a : PASS == kSquare ? sym_b : g.x[from ^ 1] + q.p * g.x_rep;
-                        const long long lo = (SYMMETRIC ? g.s_rep : g.x_rep) / 2;
-                        bulk_store(place(matrix, c), buf, 4096);
-                        if (PARTS == 2 || PASS == kApply) bulk_store(place(matrix + lo, c), buf + 4096, 4096);
+                        bulk_store(place(to, c), buf, 4096);
+                        if (PARTS == 2 || PASS == kApply) bulk_store(place(to + lo, c), buf + 4096, 4096);
                         store_commit();
                     }
                 } else {
@@ -400,10 +431,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                     T* out = static_cast<T*>(g.out.p) + q.p * g.out.rep;
                     if (g.flip) {                                 // a row of X is a column of the result
                         if (row0 + lane < g.m) {
-                            T* to = out + (long long)col0 * g.out.row + row0 + lane;
+                            T* at = out + (long long)col0 * g.out.row + row0 + lane;
 #pragma unroll
                             for (int e = 0; e < 64; ++e)
-                                if (col0 + e < g.n) to[e * g.out.row] = from_f32<T>(v[e] * scale);
+                                if (col0 + e < g.n) at[e * g.out.row] = from_f32<T>(v[e] * scale);
                         }
                     } else {
                         // through shared memory, 32 rows of 64 values, to runs along the rows
@@ -414,22 +445,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                                 make_float4(v[e] * scale, v[e + 1] * scale, v[e + 2] * scale, v[e + 3] * scale);
                         __syncwarp();
                         const int rows = min(32, g.m - row0), n = min(64, g.n - col0);
-                        T* to = out + (long long)row0 * g.out.row + col0;
+                        T* line = out + (long long)row0 * g.out.row + col0;
                         auto value = [&](int r, int x) { return buf + r * 256 + (((x >> 2) ^ (r & 15)) << 4) + (x & 3) * 4; };
-                        const bool pairs_of = sizeof(T) == 2 && ((uintptr_t)to & 3) == 0 && (g.out.row & 1) == 0;
+                        const bool pairs_of = sizeof(T) == 2 && ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
 #pragma unroll 4
-                        for (int r = 0; r < rows; ++r, to += g.out.row) {
+                        for (int r = 0; r < rows; ++r, line += g.out.row) {
                             if (pairs_of) {
                                 const int x0 = 2 * lane;
                                 const float2 f = *reinterpret_cast<const float2*>(value(r, x0));
                                 if constexpr (sizeof(T) == 2) {
-                                    if (x0 + 1 < n) *reinterpret_cast<uint32_t*>(to + x0) = pack2<T>(f.x, f.y);
-                                    else if (x0 < n) to[x0] = from_f32<T>(f.x);
+                                    if (x0 + 1 < n) *reinterpret_cast<uint32_t*>(line + x0) = pack2<T>(f.x, f.y);
+                                    else if (x0 < n) line[x0] = from_f32<T>(f.x);
                                 }
                             } else {
                                 const float f0 = *reinterpret_cast<const float*>(value(r, lane)), f1 = *reinterpret_cast<const float*>(value(r, lane + 32));
-                                if (lane < n) to[lane] = from_f32<T>(f0);
-                                if (lane + 32 < n) to[lane + 32] = from_f32<T>(f1);
+                                if (lane < n) line[lane] = from_f32<T>(f0);
+                                if (lane + 32 < n) line[lane + 32] = from_f32<T>(f1);
                             }
                         }
                         // the next box's copy comes by another way than these reads

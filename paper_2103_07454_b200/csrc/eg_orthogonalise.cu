@@ -5,8 +5,8 @@
 //   steps times   X <- a X + (b A + c A^2) X,   A = X X^T       (an odd polynomial of X's singular values, which pulls them to 1)
 //   out = scale * X
 //
-// Launches: k_ortho_norm (velocity, sums of squares), k_ortho_in (X in the workspace's boxes), then three products a step
-// (eg_orthogonal_gemm.cuh), each over all matrices of all replicas: a network's small matrices fill the machine together.
+// Launches: k_ortho_in (velocity, norms, X in the workspace's boxes), then the products (eg_orthogonal_gemm.cuh), each over all
+// matrices of all replicas: a network's small matrices fill the machine together.
 //
 // Only a power of two of 1 / |u| goes into X at first, so that gradients of 16 bits enter the products without a rounding; the rest,
 // between 1 and 2, is multiplied onto the first step's results in 32 bits.
@@ -18,9 +18,8 @@
 namespace eg {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kNormUnit = 4 * kThreads;           // values of a row that a block takes at a time
-constexpr int kNormBlocks = 128;                  // of an instance, at most
+constexpr int kThreads = 256, kInCtas = 5;        // k_ortho_in: CTAs of a multiprocessor
+constexpr int kMaxItems = 512;                    // of an instance
 constexpr long long kGroupBytes = 1ll << 30;      // workspace of one group of matrices that share their launches (one matrix may need more)
 
 // u of four neighbouring values, and v' where it is formed.
@@ -44,12 +43,15 @@ template <typename T, bool FORM> __device__ __forceinline__ void update4(const O
                 u[0] = f0.x; u[1] = f0.y; u[2] = f1.x; u[3] = f1.y;
             }
         }
-        if (v) load_vec<float, 4>(v, w);
+        if (v) {                                              // (v' comes from other multiprocessors' hands)
+            const float4 x = FORM ? *reinterpret_cast<const float4*>(v) : __ldcg(reinterpret_cast<const float4*>(v));
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             u[e] = e < n && need_g ? to_f32(g[e]) : 0.f;
-            if (v) w[e] = e < n ? v[e] : 0.f;
+            if (v) w[e] = e < n ? (FORM ? v[e] : __ldcg(v + e)) : 0.f;
         }
     }
     if (!v) return;
@@ -73,104 +75,134 @@ __device__ __forceinline__ bool quads(const OrthoMat& m, size_t size) {
     return fits(m.grad, size) && fits(m.velocity, 4) && fits(m.velocity_out, 4);
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) k_ortho_norm(const __grid_constant__ OrthoArgs a) {
+// Two phases over the boxes of all instances, in one launch.  Phase 1 updates the velocity and adds up squares; phase 2 reads the same
+// values again, `lag` items later, while they are still in the L2, and writes X.  Items are handed out in order by a counter, so
+// that an item of phase 2 waits for items only that running CTAs hold.
+//   positions 0 .. lag - 1: phase 1 of items 0 .. lag - 1;  then in turn phase 1 of the next item and phase 2 of the next one;  then the
+//   last items of phase 2
+template <typename T> __global__ void __launch_bounds__(kThreads, kInCtas) k_ortho_in(const __grid_constant__ OrthoArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ double s_sum[kThreads / 32];
-    int k = 0;
-    while (k + 1 < a.count && (int)blockIdx.x >= a.mat[k + 1].begin) ++k;
-    const OrthoMat& m = a.mat[k];
-    const int at = blockIdx.x - m.begin, p = at / m.blocks, b = at - p * m.blocks;
-    const bool vec = quads(m, sizeof(T));
-    const long long per = (m.view_cols + kNormUnit - 1) / kNormUnit;
-    double sum = 0.0;
-    for (long long q = b; q < m.units; q += m.blocks) {
-        const long long row = q / per, c = (q - row * per) * kNormUnit + threadIdx.x * 4;
-        if (c >= m.view_cols) continue;
-        const int n = m.view_cols - c < 4 ? (int)(m.view_cols - c) : 4;
-        float u[4];
-        update4<T, true>(a, m, p, row, c, n, vec, u);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < n) sum = fma((double)u[e], (double)u[e], sum);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kThreads / 32; ++w) sum += s_sum[w];
-        a.partial[(long long)(m.first + p) * kNormBlocks + b] = sum;
-    }
-}
-
-// A block: one box of X.
-template <typename T> __global__ void __launch_bounds__(kThreads) k_ortho_in(const __grid_constant__ OrthoArgs a) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    __shared__ double s_sum[kNormBlocks / 32];
     __shared__ float s_box[kBox][kBox + 1];
-    int k = 0;
-    while (k + 1 < a.count && (int)blockIdx.x >= a.mat[k + 1].boxes_begin) ++k;
-    const OrthoMat& m = a.mat[k];
-    const int boxes = m.rb * m.cb, at = blockIdx.x - m.boxes_begin, p = at / boxes, box = at - p * boxes;
-    const int cbox = box / m.rb, rbox = box - cbox * m.rb;
-    if (threadIdx.x < kNormBlocks) {
-        double s = (int)threadIdx.x < m.blocks ? a.partial[(long long)(m.first + p) * kNormBlocks + threadIdx.x] : 0.0;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = s;
-    }
-    const bool vec = quads(m, sizeof(T));
-    // quad z of a thread: row z * 16 + threadIdx.x / 16 of the box (of the gradient's), columns 4 * (threadIdx.x % 16)
-    float u[4][4];
+    __shared__ int s_next;
     const int quad = threadIdx.x & 15, first = threadIdx.x >> 4;
-    const int row0 = (m.flip ? cbox : rbox) * kBox, col0 = (m.flip ? rbox : cbox) * kBox + quad * 4;
-    const int rows = m.flip ? m.n : m.m, cols = m.flip ? m.m : m.n;
-#pragma unroll
-    for (int z = 0; z < 4; ++z) {
-        const int r = row0 + z * 16 + first;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) u[z][e] = 0.f;
-        if (r < rows && col0 < cols) update4<T, false>(a, m, p, r, col0, cols - col0 < 4 ? cols - col0 : 4, vec, u[z]);
-    }
-    __syncthreads();
-    double total = 0.0;
-#pragma unroll
-    for (int w = 0; w < kNormBlocks / 32; ++w) total += s_sum[w];
-    const double norm = sqrt(total);
-    int ex = 0;
-    double fraction = 0.0;
-    const bool finite = norm <= 1.7e308;                  // (false for NaN too)
-    if (finite) fraction = frexp(norm, &ex);              // norm = fraction * 2^ex, 1/2 <= fraction < 1
-    const double by = ldexp((double)a.sx, -ex);
-    if (box == 0 && threadIdx.x == 0)
-        a.turn[m.first + p] = !finite ? __int_as_float(0x7fffffff) : fraction > 0.0 ? (float)(1.0 / fraction) : 0.f;
-#pragma unroll
-    for (int z = 0; z < 4; ++z)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) u[z][e] = (float)((double)u[z][e] * by);
-    if (m.flip) {
-#pragma unroll
-        for (int z = 0; z < 4; ++z)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s_box[quad * 4 + e][z * 16 + first] = u[z][e];
+    for (;;) {
         __syncthreads();
+        if (threadIdx.x == 0) s_next = atomicAdd(a.ticket, 1);
+        __syncthreads();
+        const int pos = s_next, N = a.items, lag = a.lag;
+        if (pos >= 2 * N) return;
+        const bool form = pos < lag || (pos < 2 * N - lag && ((pos - lag) & 1) == 0);
+        const int item = pos < lag ? pos : pos >= 2 * N - lag ? pos - N : form ? lag + (pos - lag) / 2 : (pos - lag) / 2;
+        int k = 0;
+        while (k + 1 < a.count && item >= a.mat[k + 1].begin) ++k;
+        const OrthoMat& m = a.mat[k];
+        const int p = (item - m.begin) / m.items, b = item - m.begin - p * m.items, instance = m.first + p;
+        const bool vec = quads(m, sizeof(T));
+        const int rows = m.flip ? m.n : m.m, cols = m.flip ? m.m : m.n;         // of the gradient
+        const int wide = m.flip ? m.rb : m.cb, boxes = m.rb * m.cb;
+        const int box0 = (int)((long long)boxes * b / m.items), box1 = (int)((long long)boxes * (b + 1) / m.items);
+        // quad z of a thread: row z * 16 + first of the gradient's box, columns 4 * quad
+        auto load = [&](int box, auto forming, float (&u)[4][4]) {
+            const int grow = box / wide, r0 = grow * kBox + first, c = (box - grow * wide) * kBox + quad * 4;
 #pragma unroll
-        for (int z = 0; z < 4; ++z)
+            for (int z = 0; z < 4; ++z) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) u[z][e] = s_box[z * 16 + first][quad * 4 + e];
-    }
-    unsigned char* hi = a.ws + (m.x[0] + p * m.x_rep + box) * kBoxBytes;
-    unsigned char* lo = hi + m.x_rep / 2 * kBoxBytes;
+                for (int e = 0; e < 4; ++e) u[z][e] = 0.f;
+                if (r0 + z * 16 < rows && c < cols)
+                    update4<T, decltype(forming)::value>(a, m, p, r0 + z * 16, c, cols - c < 4 ? cols - c : 4, vec, u[z]);
+            }
+        };
+        if (form) {
+            double sum = 0.0;
+            for (int box = box0; box < box1; ++box) {
+                float u[4][4];
+                load(box, std::true_type{}, u);
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-        uint32_t h0, h1, l0, l1;
-        split_half2(u[z][0], u[z][1], h0, l0);
-        split_half2(u[z][2], u[z][3], h1, l1);
-        const uint32_t off = swz128((z * 16 + first) * 128 + quad * 8);
-        *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
-        *reinterpret_cast<uint2*>(lo + off) = make_uint2(l0, l1);
+                for (int z = 0; z < 4; ++z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum = fma((double)u[z][e], (double)u[z][e], sum);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+            __syncthreads();                                  // also: all of the velocity's stores are issued
+            if (threadIdx.x == 0) {
+                for (int w = 1; w < kThreads / 32; ++w) sum += s_sum[w];
+                a.partial[(long long)instance * kMaxItems + b] = sum;
+                __threadfence();
+                atomicAdd(a.done + instance, 1);
+            }
+            continue;
+        }
+        if (threadIdx.x == 0) {
+            const long long t0 = clock64();
+            for (unsigned spins = 1;; ++spins) {
+                int there;
+                asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(there) : "l"(a.done + instance) : "memory");
+                if (there >= m.items) break;
+                if ((spins & 63u) == 0 && clock64() - t0 > kOpWaitCycles) {
+                    atomicOr(a.err, kOpErrWaitTimeout);
+                    break;
+                }
+            }
+        }
+        __syncthreads();
+        {
+            double s = 0.0;
+            for (int q = threadIdx.x; q < m.items; q += kThreads) s += __ldcg(a.partial + (long long)instance * kMaxItems + q);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = s;
+        }
+        __syncthreads();
+        double total = 0.0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
+        const double norm = sqrt(total);
+        int ex = 0;
+        double fraction = 0.0;
+        const bool finite = norm <= 1.7e308;                  // (false for NaN too)
+        if (finite) fraction = frexp(norm, &ex);              // norm = fraction * 2^ex, 1/2 <= fraction < 1
+        const double by = ldexp((double)a.sx, -ex);
+        if (b == 0 && threadIdx.x == 0)
+            a.turn[instance] = !finite ? __int_as_float(0x7fffffff) : fraction > 0.0 ? (float)(1.0 / fraction) : 0.f;
+        for (int box = box0; box < box1; ++box) {
+            float u[4][4];
+            load(box, std::false_type{}, u);
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[z][e] = (float)((double)u[z][e] * by);
+            int rbox = box / wide, cbox = box - rbox * wide;
+            if (m.flip) {
+                const int x = rbox;
+                rbox = cbox;
+                cbox = x;
+                __syncthreads();
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s_box[quad * 4 + e][z * 16 + first] = u[z][e];
+                __syncthreads();
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[z][e] = s_box[z * 16 + first][quad * 4 + e];
+            }
+            unsigned char* hi = a.ws + (m.x[0] + p * m.x_rep + (long long)cbox * m.rb + rbox) * kBoxBytes;
+            unsigned char* lo = hi + m.x_rep / 2 * kBoxBytes;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                uint32_t h0, h1, l0, l1;
+                split_half2(u[z][0], u[z][1], h0, l0);
+                split_half2(u[z][2], u[z][3], h1, l1);
+                const uint32_t off = swz128((z * 16 + first) * 128 + quad * 8);
+                *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
+                *reinterpret_cast<uint2*>(lo + off) = make_uint2(l0, l1);
+            }
+        }
     }
 }
 
@@ -179,8 +211,8 @@ constexpr int kMaxSteps = 64;
 const double kDefault[3] = {3.4445, -4.7750, 2.0315};
 
 struct Scales {
-    float sx, sa, sb[kMaxSteps];
-    double c[kMaxSteps][3];
+    float sx, sa, sb[kMaxSteps], sc[kMaxSteps];           // powers of two before X, A, B, C = A B
+    double c[kMaxSteps][3], most[kMaxSteps];              // coefficients; bound of |B|
 };
 
 float power_below(double most) {                          // the largest power of two with most * it <= 60000, at most 2^14
@@ -203,7 +235,9 @@ bool scales(const eg_orthogonalise_args* q, Scales* s) {
         // |B| in the spectral norm: b x + c x^2 on 0 .. bound^2
         double highest = fabs(b * top + c * top * top);
         if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < top) highest = fmax(highest, fabs(b * b / (4 * c)));
-        s->sb[k] = power_below(fmax(highest, 1e-3) * 1.02);
+        s->most[k] = fmax(highest, 1e-3);
+        s->sb[k] = power_below(s->most[k] * 1.02);
+        s->sc[k] = power_below(fmax(s->most[k] * top, 1e-3) * 1.02);
         auto value = [&](double x) { return fabs(sqrt(x) * (a + x * (b + c * x))); };   // x: a square
         double next = value(top);
         const double disc = 9 * b * b - 20 * a * c;          // of a + 3 b x + 5 c x^2
@@ -251,7 +285,7 @@ bool valid(const eg_orthogonalise_args* q, Scales* s) {
         if (m.rows < 1 || m.columns < 1 || m.rows > (1 << 20) || m.columns > (1 << 20) || !(fabs(m.scale) <= 3e38)) return false;
         const int64_t boxes = (m.rows + 63) / 64 * ((m.columns + 63) / 64);
         const int64_t side = ((m.rows < m.columns ? m.rows : m.columns) + 63) / 64;
-        if (q->P * (4 * boxes + 4 * side * side) > (1ll << 24)) return false;              // 128 GB of workspace
+        if (q->P * (4 * boxes + 6 * side * side) > (1ll << 24)) return false;              // 128 GB of workspace
         if (!usable(m.grad, q->P, m.rows, m.columns, size_of(q->dtype), false)) return false;
         if (!usable(m.out, q->P, m.rows, m.columns, size_of(q->out_dtype), true)) return false;
         if (m.velocity.data && !usable(m.velocity, q->P, m.rows, m.columns, 4, !m.velocity_out.data)) return false;
@@ -264,27 +298,37 @@ int parts_of(const eg_orthogonalise_args* q) { return q->out_dtype == EG_BF16 ? 
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Sides {
-    int64_t rb, cb, boxes;                                // of one replica: X twice and A and B, in two parts
+    int64_t rb, cb, boxes;                                // of one replica: X twice and the symmetric matrices, in two parts
 };
-Sides sides(const eg_orthogonal_matrix& m) {
+Sides sides(const eg_orthogonalise_args* q, const eg_orthogonal_matrix& m) {
     const int64_t r = m.rows <= m.columns ? m.rows : m.columns, c = m.rows <= m.columns ? m.columns : m.rows;
     Sides s{up(r, kBox) / kBox, up(c, kBox) / kBox, 0};
-    s.boxes = 4 * s.rb * s.cb + 4 * s.rb * s.rb;
+    s.boxes = 4 * s.rb * s.cb + (parts_of(q) == 2 ? 6 : 4) * s.rb * s.rb;
     return s;
 }
 // Matrices [first, *end) share their launches.  Returns their boxes.
 int64_t group(const eg_orthogonalise_args* q, int64_t first, int64_t* end) {
     int64_t boxes = 0, i = first;
     for (; i < q->count && i - first < kOrthoMats; ++i) {
-        const int64_t more = q->P * sides(q->matrices[i]).boxes;
+        const int64_t more = q->P * sides(q, q->matrices[i]).boxes;
         if (i > first && (boxes + more) * kBoxBytes > kGroupBytes) break;
         boxes += more;
     }
     *end = i;
     return boxes;
 }
-int64_t tail_bytes(const eg_orthogonalise_args* q) {      // partial sums and scalars of a group
-    return up(q->P * kOrthoMats * (int64_t)kNormBlocks * 8, 1024) + up(q->P * kOrthoMats * 4, 1024);
+// Behind a group's boxes: partial sums, what is left of 1 / |u|, counters.
+struct Tail {
+    int64_t partial, turn, done, bytes;
+};
+Tail tail(const eg_orthogonalise_args* q) {
+    const int64_t instances = q->P * (q->count < kOrthoMats ? q->count : kOrthoMats);
+    Tail t;
+    t.partial = 0;
+    t.turn = up(instances * kMaxItems * 8, 256);
+    t.done = t.turn + up(instances * 4, 256);
+    t.bytes = t.done + up((instances + 1) * 4, 256);
+    return t;
 }
 int64_t workspace_of(const eg_orthogonalise_args* q) {
     int64_t most = 0, end = 0;
@@ -292,38 +336,52 @@ int64_t workspace_of(const eg_orthogonalise_args* q) {
         const int64_t boxes = group(q, i, &end);
         most = boxes > most ? boxes : most;
     }
-    return most * kBoxBytes + tail_bytes(q);
+    return most * kBoxBytes + tail(q).bytes;
 }
 
 Strided strided(const eg_matrix& m) { return Strided{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
 
-bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t end, unsigned char* ws, int64_t boxes, int* norm_blocks, int* in_blocks) {
+bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t end, unsigned char* ws, int64_t boxes) {
     const int parts = parts_of(q);
+    const Tail z = tail(q);
+    unsigned char* behind = ws + boxes * kBoxBytes;
     a->ws = ws;
-    a->partial = reinterpret_cast<double*>(ws + boxes * kBoxBytes);
-    a->turn = reinterpret_cast<float*>(ws + boxes * kBoxBytes + up(q->P * kOrthoMats * (int64_t)kNormBlocks * 8, 1024));
+    a->partial = reinterpret_cast<double*>(behind + z.partial);
+    a->turn = reinterpret_cast<float*>(behind + z.turn);
+    a->done = reinterpret_cast<int*>(behind + z.done);
     a->P = (int)q->P;
     a->count = (int)(end - first);
-    a->tiles[0] = a->tiles[1] = 0;
+    a->ticket = a->done + a->P * a->count;
     a->momentum = (float)q->momentum;
     a->nesterov = q->nesterov != 0;
-    int64_t at = 0, begin = 0, begin_boxes = 0, tiles[2] = {0, 0};
+    // longest products first: pairs of CTAs take the tiles in turn
+    int64_t order[kOrthoMats];
     for (int64_t i = first; i < end; ++i) {
-        const eg_orthogonal_matrix& s = q->matrices[i];
-        OrthoMat* m = &a->mat[i - first];
-        const Sides z = sides(s);
+        int64_t j = i - first;
+        auto longer = [&](int64_t x, int64_t y) {
+            const Sides s = sides(q, q->matrices[x]), t = sides(q, q->matrices[y]);
+            return s.cb != t.cb ? s.cb > t.cb : s.rb > t.rb;
+        };
+        for (; j > 0 && longer(i, order[j - 1]); --j) order[j] = order[j - 1];
+        order[j] = i;
+    }
+    int64_t at = 0, begin = 0, tiles[2] = {0, 0};
+    a->lag = 0;
+    for (int i = 0; i < a->count; ++i) {
+        const eg_orthogonal_matrix& s = q->matrices[order[i]];
+        OrthoMat* m = &a->mat[i];
+        const Sides z = sides(q, s);
         m->flip = s.rows > s.columns;
         m->m = (int)(m->flip ? s.columns : s.rows);
         m->n = (int)(m->flip ? s.rows : s.columns);
         m->rb = (int)z.rb; m->cb = (int)z.cb;
-        m->first = (int)((i - first) * q->P);
+        m->first = (int)(i * q->P);
         m->scale = (float)s.scale;
         const int64_t plane = z.rb * z.cb, square = z.rb * z.rb;
         m->x_rep = 2 * plane; m->s_rep = 2 * square;
         m->x[0] = at;
         m->x[1] = at + q->P * 2 * plane;
-        m->a = at + q->P * 4 * plane;
-        m->b = m->a + q->P * 2 * square;
+        for (int k = 0; k < 3; ++k) m->s[k] = at + q->P * (4 * plane + 2 * square * (parts == 2 ? k : k & 1));
         at += q->P * z.boxes;
         m->grad = strided(s.grad); m->out = strided(s.out); m->velocity = strided(s.velocity);
         m->velocity_out = s.velocity_out.data ? strided(s.velocity_out) : m->velocity;
@@ -335,24 +393,16 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
         m->tiles[1] = (int)(rt * ((z.cb + wide - 1) / wide));
         tiles[0] += q->P * low;
         tiles[1] += q->P * (int64_t)m->tiles[1];
-        // values one after another are one row
-        const bool flat = (s.grad.row_stride == s.columns || s.rows == 1) &&
-                          (!s.velocity.data || ((s.velocity.row_stride == s.columns || s.rows == 1) && (m->velocity_out.row == s.columns || s.rows == 1)));
-        m->view_rows = flat ? 1 : s.rows;
-        m->view_cols = flat ? s.rows * s.columns : s.columns;
-        m->units = m->view_rows * ((m->view_cols + kNormUnit - 1) / kNormUnit);
-        const int64_t blocks = (m->units + 1) / 2;
-        m->blocks = (int)(blocks < kNormBlocks ? blocks : kNormBlocks);
+        const int64_t items = (plane + 1) / 2;            // two boxes or more each
+        m->items = (int)(items < kMaxItems ? items : kMaxItems);
         m->begin = (int)begin;
-        m->boxes_begin = (int)begin_boxes;
-        begin += q->P * m->blocks;
-        begin_boxes += q->P * plane;
+        begin += q->P * m->items;
+        if (a->lag < m->items) a->lag = m->items;
     }
-    if (tiles[0] > 0x3fffffff || tiles[1] > 0x3fffffff || begin > 0x3fffffff || begin_boxes > 0x3fffffff) return false;
+    if (tiles[0] > 0x3fffffff || tiles[1] > 0x3fffffff || begin > 0x3fffffff) return false;
     a->tiles[0] = (int)tiles[0];
     a->tiles[1] = (int)tiles[1];
-    *norm_blocks = (int)begin;
-    *in_blocks = (int)begin_boxes;
+    a->items = (int)begin;
     EncodeFn fn = encoder();
     if (!fn) return false;
     const cuuint64_t dims[3] = {64, (cuuint64_t)(boxes * kBox), 1}, strides[2] = {128, (cuuint64_t)(boxes * kBoxBytes)};
@@ -361,7 +411,7 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& a, int step, cudaStream_t stream) {
+template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& a, const OrthoPass& pass, cudaStream_t stream) {
     constexpr int smem = OrthoShape<PARTS>::kSmem;
     static bool raised[64] = {false};
     int dev = 0;
@@ -374,38 +424,69 @@ template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& 
     }
     const int pairs = sm_count() / 2, tiles = a.tiles[PASS >= kApply ? 1 : 0];
     if (pairs < 1) return cudaErrorInvalidDevice;
-    return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kGemmThreads), smem, stream, a, step);
+    return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kGemmThreads), smem, stream, a, pass);
 }
 
-template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, int norm_blocks, int in_blocks, cudaStream_t stream) {
+template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, cudaStream_t stream) {
     constexpr int PARTS = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 2;
     a.sx = s.sx;
-    cudaError_t e;
+    a.out = 1.f / s.sx;
+    cudaError_t e = cudaMemsetAsync(a.done, 0, (size_t)(a.P * a.count + 1) * 4, stream);
+    if (e != cudaSuccess) return e;
+    const int most = sm_count() * kInCtas;
     auto given = [&](auto value) {
-        using G = decltype(value);
-        const cudaError_t r = launch_after(k_ortho_norm<G>, dim3(norm_blocks), dim3(kThreads), 0, stream, a);
-        return r != cudaSuccess ? r : launch_after(k_ortho_in<G>, dim3(in_blocks), dim3(kThreads), 0, stream, a);
+        return launch_after(k_ortho_in<decltype(value)>, dim3(2 * a.items < most ? 2 * a.items : most), dim3(kThreads), 0, stream, a);
     };
     e = q->dtype == EG_F32 ? given(0.f) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}) : given(__half{});
-    if (e != cudaSuccess) return e;
-    for (int k = 0; k < q->steps; ++k) {
-        a.a = (float)s.c[k][0];
-        a.gram = s.sa / (s.sx * s.sx);
-        a.ca = (float)(s.c[k][1] * s.sb[k] / s.sa);
-        a.cb = (float)(s.c[k][2] * s.sb[k] / ((double)s.sa * s.sa));
-        a.ci = 1.f / s.sb[k];
-        a.out = 1.f / s.sx;
-        // what only the last launch depends on is the caller's type: the others are shared
-        if ((e = product<float, PARTS, kGram>(a, k, stream)) != cudaSuccess) return e;
-        if (k + 1 < q->steps) {
-            if ((e = product<float, PARTS, kSquare>(a, k, stream)) != cudaSuccess) return e;
-            if ((e = product<float, PARTS, kApply>(a, k, stream)) != cudaSuccess) return e;
-        } else {
-            if ((e = product<float, PARTS, kSquare>(a, k, stream)) != cudaSuccess) return e;
-            if ((e = product<T, PARTS, kLast>(a, k, stream)) != cudaSuccess) return e;
+    int from = 0;
+    for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
+        const double *c0 = s.c[k], sa = s.sa, sb0 = s.sb[k];
+        OrthoPass p{};
+        p.from = from;
+        p.first = k == 0;
+        p.to = 0;
+        p.fd = s.sa / (s.sx * s.sx);
+        // (what only the last launch depends on is the caller's type: the others are shared)
+        e = product<float, PARTS, kGram>(a, p, stream);
+        auto sym = [&](int l, int r, int e0, int e1, int to, double f0, double f1, double fd) {
+            p.l = l; p.r = r; p.e0 = e0; p.e1 = e1; p.to = to;
+            p.f0 = (float)f0; p.f1 = (float)f1; p.fd = (float)fd;
+        };
+        // B0 = b A + c A^2
+        sym(0, 0, 0, 0, 1, c0[1] * sb0 / sa, 0, c0[2] * sb0 / (sa * sa));
+        if (e == cudaSuccess) e = product<float, PARTS, kSym1>(a, p, stream);
+        double outer = c0[0], scale = sb0;
+        p.l = 1;
+        ++k;
+        if constexpr (PARTS == 2) {
+            // (polynomials that make small values smaller: their products of two steps would sink below the boxes' last bit, 2^-39)
+            if (k < q->steps && fabs(c0[0]) >= 1.0 && fabs(s.c[k][0]) >= 1.0) {
+                const double *c1 = s.c[k], sb1 = s.sb[k], sc = s.sc[k - 1];
+                const double bound = fabs(c1[0]) * s.most[k - 1] + fabs(c0[0]) * s.most[k] + s.most[k - 1] * s.most[k], sr = power_below(bound * 1.02);
+                // C = A B0
+                sym(0, 1, 0, 0, 2, 0, 0, sc / (sa * sb0));
+                if (e == cudaSuccess) e = product<float, PARTS, kSym0>(a, p, stream);
+                // A1 = a0^2 A + 2 a0 C + C B0, in A's place
+                sym(2, 1, 0, 2, 0, c0[0] * c0[0], 2 * c0[0] * sa / sc, sa / (sc * sb0));
+                if (e == cudaSuccess) e = product<float, PARTS, kSym2>(a, p, stream);
+                // B1 = b A1 + c A1^2, in C's place
+                sym(0, 0, 0, 0, 2, c1[1] * sb1 / sa, 0, c1[2] * sb1 / (sa * sa));
+                if (e == cudaSuccess) e = product<float, PARTS, kSym1>(a, p, stream);
+                // a1 B0 + a0 B1 + B1 B0, in A1's place
+                sym(2, 1, 1, 2, 0, c1[0] * sr / sb0, c0[0] * sr / sb1, sr / (sb1 * sb0));
+                if (e == cudaSuccess) e = product<float, PARTS, kSym2>(a, p, stream);
+                outer = c0[0] * c1[0];
+                scale = sr;
+                p.l = 0;
+                ++k;
+            }
         }
+        p.f0 = (float)outer;
+        p.fd = (float)(1.0 / scale);
+        if (e != cudaSuccess) break;
+        e = k < q->steps ? product<float, PARTS, kApply>(a, p, stream) : product<T, PARTS, kLast>(a, p, stream);
     }
-    return cudaSuccess;
+    return e;
 }
 
 }  // namespace
@@ -434,11 +515,10 @@ eg_status eg_orthogonalise(const eg_orthogonalise_args* q, void* workspace, int6
         const int64_t boxes = group(q, i, &end);
         OrthoArgs a;
         a.err = err;
-        int norm_blocks = 0, in_blocks = 0;
-        if (!fill(&a, q, i, end, static_cast<unsigned char*>(workspace), boxes, &norm_blocks, &in_blocks)) return EG_ERR_CUDA;
-        const cudaError_t e = q->out_dtype == EG_F32    ? run<float>(a, s, q, norm_blocks, in_blocks, stream)
-                              : q->out_dtype == EG_BF16 ? run<__nv_bfloat16>(a, s, q, norm_blocks, in_blocks, stream)
-                                                        : run<__half>(a, s, q, norm_blocks, in_blocks, stream);
+        if (!fill(&a, q, i, end, static_cast<unsigned char*>(workspace), boxes)) return EG_ERR_CUDA;
+        const cudaError_t e = q->out_dtype == EG_F32    ? run<float>(a, s, q, stream)
+                              : q->out_dtype == EG_BF16 ? run<__nv_bfloat16>(a, s, q, stream)
+                                                        : run<__half>(a, s, q, stream);
         if (e != cudaSuccess) return EG_ERR_CUDA;
     }
     return EG_OK;
