@@ -53,7 +53,7 @@ struct OrthoMat {
     long long x[2], s[3];                         // first boxes of replica 0: X before and after a step, symmetric matrices
     long long x_rep, s_rep;                       // boxes from one replica to the next; lo parts lie half as far
     Strided grad, out, velocity, velocity_out;
-    int items, begin;                             // of k_ortho_in: items of an instance, the first one of replica 0
+    int items, begin;                             // of k_ortho_norm and k_ortho_in: items of an instance, the first one of replica 0
 };
 
 // One launch.
@@ -68,9 +68,7 @@ struct OrthoArgs {
     CUtensorMap map;                              // the workspace as rows of 128 bytes
     unsigned char* ws;
     double* partial;                              // [instances][kMaxItems] sums of squares
-    int* done;                                    // [instances] items whose sum of squares is there
-    int* ticket;                                  // of k_ortho_in
-    int items, lag;
+    int items;
     float* turn;                                  // [instances] what is left of 1 / |u| after a power of two
     unsigned int* err;
     int P, count;

@@ -5,7 +5,7 @@
 //   steps times   X <- a X + (b A + c A^2) X,   A = X X^T       (an odd polynomial of X's singular values, which pulls them to 1)
 //   out = scale * X
 //
-// Launches: k_ortho_in (velocity, norms, X in the workspace's boxes), then the products (eg_orthogonal_gemm.cuh), each over all
+// Launches: k_ortho_norm (velocity, sums of squares), k_ortho_in (X in the workspace's boxes), then the products (eg_orthogonal_gemm.cuh), each over all
 // matrices of all replicas: a network's small matrices fill the machine together.
 //
 // Only a power of two of 1 / |u| goes into X at first, so that gradients of 16 bits enter the products without a rounding; the rest,
@@ -18,191 +18,229 @@
 namespace eg {
 namespace {
 
-constexpr int kThreads = 256, kInCtas = 5;        // k_ortho_in: CTAs of a multiprocessor
-constexpr int kMaxItems = 512;                    // of an instance
+constexpr int kThreads = 256;
+constexpr int kMaxItems = 128;                    // of an instance
 constexpr long long kGroupBytes = 1ll << 30;      // workspace of one group of matrices that share their launches (one matrix may need more)
 
-// u of four neighbouring values, and v' where it is formed.
-template <typename T, bool FORM> __device__ __forceinline__ void update4(const OrthoArgs& a, const OrthoMat& m, int p, long long row, long long col,
-                                                                       int n, bool vec, float (&u)[4]) {
-    const T* g = static_cast<const T*>(m.grad.p) + p * m.grad.rep + row * m.grad.row + col;
-    const float* v = m.velocity.p ? static_cast<const float*>(FORM ? m.velocity.p : m.velocity_out.p) +
-                                        p * (FORM ? m.velocity.rep : m.velocity_out.rep) + row * (FORM ? m.velocity.row : m.velocity_out.row) + col
-                                  : nullptr;
-    float* to = FORM && v ? static_cast<float*>(m.velocity_out.p) + p * m.velocity_out.rep + row * m.velocity_out.row + col : nullptr;
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool need_g = FORM || !v || a.nesterov;
-    const bool whole = vec && n >= 4;
-    if (whole) {
-        if (need_g) {
+// Four neighbouring values of a row, as they lie in memory.
+template <typename T> struct Quad {
+    static constexpr int kWords = sizeof(T) == 4 ? 4 : 2;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) w[q] = 0;
+    }
+    // n of them are there; vec: on a boundary of four
+    __device__ __forceinline__ void load(const T* p, int n, bool vec) {
+        if (vec && n >= 4) {
             if constexpr (sizeof(T) == 4) {
-                load_vec<T, 4>(g, u);
+                const uint4 v = *reinterpret_cast<const uint4*>(p);
+                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
             } else {
-                const uint2 x = *reinterpret_cast<const uint2*>(g);
-                const float2 f0 = unpack2<T>(x.x), f1 = unpack2<T>(x.y);
-                u[0] = f0.x; u[1] = f0.y; u[2] = f1.x; u[3] = f1.y;
+                const uint2 v = *reinterpret_cast<const uint2*>(p);
+                w[0] = v.x; w[1] = v.y;
             }
+            return;
         }
-        if (v) {                                              // (v' comes from other multiprocessors' hands)
-            const float4 x = FORM ? *reinterpret_cast<const float4*>(v) : __ldcg(reinterpret_cast<const float4*>(v));
-            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-        }
-    } else {
+        clear();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            u[e] = e < n && need_g ? to_f32(g[e]) : 0.f;
-            if (v) w[e] = e < n ? (FORM ? v[e] : __ldcg(v + e)) : 0.f;
+            if (e >= n) continue;
+            if constexpr (sizeof(T) == 4) w[e] = *reinterpret_cast<const uint32_t*>(p + e);
+            else w[e / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + e) << (16 * (e & 1));
         }
     }
-    if (!v) return;
-    if (FORM) {
+    __device__ __forceinline__ void values(float (&v)[4]) const {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = fmaf(a.momentum, w[e], u[e]);
-        if (whole) {
-            store_vec<float, 4>(to, w);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) to[e] = w[e];
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) {
+                v[e] = __uint_as_float(w[e]);
+            } else {
+                const float2 f = unpack2<T>(w[e / 2]);
+                v[e] = e & 1 ? f.y : f.x;
+            }
         }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = a.nesterov ? fmaf(a.momentum, w[e], u[e]) : w[e];
-}
+};
 
+// Whether the rows of the gradient and the velocities begin on boundaries of four values.
 __device__ __forceinline__ bool quads(const OrthoMat& m, size_t size) {
-    auto fits = [](const Strided& s, size_t bytes) { return !s.p || (((uintptr_t)s.p | (uintptr_t)(s.rep * (long long)bytes) | (uintptr_t)(s.row * (long long)bytes)) & (4 * bytes - 1)) == 0; };
+    auto fits = [](const Strided& s, size_t bytes) {
+        return !s.p || (((uintptr_t)s.p | (uintptr_t)(s.rep * (long long)bytes) | (uintptr_t)(s.row * (long long)bytes)) & (4 * bytes - 1)) == 0;
+    };
     return fits(m.grad, size) && fits(m.velocity, 4) && fits(m.velocity_out, 4);
 }
 
-// Two phases over the boxes of all instances, in one launch.  Phase 1 updates the velocity and adds up squares; phase 2 reads the same
-// values again, `lag` items later, while they are still in the L2, and writes X.  Items are handed out in order by a counter, so
-// that an item of phase 2 waits for items only that running CTAs hold.
-//   positions 0 .. lag - 1: phase 1 of items 0 .. lag - 1;  then in turn phase 1 of the next item and phase 2 of the next one;  then the
-//   last items of phase 2
-template <typename T> __global__ void __launch_bounds__(kThreads, kInCtas) k_ortho_in(const __grid_constant__ OrthoArgs a) {
+// Walks over the boxes of an item, those of the gradient's rows of boxes one after another; a thread holds four quads of a box: rows
+// 16 z + first, columns 4 * quad.  FORM: with the velocity before, otherwise with the one after the update.
+template <typename T, bool FORM> struct Boxes {
+    const OrthoArgs& a;
+    const OrthoMat& m;
+    int p, b, quad, first, rows, cols, wide, box0, box1;
+    bool vec, need_g;
+    Strided v;
+    Quad<T> g[2][4];
+    Quad<float> w[2][4];
+
+    __device__ __forceinline__ Boxes(const OrthoArgs& args, int k, int item)
+        : a(args), m(args.mat[k]), p((item - m.begin) / m.items), b(item - m.begin - p * m.items), quad(threadIdx.x & 15), first(threadIdx.x >> 4) {
+        rows = m.flip ? m.n : m.m;
+        cols = m.flip ? m.m : m.n;
+        wide = m.flip ? m.rb : m.cb;
+        const long long boxes = (long long)m.rb * m.cb;
+        box0 = (int)(boxes * b / m.items);
+        box1 = (int)(boxes * (b + 1) / m.items);
+        vec = quads(m, sizeof(T));
+        v = FORM ? m.velocity : m.velocity_out;
+        need_g = FORM || !v.p || a.nesterov;
+    }
+    __device__ __forceinline__ void fetch(int box, int slot) {
+        const int grow = box / wide, c = (box - grow * wide) * kBox + quad * 4, n = cols - c;
+        const long long r = grow * kBox + first;
+        const T* from = static_cast<const T*>(m.grad.p) + p * m.grad.rep + r * m.grad.row + c;
+        const float* speed = static_cast<const float*>(v.p) + p * v.rep + r * v.row + c;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const int have = r + z * 16 < rows ? n : 0;
+            if (need_g) g[slot][z].load(from + z * 16 * m.grad.row, have, vec);
+            if (v.p) w[slot][z].load(speed + z * 16 * v.row, have, vec);
+        }
+    }
+    // u, four quads of it; FORM: stores the velocity.
+    __device__ __forceinline__ void update(int box, int slot, float (&u)[4][4]) {
+        const int grow = box / wide, c = (box - grow * wide) * kBox + quad * 4, n = cols - c;
+        const long long r = grow * kBox + first;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            if (need_g) g[slot][z].values(u[z]);
+            if (!v.p) continue;
+            float s[4];
+            w[slot][z].values(s);
+            if (FORM) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = fmaf(a.momentum, s[e], u[z][e]);
+                if (r + z * 16 < rows) {
+                    float* to = static_cast<float*>(m.velocity_out.p) + p * m.velocity_out.rep + (r + z * 16) * m.velocity_out.row + c;
+                    if (vec && n >= 4) {
+                        store_vec<float, 4>(to, s);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < n) to[e] = s[e];
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[z][e] = a.nesterov ? fmaf(a.momentum, s[e], u[z][e]) : s[e];
+        }
+    }
+};
+
+__device__ __forceinline__ int matrix_of(const OrthoArgs& a, int item) {
+    int k = 0;
+    while (k + 1 < a.count && item >= a.mat[k + 1].begin) ++k;
+    return k;
+}
+
+// The two kernels before the products read the same values; both are bound by memory, the next box on its way while one is worked on.
+// Tried: both phases in one launch, the second a few hundred items behind the first so that it reads from the L2: 549 us against 502 for 8 x
+// 2048 x 5504 with a velocity (an instance's 68 MB and what passes by do not stay there).
+template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_norm(const __grid_constant__ OrthoArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ double s_sum[kThreads / 32];
+    Boxes<T, true> x(a, matrix_of(a, blockIdx.x), blockIdx.x);
+    double sum = 0.0;
+    x.fetch(x.box0, 0);
+    auto work = [&](int box, int slot) {
+        if (box + 1 < x.box1) x.fetch(box + 1, slot ^ 1);
+        float u[4][4];
+        x.update(box, slot, u);
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fma((double)u[z][e], (double)u[z][e], sum);
+    };
+    for (int box = x.box0; box < x.box1; box += 2) {
+        work(box, 0);
+        if (box + 1 < x.box1) work(box + 1, 1);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / 32; ++w) sum += s_sum[w];
+        a.partial[(long long)(x.m.first + x.p) * kMaxItems + x.b] = sum;
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(const __grid_constant__ OrthoArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ double s_sum[kThreads / 32];
     __shared__ float s_box[kBox][kBox + 1];
-    __shared__ int s_next;
-    const int quad = threadIdx.x & 15, first = threadIdx.x >> 4;
-    for (;;) {
-        __syncthreads();
-        if (threadIdx.x == 0) s_next = atomicAdd(a.ticket, 1);
-        __syncthreads();
-        const int pos = s_next, N = a.items, lag = a.lag;
-        if (pos >= 2 * N) return;
-        const bool form = pos < lag || (pos < 2 * N - lag && ((pos - lag) & 1) == 0);
-        const int item = pos < lag ? pos : pos >= 2 * N - lag ? pos - N : form ? lag + (pos - lag) / 2 : (pos - lag) / 2;
-        int k = 0;
-        while (k + 1 < a.count && item >= a.mat[k + 1].begin) ++k;
-        const OrthoMat& m = a.mat[k];
-        const int p = (item - m.begin) / m.items, b = item - m.begin - p * m.items, instance = m.first + p;
-        const bool vec = quads(m, sizeof(T));
-        const int rows = m.flip ? m.n : m.m, cols = m.flip ? m.m : m.n;         // of the gradient
-        const int wide = m.flip ? m.rb : m.cb, boxes = m.rb * m.cb;
-        const int box0 = (int)((long long)boxes * b / m.items), box1 = (int)((long long)boxes * (b + 1) / m.items);
-        // quad z of a thread: row z * 16 + first of the gradient's box, columns 4 * quad
-        auto load = [&](int box, auto forming, float (&u)[4][4]) {
-            const int grow = box / wide, r0 = grow * kBox + first, c = (box - grow * wide) * kBox + quad * 4;
+    Boxes<T, false> x(a, matrix_of(a, blockIdx.x), blockIdx.x);
+    const OrthoMat& m = x.m;
+    const int instance = m.first + x.p;
+    x.fetch(x.box0, 0);
+    static_assert(kMaxItems <= kThreads, "one partial sum a thread");
+    double s = (int)threadIdx.x < m.items ? a.partial[(long long)instance * kMaxItems + threadIdx.x] : 0.0;
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = s;
+    __syncthreads();
+    double total = 0.0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) u[z][e] = 0.f;
-                if (r0 + z * 16 < rows && c < cols)
-                    update4<T, decltype(forming)::value>(a, m, p, r0 + z * 16, c, cols - c < 4 ? cols - c : 4, vec, u[z]);
-            }
-        };
-        if (form) {
-            double sum = 0.0;
-            for (int box = box0; box < box1; ++box) {
-                float u[4][4];
-                load(box, std::true_type{}, u);
+    for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
+    const double norm = sqrt(total);
+    int ex = 0;
+    double fraction = 0.0;
+    const bool finite = norm <= 1.7e308;                  // (false for NaN too)
+    if (finite) fraction = frexp(norm, &ex);              // norm = fraction * 2^ex, 1/2 <= fraction < 1
+    // sx / 2^ex as two factors, since it may pass the range of 32 bits
+    const float by0 = (float)ldexp(1.0, -ex / 2), by1 = (float)ldexp((double)a.sx, -ex + ex / 2);
+    if (x.b == 0 && threadIdx.x == 0)
+        a.turn[instance] = !finite ? __int_as_float(0x7fffffff) : fraction > 0.0 ? (float)(1.0 / fraction) : 0.f;
+    auto work = [&](int box, int slot) {
+        if (box + 1 < x.box1) x.fetch(box + 1, slot ^ 1);
+        float u[4][4];
+        x.update(box, slot, u);
 #pragma unroll
-                for (int z = 0; z < 4; ++z)
+        for (int z = 0; z < 4; ++z)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum = fma((double)u[z][e], (double)u[z][e], sum);
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
-            __syncthreads();                                  // also: all of the velocity's stores are issued
-            if (threadIdx.x == 0) {
-                for (int w = 1; w < kThreads / 32; ++w) sum += s_sum[w];
-                a.partial[(long long)instance * kMaxItems + b] = sum;
-                __threadfence();
-                atomicAdd(a.done + instance, 1);
-            }
-            continue;
-        }
-        if (threadIdx.x == 0) {
-            const long long t0 = clock64();
-            for (unsigned spins = 1;; ++spins) {
-                int there;
-                asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(there) : "l"(a.done + instance) : "memory");
-                if (there >= m.items) break;
-                if ((spins & 63u) == 0 && clock64() - t0 > kOpWaitCycles) {
-                    atomicOr(a.err, kOpErrWaitTimeout);
-                    break;
-                }
-            }
-        }
-        __syncthreads();
-        {
-            double s = 0.0;
-            for (int q = threadIdx.x; q < m.items; q += kThreads) s += __ldcg(a.partial + (long long)instance * kMaxItems + q);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = s;
-        }
-        __syncthreads();
-        double total = 0.0;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
-        const double norm = sqrt(total);
-        int ex = 0;
-        double fraction = 0.0;
-        const bool finite = norm <= 1.7e308;                  // (false for NaN too)
-        if (finite) fraction = frexp(norm, &ex);              // norm = fraction * 2^ex, 1/2 <= fraction < 1
-        const double by = ldexp((double)a.sx, -ex);
-        if (b == 0 && threadIdx.x == 0)
-            a.turn[instance] = !finite ? __int_as_float(0x7fffffff) : fraction > 0.0 ? (float)(1.0 / fraction) : 0.f;
-        for (int box = box0; box < box1; ++box) {
-            float u[4][4];
-            load(box, std::false_type{}, u);
+            for (int e = 0; e < 4; ++e) u[z][e] = u[z][e] * by0 * by1;
+        int rbox = box / x.wide, cbox = box - rbox * x.wide;
+        if (m.flip) {
+            const int r = rbox;
+            rbox = cbox;
+            cbox = r;
+            __syncthreads();
 #pragma unroll
             for (int z = 0; z < 4; ++z)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) u[z][e] = (float)((double)u[z][e] * by);
-            int rbox = box / wide, cbox = box - rbox * wide;
-            if (m.flip) {
-                const int x = rbox;
-                rbox = cbox;
-                cbox = x;
-                __syncthreads();
+                for (int e = 0; e < 4; ++e) s_box[x.quad * 4 + e][z * 16 + x.first] = u[z][e];
+            __syncthreads();
 #pragma unroll
-                for (int z = 0; z < 4; ++z)
+            for (int z = 0; z < 4; ++z)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s_box[quad * 4 + e][z * 16 + first] = u[z][e];
-                __syncthreads();
-#pragma unroll
-                for (int z = 0; z < 4; ++z)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[z][e] = s_box[z * 16 + first][quad * 4 + e];
-            }
-            unsigned char* hi = a.ws + (m.x[0] + p * m.x_rep + (long long)cbox * m.rb + rbox) * kBoxBytes;
-            unsigned char* lo = hi + m.x_rep / 2 * kBoxBytes;
-#pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                uint32_t h0, h1, l0, l1;
-                split_half2(u[z][0], u[z][1], h0, l0);
-                split_half2(u[z][2], u[z][3], h1, l1);
-                const uint32_t off = swz128((z * 16 + first) * 128 + quad * 8);
-                *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
-                *reinterpret_cast<uint2*>(lo + off) = make_uint2(l0, l1);
-            }
+                for (int e = 0; e < 4; ++e) u[z][e] = s_box[z * 16 + x.first][x.quad * 4 + e];
         }
+        unsigned char* hi = a.ws + (m.x[0] + x.p * m.x_rep + (long long)cbox * m.rb + rbox) * kBoxBytes;
+        unsigned char* lo = hi + m.x_rep / 2 * kBoxBytes;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            uint32_t h0, h1, l0, l1;
+            split_half2(u[z][0], u[z][1], h0, l0);
+            split_half2(u[z][2], u[z][3], h1, l1);
+            const uint32_t off = swz128((z * 16 + x.first) * 128 + x.quad * 8);
+            *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
+            *reinterpret_cast<uint2*>(lo + off) = make_uint2(l0, l1);
+        }
+    };
+    for (int box = x.box0; box < x.box1; box += 2) {
+        work(box, 0);
+        if (box + 1 < x.box1) work(box + 1, 1);
     }
 }
 
@@ -317,17 +355,16 @@ int64_t group(const eg_orthogonalise_args* q, int64_t first, int64_t* end) {
     *end = i;
     return boxes;
 }
-// Behind a group's boxes: partial sums, what is left of 1 / |u|, counters.
+// Behind a group's boxes: partial sums, what is left of 1 / |u|.
 struct Tail {
-    int64_t partial, turn, done, bytes;
+    int64_t partial, turn, bytes;
 };
 Tail tail(const eg_orthogonalise_args* q) {
     const int64_t instances = q->P * (q->count < kOrthoMats ? q->count : kOrthoMats);
     Tail t;
     t.partial = 0;
     t.turn = up(instances * kMaxItems * 8, 256);
-    t.done = t.turn + up(instances * 4, 256);
-    t.bytes = t.done + up((instances + 1) * 4, 256);
+    t.bytes = t.turn + up(instances * 4, 256);
     return t;
 }
 int64_t workspace_of(const eg_orthogonalise_args* q) {
@@ -348,10 +385,8 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
     a->ws = ws;
     a->partial = reinterpret_cast<double*>(behind + z.partial);
     a->turn = reinterpret_cast<float*>(behind + z.turn);
-    a->done = reinterpret_cast<int*>(behind + z.done);
     a->P = (int)q->P;
     a->count = (int)(end - first);
-    a->ticket = a->done + a->P * a->count;
     a->momentum = (float)q->momentum;
     a->nesterov = q->nesterov != 0;
     // longest products first: pairs of CTAs take the tiles in turn
@@ -366,7 +401,6 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
         order[j] = i;
     }
     int64_t at = 0, begin = 0, tiles[2] = {0, 0};
-    a->lag = 0;
     for (int i = 0; i < a->count; ++i) {
         const eg_orthogonal_matrix& s = q->matrices[order[i]];
         OrthoMat* m = &a->mat[i];
@@ -393,11 +427,10 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
         m->tiles[1] = (int)(rt * ((z.cb + wide - 1) / wide));
         tiles[0] += q->P * low;
         tiles[1] += q->P * (int64_t)m->tiles[1];
-        const int64_t items = (plane + 1) / 2;            // two boxes or more each
+        const int64_t items = (plane + 3) / 4;            // four boxes or more each
         m->items = (int)(items < kMaxItems ? items : kMaxItems);
         m->begin = (int)begin;
         begin += q->P * m->items;
-        if (a->lag < m->items) a->lag = m->items;
     }
     if (tiles[0] > 0x3fffffff || tiles[1] > 0x3fffffff || begin > 0x3fffffff) return false;
     a->tiles[0] = (int)tiles[0];
@@ -431,13 +464,11 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
     constexpr int PARTS = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 2;
     a.sx = s.sx;
     a.out = 1.f / s.sx;
-    cudaError_t e = cudaMemsetAsync(a.done, 0, (size_t)(a.P * a.count + 1) * 4, stream);
-    if (e != cudaSuccess) return e;
-    const int most = sm_count() * kInCtas;
     auto given = [&](auto value) {
-        return launch_after(k_ortho_in<decltype(value)>, dim3(2 * a.items < most ? 2 * a.items : most), dim3(kThreads), 0, stream, a);
+        const cudaError_t e = launch_after(k_ortho_norm<decltype(value)>, dim3(a.items), dim3(kThreads), 0, stream, a);
+        return e != cudaSuccess ? e : launch_after(k_ortho_in<decltype(value)>, dim3(a.items), dim3(kThreads), 0, stream, a);
     };
-    e = q->dtype == EG_F32 ? given(0.f) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}) : given(__half{});
+    cudaError_t e = q->dtype == EG_F32 ? given(0.f) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}) : given(__half{});
     int from = 0;
     for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
         const double *c0 = s.c[k], sa = s.sa, sb0 = s.sb[k];
