@@ -20,6 +20,7 @@
 //   PARTS == 1 (results of 8 bits): the products take hi alone, which costs 2^-12 of a value each, about what the result's own
 //     rounding does.  X is nevertheless carried on in both parts: the term a X, which alone carries small singular values
 //     (485 times over in five steps), sees no rounding to 11 bits.  (One part throughout: error 15 % for a matrix of rank 1.)
+//     No product reads these lo parts: they lie as the epilogue's threads want them (see lane_place), once, and are updated in place.
 //   PARTS == 2 (results of 11 and 24 bits): hi hi + hi lo + lo hi.  lo lo, 2^-22 of a product, is left out.
 //
 // A and B are symmetric: only tiles of 256 x 256 on and below the diagonal are formed and stored.  An operand above it is read
@@ -50,8 +51,8 @@ struct OrthoMat {
     int tiles[2];                                 // of one replica: of the symmetric products, of X
     int first;                                    // instance of replica 0
     float scale;
-    long long x[2], s[3];                         // first boxes of replica 0: X before and after a step, symmetric matrices
-    long long x_rep, s_rep;                       // boxes from one replica to the next; lo parts lie half as far
+    long long x[2], lo[2], s[3];                  // first boxes of replica 0: X before and after a step, its lo parts, symmetric matrices
+    long long x_rep, s_rep;                       // boxes from one replica to the next; lo parts of symmetric matrices lie half as far
     Strided grad, out, velocity, velocity_out;
     int items, begin;                             // of k_ortho_norm and k_ortho_in: items of an instance, the first one of replica 0
 };
@@ -71,7 +72,7 @@ struct OrthoArgs {
     int items;
     float* turn;                                  // [instances] what is left of 1 / |u| after a power of two
     unsigned int* err;
-    int P, count;
+    int P, count, parts;
     int tiles[2];
     float momentum;
     int nesterov;
@@ -83,7 +84,7 @@ template <int PARTS> struct OrthoShape {
     static constexpr int kBN = PARTS == 2 ? 128 : 256;
     static constexpr int kA = 2 * kBoxBytes * PARTS, kB = kBN / 128 * kBoxBytes * PARTS;     // of a stage and CTA
     static constexpr int kStages = PARTS == 2 ? 3 : 5;
-    static constexpr int kEpi = kGemmEpiWarps * kBoxBytes;                                  // hi and lo of 32 rows x 64 columns
+    static constexpr int kEpi = kGemmEpiWarps * kBoxBytes;      // a warp's 32 rows x 64 columns: hi and lo, or (PARTS == 1) two of hi
     static constexpr int kBars = kStages * (kA + kB) + kEpi;
     static constexpr int kSmem = 1024 + kBars + 1024;
     static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -135,6 +136,9 @@ __device__ __forceinline__ void split_half2(float x, float y, uint32_t& hi, uint
     lo = pack2<__half>(x - f.x, y - f.y);
 }
 
+// Byte of a lo part that no product reads: 8 columns of a row are a thread's 16 bytes, next to those of the rows above and below.
+__device__ __forceinline__ int lane_place(int row, int col) { return (row >> 5) * 4096 + (col >> 3) * 512 + (row & 31) * 16 + (col & 7) * 2; }
+
 // T: type of the caller's matrices (kLast).
 template <typename T, int PARTS, int PASS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_ortho(const __grid_constant__ OrthoArgs a, const OrthoPass pass) {
@@ -152,8 +156,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
     uint64_t* acc_empty = acc_full + 2;                                  // [2] (even CTA's are used)
     uint64_t* small_full = acc_empty + 2;                                // [2]: accumulators of the smaller products
     uint64_t* small_empty = small_full + 2;                              // [2] (even CTA's are used)
-    uint64_t* epi_full = small_empty + 2;                                // [kGemmEpiWarps]
-    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + kGemmEpiWarps);
+    uint64_t* epi_full = small_empty + 2;                                // [kGemmEpiWarps][2]
+    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + 2 * kGemmEpiWarps);
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(const_cast<int*>(s_abort) + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -165,7 +169,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
             op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps);
             op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kGemmEpiWarps);
         }
-        for (int q = 0; q < kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
+        for (int q = 0; q < 2 * kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 3 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&a.map) : "memory");
@@ -216,7 +220,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                         const bool by_column = !SYMMETRIC;
                         box = x + (by_column ? (long long)box0 * g.rb + k : (long long)k * g.rb + box0);
                         next = by_column ? g.rb : 1;
-                        lo = g.x_rep / 2;
+                        lo = g.lo[from] - g.x[from];
                     } else {
                         const bool mirror = k / 4 > box0 / 4;
                         box = sym + (mirror ? (long long)box0 * g.rb + k : (long long)k * g.rb + box0);
@@ -290,42 +294,173 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
         const int w = warp - 4, half = w >> 2, quad = w & 3;
         unsigned char* buf = epi + w * kBoxBytes;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        int count = 0, turn = 0, uses = 0;
+        int count = 0, turn = 0, uses[2] = {0, 0};
         for (int t = pair; t < tiles; t += pairs, ++turn) {
             const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
             const OrthoMat& g = a.mat[q.k];
             const int ksteps = PASS == kGram ? g.cb : g.rb;
             const int rbox = q.i * 4 + (int)rank * 2 + (quad >> 1), cols = SYMMETRIC ? g.rb : g.cb;
-            const long long x = g.x[from] + q.p * g.x_rep, lo = (SYMMETRIC ? g.s_rep : g.x_rep) / 2;
-            const long long to = SYMMETRIC ? g.s[pass.to] + q.p * g.s_rep : g.x[from ^ 1] + q.p * g.x_rep;
+            const long long x = g.x[from] + q.p * g.x_rep, to = SYMMETRIC ? g.s[pass.to] + q.p * g.s_rep : g.x[from ^ 1] + q.p * g.x_rep;
             const float left_of = pass.first && (PASS == kGram || PASS >= kApply) ? a.turn[g.first + q.p] : 1.f;
             auto cbox = [&](int c) { return q.j * (BN / kBox) + half * Shape::kChunks + c; };
             auto inside = [&](int c) { return rbox < g.rb && cbox(c) < cols; };
             auto place = [&](long long matrix, int c) { return a.ws + (matrix + (long long)cbox(c) * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096; };
-            // what the result is added to
-            auto fetch = [&](int c, int term) {
-                if (TERMS == 0 || !inside(c)) return;
-                store_wait_read<0>();
-                __syncwarp();
-                if (elect_one()) {
-                    constexpr bool BOTH = PARTS == 2 || !SYMMETRIC;
-                    const long long matrix = SYMMETRIC ? g.s[term ? pass.e1 : pass.e0] + q.p * g.s_rep : x;
-                    op_mbar_expect(&epi_full[w], BOTH ? 8192 : 4096);
-                    op_bulk_load(buf, place(matrix, c), 4096, &epi_full[w]);
-                    if (BOTH) op_bulk_load(buf + 4096, place(matrix + lo, c), 4096, &epi_full[w]);
+            if constexpr (PARTS == 1) {
+                // Two chunks of 64 columns, each with its own half of the staging memory; what they are added to is on its way while the
+                // products run.
+                uint4 low[PASS >= kApply ? 2 : 1][PASS >= kApply ? 8 : 1];
+                auto low_at = [&](int c) {
+                    return a.ws + (g.lo[0] + q.p * g.x_rep + (long long)cbox(c) * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096 + lane * 16;
+                };
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (TERMS == 0 || !inside(c)) continue;
+                    if (c == 0) store_wait_read<1>();             // (the last tile's second chunk may still be on its way out)
+                    else store_wait_read<0>();
+                    __syncwarp();
+                    if (elect_one()) {
+                        op_mbar_expect(&epi_full[2 * w + c], 4096);
+                        op_bulk_load(buf + c * 4096, place(SYMMETRIC ? g.s[pass.e0] + q.p * g.s_rep : x, c), 4096, &epi_full[2 * w + c]);
+                    }
+                    if constexpr (PASS >= kApply) {
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) low[c][z] = *reinterpret_cast<const uint4*>(low_at(c) + z * 512);
+                    }
                 }
-            };
-            fetch(0, 0);
-            float sum[PARTS == 2 ? 64 : 1];                       // this row's 64 columns: the terms, then the products' chunks
-            if constexpr (PARTS == 2) {
+                mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
+                tc_fence_after();
+                const uint32_t acc = tmem + (count & 1) * BN + lanes + half * (BN / 2);
+                const float by = PASS == kGram ? left_of * left_of : left_of;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    unsigned char* box = buf + c * 4096;
+                    if (inside(c)) {
+                        if (TERMS == 0) {
+                            store_wait_read<1>();
+                            __syncwarp();
+                        } else {
+                            mbar_wait(&epi_full[2 * w + c], uses[c] & 1, s_abort, a.err);
+                            ++uses[c];
+                        }
+                        unsigned char* low_to = PASS == kApply ? low_at(c) : nullptr;
+#pragma unroll
+                        for (int x0 = 0; x0 < 64; x0 += 32) {
+                            uint32_t d[32];
+                            tc_load(d, acc + c * 64 + x0);
+                            float r[32];
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) r[e] = pass.fd * __uint_as_float(d[e]);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) {
+                                const int piece = (x0 + e) >> 3;
+                                unsigned char* at = box + lane * 128 + ((piece ^ (lane & 7)) << 4);
+                                if constexpr (TERMS > 0) {
+                                    const uint4 h4 = *reinterpret_cast<const uint4*>(at);
+                                    const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w};
+#pragma unroll
+                                    for (int z = 0; z < 4; ++z) {
+                                        const float2 hf = unpack2<__half>(hw[z]);
+                                        r[e + 2 * z] = fmaf(pass.f0, hf.x, r[e + 2 * z]);
+                                        r[e + 2 * z + 1] = fmaf(pass.f0, hf.y, r[e + 2 * z + 1]);
+                                    }
+                                }
+                                if constexpr (PASS >= kApply) {
+                                    const uint4 l4 = low[c][piece];
+                                    const uint32_t lw[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                                    for (int z = 0; z < 4; ++z) {
+                                        const float2 lf = unpack2<__half>(lw[z]);
+                                        r[e + 2 * z] = fmaf(pass.f0, lf.x, r[e + 2 * z]);
+                                        r[e + 2 * z + 1] = fmaf(pass.f0, lf.y, r[e + 2 * z + 1]);
+                                    }
+                                }
+                                if constexpr (PASS == kGram || PASS >= kApply) {
+#pragma unroll
+                                    for (int z = 0; z < 8; ++z) r[e + z] *= by;
+                                }
+                                uint32_t hw[4], lw[4];
+                                if constexpr (PASS == kLast) {
+                                    const float scale = a.out * g.scale;
+#pragma unroll
+                                    for (int z = 0; z < 4; ++z) {
+                                        if constexpr (sizeof(T) == 2) hw[z] = pack2<T>(r[e + 2 * z] * scale, r[e + 2 * z + 1] * scale);
+                                    }
+                                } else {
+#pragma unroll
+                                    for (int z = 0; z < 4; ++z) split_half2(r[e + 2 * z], r[e + 2 * z + 1], hw[z], lw[z]);
+                                }
+                                *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                                if constexpr (PASS == kApply) *reinterpret_cast<uint4*>(low_to + piece * 512) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                            }
+                        }
+                    }
+                    if constexpr (PASS != kLast) {
+                        fence_async_shared();
+                        __syncwarp();
+                        if (elect_one()) {
+                            if (inside(c)) bulk_store(place(to, c), box, 4096);
+                            store_commit();                       // (one group a chunk, empty or not)
+                        }
+                    } else if (inside(c)) {
+                        const int row0 = rbox * kBox + (quad & 1) * 32, col0 = cbox(c) * kBox;
+                        const int rows = min(32, g.m - row0), n = min(64, g.n - col0);
+                        T* out = static_cast<T*>(g.out.p) + q.p * g.out.rep;
+                        if (g.flip) {                             // a row of X is a column of the result
+                            if (lane < rows) {
+                                T* line = out + (long long)col0 * g.out.row + row0 + lane;
+#pragma unroll 8
+                                for (int e = 0; e < n; ++e)
+                                    line[e * g.out.row] = *reinterpret_cast<const T*>(box + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4) + (e & 7) * 2);
+                            }
+                        } else {                                  // runs along the rows
+                            __syncwarp();
+                            T* line = out + (long long)row0 * g.out.row + col0;
+                            const bool words = ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
+#pragma unroll 4
+                            for (int r = 0; r < rows; ++r, line += g.out.row) {
+                                const uint32_t v = *reinterpret_cast<const uint32_t*>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+                                if (words && 2 * lane + 1 < n) {
+                                    *reinterpret_cast<uint32_t*>(line + 2 * lane) = v;
+                                } else {
+                                    uint16_t* o = reinterpret_cast<uint16_t*>(line + 2 * lane);
+                                    if (2 * lane < n) o[0] = (uint16_t)v;
+                                    if (2 * lane + 1 < n) o[1] = (uint16_t)(v >> 16);
+                                }
+                            }
+                        }
+                        // the next box's copy comes by another way than these reads
+                        fence_async_shared();
+                        __syncwarp();
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
+                ++count;
+            } else {
+                const long long lo = SYMMETRIC ? g.s_rep / 2 : g.lo[from] - g.x[from], lo_to = SYMMETRIC ? g.s_rep / 2 : g.lo[from ^ 1] - g.x[from ^ 1];
+                // what the result is added to
+                auto fetch = [&](int term) {
+                    if (TERMS == 0 || !inside(0)) return;
+                    store_wait_read<0>();
+                    __syncwarp();
+                    if (elect_one()) {
+                        const long long matrix = SYMMETRIC ? g.s[term ? pass.e1 : pass.e0] + q.p * g.s_rep : x;
+                        op_mbar_expect(&epi_full[w], 8192);
+                        op_bulk_load(buf, place(matrix, 0), 4096, &epi_full[w]);
+                        op_bulk_load(buf + 4096, place(matrix + lo, 0), 4096, &epi_full[w]);
+                    }
+                };
+                fetch(0);
+                float sum[64];                                    // this row's 64 columns: the terms, then the products' chunks
 #pragma unroll
                 for (int e = 0; e < 64; ++e) sum[e] = 0.f;
                 if (inside(0)) {
 #pragma unroll 1
                     for (int term = 0; term < TERMS; ++term) {
-                        if (term > 0) fetch(0, term);
-                        mbar_wait(&epi_full[w], uses & 1, s_abort, a.err);
-                        ++uses;
+                        if (term > 0) fetch(term);
+                        mbar_wait(&epi_full[w], uses[0] & 1, s_abort, a.err);
+                        ++uses[0];
                         const float f = term ? pass.f1 : pass.f0;
 #pragma unroll
                         for (int e = 0; e < 64; e += 8) {
@@ -362,77 +497,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                 mbar_wait(&small_full[turn & 1], (turn >> 1) & 1, s_abort, a.err);
                 take(tmem + (2 + (turn & 1)) * 128);
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&small_empty[turn & 1]), 0));
-            } else {
-                mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
-                tc_fence_after();
-            }
-            const uint32_t acc = tmem + (count & 1) * BN + lanes + half * (BN / 2);
-#pragma unroll 1
-            for (int c = 0; c < Shape::kChunks; ++c) {
-                if (PARTS == 1 && c > 0) fetch(c, 0);
-                if (!inside(c)) continue;
+                if (!inside(0)) continue;
                 if (TERMS == 0) {
                     store_wait_read<0>();
                     __syncwarp();
-                } else if (PARTS == 1) {
-                    mbar_wait(&epi_full[w], uses & 1, s_abort, a.err);
-                    ++uses;
                 }
-                float v[PASS == kLast ? 64 : 32];
-#pragma unroll
-                for (int x0 = 0; x0 < 64; x0 += 32) {
-                    uint32_t d[32];
-                    if constexpr (PARTS == 1) tc_load(d, acc + c * 64 + x0);
-                    float* r = v + (PASS == kLast ? x0 : 0);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) r[e] = PARTS == 2 ? sum[PARTS == 2 ? x0 + e : 0] : pass.fd * __uint_as_float(d[e]);
+                if constexpr (PASS == kGram || PASS >= kApply) {
                     const float by = PASS == kGram ? left_of * left_of : left_of;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        unsigned char* at = buf + lane * 128 + ((((x0 + e) >> 3) ^ (lane & 7)) << 4);
-                        if constexpr (PARTS == 1 && TERMS > 0) {
-                            const uint4 h4 = *reinterpret_cast<const uint4*>(at);
-                            uint4 l4 = make_uint4(0, 0, 0, 0);
-                            if (!SYMMETRIC) l4 = *reinterpret_cast<const uint4*>(at + 4096);
-                            const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const float2 hf = unpack2<__half>(hw[z]), lf = unpack2<__half>(lw[z]);
-                                r[e + 2 * z] = fmaf(pass.f0, hf.x, fmaf(pass.f0, lf.x, r[e + 2 * z]));
-                                r[e + 2 * z + 1] = fmaf(pass.f0, hf.y, fmaf(pass.f0, lf.y, r[e + 2 * z + 1]));
-                            }
-                        }
-                        if constexpr (PASS == kGram || PASS >= kApply) {
-#pragma unroll
-                            for (int z = 0; z < 8; ++z) r[e + z] *= by;
-                        }
-                        if constexpr (PASS != kLast) {
-                            uint32_t hw[4], lw[4];
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) split_half2(r[e + 2 * z], r[e + 2 * z + 1], hw[z], lw[z]);
-                            *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-                            if (PARTS == 2 || PASS == kApply) *reinterpret_cast<uint4*>(at + 4096) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
-                        }
-                    }
+                    for (int e = 0; e < 64; ++e) sum[e] *= by;
                 }
                 if constexpr (PASS != kLast) {
+#pragma unroll
+                    for (int e = 0; e < 64; e += 8) {
+                        unsigned char* at = buf + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4);
+                        uint32_t hw[4], lw[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) split_half2(sum[e + 2 * z], sum[e + 2 * z + 1], hw[z], lw[z]);
+                        *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                        *reinterpret_cast<uint4*>(at + 4096) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                    }
                     fence_async_shared();
                     __syncwarp();
                     if (elect_one()) {
-                        bulk_store(place(to, c), buf, 4096);
-                        if (PARTS == 2 || PASS == kApply) bulk_store(place(to + lo, c), buf + 4096, 4096);
+                        bulk_store(place(to, 0), buf, 4096);
+                        bulk_store(place(to + lo_to, 0), buf + 4096, 4096);
                         store_commit();
                     }
                 } else {
                     const float scale = a.out * g.scale;
-                    const int row0 = rbox * kBox + (quad & 1) * 32, col0 = cbox(c) * kBox;
+                    const int row0 = rbox * kBox + (quad & 1) * 32, col0 = cbox(0) * kBox;
                     T* out = static_cast<T*>(g.out.p) + q.p * g.out.rep;
                     if (g.flip) {                                 // a row of X is a column of the result
                         if (row0 + lane < g.m) {
-                            T* at = out + (long long)col0 * g.out.row + row0 + lane;
+                            T* line = out + (long long)col0 * g.out.row + row0 + lane;
 #pragma unroll
                             for (int e = 0; e < 64; ++e)
-                                if (col0 + e < g.n) at[e * g.out.row] = from_f32<T>(v[e] * scale);
+                                if (col0 + e < g.n) line[e * g.out.row] = from_f32<T>(sum[e] * scale);
                         }
                     } else {
                         // through shared memory, 32 rows of 64 values, to runs along the rows
@@ -440,15 +541,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
 #pragma unroll
                         for (int e = 0; e < 64; e += 4)
                             *reinterpret_cast<float4*>(buf + lane * 256 + (((e >> 2) ^ (lane & 15)) << 4)) =
-                                make_float4(v[e] * scale, v[e + 1] * scale, v[e + 2] * scale, v[e + 3] * scale);
+                                make_float4(sum[e] * scale, sum[e + 1] * scale, sum[e + 2] * scale, sum[e + 3] * scale);
                         __syncwarp();
                         const int rows = min(32, g.m - row0), n = min(64, g.n - col0);
                         T* line = out + (long long)row0 * g.out.row + col0;
                         auto value = [&](int r, int x) { return buf + r * 256 + (((x >> 2) ^ (r & 15)) << 4) + (x & 3) * 4; };
-                        const bool pairs_of = sizeof(T) == 2 && ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
+                        const bool words = sizeof(T) == 2 && ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
 #pragma unroll 4
                         for (int r = 0; r < rows; ++r, line += g.out.row) {
-                            if (pairs_of) {
+                            if (words) {
                                 const int x0 = 2 * lane;
                                 const float2 f = *reinterpret_cast<const float2*>(value(r, x0));
                                 if constexpr (sizeof(T) == 2) {
@@ -466,12 +567,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                         __syncwarp();
                     }
                 }
-            }
-            if constexpr (PARTS == 1) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
-                ++count;
             }
         }
         store_wait_read<0>();

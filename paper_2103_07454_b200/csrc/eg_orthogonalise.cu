@@ -227,7 +227,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(
                 for (int e = 0; e < 4; ++e) u[z][e] = s_box[z * 16 + x.first][x.quad * 4 + e];
         }
         unsigned char* hi = a.ws + (m.x[0] + x.p * m.x_rep + (long long)cbox * m.rb + rbox) * kBoxBytes;
-        unsigned char* lo = hi + m.x_rep / 2 * kBoxBytes;
+        unsigned char* lo = a.ws + (m.lo[0] + x.p * m.x_rep + (long long)cbox * m.rb + rbox) * kBoxBytes;
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
             uint32_t h0, h1, l0, l1;
@@ -235,7 +235,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(
             split_half2(u[z][2], u[z][3], h1, l1);
             const uint32_t off = swz128((z * 16 + x.first) * 128 + x.quad * 8);
             *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
-            *reinterpret_cast<uint2*>(lo + off) = make_uint2(l0, l1);
+            *reinterpret_cast<uint2*>(lo + (a.parts == 1 ? lane_place(z * 16 + x.first, x.quad * 4) : off)) = make_uint2(l0, l1);
         }
     };
     for (int box = x.box0; box < x.box1; box += 2) {
@@ -336,12 +336,12 @@ int parts_of(const eg_orthogonalise_args* q) { return q->out_dtype == EG_BF16 ? 
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Sides {
-    int64_t rb, cb, boxes;                                // of one replica: X twice and the symmetric matrices, in two parts
+    int64_t rb, cb, boxes;                                // boxes: of one replica
 };
 Sides sides(const eg_orthogonalise_args* q, const eg_orthogonal_matrix& m) {
     const int64_t r = m.rows <= m.columns ? m.rows : m.columns, c = m.rows <= m.columns ? m.columns : m.rows;
     Sides s{up(r, kBox) / kBox, up(c, kBox) / kBox, 0};
-    s.boxes = 4 * s.rb * s.cb + (parts_of(q) == 2 ? 6 : 4) * s.rb * s.rb;
+    s.boxes = parts_of(q) == 2 ? 4 * s.rb * s.cb + 6 * s.rb * s.rb : 3 * s.rb * s.cb + 2 * s.rb * s.rb;
     return s;
 }
 // Matrices [first, *end) share their launches.  Returns their boxes.
@@ -386,6 +386,7 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
     a->partial = reinterpret_cast<double*>(behind + z.partial);
     a->turn = reinterpret_cast<float*>(behind + z.turn);
     a->P = (int)q->P;
+    a->parts = parts;
     a->count = (int)(end - first);
     a->momentum = (float)q->momentum;
     a->nesterov = q->nesterov != 0;
@@ -412,10 +413,13 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
         m->first = (int)(i * q->P);
         m->scale = (float)s.scale;
         const int64_t plane = z.rb * z.cb, square = z.rb * z.rb;
-        m->x_rep = 2 * plane; m->s_rep = 2 * square;
+        // hi and lo of X twice and of three symmetric matrices; or hi of X twice, lo of X, hi of two
+        m->x_rep = parts * plane; m->s_rep = parts * square;
         m->x[0] = at;
-        m->x[1] = at + q->P * 2 * plane;
-        for (int k = 0; k < 3; ++k) m->s[k] = at + q->P * (4 * plane + 2 * square * (parts == 2 ? k : k & 1));
+        m->x[1] = at + q->P * parts * plane;
+        m->lo[0] = parts == 2 ? m->x[0] + plane : at + q->P * 2 * plane;
+        m->lo[1] = parts == 2 ? m->x[1] + plane : m->lo[0];
+        for (int k = 0; k < 3; ++k) m->s[k] = at + q->P * (parts == 2 ? 4 * plane + 2 * square * k : 3 * plane + square * (k & 1));
         at += q->P * z.boxes;
         m->grad = strided(s.grad); m->out = strided(s.out); m->velocity = strided(s.velocity);
         m->velocity_out = s.velocity_out.data ? strided(s.velocity_out) : m->velocity;
