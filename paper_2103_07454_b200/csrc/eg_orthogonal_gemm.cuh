@@ -97,7 +97,7 @@ struct OrthoWalk {
     int base = 0;
 };
 struct OrthoPos {
-    int k, p, i, j;                               // matrix, replica, tile row and column
+    int k = 0, p = 0, i = 0, j = 0;               // matrix, replica, tile row and column
 };
 template <int PARTS, int PASS> __device__ __forceinline__ OrthoPos ortho_pos(const OrthoArgs& a, OrthoWalk& w, int t) {
     constexpr int S = PASS >= kApply ? 1 : 0, BOXES = OrthoShape<PARTS>::kBN / kBox;
@@ -192,9 +192,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
         // warp 0 fetches the left operand (and announces a stage's bytes), warp 3 the right one
         if (elect_one()) {
             int s = 0, round = 0;
-            OrthoPos next = ortho_pos<PARTS, PASS>(a, walk, pair);
+            OrthoPos upcoming = ortho_pos<PARTS, PASS>(a, walk, pair);
             for (int t = pair; t < tiles; t += pairs) {
-                const OrthoPos q = next;                                  // (the one after it is looked up under the copies)
+                const OrthoPos q = upcoming;                                  // (the one after it is looked up under the copies)
                 const OrthoMat& g = a.mat[q.k];
                 const bool left = warp == 0;
                 const long long x = g.x[from] + q.p * g.x_rep, sym = g.s[left ? pass.l : pass.r] + q.p * g.s_rep;
@@ -237,7 +237,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                         }
                     }
                     if (++s == S) { s = 0; ++round; }
-                    if (k == 0 && t + pairs < tiles) next = ortho_pos<PARTS, PASS>(a, walk, t + pairs);
+                    if (k == 0 && t + pairs < tiles) upcoming = ortho_pos<PARTS, PASS>(a, walk, t + pairs);
                 }
             }
             // the last arrivals on this CTA's barriers, which the even CTA's products send, come in before it ends
@@ -246,9 +246,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
             int s = 0, round = 0, count = 0, turn = 0;          // count: accumulators handed over; turn: tiles
-            OrthoPos next = ortho_pos<PARTS, PASS>(a, walk, pair);
+            OrthoPos upcoming = ortho_pos<PARTS, PASS>(a, walk, pair);
             for (int t = pair; t < tiles; t += pairs, ++turn) {
-                const OrthoPos q = next;                                  // (the one after it is looked up under the products)
+                const OrthoPos q = upcoming;                                  // (the one after it is looked up under the products)
                 const OrthoMat& g = a.mat[q.k];
                 const int ksteps = PASS == kGram ? g.cb : g.rb, right_block = q.j * (BN / kBox) / 4;
                 uint32_t add = 0, add_small = 0;
@@ -282,7 +282,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                     }
                     tc_commit_pair(&empty[s]);
                     if (++s == S) { s = 0; ++round; }
-                    if (k == 0 && t + pairs < tiles) next = ortho_pos<PARTS, PASS>(a, walk, t + pairs);
+                    if (k == 0 && t + pairs < tiles) upcoming = ortho_pos<PARTS, PASS>(a, walk, t + pairs);
                     if (PARTS == 2 && k + 1 < ksteps && (k + 1) % kOrthoChunk == 0) {
                         tc_commit_pair(&acc_full[count & 1]);
                         ++count;
