@@ -26,9 +26,11 @@
 // A and B are symmetric: only tiles of 256 x 256 on and below the diagonal are formed and stored.  An operand above it is read
 // from the box on the other side, as its transpose: the tensor cores take either order, step by step of K.
 //
-// Tiles, warps and barriers are those of eg_gemm.cuh: pairs of CTAs share a tile of 256 x BN, tcgen05.mma by one thread, the
+// Tiles and barriers are those of eg_gemm.cuh: pairs of CTAs share a tile of 256 x BN, tcgen05.mma by one thread, the
 // accumulators of two tiles in tensor memory.  PARTS == 2: BN = 128, an accumulator for hi hi that moves to registers every
-// kOrthoChunk steps (adding into it truncates) and one for the smaller products.
+// kOrthoChunk steps (adding into it truncates) and one for the smaller products.  Sixteen warps take the results: a result is
+// added to what was there, split and written again, which is latency upon latency, and eight warps took 11700 cycles for a tile whose products take
+// 8200 (m = 1024).
 #pragma once
 #include "eg_gemm.cuh"
 
@@ -37,6 +39,7 @@ namespace eg {
 constexpr int kBox = 64, kBoxBytes = 8192;
 constexpr int kOrthoMats = 48;                    // matrices of one launch
 constexpr int kOrthoChunk = 2;
+constexpr int kOrthoEpiWarps = 16, kOrthoThreads = 128 + 32 * kOrthoEpiWarps;
 // kSym0, kSym1, kSym2: with so many terms E.
 enum { kGram = 0, kSym0 = 1, kSym1 = 2, kSym2 = 3, kApply = 4, kLast = 5 };
 
@@ -63,6 +66,7 @@ struct OrthoPass {
     int first;                                    // X is still to be multiplied by `turn`
     int l, r, e0, e1, to;                         // symmetric matrices; apply: l
     float f0, f1, fd;                             // gram: fd;  apply: f0 X + fd S X
+    int read_lower, write_lower;                  // PARTS == 1, apply: whether X has lower parts, and needs them on
 };
 
 struct OrthoArgs {
@@ -84,11 +88,10 @@ template <int PARTS> struct OrthoShape {
     static constexpr int kBN = PARTS == 2 ? 128 : 256;
     static constexpr int kA = 2 * kBoxBytes * PARTS, kB = kBN / 128 * kBoxBytes * PARTS;     // of a stage and CTA
     static constexpr int kStages = PARTS == 2 ? 3 : 5;
-    static constexpr int kEpi = kGemmEpiWarps * kBoxBytes;      // a warp's 32 rows x 64 columns: hi and lo, or (PARTS == 1) two of hi
+    static constexpr int kEpi = 8 * kBoxBytes;                  // 32 rows x 64 columns, hi and lo, of two warps; PARTS == 1: hi, of one
     static constexpr int kBars = kStages * (kA + kB) + kEpi;
     static constexpr int kSmem = 1024 + kBars + 1024;
     static_assert(kSmem <= 227 * 1024, "shared memory");
-    static constexpr int kChunks = kBN / 128;                                               // of 64 columns for a warp
 };
 
 // The tiles in order, one pair's at a time: t only grows.
@@ -136,12 +139,23 @@ __device__ __forceinline__ void split_half2(float x, float y, uint32_t& hi, uint
     lo = pack2<__half>(x - f.x, y - f.y);
 }
 
+// Eight values that a row's piece adds to.
+__device__ __forceinline__ void add_piece(float* r, float f, const uint4& v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+        const float2 h = unpack2<__half>(w[z]);
+        r[2 * z] = fmaf(f, h.x, r[2 * z]);
+        r[2 * z + 1] = fmaf(f, h.y, r[2 * z + 1]);
+    }
+}
+
 // Byte of a lo part that no product reads: 8 columns of a row are a thread's 16 bytes, next to those of the rows above and below.
 __device__ __forceinline__ int lane_place(int row, int col) { return (row >> 5) * 4096 + (col >> 3) * 512 + (row & 31) * 16 + (col & 7) * 2; }
 
 // T: type of the caller's matrices (kLast).
 template <typename T, int PARTS, int PASS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_ortho(const __grid_constant__ OrthoArgs a, const OrthoPass pass) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constant__ OrthoArgs a, const OrthoPass pass) {
     using Shape = OrthoShape<PARTS>;
     constexpr int BN = Shape::kBN, S = Shape::kStages;
     constexpr bool SYMMETRIC = PASS < kApply;
@@ -156,8 +170,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
     uint64_t* acc_empty = acc_full + 2;                                  // [2] (even CTA's are used)
     uint64_t* small_full = acc_empty + 2;                                // [2]: accumulators of the smaller products
     uint64_t* small_empty = small_full + 2;                              // [2] (even CTA's are used)
-    uint64_t* epi_full = small_empty + 2;                                // [kGemmEpiWarps][2]
-    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + 2 * kGemmEpiWarps);
+    uint64_t* epi_full = small_empty + 2;                                // [kOrthoEpiWarps]
+    volatile int* s_abort = reinterpret_cast<volatile int*>(epi_full + kOrthoEpiWarps);
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(const_cast<int*>(s_abort) + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -166,10 +180,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
         *s_abort = 0;
         for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
         for (int q = 0; q < 2; ++q) {
-            op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kGemmEpiWarps);
-            op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kGemmEpiWarps);
+            op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kOrthoEpiWarps);
+            op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kOrthoEpiWarps);
         }
-        for (int q = 0; q < 2 * kGemmEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
+        for (int q = 0; q < kOrthoEpiWarps; ++q) op_mbar_init(&epi_full[q], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 3 && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&a.map) : "memory");
@@ -202,12 +216,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                 constexpr int RIGHT = BN / 128;                           // boxes of the right operand that a CTA fetches
                 const int limit = left || SYMMETRIC ? g.rb : g.cb;
                 const int box0 = left ? q.i * 4 + (int)rank * 2 : q.j * (2 * RIGHT) + (int)rank * RIGHT;
-                // boxes that are there: what the other rows and columns of D become, nobody stores
-                const int have = max(0, min(left ? 2 : RIGHT, limit - box0));
+                // boxes that are there: what the other rows and columns of D become, nobody stores.  (The two operands of a tile on the diagonal are
+                // the same rows of one matrix: fetched once.)
+                const bool share = PARTS == 1 && SYMMETRIC && q.i == q.j;
+                const int have = !left && share ? 0 : max(0, min(left ? 2 : RIGHT, limit - box0));
                 uint32_t bytes = 0;
                 if (left && rank == 0) {
                     const int r_limit = SYMMETRIC ? g.rb : g.cb;
-                    bytes = (uint32_t)(min(4, g.rb - q.i * 4) + min(2 * RIGHT, r_limit - q.j * (2 * RIGHT))) * kBoxBytes * PARTS;
+                    bytes = (uint32_t)(min(4, g.rb - q.i * 4) + (share ? 0 : min(2 * RIGHT, r_limit - q.j * (2 * RIGHT)))) * kBoxBytes * PARTS;
                 }
                 for (int k = 0; k < ksteps; ++k) {
                     if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
@@ -251,6 +267,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                 const OrthoPos q = upcoming;                                  // (the one after it is looked up under the products)
                 const OrthoMat& g = a.mat[q.k];
                 const int ksteps = PASS == kGram ? g.cb : g.rb, right_block = q.j * (BN / kBox) / 4;
+                const bool share = PARTS == 1 && SYMMETRIC && q.i == q.j;
                 uint32_t add = 0, add_small = 0;
                 const uint32_t small = tmem + (2 + (turn & 1)) * 128;
                 if (PARTS == 2 && turn >= 2) mbar_wait(&small_empty[turn & 1], ((turn >> 1) - 1) & 1, s_abort, a.err);
@@ -267,8 +284,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                     mbar_wait(&full[s], round & 1, s_abort, a.err);
                     tc_fence_after();
                     auto product = [&](uint32_t to, int pa, int pb, uint32_t& add_to) {
-                        const uint64_t da = smem_desc(op_smem(smem + s * Shape::kA + pa * 2 * kBoxBytes), a_mn);
-                        const uint64_t db = smem_desc(op_smem(ring_b + s * Shape::kB + pb * (BN / 128) * kBoxBytes), b_mn);
+                        unsigned char* l = smem + s * Shape::kA + pa * 2 * kBoxBytes;
+                        const uint64_t da = smem_desc(op_smem(l), a_mn);
+                        const uint64_t db = smem_desc(op_smem(share ? l : ring_b + s * Shape::kB + pb * (BN / 128) * kBoxBytes), b_mn);
 #pragma unroll
                         for (int u = 0; u < kGemmK / 16; ++u) {
                             tc_mma_pair(to, da + u * a_step, db + u * b_step, idesc, add_to);
@@ -295,201 +313,165 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
             }
         }
     } else if (warp >= 4) {
-        const int w = warp - 4, half = w >> 2, quad = w & 3;
-        unsigned char* buf = epi + w * kBoxBytes;
+        // rows 32 * quad of the CTA's 128; PARTS == 1: the 64 columns of one box;  2: 32 columns, half of a box that two warps share
+        const int w = warp - 4, quad = w & 3, group = w >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        int count = 0, turn = 0, uses[2] = {0, 0};
+        int count = 0, turn = 0, uses = 0;
         for (int t = pair; t < tiles; t += pairs, ++turn) {
             const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
             const OrthoMat& g = a.mat[q.k];
             const int ksteps = PASS == kGram ? g.cb : g.rb;
-            const int rbox = q.i * 4 + (int)rank * 2 + (quad >> 1), cols = SYMMETRIC ? g.rb : g.cb;
+            const int rbox = q.i * 4 + (int)rank * 2 + (quad >> 1), cbox = q.j * (BN / kBox) + (PARTS == 1 ? group : group >> 1);
+            const bool inside = rbox < g.rb && cbox < (SYMMETRIC ? g.rb : g.cb);
             const long long x = g.x[from] + q.p * g.x_rep, to = SYMMETRIC ? g.s[pass.to] + q.p * g.s_rep : g.x[from ^ 1] + q.p * g.x_rep;
             const float left_of = pass.first && (PASS == kGram || PASS >= kApply) ? a.turn[g.first + q.p] : 1.f;
-            auto cbox = [&](int c) { return q.j * (BN / kBox) + half * Shape::kChunks + c; };
-            auto inside = [&](int c) { return rbox < g.rb && cbox(c) < cols; };
-            auto place = [&](long long matrix, int c) { return a.ws + (matrix + (long long)cbox(c) * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096; };
+            const float by = PASS == kGram ? left_of * left_of : left_of;
+            // half a box, 32 rows: 4 KB in one piece
+            auto place = [&](long long matrix) { return a.ws + (matrix + (long long)cbox * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096; };
+            const int row0 = rbox * kBox + (quad & 1) * 32;
+            const float scale = a.out * g.scale;
+            T* const out = PASS == kLast ? static_cast<T*>(g.out.p) + q.p * g.out.rep : nullptr;
             if constexpr (PARTS == 1) {
-                // Two chunks of 64 columns, each with its own half of the staging memory; what they are added to is on its way while the
-                // products run.
-                uint4 low[PASS >= kApply ? 2 : 1][PASS >= kApply ? 8 : 1];
-                auto low_at = [&](int c) {
-                    return a.ws + (g.lo[0] + q.p * g.x_rep + (long long)cbox(c) * g.rb + rbox) * kBoxBytes + (quad & 1) * 4096 + lane * 16;
-                };
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if (TERMS == 0 || !inside(c)) continue;
-                    if (c == 0) store_wait_read<1>();             // (the last tile's second chunk may still be on its way out)
-                    else store_wait_read<0>();
+                unsigned char* box = epi + w * 4096;
+                uint4 low[PASS >= kApply ? 8 : 1];
+                unsigned char* const low_at = PASS >= kApply ? place(g.lo[0] + q.p * g.x_rep) + lane * 16 : nullptr;
+                if (inside && TERMS > 0) {                        // what the result is added to comes in under the products
+                    store_wait_read<0>();
                     __syncwarp();
                     if (elect_one()) {
-                        op_mbar_expect(&epi_full[2 * w + c], 4096);
-                        op_bulk_load(buf + c * 4096, place(SYMMETRIC ? g.s[pass.e0] + q.p * g.s_rep : x, c), 4096, &epi_full[2 * w + c]);
+                        op_mbar_expect(&epi_full[w], 4096);
+                        op_bulk_load(box, place(SYMMETRIC ? g.s[pass.e0] + q.p * g.s_rep : x), 4096, &epi_full[w]);
                     }
                     if constexpr (PASS >= kApply) {
 #pragma unroll
-                        for (int z = 0; z < 8; ++z) low[c][z] = *reinterpret_cast<const uint4*>(low_at(c) + z * 512);
+                        for (int z = 0; z < 8; ++z) low[z] = pass.read_lower ? *reinterpret_cast<const uint4*>(low_at + z * 512) : make_uint4(0, 0, 0, 0);
                     }
                 }
                 mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
                 tc_fence_after();
-                const uint32_t acc = tmem + (count & 1) * BN + lanes + half * (BN / 2);
-                const float by = PASS == kGram ? left_of * left_of : left_of;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    unsigned char* box = buf + c * 4096;
-                    if (inside(c)) {
-                        if (TERMS == 0) {
-                            store_wait_read<1>();
-                            __syncwarp();
-                        } else {
-                            mbar_wait(&epi_full[2 * w + c], uses[c] & 1, s_abort, a.err);
-                            ++uses[c];
-                        }
-                        unsigned char* low_to = PASS == kApply ? low_at(c) : nullptr;
-#pragma unroll
-                        for (int x0 = 0; x0 < 64; x0 += 32) {
-                            uint32_t d[32];
-                            tc_load(d, acc + c * 64 + x0);
-                            float r[32];
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) r[e] = pass.fd * __uint_as_float(d[e]);
-#pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
-                                const int piece = (x0 + e) >> 3;
-                                unsigned char* at = box + lane * 128 + ((piece ^ (lane & 7)) << 4);
-                                if constexpr (TERMS > 0) {
-                                    const uint4 h4 = *reinterpret_cast<const uint4*>(at);
-                                    const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w};
-#pragma unroll
-                                    for (int z = 0; z < 4; ++z) {
-                                        const float2 hf = unpack2<__half>(hw[z]);
-                                        r[e + 2 * z] = fmaf(pass.f0, hf.x, r[e + 2 * z]);
-                                        r[e + 2 * z + 1] = fmaf(pass.f0, hf.y, r[e + 2 * z + 1]);
-                                    }
-                                }
-                                if constexpr (PASS >= kApply) {
-                                    const uint4 l4 = low[c][piece];
-                                    const uint32_t lw[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                                    for (int z = 0; z < 4; ++z) {
-                                        const float2 lf = unpack2<__half>(lw[z]);
-                                        r[e + 2 * z] = fmaf(pass.f0, lf.x, r[e + 2 * z]);
-                                        r[e + 2 * z + 1] = fmaf(pass.f0, lf.y, r[e + 2 * z + 1]);
-                                    }
-                                }
-                                if constexpr (PASS == kGram || PASS >= kApply) {
-#pragma unroll
-                                    for (int z = 0; z < 8; ++z) r[e + z] *= by;
-                                }
-                                uint32_t hw[4], lw[4];
-                                if constexpr (PASS == kLast) {
-                                    const float scale = a.out * g.scale;
-#pragma unroll
-                                    for (int z = 0; z < 4; ++z) {
-                                        if constexpr (sizeof(T) == 2) hw[z] = pack2<T>(r[e + 2 * z] * scale, r[e + 2 * z + 1] * scale);
-                                    }
-                                } else {
-#pragma unroll
-                                    for (int z = 0; z < 4; ++z) split_half2(r[e + 2 * z], r[e + 2 * z + 1], hw[z], lw[z]);
-                                }
-                                *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-                                if constexpr (PASS == kApply) *reinterpret_cast<uint4*>(low_to + piece * 512) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
-                            }
-                        }
+                const uint32_t acc = tmem + (count & 1) * BN + lanes + group * 64;
+                if (inside) {
+                    if (TERMS == 0) {
+                        store_wait_read<0>();
+                        __syncwarp();
+                    } else {
+                        mbar_wait(&epi_full[w], uses & 1, s_abort, a.err);
+                        ++uses;
                     }
-                    if constexpr (PASS != kLast) {
-                        fence_async_shared();
-                        __syncwarp();
-                        if (elect_one()) {
-                            if (inside(c)) bulk_store(place(to, c), box, 4096);
-                            store_commit();                       // (one group a chunk, empty or not)
-                        }
-                    } else if (inside(c)) {
-                        const int row0 = rbox * kBox + (quad & 1) * 32, col0 = cbox(c) * kBox;
-                        const int rows = min(32, g.m - row0), n = min(64, g.n - col0);
-                        T* out = static_cast<T*>(g.out.p) + q.p * g.out.rep;
-                        if (g.flip) {                             // a row of X is a column of the result
-                            if (lane < rows) {
-                                T* line = out + (long long)col0 * g.out.row + row0 + lane;
-#pragma unroll 8
-                                for (int e = 0; e < n; ++e)
-                                    line[e * g.out.row] = *reinterpret_cast<const T*>(box + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4) + (e & 7) * 2);
+#pragma unroll
+                    for (int x0 = 0; x0 < 64; x0 += 16) {
+                        uint32_t d[16];
+                        tc_load(d, acc + x0);
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8) {
+                            const int piece = (x0 + e) >> 3;
+                            unsigned char* at = box + lane * 128 + ((piece ^ (lane & 7)) << 4);
+                            float r[8];
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) r[z] = pass.fd * __uint_as_float(d[e + z]);
+                            if constexpr (TERMS > 0) add_piece(r, pass.f0, *reinterpret_cast<const uint4*>(at));
+                            if constexpr (PASS >= kApply) add_piece(r, pass.f0, low[piece]);
+                            if constexpr (PASS == kGram || PASS >= kApply) {
+#pragma unroll
+                                for (int z = 0; z < 8; ++z) r[z] *= by;
                             }
-                        } else {                                  // runs along the rows
-                            __syncwarp();
-                            T* line = out + (long long)row0 * g.out.row + col0;
-                            const bool words = ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
-#pragma unroll 4
-                            for (int r = 0; r < rows; ++r, line += g.out.row) {
-                                const uint32_t v = *reinterpret_cast<const uint32_t*>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
-                                if (words && 2 * lane + 1 < n) {
-                                    *reinterpret_cast<uint32_t*>(line + 2 * lane) = v;
-                                } else {
-                                    uint16_t* o = reinterpret_cast<uint16_t*>(line + 2 * lane);
-                                    if (2 * lane < n) o[0] = (uint16_t)v;
-                                    if (2 * lane + 1 < n) o[1] = (uint16_t)(v >> 16);
-                                }
+                            uint32_t hw[4], lw[4];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                if constexpr (PASS == kLast && sizeof(T) == 2) hw[z] = pack2<T>(r[2 * z] * scale, r[2 * z + 1] * scale);
+                                else split_half2(r[2 * z], r[2 * z + 1], hw[z], lw[z]);
                             }
+                            *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                            if constexpr (PASS == kApply)
+                                if (pass.write_lower) *reinterpret_cast<uint4*>(low_at + piece * 512) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
                         }
-                        // the next box's copy comes by another way than these reads
-                        fence_async_shared();
-                        __syncwarp();
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
                 ++count;
-            } else {
-                const long long lo = SYMMETRIC ? g.s_rep / 2 : g.lo[from] - g.x[from], lo_to = SYMMETRIC ? g.s_rep / 2 : g.lo[from ^ 1] - g.x[from ^ 1];
-                // what the result is added to
-                auto fetch = [&](int term) {
-                    if (TERMS == 0 || !inside(0)) return;
-                    store_wait_read<0>();
+                if (!inside) continue;
+                if constexpr (PASS != kLast) {
+                    fence_async_shared();
                     __syncwarp();
                     if (elect_one()) {
-                        const long long matrix = SYMMETRIC ? g.s[term ? pass.e1 : pass.e0] + q.p * g.s_rep : x;
-                        op_mbar_expect(&epi_full[w], 8192);
-                        op_bulk_load(buf, place(matrix, 0), 4096, &epi_full[w]);
-                        op_bulk_load(buf + 4096, place(matrix + lo, 0), 4096, &epi_full[w]);
+                        bulk_store(place(to), box, 4096);
+                        store_commit();
                     }
-                };
-                fetch(0);
-                float sum[64];                                    // this row's 64 columns: the terms, then the products' chunks
-#pragma unroll
-                for (int e = 0; e < 64; ++e) sum[e] = 0.f;
-                if (inside(0)) {
-#pragma unroll 1
-                    for (int term = 0; term < TERMS; ++term) {
-                        if (term > 0) fetch(term);
-                        mbar_wait(&epi_full[w], uses[0] & 1, s_abort, a.err);
-                        ++uses[0];
-                        const float f = term ? pass.f1 : pass.f0;
-#pragma unroll
-                        for (int e = 0; e < 64; e += 8) {
-                            const unsigned char* at = buf + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4);
-                            const uint4 h4 = *reinterpret_cast<const uint4*>(at), l4 = *reinterpret_cast<const uint4*>(at + 4096);
-                            const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const float2 hf = unpack2<__half>(hw[z]), lf = unpack2<__half>(lw[z]);
-                                sum[e + 2 * z] = fmaf(f, hf.x, fmaf(f, lf.x, sum[e + 2 * z]));
-                                sum[e + 2 * z + 1] = fmaf(f, hf.y, fmaf(f, lf.y, sum[e + 2 * z + 1]));
+                } else if constexpr (sizeof(T) == 2) {
+                    const int col0 = cbox * kBox, rows = min(32, g.m - row0), n = min(64, g.n - col0);
+                    if (g.flip) {                                 // a row of X is a column of the result
+                        if (lane < rows) {
+                            T* line = out + (long long)col0 * g.out.row + row0 + lane;
+#pragma unroll 8
+                            for (int e = 0; e < n; ++e)
+                                line[e * g.out.row] = *reinterpret_cast<const T*>(box + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4) + (e & 7) * 2);
+                        }
+                    } else {                                      // runs along the rows
+                        T* line = out + (long long)row0 * g.out.row + col0;
+                        const bool words = ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
+#pragma unroll 4
+                        for (int r = 0; r < rows; ++r, line += g.out.row) {
+                            const uint32_t v = *reinterpret_cast<const uint32_t*>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+                            if (words && 2 * lane + 1 < n) {
+                                *reinterpret_cast<uint32_t*>(line + 2 * lane) = v;
+                            } else {
+                                uint16_t* o = reinterpret_cast<uint16_t*>(line + 2 * lane);
+                                if (2 * lane < n) o[0] = (uint16_t)v;
+                                if (2 * lane + 1 < n) o[1] = (uint16_t)(v >> 16);
                             }
                         }
+                    }
+                    // the next box's copy comes by another way than these reads
+                    fence_async_shared();
+                    __syncwarp();
+                }
+            } else {
+                const int sub = group & 1, pair_of = quad + 4 * (group >> 1);      // the two warps of a box
+                unsigned char* box = epi + pair_of * kBoxBytes;
+                auto together = [&] { op_named_barrier(1 + pair_of, 64); };
+                const long long lo = SYMMETRIC ? g.s_rep / 2 : g.lo[from] - g.x[from], lo_to = SYMMETRIC ? g.s_rep / 2 : g.lo[from ^ 1] - g.x[from ^ 1];
+                auto fetch = [&](int term) {                      // by the first of the two warps
+                    if (sub == 0) {
+                        store_wait_read<0>();
                         __syncwarp();
+                        if (elect_one()) {
+                            const long long matrix = SYMMETRIC ? g.s[term ? pass.e1 : pass.e0] + q.p * g.s_rep : x;
+                            op_mbar_expect(&epi_full[pair_of], 8192);
+                            op_bulk_load(box, place(matrix), 4096, &epi_full[pair_of]);
+                            op_bulk_load(box + 4096, place(matrix + lo), 4096, &epi_full[pair_of]);
+                        }
+                    }
+                };
+                auto piece_at = [&](int z) { return box + lane * 128 + (((sub * 4 + z) ^ (lane & 7)) << 4); };
+                if (inside && TERMS > 0) fetch(0);
+                float sum[32];                                    // this row's 32 columns: the terms, then the products' chunks
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[e] = 0.f;
+                if (inside) {
+#pragma unroll 1
+                    for (int term = 0; term < TERMS; ++term) {
+                        if (term > 0) {
+                            together();                           // both have read the first one
+                            fetch(term);
+                        }
+                        mbar_wait(&epi_full[pair_of], uses & 1, s_abort, a.err);
+                        ++uses;
+                        const float f = term ? pass.f1 : pass.f0;
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            add_piece(sum + z * 8, f, *reinterpret_cast<const uint4*>(piece_at(z) + 4096));
+                            add_piece(sum + z * 8, f, *reinterpret_cast<const uint4*>(piece_at(z)));
+                        }
                     }
                 }
                 auto take = [&](uint32_t acc) {
                     tc_fence_after();
+                    uint32_t v[32];
+                    tc_load(v, acc + lanes + group * 32);
 #pragma unroll
-                    for (int e = 0; e < 64; e += 32) {
-                        uint32_t v[32];
-                        tc_load(v, acc + lanes + half * 64 + e);
-#pragma unroll
-                        for (int z = 0; z < 32; ++z) sum[e + z] = fmaf(pass.fd, __uint_as_float(v[z]), sum[e + z]);
-                    }
+                    for (int z = 0; z < 32; ++z) sum[z] = fmaf(pass.fd, __uint_as_float(v[z]), sum[z]);
                     tc_fence_before();
                     __syncwarp();
                 };
@@ -501,75 +483,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_o
                 mbar_wait(&small_full[turn & 1], (turn >> 1) & 1, s_abort, a.err);
                 take(tmem + (2 + (turn & 1)) * 128);
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&small_empty[turn & 1]), 0));
-                if (!inside(0)) continue;
-                if (TERMS == 0) {
-                    store_wait_read<0>();
-                    __syncwarp();
-                }
+                if (!inside) continue;
                 if constexpr (PASS == kGram || PASS >= kApply) {
-                    const float by = PASS == kGram ? left_of * left_of : left_of;
 #pragma unroll
-                    for (int e = 0; e < 64; ++e) sum[e] *= by;
+                    for (int e = 0; e < 32; ++e) sum[e] *= by;
+                }
+                if (TERMS == 0 || PASS == kLast) {                // the box is free: its store has been read; both have read what it held
+                    if (sub == 0) store_wait_read<0>();
+                    together();
                 }
                 if constexpr (PASS != kLast) {
 #pragma unroll
-                    for (int e = 0; e < 64; e += 8) {
-                        unsigned char* at = buf + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4);
+                    for (int z = 0; z < 4; ++z) {
                         uint32_t hw[4], lw[4];
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) split_half2(sum[e + 2 * z], sum[e + 2 * z + 1], hw[z], lw[z]);
-                        *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-                        *reinterpret_cast<uint4*>(at + 4096) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                        for (int y = 0; y < 4; ++y) split_half2(sum[z * 8 + 2 * y], sum[z * 8 + 2 * y + 1], hw[y], lw[y]);
+                        *reinterpret_cast<uint4*>(piece_at(z)) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                        *reinterpret_cast<uint4*>(piece_at(z) + 4096) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
                     }
                     fence_async_shared();
-                    __syncwarp();
-                    if (elect_one()) {
-                        bulk_store(place(to, 0), buf, 4096);
-                        bulk_store(place(to + lo_to, 0), buf + 4096, 4096);
+                    together();
+                    if (sub == 0 && elect_one()) {
+                        bulk_store(place(to), box, 4096);
+                        bulk_store(place(to + lo_to), box + 4096, 4096);
                         store_commit();
                     }
                 } else {
-                    const float scale = a.out * g.scale;
-                    const int row0 = rbox * kBox + (quad & 1) * 32, col0 = cbox(0) * kBox;
-                    T* out = static_cast<T*>(g.out.p) + q.p * g.out.rep;
+                    const int col0 = cbox * kBox + sub * 32, rows = min(32, g.m - row0), n = min(32, g.n - col0);
                     if (g.flip) {                                 // a row of X is a column of the result
-                        if (row0 + lane < g.m) {
+                        if (lane < rows) {
                             T* line = out + (long long)col0 * g.out.row + row0 + lane;
 #pragma unroll
-                            for (int e = 0; e < 64; ++e)
-                                if (col0 + e < g.n) line[e * g.out.row] = from_f32<T>(sum[e] * scale);
+                            for (int e = 0; e < 32; ++e)
+                                if (e < n) line[e * g.out.row] = from_f32<T>(sum[e] * scale);
                         }
                     } else {
-                        // through shared memory, 32 rows of 64 values, to runs along the rows
-                        __syncwarp();
+                        // through this warp's half of the box, 32 rows of 32 values, to runs along the rows
+                        unsigned char* mine = box + sub * 4096;
 #pragma unroll
-                        for (int e = 0; e < 64; e += 4)
-                            *reinterpret_cast<float4*>(buf + lane * 256 + (((e >> 2) ^ (lane & 15)) << 4)) =
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<float4*>(mine + lane * 128 + (((e >> 2) ^ (lane & 7)) << 4)) =
                                 make_float4(sum[e] * scale, sum[e + 1] * scale, sum[e + 2] * scale, sum[e + 3] * scale);
                         __syncwarp();
-                        const int rows = min(32, g.m - row0), n = min(64, g.n - col0);
                         T* line = out + (long long)row0 * g.out.row + col0;
-                        auto value = [&](int r, int x) { return buf + r * 256 + (((x >> 2) ^ (r & 15)) << 4) + (x & 3) * 4; };
-                        const bool words = sizeof(T) == 2 && ((uintptr_t)line & 3) == 0 && (g.out.row & 1) == 0;
-#pragma unroll 4
+#pragma unroll 8
                         for (int r = 0; r < rows; ++r, line += g.out.row) {
-                            if (words) {
-                                const int x0 = 2 * lane;
-                                const float2 f = *reinterpret_cast<const float2*>(value(r, x0));
-                                if constexpr (sizeof(T) == 2) {
-                                    if (x0 + 1 < n) *reinterpret_cast<uint32_t*>(line + x0) = pack2<T>(f.x, f.y);
-                                    else if (x0 < n) line[x0] = from_f32<T>(f.x);
-                                }
-                            } else {
-                                const float f0 = *reinterpret_cast<const float*>(value(r, lane)), f1 = *reinterpret_cast<const float*>(value(r, lane + 32));
-                                if (lane < n) line[lane] = from_f32<T>(f0);
-                                if (lane + 32 < n) line[lane + 32] = from_f32<T>(f1);
-                            }
+                            const float f = *reinterpret_cast<const float*>(mine + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+                            if (lane < n) line[lane] = from_f32<T>(f);
                         }
-                        // the next box's copy comes by another way than these reads
-                        fence_async_shared();
-                        __syncwarp();
                     }
+                    // the next box's copy comes by another way than these accesses
+                    fence_async_shared();
+                    together();
                 }
             }
         }

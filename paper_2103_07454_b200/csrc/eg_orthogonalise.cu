@@ -461,7 +461,7 @@ template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& 
     }
     const int pairs = sm_count() / 2, tiles = a.tiles[PASS >= kApply ? 1 : 0];
     if (pairs < 1) return cudaErrorInvalidDevice;
-    return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kGemmThreads), smem, stream, a, pass);
+    return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kOrthoThreads), smem, stream, a, pass);
 }
 
 template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, cudaStream_t stream) {
@@ -474,6 +474,8 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
     };
     cudaError_t e = q->dtype == EG_F32 ? given(0.f) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}) : given(__half{});
     int from = 0;
+    bool any_velocity = false, kept = false;
+    for (int i = 0; i < a.count; ++i) any_velocity = any_velocity || a.mat[i].velocity.p;
     for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
         const double *c0 = s.c[k], sa = s.sa, sb0 = s.sb[k];
         OrthoPass p{};
@@ -518,6 +520,12 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
         }
         p.f0 = (float)outer;
         p.fd = (float)(1.0 / scale);
+        // The lower parts of X.  There are none at first where u is the gradient of 8 bits; where the steps to come multiply what
+        // is lost now (2^-12.8 of X in the mean) by 4 at most, it stays below the rounding of the results.
+        p.read_lower = k == 1 ? any_velocity : kept;
+        double growth = 1.0;
+        for (int z = k; z < q->steps; ++z) growth *= fmax(1.0, fabs(s.c[z][0]));
+        p.write_lower = kept = growth > 4.0;
         if (e != cudaSuccess) break;
         e = k < q->steps ? product<float, PARTS, kApply>(a, p, stream) : product<T, PARTS, kLast>(a, p, stream);
     }
