@@ -178,7 +178,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         *s_abort = 0;
-        for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
+        for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 4); op_mbar_init(&empty[s], 1); }
         for (int q = 0; q < 2; ++q) {
             op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kOrthoEpiWarps);
             op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kOrthoEpiWarps);
@@ -225,11 +225,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                     const int r_limit = SYMMETRIC ? g.rb : g.cb;
                     bytes = (uint32_t)(min(4, g.rb - q.i * 4) + (share ? 0 : min(2 * RIGHT, r_limit - q.j * (2 * RIGHT)))) * kBoxBytes * PARTS;
                 }
+                if (*s_abort) break;                                      // (after a time-out nobody starts anything more)
                 for (int k = 0; k < ksteps; ++k) {
                     if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
+                    if (*s_abort) break;
                     unsigned char* to = left ? smem + s * Shape::kA : ring_b + s * Shape::kB;
-                    if (left && rank == 0) op_mbar_expect(&full[s], bytes);
                     const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
+                    // All four of a pair's fetching threads announce every stage, also those that fetch nothing of it: one that fell behind by
+                    // two rounds would take the phase of `empty` for the one before.
+                    if (left && rank == 0) op_mbar_expect(&full[s], bytes);
+                    else mbar_arrive_cluster(bar);
                     // (row, k) of a stored box; above the diagonal of a symmetric operand its mirror image; X by its columns
                     long long box, next, lo;
                     const bool is_x = PASS == kGram || (!SYMMETRIC && !left);
@@ -282,6 +287,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                     }
                     const uint32_t d = tmem + (count & 1) * BN;
                     mbar_wait(&full[s], round & 1, s_abort, a.err);
+                    if (*s_abort) break;
                     tc_fence_after();
                     auto product = [&](uint32_t to, int pa, int pb, uint32_t& add_to) {
                         unsigned char* l = smem + s * Shape::kA + pa * 2 * kBoxBytes;
@@ -307,6 +313,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                         add = 0;
                     }
                 }
+                if (*s_abort) break;
                 tc_commit_pair(&acc_full[count & 1]);
                 ++count;
                 if (PARTS == 2) tc_commit_pair(&small_full[turn & 1]);
@@ -318,6 +325,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         int count = 0, turn = 0, uses = 0;
         for (int t = pair; t < tiles; t += pairs, ++turn) {
+            if (__any_sync(0xffffffffu, *s_abort)) break;
             const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
             const OrthoMat& g = a.mat[q.k];
             const int ksteps = PASS == kGram ? g.cb : g.rb;
