@@ -178,7 +178,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         *s_abort = 0;
-        for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 4); op_mbar_init(&empty[s], 1); }
+        for (int s = 0; s < S; ++s) { op_mbar_init(&full[s], 1); op_mbar_init(&empty[s], 1); }
         for (int q = 0; q < 2; ++q) {
             op_mbar_init(&acc_full[q], 1); op_mbar_init(&acc_empty[q], 2 * kOrthoEpiWarps);
             op_mbar_init(&small_full[q], 1); op_mbar_init(&small_empty[q], 2 * kOrthoEpiWarps);
@@ -196,8 +196,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
-    // set up while the kernel before this one finished; from here on its results are read and overwritten
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // Set up, and the first tile looked up, while the kernel before this one finishes; whoever reads its results waits for them.
+    auto wait_before = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = a.tiles[SYMMETRIC ? 0 : 1];
     const int from = pass.from;
     OrthoWalk walk;
@@ -207,6 +207,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
         if (elect_one()) {
             int s = 0, round = 0;
             OrthoPos upcoming = ortho_pos<PARTS, PASS>(a, walk, pair);
+            wait_before();
             for (int t = pair; t < tiles; t += pairs) {
                 const OrthoPos q = upcoming;                                  // (the one after it is looked up under the copies)
                 const OrthoMat& g = a.mat[q.k];
@@ -215,26 +216,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 const int ksteps = PASS == kGram ? g.cb : g.rb;
                 constexpr int RIGHT = BN / 128;                           // boxes of the right operand that a CTA fetches
                 const int limit = left || SYMMETRIC ? g.rb : g.cb;
-                const int box0 = left ? q.i * 4 + (int)rank * 2 : q.j * (2 * RIGHT) + (int)rank * RIGHT;
-                // boxes that are there: what the other rows and columns of D become, nobody stores.  (The two operands of a tile on the diagonal are
-                // the same rows of one matrix: fetched once.)
+                // The two operands of a tile on the diagonal are the same rows of one matrix: fetched once, a box by either warp.
                 const bool share = PARTS == 1 && SYMMETRIC && q.i == q.j;
-                const int have = !left && share ? 0 : max(0, min(left ? 2 : RIGHT, limit - box0));
+                // Boxes of an operand that a CTA fetches: those that are there (what the other rows and columns of D become, nobody stores), but one at
+                // least.  Every fetching thread has a part in every stage that way: one without could fall two rounds behind, take the phase of
+                // `empty` for the one before, and wait for good.  (An arrival from each instead, across the pair: 4.9 -> 7.5 ms for the largest case.)
+                auto boxes = [&](bool of_left, int r) {
+                    const int wide = of_left ? 2 : RIGHT, first = of_left ? q.i * 4 + r * 2 : q.j * (2 * RIGHT) + r * RIGHT;
+                    return share ? 1 : max(1, min(wide, (of_left || SYMMETRIC ? g.rb : g.cb) - first));
+                };
+                const int have = boxes(left, (int)rank);
+                const int box0 = min(share ? q.i * 4 + (int)rank * 2 + (left ? 0 : 1) : left ? q.i * 4 + (int)rank * 2 : q.j * (2 * RIGHT) + (int)rank * RIGHT,
+                                     limit - 1);
+                const int block = left ? q.i : q.j * (2 * RIGHT) / 4;     // rows or columns of 256
                 uint32_t bytes = 0;
-                if (left && rank == 0) {
-                    const int r_limit = SYMMETRIC ? g.rb : g.cb;
-                    bytes = (uint32_t)(min(4, g.rb - q.i * 4) + (share ? 0 : min(2 * RIGHT, r_limit - q.j * (2 * RIGHT)))) * kBoxBytes * PARTS;
-                }
+                if (left && rank == 0) bytes = (uint32_t)(boxes(true, 0) + boxes(true, 1) + boxes(false, 0) + boxes(false, 1)) * kBoxBytes * PARTS;
                 if (*s_abort) break;                                      // (after a time-out nobody starts anything more)
                 for (int k = 0; k < ksteps; ++k) {
                     if (round > 0) mbar_wait(&empty[s], (round - 1) & 1, s_abort, a.err);
                     if (*s_abort) break;
-                    unsigned char* to = left ? smem + s * Shape::kA : ring_b + s * Shape::kB;
+                    unsigned char* to = left ? smem + s * Shape::kA : share ? smem + s * Shape::kA + kBoxBytes : ring_b + s * Shape::kB;
                     const uint32_t bar = map_to_rank(op_smem(&full[s]), 0);
-                    // All four of a pair's fetching threads announce every stage, also those that fetch nothing of it: one that fell behind by
-                    // two rounds would take the phase of `empty` for the one before.
                     if (left && rank == 0) op_mbar_expect(&full[s], bytes);
-                    else mbar_arrive_cluster(bar);
                     // (row, k) of a stored box; above the diagonal of a symmetric operand its mirror image; X by its columns
                     long long box, next, lo;
                     const bool is_x = PASS == kGram || (!SYMMETRIC && !left);
@@ -244,7 +247,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                         next = by_column ? g.rb : 1;
                         lo = g.lo[from] - g.x[from];
                     } else {
-                        const bool mirror = k / 4 > box0 / 4;
+                        const bool mirror = k / 4 > block;
                         box = sym + (mirror ? (long long)box0 * g.rb + k : (long long)k * g.rb + box0);
                         next = mirror ? g.rb : 1;
                         lo = g.s_rep / 2;
@@ -324,9 +327,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
         const int w = warp - 4, quad = w & 3, group = w >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         int count = 0, turn = 0, uses = 0;
+        OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, pair);
+        wait_before();
         for (int t = pair; t < tiles; t += pairs, ++turn) {
             if (__any_sync(0xffffffffu, *s_abort)) break;
-            const OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, t);
+            if (t != pair) q = ortho_pos<PARTS, PASS>(a, walk, t);
             const OrthoMat& g = a.mat[q.k];
             const int ksteps = PASS == kGram ? g.cb : g.rb;
             const int rbox = q.i * 4 + (int)rank * 2 + (quad >> 1), cbox = q.j * (BN / kBox) + (PARTS == 1 ? group : group >> 1);
