@@ -379,6 +379,137 @@ template <typename T> __global__ void __launch_bounds__(256) k_embed_join(const 
     }
 }
 
+// Few places: one launch.  A block owns some rows of the table and 32 * U vectors of their columns, sorts the places of its rows in
+// shared memory (warps one after another, so that the order is that of the places), and then a warp adds up and writes one row after
+// another.  Rows with many places are added up by all warps.  For how many places and how large a table, us, against the three launches:
+// 16 places of 1 x 500 x 64 in bf16 3.1 / 8.7; 122 of 2 x 1443 x 752 8.3 / 11.0; 209 of 6 x 224 x 48 7.3 / 11.3; 777 of 3 x 1009 x 509 in fp32 23 / 17;
+// 1024 of 16 x 300 x 512 in bf16 30 / 21; 1 of 4 x 32000 x 64 (16 MB) 31 / 12.
+constexpr int kFewPlaces = 256, kFewRange = 256, kFewMany = 16;
+constexpr double kFewBytes = 8e6;
+template <typename T, int VEC, int U> __global__ void __launch_bounds__(256, 4) k_embed_few(const __grid_constant__ EmbedArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    constexpr int AHEAD = 8, EACH = kFewPlaces / 8;
+    __shared__ int s_at[8][kFewRange], s_from[kFewRange + 1], s_red[8];
+    __shared__ unsigned short s_place[kFewPlaces];
+    __shared__ float s_sum[8][32 * U * VEC];
+    const int i = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int first = (int)blockIdx.x * a.range, mine = (int)(a.V - first < a.range ? a.V - first : a.range);
+    const int c0 = (int)blockIdx.z * 32 * U * VEC + lane * VEC;
+    for (int q = threadIdx.x; q < 8 * kFewRange; q += 256) (&s_at[0][0])[q] = 0;
+    const Tokens tokens(a, i);
+    unsigned rel[EACH / 32];                             // rows of this lane's places, of the block's; beyond `mine`: none
+#pragma unroll
+    for (int u = 0; u < EACH / 32; ++u) {
+        const int t = warp * EACH + u * 32 + lane, v = t < a.n ? tokens.at(t) : -1;
+        rel[u] = v >= first ? (unsigned)(v - first) : 0xffffffffu;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < EACH / 32; ++u)
+        if (rel[u] < (unsigned)mine) atomicAdd(&s_at[warp][rel[u]], 1);
+    __syncthreads();
+    // where the places of row r go that warp w finds: behind those of the rows before and of the warps before
+    const int r = threadIdx.x;
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) total += s_at[w][r];
+    int upto = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    if (lane == 31) s_red[warp] = upto;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) before += w < warp ? s_red[w] : 0;
+    int at = before + upto - total;
+    s_from[r] = at;
+    if (r == kFewRange - 1) s_from[kFewRange] = at + total;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const int x = s_at[w][r];
+        s_at[w][r] = at;
+        at += x;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < EACH / 32; ++u) {
+        const bool in = rel[u] < (unsigned)mine;
+        const unsigned same = __match_any_sync(0xffffffffu, in ? rel[u] : 0xffffffffu);
+        const int rank = __popc(same & ((1u << lane) - 1));
+        int to = 0;
+        if (in) to = s_at[warp][rel[u]];
+        __syncwarp();
+        if (in) {
+            s_place[to + rank] = (unsigned short)(warp * EACH + u * 32 + lane);
+            if (rank == 0) s_at[warp][rel[u]] = to + __popc(same);
+        }
+        __syncwarp();
+    }
+    __syncthreads();
+    // sum over the places q0, q0 + step, ... below q1
+    auto add_up = [&](int q0, int q1, int step, float (&sum)[U][VEC]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[u][e] = 0.f;
+        for (int q = q0; q < q1; q += AHEAD * step) {
+            Raw<T, VEC> v[AHEAD][U];
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h) {
+                if (q + h * step >= q1) continue;
+                const T* from = row_of<T>(a.weight, i, s_place[q + h * step]) + c0;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c0 + u * 32 * VEC < a.d) v[h][u].load(from + u * 32 * VEC);
+            }
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h) {
+                if (q + h * step >= q1) continue;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c0 + u * 32 * VEC < a.d) v[h][u].add_to(sum[u]);
+            }
+        }
+    };
+    for (int q = warp; q < mine; q += 8) {
+        const int q0 = s_from[q], q1 = s_from[q + 1];
+        if (q1 - q0 > kFewMany || (q1 == q0 && a.accumulate)) continue;
+        float sum[U][VEC];
+        add_up(q0, q1, 1, sum);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * 32 * VEC;
+            if (c >= a.d) continue;
+            if (q1 > q0) finish<T, VEC>(a, i, first + q, c, sum[u]);
+            else store_vec<T, VEC>(row_of<T>(a.out, i, first + q) + c, sum[u]);
+        }
+    }
+    for (int q = 0; q < mine; ++q) {
+        const int q0 = s_from[q], q1 = s_from[q + 1];
+        if (q1 - q0 <= kFewMany) continue;
+        float sum[U][VEC];
+        add_up(q0 + warp, q1, 8, sum);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s_sum[warp][(u * 32 + lane) * VEC + e] = sum[u][e];
+        __syncthreads();
+        for (int x = threadIdx.x; x < 32 * U * VEC; x += 256) {
+            const int c = (int)blockIdx.z * 32 * U * VEC + x;
+            if (c >= a.d) continue;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) v += s_sum[w][x];
+            finish<T, 1>(a, i, first + q, c, &v);
+        }
+        __syncthreads();
+    }
+}
+
 // ----------------------------------------------------------------------------------- host
 Rows rows(const eg_matrix& m) { return Rows{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
 
@@ -484,12 +615,19 @@ template <typename T, int VEC> cudaError_t backward(EmbedArgs a, cudaStream_t st
         if (zeros < least) zeros = least;
         if (zeros > most) zeros = most;
     }
-    const bool early = a.n <= a.V;
-    a.sort_blocks = a.n > 0 ? (int)((a.V + a.range - 1) / a.range) : 0;
-    cudaError_t e = launch_after(k_embed_sort<T, VEC>, dim3((unsigned)(a.sort_blocks + (early ? zeros : 0)), a.P), dim3(kSortThreads), 0, stream, a);
-    if (e != cudaSuccess || a.n == 0) return e;
+    cudaError_t e;
     constexpr int U = VEC > 1 ? 1 : 4;
     const int slices = (a.d + 32 * U * VEC - 1) / (32 * U * VEC);
+    if (a.n > 0 && a.n <= kFewPlaces && (double)a.P * a.V * a.d * sizeof(T) <= kFewBytes) {
+        // rows of a block: as many as still leave four blocks for every multiprocessor
+        a.range = kFewRange;
+        while (a.range > 4 && (double)a.P * slices * ((a.V + a.range - 1) / a.range) < 4.0 * sm_count()) a.range /= 2;
+        return launch_after(k_embed_few<T, VEC, U>, dim3((unsigned)((a.V + a.range - 1) / a.range), a.P, slices), dim3(256), 0, stream, a);
+    }
+    const bool early = a.n <= a.V;
+    a.sort_blocks = a.n > 0 ? (int)((a.V + a.range - 1) / a.range) : 0;
+    e = launch_after(k_embed_sort<T, VEC>, dim3((unsigned)(a.sort_blocks + (early ? zeros : 0)), a.P), dim3(kSortThreads), 0, stream, a);
+    if (e != cudaSuccess || a.n == 0) return e;
     a.sum_blocks = (int)(((long long)a.chunks * slices + 7) / 8);
     e = launch_after(k_embed_sum<T, VEC, U>, dim3((unsigned)(a.sum_blocks + (early ? 0 : zeros)), a.P), dim3(256), 0, stream, a, slices);
     if (e != cudaSuccess || a.chunks == 1) return e;
