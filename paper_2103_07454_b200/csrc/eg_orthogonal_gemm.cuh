@@ -21,9 +21,7 @@
 //     rounding does.  X is nevertheless carried on in both parts: the term a X, which alone carries small singular values
 //     (485 times over in five steps), sees no rounding to 11 bits.  (One part throughout: error 15 % for a matrix of rank 1.)
 //     No product reads these lo parts: they lie as the epilogue's threads want them (see lane_place), once, and are updated in place.
-//   PARTS == 2 (results of 11 and 24 bits): hi hi + hi lo + lo hi.  lo lo, 2^-22 of a product, is left out.  The term a X comes out of the
-//     product too: a stands on the diagonal of S, which has the bits for it.  (Added by the epilogue it had to be fetched first, which the
-//     short tiles of 8 ResNet-18s waited for.)
+//   PARTS == 2 (results of 11 and 24 bits): hi hi + hi lo + lo hi.  lo lo, 2^-22 of a product, is left out.
 //
 // A and B are symmetric: only tiles of 256 x 256 on and below the diagonal are formed and stored.  An operand above it is read
 // from the box on the other side, as its transpose: the tensor cores take either order, step by step of K.
@@ -67,8 +65,7 @@ struct OrthoPass {
     int from;                                     // which X is read
     int first;                                    // X is still to be multiplied by `turn`
     int l, r, e0, e1, to;                         // symmetric matrices; apply: l
-    float f0, f1, fd;                             // gram: fd;  apply: f0 X + fd S X  (PARTS == 2: fd S X)
-    float diagonal;                               // sym, PARTS == 2: added to the diagonal
+    float f0, f1, fd;                             // gram: fd;  apply: f0 X + fd S X
     int read_lower, write_lower;                  // PARTS == 1, apply: whether X has lower parts, and needs them on
 };
 
@@ -162,7 +159,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
     using Shape = OrthoShape<PARTS>;
     constexpr int BN = Shape::kBN, S = Shape::kStages;
     constexpr bool SYMMETRIC = PASS < kApply;
-    constexpr int TERMS = PASS == kGram || PASS == kSym0 || (PARTS == 2 && PASS >= kApply) ? 0 : PASS == kSym2 ? 2 : 1;      // that come in from memory
+    constexpr int TERMS = PASS == kGram || PASS == kSym0 ? 0 : PASS == kSym2 ? 2 : 1;      // that come in from memory
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring_b = smem + S * Shape::kA;
@@ -503,13 +500,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 if constexpr (PASS == kGram || PASS >= kApply) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) sum[e] *= by;
-                }
-                if constexpr (PASS == kSym1 || PASS == kSym2) {
-                    const int x = lane + (quad & 1) * 32 - sub * 32;      // of these 32 columns, the row's own
-                    if (rbox == cbox) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) sum[e] += e == x ? pass.diagonal : 0.f;
-                    }
                 }
                 if (TERMS == 0 || PASS == kLast) {                // the box is free: its store has been read; both have read what it held
                     if (sub == 0) store_wait_read<0>();

@@ -477,11 +477,7 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
     bool any_velocity = false, kept = false;
     for (int i = 0; i < a.count; ++i) any_velocity = any_velocity || a.mat[i].velocity.p;
     for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
-        const double *c0 = s.c[k], sa = s.sa;
-        // (polynomials that make small values smaller: their products of two steps would sink below the boxes' last bit, 2^-39)
-        const bool two = PARTS == 2 && k + 1 < q->steps && fabs(c0[0]) >= 1.0 && fabs(s.c[k + 1][0]) >= 1.0;
-        const bool last_sym = PARTS == 2 && !two;         // B0 is applied, with a on its diagonal
-        const double sb0 = last_sym ? power_below((s.most[k] + fabs(c0[0])) * 1.02) : s.sb[k];
+        const double *c0 = s.c[k], sa = s.sa, sb0 = s.sb[k];
         OrthoPass p{};
         p.from = from;
         p.first = k == 0;
@@ -494,16 +490,16 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
             p.f0 = (float)f0; p.f1 = (float)f1; p.fd = (float)fd;
         };
         // B0 = b A + c A^2
-        p.diagonal = last_sym ? (float)(c0[0] * sb0) : 0.f;
         sym(0, 0, 0, 0, 1, c0[1] * sb0 / sa, 0, c0[2] * sb0 / (sa * sa));
         if (e == cudaSuccess) e = product<float, PARTS, kSym1>(a, p, stream);
         double outer = c0[0], scale = sb0;
         p.l = 1;
         ++k;
         if constexpr (PARTS == 2) {
-            if (two) {
+            // (polynomials that make small values smaller: their products of two steps would sink below the boxes' last bit, 2^-39)
+            if (k < q->steps && fabs(c0[0]) >= 1.0 && fabs(s.c[k][0]) >= 1.0) {
                 const double *c1 = s.c[k], sb1 = s.sb[k], sc = s.sc[k - 1];
-                const double sr = power_below((fabs(c0[0]) + s.most[k - 1]) * (fabs(c1[0]) + s.most[k]) * 1.02);
+                const double bound = fabs(c1[0]) * s.most[k - 1] + fabs(c0[0]) * s.most[k] + s.most[k - 1] * s.most[k], sr = power_below(bound * 1.02);
                 // C = A B0
                 sym(0, 1, 0, 0, 2, 0, 0, sc / (sa * sb0));
                 if (e == cudaSuccess) e = product<float, PARTS, kSym0>(a, p, stream);
@@ -513,8 +509,7 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
                 // B1 = b A1 + c A1^2, in C's place
                 sym(0, 0, 0, 0, 2, c1[1] * sb1 / sa, 0, c1[2] * sb1 / (sa * sa));
                 if (e == cudaSuccess) e = product<float, PARTS, kSym1>(a, p, stream);
-                // a0 a1 + a1 B0 + a0 B1 + B1 B0, in A1's place
-                p.diagonal = (float)(c0[0] * c1[0] * sr);
+                // a1 B0 + a0 B1 + B1 B0, in A1's place
                 sym(2, 1, 1, 2, 0, c1[0] * sr / sb0, c0[0] * sr / sb1, sr / (sb1 * sb0));
                 if (e == cudaSuccess) e = product<float, PARTS, kSym2>(a, p, stream);
                 outer = c0[0] * c1[0];

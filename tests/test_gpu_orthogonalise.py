@@ -51,14 +51,13 @@ def limit(dtype, steps=5, few=False):
     polynomial between steps (1.1 at most from 0.7 to 1, 3.9 at its very end).
 
     `few`: the weight lies in few directions, and what roundings leave in the others grows 3.4445 times a step.  The gradient's own
-    (2^-24 of an element) grows 484 times.  Two steps in one multiply X by a matrix with 11.9 (a0 a1) on its diagonal, of which the rest
-    takes most away where the weight is: that entry's rounding (2^-23 / sqrt(3) of it), the products' and three sums' (2^-24 of 11.9 of an element
-    each), 11.9 * sqrt(2^2 / 3 + 4) * 2^-24, which grow 41 times after the first two steps and 3.4 times after the next two.  (Results of 8 bits
-    carry X through the steps in 22 bits: below their own rounding.)"""
+    (2^-24 of an element) grows 484 times.  Two steps in one add 11.9 X (a0 a1) and a product that takes most of it away where the weight is: three
+    roundings of 2^-24 of 11.9 of an element, sqrt(3) * 11.9, which grow 41 times after the first two steps and 3.4 times after the
+    next two.  (Results of 8 bits carry X through the steps in 22 bits: below their own rounding.)"""
     if dtype == "bf16":
         return 2 * math.sqrt(10 * steps) * 2.0 ** -11 / math.sqrt(3) + 2.0 ** -9
     own = {"fp32": 2.0 ** -25, "fp16": 2.0 ** -12}[dtype]
-    return steps * 10 * 8 * 2.0 ** -25 + 2 * math.sqrt(10 * steps) * 2.0 ** -22 / math.sqrt(3) + ((484 + math.sqrt(16 / 3) * 11.9 * (41 + 3.4)) * 2.0 ** -24 if few else 0.0) + own
+    return steps * 10 * 8 * 2.0 ** -25 + 2 * math.sqrt(10 * steps) * 2.0 ** -22 / math.sqrt(3) + ((484 + math.sqrt(3) * 11.9 * (41 + 3.4)) * 2.0 ** -24 if few else 0.0) + own
 
 
 SIZES = [(1, 1), (1, 7), (10, 32), (64, 64), (64, 784), (65, 63), (27, 64), (128, 128), (129, 257), (300, 200), (256, 576), (520, 515), (1000, 70), (3, 5000),
