@@ -44,7 +44,7 @@ def limit(dtype, steps=5, few=False):
     """Of |error| / |result|, in the Frobenius norm.
 
     A product is off by what its operands were rounded by (22 bits: 2^-22 / sqrt(3) in the mean with what is left out; 11 bits:
-    2^-11 / sqrt(3) of both) and, in full precision, by the accumulator's truncation: 2^-25 for each of the 8 additions between two
+    2^-11 / sqrt(3) of both) and, in full precision, by the accumulator's truncation: 2^-25 for each of the 16 additions between two
     hand-overs to registers, all towards zero.  With x a square of a singular value, an error d of all three products of a step
     changes its result by up to d (|b| x + 3 c x^2 + |b x + c x^2|): 10 d at x = 0.8, where the values settle.  The truncations of five steps
     may add up; roundings have random signs: sqrt(10) instead of 10, sqrt(steps) instead of steps, times 2 for the slope of the
@@ -57,7 +57,7 @@ def limit(dtype, steps=5, few=False):
     if dtype == "bf16":
         return 2 * math.sqrt(10 * steps) * 2.0 ** -11 / math.sqrt(3) + 2.0 ** -9
     own = {"fp32": 2.0 ** -25, "fp16": 2.0 ** -12}[dtype]
-    return steps * 10 * 8 * 2.0 ** -25 + 2 * math.sqrt(10 * steps) * 2.0 ** -22 / math.sqrt(3) + ((484 + math.sqrt(3) * 11.9 * (41 + 3.4)) * 2.0 ** -24 if few else 0.0) + own
+    return steps * 10 * 16 * 2.0 ** -25 + 2 * math.sqrt(10 * steps) * 2.0 ** -22 / math.sqrt(3) + ((484 + math.sqrt(3) * 11.9 * (41 + 3.4)) * 2.0 ** -24 if few else 0.0) + own
 
 
 SIZES = [(1, 1), (1, 7), (10, 32), (64, 64), (64, 784), (65, 63), (27, 64), (128, 128), (129, 257), (300, 200), (256, 576), (520, 515), (1000, 70), (3, 5000),
