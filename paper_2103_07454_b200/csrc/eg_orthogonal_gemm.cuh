@@ -6,9 +6,10 @@
 //   apply    X <- a X + S X                  (the last one: into the caller's matrix)
 // One step is gram, B = b A + c A^2, apply with B.  Where products are of full precision, two steps share one gram and one apply, since
 // the second step's gram is known from the first one's:  Q0 = a0 + B0,  A1 = Q0 A Q0 = a0^2 A + 2 a0 C + C B0 with C = A B0,
-// Q1 Q0 = a0 a1 + (a1 B0 + a0 B1 + B1 B0).  Five symmetric products of m^3 take the place of 3 m^2 n + 2 m^3: never more work, and 40 % less
-// where n = 9 m (8 ResNet-18s: 3.5 -> 2.4 ms).  With operands of 11 bits the second step would see three times the
-// error, and two steps stay two.
+// Q1 Q0 = a0 a1 + (a1 B0 + a0 B1 + B1 B0).  Five symmetric products of m^3 take the place of 3 m^2 n + 2 m^3 (8 ResNet-18s: 3.1 -> 2.35 ms).
+// The terms that cancel cost accuracy (2.9e-6, step by step 1.7e-6; with a on the diagonals of Q0 and Q1 6e-6, since the accumulators truncate
+// what stands beside it), so that two steps stay two where they save little.  With operands of 11 bits the second step would see three times
+// the error: there they always do.
 //
 // Everything in between lies in the workspace as fp16 boxes of 64 x 64, each 8 KB in one piece and already in the order that the
 // tensor cores want in shared memory (128-byte swizzle): one tensor map serves all matrices of any size, a copy is a whole box,
@@ -28,7 +29,7 @@
 //
 // Tiles and barriers are those of eg_gemm.cuh: pairs of CTAs share a tile of 256 x BN, tcgen05.mma by one thread, the
 // accumulators of two tiles in tensor memory.  PARTS == 2: BN = 128, an accumulator for hi hi that moves to registers every
-// kOrthoChunk steps (adding into it truncates) and one for the smaller products.  Sixteen warps take the results: a result is
+// one to four steps (ortho_chunk: adding into it truncates) and one for the smaller products.  Sixteen warps take the results: a result is
 // added to what was there, split and written again, which is latency upon latency, and eight warps took 11700 cycles for a tile whose products take
 // 8200 (m = 1024).
 #pragma once
@@ -38,12 +39,14 @@ namespace eg {
 
 constexpr int kBox = 64, kBoxBytes = 8192;
 constexpr int kOrthoMats = 48;                    // matrices of one launch
-// Steps of 64 between two hand-overs.  The products run two hand-overs ahead of the warps that take them: with 2 steps they waited for
-// those in every short tile (8 ResNet-18s 2.53 ms, 2.28 with 4; errors of the results 3.2e-6 and 5.0e-6 in the mean).
-constexpr int kOrthoChunk = 4;
 constexpr int kOrthoEpiWarps = 16, kOrthoThreads = 128 + 32 * kOrthoEpiWarps;
 // kSym0, kSym1, kSym2: with so many terms E.
 enum { kGram = 0, kSym0 = 1, kSym1 = 2, kSym2 = 3, kApply = 4, kLast = 5 };
+// Steps of 64 between two hand-overs.  The products run two hand-overs ahead of the warps that take them: with 2 steps they waited for
+// those in every short tile, with 1 in every tile (8 ResNet-18s: all products with 4 2.32 ms, with 2 2.5, with 1 2.98).  Products of symmetric
+// matrices are short and few, and what they truncate is what the result is off by (error 5.0e-6 with 4 for all, 2.9e-6 with 2 for these, 2.5e-6
+// with 1 for all; one 128 x 1152: 3.0e-6 with 2, 1.9e-6 with 1).
+template <int PASS> __device__ __forceinline__ int ortho_chunk(int ksteps) { return PASS == kGram || PASS >= kApply ? 4 : ksteps > 2 ? 2 : 1; }
 
 struct Strided {
     void* p;
@@ -312,7 +315,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                     tc_commit_pair(&empty[s]);
                     if (++s == S) { s = 0; ++round; }
                     if (k == 0 && t + pairs < tiles) upcoming = ortho_pos<PARTS, PASS>(a, walk, t + pairs);
-                    if (PARTS == 2 && k + 1 < ksteps && (k + 1) % kOrthoChunk == 0) {
+                    if (PARTS == 2 && k + 1 < ksteps && (k + 1) % ortho_chunk<PASS>(ksteps) == 0) {
                         tc_commit_pair(&acc_full[count & 1]);
                         ++count;
                         add = 0;
@@ -490,7 +493,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                     tc_fence_before();
                     __syncwarp();
                 };
-                for (int z = 0; z < (ksteps + kOrthoChunk - 1) / kOrthoChunk; ++z, ++count) {
+                const int chunk = ortho_chunk<PASS>(ksteps);
+                for (int z = 0; z < (ksteps + chunk - 1) / chunk; ++z, ++count) {
                     mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
                     take(tmem + (count & 1) * BN);
                     if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));

@@ -211,6 +211,20 @@ def test_steps_and_coefficients(steps, coefficients, dtype):
         assert float((out.double() @ out.double().mT - torch.eye(130, device="cuda")).abs().max()) < (1e-4 if dtype == "fp32" else 0.05)
 
 
+@pytest.mark.parametrize("kind,dtype,steps,coefficients", [
+    ("noise", "fp32", 5, None), ("fall", "fp32", 5, None), ("rank", "fp32", 5, None), ("noise", "fp16", 5, None), ("rank", "fp16", 5, None),
+    ("noise", "fp32", 2, None), ("noise", "fp32", 8, None), ("noise", "fp32", 6, CUBIC),
+    ("noise", "fp32", 3, [(4.0, -6.0, 2.9), (3.0, -3.5, 1.5), (1.875, -1.25, 0.375)]), ("noise", "fp32", 2, [(0.5, 1.0, 0.0), (3.0, -3.5, 1.5)])])
+def test_two_steps_in_one(kind, dtype, steps, coefficients):
+    """Of wide matrices with work for it, small ones among them: P m^2 (n - 2 m) is 2.3e9."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    grads = [matrix(*size, kind, gen).to(TYPES[dtype]) for size in ((640, 4100), (33, 70), (300, 129))]
+    per = coefficients if isinstance(coefficients, list) else [coefficients or DEFAULT] * steps
+    for g, o in zip(grads, B.orthogonalise(grads, out=[torch.empty_like(g) for g in grads], steps=steps, coefficients=coefficients)):
+        assert far(o, exact(g, coefficients=per)) < limit(dtype, steps=max(steps, 5), few=kind != "noise")
+    assert B.operator_status() == 0
+
+
 def test_matrices_that_share_no_launches():
     """More than one group: by number, and by memory."""
     grads, _ = make([(16, 24)] * 100, "bf16", P=1, velocity=False)
