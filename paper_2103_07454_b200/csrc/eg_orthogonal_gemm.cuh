@@ -21,6 +21,9 @@
 //   PARTS == 1 (results of 8 bits): the products take hi alone, which costs 2^-12 of a value each, about what the result's own
 //     rounding does.  X is nevertheless carried on in both parts: the term a X, which alone carries small singular values
 //     (485 times over in five steps), sees no rounding to 11 bits.  (One part throughout: error 15 % for a matrix of rank 1.)
+//     The diagonals of A and B, far larger than what stands beside them, keep what they were rounded by as a float a row, rest_A and
+//     rest_B, which the epilogues put back: (H + D)^2 = H^2 + D H + H D + D^2, and a + rest_B is what X's row is multiplied by.
+//     (Errors of 6 steps of 64 x 784 before the result's rounding 2.5e-3 without, 1.5e-3 with; 134 -> 139 us there, 4.95 -> 5.0 ms in large ones.)
 //     No product reads these lo parts: they lie as the epilogue's threads want them (see lane_place), once, and are updated in place.
 //   PARTS == 2 (results of 11 and 24 bits): hi hi + hi lo + lo hi.  lo lo, 2^-22 of a product, is left out.
 //
@@ -61,6 +64,7 @@ struct OrthoMat {
     float scale;
     long long x[2], lo[2], s[3];                  // first boxes of replica 0: X before and after a step, its lo parts, symmetric matrices
     long long x_rep, s_rep;                       // boxes from one replica to the next; lo parts of symmetric matrices lie half as far
+    long long rest, rest_rep;                     // PARTS == 1: boxes with what A's and B's diagonals were rounded by, rb * 64 floats each
     Strided grad, out, velocity, velocity_out;
     int items, begin;                             // of k_ortho_norm and k_ortho_in: items of an instance, the first one of replica 0
 };
@@ -152,6 +156,17 @@ __device__ __forceinline__ void add_piece(float* r, float f, const uint4& v) {
         const float2 h = unpack2<__half>(w[z]);
         r[2 * z] = fmaf(f, h.x, r[2 * z]);
         r[2 * z + 1] = fmaf(f, h.y, r[2 * z + 1]);
+    }
+}
+
+// The same, each with a factor of its own: f + fd rests.
+__device__ __forceinline__ void add_piece(float* r, float f, float fd, const float* rests, const uint4& v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+        const float2 h = unpack2<__half>(w[z]);
+        r[2 * z] = fmaf(fmaf(fd, rests[2 * z], f), h.x, r[2 * z]);
+        r[2 * z + 1] = fmaf(fmaf(fd, rests[2 * z + 1], f), h.y, r[2 * z + 1]);
     }
 }
 
@@ -353,12 +368,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 unsigned char* box = epi + w * 4096;
                 uint4 low[PASS >= kApply ? 8 : 1];
                 unsigned char* const low_at = PASS >= kApply ? place(g.lo[0] + q.p * g.x_rep) + lane * 16 : nullptr;
+                float* const rest_a = reinterpret_cast<float*>(a.ws + (g.rest + q.p * g.rest_rep) * kBoxBytes);
+                float* const rest_b = rest_a + g.rb * kBox;
+                const bool diagonal = SYMMETRIC && rbox == cbox;
+                float rest = 0.f, own = 0.f;                      // of this thread's row: what is put back; its value on the diagonal
                 if (inside && TERMS > 0) {                        // what the result is added to comes in under the products
                     store_wait_read<0>();
                     __syncwarp();
                     if (elect_one()) {
                         op_mbar_expect(&epi_full[w], 4096);
                         op_bulk_load(box, place(SYMMETRIC ? g.s[pass.e0] + q.p * g.s_rep : x), 4096, &epi_full[w]);
+                    }
+                    rest = (SYMMETRIC ? rest_a : rest_b)[row0 + lane];
+                    if constexpr (PASS == kSym1) {
+                        if (lane < 2) asm volatile("prefetch.global.L1 [%0];" ::"l"(rest_a + cbox * kBox + lane * 32));
                     }
                     if constexpr (PASS >= kApply) {
 #pragma unroll
@@ -368,6 +391,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
                 tc_fence_after();
                 const uint32_t acc = tmem + (count & 1) * BN + lanes + group * 64;
+                const float f0 = fmaf(pass.fd, rest, pass.f0);
                 if (inside) {
                     if (TERMS == 0) {
                         store_wait_read<0>();
@@ -387,11 +411,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                             float r[8];
 #pragma unroll
                             for (int z = 0; z < 8; ++z) r[z] = pass.fd * __uint_as_float(d[e + z]);
-                            if constexpr (TERMS > 0) add_piece(r, pass.f0, *reinterpret_cast<const uint4*>(at));
-                            if constexpr (PASS >= kApply) add_piece(r, pass.f0, low[piece]);
+                            if constexpr (PASS == kSym1) {
+                                float rests[8];
+                                *reinterpret_cast<float4*>(rests) = *reinterpret_cast<const float4*>(rest_a + cbox * kBox + x0 + e);
+                                *reinterpret_cast<float4*>(rests + 4) = *reinterpret_cast<const float4*>(rest_a + cbox * kBox + x0 + e + 4);
+                                add_piece(r, f0, pass.fd, rests, *reinterpret_cast<const uint4*>(at));
+                            } else if constexpr (TERMS > 0) {
+                                add_piece(r, f0, *reinterpret_cast<const uint4*>(at));
+                            }
+                            if constexpr (PASS >= kApply) add_piece(r, f0, low[piece]);
                             if constexpr (PASS == kGram || PASS >= kApply) {
 #pragma unroll
                                 for (int z = 0; z < 8; ++z) r[z] *= by;
+                            }
+                            if (diagonal) {
+#pragma unroll
+                                for (int z = 0; z < 8; ++z) {
+                                    if (x0 + e + z != (quad & 1) * 32 + lane) continue;
+                                    if constexpr (PASS == kSym1) r[z] = fmaf(fmaf(pass.fd, rest, pass.f0), rest, r[z]);
+                                    own = r[z];
+                                }
                             }
                             uint32_t hw[4], lw[4];
 #pragma unroll
@@ -410,6 +449,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
                 ++count;
                 if (!inside) continue;
+                if (diagonal) (PASS == kGram ? rest_a : rest_b)[row0 + lane] = own - __half2float(__float2half_rn(own));
                 if constexpr (PASS != kLast) {
                     fence_async_shared();
                     __syncwarp();

@@ -341,7 +341,7 @@ struct Sides {
 Sides sides(const eg_orthogonalise_args* q, const eg_orthogonal_matrix& m) {
     const int64_t r = m.rows <= m.columns ? m.rows : m.columns, c = m.rows <= m.columns ? m.columns : m.rows;
     Sides s{up(r, kBox) / kBox, up(c, kBox) / kBox, 0};
-    s.boxes = parts_of(q) == 2 ? 4 * s.rb * s.cb + 6 * s.rb * s.rb : 3 * s.rb * s.cb + 2 * s.rb * s.rb;
+    s.boxes = parts_of(q) == 2 ? 4 * s.rb * s.cb + 6 * s.rb * s.rb : 3 * s.rb * s.cb + 2 * s.rb * s.rb + (s.rb + 15) / 16;
     return s;
 }
 // Matrices [first, *end) share their launches.  Returns their boxes.
@@ -413,13 +413,15 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
         m->first = (int)(i * q->P);
         m->scale = (float)s.scale;
         const int64_t plane = z.rb * z.cb, square = z.rb * z.rb;
-        // hi and lo of X twice and of three symmetric matrices; or hi of X twice, lo of X, hi of two
+        // hi and lo of X twice and of three symmetric matrices; or hi of X twice, lo of X, hi of two and what their diagonals were rounded by
         m->x_rep = parts * plane; m->s_rep = parts * square;
         m->x[0] = at;
         m->x[1] = at + q->P * parts * plane;
         m->lo[0] = parts == 2 ? m->x[0] + plane : at + q->P * 2 * plane;
         m->lo[1] = parts == 2 ? m->x[1] + plane : m->lo[0];
         for (int k = 0; k < 3; ++k) m->s[k] = at + q->P * (parts == 2 ? 4 * plane + 2 * square * k : 3 * plane + square * (k & 1));
+        m->rest = at + q->P * (3 * plane + 2 * square);
+        m->rest_rep = (z.rb + 15) / 16;
         at += q->P * z.boxes;
         m->grad = strided(s.grad); m->out = strided(s.out); m->velocity = strided(s.velocity);
         m->velocity_out = s.velocity_out.data ? strided(s.velocity_out) : m->velocity;
