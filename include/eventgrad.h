@@ -489,7 +489,7 @@ eg_status eg_head_norm_backward(const eg_head_norm_args* args, void* workspace, 
 /* Orthogonal updates: for every matrix of every replica, with g its gradient and v its velocity (fp32),
  *     v' = momentum * v + g,      u = g + momentum * v' with `nesterov`, else v'       (no velocity: u = g)
  *     X = u / |u| (the root of the sum of its squares),   transposed where it has more rows than columns
- *     `steps` times:  X <- a X + (b A + c A^2) X,  A = X X^T
+ *     `steps` times (1 to 64):  X <- a X + (b A + c A^2) X,  A = X X^T
  *     out = scale * X (transposed back).
  * The polynomial pulls the singular values of X towards 1 and leaves its singular vectors: out is, roughly, the orthogonal
  * matrix next to u.  coefficients: a, b, c of every step (steps x 3, host), NULL: 3.4445, -4.7750, 2.0315 in each.  They may not
@@ -501,10 +501,10 @@ eg_status eg_head_norm_backward(const eg_head_norm_args* args, void* workspace, 
  * accuracy goes by out_dtype: bf16 results come from products whose operands are rounded to 11 bits (their error is about that of the
  * result's own rounding), fp16 and fp32 ones from operands of 22 bits; sums are fp32, the norm's fp64.
  * Any number of matrices of any sizes up to 2^20 share a call; `matrices` and `coefficients` are read before it returns.
- * `workspace` (device, 128-byte aligned) holds at least eg_orthogonalise_workspace(args) bytes (some 8 to 16 for every value,
- * of up to 1 GB of matrices at a time) and is free for reuse once the stream has passed the call.
+ * `workspace` (device, 128-byte aligned) holds at least eg_orthogonalise_workspace(args) bytes (6 to 20 for every value, of
+ * up to 1 GB of them at a time) and is free for reuse once the stream has passed the call.
  * The call only enqueues work on `stream` of the current device, holds no state and may be recorded into a graph; the results do
- * not depend on the run.  Outputs must not overlap inputs or each other except as said; rows and replicas of an output that fall on
+ * not depend on the run (fp16 and fp32 ones, in their rounding, on how much work shares the call).  Outputs must not overlap inputs or each other except as said; rows and replicas of an output that fall on
  * one another are refused.  Errors: EG_ERR_INVALID, EG_ERR_CUDA. */
 typedef struct {
     int64_t rows, columns;

@@ -73,14 +73,17 @@ __device__ __forceinline__ bool quads(const OrthoMat& m, size_t size) {
 
 // Walks over the boxes of an item, those of the gradient's rows of boxes one after another; a thread holds four quads of a box: rows
 // 16 z + first, columns 4 * quad.  FORM: with the velocity before, otherwise with the one after the update.
-template <typename T, bool FORM> struct Boxes {
+// VEL: some matrices of the launch have a velocity.  Without, a thread's registers hold more boxes on their way: of 138 M 16-bit
+// values the norm took 135 us with one box (16 KB a multiprocessor) ahead, 77 with four, the boxes 234 and 168.
+template <typename T, bool FORM, bool VEL> struct Boxes {
+    static constexpr int kSlots = VEL ? 2 : sizeof(T) == 2 ? 5 : 3;
     const OrthoArgs& a;
     const OrthoMat& m;
     int p, b, quad, first, rows, cols, wide, box0, box1;
     bool vec, need_g;
     Strided v;
-    Quad<T> g[2][4];
-    Quad<float> w[2][4];
+    Quad<T> g[kSlots][4];
+    Quad<float> w[VEL ? kSlots : 1][4];
 
     __device__ __forceinline__ Boxes(const OrthoArgs& args, int k, int item)
         : a(args), m(args.mat[k]), p((item - m.begin) / m.items), b(item - m.begin - p * m.items), quad(threadIdx.x & 15), first(threadIdx.x >> 4) {
@@ -92,7 +95,7 @@ template <typename T, bool FORM> struct Boxes {
         box1 = (int)(boxes * (b + 1) / m.items);
         vec = quads(m, sizeof(T));
         v = FORM ? m.velocity : m.velocity_out;
-        need_g = FORM || !v.p || a.nesterov;
+        need_g = !VEL || FORM || !v.p || a.nesterov;
     }
     __device__ __forceinline__ void fetch(int box, int slot) {
         const int grow = box / wide, c = (box - grow * wide) * kBox + quad * 4, n = cols - c;
@@ -103,7 +106,25 @@ template <typename T, bool FORM> struct Boxes {
         for (int z = 0; z < 4; ++z) {
             const int have = r + z * 16 < rows ? n : 0;
             if (need_g) g[slot][z].load(from + z * 16 * m.grad.row, have, vec);
-            if (v.p) w[slot][z].load(speed + z * 16 * v.row, have, vec);
+            if constexpr (VEL) {
+                if (v.p) w[slot][z].load(speed + z * 16 * v.row, have, vec);
+            }
+        }
+    }
+    // work(box, slot) for each, with the next ones on their way
+    __device__ __forceinline__ void start() {
+#pragma unroll
+        for (int q = 0; q < kSlots - 1; ++q)
+            if (box0 + q < box1) fetch(box0 + q, q);
+    }
+    template <typename F> __device__ __forceinline__ void walk(F work) {
+        for (int box = box0; box < box1; box += kSlots) {
+#pragma unroll
+            for (int q = 0; q < kSlots; ++q) {
+                if (box + q >= box1) break;
+                if (box + q + kSlots - 1 < box1) fetch(box + q + kSlots - 1, (q + kSlots - 1) % kSlots);
+                work(box + q, q);
+            }
         }
     }
     // u, four quads of it; FORM: stores the velocity.
@@ -113,9 +134,9 @@ template <typename T, bool FORM> struct Boxes {
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
             if (need_g) g[slot][z].values(u[z]);
-            if (!v.p) continue;
+            if (!VEL || !v.p) continue;
             float s[4];
-            w[slot][z].values(s);
+            w[VEL ? slot : 0][z].values(s);
             if (FORM) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[e] = fmaf(a.momentum, s[e], u[z][e]);
@@ -142,29 +163,25 @@ __device__ __forceinline__ int matrix_of(const OrthoArgs& a, int item) {
     return k;
 }
 
-// The two kernels before the products read the same values; both are bound by memory, the next box on its way while one is worked on.
+// The two kernels before the products read the same values; both are bound by memory, the next boxes on their way while one is worked on
+// (4 x 2048 x 5504 three times, bf16 with a velocity: 235 and 272 us, 5.7 and 5.0 TB/s).
 // Tried: both phases in one launch, the second a few hundred items behind the first so that it reads from the L2: 549 us against 502 for 8 x
 // 2048 x 5504 with a velocity (an instance's 68 MB and what passes by do not stay there).
-template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_norm(const __grid_constant__ OrthoArgs a) {
+template <typename T, bool VEL> __global__ void __launch_bounds__(kThreads, 2) k_ortho_norm(const __grid_constant__ OrthoArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ double s_sum[kThreads / 32];
-    Boxes<T, true> x(a, matrix_of(a, blockIdx.x), blockIdx.x);
+    Boxes<T, true, VEL> x(a, matrix_of(a, blockIdx.x), blockIdx.x);
     double sum = 0.0;
-    x.fetch(x.box0, 0);
-    auto work = [&](int box, int slot) {
-        if (box + 1 < x.box1) x.fetch(box + 1, slot ^ 1);
+    x.start();
+    x.walk([&](int box, int slot) {
         float u[4][4];
         x.update(box, slot, u);
 #pragma unroll
         for (int z = 0; z < 4; ++z)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum = fma((double)u[z][e], (double)u[z][e], sum);
-    };
-    for (int box = x.box0; box < x.box1; box += 2) {
-        work(box, 0);
-        if (box + 1 < x.box1) work(box + 1, 1);
-    }
+    });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
@@ -175,15 +192,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_nor
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(const __grid_constant__ OrthoArgs a) {
+template <typename T, bool VEL> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(const __grid_constant__ OrthoArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ double s_sum[kThreads / 32];
     __shared__ float s_box[kBox][kBox + 1];
-    Boxes<T, false> x(a, matrix_of(a, blockIdx.x), blockIdx.x);
+    Boxes<T, false, VEL> x(a, matrix_of(a, blockIdx.x), blockIdx.x);
     const OrthoMat& m = x.m;
     const int instance = m.first + x.p;
-    x.fetch(x.box0, 0);
+    x.start();
     static_assert(kMaxItems <= kThreads, "one partial sum a thread");
     double s = (int)threadIdx.x < m.items ? a.partial[(long long)instance * kMaxItems + threadIdx.x] : 0.0;
 #pragma unroll
@@ -202,8 +219,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(
     const float by0 = (float)ldexp(1.0, -ex / 2), by1 = (float)ldexp((double)a.sx, -ex + ex / 2);
     if (x.b == 0 && threadIdx.x == 0)
         a.turn[instance] = !finite ? __int_as_float(0x7fffffff) : fraction > 0.0 ? (float)(1.0 / fraction) : 0.f;
-    auto work = [&](int box, int slot) {
-        if (box + 1 < x.box1) x.fetch(box + 1, slot ^ 1);
+    x.walk([&](int box, int slot) {
         float u[4][4];
         x.update(box, slot, u);
 #pragma unroll
@@ -235,13 +251,10 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_ortho_in(
             split_half2(u[z][2], u[z][3], h1, l1);
             const uint32_t off = swz128((z * 16 + x.first) * 128 + x.quad * 8);
             *reinterpret_cast<uint2*>(hi + off) = make_uint2(h0, h1);
-            *reinterpret_cast<uint2*>(lo + (a.parts == 1 ? lane_place(z * 16 + x.first, x.quad * 4) : off)) = make_uint2(l0, l1);
+            // (a gradient of 8 bits has no lower part)
+            if (VEL || sizeof(T) == 4 || a.parts == 2) *reinterpret_cast<uint2*>(lo + (a.parts == 1 ? lane_place(z * 16 + x.first, x.quad * 4) : off)) = make_uint2(l0, l1);
         }
-    };
-    for (int box = x.box0; box < x.box1; box += 2) {
-        work(box, 0);
-        if (box + 1 < x.box1) work(box + 1, 1);
-    }
+    });
 }
 
 // ----------------------------------------------------------------------------------- host
@@ -470,19 +483,23 @@ template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_or
     constexpr int PARTS = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 2;
     a.sx = s.sx;
     a.out = 1.f / s.sx;
-    auto given = [&](auto value) {
-        const cudaError_t e = launch_after(k_ortho_norm<decltype(value)>, dim3(a.items), dim3(kThreads), 0, stream, a);
-        return e != cudaSuccess ? e : launch_after(k_ortho_in<decltype(value)>, dim3(a.items), dim3(kThreads), 0, stream, a);
-    };
-    cudaError_t e = q->dtype == EG_F32 ? given(0.f) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}) : given(__half{});
-    int from = 0;
-    bool any_velocity = false, kept = false;
+    bool any_velocity = false;
     double saved = 0;
     for (int i = 0; i < a.count; ++i) {
         any_velocity = any_velocity || a.mat[i].velocity.p;
         saved += (double)q->P * a.mat[i].m * a.mat[i].m * (a.mat[i].n - 2.0 * a.mat[i].m);
     }
     [[maybe_unused]] const bool pairs = saved >= 0x1p31;
+    auto given = [&](auto value, auto vel) {
+        using G = decltype(value);
+        constexpr bool VEL = decltype(vel)::value;
+        const cudaError_t e = launch_after(k_ortho_norm<G, VEL>, dim3(a.items), dim3(kThreads), 0, stream, a);
+        return e != cudaSuccess ? e : launch_after(k_ortho_in<G, VEL>, dim3(a.items), dim3(kThreads), 0, stream, a);
+    };
+    auto of_type = [&](auto vel) { return q->dtype == EG_F32 ? given(0.f, vel) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}, vel) : given(__half{}, vel); };
+    cudaError_t e = any_velocity ? of_type(std::true_type{}) : of_type(std::false_type{});
+    int from = 0;
+    bool kept = false;
     for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
         const double *c0 = s.c[k], sa = s.sa, sb0 = s.sb[k];
         OrthoPass p{};
