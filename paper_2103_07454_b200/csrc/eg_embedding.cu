@@ -19,6 +19,8 @@
 // there are fewer places than rows (the sort, 10 to 30 us of latencies, is then for nothing), beside the sums, for the rows
 // without a place, where there are more.
 //   3. k_embed_join: adds the partial sums of such runs, in order.
+// Measured, bf16: 8 x 1024 places of 32000 x 1024: forward 11 us (launch and latency), sort and zeros 75 us (524 MB, 7 TB/s), sums 17, joins 7;
+// 4 x 16384 places of 32000 x 2048: forward 63 us, sort and zeros 101, sums 91, joins 23.
 #include "eg_ops.cuh"
 
 namespace eg {
