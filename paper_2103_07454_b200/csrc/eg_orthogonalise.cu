@@ -345,23 +345,30 @@ bool valid(const eg_orthogonalise_args* q, Scales* s) {
     return true;
 }
 
-int parts_of(const eg_orthogonalise_args* q) { return q->out_dtype == EG_BF16 ? 1 : 2; }
+// Parts of an operand.  Results of 8 bits take two where a matrix is longer than 2^18: with one, a product's sum stays in the accumulator, which
+// truncates (64 x 2^18: error 2.3e-3 with one; 64 x 2^20: 5.7e-3, 1.7e-3 with two; 24 and 26 ms).
+int parts_of(const eg_orthogonalise_args* q) {
+    if (q->out_dtype != EG_BF16) return 2;
+    for (int64_t i = 0; i < q->count; ++i)
+        if (q->matrices[i].rows > (1 << 18) || q->matrices[i].columns > (1 << 18)) return 2;
+    return 1;
+}
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Sides {
     int64_t rb, cb, boxes;                                // boxes: of one replica
 };
-Sides sides(const eg_orthogonalise_args* q, const eg_orthogonal_matrix& m) {
+Sides sides(int parts, const eg_orthogonal_matrix& m) {
     const int64_t r = m.rows <= m.columns ? m.rows : m.columns, c = m.rows <= m.columns ? m.columns : m.rows;
     Sides s{up(r, kBox) / kBox, up(c, kBox) / kBox, 0};
-    s.boxes = parts_of(q) == 2 ? 4 * s.rb * s.cb + 6 * s.rb * s.rb : 3 * s.rb * s.cb + 2 * s.rb * s.rb + (s.rb + 15) / 16;
+    s.boxes = parts == 2 ? 4 * s.rb * s.cb + 6 * s.rb * s.rb : 3 * s.rb * s.cb + 2 * s.rb * s.rb + (s.rb + 15) / 16;
     return s;
 }
 // Matrices [first, *end) share their launches.  Returns their boxes.
-int64_t group(const eg_orthogonalise_args* q, int64_t first, int64_t* end) {
+int64_t group(const eg_orthogonalise_args* q, int parts, int64_t first, int64_t* end) {
     int64_t boxes = 0, i = first;
     for (; i < q->count && i - first < kOrthoMats; ++i) {
-        const int64_t more = q->P * sides(q, q->matrices[i]).boxes;
+        const int64_t more = q->P * sides(parts, q->matrices[i]).boxes;
         if (i > first && (boxes + more) * kBoxBytes > kGroupBytes) break;
         boxes += more;
     }
@@ -381,9 +388,10 @@ Tail tail(const eg_orthogonalise_args* q) {
     return t;
 }
 int64_t workspace_of(const eg_orthogonalise_args* q) {
+    const int parts = parts_of(q);
     int64_t most = 0, end = 0;
     for (int64_t i = 0; i < q->count; i = end) {
-        const int64_t boxes = group(q, i, &end);
+        const int64_t boxes = group(q, parts, i, &end);
         most = boxes > most ? boxes : most;
     }
     return most * kBoxBytes + tail(q).bytes;
@@ -391,8 +399,7 @@ int64_t workspace_of(const eg_orthogonalise_args* q) {
 
 Strided strided(const eg_matrix& m) { return Strided{m.data, (long long)m.replica_stride, (long long)m.row_stride}; }
 
-bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t end, unsigned char* ws, int64_t boxes) {
-    const int parts = parts_of(q);
+bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int parts, int64_t first, int64_t end, unsigned char* ws, int64_t boxes) {
     const Tail z = tail(q);
     unsigned char* behind = ws + boxes * kBoxBytes;
     a->ws = ws;
@@ -408,7 +415,7 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
     for (int64_t i = first; i < end; ++i) {
         int64_t j = i - first;
         auto longer = [&](int64_t x, int64_t y) {
-            const Sides s = sides(q, q->matrices[x]), t = sides(q, q->matrices[y]);
+            const Sides s = sides(parts, q->matrices[x]), t = sides(parts, q->matrices[y]);
             return s.cb != t.cb ? s.cb > t.cb : s.rb > t.rb;
         };
         for (; j > 0 && longer(i, order[j - 1]); --j) order[j] = order[j - 1];
@@ -418,7 +425,7 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int64_t first, int64_t e
     for (int i = 0; i < a->count; ++i) {
         const eg_orthogonal_matrix& s = q->matrices[order[i]];
         OrthoMat* m = &a->mat[i];
-        const Sides z = sides(q, s);
+        const Sides z = sides(parts, s);
         m->flip = s.rows > s.columns;
         m->m = (int)(m->flip ? s.columns : s.rows);
         m->n = (int)(m->flip ? s.rows : s.columns);
@@ -479,8 +486,7 @@ template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& 
     return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kOrthoThreads), smem, stream, a, pass);
 }
 
-template <typename T> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, cudaStream_t stream) {
-    constexpr int PARTS = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 2;
+template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, cudaStream_t stream) {
     a.sx = s.sx;
     a.out = 1.f / s.sx;
     bool any_velocity = false;
@@ -580,15 +586,17 @@ eg_status eg_orthogonalise(const eg_orthogonalise_args* q, void* workspace, int6
     unsigned int* err = operator_error_word();
     if (!err) return EG_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    const int parts = parts_of(q);
     int64_t end = 0;
     for (int64_t i = 0; i < q->count; i = end) {
-        const int64_t boxes = group(q, i, &end);
+        const int64_t boxes = group(q, parts, i, &end);
         OrthoArgs a;
         a.err = err;
-        if (!fill(&a, q, i, end, static_cast<unsigned char*>(workspace), boxes)) return EG_ERR_CUDA;
-        const cudaError_t e = q->out_dtype == EG_F32    ? run<float>(a, s, q, stream)
-                              : q->out_dtype == EG_BF16 ? run<__nv_bfloat16>(a, s, q, stream)
-                                                        : run<__half>(a, s, q, stream);
+        if (!fill(&a, q, parts, i, end, static_cast<unsigned char*>(workspace), boxes)) return EG_ERR_CUDA;
+        const cudaError_t e = q->out_dtype == EG_F32   ? run<float, 2>(a, s, q, stream)
+                              : q->out_dtype == EG_F16 ? run<__half, 2>(a, s, q, stream)
+                              : parts == 2             ? run<__nv_bfloat16, 2>(a, s, q, stream)
+                                                       : run<__nv_bfloat16, 1>(a, s, q, stream);
         if (e != cudaSuccess) return EG_ERR_CUDA;
     }
     return EG_OK;

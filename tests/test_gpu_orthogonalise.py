@@ -225,6 +225,27 @@ def test_two_steps_in_one(kind, dtype, steps, coefficients):
     assert B.operator_status() == 0
 
 
+@pytest.mark.parametrize("rows,columns", [(3, 2 ** 18), (2 ** 18 + 65, 2), (1, 2 ** 20)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_long_sides(rows, columns, dtype):
+    """Sums over up to 2^20 values.  In full precision a hand-over every 4 steps keeps the limit that of any length.  A sum of 8-bit
+    results (up to 2^18) stays in the accumulator: each of its n / 16 additions truncates up to 2^-23 of it, which makes A less by up to
+    n / 16 * 2^-23 in every step, times 10 for what a step makes of it (see limit), 5 steps."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn((1, min(rows, columns), max(rows, columns)), generator=gen, device="cuda").to(TYPES[dtype])
+    g = x if rows <= columns else x.mT.contiguous()
+    out = B.orthogonalise([g], out=[torch.empty_like(g)])[0]
+    want = x.double()
+    want = want / want.norm()
+    for _ in range(5):
+        gram = want @ want.mT
+        want = DEFAULT[0] * want + (DEFAULT[1] * gram + DEFAULT[2] * gram @ gram) @ want
+    n = max(rows, columns)
+    bound = limit(dtype) + (n / 16 * 2.0 ** -23 * 10 * 5 if dtype == "bf16" and n <= 2 ** 18 else 0.0)
+    assert far(out if rows <= columns else out.mT, want) < bound
+    assert B.operator_status() == 0
+
+
 def test_matrices_that_share_no_launches():
     """More than one group: by number, and by memory."""
     grads, _ = make([(16, 24)] * 100, "bf16", P=1, velocity=False)
