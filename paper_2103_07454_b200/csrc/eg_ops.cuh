@@ -209,5 +209,20 @@ __device__ __forceinline__ void op_bulk_load(void* dst, const void* src, uint32_
 __device__ __forceinline__ void op_named_barrier(int id, int threads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
+// The abort flag as the warps of a named barrier see it together: all of them get the same answer, true where any of them found
+// it raised.  Warps that meet at such a barrier in their walk leave the walk by this, and never by a look of their own: one that
+// stayed a turn longer than its partner would wait for it at the barrier for good, which has no limit.
+__device__ __forceinline__ bool op_leave_together(int id, int threads, const volatile int* s_abort) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred mine, some;\n\t"
+        "setp.ne.s32 mine, %3, 0;\n\t"
+        "bar.red.or.pred some, %1, %2, mine;\n\t"
+        "selp.u32 %0, 1, 0, some;\n\t}"
+        : "=r"(any)
+        : "r"(id), "r"(threads), "r"(*s_abort)
+        : "memory");
+    return any != 0;
+}
 
 }  // namespace eg

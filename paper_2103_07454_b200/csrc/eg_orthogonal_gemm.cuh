@@ -355,7 +355,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
         OrthoPos q = ortho_pos<PARTS, PASS>(a, walk, pair);
         wait_before();
         for (int t = pair; t < tiles; t += pairs, ++turn) {
-            if (__any_sync(0xffffffffu, *s_abort)) break;
+            // (after a time-out nobody starts anything more; warps that share a box leave together)
+            if (PARTS == 1 ? (bool)__any_sync(0xffffffffu, *s_abort) : op_leave_together(1 + quad + 4 * (group >> 1), 64, s_abort)) break;
             if (t != pair) q = ortho_pos<PARTS, PASS>(a, walk, t);
             const OrthoMat& g = a.mat[q.k];
             const int ksteps = PASS == kGram ? g.cb : g.rb;
@@ -499,7 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                     if (sub == 0) {
                         store_wait_read<0>();
                         __syncwarp();
-                        if (elect_one()) {
+                        if (elect_one() && !*s_abort) {           // (a time-out in this tile: the barrier may still be armed)
                             const long long matrix = SYMMETRIC ? g.s[term ? pass.e1 : pass.e0] + q.p * g.s_rep : x;
                             op_mbar_expect(&epi_full[pair_of], 8192);
                             op_bulk_load(box, place(matrix), 4096, &epi_full[pair_of]);
