@@ -221,7 +221,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
-    // Set up, and the first tile looked up, while the kernel before this one finishes; whoever reads its results waits for them.
+    // Set up, and the first tile looked up, while the kernel before this one finishes; whoever reads its results, or what others do with
+    // them, waits for its end.
     auto wait_before = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = a.tiles[SYMMETRIC ? 0 : 1];
     const int from = pass.from;
@@ -296,6 +297,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
         if (rank == 0 && elect_one()) {
             int s = 0, round = 0, count = 0, turn = 0;          // count: accumulators handed over; turn: tiles
             OrthoPos upcoming = ortho_pos<PARTS, PASS>(a, walk, pair);
+            wait_before();                                      // (reads nothing of that kernel's, but the limits of its waits start here)
             for (int t = pair; t < tiles; t += pairs, ++turn) {
                 const OrthoPos q = upcoming;                                  // (the one after it is looked up under the products)
                 const OrthoMat& g = a.mat[q.k];

@@ -1,4 +1,4 @@
-// Kernels for tests/test_gpu_operator_waits.py: warps that leave a walk together.
+// Kernels for tests/test_gpu_operator_waits.py: warps that leave a walk together, a slow predecessor.
 #include "../paper_2103_07454_b200/csrc/eg_ops.cuh"
 
 using namespace eg;
@@ -20,6 +20,23 @@ __global__ void k_walk(int* turns, int most) {
         if (mine && !(blockIdx.x & 2)) s_abort = 1;
     }
     if ((threadIdx.x & 31) == 0) turns[2 * blockIdx.x + warp] = t;
+}
+
+// Lets its successor in the stream start at once, and ends after so many nanoseconds (3 s at most).
+__global__ void k_slow(unsigned long long ns) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+    if (ns > 3000000000ull) ns = 3000000000ull;
+    const long long begin = clock64();
+    do {
+        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    } while (t - t0 < ns && clock64() - begin < 8000000000ll);
+}
+
+extern "C" int slow(unsigned long long ns, void* stream) {
+    k_slow<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(ns);
+    return (int)cudaGetLastError();
 }
 
 extern "C" int walk(int* turns, int blocks, int most, void* stream) {

@@ -56,3 +56,13 @@ def test_warps_that_share_a_box_leave_the_walk_together():
     (look, _), = looks
     alone, _, shared = look.partition(" : ")
     assert alone.startswith("PARTS == 1 ?") and not stuck("op_leave_together" in shared)
+
+
+def test_limits_of_waits_start_where_the_kernel_before_has_ended():
+    """Every role of the products' kernel that waits on a barrier waits for the kernel before first."""
+    text = source("eg_orthogonal_gemm.cuh")
+    body = text[text.index("auto wait_before = "):text.index("*s_abort) {           // a wait ran out")]
+    roles = re.split(r"\n    (?:if \(warp == 0|\} else if \(warp)", body)[1:]
+    assert len(roles) == 3
+    for role in roles:
+        assert 0 < role.find("wait_before();") < role.index("mbar_wait(")
