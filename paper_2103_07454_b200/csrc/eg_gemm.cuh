@@ -429,17 +429,24 @@ template <typename T, int EPI, int BN> struct GemmShape {
     }
 };
 
-// What one CTA fetches per stage for rows m0.. of A, rows n0.. of B.
-__device__ __forceinline__ uint32_t a_bytes(const GemmProblem& g, int m0) {
-    if (g.a_mn) return m0 + 64 < g.M ? 16384u : m0 < g.M ? 8192u : 0u;
-    return m0 < g.M ? (uint32_t)g.a_box * 128u : 0u;
+// What one CTA fetches per stage for rows m0.. of A, rows n0.. of B.  Boxes wholly outside the operands stay away (rows and columns of
+// D that nobody stores), but one box at least is fetched, so that every fetching thread has a part in every stage: one without could
+// fall two rounds behind, take the phase of `empty` for the one before, and wait for good.
+__host__ __device__ __forceinline__ uint32_t a_bytes(const GemmProblem& g, int m0) {
+    if (g.a_mn) return m0 + 64 < g.M ? 16384u : 8192u;
+    return (uint32_t)g.a_box * 128u;
 }
-template <int BN> __device__ __forceinline__ uint32_t b_bytes(const GemmProblem& g, int n0) {
-    if (!g.b_mn) return n0 < g.N ? (uint32_t)(BN / 2) * 128u : 0u;
-    uint32_t bytes = 0;
+template <int BN> __host__ __device__ __forceinline__ uint32_t b_bytes(const GemmProblem& g, int n0) {
+    if (!g.b_mn) return (uint32_t)(BN / 2) * 128u;
+    uint32_t bytes = 8192u;
 #pragma unroll
-    for (int h = 0; h < BN / 2; h += 64) bytes += n0 + h < g.N ? 8192u : 0u;
+    for (int h = 64; h < BN / 2; h += 64) bytes += n0 + h < g.N ? 8192u : 0u;
     return bytes;
+}
+// Where a CTA's first box of an operand begins: at its first row, or where it has none, over the operand's end (a box that is
+// nearly all zeros; 16-byte boundaries where the rows run along it).
+__host__ __device__ __forceinline__ int first_row(int row, int rows, bool mn) {
+    return row < rows ? row : mn ? (rows - 1) / 8 * 8 : rows - 1;
 }
 
 // T: type of the operands and of 16-bit results; EPI: what becomes of D; BN: columns of a tile; G: stages under one
@@ -499,11 +506,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                 const TilePos q = tile_pos(a, t);
                 const GemmProblem& g = a.p[q.problem];
                 const int m0 = q.m * kGemmM + (int)rank * 128, n0 = g.b_pair ? q.n * (BN / 2) : q.n * BN + (int)rank * (BN / 2);
-                // boxes wholly outside the operands stay away: rows and columns of D that nobody stores
                 const uint32_t bytes = a_bytes(g, q.m * kGemmM) + a_bytes(g, q.m * kGemmM + 128) +
                                        b_bytes<BN>(g, g.b_pair ? n0 : q.n * BN) + b_bytes<BN>(g, g.b_pair ? n0 : q.n * BN + BN / 2);
                 const bool mn = warp == 0 ? g.a_mn : g.b_mn;
-                const int row = warp == 0 ? m0 : n0, rows = warp == 0 ? g.M : g.N;
+                const int rows = warp == 0 ? g.M : g.N, row = first_row(warp == 0 ? m0 : n0, rows, mn);
                 for (int e = 0; e < g.nseg; ++e) {
                     const CUtensorMap* map = &a.maps[warp == 0 ? g.seg[e].a : rank ? g.seg[e].b1 : g.seg[e].b0];
                     const int ksteps = g.seg[e].ksteps;
@@ -520,7 +526,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                             for (int h = 0; h < G; ++h, to += pitch) {
                                 if (h >= n) break;
                                 const int at = (k + h) * kGemmK;
-                                if (row < rows) tma_load_pair(to, map + part, mn ? row : at, mn ? at : row, q.p, bar);
+                                tma_load_pair(to, map + part, mn ? row : at, mn ? at : row, q.p, bar);
                                 if (mn && (warp == 0 || BN == 256) && row + 64 < rows)
                                     tma_load_pair(to + 8192, map + part, row + 64, at, q.p, bar);
                             }
