@@ -291,15 +291,12 @@ bool scales(const eg_orthogonalise_args* q, Scales* s) {
         s->sc[k] = power_below(fmax(s->most[k] * top, 1e-3) * 1.02);
         auto value = [&](double x) { return fabs(sqrt(x) * (a + x * (b + c * x))); };   // x: a square
         double next = value(top);
-        const double disc = 9 * b * b - 20 * a * c;          // of a + 3 b x + 5 c x^2
-        if (c != 0.0 && disc >= 0.0) {
-            for (double sign : {-1.0, 1.0}) {
-                const double x = (-3 * b + sign * sqrt(disc)) / (10 * c);
+        // roots of a + 3 b x + 5 c x^2, each without a difference of like values (c may be next to nothing beside b)
+        const double disc = 9 * b * b - 20 * a * c;
+        if (disc >= 0.0) {
+            const double far = -(3 * b + copysign(sqrt(disc), b)) / 2;
+            for (double x : {c != 0.0 ? far / (5 * c) : -1.0, far != 0.0 ? a / far : -1.0})
                 if (x > 0.0 && x < top) next = fmax(next, value(x));
-            }
-        } else if (c == 0.0 && b != 0.0) {
-            const double x = -a / (3 * b);
-            if (x > 0.0 && x < top) next = fmax(next, value(x));
         }
         most = fmax(most, bound);
         bound = next * 1.01;
