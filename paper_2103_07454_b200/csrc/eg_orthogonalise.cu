@@ -262,21 +262,26 @@ constexpr int kMaxSteps = 64;
 const double kDefault[3] = {3.4445, -4.7750, 2.0315};
 
 struct Scales {
-    float sx, sa, sb[kMaxSteps], sc[kMaxSteps];           // powers of two before X, A, B, C = A B
+    float sx[kMaxSteps + 1];                              // powers of two before X: of every step, and of the result
+    float sa[kMaxSteps], sb[kMaxSteps], sc[kMaxSteps];    // before A, B, C = A B
     double c[kMaxSteps][3], most[kMaxSteps];              // coefficients; bound of |B|
 };
 
-float power_below(double most) {                          // the largest power of two with most * it <= 60000, at most 2^14
-    int e = 0;
-    frexp(60000.0 / most, &e);
-    const int k = e - 1 < 14 ? e - 1 : 14;
-    return (float)ldexp(1.0, k);
+// The largest power of two with most * it <= 60000, but no more than takes `most` to 2^14 .. 2^15, nor than 2^114: values that a
+// polynomial makes small keep their bits, down to a bound of 2^-100.
+float power_below(double most) {
+    most = fmax(most, 0x1p-100);
+    int high = 0, low = 0;
+    frexp(60000.0 / most, &high);
+    frexp(most, &low);                                    // 2^(low - 1) <= most
+    const int cap = low > 1 ? 14 : 15 - low;
+    return (float)ldexp(1.0, high - 1 < cap ? high - 1 : cap);
 }
 
 // Bounds of the singular values, step by step, and the powers of two that they allow; false where the polynomials let them grow
 // beyond 64.
 bool scales(const eg_orthogonalise_args* q, Scales* s) {
-    double bound = 1.0, most = 1.0;
+    double bound = 1.0;
     for (int k = 0; k < q->steps; ++k) {
         for (int z = 0; z < 3; ++z) {
             s->c[k][z] = q->coefficients ? q->coefficients[3 * k + z] : kDefault[z];
@@ -286,9 +291,11 @@ bool scales(const eg_orthogonalise_args* q, Scales* s) {
         // |B| in the spectral norm: b x + c x^2 on 0 .. bound^2
         double highest = fabs(b * top + c * top * top);
         if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < top) highest = fmax(highest, fabs(b * b / (4 * c)));
-        s->most[k] = fmax(highest, 1e-3);
-        s->sb[k] = power_below(s->most[k] * 1.02);
-        s->sc[k] = power_below(fmax(s->most[k] * top, 1e-3) * 1.02);
+        s->most[k] = highest;
+        s->sx[k] = power_below(bound * 1.02);
+        s->sa[k] = power_below(top * 1.02);
+        s->sb[k] = power_below(highest * 1.02);
+        s->sc[k] = power_below(highest * top * 1.02);
         auto value = [&](double x) { return fabs(sqrt(x) * (a + x * (b + c * x))); };   // x: a square
         double next = value(top);
         // roots of a + 3 b x + 5 c x^2, each without a difference of like values (c may be next to nothing beside b)
@@ -298,13 +305,10 @@ bool scales(const eg_orthogonalise_args* q, Scales* s) {
             for (double x : {c != 0.0 ? far / (5 * c) : -1.0, far != 0.0 ? a / far : -1.0})
                 if (x > 0.0 && x < top) next = fmax(next, value(x));
         }
-        most = fmax(most, bound);
         bound = next * 1.01;
         if (bound > 64.0) return false;
     }
-    most = fmax(most, bound);
-    s->sx = power_below(most * 1.02);
-    s->sa = power_below(most * most * 1.02);
+    s->sx[q->steps] = power_below(bound * 1.02);
     return true;
 }
 
@@ -484,8 +488,8 @@ template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& 
 }
 
 template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, const eg_orthogonalise_args* q, cudaStream_t stream) {
-    a.sx = s.sx;
-    a.out = 1.f / s.sx;
+    a.sx = s.sx[0];
+    a.out = 1.f / s.sx[q->steps];
     bool any_velocity = false;
     double saved = 0;
     for (int i = 0; i < a.count; ++i) {
@@ -504,12 +508,12 @@ template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, 
     int from = 0;
     bool kept = false;
     for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
-        const double *c0 = s.c[k], sa = s.sa, sb0 = s.sb[k];
+        const double *c0 = s.c[k], sx = s.sx[k], sa = s.sa[k], sb0 = s.sb[k];
         OrthoPass p{};
         p.from = from;
         p.first = k == 0;
         p.to = 0;
-        p.fd = s.sa / (s.sx * s.sx);
+        p.fd = (float)(sa / (sx * sx));
         // (what only the last launch depends on is the caller's type: the others are shared)
         e = product<float, PARTS, kGram>(a, p, stream);
         auto sym = [&](int l, int r, int e0, int e1, int to, double f0, double f1, double fd) {
@@ -528,16 +532,16 @@ template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, 
             // 8 x 128 x 1152 163 -> 166 us, 1.9e-6 -> 2.3e-6).
             // (polynomials that make small values smaller: their products of two steps would sink below the boxes' last bit, 2^-39)
             if (pairs && k < q->steps && fabs(c0[0]) >= 1.0 && fabs(s.c[k][0]) >= 1.0) {
-                const double *c1 = s.c[k], sb1 = s.sb[k], sc = s.sc[k - 1];
+                const double *c1 = s.c[k], sa1 = s.sa[k], sb1 = s.sb[k], sc = s.sc[k - 1];
                 const double bound = fabs(c1[0]) * s.most[k - 1] + fabs(c0[0]) * s.most[k] + s.most[k - 1] * s.most[k], sr = power_below(bound * 1.02);
                 // C = A B0
                 sym(0, 1, 0, 0, 2, 0, 0, sc / (sa * sb0));
                 if (e == cudaSuccess) e = product<float, PARTS, kSym0>(a, p, stream);
                 // A1 = a0^2 A + 2 a0 C + C B0, in A's place
-                sym(2, 1, 0, 2, 0, c0[0] * c0[0], 2 * c0[0] * sa / sc, sa / (sc * sb0));
+                sym(2, 1, 0, 2, 0, c0[0] * c0[0] * sa1 / sa, 2 * c0[0] * sa1 / sc, sa1 / (sc * sb0));
                 if (e == cudaSuccess) e = product<float, PARTS, kSym2>(a, p, stream);
                 // B1 = b A1 + c A1^2, in C's place
-                sym(0, 0, 0, 0, 2, c1[1] * sb1 / sa, 0, c1[2] * sb1 / (sa * sa));
+                sym(0, 0, 0, 0, 2, c1[1] * sb1 / sa1, 0, c1[2] * sb1 / (sa1 * sa1));
                 if (e == cudaSuccess) e = product<float, PARTS, kSym1>(a, p, stream);
                 // a1 B0 + a0 B1 + B1 B0, in A1's place
                 sym(2, 1, 1, 2, 0, c1[0] * sr / sb0, c0[0] * sr / sb1, sr / (sb1 * sb0));
@@ -548,8 +552,8 @@ template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, 
                 ++k;
             }
         }
-        p.f0 = (float)outer;
-        p.fd = (float)(1.0 / scale);
+        p.f0 = (float)(outer * s.sx[k] / sx);
+        p.fd = (float)(s.sx[k] / (sx * scale));
         // The lower parts of X.  There are none at first where u is the gradient of 8 bits; where the steps to come multiply what
         // is lost now (2^-12.8 of X in the mean) by 4 at most, it stays below the rounding of the results.
         p.read_lower = k == 1 ? any_velocity : kept;
