@@ -80,7 +80,7 @@ struct OrthoPass {
     int first;                                    // X is still to be multiplied by `turn`
     int l, r, e0, e1, to;                         // symmetric matrices; apply: l
     float f0, f1, fd;                             // gram: fd;  apply: f0 X + fd S X
-    int read_lower, write_lower;                  // PARTS == 1, apply: whether X has lower parts, and needs them on
+    int read_lower;                               // PARTS == 1, apply: whether X has lower parts
 };
 
 struct OrthoArgs {
@@ -447,8 +447,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                                 else split_half2(r[2 * z], r[2 * z + 1], hw[z], lw[z]);
                             }
                             *reinterpret_cast<uint4*>(at) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-                            if constexpr (PASS == kApply)
-                                if (pass.write_lower) *reinterpret_cast<uint4*>(low_at + piece * 512) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                            if constexpr (PASS == kApply) *reinterpret_cast<uint4*>(low_at + piece * 512) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
                         }
                     }
                 }

@@ -506,7 +506,6 @@ template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, 
     auto of_type = [&](auto vel) { return q->dtype == EG_F32 ? given(0.f, vel) : q->dtype == EG_BF16 ? given(__nv_bfloat16{}, vel) : given(__half{}, vel); };
     cudaError_t e = any_velocity ? of_type(std::true_type{}) : of_type(std::false_type{});
     int from = 0;
-    bool kept = false;
     for (int k = 0; k < q->steps && e == cudaSuccess; from ^= 1) {
         const double *c0 = s.c[k], sx = s.sx[k], sa = s.sa[k], sb0 = s.sb[k];
         OrthoPass p{};
@@ -554,12 +553,10 @@ template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, 
         }
         p.f0 = (float)(outer * s.sx[k] / sx);
         p.fd = (float)(s.sx[k] / (sx * scale));
-        // The lower parts of X.  There are none at first where u is the gradient of 8 bits; where the steps to come multiply what
-        // is lost now (2^-12.8 of X in the mean) by 4 at most, it stays below the rounding of the results.
-        p.read_lower = k == 1 ? any_velocity : kept;
-        double growth = 1.0;
-        for (int z = k; z < q->steps; ++z) growth *= fmax(1.0, fabs(s.c[z][0]));
-        p.write_lower = kept = growth > 4.0;
+        // The lower parts of X: there are none at first where u is the gradient of 8 bits.  Afterwards X, which the steps carry on, keeps them to
+        // the end (dropped where what is left of the steps could not raise their loss above the result's rounding, two blocks of 1024 x 2816
+        // on 8 replicas took 3.04 ms instead of 3.09, 2048 x 5504 on 4 replicas 5.05 instead of 5.13).
+        p.read_lower = k > 1 || any_velocity;
         if (e != cudaSuccess) break;
         e = k < q->steps ? product<float, PARTS, kApply>(a, p, stream) : product<T, PARTS, kLast>(a, p, stream);
     }

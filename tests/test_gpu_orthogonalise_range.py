@@ -13,8 +13,8 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("dtype,result", [("fp32", "fp32"), ("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "fp32")])
 @pytest.mark.parametrize("factor,steps", [(0.25, 20), (0.5, 64), (-0.7, 64), (0.25, 49), (3.0, 3)])
 def test_a_factor_alone(factor, steps, dtype, result):
-    """X <- factor X: results of down to 2^-98 of the gradient's direction.  Each step rounds X once (to two parts of 11 bits, 2^-23, or for 8-bit
-    results to 2^-12 in the last steps), the result once; `scale`, a power of two, brings them to where its type has all its bits."""
+    """X <- factor X: results of down to 2^-98 of the gradient's direction.  Each step rounds X once (to two parts of 11 bits, 2^-23; the
+    bound for 8-bit results leaves it 2^-12), the result once; `scale`, a power of two, brings them to where its type has all its bits."""
     gen = torch.Generator(device="cuda").manual_seed(steps)
     g = O.matrix(70, 130, "noise", gen).to(O.TYPES[dtype])
     lift = 2.0 ** round(-steps * math.log2(abs(factor)))
@@ -43,3 +43,17 @@ def test_values_that_shrink_and_grow(steps, coefficients, dtype):
         out = B.orthogonalise([g], out=[torch.empty_like(g)], steps=steps, coefficients=coefficients, scale=lift)[0]
         assert O.far(out, want * lift) < O.limit(dtype, steps=max(steps, 5))
     assert B.operator_status() == 0
+
+
+@pytest.mark.parametrize("velocity", [False, True])
+def test_what_is_carried_from_step_to_step_has_two_parts(velocity):
+    """For 8-bit results too: 20 steps of a factor alone are off by 20 * 2^-23 at most.  Between two neighbouring results, 2^-8 to 2^-7 of them apart,
+    1.2e-3 of all may then be rounded the other way than the exact value: sqrt(1.2e-3) * 2^-7.5 of the result's norm."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    g, v = O.matrix(200, 300, "noise", gen).bfloat16(), O.matrix(200, 300, "noise", gen)
+    out = torch.empty_like(g)
+    B.orthogonalise([g], out=[out], velocity=[v.clone()] if velocity else None, nesterov=False, momentum=0.5, steps=20, coefficients=(0.5, 0.0, 0.0),
+                    scale=2.0 ** 20)
+    u = g.double() + (0.5 * v.double() if velocity else 0.0)
+    want = u / u.pow(2).sum((1, 2), keepdim=True).sqrt()
+    assert O.far(out, want.bfloat16().double()) < 2.0 ** -12
