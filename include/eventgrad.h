@@ -459,7 +459,8 @@ typedef struct {
  * where pair j is (j, j + rotary / 2), or (2 j, 2 j + 1) with `interleaved`.  rotary is even; 0: no rotation.  base >= 1.
  * w_q, w_k: `width` per replica, one vector for all heads; not given: z = x.  q, k: `rows` x q_heads (k_heads) x width per replica;
  * k_heads may be 0.  positions: whole numbers of 4 or 8 bytes (position_bytes) per row, of any size and sign;
- * NULL: 0, 1, 2, ...  Everything else is of type dtype; sums are fp32, angles are reduced in 64 bits.
+ * NULL: 0, 1, 2, ...  Everything else is of type dtype; sums are fp32, angles are products
+ * of 64 bits modulo a turn, off by about |position| * 2^-64 of a turn (2^-24 of one at 2^40).
  *
  * eg_head_norm computes q_out and k_out, which may be q and k themselves.  eg_head_norm_backward takes the gradients of both
  * (dq_out, dk_out) and the inputs again, and computes dq and dk (which may be dq_out and dk_out themselves) and, as sums over rows

@@ -14,7 +14,10 @@
 // another, all heads of the queries or of the keys, a row a team at a time; cosines and sines of the place stay in registers for all
 // of them (a sine costs some forty instructions, a value of a row about six), each formed by one team and handed to
 // the others.  Angles are whole 64-bit numbers in units of 2^-64 of a turn, which overflow where a turn ends: a product of
-// position and frequency keeps its fraction for positions of any size and sign.
+// position and frequency keeps its fraction for positions of any size and sign, and is off by what the frequency was rounded by,
+// about 2^-64 of a turn for every place: 2^-24 at 2^40, 2^-19 at 2^45.
+#include <math.h>
+
 #include <type_traits>
 
 #include "eg_ops.cuh"
@@ -543,8 +546,17 @@ int fill(HeadArgs* a, const eg_head_norm_args* q, bool backward, float* partial)
         s->w = Vec{both[m].w->data, (long long)both[m].w->replica_stride};
         s->partial = backward && both[m].dw->data ? partial + (m ? q->P * (int64_t)n.ctas[0] * q->width : 0) : nullptr;
     }
-    const double full = 6.283185307179586476925, step = a->rotary > 0 ? -2.0 * log(q->base) / a->rotary : 0.0;
-    for (int j = 0; j < a->half; ++j) a->turns[j] = (unsigned long long)(exp(step * j) / full * 18446744073709551616.0);   // (below 0.16 of a turn)
+    // Turns of the pairs per place to about the last of 64 bits, in the host's 64-bit significands (53 bits left a position of 2^45 off by 2^-10
+    // of a turn).  Pair 16 c + 4 b + a is a product of three powers, so that few exponentials are formed: a call for one token waits for
+    // them (32 pairs with 7 of them 6.4 us, with 12 6.9; 32 of 53 bits 6.1).
+    const long double step = a->rotary > 0 ? -2.0L * logl((long double)q->base) / a->rotary : 0.0L;
+    long double power[3][8];
+    for (int z = 0, stride = 1; z < 3; ++z, stride *= 4)
+        for (int j = 0; j < (z < 2 ? 4 : 8) && j * stride < a->half; ++j) power[z][j] = j ? expl(step * (j * stride)) : 1.0L;
+    for (int j = 0; j < a->half; j += 4) {
+        const long double coarse = power[1][j / 4 % 4] * power[2][j / 16] * (0x1p64L / 6.283185307179586476925286766559L);
+        for (int z = 0; z < 4 && j + z < a->half; ++z) a->turns[j + z] = (unsigned long long)(long long)(coarse * power[0][z] + 0.5L);    // (below 0.16 of a turn)
+    }
     return v;
 }
 

@@ -1,0 +1,51 @@
+"""The norm of attention heads and the rotation by position at the ends of their ranges."""
+import math
+from decimal import Decimal, getcontext
+
+import pytest
+import torch
+
+import test_gpu_head_norm as H
+from paper_2103_07454_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TURN = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+
+
+def angles(positions, rotary, base):
+    """Angles in radians, ``[places, rotary / 2]``, reduced to a turn in 60 digits before they become numbers of 64 bits."""
+    getcontext().prec = 60
+    turns = [(Decimal(base).ln() * (Decimal(-2 * j) / Decimal(rotary))).exp() / TURN for j in range(rotary // 2)]
+    return torch.tensor([[float((Decimal(p) * t % 1) * TURN) for t in turns] for p in positions], dtype=torch.float64, device="cuda")
+
+
+def test_the_oracle():
+    near = angles([0, 1, -3, 1000], 8, 10000)
+    want = torch.tensor([0.0, 1.0, -3.0, 1000.0], dtype=torch.float64, device="cuda")[:, None] * 10.0 ** -torch.arange(4, device="cuda").double()
+    # Python's remainder has the sign of the first number: the same angle
+    assert ((near - want).cos() - 1).abs().max() < 1e-12
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rotary,base", [(64, 64, 10000.0), (128, 128, 500000.0), (90, 46, 10000.0), (256, 256, 1e30), (36, 6, 1.0), (16, 16, 3.0)])
+def test_far_positions(d, rotary, base, interleaved):
+    """A frequency is below 2^61.4 units of 2^-64 of a turn.  It is a product of three exponentials (a unit in the last of 64 places each, with
+    their arguments) and rounds three times on the way (half of one): 4.5 * 2^-64 of it, 0.75 units, and half a unit in the end."""
+    positions = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 36 + 12345, -2 ** 40 + 77, 2 ** 40 + 1, 2 ** 45 - 3, -2 ** 45 - 12345678901]
+    (q, _), _, (w, _) = H.inputs(1, len(positions), 3, 1, d, "fp32", seed=1)
+    at = torch.tensor([positions], device="cuda")
+    out, _ = B.head_norm(q, None, w_q=w, positions=at, rotary=rotary, base=base, interleaved=interleaved)
+    x = q.double()
+    z = x / torch.sqrt(x.pow(2).mean(-1, keepdim=True) + 1e-6) * w.double()[:, None, None]
+    a = angles(positions, rotary, base)[None, :, None]
+    lead = z[..., :rotary]
+    u, v = (lead[..., 0::2], lead[..., 1::2]) if interleaved else (lead[..., :rotary // 2], lead[..., rotary // 2:])
+    u, v = u * a.cos() - v * a.sin(), u * a.sin() + v * a.cos()
+    want = torch.cat([torch.stack([u, v], -1).flatten(-2) if interleaved else torch.cat([u, v], -1), z[..., rotary:]], -1)
+    size = z.abs().amax(-1, keepdim=True)
+    off = torch.tensor(positions, device="cuda").double().abs()[None, :, None, None] * 1.25 * 2.0 ** -64 * 2 * math.pi
+    # a turned pair moves by the angle's error; the rest as in the tests of ordinary positions
+    bound = 2.0 ** -24 * 1.001 * want.abs() + 1.5 * size * (2.0 ** -24 * (24 + 4 * math.sqrt(d)) + off)
+    bad = (out.double() - want).abs() > bound
+    assert not bad.any(), (bad.nonzero()[:5].tolist(), float(((out.double() - want).abs() / bound).max()))
