@@ -466,7 +466,9 @@ typedef struct {
  * (dq_out, dk_out) and the inputs again, and computes dq and dk (which may be dq_out and dk_out themselves) and, as sums over rows
  * and heads in a fixed order, d_w_q and d_w_k; each of the four may be left out.  rows == 0 gives zero sums.  It
  * needs `workspace` (device, 16-byte aligned) of at least eg_head_norm_workspace(args) bytes, free for reuse once the stream has passed
- * the call.  A row with an infinity or a NaN in it has results that are not finite in general, the other rows their own.
+ * the call.  A row with an infinity or a NaN in it has results that are not finite in general, the other rows their own.  Where the
+ * squares of a row pass the range of 32 bits (values beyond 1.8e19; as in eg_residual_norm), 1 / sqrt(.) is zero and so are its results; where they sink
+ * below it, eps is what counts, and with eps == 0 results have few bits or are not finite (a row of zeros is 0 / 0).
  * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded into a
  * graph.  Outputs must not overlap inputs or each other except as said; elements of an output that fall on one
  * another are refused (EG_ERR_INVALID). */

@@ -49,3 +49,47 @@ def test_far_positions(d, rotary, base, interleaved):
     bound = 2.0 ** -24 * 1.001 * want.abs() + 1.5 * size * (2.0 ** -24 * (24 + 4 * math.sqrt(d)) + off)
     bad = (out.double() - want).abs() > bound
     assert not bad.any(), (bad.nonzero()[:5].tolist(), float(((out.double() - want).abs() / bound).max()))
+
+
+def far_rows(dtype, sizes):
+    """Heads of ordinary size, one of each kind multiplied by each of the sizes; which ones."""
+    x, g, w = H.inputs(2, 37, 5, 2, 64, dtype, seed=12)
+    plain = [t.clone() for t in x]
+    for t in x:
+        for k, size in enumerate(sizes):
+            t[1, 3 * k + 1, k % t.shape[2]] *= size
+    return x, plain, g, w, [(a != b).any(-1) for a, b in zip(x, plain)]
+
+
+@pytest.mark.parametrize("d", [64, 67])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rows_whose_squares_pass_the_range(dtype, d):
+    """As the header has it: their results are zeros, and the gradients with them; the other rows keep their bits."""
+    x, plain, g, w, far = far_rows(dtype, [2.0 ** 68, 2.0 ** 100, 2.0 ** 118])
+    if d == 67:                                          # off the 16-byte boundaries
+        apart = [torch.zeros((*t.shape[:3], d), dtype=t.dtype, device="cuda")[..., 3:] for t in (*x, *plain)]
+        for to, t in zip(apart, (*x, *plain)):
+            to.copy_(t)
+        x, plain = apart[:2], apart[2:]
+    how = dict(w_q=w[0], w_k=w[1])
+    for results in (lambda v: B.head_norm(*v, **how), lambda v: B.head_norm_backward(*g, *v, **how)[:2]):
+        for rows, a, b in zip(far, results(x), results(plain)):
+            assert int(rows.sum()) == 3 and (a[rows] == 0).all() and torch.equal(a[~rows], b[~rows])
+    dws = [B.head_norm_backward(*g, *v, **how)[2] for v in (x, plain)]
+    for a, b in zip(*dws):
+        assert torch.isfinite(a).all() and torch.equal(a[0], b[0])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rows_whose_squares_sink_below_the_range(dtype):
+    """Beside an epsilon they are what the formula makes them; without one they spoil nobody else's results."""
+    x, plain, g, w, far = far_rows(dtype, [2.0 ** -40, 2.0 ** -70, 2.0 ** -100])
+    H.run_and_check(x, g, w, dtype)
+    x[0][0, 2, 1] = 0
+    q, k = B.head_norm(*x, w_q=w[0], w_k=w[1])
+    assert (q[0, 2, 1] == 0).all()
+    far[0][0, 2, 1] = True
+    how = dict(w_q=w[0], w_k=w[1], eps=0.0)
+    for rows, a, b in zip(far, B.head_norm(*x, **how), B.head_norm(*plain, **how)):
+        assert torch.equal(a[~rows], b[~rows]) and torch.isfinite(a[~rows]).all()
+    assert torch.isnan(B.head_norm(*x, **how)[0][0, 2, 1]).all()
