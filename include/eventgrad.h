@@ -428,7 +428,8 @@ eg_status eg_feed_forward_backward(const eg_feed_forward_args* args, void* works
  *
  * eg_embedding computes out.  eg_embedding_backward overwrites d_weight (rows of tokens that do not come become zero) or, with
  * `accumulate`, adds to it (a table that is also the output's matrix) and leaves the rows of other tokens alone.  It
- * sums in fp32, in an order that depends on the tokens only, and needs `workspace` (device, 16-byte aligned) of at least
+ * sums in fp32, in an order that the tokens and the sizes of the call fix (P, rows, vocabulary, width and type: another P may
+ * give a replica's sums another rounding), and needs `workspace` (device, 16-byte aligned) of at least
  * eg_embedding_workspace(args) bytes, free for reuse once the stream has passed the call.
  * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded into a
  * graph.  Outputs must not overlap inputs, and neither rows nor replicas of an output each other (EG_ERR_INVALID). */
@@ -506,8 +507,9 @@ eg_status eg_head_norm_backward(const eg_head_norm_args* args, void* workspace, 
  * accuracy goes by out_dtype: bf16 results come from products whose operands are rounded to 11 bits (their error is about that of the
  * result's own rounding; a call with a matrix longer than 2^18 takes 22), fp16 and fp32 ones from operands of 22 bits; sums are fp32, the norm's fp64.
  * Any number of matrices of any sizes up to 2^20 share a call; `matrices` and `coefficients` are read before it returns.
- * `workspace` (device, 128-byte aligned) holds at least eg_orthogonalise_workspace(args) bytes (6 to 20 for every value, of
- * up to 1 GB of them at a time) and is free for reuse once the stream has passed the call.
+ * `workspace` (device, 128-byte aligned) holds at least eg_orthogonalise_workspace(args) bytes and is free for reuse once the stream has
+ * passed the call: 6 to 20 for every value of matrices whose sides are filled up to multiples of 64, and 1 KB for every matrix and
+ * replica.  Matrices take turns in 1 GB of it; one that needs more by itself (all its replicas) has it.
  * The call only enqueues work on `stream` of the current device, holds no state and may be recorded into a graph; the results do
  * not depend on the run (fp16 and fp32 ones, in their rounding, on how much work shares the call).  Outputs must not overlap inputs or each other except as said; rows and replicas of an output that fall on
  * one another are refused.  Errors: EG_ERR_INVALID, EG_ERR_CUDA. */

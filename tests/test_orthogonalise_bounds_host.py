@@ -3,7 +3,8 @@ import math
 
 import pytest
 
-from test_more_operators_host import orthogonalise, refused, workspace
+from paper_2103_07454_b200 import binding as B
+from test_more_operators_host import A, Matrix, orthogonalise, refused, workspace
 
 
 def largest(coefficients):
@@ -30,3 +31,16 @@ def test_growth_inside_the_range_is_found(a, b, c):
 def test_the_model_of_the_growth():
     assert math.isclose(largest([(1.5, -0.5, 0.0)]), 1.0)
     assert math.isclose(largest([(30.0, -30.0, 0.0)]), 20 / math.sqrt(3), rel_tol=1e-4)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("rows,columns", [(1, 1), (64, 64), (65, 63), (1, 1 << 20), (1 << 20, 1), (64, 1 << 18), (1000, 3000), (2048, 2048), (16384, 8192)])
+def test_the_workspace_is_what_the_header_says(rows, columns, dtype):
+    m = dict(rows=rows, columns=columns, velocity=Matrix())
+    m["grad"] = m["out"] = Matrix(A, rows * columns, columns)
+    for P in (1, 3):
+        values = P * (-rows % 64 + rows) * (-columns % 64 + columns)
+        need = workspace(orthogonalise(matrices=[m], P=P, dtype=dtype, out_dtype=dtype))
+        # (8-bit results: a float a row beside the boxes, in whole boxes; tables on boundaries of 256 bytes)
+        assert 6 * values <= need <= 20 * values + 1024 * P + 3 * 256 + 8192 * P
+        assert workspace(orthogonalise(matrices=[m] * 7, P=P, dtype=dtype, out_dtype=dtype)) <= max(need, 1 << 30) + 7 * 2048 * P
