@@ -470,6 +470,8 @@ typedef struct {
  * the call.  A row with an infinity or a NaN in it has results that are not finite in general, the other rows their own.  Where the
  * squares of a row pass the range of 32 bits (values beyond 1.8e19; as in eg_residual_norm), 1 / sqrt(.) is zero and so are its results; where they sink
  * below it, eps is what counts, and with eps == 0 results have few bits or are not finite (a row of zeros is 0 / 0).
+ * 16-bit rows that begin off the 4-byte boundaries, or have an odd number of values, are read in whole words of 4 bytes: two bytes in front
+ * of a head's first value and two behind its last may be read too, also while others write them; they are not used.
  * The calls only enqueue work on `stream` of the current device, hold no state and may be recorded into a
  * graph.  Outputs must not overlap inputs or each other except as said; elements of an output that fall on one
  * another are refused (EG_ERR_INVALID). */

@@ -93,3 +93,23 @@ def test_rows_whose_squares_sink_below_the_range(dtype):
     for rows, a, b in zip(far, B.head_norm(*x, **how), B.head_norm(*plain, **how)):
         assert torch.equal(a[~rows], b[~rows]) and torch.isfinite(a[~rows]).all()
     assert torch.isnan(B.head_norm(*x, **how)[0][0, 2, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("shift,d", [(0, 63), (1, 62), (1, 63), (3, 9)])
+def test_what_stands_beside_a_head_is_not_used(shift, d, dtype):
+    """Single 16-bit values come as words of 4 bytes: NaN in the halves that belong to nobody, and heads that others write meanwhile, change nothing."""
+    x, g, w = H.inputs(2, 41, 5, 2, d, dtype, seed=14)
+    wide = [torch.full((*t.shape[:3], d + 5), float("nan"), dtype=t.dtype, device="cuda") for t in (*x, *g)]
+    parts = [b[..., shift:shift + d] for b in wide]
+    for to, t in zip(parts, (*x, *g)):
+        to.copy_(t)
+    H.run_and_check(parts[:2], parts[2:], w, dtype)
+    how = dict(w_q=w[0], w_k=w[1])
+    want = B.head_norm(*parts[:2], **how)
+    # results into the same words: the inputs' neighbours change while they are read
+    B.head_norm(*parts[:2], q_out=parts[0], k_out=parts[1], **how)
+    assert all(torch.equal(a, b) for a, b in zip(parts, want))
+    for b, p in zip(wide, parts):
+        p.fill_(float("nan"))
+        assert torch.isnan(b).all()
