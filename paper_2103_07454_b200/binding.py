@@ -70,9 +70,10 @@ class EventGradError(RuntimeError):
 _lib = None
 _native = None        # csrc/marshal.cpp: the operators' arguments (see _operators)
 _OPERATORS = ("eg_clip_gradients", "eg_residual_norm", "eg_residual_norm_backward", "eg_residual_norm_workspace", "eg_feed_forward",
-              "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace", "eg_embedding",
-              "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward", "eg_head_norm_workspace",
-              "eg_orthogonalise", "eg_orthogonalise_workspace")
+              "eg_feed_forward_backward", "eg_feed_forward_saved_bytes", "eg_feed_forward_workspace")
+#: what builds of the library with the operators around the step may lack: only calls of these need it
+_LANGUAGE_OPERATORS = ("eg_embedding", "eg_embedding_backward", "eg_embedding_workspace", "eg_head_norm", "eg_head_norm_backward",
+                       "eg_head_norm_workspace", "eg_orthogonalise", "eg_orthogonalise_workspace")
 
 
 def load_library() -> C.CDLL:
@@ -155,6 +156,7 @@ def _operators():
         try:
             from . import _marshal
             addresses = [C.cast(getattr(lib, f), C.c_void_p).value for f in _OPERATORS]
+            addresses += [C.cast(getattr(lib, f), C.c_void_p).value if hasattr(lib, f) else 0 for f in _LANGUAGE_OPERATORS]
         except (ImportError, AttributeError) as e:
             raise EventGradError(f"{e}: build it with `python -m paper_2103_07454_b200.build`") from e
         _marshal.init(EventGradError, *addresses)

@@ -121,6 +121,11 @@ template <typename F> eg_status unlocked(F&& f) {
     return st;
 }
 
+// An entry point that builds of the library from before it lack.
+template <typename F> void needed(F* f, const char* what) {
+    if (!f) throw Refused{std::string(what) + " is not in this build of the library: build it with `python -m paper_2103_07454_b200.build`"};
+}
+
 // Every entry: the number of arguments is checked, no C++ exception leaves.
 template <PyObject* (*F)(PyObject* const*), int N> PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -343,6 +348,7 @@ void set_tokens(eg_embedding_args& q, const at::Tensor& tokens, const Kind& k, c
 
 // tokens, weight, scale, out
 PyObject* embedding(PyObject* const* a) {
+    needed(lib.embed, "eg_embedding");
     const at::Tensor &tokens = tensor(a[0], "tokens"), &w = on_device(tensor(a[1], "weight"));
     if (w.dim() != 3 || type_of(w) < 0) throw Refused{"embedding: weight must be [P, vocabulary, width] fp32, bf16 or fp16"};
     const Kind k{w.scalar_type(), w.device()};
@@ -363,6 +369,7 @@ PyObject* embedding(PyObject* const* a) {
 
 // dy, tokens, vocabulary, scale, d_weight, accumulate
 PyObject* embedding_backward(PyObject* const* a) {
+    needed(lib.embed_backward, "eg_embedding_backward");
     const at::Tensor &dy = on_device(tensor(a[0], "dy")), &tokens = tensor(a[1], "tokens");
     if (dy.dim() != 3 || type_of(dy) < 0) throw Refused{"embedding_backward: dy must be [P, rows, width] fp32, bf16 or fp16"};
     const Kind k{dy.scalar_type(), dy.device()};
@@ -454,6 +461,7 @@ struct HeadsCall {
 
 // q, k, w_q, w_k, positions, rotary, base, interleaved, eps, q_out, k_out
 PyObject* head_norm(PyObject* const* a) {
+    needed(lib.heads, "eg_head_norm");
     HeadsCall c(a, "head_norm");
     if (!c.keys && a[10] != Py_None) throw Refused{"head_norm: k_out without k"};
     at::Tensor q_out, k_out;
@@ -468,6 +476,7 @@ PyObject* head_norm(PyObject* const* a) {
 
 // q, k, w_q, w_k, positions, rotary, base, interleaved, eps, dq_out, dk_out, dq, dk, d_weights (tuple of two, or None)
 PyObject* head_norm_backward(PyObject* const* a) {
+    needed(lib.heads_backward, "eg_head_norm_backward");
     HeadsCall c(a, "head_norm_backward");
     if (!c.keys && (a[10] != Py_None || a[12] != Py_None)) throw Refused{"head_norm_backward: dk_out or dk without k"};
     if (a[9] == Py_None || (c.keys && a[10] == Py_None)) throw Refused{"head_norm_backward: the gradients of both outputs are needed"};
@@ -498,6 +507,7 @@ PyObject* item(PyObject* o, Py_ssize_t i) { return o == Py_None ? Py_None : PyTu
 
 // grads, out, velocity, velocity_out (tuples or None), momentum, nesterov, steps, coefficients (tuple of numbers, or None), scales (tuple)
 PyObject* orthogonalise(PyObject* const* a) {
+    needed(lib.ortho, "eg_orthogonalise");
     const Py_ssize_t count = PyTuple_GET_SIZE(a[0]);
     if (count == 0) return PyTuple_New(0);
     const at::Tensor& first = on_device(tensor(PyTuple_GET_ITEM(a[0], 0), "grads"));
