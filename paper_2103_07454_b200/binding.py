@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import numbers
 import os
 import struct
 from typing import Optional, Sequence
@@ -647,7 +648,10 @@ def head_norm_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: 
 def _tensors(tensors: Optional[Sequence], n: int, what: str) -> Optional[tuple]:
     if tensors is None:
         return None
-    tensors = tuple(tensors)
+    try:
+        tensors = tuple(tensors)
+    except TypeError as e:
+        raise EventGradError(f"orthogonalise: {what}: {e}") from e
     if len(tensors) != n:
         raise EventGradError(f"orthogonalise: {what} holds one entry for every gradient")
     return tensors
@@ -670,7 +674,9 @@ def orthogonalise(grads: Sequence[torch.Tensor], *, out: Optional[Sequence[torch
     grads = tuple(grads)
     n = len(grads)
     out, velocity, velocity_out = (_tensors(v, n, what) for v, what in ((out, "out"), (velocity, "velocity"), (velocity_out, "velocity_out")))
-    scales = (scale,) * n if isinstance(scale, (int, float)) else _tensors(scale, n, "scale")
+    scales = (scale,) * n if isinstance(scale, numbers.Real) else _tensors(scale, n, "scale")
+    if scales is None:
+        raise EventGradError("orthogonalise: scale: expected a number, or one for every gradient")
     if coefficients is not None:
         rows = [tuple(c) if isinstance(c, Sequence) else (c,) for c in coefficients]
         coefficients = sum(rows, ())

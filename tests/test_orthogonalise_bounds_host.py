@@ -1,7 +1,9 @@
 """Which polynomials orthogonal updates take: bounds of singular values that the host derives, before anything reaches a device."""
 import math
 
+import numpy as np
 import pytest
+import torch
 
 from paper_2103_07454_b200 import binding as B
 from test_more_operators_host import A, Matrix, orthogonalise, refused, workspace
@@ -44,3 +46,24 @@ def test_the_workspace_is_what_the_header_says(rows, columns, dtype):
         # (8-bit results: a float a row beside the boxes, in whole boxes; tables on boundaries of 256 bytes)
         assert 6 * values <= need <= 20 * values + 1024 * P + 3 * 256 + 8192 * P
         assert workspace(orthogonalise(matrices=[m] * 7, P=P, dtype=dtype, out_dtype=dtype)) <= max(need, 1 << 30) + 7 * 2048 * P
+
+
+@pytest.mark.parametrize("scale", [1, 2.0, np.float32(0.5), np.float64(0.5), np.int64(2), [0.5], np.array([0.5]), torch.tensor([0.5])])
+def test_numbers_of_any_kind_scale(scale):
+    """They get as far as the tensor that is not on a device."""
+    with pytest.raises(B.EventGradError, match="no CUDA device"):
+        B.orthogonalise([torch.zeros(1, 4, 8)], scale=scale)
+
+
+@pytest.mark.parametrize("bad", [None, "xy", 1j, np.array(0.5), torch.tensor(0.5), [0.5, 0.5], object()])
+def test_other_scales_are_refused_as_other_arguments_are(bad):
+    """Before anything asks for their entries."""
+    with pytest.raises(B.EventGradError, match="scale"):
+        B.orthogonalise([torch.zeros(1, 4, 8)], scale=bad)
+
+
+@pytest.mark.parametrize("bad", [1, torch.tensor(0.5)])
+def test_arguments_that_hold_nothing_are_refused_as_others_are(bad):
+    for name in ("out", "velocity", "velocity_out"):
+        with pytest.raises(B.EventGradError):
+            B.orthogonalise([torch.zeros(1, 4, 8)], **{name: bad})
