@@ -365,15 +365,9 @@ struct Builder {
 
 template <typename T, int EPI, int BN, int G> cudaError_t launch_kernel(const GemmArgs& a, cudaStream_t stream) {
     constexpr int smem = GemmShape<T, EPI, BN>::kSmem;
-    static bool raised[64] = {false};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static std::atomic<bool> raised[64];
+    const cudaError_t e = raise_smem(k_gemm<T, EPI, BN, G>, smem, raised);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !raised[dev]) {
-        e = cudaFuncSetAttribute(k_gemm<T, EPI, BN, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) raised[dev] = true;
-    }
     const int pairs = sm_count() / 2;
     if (pairs < 1) return cudaErrorInvalidDevice;
     return launch_after(k_gemm<T, EPI, BN, G>, dim3(2 * (a.tiles < pairs ? a.tiles : pairs)), dim3(kGemmThreads), smem, stream, a);

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/eventgrad.h"
 
 namespace eg {
@@ -112,16 +114,29 @@ cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// Multiprocessors of the current device, asked for once per device.
+// Multiprocessors of the current device, asked for once per device (by several threads at once, it may be: they find the same).
 inline int sm_count() {
-    static int known[64] = {0};
+    static std::atomic<int> known[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    if (dev >= 0 && dev < 64 && known[dev]) return known[dev];
-    int n = 0;
+    const bool kept = dev >= 0 && dev < 64;
+    int n = kept ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (n) return n;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    if (dev >= 0 && dev < 64) known[dev] = n;
+    if (kept) known[dev].store(n, std::memory_order_relaxed);
     return n;
+}
+
+// Raises a kernel's limit of dynamic shared memory on the current device, once per device; `raised`: the kernel's own, 64 of them.
+template <typename K> cudaError_t raise_smem(K* kernel, int smem, std::atomic<bool>* raised) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool kept = dev >= 0 && dev < 64;
+    if (kept && raised[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && kept) raised[dev].store(true, std::memory_order_relaxed);
+    return e;
 }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }

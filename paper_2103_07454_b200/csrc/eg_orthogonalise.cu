@@ -473,15 +473,9 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int parts, int64_t first
 
 template <typename T, int PARTS, int PASS> cudaError_t product(const OrthoArgs& a, const OrthoPass& pass, cudaStream_t stream) {
     constexpr int smem = OrthoShape<PARTS>::kSmem;
-    static bool raised[64] = {false};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static std::atomic<bool> raised[64];
+    const cudaError_t e = raise_smem(k_ortho<T, PARTS, PASS>, smem, raised);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !raised[dev]) {
-        e = cudaFuncSetAttribute(k_ortho<T, PARTS, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) raised[dev] = true;
-    }
     const int pairs = sm_count() / 2, tiles = a.tiles[PASS >= kApply ? 1 : 0];
     if (pairs < 1) return cudaErrorInvalidDevice;
     return launch_after(k_ortho<T, PARTS, PASS>, dim3(2 * (tiles < pairs ? tiles : pairs)), dim3(kOrthoThreads), smem, stream, a, pass);

@@ -1031,15 +1031,9 @@ cudaError_t stream_rows(NormArgs a, int* G, cudaStream_t stream) {
     // replicas and pays twice for factors and column sums (8 replicas of 1024 rows of 1024, forward and backward: 65 us, 78 with runs cut regardless).
     const int even = *G / a.P * a.P;
     if (even * 10 >= *G * 9) *G = even;
-    const void* kernel = (const void*)k_norm_stream<T, VEC, BWD>;
-    static bool raised[64] = {false};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static std::atomic<bool> raised[64];
+    cudaError_t e = raise_smem(k_norm_stream<T, VEC, BWD>, kSmemMax - 8192, raised);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !raised[dev]) {
-        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax - 8192)) != cudaSuccess) return e;
-        if (dev < 64) raised[dev] = true;
-    }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(*G * a.ctas);
     cfg.blockDim = dim3(a.teams * team);
@@ -1113,15 +1107,17 @@ __device__ unsigned int g_operator_error;
 }  // namespace
 
 unsigned int* operator_error_word() {
-    static unsigned int* known[64] = {nullptr};
+    static std::atomic<unsigned int*> known[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-    if (!known[dev]) {
+    unsigned int* word = known[dev].load(std::memory_order_relaxed);
+    if (!word) {
         void* p = nullptr;
         if (cudaGetSymbolAddress(&p, g_operator_error) != cudaSuccess) return nullptr;
-        known[dev] = static_cast<unsigned int*>(p);
+        word = static_cast<unsigned int*>(p);
+        known[dev].store(word, std::memory_order_relaxed);
     }
-    return known[dev];
+    return word;
 }
 
 }  // namespace eg

@@ -3,6 +3,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 namespace eg {
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -10,7 +12,8 @@ using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, voi
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 inline EncodeFn encoder() {
-    static EncodeFn fn = nullptr;
+    static std::atomic<EncodeFn> known{nullptr};          // several threads may look it up at once: they find the same
+    EncodeFn fn = known.load(std::memory_order_relaxed);
     if (!fn) {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult r;
@@ -18,6 +21,7 @@ inline EncodeFn encoder() {
             r != cudaDriverEntryPointSuccess)
             return nullptr;
         fn = reinterpret_cast<EncodeFn>(p);
+        known.store(fn, std::memory_order_relaxed);
     }
     return fn;
 }
