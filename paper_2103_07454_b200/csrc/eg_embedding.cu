@@ -528,7 +528,7 @@ bool usable(const eg_matrix& m, int64_t P, int64_t rows, int64_t cols, size_t si
     if (!written) return true;
     if (rows > 1 && m.row_stride < cols) return false;
     if (P > 1) {
-        const int64_t rep = m.replica_stride, row = rows > 1 ? m.row_stride : 0;
+        const __int128 rep = m.replica_stride, row = rows > 1 ? m.row_stride : 0;       // (2^30 rows 2^36 apart)
         if (!(rep >= (rows - 1) * row + cols || (rep >= cols && row >= (P - 1) * rep + cols))) return false;
     }
     return true;
