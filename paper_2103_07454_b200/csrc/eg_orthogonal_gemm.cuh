@@ -21,9 +21,12 @@
 //   PARTS == 1 (results of 8 bits): the products take hi alone, which costs 2^-12 of a value each, about what the result's own
 //     rounding does.  X is nevertheless carried on in both parts: the term a X, which alone carries small singular values
 //     (485 times over in five steps), sees no rounding to 11 bits.  (One part throughout: error 15 % for a matrix of rank 1.)
-//     The diagonals of A and B, far larger than what stands beside them, keep what they were rounded by as a float a row, rest_A and
-//     rest_B, which the epilogues put back: (H + D)^2 = H^2 + D H + H D + D^2, and a + rest_B is what X's row is multiplied by.
-//     (Errors of 6 steps of 64 x 784 before the result's rounding 2.5e-3 without, 1.5e-3 with; 134 -> 139 us there, 4.95 -> 5.0 ms in large ones.)
+//     The diagonals of A and B, far larger than what stands beside them, keep what they were rounded by, rest_A and rest_B, as a float a
+//     row that the epilogues put back: (H + D)^2 = H^2 + D H + H D + D^2, and a + rest_B is what the row of X's first parts is multiplied by.
+//     Its lower parts, which no product takes, are multiplied by a + B_ii: by a alone, X's two parts would be treated unlike where B is far from
+//     zero (-2.7 where singular values are 1): errors of 1.9e-3 instead of 2.2e-3 there, 1.70e-3 instead of 1.83e-3 for 1024 x 2816, 1.66e-3 being
+//     the rounding alone, at the same times.
+//     (Errors of 6 steps of 64 x 784, result's rounding included, 3.0e-3 without, 2.2e-3 with; 134 -> 139 us there, 4.95 -> 5.0 ms in large ones.)
 //     No product reads the lo parts of X: they lie as the epilogue's threads want them (see lane_place), once, and are updated in place.
 //   PARTS == 2 (results of 11 and 24 bits): hi hi + hi lo + lo hi.  lo lo, 2^-22 of a product, is left out.
 //
@@ -69,7 +72,7 @@ struct OrthoMat {
     float scale;
     long long x[2], lo[2], s[3];                  // first boxes of replica 0: X before and after a step, its lo parts, symmetric matrices
     long long x_rep, s_rep;                       // boxes from one replica to the next; lo parts of symmetric matrices lie half as far
-    long long rest, rest_rep;                     // PARTS == 1: boxes with what A's and B's diagonals were rounded by, rb * 64 floats each
+    long long rest, rest_rep;                     // PARTS == 1: boxes with what A's diagonal was rounded by and with B's, rb * 64 floats each
     Strided grad, out, velocity, velocity_out;
     int items, begin;                             // of k_ortho_norm and k_ortho_in: items of an instance, the first one of replica 0
 };
@@ -377,9 +380,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 uint4 low[PASS >= kApply ? 8 : 1];
                 unsigned char* const low_at = PASS >= kApply ? place(g.lo[0] + q.p * g.x_rep) + lane * 16 : nullptr;
                 float* const rest_a = reinterpret_cast<float*>(a.ws + (g.rest + q.p * g.rest_rep) * kBoxBytes);
-                float* const rest_b = rest_a + g.rb * kBox;
+                float* const diagonal_b = rest_a + g.rb * kBox;
                 const bool diagonal = SYMMETRIC && rbox == cbox;
-                float rest = 0.f, own = 0.f;                      // of this thread's row: what is put back; its value on the diagonal
+                // of this thread's row: what is put back; its value on the diagonal, formed (symmetric) or read (applications, of B)
+                float rest = 0.f, own = 0.f;
+                auto rounded_by = [](float v) { return v - __half2float(__float2half_rn(v)); };
                 if (inside && TERMS > 0) {                        // what the result is added to comes in under the products
                     store_wait_read<0>();
                     __syncwarp();
@@ -387,7 +392,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                         op_mbar_expect(&epi_full[w], 4096);
                         op_bulk_load(box, place(SYMMETRIC ? g.s[pass.e0] + q.p * g.s_rep : x), 4096, &epi_full[w]);
                     }
-                    rest = (SYMMETRIC ? rest_a : rest_b)[row0 + lane];
+                    if constexpr (SYMMETRIC) {
+                        rest = rest_a[row0 + lane];
+                    } else {
+                        own = diagonal_b[row0 + lane];
+                        rest = rounded_by(own);
+                    }
                     if constexpr (PASS == kSym1) {
                         if (lane < 2) asm volatile("prefetch.global.L1 [%0];" ::"l"(rest_a + cbox * kBox + lane * 32));
                     }
@@ -399,7 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 mbar_wait(&acc_full[count & 1], (count >> 1) & 1, s_abort, a.err);
                 tc_fence_after();
                 const uint32_t acc = tmem + (count & 1) * BN + lanes + group * 64;
-                const float f0 = fmaf(pass.fd, rest, pass.f0);
+                const float f0 = fmaf(pass.fd, rest, pass.f0), f0_low = PASS >= kApply ? fmaf(pass.fd, own, pass.f0) : 0.f;
                 if (inside) {
                     if (TERMS == 0) {
                         store_wait_read<0>();
@@ -427,7 +437,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                             } else if constexpr (TERMS > 0) {
                                 add_piece(r, f0, *reinterpret_cast<const uint4*>(at));
                             }
-                            if constexpr (PASS >= kApply) add_piece(r, f0, low[piece]);
+                            if constexpr (PASS >= kApply) add_piece(r, f0_low, low[piece]);
                             if constexpr (PASS == kGram || PASS >= kApply) {
 #pragma unroll
                                 for (int z = 0; z < 8; ++z) r[z] *= by;
@@ -456,7 +466,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kOrthoThreads, 1) k_
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(op_smem(&acc_empty[count & 1]), 0));
                 ++count;
                 if (!inside) continue;
-                if (diagonal) (PASS == kGram ? rest_a : rest_b)[row0 + lane] = own - __half2float(__float2half_rn(own));
+                if (diagonal) (PASS == kGram ? rest_a : diagonal_b)[row0 + lane] = PASS == kGram ? rounded_by(own) : own;
                 if constexpr (PASS != kLast) {
                     fence_async_shared();
                     __syncwarp();

@@ -347,7 +347,7 @@ bool valid(const eg_orthogonalise_args* q, Scales* s) {
 }
 
 // Parts of an operand.  Results of 8 bits take two where a matrix is longer than 2^18: with one, a product's sum stays in the accumulator, which
-// truncates (64 x 2^18: error 2.3e-3 with one; 64 x 2^20: 5.7e-3, 1.7e-3 with two; 24 and 26 ms).
+// truncates (64 x 2^18: error 2.1e-3 with one; 64 x 2^20: 5.7e-3, 1.7e-3 with two; 24 and 26 ms).
 int parts_of(const eg_orthogonalise_args* q) {
     if (q->out_dtype != EG_BF16) return 2;
     for (int64_t i = 0; i < q->count; ++i)
@@ -434,7 +434,7 @@ bool fill(OrthoArgs* a, const eg_orthogonalise_args* q, int parts, int64_t first
         m->first = (int)(i * q->P);
         m->scale = (float)s.scale;
         const int64_t plane = z.rb * z.cb, square = z.rb * z.rb;
-        // hi and lo of X twice and of three symmetric matrices; or hi of X twice, lo of X, hi of two and what their diagonals were rounded by
+        // hi and lo of X twice and of three symmetric matrices; or hi of X twice, lo of X, hi of two and their diagonals (rounding, values)
         m->x_rep = parts * plane; m->s_rep = parts * square;
         m->x[0] = at;
         m->x[1] = at + q->P * parts * plane;
@@ -548,8 +548,8 @@ template <typename T, int PARTS> cudaError_t run(OrthoArgs& a, const Scales& s, 
         p.f0 = (float)(outer * s.sx[k] / sx);
         p.fd = (float)(s.sx[k] / (sx * scale));
         // The lower parts of X: there are none at first where u is the gradient of 8 bits.  Afterwards X, which the steps carry on, keeps them to
-        // the end (dropped where what is left of the steps could not raise their loss above the result's rounding, two blocks of 1024 x 2816
-        // on 8 replicas took 3.04 ms instead of 3.09, 2048 x 5504 on 4 replicas 5.05 instead of 5.13).
+        // the end (without them in the last step two blocks of 1024 x 2816 on 8 replicas took 3.04 ms instead of 3.09, 2048 x 5504 on 4 replicas 5.05
+        // instead of 5.10).
         p.read_lower = k > 1 || any_velocity;
         if (e != cudaSuccess) break;
         e = k < q->steps ? product<float, PARTS, kApply>(a, p, stream) : product<T, PARTS, kLast>(a, p, stream);
