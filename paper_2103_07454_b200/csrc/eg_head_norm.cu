@@ -529,7 +529,9 @@ int fill(HeadArgs* a, const eg_head_norm_args* q, bool backward, float* partial)
         Side* s = &a->side[m];
         s->heads = (int)both[m].H;
         s->ctas = n.ctas[m];
-        // few places of a CTA: warps share their heads.  A warp's places times its turns for each, and about one for the sines
+        // few places of a CTA: warps share their heads.  A warp's places times its turns for each, and about one for the sines.  (us, forward and
+        // backward, and with a warp a place: 1 place of 32 + 8 heads of 128 in bf16 8 + 10, 10 + 13; 100 of them 8 + 12, 10 + 14; 300 in fp32 10 + 14,
+        // 14 + 21; 1 of 64 + 64 heads of 90 in fp32 10 + 12, 31 + 41; 8 x 1024 of 16 + 4 of 64 in bf16, where the rule shares nothing, 18 + 27)
         const int64_t places = s->ctas ? (q->rows + s->ctas - 1) / s->ctas : 1;
         int team = v * (int)size == 16 ? 2 : 32;
         while (team < 32 && team < a->slots) team *= 2;

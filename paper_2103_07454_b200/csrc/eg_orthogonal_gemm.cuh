@@ -41,7 +41,8 @@
 //
 // Measured, six matrices of 1024 x 2816 on 8 replicas, bf16 results: gram 127 us (1.1 PFLOP/s of what a symmetric product needs, 1.4 of
 // what the tiles on and below the diagonal are), sym 60 us, apply 252 to 280 us (1.1 PFLOP/s; 0.6 GB read, 0.5 GB written: boxes of X and its
-// lo parts, whose epilogue takes turns with the products).  Long runs are bound by power: the clock falls to 1.5 GHz.  ResNet-18 on 8 replicas, fp32
+// lo parts: a warp's epilogue has one box, so that load, sums and store of a tile follow one another and then the next tile's; the clock falls to
+// 1.5 GHz in long runs, which is not what bounds them, since a library product keeps 1.4 PFLOP/s up at 1.34).  ResNet-18 on 8 replicas, fp32
 // results: gram 157 us, symmetric products 42 to 52 us, each with tiles for less than two rounds of the machine, apply 267 us.
 #pragma once
 #include "eg_gemm.cuh"
