@@ -500,8 +500,8 @@ eg_status eg_head_norm_backward(const eg_head_norm_args* args, void* workspace, 
  * The polynomial pulls the singular values of X towards 1 and leaves its singular vectors: out is, roughly, the orthogonal
  * matrix next to u.  coefficients: a, b, c of every step (steps x 3, host), NULL: 3.4445, -4.7750, 2.0315 in each.  They may not
  * let the singular values grow beyond 64 on their way from 0 .. 1.  They may make them small: a step's operands are held under a power of two
- * that follows from the largest singular value the coefficients can leave (of 0 .. 1), with a last bit of 2^-39 of that value, as long as
- * it is not below 2^-100.  A matrix of zeros gives zeros, one whose norm is not finite
+ * that follows from the largest singular value the coefficients can leave (of 0 .. 1), and rounded to 2^-39 of that value at worst,
+ * as long as it is not below 2^-100.  A matrix of zeros gives zeros, one whose norm is not finite
  * NaN everywhere.
  *
  * grad is of type dtype, out of out_dtype, which is dtype or EG_F32; velocity and velocity_out are fp32 (velocity not given: none;

@@ -23,7 +23,7 @@ def test_a_factor_alone(factor, steps, dtype, result):
     want = g.double() / g.double().pow(2).sum((1, 2), keepdim=True).sqrt() * (factor ** steps * lift)
     own = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}[result]
     each = 2.0 ** -12 if result == "bf16" else 2.0 ** -23
-    # elements of 1 / 95 in the mean: of the bound on singular values, 1, the last bit of two parts is 2^-39
+    # elements of 1 / 95 in the mean: of the bound on singular values, 1, two parts are rounded to 2^-39
     assert float((out.double() - want).norm() / want.norm()) < own + steps * (each + 2.0 ** -39 * 95)
     assert B.operator_status() == 0
 
